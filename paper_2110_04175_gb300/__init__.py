@@ -7,6 +7,10 @@ becomes a ``cudaStream_t`` -- while every step of the method runs in the
 library's CUDA kernels.  There is no CPU fallback: if the library has not
 been built, the first call raises.
 
+The layer operators (``layers``, declared in ``include/relaylayers.h``) run one
+layer of all n workers' models at once, forward and backward, with activations
+held in 8 bits.
+
 ``RelayRun`` is a convenience owner of the device buffers of one run
 (allocated with torch) that swaps the double-buffered messages between
 steps.
@@ -31,6 +35,10 @@ from ._native import (RELAY_EINVAL, RELAY_ECUDA, RELAY_ENOMEM, RELAY_ENOTTREE, R
                       relay_set_received_sums, relay_message_rows, relay_step, relay_step_windows,
                       relay_step_counts, relay_step_models, relay_steps)
 
+from .layers import (RELAY_BF16, RELAY_FP16, RELAY_FP32, RELAY_NORM_MAX_D, ActivationCheckpoint,  # noqa: E402
+                     relay_checkpoint_pack, relay_checkpoint_pitch, relay_checkpoint_unpack,
+                     relay_gated, relay_gated_backward, relay_rms_norm, relay_rms_norm_backward,
+                     relay_rms_norm_backward_workspace, relay_weight_grad, relay_weight_grad_workspace)
 from .lr_correction import lr_correction  # noqa: E402
 
 __all__ = [
@@ -49,4 +57,8 @@ __all__ = [
     "relay_nbar", "relay_program", "relay_metrics", "relay_metrics_workspace",
     "relay_metrics_static",
     "relay_error_string", "lr_correction",
+    "RELAY_BF16", "RELAY_FP16", "RELAY_FP32", "RELAY_NORM_MAX_D", "ActivationCheckpoint",
+    "relay_checkpoint_pack", "relay_checkpoint_pitch", "relay_checkpoint_unpack", "relay_gated",
+    "relay_gated_backward", "relay_rms_norm", "relay_rms_norm_backward", "relay_rms_norm_backward_workspace",
+    "relay_weight_grad", "relay_weight_grad_workspace",
 ]

@@ -1,8 +1,8 @@
 """Builds librelaysum.so in-tree with nvcc for sm_103a (GB300).
 
 Translation units compiled in parallel (host program builder, C ABI with the
-setup kernels, host-state step, and the step kernels once per capacity),
-linked into one shared library with the CUDA runtime statically linked, so the
+setup kernels, host-state step, the step kernels once per capacity, and the
+layer operators), linked into one shared library with the CUDA runtime statically linked, so the
 library loads on a machine without a GPU.
 """
 from __future__ import annotations
@@ -23,9 +23,10 @@ LIB = os.path.join(BUILD, "librelaysum.so")
 # (relaysum::kSmallN) and for up to 256 (relaysum::kMaxN)
 SOURCES = [("step_kernels.cu", ["-DRELAY_CAP=256", "-DRELAY_SPACE=large"]),
            ("step_kernels.cu", ["-DRELAY_CAP=64", "-DRELAY_SPACE=small"]),
-           ("relaysum.cu", []), ("program.cpp", []), ("host_step.cpp", [])]
-HEADERS = [os.path.join(CSRC, h) for h in ("program.h", "handle.h", "device.cuh", "step_launch.h")] + [
-    os.path.join(INCLUDE, "relaysum.h")]
+           ("relaysum.cu", []), ("layer_kernels.cu", []), ("weight_grad.cu", []), ("program.cpp", []),
+           ("host_step.cpp", [])]
+HEADERS = [os.path.join(CSRC, h) for h in ("program.h", "handle.h", "device.cuh", "step_launch.h", "layers.cuh")] + [
+    os.path.join(INCLUDE, h) for h in ("relaysum.h", "relaylayers.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
               "-I" + INCLUDE, "-I" + CSRC]

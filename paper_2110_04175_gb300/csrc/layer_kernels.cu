@@ -1,0 +1,579 @@
+// layer_kernels.cu -- the row-wise layer operators of relaylayers.h on GB300
+// (sm_103a): the 8-bit checkpoint, the root-mean-square norm with the
+// residual's addition, and the gated activation, forward and backward.
+//
+// All of them move rows and compute little, so memory bounds them.  A warp
+// works on strips of 256 features (layers.cuh); what a row needs twice stays in
+// registers between its two uses.
+#include "layers.cuh"
+
+namespace {
+
+template <typename F>
+int by_type(int32_t type, F f) {
+    return type == RELAY_BF16 ? f(__nv_bfloat16()) : type == RELAY_FP16 ? f(__half()) : f(float());
+}
+
+// ------------------------------------------------------- element-wise kernels
+
+constexpr int kWarps = 8;  // of an element-wise CTA
+
+struct Grid {
+    int64_t rows;    // n tokens
+    int32_t tokens;
+    int32_t strips;  // of a row
+    int32_t d, pitch;
+};
+
+// Calls f(row, worker, token, first feature) for this warp's strips.
+template <typename F>
+__device__ __forceinline__ void each_strip(const Grid& g, F f) {
+    const int64_t all = g.rows * g.strips, step = static_cast<int64_t>(gridDim.x) * kWarps;
+    for (int64_t s = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32; s < all; s += step) {
+        const int64_t row = s / g.strips;
+        const int worker = static_cast<int>(row / g.tokens);
+        f(row, worker, static_cast<int>(row - static_cast<int64_t>(worker) * g.tokens),
+          static_cast<int>(s - row * g.strips) * kStrip);
+    }
+}
+
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(32 * kWarps)
+relay_checkpoint_pack_kernel(Grid g, View<const T> x, int8_t* codes, uint8_t* scales) {
+    const int lane = threadIdx.x % 32;
+    each_strip(g, [&](int64_t row, int worker, int token, int base) {
+        float v[8];
+        load_strip<kVec>(x.row(worker, token) + base, lane, g.d - base, v);
+        put_strip<kVec>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base, lane, g.pitch, v);
+    });
+}
+
+// fp16 cannot hold all that 8 bits can: held at the largest finite magnitude.
+template <typename T>
+__device__ __forceinline__ float within(float v) { return v; }
+template <>
+__device__ __forceinline__ float within<__half>(float v) { return fabsf(v) > 65504.0f ? copysignf(65504.0f, v) : v; }
+
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(32 * kWarps)
+relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scales, View<T> out) {
+    const int lane = threadIdx.x % 32;
+    each_strip(g, [&](int64_t row, int worker, int token, int base) {
+        float v[8];
+        get_strip<kVec>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base, lane, g.pitch, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = within<T>(v[k]);
+        store_strip<kVec>(out.row(worker, token) + base, lane, g.d - base, v);
+    });
+}
+
+// sigma(g) and 1 - sigma(g) without cancellation: with e = exp(-|g|) they are
+// 1 / (1 + e) and e / (1 + e), in the order that the sign of g gives.
+struct Sigmoid {
+    float at, rest;
+    __device__ __forceinline__ explicit Sigmoid(float g) {
+        const float e = expf(-fabsf(g)), r = 1.0f / (1.0f + e);
+        at = g < 0.0f ? e * r : r;
+        rest = g < 0.0f ? r : e * r;
+    }
+};
+
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(32 * kWarps)
+relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, int8_t* gate_codes,
+                   uint8_t* gate_scales, int8_t* up_codes, uint8_t* up_scales) {
+    const int lane = threadIdx.x % 32;
+    each_strip(g, [&](int64_t row, int worker, int token, int base) {
+        float a[8], b[8];
+        load_strip<kVec>(gate.row(worker, token) + base, lane, g.d - base, a);
+        load_strip<kVec>(up.row(worker, token) + base, lane, g.d - base, b);
+        const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
+        if (gate_codes != nullptr) put_strip<kVec>(gate_codes + at, gate_scales + scale_at, base, lane, g.pitch, a);
+        if (up_codes != nullptr) put_strip<kVec>(up_codes + at, up_scales + scale_at, base, lane, g.pitch, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid(a[k]).at * b[k];
+        store_strip<kVec>(out.row(worker, token) + base, lane, g.d - base, a);
+    });
+}
+
+struct GatedSource {  // one of the two
+    const int8_t *gate_codes, *up_codes;
+    const uint8_t *gate_scales, *up_scales;
+};
+
+template <typename T, bool kVec, bool kEight>
+__global__ void __launch_bounds__(32 * kWarps)
+relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View<const T> up, GatedSource from,
+                            View<T> dgate, View<T> dup, int8_t* out_codes, uint8_t* out_scales) {
+    const int lane = threadIdx.x % 32;
+    each_strip(g, [&](int64_t row, int worker, int token, int base) {
+        const int left = g.d - base;
+        const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
+        float da[8], a[8], b[8];
+        load_strip<kVec>(dout.row(worker, token) + base, lane, left, da);
+        if (kEight) {
+            get_strip<kVec>(from.gate_codes + at, from.gate_scales + scale_at, base, lane, g.pitch, a);
+            get_strip<kVec>(from.up_codes + at, from.up_scales + scale_at, base, lane, g.pitch, b);
+        } else {
+            load_strip<kVec>(gate.row(worker, token) + base, lane, left, a);
+            load_strip<kVec>(up.row(worker, token) + base, lane, left, b);
+        }
+        float dg[8], du[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const Sigmoid s(a[k]);
+            const float silu = a[k] * s.at;
+            dg[k] = da[k] * b[k] * s.at * (1.0f + a[k] * s.rest);
+            du[k] = da[k] * silu;
+            a[k] = silu * b[k];
+        }
+        store_strip<kVec>(dgate.row(worker, token) + base, lane, left, dg);
+        store_strip<kVec>(dup.row(worker, token) + base, lane, left, du);
+        if (out_codes != nullptr) {
+            // a block that reads as NaN does so past d too: those stay 0
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (feature<kVec>(lane, k) >= left) a[k] = 0.0f;
+            put_strip<kVec>(out_codes + at, out_scales + scale_at, base, lane, g.pitch, a);
+        }
+    });
+}
+
+// ----------------------------------------------------------------- the norm
+
+template <typename T>
+struct NormArgs {
+    View<const T> x, residual;
+    View<T> total, y;
+    const float* weight;
+    int64_t weight_stride;
+    bool weight_quads;
+    float eps;
+    float* rstd;
+    int8_t* codes;
+    uint8_t* scales;
+    int32_t rows, tokens, d, pitch;
+};
+
+// The sum of v over the kParts warps of a row (each warp's lanes included), the
+// same on all of them.  `slot`: the row's place in the CTA.  Called by all threads.
+template <int kParts>
+__device__ __forceinline__ float row_sum(float v, float* shared, int slot, int part) {
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    if (kParts == 1) return v;
+    __syncthreads();  // the last sum's readers are done
+    if (threadIdx.x % 32 == 0) shared[slot * kParts + part] = v;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) s += shared[slot * kParts + p];
+    return s;
+}
+
+template <int kParts>
+constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
+
+// kParts warps share a row, each with kStrips strips of it in registers.
+template <typename T, bool kVec, int kParts, int kStrips>
+__global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel(NormArgs<T> a) {
+    constexpr int kRows = kNormWarps<kParts> / kParts;
+    __shared__ float shared[kNormWarps<kParts>];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot;
+    const bool on = row < a.rows;
+    const int worker = on ? static_cast<int>(row / a.tokens) : 0;
+    const int token = on ? static_cast<int>(row - static_cast<int64_t>(worker) * a.tokens) : 0;
+    float h[kStrips][8];
+    float squares = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kStrips; ++j) {
+        const int base = (part + kParts * j) * kStrip, left = on ? a.d - base : 0;
+        load_strip<kVec>(a.x.row(worker, token) + base, lane, left, h[j]);
+        if (a.residual.p != nullptr) {
+            float r[8];
+            load_strip<kVec>(a.residual.row(worker, token) + base, lane, left, r);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[j][k] += r[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) squares = fmaf(h[j][k], h[j][k], squares);
+    }
+    squares = row_sum<kParts>(squares, shared, slot, part);
+    if (!on) return;
+    const float rstd = 1.0f / sqrtf(squares / static_cast<float>(a.d) + a.eps);
+    if (a.rstd != nullptr && part == 0 && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int j = 0; j < kStrips; ++j) {
+        const int base = (part + kParts * j) * kStrip, left = a.d - base;
+        if (base >= a.pitch) break;
+        if (a.total.p != nullptr) store_strip<kVec>(a.total.row(worker, token) + base, lane, left, h[j]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[j][k] = feature<kVec>(lane, k) < left ? h[j][k] * rstd : 0.0f;
+        if (a.codes != nullptr)
+            put_strip<kVec>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j]);
+        float w[8];
+        load_weight<kVec>(a.weight + worker * a.weight_stride + base, lane, left, a.weight_quads, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[j][k] *= w[k];
+        store_strip<kVec>(a.y.row(worker, token) + base, lane, left, h[j]);
+    }
+}
+
+template <typename T>
+struct NormBackwardArgs {
+    View<const T> dy, dtotal, total;
+    View<T> dx;
+    const float* weight;
+    int64_t weight_stride;
+    bool weight_quads;
+    const float* rstd;
+    const int8_t* codes;
+    const uint8_t* scales;
+    const int32_t* lengths;
+    float* partial;  // [n][gridDim.x][d]
+    int32_t tokens, d, pitch;
+};
+
+// CTA (p, i) takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i and
+// leaves their sum of dy xhat in its row of `partial`.
+template <typename T, bool kVec, int kParts, int kStrips, bool kEight>
+__global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
+    constexpr int kRows = kNormWarps<kParts> / kParts;
+    __shared__ float shared[kNormWarps<kParts>];
+    extern __shared__ float sums[];  // kRows > 1: [kRows - 1][kStrips][kParts][256]
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
+    const int worker = blockIdx.y;
+    const int length = a.lengths == nullptr ? a.tokens : min(max(a.lengths[worker], 0), a.tokens);
+    const float* weight = a.weight + worker * a.weight_stride;
+    float dw[kStrips][8] = {};
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.tokens;
+         first += static_cast<int64_t>(gridDim.x) * kRows) {
+        const int token = static_cast<int>(first) + slot;
+        const bool on = token < length;
+        const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
+        const float rstd = on ? a.rstd[row] : 0.0f;
+        float dy[kStrips][8], xhat[kStrips][8];
+        float along = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kStrips; ++j) {
+            const int base = (part + kParts * j) * kStrip, left = on ? a.d - base : 0;
+            load_strip<kVec>(a.dy.row(worker, token) + base, lane, left, dy[j]);
+            if (kEight) {
+                get_strip<kVec>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane,
+                                on ? a.pitch : 0, xhat[j]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (feature<kVec>(lane, k) >= left) xhat[j][k] = 0.0f;  // a NaN block's features past d
+            } else {
+                load_strip<kVec>(a.total.row(worker, token) + base, lane, left, xhat[j]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) xhat[j][k] *= rstd;
+            }
+            float w[8];
+            load_weight<kVec>(weight + base, lane, left, a.weight_quads, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                dw[j][k] = fmaf(dy[j][k], xhat[j][k], dw[j][k]);
+                dy[j][k] *= w[k];
+                along = fmaf(dy[j][k], xhat[j][k], along);
+            }
+        }
+        along = row_sum<kParts>(along, shared, slot, part) / static_cast<float>(a.d);
+        if (token >= a.tokens) continue;
+#pragma unroll
+        for (int j = 0; j < kStrips; ++j) {
+            const int base = (part + kParts * j) * kStrip, left = a.d - base;
+            if (left <= 0) break;
+            float dh[8] = {};
+            if (a.dtotal.p != nullptr) load_strip<kVec>(a.dtotal.row(worker, token) + base, lane, on ? left : 0, dh);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dh[k] = fmaf(rstd, dy[j][k] - xhat[j][k] * along, dh[k]);
+            store_strip<kVec>(a.dx.row(worker, token) + base, lane, left, dh);
+        }
+    }
+    if (kRows > 1) {  // the rows that went side by side, in their order
+        if (slot > 0) {
+#pragma unroll
+            for (int j = 0; j < kStrips; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    sums[(((slot - 1) * kStrips + j) * kParts + part) * kStrip + 32 * k + lane] = dw[j][k];
+        }
+        __syncthreads();
+        if (slot > 0) return;
+        for (int s = 0; s < kRows - 1; ++s)
+#pragma unroll
+            for (int j = 0; j < kStrips; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    dw[j][k] += sums[((s * kStrips + j) * kParts + part) * kStrip + 32 * k + lane];
+    }
+    float* out = a.partial + (static_cast<int64_t>(worker) * gridDim.x + blockIdx.x) * a.d;
+#pragma unroll
+    for (int j = 0; j < kStrips; ++j) {
+        const int base = (part + kParts * j) * kStrip;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (base + feature<kVec>(lane, k) < a.d) out[base + feature<kVec>(lane, k)] = dw[j][k];
+    }
+}
+
+// dweight[i][k] = sum_p partial[i][p][k]: a CTA sums 32 columns, 8 rows at a time.
+__global__ void __launch_bounds__(256)
+relay_norm_join_kernel(const float* partial, int parts, int d, float* dweight, int64_t dweight_stride) {
+    __shared__ float shared[8][32];
+    const int column = blockIdx.x * 32 + threadIdx.x % 32, lead = threadIdx.x / 32;
+    const float* p = partial + static_cast<int64_t>(blockIdx.y) * parts * d;
+    float s = 0.0f;
+    if (column < d)
+        for (int r = lead; r < parts; r += 8) s += p[static_cast<int64_t>(r) * d + column];
+    shared[lead][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (lead > 0 || column >= d) return;
+#pragma unroll
+    for (int r = 1; r < 8; ++r) s += shared[r][threadIdx.x];
+    dweight[blockIdx.y * dweight_stride + column] = s;
+}
+
+// ---------------------------------------------------------------- launching
+
+Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint) {
+    const int64_t pitch = pitch_of(d), width = checkpoint ? pitch : d;
+    return Grid{n * tokens, static_cast<int32_t>(tokens), static_cast<int32_t>((width + kStrip - 1) / kStrip),
+                static_cast<int32_t>(d), static_cast<int32_t>(pitch)};
+}
+
+int elementwise_ctas(const Grid& g) {
+    const int64_t want = (g.rows * g.strips + kWarps - 1) / kWarps, most = int64_t(32) * sm_count();
+    return static_cast<int>(want < most ? want : most);  // 0: no device
+}
+
+// Calls f(kParts, kStrips) as constants for the smallest instance that holds a row.
+template <int kParts_, int kStrips_>
+struct Hold {
+    static constexpr int kParts = kParts_, kStrips = kStrips_;
+};
+
+template <typename F>
+int by_width(int64_t pitch, F f) {
+    if (pitch <= 512) return f(Hold<1, 2>());
+    if (pitch <= 1024) return f(Hold<2, 2>());
+    if (pitch <= 2048) return f(Hold<4, 2>());
+    if (pitch <= 4096) return f(Hold<8, 2>());
+    if (pitch <= 8192) return f(Hold<16, 2>());
+    if (pitch <= 16384) return f(Hold<16, 4>());
+    return f(Hold<32, 4>());
+}
+
+// Rows of partial sums per worker in the norm's backward pass: about two CTAs per
+// SM over all workers, no more than there are tokens.
+int64_t norm_partials(int32_t n, int64_t tokens) {
+    const int64_t want = (304 + n - 1) / n;
+    return tokens < want ? (tokens > 0 ? tokens : 1) : want;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t relay_checkpoint_pitch(int64_t d) { return d < 1 || d > kMaxD ? RELAY_EINVAL : pitch_of(d); }
+
+int relay_checkpoint_pack(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* x, int8_t* codes,
+                          uint8_t* scales, relay_stream_t stream) {
+    if (const int rc = check_shape(type, n, tokens, d)) return rc;
+    if (!rows_fit(x, type, n, tokens, d, false) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
+    if (tokens == 0) return RELAY_OK;
+    const Grid g = make_grid(n, tokens, d, true);
+    const int ctas = elementwise_ctas(g);
+    if (ctas == 0) return RELAY_ECUDA;
+    const bool vec = d % 8 == 0 && vectors(x, type, n, tokens);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        (vec ? relay_checkpoint_pack_kernel<T, true> : relay_checkpoint_pack_kernel<T, false>)
+            <<<ctas, 32 * kWarps, 0, stream>>>(g, view<const T>(x, n, tokens), codes, scales);
+        return status_of_launch();
+    });
+}
+
+int relay_checkpoint_unpack(int32_t type, int32_t n, int64_t tokens, int64_t d, const int8_t* codes,
+                            const uint8_t* scales, const relay_rows* out, relay_stream_t stream) {
+    if (const int rc = check_shape(type, n, tokens, d)) return rc;
+    if (!rows_fit(out, type, n, tokens, d, true) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
+    if (tokens == 0) return RELAY_OK;
+    const Grid g = make_grid(n, tokens, d, false);
+    const int ctas = elementwise_ctas(g);
+    if (ctas == 0) return RELAY_ECUDA;
+    const bool vec = d % 8 == 0 && vectors(out, type, n, tokens);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        (vec ? relay_checkpoint_unpack_kernel<T, true> : relay_checkpoint_unpack_kernel<T, false>)
+            <<<ctas, 32 * kWarps, 0, stream>>>(g, codes, scales, view<T>(out, n, tokens));
+        return status_of_launch();
+    });
+}
+
+int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* x,
+                   const relay_rows* residual, const float* weight, int64_t weight_stride, float eps,
+                   const relay_rows* total, const relay_rows* y, float* rstd, int8_t* codes, uint8_t* scales,
+                   relay_stream_t stream) {
+    if (const int rc = check_shape(type, n, tokens, d)) return rc;
+    if (d > RELAY_NORM_MAX_D) return RELAY_EUNSUPPORTED;
+    if (!(eps > 0.0f) || !(eps < 1e30f) || weight == nullptr || !aligned(weight, 4) || weight_stride < 0)
+        return RELAY_EINVAL;
+    if (!rows_fit(x, type, n, tokens, d, false) || !rows_fit(y, type, n, tokens, d, true)) return RELAY_EINVAL;
+    if (residual != nullptr && !rows_fit(residual, type, n, tokens, d, false)) return RELAY_EINVAL;
+    if (total != nullptr && !rows_fit(total, type, n, tokens, d, true)) return RELAY_EINVAL;
+    if (!aligned(rstd, 4) || (codes == nullptr) != (scales == nullptr)) return RELAY_EINVAL;
+    if (codes != nullptr && !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
+    if (tokens == 0) return RELAY_OK;
+    if (y->data == x->data || (residual != nullptr && y->data == residual->data) ||
+        (total != nullptr && y->data == total->data))
+        return RELAY_EINVAL;
+    const bool vec = d % 8 == 0 && vectors(x, type, n, tokens) && vectors(residual, type, n, tokens) &&
+                     vectors(total, type, n, tokens) && vectors(y, type, n, tokens);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        const NormArgs<T> a{view<const T>(x, n, tokens), view<const T>(residual, n, tokens),
+                            view<T>(total, n, tokens), view<T>(y, n, tokens), weight, n > 1 ? weight_stride : 0,
+                            aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), eps, rstd, codes, scales,
+                            static_cast<int32_t>(n * tokens), static_cast<int32_t>(tokens), static_cast<int32_t>(d),
+                            static_cast<int32_t>(pitch_of(d))};
+        return by_width(a.pitch, [&](auto hold) {
+            constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
+            constexpr int kRows = kNormWarps<kParts> / kParts;
+            (vec ? relay_rms_norm_kernel<T, true, kParts, kStrips> : relay_rms_norm_kernel<T, false, kParts, kStrips>)
+                <<<(a.rows - 1) / kRows + 1, 32 * kNormWarps<kParts>, 0, stream>>>(a);
+            return status_of_launch();
+        });
+    });
+}
+
+int64_t relay_rms_norm_backward_workspace(int32_t n, int64_t tokens, int64_t d) {
+    if (const int rc = check_shape(RELAY_FP32, n, tokens, d)) return rc;
+    if (d > RELAY_NORM_MAX_D) return RELAY_EUNSUPPORTED;
+    return 4 * n * norm_partials(n, tokens) * d;
+}
+
+int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* dy,
+                            const relay_rows* dtotal, const float* weight, int64_t weight_stride, const float* rstd,
+                            const relay_rows* total, const int8_t* codes, const uint8_t* scales,
+                            const int32_t* lengths, const relay_rows* dx, float* dweight, int64_t dweight_stride,
+                            void* workspace, int64_t workspace_bytes, relay_stream_t stream) {
+    if (const int rc = check_shape(type, n, tokens, d)) return rc;
+    if (d > RELAY_NORM_MAX_D) return RELAY_EUNSUPPORTED;
+    if (weight == nullptr || !aligned(weight, 4) || weight_stride < 0) return RELAY_EINVAL;
+    if (!rows_fit(dy, type, n, tokens, d, false) || !rows_fit(dx, type, n, tokens, d, true)) return RELAY_EINVAL;
+    if (dtotal != nullptr && !rows_fit(dtotal, type, n, tokens, d, false)) return RELAY_EINVAL;
+    if (tokens > 0 && (rstd == nullptr || !aligned(rstd, 4))) return RELAY_EINVAL;
+    const bool eight = codes != nullptr || scales != nullptr;
+    if (eight ? total != nullptr || !checkpoint_fits(codes, scales, tokens)
+              : tokens > 0 && !rows_fit(total, type, n, tokens, d, false))
+        return RELAY_EINVAL;
+    if (!aligned(lengths, 4)) return RELAY_EINVAL;
+    if (dweight == nullptr || !aligned(dweight, 4) || (n > 1 && dweight_stride < d)) return RELAY_EINVAL;
+    if (workspace == nullptr || !aligned(workspace, 16) ||
+        workspace_bytes < relay_rms_norm_backward_workspace(n, tokens, d))
+        return RELAY_EINVAL;
+    if (tokens > 0 && (dx->data == dy->data || (dtotal != nullptr && dx->data == dtotal->data) ||
+                       (!eight && dx->data == total->data)))
+        return RELAY_EINVAL;
+    const bool vec = d % 8 == 0 && vectors(dy, type, n, tokens) && vectors(dtotal, type, n, tokens) &&
+                     vectors(eight ? nullptr : total, type, n, tokens) && vectors(dx, type, n, tokens);
+    const int parts = static_cast<int>(norm_partials(n, tokens));
+    const int rc = by_type(type, [&](auto t) {
+        using T = decltype(t);
+        const NormBackwardArgs<T> a{view<const T>(dy, n, tokens), view<const T>(dtotal, n, tokens),
+                                    view<const T>(total, n, tokens), view<T>(dx, n, tokens), weight,
+                                    n > 1 ? weight_stride : 0,
+                                    aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), rstd, codes, scales,
+                                    lengths, static_cast<float*>(workspace), static_cast<int32_t>(tokens),
+                                    static_cast<int32_t>(d), static_cast<int32_t>(pitch_of(d))};
+        return by_width(a.pitch, [&](auto hold) {
+            constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
+            constexpr size_t kSmem = (kNormWarps<kParts> / kParts - 1) * kStrips * kParts * kStrip * sizeof(float);
+            (vec ? (eight ? relay_rms_norm_backward_kernel<T, true, kParts, kStrips, true>
+                          : relay_rms_norm_backward_kernel<T, true, kParts, kStrips, false>)
+                 : (eight ? relay_rms_norm_backward_kernel<T, false, kParts, kStrips, true>
+                          : relay_rms_norm_backward_kernel<T, false, kParts, kStrips, false>))
+                <<<dim3(parts, n), 32 * kNormWarps<kParts>, kSmem, stream>>>(a);
+            return status_of_launch();
+        });
+    });
+    if (rc != RELAY_OK) return rc;
+    relay_norm_join_kernel<<<dim3(static_cast<unsigned>((d + 31) / 32), n), 256, 0, stream>>>(
+        static_cast<const float*>(workspace), parts, static_cast<int>(d), dweight, dweight_stride);
+    return status_of_launch();
+}
+
+int relay_gated(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* gate, const relay_rows* up,
+                const relay_rows* out, int8_t* gate_codes, uint8_t* gate_scales, int8_t* up_codes,
+                uint8_t* up_scales, relay_stream_t stream) {
+    if (const int rc = check_shape(type, n, tokens, d)) return rc;
+    if (!rows_fit(gate, type, n, tokens, d, false) || !rows_fit(up, type, n, tokens, d, false) ||
+        !rows_fit(out, type, n, tokens, d, true))
+        return RELAY_EINVAL;
+    if ((gate_codes == nullptr) != (gate_scales == nullptr) || (up_codes == nullptr) != (up_scales == nullptr))
+        return RELAY_EINVAL;
+    if (gate_codes != nullptr && !checkpoint_fits(gate_codes, gate_scales, tokens)) return RELAY_EINVAL;
+    if (up_codes != nullptr && !checkpoint_fits(up_codes, up_scales, tokens)) return RELAY_EINVAL;
+    if (gate_codes != nullptr && (gate_codes == up_codes || gate_scales == up_scales)) return RELAY_EINVAL;
+    if (tokens == 0) return RELAY_OK;
+    if (out->data == gate->data || out->data == up->data) return RELAY_EINVAL;
+    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr);
+    const int ctas = elementwise_ctas(g);
+    if (ctas == 0) return RELAY_ECUDA;
+    const bool vec = d % 8 == 0 && vectors(gate, type, n, tokens) && vectors(up, type, n, tokens) &&
+                     vectors(out, type, n, tokens);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        (vec ? relay_gated_kernel<T, true> : relay_gated_kernel<T, false>)<<<ctas, 32 * kWarps, 0, stream>>>(
+            g, view<const T>(gate, n, tokens), view<const T>(up, n, tokens), view<T>(out, n, tokens), gate_codes,
+            gate_scales, up_codes, up_scales);
+        return status_of_launch();
+    });
+}
+
+int relay_gated_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* dout,
+                         const relay_rows* gate, const relay_rows* up, const int8_t* gate_codes,
+                         const uint8_t* gate_scales, const int8_t* up_codes, const uint8_t* up_scales,
+                         const relay_rows* dgate, const relay_rows* dup, int8_t* out_codes, uint8_t* out_scales,
+                         relay_stream_t stream) {
+    if (const int rc = check_shape(type, n, tokens, d)) return rc;
+    if (!rows_fit(dout, type, n, tokens, d, false) || !rows_fit(dgate, type, n, tokens, d, true) ||
+        !rows_fit(dup, type, n, tokens, d, true))
+        return RELAY_EINVAL;
+    const bool eight = gate_codes != nullptr || gate_scales != nullptr || up_codes != nullptr || up_scales != nullptr;
+    if (eight ? gate != nullptr || up != nullptr || !checkpoint_fits(gate_codes, gate_scales, tokens) ||
+                    !checkpoint_fits(up_codes, up_scales, tokens)
+              : tokens > 0 && (!rows_fit(gate, type, n, tokens, d, false) || !rows_fit(up, type, n, tokens, d, false)))
+        return RELAY_EINVAL;
+    if ((out_codes == nullptr) != (out_scales == nullptr)) return RELAY_EINVAL;
+    if (out_codes != nullptr && (!checkpoint_fits(out_codes, out_scales, tokens) || out_codes == gate_codes ||
+                                 out_codes == up_codes || out_scales == gate_scales || out_scales == up_scales))
+        return RELAY_EINVAL;
+    if (tokens == 0) return RELAY_OK;
+    for (const relay_rows* o : {dgate, dup})
+        if (o->data == dout->data || (!eight && (o->data == gate->data || o->data == up->data))) return RELAY_EINVAL;
+    if (dgate->data == dup->data) return RELAY_EINVAL;
+    const Grid g = make_grid(n, tokens, d, out_codes != nullptr);
+    const int ctas = elementwise_ctas(g);
+    if (ctas == 0) return RELAY_ECUDA;
+    const bool vec = d % 8 == 0 && vectors(dout, type, n, tokens) && vectors(dgate, type, n, tokens) &&
+                     vectors(dup, type, n, tokens) && vectors(eight ? nullptr : gate, type, n, tokens) &&
+                     vectors(eight ? nullptr : up, type, n, tokens);
+    const GatedSource from{gate_codes, up_codes, gate_scales, up_scales};
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        (vec ? (eight ? relay_gated_backward_kernel<T, true, true> : relay_gated_backward_kernel<T, true, false>)
+             : (eight ? relay_gated_backward_kernel<T, false, true> : relay_gated_backward_kernel<T, false, false>))
+            <<<ctas, 32 * kWarps, 0, stream>>>(g, view<const T>(dout, n, tokens),
+                                               view<const T>(eight ? nullptr : gate, n, tokens),
+                                               view<const T>(eight ? nullptr : up, n, tokens), from,
+                                               view<T>(dgate, n, tokens), view<T>(dup, n, tokens), out_codes,
+                                               out_scales);
+        return status_of_launch();
+    });
+}
+
+}  // extern "C"
