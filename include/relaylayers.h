@@ -47,8 +47,9 @@
  *     (n < 1, tokens < 0, d < 1, overlapping output rows), an address that
  *     is not a multiple of its element's size, checkpoint or workspace
  *     addresses that are not multiples of 16, a workspace too small.
- *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N, n tokens >= 2^31, d > 2^24, or in
- *     the norm d > RELAY_NORM_MAX_D.
+ *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N, n tokens >= 2^31, d > 2^24, in
+ *     the norm d > RELAY_NORM_MAX_D, in the weight gradient inputs >
+ *     RELAY_WEIGHT_GRAD_MAX_INPUTS.
  *
  * The 8-bit format.  A row of d features is blocks of 32 with one scale byte
  * c per block and one signed code q per feature:
@@ -81,6 +82,7 @@ extern "C" {
 #define RELAY_FP32 2
 
 #define RELAY_NORM_MAX_D 32768
+#define RELAY_WEIGHT_GRAD_MAX_INPUTS (1 << 22)
 
 /* A view [n][tokens][d] of device memory: element (i, t, k) is at
  * data + i worker_stride + t token_stride + k, strides in elements, >= 0. */

@@ -25,7 +25,8 @@ SOURCES = [("step_kernels.cu", ["-DRELAY_CAP=256", "-DRELAY_SPACE=large"]),
            ("step_kernels.cu", ["-DRELAY_CAP=64", "-DRELAY_SPACE=small"]),
            ("relaysum.cu", []), ("layer_kernels.cu", []), ("weight_grad.cu", []), ("program.cpp", []),
            ("host_step.cpp", [])]
-HEADERS = [os.path.join(CSRC, h) for h in ("program.h", "handle.h", "device.cuh", "step_launch.h", "layers.cuh")] + [
+HEADERS = [os.path.join(CSRC, h) for h in ("program.h", "handle.h", "device.cuh", "step_launch.h", "layers.cuh",
+                                              "blackwell.cuh")] + [
     os.path.join(INCLUDE, h) for h in ("relaysum.h", "relaylayers.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

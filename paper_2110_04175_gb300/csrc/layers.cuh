@@ -55,39 +55,39 @@ __device__ __forceinline__ int feature(int lane, int k) { return kVec ? 8 * lane
 
 template <bool kVec, typename T>
 __device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8]) {
-    if (!kVec) {
+    if constexpr (kVec) {
+        constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+        for (int h = 0; h < 8 / kPer; ++h) {
+            uint4 w = make_uint4(0, 0, 0, 0);  // +0 in every type
+            if (8 * lane < left) w = *reinterpret_cast<const uint4*>(p + 8 * lane + h * kPer);
+            const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) v[h * kPer + k] = widen(e[k]);
+        }
+    } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 32 * k + lane < left ? widen(p[32 * k + lane]) : 0.0f;
-        return;
-    }
-    constexpr int kPer = 16 / sizeof(T);
-#pragma unroll
-    for (int h = 0; h < 8 / kPer; ++h) {
-        uint4 w = make_uint4(0, 0, 0, 0);  // +0 in every type
-        if (8 * lane < left) w = *reinterpret_cast<const uint4*>(p + 8 * lane + h * kPer);
-        const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) v[h * kPer + k] = widen(e[k]);
     }
 }
 
 template <bool kVec, typename T>
 __device__ __forceinline__ void store_strip(T* p, int lane, int left, const float (&v)[8]) {
-    if (!kVec) {
+    if constexpr (kVec) {
+        if (8 * lane >= left) return;
+        constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+        for (int h = 0; h < 8 / kPer; ++h) {
+            uint4 w;
+            T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) e[k] = narrow<T>(v[h * kPer + k]);
+            *reinterpret_cast<uint4*>(p + 8 * lane + h * kPer) = w;
+        }
+    } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (32 * k + lane < left) p[32 * k + lane] = narrow<T>(v[k]);
-        return;
-    }
-    if (8 * lane >= left) return;
-    constexpr int kPer = 16 / sizeof(T);
-#pragma unroll
-    for (int h = 0; h < 8 / kPer; ++h) {
-        uint4 w;
-        T* e = reinterpret_cast<T*>(&w);
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) e[k] = narrow<T>(v[h * kPer + k]);
-        *reinterpret_cast<uint4*>(p + 8 * lane + h * kPer) = w;
     }
 }
 
@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 template <bool kVec>
 __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int base, int lane, int pitch,
                                           const float (&v)[8]) {
-    if (kVec) {
+    if constexpr (kVec) {
         uint32_t most = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) most = max(most, magnitude(v[k]));
@@ -154,23 +154,23 @@ __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int ba
         }
         *reinterpret_cast<uint2*>(codes + base + 8 * lane) = make_uint2(w[0], w[1]);
         if (lane % 4 == 0) scales[base / kBlock + lane / 4] = static_cast<uint8_t>(c);
-        return;
-    }
-    uint32_t mine = 0;
+    } else {
+        uint32_t mine = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const uint32_t c = scale_byte(__reduce_max_sync(0xffffffffu, magnitude(v[k])));
-        if (lane == k) mine = c;
-        if (base + 32 * k < pitch)
-            codes[base + 32 * k + lane] = c == 255u ? 0 : static_cast<int8_t>(code_bits(v[k], c) & 0xffu);
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t c = scale_byte(__reduce_max_sync(0xffffffffu, magnitude(v[k])));
+            if (lane == k) mine = c;
+            if (base + 32 * k < pitch)
+                codes[base + 32 * k + lane] = c == 255u ? 0 : static_cast<int8_t>(code_bits(v[k], c) & 0xffu);
+        }
+        if (lane < 8 && base + 32 * lane < pitch) scales[base / kBlock + lane] = static_cast<uint8_t>(mine);
     }
-    if (lane < 8 && base + 32 * lane < pitch) scales[base / kBlock + lane] = static_cast<uint8_t>(mine);
 }
 
 template <bool kVec>
 __device__ __forceinline__ void get_strip(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch,
                                           float (&v)[8]) {
-    if (kVec) {
+    if constexpr (kVec) {
         uint2 w = make_uint2(0, 0);
         float unit = 0.0f;
         if (base + 8 * lane < pitch) {
@@ -179,13 +179,13 @@ __device__ __forceinline__ void get_strip(const int8_t* codes, const uint8_t* sc
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = code_value(k < 4 ? w.x : w.y, k % 4) * unit;
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        v[k] = 0.0f;
-        if (base + 32 * k < pitch)
-            v[k] = static_cast<float>(codes[base + 32 * k + lane]) * scale_unit(scales[base / kBlock + k]);
+        for (int k = 0; k < 8; ++k) {
+            v[k] = 0.0f;
+            if (base + 32 * k < pitch)
+                v[k] = static_cast<float>(codes[base + 32 * k + lane]) * scale_unit(scales[base / kBlock + k]);
+        }
     }
 }
 
