@@ -28,9 +28,16 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t at, uint32_t rank) {
     return to;
 }
 
-// `bar`: an address from in_cta.
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// The same at a barrier of another CTA (an address from in_cta).  Not a release to
+// the cluster, which would wait for the whole SM's traffic (2,000 cycles measured):
+// it says that writes to shared memory have reached it, as fence_async and a local
+// barrier have made sure before.
+__device__ __forceinline__ void barrier_arrive_there(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
@@ -42,7 +49,7 @@ __device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity) {
     asm volatile(
         "{\n"
         ".reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
         "selp.u32 %0, 1, 0, p;\n"
         "}\n"
         : "=r"(done)
@@ -91,6 +98,13 @@ __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, in
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(to),
         "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
+        "l"(map), "r"(bar), "r"(x), "r"(y)
         : "memory");
 }
 

@@ -29,7 +29,7 @@ namespace {
 constexpr int kM = 128;        // outputs of a CTA
 constexpr int kDepth = 64;     // tokens of a stage
 constexpr int kMakers = 8;     // warps that write stages, and the results at the end
-constexpr int kThreads = 32 * (kMakers + 4);  // whole warpgroups; the last two warps are idle
+constexpr int kThreads = 32 * (kMakers + 4);  // whole warpgroups; the last warp is idle
 // 3 warpgroups are launched with 168 registers a thread: 2 x 208 + 88 = 3 x 168
 constexpr int kMakerRegisters = 208, kOtherRegisters = 88;
 constexpr int kPanel = kDepth * 128;  // bytes of 64 outputs or inputs x kDepth tokens
@@ -48,7 +48,11 @@ template <typename T, int kN>
 struct Stages {  // in a CTA
     static constexpr int kLeft = kTerms<T> * kM / 64 * kPanel, kBytes = kLeft + kN / 2 / 64 * kPanel;
     static constexpr int kCount = 196608 / kBytes < 4 ? 196608 / kBytes : 4;
-    static constexpr int kShared = kCount * kBytes + 1024 + 256;  // alignment, barriers
+    // stages of codes, as they lie in memory: they come well before they are needed
+    static constexpr int kCodes = kN / 2 * kDepth;
+    static constexpr int kAhead = kCount * kBytes + 8 * kCodes <= 196608 ? 8 : 4;
+    static constexpr int kShared = kCount * kBytes + kAhead * kCodes + 1024 + 512;  // alignment, barriers
+    static_assert(kShared <= 232448, "shared memory of a CTA");
 };
 
 template <typename T>
@@ -95,44 +99,48 @@ __device__ __forceinline__ uint32_t unit_pair(uint32_t c) {
     return u | u << 16;
 }
 
-// A warp's part of a stage of kWide inputs of xhat: 8 codes per lane and pass.
+// A warp's part of a stage of kWide inputs of xhat: a lane recalls 8 codes of a
+// token per pass.
 template <int kWide>
-struct Codes {
-    static constexpr int kLanes = kWide / 8;                          // lanes of a token
+struct Recall {
+    static constexpr int kLanes = kWide / 8;                         // lanes of a token
     static constexpr int kRows = 32 / kLanes;                        // tokens of a pass
     static constexpr int kPasses = kDepth / (kRows * kMakers);
-    uint2 q[kPasses];
-    uint32_t c[kPasses];
+    static constexpr int kTokens = kRows * kPasses;                  // of the warp
+    static_assert(kTokens * kMakers == kDepth && kTokens <= 32 && kWide <= 128, "a lane per token's scales");
 
-    // The token of the stage that this lane has in pass r.
-    static __device__ __forceinline__ int token(int warp, int lane, int r) {
-        return (r * kMakers + warp) * kRows + lane / kLanes;
+    // The stage's token number `i` of the warp.
+    static __device__ __forceinline__ int token(int warp, int i) { return (i / kRows * kMakers + warp) * kRows + i % kRows; }
+
+    // The scale bytes of one token, by the first kTokens lanes (a word holds kWide / 32 of
+    // them and what follows, inside the row: its pitch is a multiple of 4).
+    static __device__ __forceinline__ uint32_t scales(const uint8_t* p, int64_t row0, int left, int k0, int pitch,
+                                                      int warp, int lane) {
+        const int t = token(warp, lane);
+        if (lane >= kTokens || t >= left || k0 >= pitch) return 0x07070707u;
+        const uint8_t* at = p + (row0 + t) * (pitch / kBlock) + k0 / kBlock;
+        if constexpr (kWide == 128) return __ldg(reinterpret_cast<const uint32_t*>(at));
+        return __ldg(reinterpret_cast<const uint16_t*>(at));
     }
 
-    // `row0`: the stage's first row in the checkpoint; `left`: its tokens that count.
-    __device__ __forceinline__ void load(const int8_t* codes, const uint8_t* scales, int64_t row0, int left, int k0,
-                                         int pitch, int warp, int lane) {
-        const int k = k0 + 8 * (lane % kLanes);
+    // `from`: the stage's codes; tokens from `left` on do not count.
+    static __device__ __forceinline__ void make(uint32_t from, uint32_t to, uint32_t scales, int left, int warp,
+                                                int lane) {
+        const int j = lane % kLanes;
+        uint2 q[kPasses];
+        uint32_t u[kPasses];
 #pragma unroll
         for (int r = 0; r < kPasses; ++r) {
-            const int t = token(warp, lane, r);
-            q[r] = make_uint2(0, 0);
-            c[r] = 7;
-            if (t < left && k < pitch) {
-                q[r] = __ldg(reinterpret_cast<const uint2*>(codes + (row0 + t) * pitch + k));
-                c[r] = __ldg(scales + (row0 + t) * (pitch / kBlock) + k / kBlock);
-            }
+            const int i = r * kRows + lane / kLanes, t = token(warp, i);
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(q[r].x), "=r"(q[r].y) : "r"(from + t * kWide + 8 * j));
+            u[r] = unit_pair(__shfl_sync(0xffffffffu, scales, i) >> (j / 4 * 8) & 0xffu);
+            if (t >= left) q[r] = make_uint2(0, 0);
         }
-    }
-
-    __device__ __forceinline__ void store(uint32_t to, int warp, int lane) const {
 #pragma unroll
-        for (int r = 0; r < kPasses; ++r) {
-            const uint32_t u = unit_pair(c[r]);
-            put_shared(to + piece(lane % kLanes, token(warp, lane, r)),
-                       make_uint4(recall_pair(q[r].x, 0, u), recall_pair(q[r].x, 1, u), recall_pair(q[r].y, 0, u),
-                                  recall_pair(q[r].y, 1, u)));
-        }
+        for (int r = 0; r < kPasses; ++r)
+            put_shared(to + piece(j, token(warp, r * kRows + lane / kLanes)),
+                       make_uint4(recall_pair(q[r].x, 0, u[r]), recall_pair(q[r].x, 1, u[r]),
+                                  recall_pair(q[r].y, 0, u[r]), recall_pair(q[r].y, 1, u[r])));
     }
 };
 
@@ -182,24 +190,29 @@ __device__ __forceinline__ void split_rows(const WeightGradArgs<T>& a, int worke
 // A pair of CTAs per tile of 256 outputs x kN inputs and per split of the tokens.
 // Warps 0 .. 7 write xhat (and dy, without TMA) into the stages, add up the sums
 // and write them to memory; warp 8 of CTA 0 issues the products (that of CTA 1
-// sees to its copies); warp 9 issues the copies.  A wait that runs out ends the
+// says when its half is ready); warps 9 and 10 issue the copies.  A wait that runs out ends the
 // work on the tile, and its results are NaN.
 template <typename T, bool kTma, int kN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __grid_constant__ CUtensorMap dy_map) {
+relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __grid_constant__ CUtensorMap dy_map,
+                         const __grid_constant__ CUtensorMap codes_map) {
     using S = Stages<T, kN>;
     constexpr int kCount = S::kCount, kColumns = kN / 2;  // columns: of a warp, in the end
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
-    const uint32_t bars = stages + kCount * S::kBytes;
-    // per stage: written (on CTA 0: by both), copied (dy by TMA), free again; per accumulator:
-    // summed by the tensor cores, and read (on CTA 0: by both)
+    const uint32_t codes = stages + kCount * S::kBytes, bars = codes + S::kAhead * S::kCodes;
+    // per stage: written, copied (dy by TMA), free again, and, on CTA 0, ready on CTA 1; per
+    // accumulator: summed by the tensor cores, and read
     const auto written = [&](int s) { return bars + 8 * s; };
     const auto copied = [&](int s) { return bars + 8 * (kCount + s); };
     const auto freed = [&](int s) { return bars + 8 * (2 * kCount + s); };
-    const auto summed = [&](int b) { return bars + 8 * (3 * kCount + b); };
-    const auto read = [&](int b) { return bars + 8 * (3 * kCount + 2 + b); };
-    const uint32_t tensor_at = bars + 8 * (3 * kCount + 4);
+    const auto ready = [&](int s) { return bars + 8 * (3 * kCount + s); };
+    const auto summed = [&](int b) { return bars + 8 * (4 * kCount + b); };
+    const auto read = [&](int b) { return bars + 8 * (4 * kCount + 2 + b); };
+    // per stage of codes: there, and used
+    const auto fetched = [&](int s) { return bars + 8 * (4 * kCount + 4 + s); };
+    const auto used = [&](int s) { return bars + 8 * (4 * kCount + 4 + S::kAhead + s); };
+    const uint32_t tensor_at = bars + 8 * (4 * kCount + 4 + 2 * S::kAhead);
     __shared__ int stalled;
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -213,13 +226,18 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kCount; ++s) {
-            barrier_init(written(s), 2 * kMakers + (kTma ? 1 : 0));
+            barrier_init(written(s), kMakers);
             barrier_init(copied(s), 1);
             barrier_init(freed(s), 1);
+            barrier_init(ready(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(summed(b), 1);
-            barrier_init(read(b), 2 * kMakers);
+            barrier_init(read(b), kMakers);
+        }
+        for (int s = 0; s < S::kAhead; ++s) {
+            barrier_init(fetched(s), 1);
+            barrier_init(used(s), kMakers);
         }
         barriers_ready();
         stalled = 0;
@@ -233,17 +251,17 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
 
     bool ok = true;
+    const int half = k0 + kN / 2 * static_cast<int>(rank);  // the inputs that this CTA recalls
+    const int64_t row0 = static_cast<int64_t>(worker) * a.tokens + first * kDepth;
     if (warp < kMakers)
         more_registers<kMakerRegisters>();
     else
         fewer_registers<kOtherRegisters>();
     if (warp < kMakers) {
-        const int half = k0 + kN / 2 * static_cast<int>(rank);  // the inputs that this CTA recalls
-        const int64_t row0 = static_cast<int64_t>(worker) * a.tokens;
-        Codes<kN / 2> now, next, later;
-        const auto load = [&](Codes<kN / 2>& c, int i) {
-            const int t = (first + i) * kDepth;
-            c.load(a.codes, a.scales, row0 + t, i < count ? length - t : 0, half, a.pitch, warp, lane);
+        using R = Recall<kN / 2>;
+        const auto load = [&](int i) {
+            const int left = i < count ? length - (first + i) * kDepth : 0;
+            return R::scales(a.scales, row0 + i * kDepth, left, half, a.pitch, warp, lane);
         };
         // outputs 32 (warp % 4) + lane, inputs kColumns (warp / 4) ..
         float sum[kColumns] = {};
@@ -263,24 +281,27 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             }
             tensor_fence_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive(in_cta(read(b), 0));
+            if (lane == 0) barrier_arrive(read(b));
             ++groups;
             return true;
         };
-        load(now, 0);
-        load(next, 1);
+        uint32_t now = load(0), next = load(1), later = load(2);
         for (int i = 0; i < count; ++i) {
-            const int s = i % kCount;
-            load(later, i + 2);
+            const int s = i % kCount, f = i % S::kAhead, t = (first + i) * kDepth;
+            const uint32_t last = load(i + 3);
             if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-            const int t = (first + i) * kDepth;
             if (!kTma) split_rows(a, worker, t, length - t, o0, stages + s * S::kBytes, warp, lane);
-            now.store(stages + s * S::kBytes + S::kLeft, warp, lane);
+            if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
+            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, length - t, warp, lane);
             fence_async();
             __syncwarp();
-            if (lane == 0) barrier_arrive(in_cta(written(s), 0));
+            if (lane == 0) {
+                barrier_arrive(written(s));
+                barrier_arrive(used(f));
+            }
             now = next;
             next = later;
+            later = last;
             // stage i - kCount is done, and with it a whole group
             if (i + 1 - kCount == (groups + 1) * kGroup<T> && !(ok = add_group())) break;
         }
@@ -323,15 +344,15 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                 }
                 fence_async();
                 __syncwarp();
-                if (rank != 0) {
-                    if (lane == 0) barrier_arrive(in_cta(written(s), 0));
-                    continue;
-                }
             }
-            if (rank != 0) break;
             const int group = i / kGroup<T>, b = group & 1;
             if (i % kGroup<T> == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
             if (!(ok = barrier_wait(written(s), parity))) break;
+            if (rank != 0) {  // one arrival for all of this CTA, by a thread with no loads under way
+                if (lane == 0) barrier_arrive_there(in_cta(ready(s), 0));
+                continue;
+            }
+            if (!(ok = barrier_wait(ready(s), parity))) break;
             tensor_fence_after();
             if (lane == 0) {
                 const uint32_t right = left + S::kLeft;
@@ -359,6 +380,16 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
         for (int i = max(0, sent - kCount); i < sent; ++i)  // nothing is left in flight
             if (!barrier_wait(copied(i % kCount), i / kCount & 1)) break;
+    } else if (warp == kMakers + 2 && lane == 0) {
+        int sent = 0;
+        for (; sent < count; ++sent) {
+            const int f = sent % S::kAhead;
+            if (!(ok = barrier_wait(used(f), (sent / S::kAhead & 1) ^ 1))) break;
+            barrier_expect(fetched(f), S::kCodes);
+            copy_box(codes + f * S::kCodes, &codes_map, half, static_cast<int>(row0) + sent * kDepth, fetched(f));
+        }
+        for (int i = max(0, sent - S::kAhead); i < sent; ++i)
+            if (!barrier_wait(fetched(i % S::kAhead), i / S::kAhead & 1)) break;
     }
     __syncwarp();
     __syncthreads();
@@ -402,11 +433,12 @@ int token_splits(int64_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
     return s > 1 ? static_cast<int>(s) : 1;
 }
 
-// The map of dy for 64 x 64 boxes; false where TMA cannot take its rows.
-bool map_rows(CUtensorMap* map, const View<const __nv_bfloat16>& dy, int32_t n, int64_t tokens, int64_t outputs) {
-    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                            const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                            CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's cuTensorMapEncodeTiled, NULL where it has none.
+Encode encoder() {
     static const Encode encode = [] {
         void* f = nullptr;
         cudaDriverEntryPointQueryResult found;
@@ -418,16 +450,32 @@ bool map_rows(CUtensorMap* map, const View<const __nv_bfloat16>& dy, int32_t n, 
         }
         return reinterpret_cast<Encode>(f);
     }();
-    if (encode == nullptr || tokens == 0 || (tokens > 1 && dy.ts < outputs) || (n > 1 && dy.ws < outputs)) return false;
+    return encode;
+}
+
+// The map of dy for 64 x 64 boxes; false where TMA cannot take its rows.
+bool map_rows(CUtensorMap* map, const View<const __nv_bfloat16>& dy, int32_t n, int64_t tokens, int64_t outputs) {
+    if (tokens == 0 || (tokens > 1 && dy.ts < outputs) || (n > 1 && dy.ws < outputs)) return false;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(outputs), static_cast<cuuint64_t>(tokens),
                                 static_cast<cuuint64_t>(n)};
     // an axis of one row or one worker is never walked: any stride will do
     const cuuint64_t row = tokens > 1 ? static_cast<cuuint64_t>(dy.ts) * 2 : (outputs * 2 + 15) / 16 * 16;
     const cuuint64_t strides[2] = {row, n > 1 ? static_cast<cuuint64_t>(dy.ws) * 2 : row};
     const cuuint32_t box[3] = {64, kDepth, 1}, steps[3] = {1, 1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(dy.p), dims, strides, box,
-                  steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(dy.p), dims, strides, box,
+                     steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The map of the codes for boxes of 64 tokens x `wide` inputs.
+bool map_codes(CUtensorMap* map, const int8_t* codes, int64_t rows, int64_t pitch, int wide) {
+    if (rows == 0) return true;  // nothing is copied
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(pitch), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(wide), kDepth}, steps[2] = {1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(codes), dims, strides, box, steps,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Lets Kernel use its shared memory, once per device.
@@ -446,13 +494,15 @@ bool allow_shared(int bytes) {
 }
 
 template <typename T, bool kTma, int kN>
-int launch(const WeightGradArgs<T>& a, const CUtensorMap& map, cudaStream_t stream) {
+int launch(const WeightGradArgs<T>& a, const CUtensorMap& dy_map, cudaStream_t stream) {
     constexpr auto kernel = relay_weight_grad_kernel<T, kTma, kN>;
     constexpr int kShared = Stages<T, kN>::kShared;
     if (!allow_shared<kernel>(kShared)) return RELAY_ECUDA;
+    CUtensorMap codes_map = {};
+    if (!map_codes(&codes_map, a.codes, static_cast<int64_t>(a.n) * a.tokens, a.pitch, kN / 2)) return RELAY_ECUDA;
     const dim3 grid(static_cast<unsigned>((a.outputs + 2 * kM - 1) / (2 * kM) * 2),
                     static_cast<unsigned>((a.inputs + kN - 1) / kN), static_cast<unsigned>(a.n * a.splits));
-    kernel<<<grid, kThreads, kShared, stream>>>(a, map);
+    kernel<<<grid, kThreads, kShared, stream>>>(a, dy_map, codes_map);
     return status_of_launch();
 }
 
@@ -481,6 +531,7 @@ int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, 
     const relay_rows out{dweight, worker_stride, row_stride};
     if (!rows_fit(&out, RELAY_FP32, n, outputs, inputs, true)) return RELAY_EINVAL;
     if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned(workspace, 16)))) return RELAY_EINVAL;
+    if (encoder() == nullptr) return RELAY_ECUDA;
     const int splits = token_splits(n, tokens, outputs, inputs);
     float* partial = static_cast<float*>(workspace);
     const int64_t plane = outputs * inputs;
