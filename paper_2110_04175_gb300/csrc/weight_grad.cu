@@ -94,11 +94,6 @@ __device__ __forceinline__ uint32_t recall_pair(uint32_t w, int h, uint32_t unit
     return bits(__hmul2(__hsub2(pair(low), pair(sign)), pair(unit)));
 }
 
-__device__ __forceinline__ uint32_t unit_pair(uint32_t c) {
-    const uint32_t u = c == 255u ? 0x7fffu : (max(c, 7u) - 6u) << 7;
-    return u | u << 16;
-}
-
 // A warp's part of a stage of kWide inputs of xhat: a lane recalls 8 codes of a
 // token per pass.
 template <int kWide>
@@ -109,36 +104,53 @@ struct Recall {
     static constexpr int kTokens = kRows * kPasses;                  // of the warp
     static_assert(kTokens * kMakers == kDepth && kTokens <= 32 && kWide <= 128, "a lane per token's scales");
 
-    // The stage's token number `i` of the warp.
-    static __device__ __forceinline__ int token(int warp, int i) { return (i / kRows * kMakers + warp) * kRows + i % kRows; }
+    static constexpr int kScaled = 32 / kTokens;                     // stages whose scales a load brings
 
-    // The scale bytes of one token, by the first kTokens lanes (a word holds kWide / 32 of
-    // them and what follows, inside the row: its pitch is a multiple of 4).
+    // The stage's token that sub-row `sub` of the warp has in pass r.
+    static __device__ __forceinline__ int token(int warp, int r, int sub) { return (r * kMakers + warp) * kRows + sub; }
+
+    // Lane l's word of scales: those of token l % kTokens (in the order of passes) of
+    // stage l / kTokens from the given one on, each byte less 6 (see unit).  `odd`:
+    // whether some byte says that its block is no number.
     static __device__ __forceinline__ uint32_t scales(const uint8_t* p, int64_t row0, int left, int k0, int pitch,
                                                       int warp, int lane) {
-        const int t = token(warp, lane);
-        if (lane >= kTokens || t >= left || k0 >= pitch) return 0x07070707u;
+        const int i = lane % kTokens, t = lane / kTokens * kDepth + token(warp, i / kRows, i % kRows);
+        if (t >= left || k0 >= pitch) return 0x07070707u;
         const uint8_t* at = p + (row0 + t) * (pitch / kBlock) + k0 / kBlock;
         if constexpr (kWide == 128) return __ldg(reinterpret_cast<const uint32_t*>(at));
         return __ldg(reinterpret_cast<const uint16_t*>(at));
     }
 
-    // `from`: the stage's codes; tokens from `left` on do not count.
-    static __device__ __forceinline__ void make(uint32_t from, uint32_t to, uint32_t scales, int left, int warp,
-                                                int lane) {
-        const int j = lane % kLanes;
+    // `from`: the stage's codes; tokens from `left` on do not count.  scales: what scales()
+    // gave, each byte at least 7, less 6; 249 says that the block is no number.
+    static __device__ __forceinline__ void make(uint32_t from, uint32_t to, uint32_t scales, bool odd, int stage,
+                                                int left, int warp, int lane) {
+        const int j = lane % kLanes, sub = lane / kLanes;
+        const uint32_t pick = 0x4040u | (j / 4) * 0x0101u;  // this lane's byte, in both halves
+        const uint32_t at = from + token(warp, 0, sub) * kWide + 8 * j, put = to + piece(j, token(warp, 0, sub));
         uint2 q[kPasses];
         uint32_t u[kPasses];
 #pragma unroll
         for (int r = 0; r < kPasses; ++r) {
-            const int i = r * kRows + lane / kLanes, t = token(warp, i);
-            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(q[r].x), "=r"(q[r].y) : "r"(from + t * kWide + 8 * j));
-            u[r] = unit_pair(__shfl_sync(0xffffffffu, scales, i) >> (j / 4 * 8) & 0xffu);
-            if (t >= left) q[r] = make_uint2(0, 0);
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
+                         : "=r"(q[r].x), "=r"(q[r].y)
+                         : "r"(at + r * (kMakers * kRows * kWide)));
+            const uint32_t w = __shfl_sync(0xffffffffu, scales, stage % kScaled * kTokens + r * kRows + sub);
+            u[r] = __byte_perm(w, 0u, pick) << 7;
+        }
+        if (odd) {
+#pragma unroll
+            for (int r = 0; r < kPasses; ++r)
+                if (u[r] == (249u << 7 | 249u << 23)) u[r] = 0x7fff7fffu;
+        }
+        if (left < kDepth) {
+#pragma unroll
+            for (int r = 0; r < kPasses; ++r)
+                if (token(warp, r, sub) >= left) q[r] = make_uint2(0, 0), u[r] = 0;
         }
 #pragma unroll
         for (int r = 0; r < kPasses; ++r)
-            put_shared(to + piece(j, token(warp, r * kRows + lane / kLanes)),
+            put_shared(put + r * (kMakers * kRows * 128),
                        make_uint4(recall_pair(q[r].x, 0, u[r]), recall_pair(q[r].x, 1, u[r]),
                                   recall_pair(q[r].y, 0, u[r]), recall_pair(q[r].y, 1, u[r])));
     }
@@ -259,9 +271,9 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         fewer_registers<kOtherRegisters>();
     if (warp < kMakers) {
         using R = Recall<kN / 2>;
-        const auto load = [&](int i) {
-            const int left = i < count ? length - (first + i) * kDepth : 0;
-            return R::scales(a.scales, row0 + i * kDepth, left, half, a.pitch, warp, lane);
+        const auto load = [&](int i) {  // the scales of stages i .. i + R::kScaled - 1
+            const int left = length - (first + i) * kDepth;
+            return R::scales(a.scales, row0 + static_cast<int64_t>(i) * kDepth, left, half, a.pitch, warp, lane);
         };
         // outputs 32 (warp % 4) + lane, inputs kColumns (warp / 4) ..
         float sum[kColumns] = {};
@@ -285,23 +297,25 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             ++groups;
             return true;
         };
-        uint32_t now = load(0), next = load(1), later = load(2);
+        uint32_t now = 0, next = load(0);
+        bool odd = false;
         for (int i = 0; i < count; ++i) {
             const int s = i % kCount, f = i % S::kAhead, t = (first + i) * kDepth;
-            const uint32_t last = load(i + 3);
+            if (i % R::kScaled == 0) {
+                odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
+                now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
+                next = load(i + R::kScaled);
+            }
             if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
             if (!kTma) split_rows(a, worker, t, length - t, o0, stages + s * S::kBytes, warp, lane);
             if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
-            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, length - t, warp, lane);
+            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, i, length - t, warp, lane);
             fence_async();
             __syncwarp();
             if (lane == 0) {
                 barrier_arrive(written(s));
                 barrier_arrive(used(f));
             }
-            now = next;
-            next = later;
-            later = last;
             // stage i - kCount is done, and with it a whole group
             if (i + 1 - kCount == (groups + 1) * kGroup<T> && !(ok = add_group())) break;
         }
@@ -341,9 +355,9 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                 if (from < kDepth) {
                     for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
                         for (int p = 0; p < kM / 64; ++p) put_shared(left + p * kPanel + e * 16, make_uint4(0, 0, 0, 0));
+                    fence_async();
+                    __syncwarp();
                 }
-                fence_async();
-                __syncwarp();
             }
             const int group = i / kGroup<T>, b = group & 1;
             if (i % kGroup<T> == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
