@@ -29,6 +29,8 @@ namespace {
 constexpr int kM = 128;        // outputs of a CTA
 constexpr int kDepth = 64;     // tokens of a stage
 constexpr int kMakers = 8;     // warps that write stages, and the results at the end
+constexpr int kTeams = 2;      // of makers: they take stages in turn, which halves what a stage costs in waits
+constexpr int kTeam = kMakers / kTeams;
 constexpr int kThreads = 32 * (kMakers + 4);  // whole warpgroups; the last warp is idle
 // 3 warpgroups are launched with 168 registers a thread: 2 x 208 + 88 = 3 x 168
 constexpr int kMakerRegisters = 208, kOtherRegisters = 88;
@@ -100,21 +102,20 @@ template <int kWide>
 struct Recall {
     static constexpr int kLanes = kWide / 8;                         // lanes of a token
     static constexpr int kRows = 32 / kLanes;                        // tokens of a pass
-    static constexpr int kPasses = kDepth / (kRows * kMakers);
+    static constexpr int kPasses = kDepth / (kRows * kTeam);
     static constexpr int kTokens = kRows * kPasses;                  // of the warp
-    static_assert(kTokens * kMakers == kDepth && kTokens <= 32 && kWide <= 128, "a lane per token's scales");
+    static_assert(kTokens * kTeam == kDepth && kTokens <= 32 && kWide <= 128, "a lane per token's scales");
 
-    static constexpr int kScaled = 32 / kTokens;                     // stages whose scales a load brings
+    static constexpr int kScaled = 32 / kTokens;                     // of the team's stages: those whose scales a load brings
 
     // The stage's token that sub-row `sub` of the warp has in pass r.
-    static __device__ __forceinline__ int token(int warp, int r, int sub) { return (r * kMakers + warp) * kRows + sub; }
+    static __device__ __forceinline__ int token(int warp, int r, int sub) { return (r * kTeam + warp) * kRows + sub; }
 
     // Lane l's word of scales: those of token l % kTokens (in the order of passes) of
-    // stage l / kTokens from the given one on, each byte less 6 (see unit).  `odd`:
-    // whether some byte says that its block is no number.
+    // the team's stage l / kTokens from the given one on.  warp: in the team.
     static __device__ __forceinline__ uint32_t scales(const uint8_t* p, int64_t row0, int left, int k0, int pitch,
                                                       int warp, int lane) {
-        const int i = lane % kTokens, t = lane / kTokens * kDepth + token(warp, i / kRows, i % kRows);
+        const int i = lane % kTokens, t = lane / kTokens * (kTeams * kDepth) + token(warp, i / kRows, i % kRows);
         if (t >= left || k0 >= pitch) return 0x07070707u;
         const uint8_t* at = p + (row0 + t) * (pitch / kBlock) + k0 / kBlock;
         if constexpr (kWide == 128) return __ldg(reinterpret_cast<const uint32_t*>(at));
@@ -122,8 +123,9 @@ struct Recall {
     }
 
     // `from`: the stage's codes; tokens from `left` on do not count.  scales: what scales()
-    // gave, each byte at least 7, less 6; 249 says that the block is no number.
-    static __device__ __forceinline__ void make(uint32_t from, uint32_t to, uint32_t scales, bool odd, int stage,
+    // gave, each byte at least 7, less 6; 249 says that the block is no number (`odd`: some
+    // byte says so).  turn: the stage's place among those of the load.
+    static __device__ __forceinline__ void make(uint32_t from, uint32_t to, uint32_t scales, bool odd, int turn,
                                                 int left, int warp, int lane) {
         const int j = lane % kLanes, sub = lane / kLanes;
         const uint32_t pick = 0x4040u | (j / 4) * 0x0101u;  // this lane's byte, in both halves
@@ -134,8 +136,8 @@ struct Recall {
         for (int r = 0; r < kPasses; ++r) {
             asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
                          : "=r"(q[r].x), "=r"(q[r].y)
-                         : "r"(at + r * (kMakers * kRows * kWide)));
-            const uint32_t w = __shfl_sync(0xffffffffu, scales, stage % kScaled * kTokens + r * kRows + sub);
+                         : "r"(at + r * (kTeam * kRows * kWide)));
+            const uint32_t w = __shfl_sync(0xffffffffu, scales, turn * kTokens + r * kRows + sub);
             u[r] = __byte_perm(w, 0u, pick) << 7;
         }
         if (odd) {
@@ -150,7 +152,7 @@ struct Recall {
         }
 #pragma unroll
         for (int r = 0; r < kPasses; ++r)
-            put_shared(put + r * (kMakers * kRows * 128),
+            put_shared(put + r * (kTeam * kRows * 128),
                        make_uint4(recall_pair(q[r].x, 0, u[r]), recall_pair(q[r].x, 1, u[r]),
                                   recall_pair(q[r].y, 0, u[r]), recall_pair(q[r].y, 1, u[r])));
     }
@@ -163,8 +165,8 @@ __device__ __forceinline__ void split_rows(const WeightGradArgs<T>& a, int worke
                                            uint32_t to, int warp, int lane) {
     const int j = lane % 16, o = o0 + 8 * j;
 #pragma unroll
-    for (int r = 0; r < kDepth / (2 * kMakers); ++r) {
-        const int t = (r * kMakers + warp) * 2 + lane / 16;
+    for (int r = 0; r < kDepth / (2 * kTeam); ++r) {
+        const int t = (r * kTeam + warp) * 2 + lane / 16;
         float v[8] = {};
         if (t < left && o < a.outputs) {
             const T* p = a.dy.row(worker, token0 + t) + o;
@@ -213,18 +215,15 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t codes = stages + kCount * S::kBytes, bars = codes + S::kAhead * S::kCodes;
-    // per stage: written, copied (dy by TMA), free again, and, on CTA 0, ready on CTA 1; per
-    // accumulator: summed by the tensor cores, and read
-    const auto written = [&](int s) { return bars + 8 * s; };
-    const auto copied = [&](int s) { return bars + 8 * (kCount + s); };
-    const auto freed = [&](int s) { return bars + 8 * (2 * kCount + s); };
-    const auto ready = [&](int s) { return bars + 8 * (3 * kCount + s); };
-    const auto summed = [&](int b) { return bars + 8 * (4 * kCount + b); };
-    const auto read = [&](int b) { return bars + 8 * (4 * kCount + 2 + b); };
-    // per stage of codes: there, and used
-    const auto fetched = [&](int s) { return bars + 8 * (4 * kCount + 4 + s); };
-    const auto used = [&](int s) { return bars + 8 * (4 * kCount + 4 + S::kAhead + s); };
-    const uint32_t tensor_at = bars + 8 * (4 * kCount + 4 + 2 * S::kAhead);
+    // per stage: full (of codes recalled, of dy; on CTA 0 of the other CTA's half too) and free
+    // again; per accumulator: summed by the tensor cores, and read; per stage of codes: there, and used
+    const auto full = [&](int s) { return bars + 8 * s; };
+    const auto freed = [&](int s) { return bars + 8 * (kCount + s); };
+    const auto summed = [&](int b) { return bars + 8 * (2 * kCount + b); };
+    const auto read = [&](int b) { return bars + 8 * (2 * kCount + 2 + b); };
+    const auto fetched = [&](int s) { return bars + 8 * (2 * kCount + 4 + s); };
+    const auto used = [&](int s) { return bars + 8 * (2 * kCount + 4 + S::kAhead + s); };
+    const uint32_t tensor_at = bars + 8 * (2 * kCount + 4 + 2 * S::kAhead);
     __shared__ int stalled;
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -238,10 +237,8 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kCount; ++s) {
-            barrier_init(written(s), kMakers);
-            barrier_init(copied(s), 1);
+            barrier_init(full(s), kTeam + (kTma ? 1 : 0) + (rank == 0 ? 1 : 0));
             barrier_init(freed(s), 1);
-            barrier_init(ready(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(summed(b), 1);
@@ -249,7 +246,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
         for (int s = 0; s < S::kAhead; ++s) {
             barrier_init(fetched(s), 1);
-            barrier_init(used(s), kMakers);
+            barrier_init(used(s), kTeam);
         }
         barriers_ready();
         stalled = 0;
@@ -271,9 +268,10 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         fewer_registers<kOtherRegisters>();
     if (warp < kMakers) {
         using R = Recall<kN / 2>;
-        const auto load = [&](int i) {  // the scales of stages i .. i + R::kScaled - 1
+        const int team = warp / kTeam, member = warp % kTeam;
+        const auto load = [&](int i) {  // the scales of the team's R::kScaled stages from i on
             const int left = length - (first + i) * kDepth;
-            return R::scales(a.scales, row0 + static_cast<int64_t>(i) * kDepth, left, half, a.pitch, warp, lane);
+            return R::scales(a.scales, row0 + static_cast<int64_t>(i) * kDepth, left, half, a.pitch, member, lane);
         };
         // outputs 32 (warp % 4) + lane, inputs kColumns (warp / 4) ..
         float sum[kColumns] = {};
@@ -297,27 +295,29 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             ++groups;
             return true;
         };
-        uint32_t now = 0, next = load(0);
+        uint32_t now = 0, next = load(team);
         bool odd = false;
-        for (int i = 0; i < count; ++i) {
-            const int s = i % kCount, f = i % S::kAhead, t = (first + i) * kDepth;
-            if (i % R::kScaled == 0) {
+        for (int i = team, turn = 0; i < count; i += kTeams) {
+            const int s = i % kCount, f = i % S::kAhead, left = length - (first + i) * kDepth;
+            if (turn == 0) {
                 odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
                 now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
-                next = load(i + R::kScaled);
+                next = load(i + kTeams * R::kScaled);
             }
             if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-            if (!kTma) split_rows(a, worker, t, length - t, o0, stages + s * S::kBytes, warp, lane);
+            if (!kTma)
+                split_rows(a, worker, (first + i) * kDepth, left, o0, stages + s * S::kBytes, member, lane);
             if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
-            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, i, length - t, warp, lane);
+            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
             fence_async();
             __syncwarp();
             if (lane == 0) {
-                barrier_arrive(written(s));
+                barrier_arrive(full(s));
                 barrier_arrive(used(f));
             }
-            // stage i - kCount is done, and with it a whole group
-            if (i + 1 - kCount == (groups + 1) * kGroup<T> && !(ok = add_group())) break;
+            turn = turn == R::kScaled - 1 ? 0 : turn + 1;
+            // stage i - kCount is done, and with it perhaps a whole group
+            if (i + 1 - kCount >= (groups + 1) * kGroup<T> && !(ok = add_group())) break;
         }
         while (ok && groups * kGroup<T> < count) ok = add_group();
         if (!ok) stalled = 1;
@@ -346,39 +346,32 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
     } else if (warp == kMakers) {
         for (int i = 0; i < count; ++i) {
-            const int s = i % kCount;
-            const uint32_t parity = i / kCount & 1, left = stages + s * S::kBytes;
-            if (kTma) {
-                if (!(ok = barrier_wait(copied(s), parity))) break;
-                // the copy brought the rows past the length too, whatever they hold
-                const int from = length - (first + i) * kDepth;
-                if (from < kDepth) {
-                    for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
-                        for (int p = 0; p < kM / 64; ++p) put_shared(left + p * kPanel + e * 16, make_uint4(0, 0, 0, 0));
-                    fence_async();
-                    __syncwarp();
-                }
-            }
-            const int group = i / kGroup<T>, b = group & 1;
+            const int s = i % kCount, group = i / kGroup<T>, b = group & 1;
+            const uint32_t left = stages + s * S::kBytes;
             if (i % kGroup<T> == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
-            if (!(ok = barrier_wait(written(s), parity))) break;
-            if (rank != 0) {  // one arrival for all of this CTA, by a thread with no loads under way
-                if (lane == 0) barrier_arrive_there(in_cta(ready(s), 0));
-                continue;
+            if (!(ok = barrier_wait(full(s), i / kCount & 1))) break;
+            const int from = length - (first + i) * kDepth;
+            if (kTma && from < kDepth) {  // the copy brought the rows past the length too, whatever they hold
+                for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
+                    for (int p = 0; p < kM / 64; ++p) put_shared(left + p * kPanel + e * 16, make_uint4(0, 0, 0, 0));
+                fence_async();
+                __syncwarp();
             }
-            if (!(ok = barrier_wait(ready(s), parity))) break;
-            tensor_fence_after();
             if (lane == 0) {
-                const uint32_t right = left + S::kLeft;
+                if (rank != 0) {
+                    barrier_arrive_there(in_cta(full(s), 0));
+                } else {
+                    tensor_fence_after();
 #pragma unroll
-                for (int term = 0; term < kTerms<T>; ++term)
+                    for (int term = 0; term < kTerms<T>; ++term)
 #pragma unroll
-                    for (int k = 0; k < kDepth / 16; ++k)
-                        product(tensor + b * kN, operand(left + term * (kM / 64 * kPanel) + k * 2048, kPanel, 1024),
-                                operand(right + k * 2048, kPanel, 1024), kProductKind<2 * kM, kN>,
-                                i % kGroup<T> + term + k > 0);
-                products_arrive(freed(s));
-                if (i % kGroup<T> == kGroup<T> - 1 || i == count - 1) products_arrive(summed(b));
+                        for (int k = 0; k < kDepth / 16; ++k)
+                            product(tensor + b * kN, operand(left + term * (kM / 64 * kPanel) + k * 2048, kPanel, 1024),
+                                    operand(left + S::kLeft + k * 2048, kPanel, 1024), kProductKind<2 * kM, kN>,
+                                    i % kGroup<T> + term + k > 0);
+                    products_arrive(freed(s));
+                    if (i % kGroup<T> == kGroup<T> - 1 || i == count - 1) products_arrive(summed(b));
+                }
             }
             __syncwarp();
         }
@@ -387,13 +380,13 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         for (; sent < count; ++sent) {
             const int s = sent % kCount;
             if (!(ok = barrier_wait(freed(s), (sent / kCount & 1) ^ 1))) break;
-            barrier_expect(copied(s), kM / 64 * kPanel);
+            barrier_expect(full(s), kM / 64 * kPanel);
             for (int p = 0; p < kM / 64; ++p)
                 copy_box(stages + s * S::kBytes + p * kPanel, &dy_map, o0 + 64 * p, (first + sent) * kDepth, worker,
-                         copied(s));
+                         full(s));
         }
         for (int i = max(0, sent - kCount); i < sent; ++i)  // nothing is left in flight
-            if (!barrier_wait(copied(i % kCount), i / kCount & 1)) break;
+            if (!barrier_wait(full(i % kCount), i / kCount & 1)) break;
     } else if (warp == kMakers + 2 && lane == 0) {
         int sent = 0;
         for (; sent < count; ++sent) {
