@@ -13,6 +13,19 @@ __device__ __forceinline__ uint32_t shared_address(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
+// One lane of a whole warp, the same every time.
+__device__ __forceinline__ bool elected() {
+    uint32_t is;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(is));
+    return is != 0;
+}
+
 // ------------------------------------------------------------------ mbarriers
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t arrivals) {

@@ -226,7 +226,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
     const uint32_t tensor_at = bars + 8 * (2 * kCount + 4 + 2 * S::kAhead);
     __shared__ int stalled;
 
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x / 32), 0), lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
     const int o0 = blockIdx.x * kM, k0 = blockIdx.y * kN;
     const int worker = blockIdx.z / a.splits, split = blockIdx.z % a.splits;
@@ -357,25 +357,25 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                 fence_async();
                 __syncwarp();
             }
-            if (lane == 0) {
-                if (rank != 0) {
-                    barrier_arrive_there(in_cta(full(s), 0));
-                } else {
-                    tensor_fence_after();
+            if (rank != 0) {
+                if (elected()) barrier_arrive_there(in_cta(full(s), 0));
+                continue;
+            }
+            tensor_fence_after();
+            if (elected()) {
+                const uint64_t dy = operand(left, kPanel, 1024), xhat = operand(left + S::kLeft, kPanel, 1024);
 #pragma unroll
-                    for (int term = 0; term < kTerms<T>; ++term)
+                for (int term = 0; term < kTerms<T>; ++term)
 #pragma unroll
-                        for (int k = 0; k < kDepth / 16; ++k)
-                            product(tensor + b * kN, operand(left + term * (kM / 64 * kPanel) + k * 2048, kPanel, 1024),
-                                    operand(left + S::kLeft + k * 2048, kPanel, 1024), kProductKind<2 * kM, kN>,
-                                    i % kGroup<T> + term + k > 0);
-                    products_arrive(freed(s));
-                    if (i % kGroup<T> == kGroup<T> - 1 || i == count - 1) products_arrive(summed(b));
-                }
+                    for (int k = 0; k < kDepth / 16; ++k)  // addresses count 16 bytes
+                        product(tensor + b * kN, dy + (term * (kM / 64 * kPanel) + k * 2048) / 16, xhat + k * 2048 / 16,
+                                kProductKind<2 * kM, kN>, i % kGroup<T> + term + k > 0);
+                products_arrive(freed(s));
+                if (i % kGroup<T> == kGroup<T> - 1 || i == count - 1) products_arrive(summed(b));
             }
             __syncwarp();
         }
-    } else if (kTma && warp == kMakers + 1 && lane == 0) {
+    } else if (kTma && warp == kMakers + 1 && elected()) {
         int sent = 0;
         for (; sent < count; ++sent) {
             const int s = sent % kCount;
@@ -387,7 +387,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
         for (int i = max(0, sent - kCount); i < sent; ++i)  // nothing is left in flight
             if (!barrier_wait(full(i % kCount), i / kCount & 1)) break;
-    } else if (warp == kMakers + 2 && lane == 0) {
+    } else if (warp == kMakers + 2 && elected()) {
         int sent = 0;
         for (; sent < count; ++sent) {
             const int f = sent % S::kAhead;
