@@ -28,12 +28,13 @@ namespace {
 
 constexpr int kM = 128;        // outputs of a CTA
 constexpr int kDepth = 64;     // tokens of a stage
-constexpr int kMakers = 8;     // warps that write stages, and the results at the end
-constexpr int kTeams = 2;      // of makers: they take stages in turn, which halves what a stage costs in waits
-constexpr int kTeam = kMakers / kTeams;
-constexpr int kThreads = 32 * (kMakers + 4);  // whole warpgroups; the last warp is idle
-// 3 warpgroups are launched with 168 registers a thread: 2 x 208 + 88 = 3 x 168
-constexpr int kMakerRegisters = 208, kOtherRegisters = 88;
+// Warps: 0 .. 7 write stages and add up the sums, 8 .. 11 issue products and copies
+// (one of them is idle), 12 .. 15 write stages only.  The writers are teams of 4 that
+// take stages in turn, so that one team's waits are the others' work.
+constexpr int kAdders = 8, kIssuer = 8, kTeam = 4, kTeams = 3;
+constexpr int kThreads = 32 * 16;
+// 4 warpgroups are launched with 128 registers a thread: 2 x 176 + 64 + 96 = 4 x 128
+constexpr int kAdderRegisters = 176, kIssuerRegisters = 64, kMakerRegisters = 96;
 constexpr int kPanel = kDepth * 128;  // bytes of 64 outputs or inputs x kDepth tokens
 constexpr int kSms = 152;
 
@@ -242,7 +243,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(summed(b), 1);
-            barrier_init(read(b), kMakers);
+            barrier_init(read(b), kAdders);
         }
         for (int s = 0; s < S::kAhead; ++s) {
             barrier_init(fetched(s), 1);
@@ -251,7 +252,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         barriers_ready();
         stalled = 0;
     }
-    if (warp == kMakers) tensor_alloc<2 * kN>(tensor_at);
+    if (warp == kIssuer) tensor_alloc<2 * kN>(tensor_at);
     tensor_fence_before();
     __syncthreads();
     cluster_sync();
@@ -262,17 +263,41 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
     bool ok = true;
     const int half = k0 + kN / 2 * static_cast<int>(rank);  // the inputs that this CTA recalls
     const int64_t row0 = static_cast<int64_t>(worker) * a.tokens + first * kDepth;
-    if (warp < kMakers)
-        more_registers<kMakerRegisters>();
-    else
-        fewer_registers<kOtherRegisters>();
-    if (warp < kMakers) {
+    // Writes the team's stages; after each calls after(i), and ends where that fails.
+    const auto write_stages = [&](int team, auto after) {
         using R = Recall<kN / 2>;
-        const int team = warp / kTeam, member = warp % kTeam;
+        const int member = warp % kTeam;
         const auto load = [&](int i) {  // the scales of the team's R::kScaled stages from i on
             const int left = length - (first + i) * kDepth;
             return R::scales(a.scales, row0 + static_cast<int64_t>(i) * kDepth, left, half, a.pitch, member, lane);
         };
+        uint32_t now = 0, next = load(team);
+        bool odd = false;
+        for (int i = team, turn = 0; i < count; i += kTeams) {
+            const int s = i % kCount, f = i % S::kAhead, left = length - (first + i) * kDepth;
+            if (turn == 0) {
+                odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
+                now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
+                next = load(i + kTeams * R::kScaled);
+            }
+            if (!barrier_wait(freed(s), (i / kCount & 1) ^ 1)) return false;
+            if (!kTma)
+                split_rows(a, worker, (first + i) * kDepth, left, o0, stages + s * S::kBytes, member, lane);
+            if (!barrier_wait(fetched(f), i / S::kAhead & 1)) return false;
+            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+                barrier_arrive(full(s));
+                barrier_arrive(used(f));
+            }
+            turn = turn == R::kScaled - 1 ? 0 : turn + 1;
+            if (!after(i)) return false;
+        }
+        return true;
+    };
+    if (warp < kAdders) {
+        more_registers<kAdderRegisters>();
         // outputs 32 (warp % 4) + lane, inputs kColumns (warp / 4) ..
         float sum[kColumns] = {};
         int groups = 0;  // added up so far
@@ -295,33 +320,13 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             ++groups;
             return true;
         };
-        uint32_t now = 0, next = load(team);
-        bool odd = false;
-        for (int i = team, turn = 0; i < count; i += kTeams) {
-            const int s = i % kCount, f = i % S::kAhead, left = length - (first + i) * kDepth;
-            if (turn == 0) {
-                odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
-                now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
-                next = load(i + kTeams * R::kScaled);
-            }
-            if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-            if (!kTma)
-                split_rows(a, worker, (first + i) * kDepth, left, o0, stages + s * S::kBytes, member, lane);
-            if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
-            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
-            fence_async();
-            __syncwarp();
-            if (lane == 0) {
-                barrier_arrive(full(s));
-                barrier_arrive(used(f));
-            }
-            turn = turn == R::kScaled - 1 ? 0 : turn + 1;
+        ok = write_stages(warp / kTeam, [&](int i) {
             // stage i - kCount is done, and with it perhaps a whole group
-            if (i + 1 - kCount >= (groups + 1) * kGroup<T> && !(ok = add_group())) break;
-        }
+            return i + 1 - kCount < (groups + 1) * kGroup<T> || add_group();
+        });
         while (ok && groups * kGroup<T> < count) ok = add_group();
         if (!ok) stalled = 1;
-        asm volatile("bar.sync 1, %0;" ::"n"(32 * kMakers) : "memory");  // all stages are read: their memory is free
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kAdders) : "memory");  // all stages are read: their memory is free
 
         // through shared memory, so that a warp's stores are contiguous whatever the rows' alignment
         float* turn = reinterpret_cast<float*>(raw + (stages - shared_address(raw))) + warp * (32 * 33);
@@ -344,7 +349,12 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             }
             __syncwarp();
         }
-    } else if (warp == kMakers) {
+    } else if (warp >= kIssuer + 4) {
+        fewer_registers<kMakerRegisters>();
+        ok = write_stages(2, [](int) { return true; });
+    } else {
+      fewer_registers<kIssuerRegisters>();
+      if (warp == kIssuer) {
         for (int i = 0; i < count; ++i) {
             const int s = i % kCount, group = i / kGroup<T>, b = group & 1;
             const uint32_t left = stages + s * S::kBytes;
@@ -375,7 +385,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             }
             __syncwarp();
         }
-    } else if (kTma && warp == kMakers + 1 && elected()) {
+      } else if (kTma && warp == kIssuer + 1 && elected()) {
         int sent = 0;
         for (; sent < count; ++sent) {
             const int s = sent % kCount;
@@ -387,7 +397,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
         for (int i = max(0, sent - kCount); i < sent; ++i)  // nothing is left in flight
             if (!barrier_wait(full(i % kCount), i / kCount & 1)) break;
-    } else if (warp == kMakers + 2 && elected()) {
+      } else if (warp == kIssuer + 2 && elected()) {
         int sent = 0;
         for (; sent < count; ++sent) {
             const int f = sent % S::kAhead;
@@ -397,11 +407,13 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
         for (int i = max(0, sent - S::kAhead); i < sent; ++i)
             if (!barrier_wait(fetched(i % S::kAhead), i / S::kAhead & 1)) break;
+      }
     }
+    if (!ok) stalled = 1;
     __syncwarp();
     __syncthreads();
     cluster_sync();  // the other CTA is done with this one's memory too
-    if (warp == kMakers) tensor_free<2 * kN>(tensor);
+    if (warp == kIssuer) tensor_free<2 * kN>(tensor);
 }
 
 // dweight = scale times the sum of the splits' partial sums, in their order.
