@@ -28,13 +28,13 @@ namespace {
 
 constexpr int kM = 128;        // outputs of a CTA
 constexpr int kDepth = 64;     // tokens of a stage
-// Warps: 0 .. 7 write stages and add up the sums, 8 .. 11 issue products and copies
-// (one of them is idle), 12 .. 15 write stages only.  The writers are teams of 4 that
-// take stages in turn, so that one team's waits are the others' work.
-constexpr int kAdders = 8, kIssuer = 8, kTeam = 4, kTeams = 3;
-constexpr int kThreads = 32 * 16;
-// 4 warpgroups are launched with 128 registers a thread: 2 x 176 + 64 + 96 = 4 x 128
-constexpr int kAdderRegisters = 176, kIssuerRegisters = 64, kMakerRegisters = 96;
+// Warps: 0 .. 7 add up the sums and write them to memory, 8 .. 11 issue products and
+// copies (one of them is idle), 12 .. 19 write stages: two teams of 4 take them in
+// turn, so that one team's waits are the other's work.
+constexpr int kAdders = 8, kIssuer = 8, kMaker = 12, kTeam = 4, kTeams = 2;
+constexpr int kThreads = 32 * (kMaker + kTeam * kTeams);
+// 5 warpgroups are launched with 96 registers a thread: 2 x 152 + 48 + 2 x 64 = 5 x 96
+constexpr int kAdderRegisters = 152, kIssuerRegisters = 48, kMakerRegisters = 64;
 constexpr int kPanel = kDepth * 128;  // bytes of 64 outputs or inputs x kDepth tokens
 constexpr int kSms = 152;
 
@@ -47,15 +47,19 @@ constexpr int kTerms<__nv_bfloat16> = 1;
 template <typename T>
 constexpr int kGroup = kTerms<T> == 1 ? 8 : 4;
 
+// An adder's 32 rows x 16 columns on their way to memory, rows 80 bytes apart.
+constexpr int kTurnRow = 20, kTurn = 32 * kTurnRow * 4;
+
 template <typename T, int kN>
 struct Stages {  // in a CTA
     static constexpr int kLeft = kTerms<T> * kM / 64 * kPanel, kBytes = kLeft + kN / 2 / 64 * kPanel;
-    static constexpr int kCount = 196608 / kBytes < 4 ? 196608 / kBytes : 4;
     // stages of codes, as they lie in memory: they come well before they are needed
     static constexpr int kCodes = kN / 2 * kDepth;
-    static constexpr int kAhead = kCount * kBytes + 8 * kCodes <= 196608 ? 8 : 4;
-    static constexpr int kShared = kCount * kBytes + kAhead * kCodes + 1024 + 512;  // alignment, barriers
-    static_assert(kShared <= 232448, "shared memory of a CTA");
+    static constexpr int kRoom = 232448 - 1024 - 512 - kAdders * kTurn;  // less alignment, barriers
+    static constexpr int kMost = (kRoom - 4 * kCodes) / kBytes, kCount = kMost < 4 ? kMost : 4;
+    static constexpr int kFit = (kRoom - kCount * kBytes) / kCodes, kAhead = kFit < 8 ? 4 : 8;
+    static constexpr int kShared = kCount * kBytes + kAhead * kCodes + kAdders * kTurn + 1024 + 512;
+    static_assert(kCount >= 2 && kFit >= kAhead && kShared <= 232448, "shared memory of a CTA");
 };
 
 template <typename T>
@@ -69,7 +73,32 @@ struct WeightGradArgs {
     const int32_t* lengths;
     float* out;  // dweight, or with several splits the partial sums [split][n][outputs][inputs]
     int64_t worker_stride, row_stride, split_stride;
+    bool out_quads;  // rows of `out` can be written 16 bytes at a time
     int32_t n, tokens, outputs, inputs, pitch, splits;
+    int32_t tiles_o, tiles_k;  // of a worker and split: 256 outputs, kN inputs
+    int32_t tiles;             // of all
+};
+
+// One tile of the work and the stages of tokens that it sums.
+struct Tile {
+    int o0, k0, worker, split, length, first, count;
+
+    // Tiles are taken in bands of 8 x 256 outputs, so that those in work at a time share
+    // rows of both operands.
+    template <typename T>
+    __device__ __forceinline__ Tile(const WeightGradArgs<T>& a, int tile, int wide) {
+        const int plane = a.tiles_o * a.tiles_k, z = tile / plane, at = tile - z * plane;
+        const int band = at / (8 * a.tiles_k), in = at - band * 8 * a.tiles_k;
+        const int rows = min(8, a.tiles_o - 8 * band);
+        o0 = (8 * band + in % rows) * 2 * kM;
+        k0 = in / rows * wide;
+        worker = z / a.splits;
+        split = z - worker * a.splits;
+        length = a.lengths == nullptr ? a.tokens : min(max(a.lengths[worker], 0), a.tokens);
+        const int all = (length + kDepth - 1) / kDepth, each = (all + a.splits - 1) / a.splits;
+        first = min(split * each, all);
+        count = min(first + each, all) - first;
+    }
 };
 
 // ----------------------------------------------------------------- the stages
@@ -88,13 +117,20 @@ __device__ __forceinline__ void put_shared(uint32_t at, uint4 v) {
 __device__ __forceinline__ uint32_t bits(__nv_bfloat162 v) { return *reinterpret_cast<uint32_t*>(&v); }
 __device__ __forceinline__ __nv_bfloat162 pair(uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); }
 
-// Codes 2h and 2h + 1 of the word w times `unit` (twice the same bf16).  A byte b
-// stands for (b & 127) - (b & 128); under the exponent of 128 the two parts are
-// the bf16 values 128 + (b & 127) and 128 + (b & 128), whose difference is exact.
-__device__ __forceinline__ uint32_t recall_pair(uint32_t w, int h, uint32_t unit) {
-    const uint32_t p = __byte_perm(w, 0u, h ? 0x4342 : 0x4140);
-    const uint32_t low = (p & 0x007f007fu) | 0x43004300u, sign = (p & 0x00800080u) | 0x43004300u;
+// The bytes 0 and 2 of w as codes, times `unit` (twice the same bf16).  A byte b stands
+// for (b & 127) - (b & 128); under the exponent of 128 the two parts are the bf16
+// values 128 + (b & 127) and 128 + (b & 128), whose difference is exact.
+__device__ __forceinline__ uint32_t recall_pair(uint32_t w, uint32_t unit) {
+    const uint32_t low = (w & 0x007f007fu) | 0x43004300u, sign = (w & 0x00800080u) | 0x43004300u;
     return bits(__hmul2(__hsub2(pair(low), pair(sign)), pair(unit)));
+}
+
+// Inputs lie in the operand in the order 0 2 1 3 of each four, which is how two bytes
+// of a word come to the halves of another; the sums are put back in order on their
+// way to memory.
+__device__ __forceinline__ uint4 recall(uint2 q, uint32_t unit) {
+    return make_uint4(recall_pair(q.x, unit), recall_pair(q.x >> 8, unit), recall_pair(q.y, unit),
+                      recall_pair(q.y >> 8, unit));
 }
 
 // A warp's part of a stage of kWide inputs of xhat: a lane recalls 8 codes of a
@@ -112,13 +148,13 @@ struct Recall {
     // The stage's token that sub-row `sub` of the warp has in pass r.
     static __device__ __forceinline__ int token(int warp, int r, int sub) { return (r * kTeam + warp) * kRows + sub; }
 
-    // Lane l's word of scales: those of token l % kTokens (in the order of passes) of
-    // the team's stage l / kTokens from the given one on.  warp: in the team.
-    static __device__ __forceinline__ uint32_t scales(const uint8_t* p, int64_t row0, int left, int k0, int pitch,
-                                                      int warp, int lane) {
-        const int i = lane % kTokens, t = lane / kTokens * (kTeams * kDepth) + token(warp, i / kRows, i % kRows);
-        if (t >= left || k0 >= pitch) return 0x07070707u;
-        const uint8_t* at = p + (row0 + t) * (pitch / kBlock) + k0 / kBlock;
+    // Lane l's word of scales is that of the warp's token l % kTokens (in the order of
+    // passes) of the team's stage l / kTokens; warp: in the team.
+    static __device__ __forceinline__ int scale_token(int warp, int lane) {
+        const int i = lane % kTokens;
+        return lane / kTokens * (kTeams * kDepth) + token(warp, i / kRows, i % kRows);
+    }
+    static __device__ __forceinline__ uint32_t scales(const uint8_t* at) {
         if constexpr (kWide == 128) return __ldg(reinterpret_cast<const uint32_t*>(at));
         return __ldg(reinterpret_cast<const uint16_t*>(at));
     }
@@ -153,9 +189,7 @@ struct Recall {
         }
 #pragma unroll
         for (int r = 0; r < kPasses; ++r)
-            put_shared(put + r * (kTeam * kRows * 128),
-                       make_uint4(recall_pair(q[r].x, 0, u[r]), recall_pair(q[r].x, 1, u[r]),
-                                  recall_pair(q[r].y, 0, u[r]), recall_pair(q[r].y, 1, u[r])));
+            put_shared(put + r * (kTeam * kRows * 128), recall(q[r], u[r]));
     }
 };
 
@@ -202,20 +236,20 @@ __device__ __forceinline__ void split_rows(const WeightGradArgs<T>& a, int worke
 
 // ----------------------------------------------------------------- the kernel
 
-// A pair of CTAs per tile of 256 outputs x kN inputs and per split of the tokens.
-// Warps 0 .. 7 write xhat (and dy, without TMA) into the stages, add up the sums
-// and write them to memory; warp 8 of CTA 0 issues the products (that of CTA 1
-// says when its half is ready); warps 9 and 10 issue the copies.  A wait that runs out ends the
-// work on the tile, and its results are NaN.
+// Pairs of CTAs take tiles of 256 outputs x kN inputs (of a worker, of a split of the
+// tokens) one after the other: the next one's products run while the last one's sums
+// go to memory.  A wait that runs out ends a pair's work, and its results from there
+// on are NaN.
 template <typename T, bool kTma, int kN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __grid_constant__ CUtensorMap dy_map,
                          const __grid_constant__ CUtensorMap codes_map) {
     using S = Stages<T, kN>;
-    constexpr int kCount = S::kCount, kColumns = kN / 2;  // columns: of a warp, in the end
+    constexpr int kCount = S::kCount;
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
-    const uint32_t codes = stages + kCount * S::kBytes, bars = codes + S::kAhead * S::kCodes;
+    const uint32_t codes = stages + kCount * S::kBytes, turns = codes + S::kAhead * S::kCodes;
+    const uint32_t bars = turns + kAdders * kTurn;
     // per stage: full (of codes recalled, of dy; on CTA 0 of the other CTA's half too) and free
     // again; per accumulator: summed by the tensor cores, and read; per stage of codes: there, and used
     const auto full = [&](int s) { return bars + 8 * s; };
@@ -225,16 +259,10 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
     const auto fetched = [&](int s) { return bars + 8 * (2 * kCount + 4 + s); };
     const auto used = [&](int s) { return bars + 8 * (2 * kCount + 4 + S::kAhead + s); };
     const uint32_t tensor_at = bars + 8 * (2 * kCount + 4 + 2 * S::kAhead);
-    __shared__ int stalled;
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x / 32), 0), lane = threadIdx.x % 32;
-    const uint32_t rank = cluster_rank();
-    const int o0 = blockIdx.x * kM, k0 = blockIdx.y * kN;
-    const int worker = blockIdx.z / a.splits, split = blockIdx.z % a.splits;
-    const int length = a.lengths == nullptr ? a.tokens : min(max(a.lengths[worker], 0), a.tokens);
-    // this split's stages of the tokens
-    const int all = (length + kDepth - 1) / kDepth, each = (all + a.splits - 1) / a.splits;
-    const int first = min(split * each, all), count = min(first + each, all) - first;
+    const int rank = static_cast<int>(cluster_rank());
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kCount; ++s) {
@@ -250,7 +278,6 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             barrier_init(used(s), kTeam);
         }
         barriers_ready();
-        stalled = 0;
     }
     if (warp == kIssuer) tensor_alloc<2 * kN>(tensor_at);
     tensor_fence_before();
@@ -260,156 +287,210 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
     uint32_t tensor;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
 
-    bool ok = true;
-    const int half = k0 + kN / 2 * static_cast<int>(rank);  // the inputs that this CTA recalls
-    const int64_t row0 = static_cast<int64_t>(worker) * a.tokens + first * kDepth;
-    // Writes the team's stages; after each calls after(i), and ends where that fails.
-    const auto write_stages = [&](int team, auto after) {
-        using R = Recall<kN / 2>;
-        const int member = warp % kTeam;
-        const auto load = [&](int i) {  // the scales of the team's R::kScaled stages from i on
-            const int left = length - (first + i) * kDepth;
-            return R::scales(a.scales, row0 + static_cast<int64_t>(i) * kDepth, left, half, a.pitch, member, lane);
-        };
-        uint32_t now = 0, next = load(team);
-        bool odd = false;
-        for (int i = team, turn = 0; i < count; i += kTeams) {
-            const int s = i % kCount, f = i % S::kAhead, left = length - (first + i) * kDepth;
-            if (turn == 0) {
-                odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
-                now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
-                next = load(i + kTeams * R::kScaled);
-            }
-            if (!barrier_wait(freed(s), (i / kCount & 1) ^ 1)) return false;
-            if (!kTma)
-                split_rows(a, worker, (first + i) * kDepth, left, o0, stages + s * S::kBytes, member, lane);
-            if (!barrier_wait(fetched(f), i / S::kAhead & 1)) return false;
-            R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
-            fence_async();
-            __syncwarp();
-            if (lane == 0) {
-                barrier_arrive(full(s));
-                barrier_arrive(used(f));
-            }
-            turn = turn == R::kScaled - 1 ? 0 : turn + 1;
-            if (!after(i)) return false;
-        }
-        return true;
-    };
     if (warp < kAdders) {
         more_registers<kAdderRegisters>();
-        // outputs 32 (warp % 4) + lane, inputs kColumns (warp / 4) ..
-        float sum[kColumns] = {};
-        int groups = 0;  // added up so far
-        const auto add_group = [&] {
-            const int b = groups & 1;
-            if (!barrier_wait(summed(b), groups >> 1 & 1)) return false;
-            tensor_fence_after();
-            const uint32_t at =
-                tensor + (static_cast<uint32_t>(32 * (warp % 4)) << 16) + b * kN + kColumns * (warp / 4);
+        constexpr int kColumns = kN / 2;
+        const int row = 32 * (warp % 4), column = kColumns * (warp / 4);  // of the CTA's 128 x kN
+        const uint32_t turn = turns + warp * kTurn;
+        bool ok = true;
+        int group = 0;  // of all that the pair has summed
+        for (int tile = pair; tile < a.tiles; tile += pairs) {
+            const Tile at(a, tile, kN);
+            float sum[kColumns] = {};
+            for (int done = 0; done < at.count && ok; done += kGroup<T>, ++group) {
+                const int b = group & 1;
+                if (!(ok = barrier_wait(summed(b), group >> 1 & 1))) break;
+                tensor_fence_after();
+                const uint32_t from = tensor + (static_cast<uint32_t>(row) << 16) + b * kN + column;
+#pragma unroll
+                for (int c = 0; c < kColumns; c += 16) {
+                    float v[16];
+                    tensor_load(from + c, v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[c + e] += v[e];
+                }
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(read(b));
+            }
+            // through shared memory, so that a warp writes 64 contiguous bytes of each row
+            const int o = at.o0 + kM * rank + row;
+            float* out = a.out + at.split * a.split_stride + at.worker * a.worker_stride;
+            const float* scale =
+                a.column_scale == nullptr || a.splits > 1 ? nullptr : a.column_scale + at.worker * a.column_scale_stride;
 #pragma unroll
             for (int c = 0; c < kColumns; c += 16) {
-                float v[16];
-                tensor_load(at + c, v);
+                const int k0 = at.k0 + column + c;
+                if (k0 < a.inputs) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum[c + e] += v[e];
+                    for (int e = 0; e < 16; e += 4)
+                        put_shared(turn + lane * (4 * kTurnRow) + 4 * e,
+                                   make_uint4(__float_as_uint(sum[c + e]), __float_as_uint(sum[c + e + 2]),
+                                              __float_as_uint(sum[c + e + 1]), __float_as_uint(sum[c + e + 3])));
+                    __syncwarp();
+                    if (a.out_quads) {
+                        const int k = k0 + 4 * (lane % 4);
+                        float4 m = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                        if (scale != nullptr && k < a.inputs) m = make_float4(scale[k], scale[k + 1], scale[k + 2], scale[k + 3]);
+                        if (!ok) m.x = m.y = m.z = m.w = __int_as_float(0x7fffffff);
+#pragma unroll
+                        for (int r = lane / 4; r < 32; r += 8) {
+                            float4 v;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                         : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                                         : "r"(turn + r * (4 * kTurnRow) + 16 * (lane % 4)));
+                            v.x *= m.x, v.y *= m.y, v.z *= m.z, v.w *= m.w;
+                            if (o + r < a.outputs && k < a.inputs)
+                                *reinterpret_cast<float4*>(out + (o + r) * a.row_stride + k) = v;
+                        }
+                    } else {
+                        const int k = k0 + lane % 16;
+                        float m = scale == nullptr || k >= a.inputs ? 1.0f : scale[k];
+                        if (!ok) m = __int_as_float(0x7fffffff);
+#pragma unroll 4
+                        for (int r = lane / 16; r < 32; r += 2) {
+                            float v;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(turn + r * (4 * kTurnRow) + 4 * (lane % 16)));
+                            if (o + r < a.outputs && k < a.inputs) out[(o + r) * a.row_stride + k] = v * m;
+                        }
+                    }
+                    __syncwarp();
+                }
             }
-            tensor_fence_before();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(read(b));
-            ++groups;
-            return true;
-        };
-        ok = write_stages(warp / kTeam, [&](int i) {
-            // stage i - kCount is done, and with it perhaps a whole group
-            return i + 1 - kCount < (groups + 1) * kGroup<T> || add_group();
-        });
-        while (ok && groups * kGroup<T> < count) ok = add_group();
-        if (!ok) stalled = 1;
-        asm volatile("bar.sync 1, %0;" ::"n"(32 * kAdders) : "memory");  // all stages are read: their memory is free
-
-        // through shared memory, so that a warp's stores are contiguous whatever the rows' alignment
-        float* turn = reinterpret_cast<float*>(raw + (stages - shared_address(raw))) + warp * (32 * 33);
-        float* out = a.out + split * a.split_stride + worker * a.worker_stride;
-        const int o = o0 + 32 * (warp % 4);
-#pragma unroll
-        for (int c = 0; c < kColumns; c += 32) {
-            const int k = k0 + kColumns * (warp / 4) + c + lane;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) turn[lane * 33 + e] = sum[c + e];
-            __syncwarp();
-            if (k < a.inputs) {
-                float scale = a.column_scale == nullptr || a.splits > 1
-                                  ? 1.0f
-                                  : a.column_scale[worker * a.column_scale_stride + k];
-                if (stalled) scale = __int_as_float(0x7fffffff);
-#pragma unroll 8
-                for (int r = 0; r < 32; ++r)
-                    if (o + r < a.outputs) out[(o + r) * a.row_stride + k] = turn[r * 33 + lane] * scale;
-            }
-            __syncwarp();
         }
-    } else if (warp >= kIssuer + 4) {
-        fewer_registers<kMakerRegisters>();
-        ok = write_stages(2, [](int) { return true; });
+    } else if (warp < kMaker) {
+        fewer_registers<kIssuerRegisters>();
+        if (warp == kIssuer) {
+            int i = 0, group = 0;  // of all that the pair has summed
+            bool ok = true;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const Tile at(a, tile, kN);
+                for (int n = 0; n < at.count; ++n, ++i) {
+                    const int s = i % kCount, place = n % kGroup<T>, b = group & 1;
+                    const uint32_t left = stages + s * S::kBytes;
+                    if (place == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
+                    if (!(ok = barrier_wait(full(s), i / kCount & 1))) break;
+                    const int from = at.length - (at.first + n) * kDepth;
+                    if (kTma && from < kDepth) {  // the copy brought the rows past the length too, whatever they hold
+                        for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
+                            for (int p = 0; p < kM / 64; ++p)
+                                put_shared(left + p * kPanel + e * 16, make_uint4(0, 0, 0, 0));
+                        fence_async();
+                        __syncwarp();
+                    }
+                    const bool last = place == kGroup<T> - 1 || n == at.count - 1;
+                    if (rank != 0) {
+                        if (elected()) barrier_arrive_there(in_cta(full(s), 0));
+                    } else {
+                        tensor_fence_after();
+                        if (elected()) {
+                            const uint64_t dy = operand(left, kPanel, 1024), xhat = operand(left + S::kLeft, kPanel, 1024);
+#pragma unroll
+                            for (int term = 0; term < kTerms<T>; ++term)
+#pragma unroll
+                                for (int k = 0; k < kDepth / 16; ++k)  // addresses count 16 bytes
+                                    product(tensor + b * kN, dy + (term * (kM / 64 * kPanel) + k * 2048) / 16,
+                                            xhat + k * 2048 / 16, kProductKind<2 * kM, kN>, place + term + k > 0);
+                            products_arrive(freed(s));
+                            if (last) products_arrive(summed(b));
+                        }
+                        __syncwarp();
+                    }
+                    if (last) ++group;
+                }
+            }
+        } else if (kTma && warp == kIssuer + 1 && elected()) {
+            int i = 0;
+            bool ok = true;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const Tile at(a, tile, kN);
+                for (int n = 0; n < at.count; ++n, ++i) {
+                    const int s = i % kCount;
+                    if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
+                    barrier_expect(full(s), kM / 64 * kPanel);
+                    for (int p = 0; p < kM / 64; ++p)
+                        copy_box(stages + s * S::kBytes + p * kPanel, &dy_map, at.o0 + kM * rank + 64 * p,
+                                 (at.first + n) * kDepth, at.worker, full(s));
+                }
+            }
+            for (int j = max(0, i - kCount); j < i; ++j)  // nothing is left in flight
+                if (!barrier_wait(full(j % kCount), j / kCount & 1)) break;
+        } else if (warp == kIssuer + 2 && elected()) {
+            int i = 0;
+            bool ok = true;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const Tile at(a, tile, kN);
+                const int row0 = at.worker * a.tokens + at.first * kDepth, half = at.k0 + kN / 2 * rank;
+                for (int n = 0; n < at.count; ++n, ++i) {
+                    const int f = i % S::kAhead;
+                    if (!(ok = barrier_wait(used(f), (i / S::kAhead & 1) ^ 1))) break;
+                    barrier_expect(fetched(f), S::kCodes);
+                    copy_box(codes + f * S::kCodes, &codes_map, half, row0 + n * kDepth, fetched(f));
+                }
+            }
+            for (int j = max(0, i - S::kAhead); j < i; ++j)
+                if (!barrier_wait(fetched(j % S::kAhead), j / S::kAhead & 1)) break;
+        }
     } else {
-      fewer_registers<kIssuerRegisters>();
-      if (warp == kIssuer) {
-        for (int i = 0; i < count; ++i) {
-            const int s = i % kCount, group = i / kGroup<T>, b = group & 1;
-            const uint32_t left = stages + s * S::kBytes;
-            if (i % kGroup<T> == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
-            if (!(ok = barrier_wait(full(s), i / kCount & 1))) break;
-            const int from = length - (first + i) * kDepth;
-            if (kTma && from < kDepth) {  // the copy brought the rows past the length too, whatever they hold
-                for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
-                    for (int p = 0; p < kM / 64; ++p) put_shared(left + p * kPanel + e * 16, make_uint4(0, 0, 0, 0));
+        fewer_registers<kMakerRegisters>();
+        using R = Recall<kN / 2>;
+        const int team = (warp - kMaker) / kTeam, member = warp % kTeam;
+        // The scales come one load of R::kScaled stages ahead, across tiles: `ahead` is where the
+        // lane's next word is, `ahead_left` how many of the tile's tokens there are from its
+        // stage on, `ahead_stages` how many stages.
+        const int mine = R::scale_token(member, lane);
+        const int64_t stride = int64_t(kTeams) * R::kScaled * kDepth * (a.pitch / kBlock);
+        const uint8_t* ahead = nullptr;
+        int ahead_tile = pair - pairs, ahead_left = 0, ahead_stages = 0, ahead_base = 0, ahead_count = 0;
+        uint32_t now = 0, next = 0;
+        bool ok = true, odd = false;
+        const auto load_next = [&] {
+            while (ahead_stages <= 0) {
+                ahead_tile += pairs;
+                if (ahead_tile >= a.tiles) return 0u;
+                const Tile at(a, ahead_tile, kN);
+                ahead_base += ahead_count;  // the team's first stage has its number among all
+                ahead_count = at.count;
+                const int n = (team + ahead_base) % kTeams, k = at.k0 + kN / 2 * rank, t = (at.first + n) * kDepth;
+                ahead_stages = at.count - n;
+                ahead_left = k < a.pitch ? at.length - t : 0;
+                ahead = a.scales + (static_cast<int64_t>(at.worker) * a.tokens + t + mine) * (a.pitch / kBlock) + k / kBlock;
+            }
+            const uint32_t w = mine < ahead_left ? R::scales(ahead) : 0x07070707u;
+            ahead += stride;
+            ahead_left -= kTeams * R::kScaled * kDepth;
+            ahead_stages -= kTeams * R::kScaled;
+            return w;
+        };
+        int base = 0;
+        next = load_next();
+        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+            const Tile at(a, tile, kN);
+            int turn = 0;
+            for (int n = (team + base) % kTeams; n < at.count; n += kTeams) {
+                const int i = base + n, s = i % kCount, f = i % S::kAhead, left = at.length - (at.first + n) * kDepth;
+                if (turn == 0) {
+                    odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
+                    now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
+                    next = load_next();
+                }
+                if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
+                if (!kTma)
+                    split_rows(a, at.worker, (at.first + n) * kDepth, left, at.o0 + kM * rank, stages + s * S::kBytes,
+                               member, lane);
+                if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
+                R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
                 fence_async();
                 __syncwarp();
+                if (lane == 0) {
+                    barrier_arrive(full(s));
+                    barrier_arrive(used(f));
+                }
+                turn = turn == R::kScaled - 1 ? 0 : turn + 1;
             }
-            if (rank != 0) {
-                if (elected()) barrier_arrive_there(in_cta(full(s), 0));
-                continue;
-            }
-            tensor_fence_after();
-            if (elected()) {
-                const uint64_t dy = operand(left, kPanel, 1024), xhat = operand(left + S::kLeft, kPanel, 1024);
-#pragma unroll
-                for (int term = 0; term < kTerms<T>; ++term)
-#pragma unroll
-                    for (int k = 0; k < kDepth / 16; ++k)  // addresses count 16 bytes
-                        product(tensor + b * kN, dy + (term * (kM / 64 * kPanel) + k * 2048) / 16, xhat + k * 2048 / 16,
-                                kProductKind<2 * kM, kN>, i % kGroup<T> + term + k > 0);
-                products_arrive(freed(s));
-                if (i % kGroup<T> == kGroup<T> - 1 || i == count - 1) products_arrive(summed(b));
-            }
-            __syncwarp();
+            base += at.count;
         }
-      } else if (kTma && warp == kIssuer + 1 && elected()) {
-        int sent = 0;
-        for (; sent < count; ++sent) {
-            const int s = sent % kCount;
-            if (!(ok = barrier_wait(freed(s), (sent / kCount & 1) ^ 1))) break;
-            barrier_expect(full(s), kM / 64 * kPanel);
-            for (int p = 0; p < kM / 64; ++p)
-                copy_box(stages + s * S::kBytes + p * kPanel, &dy_map, o0 + 64 * p, (first + sent) * kDepth, worker,
-                         full(s));
-        }
-        for (int i = max(0, sent - kCount); i < sent; ++i)  // nothing is left in flight
-            if (!barrier_wait(full(i % kCount), i / kCount & 1)) break;
-      } else if (warp == kIssuer + 2 && elected()) {
-        int sent = 0;
-        for (; sent < count; ++sent) {
-            const int f = sent % S::kAhead;
-            if (!(ok = barrier_wait(used(f), (sent / S::kAhead & 1) ^ 1))) break;
-            barrier_expect(fetched(f), S::kCodes);
-            copy_box(codes + f * S::kCodes, &codes_map, half, static_cast<int>(row0) + sent * kDepth, fetched(f));
-        }
-        for (int i = max(0, sent - S::kAhead); i < sent; ++i)
-            if (!barrier_wait(fetched(i % S::kAhead), i / S::kAhead & 1)) break;
-      }
     }
-    if (!ok) stalled = 1;
     __syncwarp();
     __syncthreads();
     cluster_sync();  // the other CTA is done with this one's memory too
@@ -513,15 +594,19 @@ bool allow_shared(int bytes) {
 }
 
 template <typename T, bool kTma, int kN>
-int launch(const WeightGradArgs<T>& a, const CUtensorMap& dy_map, cudaStream_t stream) {
+int launch(WeightGradArgs<T> a, const CUtensorMap& dy_map, cudaStream_t stream) {
     constexpr auto kernel = relay_weight_grad_kernel<T, kTma, kN>;
     constexpr int kShared = Stages<T, kN>::kShared;
     if (!allow_shared<kernel>(kShared)) return RELAY_ECUDA;
     CUtensorMap codes_map = {};
     if (!map_codes(&codes_map, a.codes, static_cast<int64_t>(a.n) * a.tokens, a.pitch, kN / 2)) return RELAY_ECUDA;
-    const dim3 grid(static_cast<unsigned>((a.outputs + 2 * kM - 1) / (2 * kM) * 2),
-                    static_cast<unsigned>((a.inputs + kN - 1) / kN), static_cast<unsigned>(a.n * a.splits));
-    kernel<<<grid, kThreads, kShared, stream>>>(a, dy_map, codes_map);
+    const int64_t tiles = tile_count(a.n, a.outputs, a.inputs, kN) * a.splits;
+    if (tiles > INT32_MAX - kSms) return RELAY_EUNSUPPORTED;
+    a.tiles_o = (a.outputs + 2 * kM - 1) / (2 * kM);
+    a.tiles_k = (a.inputs + kN - 1) / kN;
+    a.tiles = static_cast<int32_t>(tiles);
+    const int pairs = tiles < kSms / 2 ? static_cast<int>(tiles) : kSms / 2;
+    kernel<<<2 * pairs, kThreads, kShared, stream>>>(a, dy_map, codes_map);
     return status_of_launch();
 }
 
@@ -560,9 +645,13 @@ int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, 
         const WeightGradArgs<T> a{rows, outputs % 8 == 0 && vectors(dy, type, n, tokens), codes, scales, column_scale,
                                   n > 1 ? column_scale_stride : 0, lengths, splits > 1 ? partial : dweight,
                                   splits > 1 ? plane : n > 1 ? worker_stride : 0,
-                                  splits > 1 ? inputs : outputs > 1 ? row_stride : 0, splits > 1 ? n * plane : 0, n,
+                                  splits > 1 ? inputs : outputs > 1 ? row_stride : 0, splits > 1 ? n * plane : 0,
+                                  inputs % 4 == 0 && (splits > 1 || (aligned(dweight, 16) &&
+                                                                     (n == 1 || worker_stride % 4 == 0) &&
+                                                                     (outputs == 1 || row_stride % 4 == 0))),
+                                  n,
                                   static_cast<int32_t>(tokens), static_cast<int32_t>(outputs),
-                                  static_cast<int32_t>(inputs), static_cast<int32_t>(pitch_of(inputs)), splits};
+                                  static_cast<int32_t>(inputs), static_cast<int32_t>(pitch_of(inputs)), splits, 0, 0, 0};
         CUtensorMap map = {};
         const bool wide = tile_inputs(n, outputs, inputs) == 256;
         if constexpr (sizeof(T) == 2 && kTerms<T> == 1) {
