@@ -29,12 +29,12 @@ namespace {
 constexpr int kM = 128;        // outputs of a CTA
 constexpr int kDepth = 64;     // tokens of a stage
 // Warps: 0 .. 7 add up the sums and write them to memory, 8 .. 11 issue products and
-// copies (one of them is idle), 12 .. 19 write stages: two teams of 4 take them in
-// turn, so that one team's waits are the other's work.
-constexpr int kAdders = 8, kIssuer = 8, kMaker = 12, kTeam = 4, kTeams = 2;
+// copies (one of them is idle), 12 .. 23 write stages: three teams of 4 take them in
+// turn, so that one team's waits are the others' work (two teams: 6 % slower).
+constexpr int kAdders = 8, kIssuer = 8, kMaker = 12, kTeam = 4, kTeams = 3;
 constexpr int kThreads = 32 * (kMaker + kTeam * kTeams);
-// 5 warpgroups are launched with 96 registers a thread: 2 x 152 + 48 + 2 x 64 = 5 x 96
-constexpr int kAdderRegisters = 152, kIssuerRegisters = 48, kMakerRegisters = 64;
+// 6 warpgroups are launched with 80 registers a thread: 2 x 144 + 48 + 3 x 48 = 6 x 80
+constexpr int kAdderRegisters = 144, kIssuerRegisters = 48, kMakerRegisters = 48;
 constexpr int kPanel = kDepth * 128;  // bytes of 64 outputs or inputs x kDepth tokens
 constexpr int kSms = 152;
 
@@ -132,6 +132,9 @@ __device__ __forceinline__ uint4 recall(uint2 q, uint32_t unit) {
     return make_uint4(recall_pair(q.x, unit), recall_pair(q.x >> 8, unit), recall_pair(q.y, unit),
                       recall_pair(q.y >> 8, unit));
 }
+
+// The first stage of `team` from number `base` of all on, counted from there.
+__device__ __forceinline__ int first_stage(int team, int base) { return (team + kTeams - base % kTeams) % kTeams; }
 
 // A warp's part of a stage of kWide inputs of xhat: a lane recalls 8 codes of a
 // token per pass.
@@ -449,9 +452,9 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                 ahead_tile += pairs;
                 if (ahead_tile >= a.tiles) return 0u;
                 const Tile at(a, ahead_tile, kN);
-                ahead_base += ahead_count;  // the team's first stage has its number among all
+                ahead_base += ahead_count;
                 ahead_count = at.count;
-                const int n = (team + ahead_base) % kTeams, k = at.k0 + kN / 2 * rank, t = (at.first + n) * kDepth;
+                const int n = first_stage(team, ahead_base), k = at.k0 + kN / 2 * rank, t = (at.first + n) * kDepth;
                 ahead_stages = at.count - n;
                 ahead_left = k < a.pitch ? at.length - t : 0;
                 ahead = a.scales + (static_cast<int64_t>(at.worker) * a.tokens + t + mine) * (a.pitch / kBlock) + k / kBlock;
@@ -467,7 +470,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
             const Tile at(a, tile, kN);
             int turn = 0;
-            for (int n = (team + base) % kTeams; n < at.count; n += kTeams) {
+            for (int n = first_stage(team, base); n < at.count; n += kTeams) {
                 const int i = base + n, s = i % kCount, f = i % S::kAhead, left = at.length - (at.first + n) * kDepth;
                 if (turn == 0) {
                     odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
