@@ -141,8 +141,13 @@ int relay_gated_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, con
                          const relay_rows *dgate, const relay_rows *dup, int8_t *out_codes, uint8_t *out_scales,
                          relay_stream_t stream);
 
-/* Bytes of workspace for relay_weight_grad (may be 0), or a negative status. */
-int64_t relay_weight_grad_workspace(int32_t n, int64_t tokens, int64_t outputs, int64_t inputs);
+/* Bytes of workspace for relay_weight_grad (may be 0), or a negative status.
+ * dy: the rows that it will get, or NULL for any strides and alignment.  fp16
+ * and fp32 rows, and bf16 rows that are not 16-byte aligned or that repeat,
+ * are copied into it (2, 3 or 1 times 2 bytes an element).  The size for
+ * RELAY_FP32 and NULL is enough for every call of the other sizes. */
+int64_t relay_weight_grad_workspace(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs,
+                                    const relay_rows *dy);
 
 /* The weight gradient of a linear layer, per worker, from the gradient of its
  * outputs dy [n][tokens][outputs] and its inputs in 8 bits; overwrites

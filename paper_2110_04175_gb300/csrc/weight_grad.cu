@@ -9,9 +9,9 @@
 // memory, M and N fastest, 64 tokens at a time:
 //   - xhat is recalled from its codes on the way: a code is a whole number of 7
 //     bits and its scale a power of two, so the bf16 values are exact;
-//   - dy in bf16 comes by TMA.  fp16 and fp32 (and rows that TMA cannot take) are
-//     read by the warps that recall xhat and split into bf16 terms that add up to
-//     them exactly, 8 bits each: 2 for fp16, 3 for fp32, one product each.
+//   - dy comes by TMA, as bf16.  fp16 and fp32 rows (and bf16 rows that TMA cannot
+//     take) are written to the workspace first as bf16 terms that add up to them
+//     exactly, 8 bits each: 2 for fp16, 3 for fp32, one product each.
 //
 // A pair of CTAs makes a tile of 256 outputs x kN inputs (cta_group::2): each
 // brings half of both operands, so that a code is recalled once for 256 outputs.
@@ -38,34 +38,33 @@ constexpr int kAdderRegisters = 144, kIssuerRegisters = 48, kMakerRegisters = 48
 constexpr int kPanel = kDepth * 128;  // bytes of 64 outputs or inputs x kDepth tokens
 constexpr int kSms = 152;
 
-template <typename T>
-constexpr int kTerms = sizeof(T) == 4 ? 3 : 2;  // bf16 terms of a value
-template <>
-constexpr int kTerms<__nv_bfloat16> = 1;
-
 // Stages that the tensor cores sum before the sums are added up in registers.
-template <typename T>
-constexpr int kGroup = kTerms<T> == 1 ? 8 : 4;
+template <int kTerms>
+constexpr int kGroup = kTerms == 1 ? 8 : 4;
 
 // An adder's 32 rows x 16 columns on their way to memory, rows 80 bytes apart.
 constexpr int kTurnRow = 20, kTurn = 32 * kTurnRow * 4;
 
-template <typename T, int kN>
+template <int kTerms, int kN>
 struct Stages {  // in a CTA
-    static constexpr int kLeft = kTerms<T> * kM / 64 * kPanel, kBytes = kLeft + kN / 2 / 64 * kPanel;
+    static constexpr int kLeft = kTerms * kM / 64 * kPanel, kBytes = kLeft + kN / 2 / 64 * kPanel;
     // stages of codes, as they lie in memory: they come well before they are needed
     static constexpr int kCodes = kN / 2 * kDepth;
     static constexpr int kRoom = 232448 - 1024 - 512 - kAdders * kTurn;  // less alignment, barriers
     static constexpr int kMost = (kRoom - 4 * kCodes) / kBytes, kCount = kMost < 4 ? kMost : 4;
     static constexpr int kFit = (kRoom - kCount * kBytes) / kCodes, kAhead = kFit < 8 ? 4 : 8;
     static constexpr int kShared = kCount * kBytes + kAhead * kCodes + kAdders * kTurn + 1024 + 512;
-    static_assert(kCount >= 2 && kFit >= kAhead && kShared <= 232448, "shared memory of a CTA");
+    static_assert(kFit >= kAhead && kShared <= 232448, "shared memory of a CTA");
+    // Teams at work: no more than stages.  A wait for a phase passes too when the barrier is
+    // two phases behind, and a team that goes from stage i to stage i + teams knows only that
+    // stage i - kCount was freed, which is the phase before the one it waits for if
+    // i + teams - 2 kCount is that stage or an earlier one.  The same for stages of codes, of
+    // which there are as many or more.
+    static constexpr int kTeamsIn = kCount < kTeams ? kCount : kTeams;
+    static_assert(kCount >= 2 && kTeamsIn <= kCount && kAhead >= kCount, "phases of the barriers");
 };
 
-template <typename T>
 struct WeightGradArgs {
-    View<const T> dy;
-    bool dy_vectors;
     const int8_t* codes;
     const uint8_t* scales;
     const float* column_scale;
@@ -85,8 +84,7 @@ struct Tile {
 
     // Tiles are taken in bands of 8 x 256 outputs, so that those in work at a time share
     // rows of both operands.
-    template <typename T>
-    __device__ __forceinline__ Tile(const WeightGradArgs<T>& a, int tile, int wide) {
+    __device__ __forceinline__ Tile(const WeightGradArgs& a, int tile, int wide) {
         const int plane = a.tiles_o * a.tiles_k, z = tile / plane, at = tile - z * plane;
         const int band = at / (8 * a.tiles_k), in = at - band * 8 * a.tiles_k;
         const int rows = min(8, a.tiles_o - 8 * band);
@@ -134,11 +132,14 @@ __device__ __forceinline__ uint4 recall(uint2 q, uint32_t unit) {
 }
 
 // The first stage of `team` from number `base` of all on, counted from there.
-__device__ __forceinline__ int first_stage(int team, int base) { return (team + kTeams - base % kTeams) % kTeams; }
+template <int kTeamsIn>
+__device__ __forceinline__ int first_stage(int team, int base) {
+    return (team + kTeamsIn - base % kTeamsIn) % kTeamsIn;
+}
 
 // A warp's part of a stage of kWide inputs of xhat: a lane recalls 8 codes of a
 // token per pass.
-template <int kWide>
+template <int kWide, int kTeamsIn>
 struct Recall {
     static constexpr int kLanes = kWide / 8;                         // lanes of a token
     static constexpr int kRows = 32 / kLanes;                        // tokens of a pass
@@ -155,7 +156,7 @@ struct Recall {
     // passes) of the team's stage l / kTokens; warp: in the team.
     static __device__ __forceinline__ int scale_token(int warp, int lane) {
         const int i = lane % kTokens;
-        return lane / kTokens * (kTeams * kDepth) + token(warp, i / kRows, i % kRows);
+        return lane / kTokens * (kTeamsIn * kDepth) + token(warp, i / kRows, i % kRows);
     }
     static __device__ __forceinline__ uint32_t scales(const uint8_t* at) {
         if constexpr (kWide == 128) return __ldg(reinterpret_cast<const uint32_t*>(at));
@@ -196,43 +197,37 @@ struct Recall {
     }
 };
 
-// A warp's part of a stage of dy, read and split into bf16 terms: each term is
-// what is left with all but 8 bits cut off, so that the terms add up exactly.
-template <typename T>
-__device__ __forceinline__ void split_rows(const WeightGradArgs<T>& a, int worker, int token0, int left, int o0,
-                                           uint32_t to, int warp, int lane) {
-    const int j = lane % 16, o = o0 + 8 * j;
+// dy as bf16 terms [n][kTerms][tokens][width], width = outputs rounded up to a multiple
+// of 8: each term is what is left with all but 8 bits cut off, so that the terms add up
+// exactly.  Rows that do not count are 0.
+template <typename T, int kTerms, bool kVec>
+__global__ void __launch_bounds__(256)
+relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bfloat16* to, int n, int tokens,
+                               int outputs, int width) {
+    const int lane = threadIdx.x % 32, strips = (outputs + kStrip - 1) / kStrip;
+    const int64_t all = static_cast<int64_t>(n) * tokens * strips;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
+        const int64_t row = i / strips;
+        const int base = static_cast<int>(i - row * strips) * kStrip, worker = static_cast<int>(row / tokens);
+        const int token = static_cast<int>(row - static_cast<int64_t>(worker) * tokens);
+        float v[8];
+        load_strip<kVec>(dy.row(worker, token) + base, lane,
+                         lengths == nullptr || token < lengths[worker] ? outputs - base : 0, v);
 #pragma unroll
-    for (int r = 0; r < kDepth / (2 * kTeam); ++r) {
-        const int t = (r * kTeam + warp) * 2 + lane / 16;
-        float v[8] = {};
-        if (t < left && o < a.outputs) {
-            const T* p = a.dy.row(worker, token0 + t) + o;
-            if (a.dy_vectors) {
-                load_strip<true>(p, 0, 8, v);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (o + k < a.outputs) v[k] = widen(p[k]);
-            }
-        }
-#pragma unroll
-        for (int term = 0; term < kTerms<T>; ++term) {
-            uint32_t w[8];
+        for (int term = 0; term < kTerms; ++term) {
+            float high[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                uint32_t high = __float_as_uint(v[k]) & 0xffff0000u;
-                if ((high & 0x7f800000u) == 0x7f800000u) {  // infinity or NaN: all in the first term
-                    high = v[k] != v[k] ? 0x7fff0000u : high;
+                high[k] = __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u);
+                if ((__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u) {  // infinity or NaN: all in the first term
+                    high[k] = v[k];
                     v[k] = 0.0f;
                 } else {
-                    v[k] -= __uint_as_float(high);
+                    v[k] -= high[k];
                 }
-                w[k] = high;
             }
-            put_shared(to + term * (kM / 64 * kPanel) + piece(j, t),
-                       make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632),
-                                  __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632)));
+            store_strip<kVec>(to + ((static_cast<int64_t>(worker) * kTerms + term) * tokens + token) * width + base, lane,
+                              outputs - base, high);
         }
     }
 }
@@ -243,11 +238,11 @@ __device__ __forceinline__ void split_rows(const WeightGradArgs<T>& a, int worke
 // tokens) one after the other: the next one's products run while the last one's sums
 // go to memory.  A wait that runs out ends a pair's work, and its results from there
 // on are NaN.
-template <typename T, bool kTma, int kN>
+template <int kTerms, int kN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __grid_constant__ CUtensorMap dy_map,
+relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap dy_map,
                          const __grid_constant__ CUtensorMap codes_map) {
-    using S = Stages<T, kN>;
+    using S = Stages<kTerms, kN>;
     constexpr int kCount = S::kCount;
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
@@ -269,7 +264,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kCount; ++s) {
-            barrier_init(full(s), kTeam + (kTma ? 1 : 0) + (rank == 0 ? 1 : 0));
+            barrier_init(full(s), kTeam + 1 + (rank == 0 ? 1 : 0));
             barrier_init(freed(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -300,7 +295,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         for (int tile = pair; tile < a.tiles; tile += pairs) {
             const Tile at(a, tile, kN);
             float sum[kColumns] = {};
-            for (int done = 0; done < at.count && ok; done += kGroup<T>, ++group) {
+            for (int done = 0; done < at.count && ok; done += kGroup<kTerms>, ++group) {
                 const int b = group & 1;
                 if (!(ok = barrier_wait(summed(b), group >> 1 & 1))) break;
                 tensor_fence_after();
@@ -369,19 +364,19 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
             for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
                 const Tile at(a, tile, kN);
                 for (int n = 0; n < at.count; ++n, ++i) {
-                    const int s = i % kCount, place = n % kGroup<T>, b = group & 1;
+                    const int s = i % kCount, place = n % kGroup<kTerms>, b = group & 1;
                     const uint32_t left = stages + s * S::kBytes;
                     if (place == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
                     if (!(ok = barrier_wait(full(s), i / kCount & 1))) break;
                     const int from = at.length - (at.first + n) * kDepth;
-                    if (kTma && from < kDepth) {  // the copy brought the rows past the length too, whatever they hold
+                    if (kTerms == 1 && from < kDepth) {  // the copy brought the rows past the length too, whatever they hold
                         for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
                             for (int p = 0; p < kM / 64; ++p)
                                 put_shared(left + p * kPanel + e * 16, make_uint4(0, 0, 0, 0));
                         fence_async();
                         __syncwarp();
                     }
-                    const bool last = place == kGroup<T> - 1 || n == at.count - 1;
+                    const bool last = place == kGroup<kTerms> - 1 || n == at.count - 1;
                     if (rank != 0) {
                         if (elected()) barrier_arrive_there(in_cta(full(s), 0));
                     } else {
@@ -389,7 +384,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                         if (elected()) {
                             const uint64_t dy = operand(left, kPanel, 1024), xhat = operand(left + S::kLeft, kPanel, 1024);
 #pragma unroll
-                            for (int term = 0; term < kTerms<T>; ++term)
+                            for (int term = 0; term < kTerms; ++term)
 #pragma unroll
                                 for (int k = 0; k < kDepth / 16; ++k)  // addresses count 16 bytes
                                     product(tensor + b * kN, dy + (term * (kM / 64 * kPanel) + k * 2048) / 16,
@@ -402,7 +397,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                     if (last) ++group;
                 }
             }
-        } else if (kTma && warp == kIssuer + 1 && elected()) {
+        } else if (warp == kIssuer + 1 && elected()) {
             int i = 0;
             bool ok = true;
             for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
@@ -410,10 +405,10 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                 for (int n = 0; n < at.count; ++n, ++i) {
                     const int s = i % kCount;
                     if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-                    barrier_expect(full(s), kM / 64 * kPanel);
-                    for (int p = 0; p < kM / 64; ++p)
-                        copy_box(stages + s * S::kBytes + p * kPanel, &dy_map, at.o0 + kM * rank + 64 * p,
-                                 (at.first + n) * kDepth, at.worker, full(s));
+                    barrier_expect(full(s), S::kLeft);
+                    for (int p = 0; p < S::kLeft / kPanel; ++p)
+                        copy_box(stages + s * S::kBytes + p * kPanel, &dy_map, at.o0 + kM * rank + 64 * (p % (kM / 64)),
+                                 (at.first + n) * kDepth, at.worker * kTerms + p / (kM / 64), full(s));
                 }
             }
             for (int j = max(0, i - kCount); j < i; ++j)  // nothing is left in flight
@@ -436,13 +431,13 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
         }
     } else {
         fewer_registers<kMakerRegisters>();
-        using R = Recall<kN / 2>;
+        using R = Recall<kN / 2, S::kTeamsIn>;
         const int team = (warp - kMaker) / kTeam, member = warp % kTeam;
         // The scales come one load of R::kScaled stages ahead, across tiles: `ahead` is where the
         // lane's next word is, `ahead_left` how many of the tile's tokens there are from its
         // stage on, `ahead_stages` how many stages.
         const int mine = R::scale_token(member, lane);
-        const int64_t stride = int64_t(kTeams) * R::kScaled * kDepth * (a.pitch / kBlock);
+        const int64_t stride = int64_t(S::kTeamsIn) * R::kScaled * kDepth * (a.pitch / kBlock);
         const uint8_t* ahead = nullptr;
         int ahead_tile = pair - pairs, ahead_left = 0, ahead_stages = 0, ahead_base = 0, ahead_count = 0;
         uint32_t now = 0, next = 0;
@@ -454,23 +449,23 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                 const Tile at(a, ahead_tile, kN);
                 ahead_base += ahead_count;
                 ahead_count = at.count;
-                const int n = first_stage(team, ahead_base), k = at.k0 + kN / 2 * rank, t = (at.first + n) * kDepth;
+                const int n = first_stage<S::kTeamsIn>(team, ahead_base), k = at.k0 + kN / 2 * rank, t = (at.first + n) * kDepth;
                 ahead_stages = at.count - n;
                 ahead_left = k < a.pitch ? at.length - t : 0;
                 ahead = a.scales + (static_cast<int64_t>(at.worker) * a.tokens + t + mine) * (a.pitch / kBlock) + k / kBlock;
             }
             const uint32_t w = mine < ahead_left ? R::scales(ahead) : 0x07070707u;
             ahead += stride;
-            ahead_left -= kTeams * R::kScaled * kDepth;
-            ahead_stages -= kTeams * R::kScaled;
+            ahead_left -= S::kTeamsIn * R::kScaled * kDepth;
+            ahead_stages -= S::kTeamsIn * R::kScaled;
             return w;
         };
         int base = 0;
-        next = load_next();
-        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+        if (team < S::kTeamsIn) next = load_next();
+        for (int tile = pair; tile < a.tiles && ok && team < S::kTeamsIn; tile += pairs) {
             const Tile at(a, tile, kN);
             int turn = 0;
-            for (int n = first_stage(team, base); n < at.count; n += kTeams) {
+            for (int n = first_stage<S::kTeamsIn>(team, base); n < at.count; n += S::kTeamsIn) {
                 const int i = base + n, s = i % kCount, f = i % S::kAhead, left = at.length - (at.first + n) * kDepth;
                 if (turn == 0) {
                     odd = __any_sync(0xffffffffu, __vcmpeq4(next, 0xffffffffu) != 0u);
@@ -478,9 +473,6 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs<T> a, const __gr
                     next = load_next();
                 }
                 if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-                if (!kTma)
-                    split_rows(a, at.worker, (at.first + n) * kDepth, left, at.o0 + kM * rank, stages + s * S::kBytes,
-                               member, lane);
                 if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
                 R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
                 fence_async();
@@ -523,17 +515,31 @@ int64_t tile_count(int64_t n, int64_t outputs, int64_t inputs, int wide) {
     return n * ((outputs + 2 * kM - 1) / (2 * kM)) * ((inputs + wide - 1) / wide);
 }
 
-// Inputs of a tile: 256, or 128 where those would leave SMs idle.
-int tile_inputs(int64_t n, int64_t outputs, int64_t inputs) {
-    return tile_count(n, outputs, inputs, 256) >= kSms / 2 ? 256 : 128;
-}
+// How the work is cut: inputs of a tile, and splits of the tokens.
+struct Cut {
+    int wide, splits;
+};
 
-// Splits of the tokens: as many as there are pairs of SMs for, of at least 8 stages each.
-int token_splits(int64_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
-    const int64_t tiles = tile_count(n, outputs, inputs, tile_inputs(n, outputs, inputs));
-    const int64_t room = kSms / 2 / tiles, most = tokens / (8 * kDepth);
-    const int64_t s = room < most ? room : most;
-    return s > 1 ? static_cast<int>(s) : 1;
+// The cut that should take the least time, by what was measured: a pair takes 0.37 us
+// for a stage of a 256 x 256 tile and 0.26 us for one of 256 x 128 (more where two or
+// three terms keep the tensor cores longer), and 6 us for a tile besides; splits cost
+// the partial sums' way to memory and back and a launch.
+Cut best_cut(int terms, int64_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
+    const int64_t stages = (tokens + kDepth - 1) / kDepth, pairs = kSms / 2;
+    Cut best{256, 1};
+    double least = 0.0;
+    for (const int wide : {256, 128}) {
+        const int64_t tiles = tile_count(n, outputs, inputs, wide);
+        const double stage = wide == 256 ? (terms == 1 ? 0.37 : 0.32 * terms) : (terms == 1 ? 0.26 : 0.2 * terms);
+        for (int64_t splits = 1; splits <= pairs && (splits == 1 || (tiles * (splits - 1) < 2 * pairs && stages >= 4 * splits));
+             ++splits) {
+            const double rounds = static_cast<double>((tiles * splits + pairs - 1) / pairs);
+            double us = rounds * (6.0 + stage * static_cast<double>((stages + splits - 1) / splits));
+            if (splits > 1) us += 4.0 + 4e-6 * (splits + 1) * static_cast<double>(n * outputs * inputs) / 5.0;
+            if ((wide == 256 && splits == 1) || us < least) least = us, best = Cut{wide, static_cast<int>(splits)};
+        }
+    }
+    return best;
 }
 
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -556,18 +562,38 @@ Encode encoder() {
     return encode;
 }
 
-// The map of dy for 64 x 64 boxes; false where TMA cannot take its rows.
-bool map_rows(CUtensorMap* map, const View<const __nv_bfloat16>& dy, int32_t n, int64_t tokens, int64_t outputs) {
-    if (tokens == 0 || (tokens > 1 && dy.ts < outputs) || (n > 1 && dy.ws < outputs)) return false;
+// The map of bf16 rows [planes][tokens][outputs] for boxes of 64 x 64.
+bool map_rows(CUtensorMap* map, const void* rows, int64_t planes, int64_t tokens, int64_t outputs,
+              int64_t plane_bytes, int64_t row_bytes) {
+    if (tokens == 0) return true;  // nothing is copied
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(outputs), static_cast<cuuint64_t>(tokens),
-                                static_cast<cuuint64_t>(n)};
-    // an axis of one row or one worker is never walked: any stride will do
-    const cuuint64_t row = tokens > 1 ? static_cast<cuuint64_t>(dy.ts) * 2 : (outputs * 2 + 15) / 16 * 16;
-    const cuuint64_t strides[2] = {row, n > 1 ? static_cast<cuuint64_t>(dy.ws) * 2 : row};
+                                static_cast<cuuint64_t>(planes)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_bytes), static_cast<cuuint64_t>(plane_bytes)};
     const cuuint32_t box[3] = {64, kDepth, 1}, steps[3] = {1, 1, 1};
-    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(dy.p), dims, strides, box,
-                     steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(rows), dims, strides, box, steps,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Whether TMA takes the rows as they are: bf16, 16-byte steps, no row read twice.
+bool direct(int32_t type, const relay_rows* dy, int32_t n, int64_t tokens, int64_t outputs) {
+    constexpr int64_t kMost = int64_t(1) << 38;  // elements: a map's strides end at 2^40 bytes
+    return type == RELAY_BF16 && dy != nullptr && vectors(dy, type, n, tokens) &&
+           (tokens <= 1 || (dy->token_stride >= outputs && dy->token_stride < kMost)) &&
+           (n == 1 || (dy->worker_stride >= outputs && dy->worker_stride < kMost));
+}
+
+int terms_of(int32_t type) { return type == RELAY_BF16 ? 1 : type == RELAY_FP16 ? 2 : 3; }
+int64_t width_of(int64_t outputs) { return (outputs + 7) / 8 * 8; }
+
+// Bytes of the workspace's two parts: dy's terms, and the splits' partial sums.
+int64_t terms_bytes(int32_t type, const relay_rows* dy, int32_t n, int64_t tokens, int64_t outputs) {
+    if (direct(type, dy, n, tokens, outputs)) return 0;
+    return 2 * terms_of(type) * n * tokens * width_of(outputs);
+}
+int64_t partial_bytes(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
+    const int splits = best_cut(terms_of(type), n, tokens, outputs, inputs).splits;
+    return splits > 1 ? 4 * splits * n * outputs * inputs : 0;
 }
 
 // The map of the codes for boxes of 64 tokens x `wide` inputs.
@@ -596,10 +622,10 @@ bool allow_shared(int bytes) {
     return true;
 }
 
-template <typename T, bool kTma, int kN>
-int launch(WeightGradArgs<T> a, const CUtensorMap& dy_map, cudaStream_t stream) {
-    constexpr auto kernel = relay_weight_grad_kernel<T, kTma, kN>;
-    constexpr int kShared = Stages<T, kN>::kShared;
+template <int kTerms, int kN>
+int launch(WeightGradArgs a, const CUtensorMap& dy_map, cudaStream_t stream) {
+    constexpr auto kernel = relay_weight_grad_kernel<kTerms, kN>;
+    constexpr int kShared = Stages<kTerms, kN>::kShared;
     if (!allow_shared<kernel>(kShared)) return RELAY_ECUDA;
     CUtensorMap codes_map = {};
     if (!map_codes(&codes_map, a.codes, static_cast<int64_t>(a.n) * a.tokens, a.pitch, kN / 2)) return RELAY_ECUDA;
@@ -613,16 +639,34 @@ int launch(WeightGradArgs<T> a, const CUtensorMap& dy_map, cudaStream_t stream) 
     return status_of_launch();
 }
 
+template <int kTerms>
+int launch(const WeightGradArgs& a, const CUtensorMap& dy_map, int wide, cudaStream_t stream) {
+    return wide == 256 ? launch<kTerms, 256>(a, dy_map, stream) : launch<kTerms, 128>(a, dy_map, stream);
+}
+
+template <typename T, int kTerms>
+int write_terms(const relay_rows* dy, int32_t type, const int32_t* lengths, void* to, int32_t n, int64_t tokens,
+                int64_t outputs, cudaStream_t stream) {
+    const int64_t warps = n * tokens * ((outputs + kStrip - 1) / kStrip), most = 16 * kSms;
+    const int ctas = static_cast<int>((warps + 7) / 8 < most ? (warps + 7) / 8 : most);
+    const bool vec = outputs % 8 == 0 && vectors(dy, type, n, tokens);
+    (vec ? relay_weight_grad_terms_kernel<T, kTerms, true> : relay_weight_grad_terms_kernel<T, kTerms, false>)
+        <<<ctas, 256, 0, stream>>>(view<const T>(dy, n, tokens), lengths, static_cast<__nv_bfloat16*>(to), n,
+                                   static_cast<int>(tokens), static_cast<int>(outputs),
+                                   static_cast<int>(width_of(outputs)));
+    return status_of_launch();
+}
+
 }  // namespace
 
 extern "C" {
 
-int64_t relay_weight_grad_workspace(int32_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
-    if (const int rc = check_shape(RELAY_FP32, n, tokens, inputs)) return rc;
-    if (const int rc = check_shape(RELAY_FP32, n, tokens, outputs)) return rc;
+int64_t relay_weight_grad_workspace(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs,
+                                    const relay_rows* dy) {
+    if (const int rc = check_shape(type, n, tokens, inputs)) return rc;
+    if (const int rc = check_shape(type, n, tokens, outputs)) return rc;
     if (inputs > RELAY_WEIGHT_GRAD_MAX_INPUTS) return RELAY_EUNSUPPORTED;
-    const int splits = token_splits(n, tokens, outputs, inputs);
-    return splits > 1 ? 4 * splits * n * outputs * inputs : 0;
+    return terms_bytes(type, dy, n, tokens, outputs) + partial_bytes(type, n, tokens, outputs, inputs);
 }
 
 int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs, const relay_rows* dy,
@@ -630,7 +674,7 @@ int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, 
                       int64_t column_scale_stride, const int32_t* lengths, float* dweight, int64_t worker_stride,
                       int64_t row_stride, void* workspace, int64_t workspace_bytes, relay_stream_t stream) {
     if (const int rc = check_shape(type, n, tokens, inputs)) return rc;
-    const int64_t need = relay_weight_grad_workspace(n, tokens, outputs, inputs);
+    const int64_t need = relay_weight_grad_workspace(type, n, tokens, outputs, inputs, dy);
     if (need < 0) return static_cast<int>(need);
     if (!rows_fit(dy, type, n, tokens, outputs, false) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
     if (!aligned(column_scale, 4) || (column_scale != nullptr && column_scale_stride < 0) || !aligned(lengths, 4))
@@ -639,38 +683,52 @@ int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, 
     if (!rows_fit(&out, RELAY_FP32, n, outputs, inputs, true)) return RELAY_EINVAL;
     if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned(workspace, 16)))) return RELAY_EINVAL;
     if (encoder() == nullptr) return RELAY_ECUDA;
-    const int splits = token_splits(n, tokens, outputs, inputs);
-    float* partial = static_cast<float*>(workspace);
-    const int64_t plane = outputs * inputs;
-    const auto run = [&](auto t) {
-        using T = decltype(t);
-        const View<const T> rows = view<const T>(dy, n, tokens);
-        const WeightGradArgs<T> a{rows, outputs % 8 == 0 && vectors(dy, type, n, tokens), codes, scales, column_scale,
-                                  n > 1 ? column_scale_stride : 0, lengths, splits > 1 ? partial : dweight,
-                                  splits > 1 ? plane : n > 1 ? worker_stride : 0,
-                                  splits > 1 ? inputs : outputs > 1 ? row_stride : 0, splits > 1 ? n * plane : 0,
-                                  inputs % 4 == 0 && (splits > 1 || (aligned(dweight, 16) &&
-                                                                     (n == 1 || worker_stride % 4 == 0) &&
-                                                                     (outputs == 1 || row_stride % 4 == 0))),
-                                  n,
-                                  static_cast<int32_t>(tokens), static_cast<int32_t>(outputs),
-                                  static_cast<int32_t>(inputs), static_cast<int32_t>(pitch_of(inputs)), splits, 0, 0, 0};
-        CUtensorMap map = {};
-        const bool wide = tile_inputs(n, outputs, inputs) == 256;
-        if constexpr (sizeof(T) == 2 && kTerms<T> == 1) {
-            if (vectors(dy, type, n, tokens) && map_rows(&map, rows, n, tokens, outputs))
-                return wide ? launch<T, true, 256>(a, map, stream) : launch<T, true, 128>(a, map, stream);
-        }
-        return wide ? launch<T, false, 256>(a, map, stream) : launch<T, false, 128>(a, map, stream);
-    };
-    const int rc =
-        type == RELAY_BF16 ? run(__nv_bfloat16()) : type == RELAY_FP16 ? run(__half()) : run(float());
-    if (rc != RELAY_OK || splits == 1) return rc;
+
+    const int terms = terms_of(type);
+    const Cut cut = best_cut(terms, n, tokens, outputs, inputs);
+    const int64_t terms_size = terms_bytes(type, dy, n, tokens, outputs), plane = outputs * inputs;
+    CUtensorMap map = {};
+    if (terms_size == 0) {
+        // an axis of one row or one worker is never walked: any stride will do
+        const int64_t row = tokens > 1 ? dy->token_stride * 2 : width_of(outputs) * 2;
+        if (!map_rows(&map, dy->data, n, tokens, outputs, n > 1 ? dy->worker_stride * 2 : row, row)) return RELAY_ECUDA;
+    } else {
+        const int64_t row = width_of(outputs) * 2;
+        if (!map_rows(&map, workspace, n * terms, tokens, outputs, tokens * row, row)) return RELAY_ECUDA;
+        const int rc = type == RELAY_BF16
+                           ? write_terms<__nv_bfloat16, 1>(dy, type, lengths, workspace, n, tokens, outputs, stream)
+                       : type == RELAY_FP16 ? write_terms<__half, 2>(dy, type, lengths, workspace, n, tokens, outputs, stream)
+                                            : write_terms<float, 3>(dy, type, lengths, workspace, n, tokens, outputs, stream);
+        if (rc != RELAY_OK) return rc;
+    }
+    float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + terms_size);
+    const bool split = cut.splits > 1;
+    WeightGradArgs a{};
+    a.codes = codes;
+    a.scales = scales;
+    a.column_scale = column_scale;
+    a.column_scale_stride = n > 1 ? column_scale_stride : 0;
+    a.lengths = lengths;
+    a.out = split ? partial : dweight;
+    a.worker_stride = split ? plane : n > 1 ? worker_stride : 0;
+    a.row_stride = split ? inputs : outputs > 1 ? row_stride : 0;
+    a.split_stride = split ? n * plane : 0;
+    a.out_quads = inputs % 4 == 0 && aligned(a.out, 16) && a.worker_stride % 4 == 0 && a.row_stride % 4 == 0;
+    a.n = n;
+    a.tokens = static_cast<int32_t>(tokens);
+    a.outputs = static_cast<int32_t>(outputs);
+    a.inputs = static_cast<int32_t>(inputs);
+    a.pitch = static_cast<int32_t>(pitch_of(inputs));
+    a.splits = cut.splits;
+    const int rc = terms == 1   ? launch<1>(a, map, cut.wide, stream)
+                   : terms == 2 ? launch<2>(a, map, cut.wide, stream)
+                                : launch<3>(a, map, cut.wide, stream);
+    if (rc != RELAY_OK || !split) return rc;
     const dim3 grid(static_cast<unsigned>((inputs + 255) / 256),
                     static_cast<unsigned>(outputs < 65535 ? outputs : 65535), static_cast<unsigned>(n));
     relay_weight_grad_join_kernel<<<grid, 256, 0, stream>>>(
-        partial, n * plane, splits, static_cast<int>(outputs), static_cast<int>(inputs), column_scale,
-        n > 1 ? column_scale_stride : 0, dweight, n > 1 ? worker_stride : 0, outputs > 1 ? row_stride : 0);
+        partial, n * plane, cut.splits, static_cast<int>(outputs), static_cast<int>(inputs), column_scale,
+        a.column_scale_stride, dweight, n > 1 ? worker_stride : 0, outputs > 1 ? row_stride : 0);
     return status_of_launch();
 }
 

@@ -40,7 +40,7 @@ _SIGNATURES = {
     "relay_gated": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _rows_p, _vp, _vp, _vp, _vp, _vp]),
     "relay_gated_backward": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _rows_p, _vp, _vp, _vp, _vp, _rows_p, _rows_p,
                                                      _vp, _vp, _vp]),
-    "relay_weight_grad_workspace": (_i64, [_i32, _i64, _i64, _i64]),
+    "relay_weight_grad_workspace": (_i64, [_i32, _i32, _i64, _i64, _i64, _rows_p]),
     "relay_weight_grad": (ctypes.c_int, [_i32, _i32, _i64, _i64, _i64, _rows_p, _vp, _vp, _vp, _i64, _vp, _vp, _i64,
                                          _i64, _vp, _i64, _vp]),
 }
@@ -261,9 +261,18 @@ def relay_gated_backward(dout, dgate, dup, gate=None, up=None, gate_checkpoint=N
         "relay_gated_backward")
 
 
-def relay_weight_grad_workspace(n: int, tokens: int, outputs: int, inputs: int) -> int:
-    """Bytes of workspace for relay_weight_grad (may be 0)."""
-    return _bytes(_library().relay_weight_grad_workspace(n, tokens, outputs, inputs), "relay_weight_grad_workspace")
+def relay_weight_grad_workspace(n: int, tokens: int, outputs: int, inputs: int, dy=None) -> int:
+    """Bytes of workspace for relay_weight_grad: for the tensor dy, or without one enough
+    for any type and strides.  Rows that are not bf16 on 16-byte boundaries are copied
+    into it as bf16 terms; for those that are it is 0, or the split sums of few outputs."""
+    lib = _library()
+    if dy is None:
+        return _bytes(max(lib.relay_weight_grad_workspace(t, n, tokens, outputs, inputs, None)
+                          for t in (RELAY_BF16, RELAY_FP16, RELAY_FP32)), "relay_weight_grad_workspace")
+    type_, *_ = _shape_of("dy", dy)
+    return _bytes(lib.relay_weight_grad_workspace(type_, n, tokens, outputs, inputs,
+                                                  _rows("dy", dy, dy.dtype, (n, tokens, outputs))),
+                  "relay_weight_grad_workspace")
 
 
 def relay_weight_grad(dy, checkpoint, dweight, workspace, column_scale=None, lengths=None, stream=None):

@@ -369,8 +369,8 @@ def _weight_grad(dtype, layout, n, T, outputs, inputs, lengths=None, scaled=Fals
     w = _weight(seed + 3, n, inputs, 3) if scaled else None
     scale = np.ones((n, inputs)) if w is None else np64(w)
     clean = np.where(used, dy, 0)
-    want = np.einsum("nto,nti->noi", clean, xhat) * scale[:, None]
-    bound = np.einsum("nto,nti->noi", np.abs(clean), np.abs(xhat)) * np.abs(scale[:, None])
+    want = np.matmul(clean.transpose(0, 2, 1), xhat) * scale[:, None]
+    bound = np.matmul(np.abs(clean).transpose(0, 2, 1), np.abs(xhat)) * np.abs(scale[:, None])
     # products are exact; each of T additions is off by one unit of the last place of a partial sum at most
     bound = (T + 16) * 2 * U * bound + 4 * U * np.abs(want)
     flat = torch.full((n, first + outputs * (inputs + gap) + 3), 77.0, device="cuda")
@@ -409,7 +409,8 @@ def test_weight_grad_lengths(dtype, layout, T):
 
 @pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
 @pytest.mark.parametrize("n,T,outputs,inputs", [(1, 4099, 130, 257), (1, 3000, 64, 64), (3, 2500, 640, 520),
-                                                (1, 2048, 2048, 1024), (256, 5, 9, 11)])
+                                                (1, 2048, 2048, 1024), (256, 5, 9, 11), (3, 1000, 1111, 1537),
+                                                (2, 700, 4100, 2600), (40, 200, 520, 300)])
 def test_weight_grad_long_and_wide(dtype, n, T, outputs, inputs):
     _weight_grad(dtype, "dense", n, T, outputs, inputs, first=4)
 

@@ -67,8 +67,8 @@ def test_sizes_and_types(lib):
                                      None) == want
         if type_ == 0:
             assert lib.relay_rms_norm_backward_workspace(n, tokens, d) == want
-            assert lib.relay_weight_grad_workspace(n, tokens, d, 64) == want
-            assert lib.relay_weight_grad_workspace(n, tokens, 64, d) == want
+            assert lib.relay_weight_grad_workspace(2, n, tokens, d, 64, None) == want
+            assert lib.relay_weight_grad_workspace(2, n, tokens, 64, d, None) == want
     assert lib.relay_checkpoint_pitch(0) == BAD and lib.relay_checkpoint_pitch(1) == 128
     assert lib.relay_checkpoint_pitch(128) == 128 and lib.relay_checkpoint_pitch(129) == 256
     wide = _r(A, 0, 40000)
@@ -152,15 +152,20 @@ def test_gated_refusals(lib):
 
 
 def test_weight_grad_refusals(lib):
-    need = lib.relay_weight_grad_workspace(2, 10, 48, 64)
-    assert need >= 0
+    need = lib.relay_weight_grad_workspace(0, 2, 10, 48, 64, _r(A + 2, 480, 48))
+    assert need == 2 * 2 * 10 * 48  # unaligned: copied
+    assert lib.relay_weight_grad_workspace(0, 2, 10, 48, 64, _r(A, 480, 48)) == 0
+    assert lib.relay_weight_grad_workspace(0, 2, 10, 48, 64, None) == need
+    assert lib.relay_weight_grad_workspace(2, 2, 10, 48, 64, None) == 3 * need
+    assert lib.relay_weight_grad_workspace(0, 2, 10, 48, 64, _r(A, 480, 0)) == need  # one row, repeated
 
-    def call(dy=_r(A, 480, 48), q=B, c=C, scale=None, ss=0, lengths=None, dw=D, ws=48 * 64, row=64, work=E, size=need):
+    def call(dy=_r(A + 2, 480, 48), q=B, c=C, scale=None, ss=0, lengths=None, dw=D, ws=48 * 64, row=64, work=E,
+             size=need):
         return lib.relay_weight_grad(0, 2, 10, 48, 64, dy, q, c, scale, ss, lengths, dw, ws, row, work, size, None)
 
     for kw in (dict(dy=None), dict(q=None), dict(c=None), dict(q=B + 8), dict(scale=A + 1), dict(scale=A, ss=-1),
                dict(lengths=A + 2), dict(dw=None), dict(dw=D + 2), dict(ws=48 * 64 - 1), dict(row=63), dict(row=-1),
-               dict(size=need - 1)):
+               dict(size=need - 1), dict(work=None), dict(work=E + 8)):
         assert call(**kw) == BAD, kw
 
 
