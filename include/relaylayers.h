@@ -47,7 +47,7 @@
  *     (n < 1, tokens < 0, d < 1, overlapping output rows), an address that
  *     is not a multiple of its element's size, checkpoint or workspace
  *     addresses that are not multiples of 16, a workspace too small.
- *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N, n tokens >= 2^31, d > 2^24, in
+ *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N, n tokens >= 2^30, d > 2^24, in
  *     the norm d > RELAY_NORM_MAX_D, in the weight gradient inputs >
  *     RELAY_WEIGHT_GRAD_MAX_INPUTS.
  *

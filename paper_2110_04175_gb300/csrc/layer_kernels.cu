@@ -23,17 +23,26 @@ struct Grid {
     int32_t tokens;
     int32_t strips;  // of a row
     int32_t d, pitch;
+    // what the whole grid's warps step over together, in workers, tokens and strips
+    int32_t step_worker, step_token, step_strip;
 };
 
-// Calls f(row, worker, token, first feature) for this warp's strips.
+// Calls f(row, worker, token, first feature) for this warp's strips: every
+// (gridDim.x kWarps)-th one, found without a division past the first.
 template <typename F>
 __device__ __forceinline__ void each_strip(const Grid& g, F f) {
-    const int64_t all = g.rows * g.strips, step = static_cast<int64_t>(gridDim.x) * kWarps;
-    for (int64_t s = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32; s < all; s += step) {
-        const int64_t row = s / g.strips;
-        const int worker = static_cast<int>(row / g.tokens);
-        f(row, worker, static_cast<int>(row - static_cast<int64_t>(worker) * g.tokens),
-          static_cast<int>(s - row * g.strips) * kStrip);
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
+    int64_t row = first / g.strips;
+    int strip = static_cast<int>(first - row * g.strips), worker = static_cast<int>(row / g.tokens);
+    int token = static_cast<int>(row - static_cast<int64_t>(worker) * g.tokens);
+    while (row < g.rows) {
+        f(row, worker, token, strip * kStrip);
+        strip += g.step_strip;
+        token += g.step_token;
+        worker += g.step_worker;
+        if (strip >= g.strips) strip -= g.strips, ++token;
+        if (token >= g.tokens) token -= g.tokens, ++worker;
+        row = static_cast<int64_t>(worker) * g.tokens + token;
     }
 }
 
@@ -68,11 +77,21 @@ relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scale
 }
 
 // sigma(g) and 1 - sigma(g) without cancellation: with e = exp(-|g|) they are
-// 1 / (1 + e) and e / (1 + e), in the order that the sign of g gives.
+// 1 / (1 + e) and e / (1 + e), in the order that the sign of g gives.  Rows of 16 bits
+// take the hardware's exponential and reciprocal, which are off by less than
+// (2 + |g|) 2^-23 relative, far below their rounding; fp32 rows take the exact ones.
+template <typename T>
 struct Sigmoid {
     float at, rest;
     __device__ __forceinline__ explicit Sigmoid(float g) {
-        const float e = expf(-fabsf(g)), r = 1.0f / (1.0f + e);
+        float e, r;
+        if constexpr (sizeof(T) == 2) {
+            e = __expf(-fabsf(g));
+            r = __fdividef(1.0f, 1.0f + e);
+        } else {
+            e = expf(-fabsf(g));
+            r = 1.0f / (1.0f + e);
+        }
         at = g < 0.0f ? e * r : r;
         rest = g < 0.0f ? r : e * r;
     }
@@ -91,7 +110,7 @@ relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, in
         if (gate_codes != nullptr) put_strip<kVec>(gate_codes + at, gate_scales + scale_at, base, lane, g.pitch, a);
         if (up_codes != nullptr) put_strip<kVec>(up_codes + at, up_scales + scale_at, base, lane, g.pitch, b);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid(a[k]).at * b[k];
+        for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid<T>(a[k]).at * b[k];
         store_strip<kVec>(out.row(worker, token) + base, lane, g.d - base, a);
     });
 }
@@ -121,7 +140,7 @@ relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View
         float dg[8], du[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const Sigmoid s(a[k]);
+            const Sigmoid<T> s(a[k]);
             const float silu = a[k] * s.at;
             dg[k] = da[k] * b[k] * s.at * (1.0f + a[k] * s.rest);
             du[k] = da[k] * silu;
@@ -236,60 +255,122 @@ struct NormBackwardArgs {
 };
 
 // CTA (p, i) takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i and
-// leaves their sum of dy xhat in its row of `partial`.
+// leaves their sum of dy xhat in its row of `partial`.  The next row is asked for
+// before this one's sum over the CTA, and the weight stays in registers; rows of more
+// than 8192 features, and unaligned ones, leave no room for that (kLean), and the
+// widest are read twice (kTwice), the second time from the caches.
 template <typename T, bool kVec, int kParts, int kStrips, bool kEight>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
+    constexpr bool kLean = kStrips > 2 || !kVec, kTwice = kParts > 16;
     __shared__ float shared[kNormWarps<kParts>];
     extern __shared__ float sums[];  // kRows > 1: [kRows - 1][kStrips][kParts][256]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
     const int worker = blockIdx.y;
     const int length = a.lengths == nullptr ? a.tokens : min(max(a.lengths[worker], 0), a.tokens);
     const float* weight = a.weight + worker * a.weight_stride;
-    float dw[kStrips][8] = {};
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.tokens;
-         first += static_cast<int64_t>(gridDim.x) * kRows) {
-        const int token = static_cast<int>(first) + slot;
+    const auto base_of = [&](int j) { return (part + kParts * j) * kStrip; };
+
+    struct Row {  // what a lane needs of a row, as it lies in memory
+        Piece<T, kVec> dy[kStrips], total[kEight ? 1 : kStrips], dtotal[kLean ? 1 : kStrips];
+        CodePiece<kVec> codes[kEight ? kStrips : 1];
+        float rstd;
+    };
+    const auto ask_strip = [&](Row& r, int token, int j, int to) {
         const bool on = token < length;
+        const int base = base_of(j), left = on ? a.d - base : 0;
         const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
-        const float rstd = on ? a.rstd[row] : 0.0f;
-        float dy[kStrips][8], xhat[kStrips][8];
+        r.dy[to].load(a.dy.row(worker, token) + base, lane, left);
+        if constexpr (kEight)
+            r.codes[to].load(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, on ? a.pitch : 0);
+        else
+            r.total[to].load(a.total.row(worker, token) + base, lane, left);
+    };
+    const auto ask = [&](Row& r, int token) {
+        r.rstd = token < length ? a.rstd[static_cast<int64_t>(worker) * a.tokens + token] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < kStrips; ++j) {
+            ask_strip(r, token, j, j);
+            if constexpr (!kLean)
+                if (a.dtotal.p != nullptr)
+                    r.dtotal[j].load(a.dtotal.row(worker, token) + base_of(j), lane, token < length ? a.d - base_of(j) : 0);
+        }
+    };
+    // dy and xhat of strip j, from `from` of the row
+    const auto widen_strip = [&](const Row& r, int token, int j, int from, float (&dy)[8], float (&xhat)[8]) {
+        r.dy[from].get(dy);
+        if constexpr (kEight) {
+            r.codes[from].get(xhat);
+            const int left = token < length ? a.d - base_of(j) : 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (feature<kVec>(lane, k) >= left) xhat[k] = 0.0f;  // a NaN block's features past d
+        } else {
+            r.total[from].get(xhat);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) xhat[k] *= r.rstd;
+        }
+    };
+
+    float w[kLean ? 1 : kStrips][8];
+    if constexpr (!kLean) {
+#pragma unroll
+        for (int j = 0; j < kStrips; ++j) load_weight<kVec>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[j]);
+    }
+    float dw[kStrips][8] = {};
+    const int step = static_cast<int>(gridDim.x) * kRows;
+    Row next;
+    int first = static_cast<int>(blockIdx.x) * kRows;
+    if (!kTwice && !kLean) ask(next, first + slot);
+    for (; first < a.tokens; first += step) {
+        const int token = first + slot;
+        Row r;
+        if (kTwice)
+            r.rstd = token < length ? a.rstd[static_cast<int64_t>(worker) * a.tokens + token] : 0.0f;
+        else if (kLean)
+            ask(r, token);
+        else
+            r = next;
+        float u[kTwice ? 1 : kStrips][8], xhat[kTwice ? 1 : kStrips][8];
         float along = 0.0f;
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
-            const int base = (part + kParts * j) * kStrip, left = on ? a.d - base : 0;
-            load_strip<kVec>(a.dy.row(worker, token) + base, lane, left, dy[j]);
-            if (kEight) {
-                get_strip<kVec>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane,
-                                on ? a.pitch : 0, xhat[j]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (feature<kVec>(lane, k) >= left) xhat[j][k] = 0.0f;  // a NaN block's features past d
-            } else {
-                load_strip<kVec>(a.total.row(worker, token) + base, lane, left, xhat[j]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) xhat[j][k] *= rstd;
-            }
-            float w[8];
-            load_weight<kVec>(weight + base, lane, left, a.weight_quads, w);
+            const int at = kTwice ? 0 : j;
+            if (kTwice) ask_strip(r, token, j, 0);
+            widen_strip(r, token, j, at, u[at], xhat[at]);
+            float m[8];
+            if constexpr (kLean) load_weight<kVec>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                dw[j][k] = fmaf(dy[j][k], xhat[j][k], dw[j][k]);
-                dy[j][k] *= w[k];
-                along = fmaf(dy[j][k], xhat[j][k], along);
+                dw[j][k] = fmaf(u[at][k], xhat[at][k], dw[j][k]);
+                u[at][k] *= kLean ? m[k] : w[kLean ? 0 : j][k];
+                along = fmaf(u[at][k], xhat[at][k], along);
             }
         }
+        if (!kTwice && !kLean && first + step < a.tokens) ask(next, first + step + slot);
         along = row_sum<kParts>(along, shared, slot, part) / static_cast<float>(a.d);
-        if (token >= a.tokens) continue;
+        if (token < a.tokens) {
 #pragma unroll
-        for (int j = 0; j < kStrips; ++j) {
-            const int base = (part + kParts * j) * kStrip, left = a.d - base;
-            if (left <= 0) break;
-            float dh[8] = {};
-            if (a.dtotal.p != nullptr) load_strip<kVec>(a.dtotal.row(worker, token) + base, lane, on ? left : 0, dh);
+            for (int j = 0; j < kStrips; ++j) {
+                const int base = base_of(j), left = a.d - base, at = kTwice ? 0 : j;
+                if (left <= 0) break;
+                if constexpr (kTwice) {
+                    ask_strip(r, token, j, 0);
+                    widen_strip(r, token, j, 0, u[0], xhat[0]);
+                    float m[8];
+                    load_weight<kVec>(weight + base, lane, left, a.weight_quads, m);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) dh[k] = fmaf(rstd, dy[j][k] - xhat[j][k] * along, dh[k]);
-            store_strip<kVec>(a.dx.row(worker, token) + base, lane, left, dh);
+                    for (int k = 0; k < 8; ++k) u[0][k] *= m[k];
+                }
+                float dh[8] = {};
+                if (a.dtotal.p != nullptr) {
+                    if constexpr (kLean) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, token < length ? left : 0);
+                    r.dtotal[kLean ? 0 : j].get(dh);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) dh[k] = fmaf(r.rstd, u[at][k] - xhat[at][k] * along, dh[k]);
+                store_strip<kVec>(a.dx.row(worker, token) + base, lane, left, dh);
+            }
         }
     }
     if (kRows > 1) {  // the rows that went side by side, in their order
@@ -338,15 +419,21 @@ relay_norm_join_kernel(const float* partial, int parts, int d, float* dweight, i
 
 // ---------------------------------------------------------------- launching
 
-Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint) {
-    const int64_t pitch = pitch_of(d), width = checkpoint ? pitch : d;
-    return Grid{n * tokens, static_cast<int32_t>(tokens), static_cast<int32_t>((width + kStrip - 1) / kStrip),
-                static_cast<int32_t>(d), static_cast<int32_t>(pitch)};
-}
-
-int elementwise_ctas(const Grid& g) {
-    const int64_t want = (g.rows * g.strips + kWarps - 1) / kWarps, most = int64_t(32) * sm_count();
-    return static_cast<int>(want < most ? want : most);  // 0: no device
+// The strips of an activation (with its checkpoint's padding), and the CTAs that take
+// them: 0 where there is no device.
+Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint, int* ctas) {
+    const int64_t pitch = pitch_of(d), strips = ((checkpoint ? pitch : d) + kStrip - 1) / kStrip, rows = n * tokens;
+    const int64_t want = (rows * strips + kWarps - 1) / kWarps, most = int64_t(32) * sm_count();
+    *ctas = static_cast<int>(want < most ? want : most);
+    const int64_t step = int64_t(*ctas) * kWarps, step_rows = step / strips;
+    return Grid{rows,
+                static_cast<int32_t>(tokens),
+                static_cast<int32_t>(strips),
+                static_cast<int32_t>(d),
+                static_cast<int32_t>(pitch),
+                static_cast<int32_t>(step_rows / tokens),
+                static_cast<int32_t>(step_rows % tokens),
+                static_cast<int32_t>(step % strips)};
 }
 
 // Calls f(kParts, kStrips) as constants for the smallest instance that holds a row.
@@ -369,7 +456,7 @@ int by_width(int64_t pitch, F f) {
 // Rows of partial sums per worker in the norm's backward pass: about two CTAs per
 // SM over all workers, no more than there are tokens.
 int64_t norm_partials(int32_t n, int64_t tokens) {
-    const int64_t want = (304 + n - 1) / n;
+    const int64_t want = 304 / n > 0 ? 304 / n : 1;
     return tokens < want ? (tokens > 0 ? tokens : 1) : want;
 }
 
@@ -384,8 +471,8 @@ int relay_checkpoint_pack(int32_t type, int32_t n, int64_t tokens, int64_t d, co
     if (const int rc = check_shape(type, n, tokens, d)) return rc;
     if (!rows_fit(x, type, n, tokens, d, false) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
     if (tokens == 0) return RELAY_OK;
-    const Grid g = make_grid(n, tokens, d, true);
-    const int ctas = elementwise_ctas(g);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, true, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(x, type, n, tokens);
     return by_type(type, [&](auto t) {
@@ -401,8 +488,8 @@ int relay_checkpoint_unpack(int32_t type, int32_t n, int64_t tokens, int64_t d, 
     if (const int rc = check_shape(type, n, tokens, d)) return rc;
     if (!rows_fit(out, type, n, tokens, d, true) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
     if (tokens == 0) return RELAY_OK;
-    const Grid g = make_grid(n, tokens, d, false);
-    const int ctas = elementwise_ctas(g);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, false, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(out, type, n, tokens);
     return by_type(type, [&](auto t) {
@@ -520,8 +607,8 @@ int relay_gated(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_
     if (gate_codes != nullptr && (gate_codes == up_codes || gate_scales == up_scales)) return RELAY_EINVAL;
     if (tokens == 0) return RELAY_OK;
     if (out->data == gate->data || out->data == up->data) return RELAY_EINVAL;
-    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr);
-    const int ctas = elementwise_ctas(g);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(gate, type, n, tokens) && vectors(up, type, n, tokens) &&
                      vectors(out, type, n, tokens);
@@ -556,8 +643,8 @@ int relay_gated_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, con
     for (const relay_rows* o : {dgate, dup})
         if (o->data == dout->data || (!eight && (o->data == gate->data || o->data == up->data))) return RELAY_EINVAL;
     if (dgate->data == dup->data) return RELAY_EINVAL;
-    const Grid g = make_grid(n, tokens, d, out_codes != nullptr);
-    const int ctas = elementwise_ctas(g);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, out_codes != nullptr, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(dout, type, n, tokens) && vectors(dgate, type, n, tokens) &&
                      vectors(dup, type, n, tokens) && vectors(eight ? nullptr : gate, type, n, tokens) &&

@@ -17,7 +17,7 @@ namespace {
 constexpr int kStrip = 256;     // features that a warp handles together: 8 per lane
 constexpr int kBlock = 32;      // features that share a scale
 constexpr int kPitch = 128;     // checkpoint rows are whole multiples of this
-constexpr int64_t kMaxD = int64_t(1) << 24;
+constexpr int64_t kMaxD = int64_t(1) << 24, kMaxRows = int64_t(1) << 30;
 
 // -------------------------------------------------------------------- types
 
@@ -53,22 +53,45 @@ struct View {
 template <bool kVec>
 __device__ __forceinline__ int feature(int lane, int k) { return kVec ? 8 * lane + k : 32 * k + lane; }
 
-template <bool kVec, typename T>
-__device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8]) {
-    if constexpr (kVec) {
-        constexpr int kPer = 16 / sizeof(T);
+// A lane's 8 features as they lie in memory, so that they can be asked for long before
+// they are used.
+template <typename T, bool kVec>
+struct Piece {
+    T e[8];
+    __device__ __forceinline__ void load(const T* p, int lane, int left) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = 32 * k + lane < left ? p[32 * k + lane] : T(0.0f);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = widen(e[k]);
+    }
+};
+template <typename T>
+struct Piece<T, true> {
+    static constexpr int kPer = 16 / sizeof(T);
+    uint4 w[8 / kPer];
+    __device__ __forceinline__ void load(const T* p, int lane, int left) {
+#pragma unroll
+        for (int h = 0; h < 8 / kPer; ++h)
+            w[h] = 8 * lane < left ? *reinterpret_cast<const uint4*>(p + 8 * lane + h * kPer)
+                                   : make_uint4(0, 0, 0, 0);  // +0 in every type
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
         for (int h = 0; h < 8 / kPer; ++h) {
-            uint4 w = make_uint4(0, 0, 0, 0);  // +0 in every type
-            if (8 * lane < left) w = *reinterpret_cast<const uint4*>(p + 8 * lane + h * kPer);
-            const T* e = reinterpret_cast<const T*>(&w);
+            const T* e = reinterpret_cast<const T*>(&w[h]);
 #pragma unroll
             for (int k = 0; k < kPer; ++k) v[h * kPer + k] = widen(e[k]);
         }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = 32 * k + lane < left ? widen(p[32 * k + lane]) : 0.0f;
     }
+};
+
+template <bool kVec, typename T>
+__device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8]) {
+    Piece<T, kVec> piece;
+    piece.load(p, lane, left);
+    piece.get(v);
 }
 
 template <bool kVec, typename T>
@@ -167,26 +190,52 @@ __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int ba
     }
 }
 
+// A lane's 8 codes and their scales as they lie in memory.
+template <bool kVec>
+struct CodePiece {
+    int8_t q[8];
+    uint8_t c[8];
+    __device__ __forceinline__ void load(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            q[k] = 0;
+            c[k] = 7;
+            if (base + 32 * k < pitch) {
+                q[k] = codes[base + 32 * k + lane];
+                c[k] = scales[base / kBlock + k];
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(q[k]) * scale_unit(c[k]);
+    }
+};
+template <>
+struct CodePiece<true> {
+    uint2 q;
+    uint32_t c;
+    __device__ __forceinline__ void load(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch) {
+        q = make_uint2(0, 0);
+        c = 7;
+        if (base + 8 * lane < pitch) {
+            q = *reinterpret_cast<const uint2*>(codes + base + 8 * lane);
+            c = scales[base / kBlock + lane / 4];
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const float unit = scale_unit(c);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = code_value(k < 4 ? q.x : q.y, k % 4) * unit;
+    }
+};
+
 template <bool kVec>
 __device__ __forceinline__ void get_strip(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch,
                                           float (&v)[8]) {
-    if constexpr (kVec) {
-        uint2 w = make_uint2(0, 0);
-        float unit = 0.0f;
-        if (base + 8 * lane < pitch) {
-            w = *reinterpret_cast<const uint2*>(codes + base + 8 * lane);
-            unit = scale_unit(scales[base / kBlock + lane / 4]);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = code_value(k < 4 ? w.x : w.y, k % 4) * unit;
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            v[k] = 0.0f;
-            if (base + 32 * k < pitch)
-                v[k] = static_cast<float>(codes[base + 32 * k + lane]) * scale_unit(scales[base / kBlock + k]);
-        }
-    }
+    CodePiece<kVec> piece;
+    piece.load(codes, scales, base, lane, pitch);
+    piece.get(v);
 }
 
 // ----------------------------------------------------------- argument checks
@@ -198,8 +247,7 @@ inline bool aligned(const void* p, int64_t to) { return reinterpret_cast<uintptr
 // RELAY_OK or why (n, tokens, d) and the type are refused.
 inline int check_shape(int32_t type, int32_t n, int64_t tokens, int64_t d) {
     if (type < RELAY_BF16 || type > RELAY_FP32 || n < 1 || tokens < 0 || d < 1) return RELAY_EINVAL;
-    if (n > RELAY_MAX_N || tokens * n >= (int64_t(1) << 31) || tokens >= (int64_t(1) << 31) || d > kMaxD)
-        return RELAY_EUNSUPPORTED;
+    if (n > RELAY_MAX_N || tokens >= kMaxRows || tokens * n >= kMaxRows || d > kMaxD) return RELAY_EUNSUPPORTED;
     return RELAY_OK;
 }
 

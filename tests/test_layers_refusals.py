@@ -25,7 +25,7 @@ def lib():
 
 
 def _r(data, ws, ts):
-    return layers._Rows(data, ws, ts)
+    return layers._pack_rows(data or 0, ws, ts)
 
 
 def test_header_and_library_agree(lib):
@@ -55,7 +55,7 @@ def test_sizes_and_types(lib):
     rows = _r(A, 640, 64)
     for type_, n, tokens, d, want in [(3, 1, 10, 64, BAD), (-1, 1, 10, 64, BAD), (0, 0, 10, 64, BAD),
                                       (0, 1, -1, 64, BAD), (0, 1, 10, 0, BAD), (0, 257, 1, 64, BIG),
-                                      (0, 1, 1 << 31, 64, BIG), (0, 16, 1 << 27, 64, BIG),
+                                      (0, 1, 1 << 30, 64, BIG), (0, 16, 1 << 26, 64, BIG),
                                       (0, 1, 1, (1 << 24) + 1, BIG), (0, 1, 1 << 62, 64, BIG)]:
         assert lib.relay_checkpoint_pack(type_, n, tokens, d, rows, B, C, None) == want
         assert lib.relay_gated(type_, n, tokens, d, rows, rows, _r(B, 640, 64), None, None, None, None, None) == want
