@@ -18,29 +18,42 @@ int by_type(int32_t type, F f) {
 
 constexpr int kWarps = 8;  // of an element-wise CTA
 
+// A warp takes this many strips of a row at a time, all of them asked for first.
+template <bool kVec>
+constexpr int kRun = kVec ? 2 : 1;
+
+// largest() where put_strip wants it.
+template <bool kVec, typename T>
+__device__ __forceinline__ uint32_t most_of(const Piece<T, kVec>& p) {
+    if constexpr (kVec)
+        return largest(p);
+    else
+        return 0u;
+}
+
 struct Grid {
     int64_t rows;    // n tokens
     int32_t tokens;
-    int32_t strips;  // of a row
+    int32_t runs;    // of a row
     int32_t d, pitch;
-    // what the whole grid's warps step over together, in workers, tokens and strips
-    int32_t step_worker, step_token, step_strip;
+    // what the whole grid's warps step over together, in workers, tokens and runs
+    int32_t step_worker, step_token, step_run;
 };
 
-// Calls f(row, worker, token, first feature) for this warp's strips: every
+// Calls f(row, worker, token, first feature) for this warp's runs of strips: every
 // (gridDim.x kWarps)-th one, found without a division past the first.
-template <typename F>
-__device__ __forceinline__ void each_strip(const Grid& g, F f) {
+template <bool kVec, typename F>
+__device__ __forceinline__ void each_run(const Grid& g, F f) {
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
-    int64_t row = first / g.strips;
-    int strip = static_cast<int>(first - row * g.strips), worker = static_cast<int>(row / g.tokens);
+    int64_t row = first / g.runs;
+    int run = static_cast<int>(first - row * g.runs), worker = static_cast<int>(row / g.tokens);
     int token = static_cast<int>(row - static_cast<int64_t>(worker) * g.tokens);
     while (row < g.rows) {
-        f(row, worker, token, strip * kStrip);
-        strip += g.step_strip;
+        f(row, worker, token, run * (kRun<kVec> * kStrip));
+        run += g.step_run;
         token += g.step_token;
         worker += g.step_worker;
-        if (strip >= g.strips) strip -= g.strips, ++token;
+        if (run >= g.runs) run -= g.runs, ++token;
         if (token >= g.tokens) token -= g.tokens, ++worker;
         row = static_cast<int64_t>(worker) * g.tokens + token;
     }
@@ -50,10 +63,18 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_pack_kernel(Grid g, View<const T> x, int8_t* codes, uint8_t* scales) {
     const int lane = threadIdx.x % 32;
-    each_strip(g, [&](int64_t row, int worker, int token, int base) {
-        float v[8];
-        load_strip<kVec>(x.row(worker, token) + base, lane, g.d - base, v);
-        put_strip<kVec>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base, lane, g.pitch, v);
+    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
+        Piece<T, kVec> p[kRun<kVec>];
+        const T* from = x.row(worker, token) + base;
+#pragma unroll
+        for (int j = 0; j < kRun<kVec>; ++j) p[j].load(from + j * kStrip, lane, g.d - base - j * kStrip);
+#pragma unroll
+        for (int j = 0; j < kRun<kVec>; ++j) {
+            float v[8];
+            p[j].get(v);
+            put_strip<kVec>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch, v,
+                            most_of<kVec>(p[j]));
+        }
     });
 }
 
@@ -67,33 +88,42 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scales, View<T> out) {
     const int lane = threadIdx.x % 32;
-    each_strip(g, [&](int64_t row, int worker, int token, int base) {
-        float v[8];
-        get_strip<kVec>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base, lane, g.pitch, v);
+    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
+        CodePiece<kVec> p[kRun<kVec>];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = within<T>(v[k]);
-        store_strip<kVec>(out.row(worker, token) + base, lane, g.d - base, v);
+        for (int j = 0; j < kRun<kVec>; ++j)
+            p[j].load(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch);
+        T* to = out.row(worker, token) + base;
+#pragma unroll
+        for (int j = 0; j < kRun<kVec>; ++j) {
+            float v[8];
+            p[j].get(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = within<T>(v[k]);
+            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, v);
+        }
     });
 }
 
-// sigma(g) and 1 - sigma(g) without cancellation: with e = exp(-|g|) they are
-// 1 / (1 + e) and e / (1 + e), in the order that the sign of g gives.  Rows of 16 bits
-// take the hardware's exponential and reciprocal, which are off by less than
-// (2 + |g|) 2^-23 relative, far below their rounding; fp32 rows take the exact ones.
+// sigma(g) and 1 - sigma(g) without cancellation.  Rows of 16 bits take the hardware's
+// exponential and reciprocal: with e = exp(-g) they are 1 / (1 + e) and e / (1 + e),
+// off by less than (3 + 2 |g|) 2^-23 relative, far below the rows' rounding; e is held
+// at 2^126, where sigma(g) is 2^-126, so that neither turns into 0 times infinity.  fp32
+// rows take the exact ones, of exp(-|g|), in the order that the sign of g gives.
 template <typename T>
 struct Sigmoid {
     float at, rest;
     __device__ __forceinline__ explicit Sigmoid(float g) {
-        float e, r;
         if constexpr (sizeof(T) == 2) {
-            e = __expf(-fabsf(g));
-            r = __fdividef(1.0f, 1.0f + e);
+            float e;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(g * -1.44269504f, 126.0f)));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(at) : "f"(1.0f + e));
+            rest = e * at;
         } else {
-            e = expf(-fabsf(g));
-            r = 1.0f / (1.0f + e);
+            const float e = expf(-fabsf(g)), r = 1.0f / (1.0f + e);
+            at = g < 0.0f ? e * r : r;
+            rest = g < 0.0f ? r : e * r;
         }
-        at = g < 0.0f ? e * r : r;
-        rest = g < 0.0f ? r : e * r;
     }
 };
 
@@ -102,16 +132,29 @@ __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, int8_t* gate_codes,
                    uint8_t* gate_scales, int8_t* up_codes, uint8_t* up_scales) {
     const int lane = threadIdx.x % 32;
-    each_strip(g, [&](int64_t row, int worker, int token, int base) {
-        float a[8], b[8];
-        load_strip<kVec>(gate.row(worker, token) + base, lane, g.d - base, a);
-        load_strip<kVec>(up.row(worker, token) + base, lane, g.d - base, b);
-        const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
-        if (gate_codes != nullptr) put_strip<kVec>(gate_codes + at, gate_scales + scale_at, base, lane, g.pitch, a);
-        if (up_codes != nullptr) put_strip<kVec>(up_codes + at, up_scales + scale_at, base, lane, g.pitch, b);
+    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
+        Piece<T, kVec> p[kRun<kVec>], q[kRun<kVec>];
+        const T *from = gate.row(worker, token) + base, *from_up = up.row(worker, token) + base;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid<T>(a[k]).at * b[k];
-        store_strip<kVec>(out.row(worker, token) + base, lane, g.d - base, a);
+        for (int j = 0; j < kRun<kVec>; ++j) {
+            p[j].load(from + j * kStrip, lane, g.d - base - j * kStrip);
+            q[j].load(from_up + j * kStrip, lane, g.d - base - j * kStrip);
+        }
+        const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
+        T* to = out.row(worker, token) + base;
+#pragma unroll
+        for (int j = 0; j < kRun<kVec>; ++j) {
+            float a[8], b[8];
+            p[j].get(a);
+            q[j].get(b);
+            if (gate_codes != nullptr)
+                put_strip<kVec>(gate_codes + at, gate_scales + scale_at, base + j * kStrip, lane, g.pitch, a, most_of<kVec>(p[j]));
+            if (up_codes != nullptr)
+                put_strip<kVec>(up_codes + at, up_scales + scale_at, base + j * kStrip, lane, g.pitch, b, most_of<kVec>(q[j]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid<T>(a[k]).at * b[k];
+            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, a);
+        }
     });
 }
 
@@ -124,36 +167,55 @@ template <typename T, bool kVec, bool kEight>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View<const T> up, GatedSource from,
                             View<T> dgate, View<T> dup, int8_t* out_codes, uint8_t* out_scales) {
+    constexpr int kR = kRun<kVec>;
     const int lane = threadIdx.x % 32;
-    each_strip(g, [&](int64_t row, int worker, int token, int base) {
-        const int left = g.d - base;
+    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
         const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
-        float da[8], a[8], b[8];
-        load_strip<kVec>(dout.row(worker, token) + base, lane, left, da);
-        if (kEight) {
-            get_strip<kVec>(from.gate_codes + at, from.gate_scales + scale_at, base, lane, g.pitch, a);
-            get_strip<kVec>(from.up_codes + at, from.up_scales + scale_at, base, lane, g.pitch, b);
-        } else {
-            load_strip<kVec>(gate.row(worker, token) + base, lane, left, a);
-            load_strip<kVec>(up.row(worker, token) + base, lane, left, b);
-        }
-        float dg[8], du[8];
+        Piece<T, kVec> p[kR], gp[kEight ? 1 : kR], up_p[kEight ? 1 : kR];
+        CodePiece<kVec> gq[kEight ? kR : 1], uq[kEight ? kR : 1];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const Sigmoid<T> s(a[k]);
-            const float silu = a[k] * s.at;
-            dg[k] = da[k] * b[k] * s.at * (1.0f + a[k] * s.rest);
-            du[k] = da[k] * silu;
-            a[k] = silu * b[k];
+        for (int j = 0; j < kR; ++j) {
+            const int first = base + j * kStrip;
+            p[j].load(dout.row(worker, token) + first, lane, g.d - first);
+            if constexpr (kEight) {
+                gq[j].load(from.gate_codes + at, from.gate_scales + scale_at, first, lane, g.pitch);
+                uq[j].load(from.up_codes + at, from.up_scales + scale_at, first, lane, g.pitch);
+            } else {
+                gp[j].load(gate.row(worker, token) + first, lane, g.d - first);
+                up_p[j].load(up.row(worker, token) + first, lane, g.d - first);
+            }
         }
-        store_strip<kVec>(dgate.row(worker, token) + base, lane, left, dg);
-        store_strip<kVec>(dup.row(worker, token) + base, lane, left, du);
-        if (out_codes != nullptr) {
-            // a block that reads as NaN does so past d too: those stay 0
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (feature<kVec>(lane, k) >= left) a[k] = 0.0f;
-            put_strip<kVec>(out_codes + at, out_scales + scale_at, base, lane, g.pitch, a);
+        for (int j = 0; j < kR; ++j) {
+            const int first = base + j * kStrip, left = g.d - first;
+            float da[8], a[8], b[8], dg[8];
+            p[j].get(da);
+            if constexpr (kEight) {
+                gq[j].get(a);
+                uq[j].get(b);
+            } else {
+                gp[j].get(a);
+                up_p[j].get(b);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const Sigmoid<T> s(a[k]);
+                const float silu = a[k] * s.at;
+                dg[k] = da[k] * b[k] * s.at * fmaf(a[k], s.rest, 1.0f);
+                da[k] *= silu;
+                a[k] = silu * b[k];
+            }
+            store_strip<kVec>(dgate.row(worker, token) + first, lane, left, dg);
+            store_strip<kVec>(dup.row(worker, token) + first, lane, left, da);
+            if (out_codes != nullptr) {
+                // a block that reads as NaN does so past d too: those stay 0
+                if (left < kStrip) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (feature<kVec>(lane, k) >= left) a[k] = 0.0f;
+                }
+                put_strip<kVec>(out_codes + at, out_scales + scale_at, first, lane, g.pitch, a);
+            }
         }
     });
 }
@@ -419,21 +481,22 @@ relay_norm_join_kernel(const float* partial, int parts, int d, float* dweight, i
 
 // ---------------------------------------------------------------- launching
 
-// The strips of an activation (with its checkpoint's padding), and the CTAs that take
+// The runs of an activation (with its checkpoint's padding), and the CTAs that take
 // them: 0 where there is no device.
-Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint, int* ctas) {
-    const int64_t pitch = pitch_of(d), strips = ((checkpoint ? pitch : d) + kStrip - 1) / kStrip, rows = n * tokens;
-    const int64_t want = (rows * strips + kWarps - 1) / kWarps, most = int64_t(32) * sm_count();
+Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint, bool vec, int* ctas) {
+    const int64_t run = kStrip * (vec ? kRun<true> : kRun<false>);
+    const int64_t pitch = pitch_of(d), runs = ((checkpoint ? pitch : d) + run - 1) / run, rows = n * tokens;
+    const int64_t want = (rows * runs + kWarps - 1) / kWarps, most = int64_t(32) * sm_count();
     *ctas = static_cast<int>(want < most ? want : most);
-    const int64_t step = int64_t(*ctas) * kWarps, step_rows = step / strips;
+    const int64_t step = int64_t(*ctas) * kWarps, step_rows = step / runs;
     return Grid{rows,
                 static_cast<int32_t>(tokens),
-                static_cast<int32_t>(strips),
+                static_cast<int32_t>(runs),
                 static_cast<int32_t>(d),
                 static_cast<int32_t>(pitch),
                 static_cast<int32_t>(step_rows / tokens),
                 static_cast<int32_t>(step_rows % tokens),
-                static_cast<int32_t>(step % strips)};
+                static_cast<int32_t>(step % runs)};
 }
 
 // Calls f(kParts, kStrips) as constants for the smallest instance that holds a row.
@@ -471,10 +534,10 @@ int relay_checkpoint_pack(int32_t type, int32_t n, int64_t tokens, int64_t d, co
     if (const int rc = check_shape(type, n, tokens, d)) return rc;
     if (!rows_fit(x, type, n, tokens, d, false) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
     if (tokens == 0) return RELAY_OK;
-    int ctas;
-    const Grid g = make_grid(n, tokens, d, true, &ctas);
-    if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(x, type, n, tokens);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, true, vec, &ctas);
+    if (ctas == 0) return RELAY_ECUDA;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         (vec ? relay_checkpoint_pack_kernel<T, true> : relay_checkpoint_pack_kernel<T, false>)
@@ -488,10 +551,10 @@ int relay_checkpoint_unpack(int32_t type, int32_t n, int64_t tokens, int64_t d, 
     if (const int rc = check_shape(type, n, tokens, d)) return rc;
     if (!rows_fit(out, type, n, tokens, d, true) || !checkpoint_fits(codes, scales, tokens)) return RELAY_EINVAL;
     if (tokens == 0) return RELAY_OK;
-    int ctas;
-    const Grid g = make_grid(n, tokens, d, false, &ctas);
-    if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(out, type, n, tokens);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, false, vec, &ctas);
+    if (ctas == 0) return RELAY_ECUDA;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         (vec ? relay_checkpoint_unpack_kernel<T, true> : relay_checkpoint_unpack_kernel<T, false>)
@@ -607,11 +670,11 @@ int relay_gated(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_
     if (gate_codes != nullptr && (gate_codes == up_codes || gate_scales == up_scales)) return RELAY_EINVAL;
     if (tokens == 0) return RELAY_OK;
     if (out->data == gate->data || out->data == up->data) return RELAY_EINVAL;
-    int ctas;
-    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr, &ctas);
-    if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(gate, type, n, tokens) && vectors(up, type, n, tokens) &&
                      vectors(out, type, n, tokens);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr, vec, &ctas);
+    if (ctas == 0) return RELAY_ECUDA;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         (vec ? relay_gated_kernel<T, true> : relay_gated_kernel<T, false>)<<<ctas, 32 * kWarps, 0, stream>>>(
@@ -643,12 +706,12 @@ int relay_gated_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, con
     for (const relay_rows* o : {dgate, dup})
         if (o->data == dout->data || (!eight && (o->data == gate->data || o->data == up->data))) return RELAY_EINVAL;
     if (dgate->data == dup->data) return RELAY_EINVAL;
-    int ctas;
-    const Grid g = make_grid(n, tokens, d, out_codes != nullptr, &ctas);
-    if (ctas == 0) return RELAY_ECUDA;
     const bool vec = d % 8 == 0 && vectors(dout, type, n, tokens) && vectors(dgate, type, n, tokens) &&
                      vectors(dup, type, n, tokens) && vectors(eight ? nullptr : gate, type, n, tokens) &&
                      vectors(eight ? nullptr : up, type, n, tokens);
+    int ctas;
+    const Grid g = make_grid(n, tokens, d, out_codes != nullptr, vec, &ctas);
+    if (ctas == 0) return RELAY_ECUDA;
     const GatedSource from{gate_codes, up_codes, gate_scales, up_scales};
     return by_type(type, [&](auto t) {
         using T = decltype(t);

@@ -69,7 +69,7 @@ struct Piece {
 };
 template <typename T>
 struct Piece<T, true> {
-    static constexpr int kPer = 16 / sizeof(T);
+    static constexpr int kPer = 16 / sizeof(T);  // features of 16 bytes
     uint4 w[8 / kPer];
     __device__ __forceinline__ void load(const T* p, int lane, int left) {
 #pragma unroll
@@ -155,15 +155,38 @@ __device__ __forceinline__ float code_value(uint32_t w, int k) {
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// The largest magnitude among a lane's 8 features, as bits.
+__device__ __forceinline__ uint32_t largest(const float (&v)[8]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = max(most, magnitude(v[k]));
+    return most;
+}
+
+// The same from 16-bit features as they lie in memory, two at a time: their bits
+// without the sign order as their magnitudes do, NaN last.
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Piece<T, true>& p) {
+    if constexpr (sizeof(T) == 2) {
+        const uint4 w = p.w[0];
+        const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu),
+                                    __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+        const unsigned short most = static_cast<unsigned short>(max(m & 0xffffu, m >> 16));
+        return magnitude(widen(*reinterpret_cast<const T*>(&most)));
+    } else {
+        float v[8];
+        p.get(v);
+        return largest(v);
+    }
+}
+
 // Puts the strip that starts at feature `base` of a row away; `codes` and `scales`
-// are the row's.  v is 0 past d.  All lanes of the warp take part.
+// are the row's.  v is 0 past d; most: largest() of the lane's (unused without kVec).
+// All lanes of the warp take part.
 template <bool kVec>
 __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int base, int lane, int pitch,
-                                          const float (&v)[8]) {
+                                          const float (&v)[8], uint32_t most) {
     if constexpr (kVec) {
-        uint32_t most = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) most = max(most, magnitude(v[k]));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const uint32_t c = scale_byte(most);
@@ -188,6 +211,12 @@ __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int ba
         }
         if (lane < 8 && base + 32 * lane < pitch) scales[base / kBlock + lane] = static_cast<uint8_t>(mine);
     }
+}
+
+template <bool kVec>
+__device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int base, int lane, int pitch,
+                                          const float (&v)[8]) {
+    put_strip<kVec>(codes, scales, base, lane, pitch, v, kVec ? largest(v) : 0u);
 }
 
 // A lane's 8 codes and their scales as they lie in memory.
@@ -229,14 +258,6 @@ struct CodePiece<true> {
         for (int k = 0; k < 8; ++k) v[k] = code_value(k < 4 ? q.x : q.y, k % 4) * unit;
     }
 };
-
-template <bool kVec>
-__device__ __forceinline__ void get_strip(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch,
-                                          float (&v)[8]) {
-    CodePiece<kVec> piece;
-    piece.load(codes, scales, base, lane, pitch);
-    piece.get(v);
-}
 
 // ----------------------------------------------------------- argument checks
 
