@@ -14,6 +14,15 @@ int by_type(int32_t type, F f) {
     return type == RELAY_BF16 ? f(__nv_bfloat16()) : type == RELAY_FP16 ? f(__half()) : f(float());
 }
 
+// The warp's `turn` (layers.cuh) in a kernel of `warps` warps; the norm's kernels need
+// it for unaligned weights too.
+#define WARP_TURN(warps)                                      \
+    __shared__ __align__(16) float turns[kVec ? 1 : warps][kVec ? 1 : kStrip]; \
+    float* turn = turns[kVec ? 0 : threadIdx.x / 32]
+#define WARP_NORM_TURN(warps)                               \
+    __shared__ __align__(16) float turns[warps][kStrip]; \
+    float* turn = turns[threadIdx.x / 32]
+
 // ------------------------------------------------------- element-wise kernels
 
 constexpr int kWarps = 8;  // of an element-wise CTA
@@ -21,15 +30,6 @@ constexpr int kWarps = 8;  // of an element-wise CTA
 // A warp takes this many strips of a row at a time, all of them asked for first.
 template <bool kVec>
 constexpr int kRun = kVec ? 2 : 1;
-
-// largest() where put_strip wants it.
-template <bool kVec, typename T>
-__device__ __forceinline__ uint32_t most_of(const Piece<T, kVec>& p) {
-    if constexpr (kVec)
-        return largest(p);
-    else
-        return 0u;
-}
 
 struct Grid {
     int64_t rows;    // n tokens
@@ -62,6 +62,7 @@ __device__ __forceinline__ void each_run(const Grid& g, F f) {
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_pack_kernel(Grid g, View<const T> x, int8_t* codes, uint8_t* scales) {
+    WARP_TURN(kWarps);
     const int lane = threadIdx.x % 32;
     each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
         Piece<T, kVec> p[kRun<kVec>];
@@ -71,9 +72,9 @@ relay_checkpoint_pack_kernel(Grid g, View<const T> x, int8_t* codes, uint8_t* sc
 #pragma unroll
         for (int j = 0; j < kRun<kVec>; ++j) {
             float v[8];
-            p[j].get(v);
-            put_strip<kVec>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch, v,
-                            most_of<kVec>(p[j]));
+            p[j].get(v, lane, turn);
+            put_strip(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch, v,
+                            largest(p[j], v));
         }
     });
 }
@@ -87,9 +88,10 @@ __device__ __forceinline__ float within<__half>(float v) { return fabsf(v) > 655
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scales, View<T> out) {
+    WARP_TURN(kWarps);
     const int lane = threadIdx.x % 32;
     each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
-        CodePiece<kVec> p[kRun<kVec>];
+        CodePiece p[kRun<kVec>];
 #pragma unroll
         for (int j = 0; j < kRun<kVec>; ++j)
             p[j].load(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch);
@@ -100,7 +102,7 @@ relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scale
             p[j].get(v);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = within<T>(v[k]);
-            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, v);
+            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, v, turn);
         }
     });
 }
@@ -131,6 +133,7 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, int8_t* gate_codes,
                    uint8_t* gate_scales, int8_t* up_codes, uint8_t* up_scales) {
+    WARP_TURN(kWarps);
     const int lane = threadIdx.x % 32;
     each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
         Piece<T, kVec> p[kRun<kVec>], q[kRun<kVec>];
@@ -145,15 +148,15 @@ relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, in
 #pragma unroll
         for (int j = 0; j < kRun<kVec>; ++j) {
             float a[8], b[8];
-            p[j].get(a);
-            q[j].get(b);
+            p[j].get(a, lane, turn);
+            q[j].get(b, lane, turn);
             if (gate_codes != nullptr)
-                put_strip<kVec>(gate_codes + at, gate_scales + scale_at, base + j * kStrip, lane, g.pitch, a, most_of<kVec>(p[j]));
+                put_strip(gate_codes + at, gate_scales + scale_at, base + j * kStrip, lane, g.pitch, a, largest(p[j], a));
             if (up_codes != nullptr)
-                put_strip<kVec>(up_codes + at, up_scales + scale_at, base + j * kStrip, lane, g.pitch, b, most_of<kVec>(q[j]));
+                put_strip(up_codes + at, up_scales + scale_at, base + j * kStrip, lane, g.pitch, b, largest(q[j], b));
 #pragma unroll
             for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid<T>(a[k]).at * b[k];
-            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, a);
+            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, a, turn);
         }
     });
 }
@@ -168,11 +171,12 @@ __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View<const T> up, GatedSource from,
                             View<T> dgate, View<T> dup, int8_t* out_codes, uint8_t* out_scales) {
     constexpr int kR = kRun<kVec>;
+    WARP_TURN(kWarps);
     const int lane = threadIdx.x % 32;
     each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
         const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
         Piece<T, kVec> p[kR], gp[kEight ? 1 : kR], up_p[kEight ? 1 : kR];
-        CodePiece<kVec> gq[kEight ? kR : 1], uq[kEight ? kR : 1];
+        CodePiece gq[kEight ? kR : 1], uq[kEight ? kR : 1];
 #pragma unroll
         for (int j = 0; j < kR; ++j) {
             const int first = base + j * kStrip;
@@ -189,13 +193,13 @@ relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View
         for (int j = 0; j < kR; ++j) {
             const int first = base + j * kStrip, left = g.d - first;
             float da[8], a[8], b[8], dg[8];
-            p[j].get(da);
+            p[j].get(da, lane, turn);
             if constexpr (kEight) {
                 gq[j].get(a);
                 uq[j].get(b);
             } else {
-                gp[j].get(a);
-                up_p[j].get(b);
+                gp[j].get(a, lane, turn);
+                up_p[j].get(b, lane, turn);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -205,16 +209,12 @@ relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View
                 da[k] *= silu;
                 a[k] = silu * b[k];
             }
-            store_strip<kVec>(dgate.row(worker, token) + first, lane, left, dg);
-            store_strip<kVec>(dup.row(worker, token) + first, lane, left, da);
+            store_strip<kVec>(dgate.row(worker, token) + first, lane, left, dg, turn);
+            store_strip<kVec>(dup.row(worker, token) + first, lane, left, da, turn);
             if (out_codes != nullptr) {
                 // a block that reads as NaN does so past d too: those stay 0
-                if (left < kStrip) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (feature<kVec>(lane, k) >= left) a[k] = 0.0f;
-                }
-                put_strip<kVec>(out_codes + at, out_scales + scale_at, first, lane, g.pitch, a);
+                clear_past(a, lane, left);
+                put_strip(out_codes + at, out_scales + scale_at, first, lane, g.pitch, a, largest(a));
             }
         }
     });
@@ -260,6 +260,7 @@ template <typename T, bool kVec, int kParts, int kStrips>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel(NormArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
     __shared__ float shared[kNormWarps<kParts>];
+    WARP_NORM_TURN(kNormWarps<kParts>);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot;
     const bool on = row < a.rows;
@@ -270,10 +271,10 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel
 #pragma unroll
     for (int j = 0; j < kStrips; ++j) {
         const int base = (part + kParts * j) * kStrip, left = on ? a.d - base : 0;
-        load_strip<kVec>(a.x.row(worker, token) + base, lane, left, h[j]);
+        load_strip<kVec>(a.x.row(worker, token) + base, lane, left, h[j], turn);
         if (a.residual.p != nullptr) {
             float r[8];
-            load_strip<kVec>(a.residual.row(worker, token) + base, lane, left, r);
+            load_strip<kVec>(a.residual.row(worker, token) + base, lane, left, r, turn);
 #pragma unroll
             for (int k = 0; k < 8; ++k) h[j][k] += r[k];
         }
@@ -288,16 +289,18 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel
     for (int j = 0; j < kStrips; ++j) {
         const int base = (part + kParts * j) * kStrip, left = a.d - base;
         if (base >= a.pitch) break;
-        if (a.total.p != nullptr) store_strip<kVec>(a.total.row(worker, token) + base, lane, left, h[j]);
+        if (a.total.p != nullptr) store_strip<kVec>(a.total.row(worker, token) + base, lane, left, h[j], turn);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) h[j][k] = feature<kVec>(lane, k) < left ? h[j][k] * rstd : 0.0f;
+        for (int k = 0; k < 8; ++k) h[j][k] *= rstd;
+        clear_past(h[j], lane, left);
         if (a.codes != nullptr)
-            put_strip<kVec>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j]);
+            put_strip(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j],
+                      largest(h[j]));
         float w[8];
-        load_weight<kVec>(a.weight + worker * a.weight_stride + base, lane, left, a.weight_quads, w);
+        load_weight(a.weight + worker * a.weight_stride + base, lane, left, a.weight_quads, w, turn);
 #pragma unroll
         for (int k = 0; k < 8; ++k) h[j][k] *= w[k];
-        store_strip<kVec>(a.y.row(worker, token) + base, lane, left, h[j]);
+        store_strip<kVec>(a.y.row(worker, token) + base, lane, left, h[j], turn);
     }
 }
 
@@ -312,7 +315,7 @@ struct NormBackwardArgs {
     const int8_t* codes;
     const uint8_t* scales;
     const int32_t* lengths;
-    float* partial;  // [n][gridDim.x][d]
+    float* partial;  // [n][gridDim.x][pitch]
     int32_t tokens, d, pitch;
 };
 
@@ -322,10 +325,12 @@ struct NormBackwardArgs {
 // than 8192 features, and unaligned ones, leave no room for that (kLean), and the
 // widest are read twice (kTwice), the second time from the caches.
 template <typename T, bool kVec, int kParts, int kStrips, bool kEight>
-__global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
+__global__ void __launch_bounds__(32 * kNormWarps<kParts>, kNormWarps<kParts> > 8 ? 1 : 2)
+relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
     constexpr bool kLean = kStrips > 2 || !kVec, kTwice = kParts > 16;
     __shared__ float shared[kNormWarps<kParts>];
+    WARP_NORM_TURN(kNormWarps<kParts>);
     extern __shared__ float sums[];  // kRows > 1: [kRows - 1][kStrips][kParts][256]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
     const int worker = blockIdx.y;
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backwa
 
     struct Row {  // what a lane needs of a row, as it lies in memory
         Piece<T, kVec> dy[kStrips], total[kEight ? 1 : kStrips], dtotal[kLean ? 1 : kStrips];
-        CodePiece<kVec> codes[kEight ? kStrips : 1];
+        CodePiece codes[kEight ? kStrips : 1];
         float rstd;
     };
     const auto ask_strip = [&](Row& r, int token, int j, int to) {
@@ -360,15 +365,12 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backwa
     };
     // dy and xhat of strip j, from `from` of the row
     const auto widen_strip = [&](const Row& r, int token, int j, int from, float (&dy)[8], float (&xhat)[8]) {
-        r.dy[from].get(dy);
+        r.dy[from].get(dy, lane, turn);
         if constexpr (kEight) {
             r.codes[from].get(xhat);
-            const int left = token < length ? a.d - base_of(j) : 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (feature<kVec>(lane, k) >= left) xhat[k] = 0.0f;  // a NaN block's features past d
+            clear_past(xhat, lane, token < length ? a.d - base_of(j) : 0);
         } else {
-            r.total[from].get(xhat);
+            r.total[from].get(xhat, lane, turn);
 #pragma unroll
             for (int k = 0; k < 8; ++k) xhat[k] *= r.rstd;
         }
@@ -377,7 +379,7 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backwa
     float w[kLean ? 1 : kStrips][8];
     if constexpr (!kLean) {
 #pragma unroll
-        for (int j = 0; j < kStrips; ++j) load_weight<kVec>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[j]);
+        for (int j = 0; j < kStrips; ++j) load_weight(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[j], turn);
     }
     float dw[kStrips][8] = {};
     const int step = static_cast<int>(gridDim.x) * kRows;
@@ -401,7 +403,7 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backwa
             if (kTwice) ask_strip(r, token, j, 0);
             widen_strip(r, token, j, at, u[at], xhat[at]);
             float m[8];
-            if constexpr (kLean) load_weight<kVec>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m);
+            if constexpr (kLean) load_weight(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m, turn);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 dw[j][k] = fmaf(u[at][k], xhat[at][k], dw[j][k]);
@@ -420,18 +422,18 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backwa
                     ask_strip(r, token, j, 0);
                     widen_strip(r, token, j, 0, u[0], xhat[0]);
                     float m[8];
-                    load_weight<kVec>(weight + base, lane, left, a.weight_quads, m);
+                    load_weight(weight + base, lane, left, a.weight_quads, m, turn);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) u[0][k] *= m[k];
                 }
                 float dh[8] = {};
                 if (a.dtotal.p != nullptr) {
                     if constexpr (kLean) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, token < length ? left : 0);
-                    r.dtotal[kLean ? 0 : j].get(dh);
+                    r.dtotal[kLean ? 0 : j].get(dh, lane, turn);
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) dh[k] = fmaf(r.rstd, u[at][k] - xhat[at][k] * along, dh[k]);
-                store_strip<kVec>(a.dx.row(worker, token) + base, lane, left, dh);
+                store_strip<kVec>(a.dx.row(worker, token) + base, lane, left, dh, turn);
             }
         }
     }
@@ -452,25 +454,21 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_backwa
                 for (int k = 0; k < 8; ++k)
                     dw[j][k] += sums[((s * kStrips + j) * kParts + part) * kStrip + 32 * k + lane];
     }
-    float* out = a.partial + (static_cast<int64_t>(worker) * gridDim.x + blockIdx.x) * a.d;
+    float* out = a.partial + (static_cast<int64_t>(worker) * gridDim.x + blockIdx.x) * a.pitch;
 #pragma unroll
-    for (int j = 0; j < kStrips; ++j) {
-        const int base = (part + kParts * j) * kStrip;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (base + feature<kVec>(lane, k) < a.d) out[base + feature<kVec>(lane, k)] = dw[j][k];
-    }
+    for (int j = 0; j < kStrips; ++j)
+        if (base_of(j) + 8 * lane < a.pitch) store_strip<true>(out + base_of(j), lane, kStrip, dw[j], turn);
 }
 
 // dweight[i][k] = sum_p partial[i][p][k]: a CTA sums 32 columns, 8 rows at a time.
 __global__ void __launch_bounds__(256)
-relay_norm_join_kernel(const float* partial, int parts, int d, float* dweight, int64_t dweight_stride) {
+relay_norm_join_kernel(const float* partial, int parts, int d, int pitch, float* dweight, int64_t dweight_stride) {
     __shared__ float shared[8][32];
     const int column = blockIdx.x * 32 + threadIdx.x % 32, lead = threadIdx.x / 32;
-    const float* p = partial + static_cast<int64_t>(blockIdx.y) * parts * d;
+    const float* p = partial + static_cast<int64_t>(blockIdx.y) * parts * pitch;
     float s = 0.0f;
     if (column < d)
-        for (int r = lead; r < parts; r += 8) s += p[static_cast<int64_t>(r) * d + column];
+        for (int r = lead; r < parts; r += 8) s += p[static_cast<int64_t>(r) * pitch + column];
     shared[lead][threadIdx.x % 32] = s;
     __syncthreads();
     if (lead > 0 || column >= d) return;
@@ -586,7 +584,7 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
         using T = decltype(t);
         const NormArgs<T> a{view<const T>(x, n, tokens), view<const T>(residual, n, tokens),
                             view<T>(total, n, tokens), view<T>(y, n, tokens), weight, n > 1 ? weight_stride : 0,
-                            aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), eps, rstd, codes, scales,
+                            d % 8 == 0 && aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), eps, rstd, codes, scales,
                             static_cast<int32_t>(n * tokens), static_cast<int32_t>(tokens), static_cast<int32_t>(d),
                             static_cast<int32_t>(pitch_of(d))};
         return by_width(a.pitch, [&](auto hold) {
@@ -602,7 +600,7 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
 int64_t relay_rms_norm_backward_workspace(int32_t n, int64_t tokens, int64_t d) {
     if (const int rc = check_shape(RELAY_FP32, n, tokens, d)) return rc;
     if (d > RELAY_NORM_MAX_D) return RELAY_EUNSUPPORTED;
-    return 4 * n * norm_partials(n, tokens) * d;
+    return 4 * n * norm_partials(n, tokens) * pitch_of(d);
 }
 
 int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* dy,
@@ -636,7 +634,7 @@ int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, 
         const NormBackwardArgs<T> a{view<const T>(dy, n, tokens), view<const T>(dtotal, n, tokens),
                                     view<const T>(total, n, tokens), view<T>(dx, n, tokens), weight,
                                     n > 1 ? weight_stride : 0,
-                                    aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), rstd, codes, scales,
+                                    d % 8 == 0 && aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), rstd, codes, scales,
                                     lengths, static_cast<float*>(workspace), static_cast<int32_t>(tokens),
                                     static_cast<int32_t>(d), static_cast<int32_t>(pitch_of(d))};
         return by_width(a.pitch, [&](auto hold) {
@@ -652,7 +650,8 @@ int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, 
     });
     if (rc != RELAY_OK) return rc;
     relay_norm_join_kernel<<<dim3(static_cast<unsigned>((d + 31) / 32), n), 256, 0, stream>>>(
-        static_cast<const float*>(workspace), parts, static_cast<int>(d), dweight, dweight_stride);
+        static_cast<const float*>(workspace), parts, static_cast<int>(d), static_cast<int>(pitch_of(d)), dweight,
+        dweight_stride);
     return status_of_launch();
 }
 

@@ -44,85 +44,94 @@ struct View {
 
 // ------------------------------------------------------- a strip of 256 features
 //
-// kVec: lane l holds features 8l .. 8l+7 of the strip and moves them in 16-byte
-// pieces (d is a multiple of 8 then).  Otherwise lane l holds features l, 32 + l,
-// ... 224 + l, so that every element-wise access of the warp is one contiguous
-// piece whatever the rows' alignment, and a block of the 8-bit format is one
-// element of every lane.  `left`: features of the row from the strip's first on.
+// Lane l has features 8l .. 8l + 7 of the strip.  With kVec they are moved in 16-byte
+// pieces (rows on 16-byte boundaries, d a multiple of 8).  Other rows are moved
+// element by element, each of the warp's accesses one contiguous piece, and change
+// places in `turn`, 256 elements of shared memory of the warp's own: that measured
+// half the time of a warp whose lanes hold every 32nd feature, because codes, scales
+// and block maxima stay those of the other case.  `left`: features of the row from
+// the strip's first on.  All lanes of the warp call these together.
 
-template <bool kVec>
-__device__ __forceinline__ int feature(int lane, int k) { return kVec ? 8 * lane + k : 32 * k + lane; }
+template <typename T>
+__device__ __forceinline__ void widen_octet(const T* e, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = widen(e[k]);
+}
 
-// A lane's 8 features as they lie in memory, so that they can be asked for long before
-// they are used.
+// A lane's 8 features of 16 bits, or 4 of the 32-bit ones, per piece.
+template <typename T>
+constexpr int kPieces = sizeof(T) * 8 / 16;
+
+// A lane's features as they came from memory, so that they can be asked for long
+// before they are used.
 template <typename T, bool kVec>
 struct Piece {
-    T e[8];
+    T e[8];  // 32 k + lane
     __device__ __forceinline__ void load(const T* p, int lane, int left) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) e[k] = 32 * k + lane < left ? p[32 * k + lane] : T(0.0f);
     }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
+    __device__ __forceinline__ void get(float (&v)[8], int lane, float* turn) const {
+        T* t = reinterpret_cast<T*>(turn);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = widen(e[k]);
+        for (int k = 0; k < 8; ++k) t[32 * k + lane] = e[k];
+        __syncwarp();
+        uint4 w[kPieces<T>];
+#pragma unroll
+        for (int h = 0; h < kPieces<T>; ++h) w[h] = reinterpret_cast<const uint4*>(t + 8 * lane)[h];
+        widen_octet(reinterpret_cast<const T*>(w), v);
+        __syncwarp();
     }
 };
 template <typename T>
 struct Piece<T, true> {
-    static constexpr int kPer = 16 / sizeof(T);  // features of 16 bytes
-    uint4 w[8 / kPer];
+    uint4 w[kPieces<T>];
     __device__ __forceinline__ void load(const T* p, int lane, int left) {
 #pragma unroll
-        for (int h = 0; h < 8 / kPer; ++h)
-            w[h] = 8 * lane < left ? *reinterpret_cast<const uint4*>(p + 8 * lane + h * kPer)
+        for (int h = 0; h < kPieces<T>; ++h)
+            w[h] = 8 * lane < left ? reinterpret_cast<const uint4*>(p + 8 * lane)[h]
                                    : make_uint4(0, 0, 0, 0);  // +0 in every type
     }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-        for (int h = 0; h < 8 / kPer; ++h) {
-            const T* e = reinterpret_cast<const T*>(&w[h]);
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) v[h * kPer + k] = widen(e[k]);
-        }
+    __device__ __forceinline__ void get(float (&v)[8], int, float*) const {
+        widen_octet(reinterpret_cast<const T*>(w), v);
     }
 };
 
 template <bool kVec, typename T>
-__device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8]) {
+__device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8], float* turn) {
     Piece<T, kVec> piece;
     piece.load(p, lane, left);
-    piece.get(v);
+    piece.get(v, lane, turn);
 }
 
 template <bool kVec, typename T>
-__device__ __forceinline__ void store_strip(T* p, int lane, int left, const float (&v)[8]) {
+__device__ __forceinline__ void store_strip(T* p, int lane, int left, const float (&v)[8], float* turn) {
+    uint4 w[kPieces<T>];
+    T* e = reinterpret_cast<T*>(w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e[k] = narrow<T>(v[k]);
     if constexpr (kVec) {
         if (8 * lane >= left) return;
-        constexpr int kPer = 16 / sizeof(T);
 #pragma unroll
-        for (int h = 0; h < 8 / kPer; ++h) {
-            uint4 w;
-            T* e = reinterpret_cast<T*>(&w);
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) e[k] = narrow<T>(v[h * kPer + k]);
-            *reinterpret_cast<uint4*>(p + 8 * lane + h * kPer) = w;
-        }
+        for (int h = 0; h < kPieces<T>; ++h) reinterpret_cast<uint4*>(p + 8 * lane)[h] = w[h];
     } else {
+        T* t = reinterpret_cast<T*>(turn);
+#pragma unroll
+        for (int h = 0; h < kPieces<T>; ++h) reinterpret_cast<uint4*>(t + 8 * lane)[h] = w[h];
+        __syncwarp();
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (32 * k + lane < left) p[32 * k + lane] = narrow<T>(v[k]);
+            if (32 * k + lane < left) p[32 * k + lane] = t[32 * k + lane];
+        __syncwarp();
     }
 }
 
-// fp32 weights at the same features; `quads`: their addresses are multiples of 16 bytes.
-template <bool kVec>
-__device__ __forceinline__ void load_weight(const float* p, int lane, int left, bool quads, float (&v)[8]) {
-    if (kVec && quads) {
-        load_strip<true>(p, lane, left, v);
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = feature<kVec>(lane, k) < left ? p[feature<kVec>(lane, k)] : 0.0f;
+// fp32 weights of the strip; `quads`: on 16-byte boundaries, with whole octets.
+__device__ __forceinline__ void load_weight(const float* p, int lane, int left, bool quads, float (&v)[8], float* turn) {
+    if (quads)
+        load_strip<true>(p, lane, left, v, turn);
+    else
+        load_strip<false>(p, lane, left, v, turn);
 }
 
 // ------------------------------------------------------------- the 8-bit format
@@ -167,81 +176,44 @@ __device__ __forceinline__ uint32_t largest(const float (&v)[8]) {
 // without the sign order as their magnitudes do, NaN last.
 template <typename T>
 __device__ __forceinline__ uint32_t largest(const Piece<T, true>& p) {
-    if constexpr (sizeof(T) == 2) {
-        const uint4 w = p.w[0];
-        const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu),
-                                    __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
-        const unsigned short most = static_cast<unsigned short>(max(m & 0xffffu, m >> 16));
-        return magnitude(widen(*reinterpret_cast<const T*>(&most)));
-    } else {
-        float v[8];
-        p.get(v);
+    const uint4 w = p.w[0];
+    const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu),
+                                __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+    const unsigned short most = static_cast<unsigned short>(max(m & 0xffffu, m >> 16));
+    return magnitude(widen(*reinterpret_cast<const T*>(&most)));
+}
+
+// The same, by what is at hand.
+template <typename T, bool kVec>
+__device__ __forceinline__ uint32_t largest(const Piece<T, kVec>& p, const float (&v)[8]) {
+    if constexpr (kVec && sizeof(T) == 2)
+        return largest(p);
+    else
         return largest(v);
-    }
 }
 
 // Puts the strip that starts at feature `base` of a row away; `codes` and `scales`
-// are the row's.  v is 0 past d; most: largest() of the lane's (unused without kVec).
-// All lanes of the warp take part.
-template <bool kVec>
+// are the row's.  v is 0 past d; most: the lane's largest().  All lanes of the warp
+// take part.
 __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int base, int lane, int pitch,
                                           const float (&v)[8], uint32_t most) {
-    if constexpr (kVec) {
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const uint32_t c = scale_byte(most);
-        if (base + 8 * lane >= pitch) return;
-        uint32_t w[2];
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    const uint32_t c = scale_byte(most);
+    if (base + 8 * lane >= pitch) return;
+    uint32_t w[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t ab = __byte_perm(code_bits(v[4 * h], c), code_bits(v[4 * h + 1], c), 0x0040);
-            const uint32_t cd = __byte_perm(code_bits(v[4 * h + 2], c), code_bits(v[4 * h + 3], c), 0x0040);
-            w[h] = c == 255u ? 0u : __byte_perm(ab, cd, 0x5410);
-        }
-        *reinterpret_cast<uint2*>(codes + base + 8 * lane) = make_uint2(w[0], w[1]);
-        if (lane % 4 == 0) scales[base / kBlock + lane / 4] = static_cast<uint8_t>(c);
-    } else {
-        uint32_t mine = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t c = scale_byte(__reduce_max_sync(0xffffffffu, magnitude(v[k])));
-            if (lane == k) mine = c;
-            if (base + 32 * k < pitch)
-                codes[base + 32 * k + lane] = c == 255u ? 0 : static_cast<int8_t>(code_bits(v[k], c) & 0xffu);
-        }
-        if (lane < 8 && base + 32 * lane < pitch) scales[base / kBlock + lane] = static_cast<uint8_t>(mine);
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t ab = __byte_perm(code_bits(v[4 * h], c), code_bits(v[4 * h + 1], c), 0x0040);
+        const uint32_t cd = __byte_perm(code_bits(v[4 * h + 2], c), code_bits(v[4 * h + 3], c), 0x0040);
+        w[h] = c == 255u ? 0u : __byte_perm(ab, cd, 0x5410);
     }
+    *reinterpret_cast<uint2*>(codes + base + 8 * lane) = make_uint2(w[0], w[1]);
+    if (lane % 4 == 0) scales[base / kBlock + lane / 4] = static_cast<uint8_t>(c);
 }
 
-template <bool kVec>
-__device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int base, int lane, int pitch,
-                                          const float (&v)[8]) {
-    put_strip<kVec>(codes, scales, base, lane, pitch, v, kVec ? largest(v) : 0u);
-}
-
-// A lane's 8 codes and their scales as they lie in memory.
-template <bool kVec>
+// A lane's 8 codes and their scale as they lie in memory.
 struct CodePiece {
-    int8_t q[8];
-    uint8_t c[8];
-    __device__ __forceinline__ void load(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            q[k] = 0;
-            c[k] = 7;
-            if (base + 32 * k < pitch) {
-                q[k] = codes[base + 32 * k + lane];
-                c[k] = scales[base / kBlock + k];
-            }
-        }
-    }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(q[k]) * scale_unit(c[k]);
-    }
-};
-template <>
-struct CodePiece<true> {
     uint2 q;
     uint32_t c;
     __device__ __forceinline__ void load(const int8_t* codes, const uint8_t* scales, int base, int lane, int pitch) {
@@ -258,6 +230,14 @@ struct CodePiece<true> {
         for (int k = 0; k < 8; ++k) v[k] = code_value(k < 4 ? q.x : q.y, k % 4) * unit;
     }
 };
+
+// v is 0 past the row's end, also where its block reads as NaN.
+__device__ __forceinline__ void clear_past(float (&v)[8], int lane, int left) {
+    if (left >= kStrip) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (8 * lane + k >= left) v[k] = 0.0f;
+}
 
 // ----------------------------------------------------------- argument checks
 

@@ -204,6 +204,8 @@ template <typename T, int kTerms, bool kVec>
 __global__ void __launch_bounds__(256)
 relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bfloat16* to, int n, int tokens,
                                int outputs, int width) {
+    __shared__ __align__(16) float turns[kVec ? 1 : 8][kVec ? 1 : kStrip];
+    float* turn = turns[kVec ? 0 : threadIdx.x / 32];
     const int lane = threadIdx.x % 32, strips = (outputs + kStrip - 1) / kStrip;
     const int64_t all = static_cast<int64_t>(n) * tokens * strips;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
@@ -212,7 +214,7 @@ relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bf
         const int token = static_cast<int>(row - static_cast<int64_t>(worker) * tokens);
         float v[8];
         load_strip<kVec>(dy.row(worker, token) + base, lane,
-                         lengths == nullptr || token < lengths[worker] ? outputs - base : 0, v);
+                         lengths == nullptr || token < lengths[worker] ? outputs - base : 0, v, turn);
 #pragma unroll
         for (int term = 0; term < kTerms; ++term) {
             float high[8];
@@ -226,8 +228,9 @@ relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bf
                     v[k] -= high[k];
                 }
             }
-            store_strip<kVec>(to + ((static_cast<int64_t>(worker) * kTerms + term) * tokens + token) * width + base, lane,
-                              outputs - base, high);
+            // the terms' rows are aligned whatever dy's are
+            store_strip<true>(to + ((static_cast<int64_t>(worker) * kTerms + term) * tokens + token) * width + base, lane,
+                              width - base, high, turn);
         }
     }
 }
