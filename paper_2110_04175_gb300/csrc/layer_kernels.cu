@@ -14,22 +14,17 @@ int by_type(int32_t type, F f) {
     return type == RELAY_BF16 ? f(__nv_bfloat16()) : type == RELAY_FP16 ? f(__half()) : f(float());
 }
 
-// The warp's `turn` (layers.cuh) in a kernel of `warps` warps; the norm's kernels need
-// it for unaligned weights too.
-#define WARP_TURN(warps)                                      \
-    __shared__ __align__(16) float turns[kVec ? 1 : warps][kVec ? 1 : kStrip]; \
-    float* turn = turns[kVec ? 0 : threadIdx.x / 32]
-#define WARP_NORM_TURN(warps)                               \
-    __shared__ __align__(16) float turns[warps][kStrip]; \
-    float* turn = turns[threadIdx.x / 32]
+// The warp's `turn` (layers.cuh) in a kernel of `warps` warps, if it is `used`.
+#define WARP_TURN(warps, used)                                                  \
+    __shared__ __align__(16) float turns[(used) ? (warps) : 1][(used) ? kStrip : 1]; \
+    float* turn = turns[(used) ? threadIdx.x / 32 : 0]
 
 // ------------------------------------------------------- element-wise kernels
 
 constexpr int kWarps = 8;  // of an element-wise CTA
 
 // A warp takes this many strips of a row at a time, all of them asked for first.
-template <bool kVec>
-constexpr int kRun = kVec ? 2 : 1;
+constexpr int kRun = 2;
 
 struct Grid {
     int64_t rows;    // n tokens
@@ -42,14 +37,14 @@ struct Grid {
 
 // Calls f(row, worker, token, first feature) for this warp's runs of strips: every
 // (gridDim.x kWarps)-th one, found without a division past the first.
-template <bool kVec, typename F>
+template <typename F>
 __device__ __forceinline__ void each_run(const Grid& g, F f) {
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     int64_t row = first / g.runs;
     int run = static_cast<int>(first - row * g.runs), worker = static_cast<int>(row / g.tokens);
     int token = static_cast<int>(row - static_cast<int64_t>(worker) * g.tokens);
     while (row < g.rows) {
-        f(row, worker, token, run * (kRun<kVec> * kStrip));
+        f(row, worker, token, run * (kRun * kStrip));
         run += g.step_run;
         token += g.step_token;
         worker += g.step_worker;
@@ -59,22 +54,22 @@ __device__ __forceinline__ void each_run(const Grid& g, F f) {
     }
 }
 
-template <typename T, bool kVec>
+template <typename T, Way kWay>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_pack_kernel(Grid g, View<const T> x, int8_t* codes, uint8_t* scales) {
-    WARP_TURN(kWarps);
+    WARP_TURN(kWarps, kWay == kDirect);
     const int lane = threadIdx.x % 32;
-    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
-        Piece<T, kVec> p[kRun<kVec>];
+    each_run(g, [&](int64_t row, int worker, int token, int base) {
+        Piece<T, kWay> p[kRun];
         const T* from = x.row(worker, token) + base;
 #pragma unroll
-        for (int j = 0; j < kRun<kVec>; ++j) p[j].load(from + j * kStrip, lane, g.d - base - j * kStrip);
+        for (int j = 0; j < kRun; ++j) p[j].load(from + j * kStrip, lane, g.d - base - j * kStrip);
 #pragma unroll
-        for (int j = 0; j < kRun<kVec>; ++j) {
+        for (int j = 0; j < kRun; ++j) {
             float v[8];
-            p[j].get(v, lane, turn);
-            put_strip(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch, v,
-                            largest(p[j], v));
+            p[j].get(v);
+            put_strip<kWay>(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch, v,
+                            largest(p[j], v), turn);
         }
     });
 }
@@ -85,24 +80,24 @@ __device__ __forceinline__ float within(float v) { return v; }
 template <>
 __device__ __forceinline__ float within<__half>(float v) { return fabsf(v) > 65504.0f ? copysignf(65504.0f, v) : v; }
 
-template <typename T, bool kVec>
+template <typename T, Way kWay>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scales, View<T> out) {
-    WARP_TURN(kWarps);
+    WARP_TURN(kWarps, kWay == kDirect);
     const int lane = threadIdx.x % 32;
-    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
-        CodePiece p[kRun<kVec>];
+    each_run(g, [&](int64_t row, int worker, int token, int base) {
+        CodePiece p[kRun];
 #pragma unroll
-        for (int j = 0; j < kRun<kVec>; ++j)
+        for (int j = 0; j < kRun; ++j)
             p[j].load(codes + row * g.pitch, scales + row * (g.pitch / kBlock), base + j * kStrip, lane, g.pitch);
         T* to = out.row(worker, token) + base;
 #pragma unroll
-        for (int j = 0; j < kRun<kVec>; ++j) {
+        for (int j = 0; j < kRun; ++j) {
             float v[8];
-            p[j].get(v);
+            p[j].template get<kWay>(v, lane, turn);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = within<T>(v[k]);
-            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, v, turn);
+            store_strip<kWay>(to + j * kStrip, lane, g.d - base - j * kStrip, v);
         }
     });
 }
@@ -129,34 +124,34 @@ struct Sigmoid {
     }
 };
 
-template <typename T, bool kVec>
+template <typename T, Way kWay>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, int8_t* gate_codes,
                    uint8_t* gate_scales, int8_t* up_codes, uint8_t* up_scales) {
-    WARP_TURN(kWarps);
+    WARP_TURN(kWarps, kWay == kDirect);
     const int lane = threadIdx.x % 32;
-    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
-        Piece<T, kVec> p[kRun<kVec>], q[kRun<kVec>];
+    each_run(g, [&](int64_t row, int worker, int token, int base) {
+        Piece<T, kWay> p[kRun], q[kRun];
         const T *from = gate.row(worker, token) + base, *from_up = up.row(worker, token) + base;
 #pragma unroll
-        for (int j = 0; j < kRun<kVec>; ++j) {
+        for (int j = 0; j < kRun; ++j) {
             p[j].load(from + j * kStrip, lane, g.d - base - j * kStrip);
             q[j].load(from_up + j * kStrip, lane, g.d - base - j * kStrip);
         }
         const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
         T* to = out.row(worker, token) + base;
 #pragma unroll
-        for (int j = 0; j < kRun<kVec>; ++j) {
+        for (int j = 0; j < kRun; ++j) {
             float a[8], b[8];
-            p[j].get(a, lane, turn);
-            q[j].get(b, lane, turn);
+            p[j].get(a);
+            q[j].get(b);
             if (gate_codes != nullptr)
-                put_strip(gate_codes + at, gate_scales + scale_at, base + j * kStrip, lane, g.pitch, a, largest(p[j], a));
+                put_strip<kWay>(gate_codes + at, gate_scales + scale_at, base + j * kStrip, lane, g.pitch, a, largest(p[j], a), turn);
             if (up_codes != nullptr)
-                put_strip(up_codes + at, up_scales + scale_at, base + j * kStrip, lane, g.pitch, b, largest(q[j], b));
+                put_strip<kWay>(up_codes + at, up_scales + scale_at, base + j * kStrip, lane, g.pitch, b, largest(q[j], b), turn);
 #pragma unroll
             for (int k = 0; k < 8; ++k) a[k] = a[k] * Sigmoid<T>(a[k]).at * b[k];
-            store_strip<kVec>(to + j * kStrip, lane, g.d - base - j * kStrip, a, turn);
+            store_strip<kWay>(to + j * kStrip, lane, g.d - base - j * kStrip, a);
         }
     });
 }
@@ -166,19 +161,18 @@ struct GatedSource {  // one of the two
     const uint8_t *gate_scales, *up_scales;
 };
 
-template <typename T, bool kVec, bool kEight>
+template <typename T, Way kWay, bool kEight>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View<const T> up, GatedSource from,
                             View<T> dgate, View<T> dup, int8_t* out_codes, uint8_t* out_scales) {
-    constexpr int kR = kRun<kVec>;
-    WARP_TURN(kWarps);
+    WARP_TURN(kWarps, kWay == kDirect);
     const int lane = threadIdx.x % 32;
-    each_run<kVec>(g, [&](int64_t row, int worker, int token, int base) {
+    each_run(g, [&](int64_t row, int worker, int token, int base) {
         const int64_t at = row * g.pitch, scale_at = row * (g.pitch / kBlock);
-        Piece<T, kVec> p[kR], gp[kEight ? 1 : kR], up_p[kEight ? 1 : kR];
-        CodePiece gq[kEight ? kR : 1], uq[kEight ? kR : 1];
+        Piece<T, kWay> p[kRun], gp[kEight ? 1 : kRun], up_p[kEight ? 1 : kRun];
+        CodePiece gq[kEight ? kRun : 1], uq[kEight ? kRun : 1];
 #pragma unroll
-        for (int j = 0; j < kR; ++j) {
+        for (int j = 0; j < kRun; ++j) {
             const int first = base + j * kStrip;
             p[j].load(dout.row(worker, token) + first, lane, g.d - first);
             if constexpr (kEight) {
@@ -190,16 +184,16 @@ relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View
             }
         }
 #pragma unroll
-        for (int j = 0; j < kR; ++j) {
+        for (int j = 0; j < kRun; ++j) {
             const int first = base + j * kStrip, left = g.d - first;
             float da[8], a[8], b[8], dg[8];
-            p[j].get(da, lane, turn);
+            p[j].get(da);
             if constexpr (kEight) {
-                gq[j].get(a);
-                uq[j].get(b);
+                gq[j].template get<kWay>(a, lane, turn);
+                uq[j].template get<kWay>(b, lane, turn);
             } else {
-                gp[j].get(a, lane, turn);
-                up_p[j].get(b, lane, turn);
+                gp[j].get(a);
+                up_p[j].get(b);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -209,12 +203,12 @@ relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View
                 da[k] *= silu;
                 a[k] = silu * b[k];
             }
-            store_strip<kVec>(dgate.row(worker, token) + first, lane, left, dg, turn);
-            store_strip<kVec>(dup.row(worker, token) + first, lane, left, da, turn);
+            store_strip<kWay>(dgate.row(worker, token) + first, lane, left, dg);
+            store_strip<kWay>(dup.row(worker, token) + first, lane, left, da);
             if (out_codes != nullptr) {
                 // a block that reads as NaN does so past d too: those stay 0
-                clear_past(a, lane, left);
-                put_strip(out_codes + at, out_scales + scale_at, first, lane, g.pitch, a, largest(a));
+                clear_past<kWay>(a, lane, left);
+                put_strip<kWay>(out_codes + at, out_scales + scale_at, first, lane, g.pitch, a, kWay == kVector ? largest(a) : 0u, turn);
             }
         }
     });
@@ -256,11 +250,11 @@ template <int kParts>
 constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
 
 // kParts warps share a row, each with kStrips strips of it in registers.
-template <typename T, bool kVec, int kParts, int kStrips>
+template <typename T, Way kWay, int kParts, int kStrips>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel(NormArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
     __shared__ float shared[kNormWarps<kParts>];
-    WARP_NORM_TURN(kNormWarps<kParts>);
+    WARP_TURN(kNormWarps<kParts>, true);  // kVector: for unaligned weights
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot;
     const bool on = row < a.rows;
@@ -271,10 +265,10 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel
 #pragma unroll
     for (int j = 0; j < kStrips; ++j) {
         const int base = (part + kParts * j) * kStrip, left = on ? a.d - base : 0;
-        load_strip<kVec>(a.x.row(worker, token) + base, lane, left, h[j], turn);
+        load_strip<kWay>(a.x.row(worker, token) + base, lane, left, h[j]);
         if (a.residual.p != nullptr) {
             float r[8];
-            load_strip<kVec>(a.residual.row(worker, token) + base, lane, left, r, turn);
+            load_strip<kWay>(a.residual.row(worker, token) + base, lane, left, r);
 #pragma unroll
             for (int k = 0; k < 8; ++k) h[j][k] += r[k];
         }
@@ -289,18 +283,18 @@ __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel
     for (int j = 0; j < kStrips; ++j) {
         const int base = (part + kParts * j) * kStrip, left = a.d - base;
         if (base >= a.pitch) break;
-        if (a.total.p != nullptr) store_strip<kVec>(a.total.row(worker, token) + base, lane, left, h[j], turn);
+        if (a.total.p != nullptr) store_strip<kWay>(a.total.row(worker, token) + base, lane, left, h[j]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) h[j][k] *= rstd;
-        clear_past(h[j], lane, left);
+        clear_past<kWay>(h[j], lane, left);
         if (a.codes != nullptr)
-            put_strip(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j],
-                      largest(h[j]));
+            put_strip<kWay>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j],
+                      kWay == kVector ? largest(h[j]) : 0u, turn);
         float w[8];
-        load_weight(a.weight + worker * a.weight_stride + base, lane, left, a.weight_quads, w, turn);
+        load_weight<kWay>(a.weight + worker * a.weight_stride + base, lane, left, a.weight_quads, w, turn);
 #pragma unroll
         for (int k = 0; k < 8; ++k) h[j][k] *= w[k];
-        store_strip<kVec>(a.y.row(worker, token) + base, lane, left, h[j], turn);
+        store_strip<kWay>(a.y.row(worker, token) + base, lane, left, h[j]);
     }
 }
 
@@ -324,13 +318,13 @@ struct NormBackwardArgs {
 // before this one's sum over the CTA, and the weight stays in registers; rows of more
 // than 8192 features, and unaligned ones, leave no room for that (kLean), and the
 // widest are read twice (kTwice), the second time from the caches.
-template <typename T, bool kVec, int kParts, int kStrips, bool kEight>
+template <typename T, Way kWay, int kParts, int kStrips, bool kEight>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>, kNormWarps<kParts> > 8 ? 1 : 2)
 relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
-    constexpr bool kLean = kStrips > 2 || !kVec, kTwice = kParts > 16;
+    constexpr bool kLean = kStrips > 2 || kWay != kVector, kTwice = kParts > 16;
     __shared__ float shared[kNormWarps<kParts>];
-    WARP_NORM_TURN(kNormWarps<kParts>);
+    WARP_TURN(kNormWarps<kParts>, true);  // kVector: for unaligned weights
     extern __shared__ float sums[];  // kRows > 1: [kRows - 1][kStrips][kParts][256]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
     const int worker = blockIdx.y;
@@ -339,7 +333,7 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     const auto base_of = [&](int j) { return (part + kParts * j) * kStrip; };
 
     struct Row {  // what a lane needs of a row, as it lies in memory
-        Piece<T, kVec> dy[kStrips], total[kEight ? 1 : kStrips], dtotal[kLean ? 1 : kStrips];
+        Piece<T, kWay> dy[kStrips], total[kEight ? 1 : kStrips], dtotal[kLean ? 1 : kStrips];
         CodePiece codes[kEight ? kStrips : 1];
         float rstd;
     };
@@ -365,12 +359,12 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     };
     // dy and xhat of strip j, from `from` of the row
     const auto widen_strip = [&](const Row& r, int token, int j, int from, float (&dy)[8], float (&xhat)[8]) {
-        r.dy[from].get(dy, lane, turn);
+        r.dy[from].get(dy);
         if constexpr (kEight) {
-            r.codes[from].get(xhat);
-            clear_past(xhat, lane, token < length ? a.d - base_of(j) : 0);
+            r.codes[from].template get<kWay>(xhat, lane, turn);
+            clear_past<kWay>(xhat, lane, token < length ? a.d - base_of(j) : 0);
         } else {
-            r.total[from].get(xhat, lane, turn);
+            r.total[from].get(xhat);
 #pragma unroll
             for (int k = 0; k < 8; ++k) xhat[k] *= r.rstd;
         }
@@ -379,7 +373,7 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     float w[kLean ? 1 : kStrips][8];
     if constexpr (!kLean) {
 #pragma unroll
-        for (int j = 0; j < kStrips; ++j) load_weight(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[j], turn);
+        for (int j = 0; j < kStrips; ++j) load_weight<kWay>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[j], turn);
     }
     float dw[kStrips][8] = {};
     const int step = static_cast<int>(gridDim.x) * kRows;
@@ -403,7 +397,7 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
             if (kTwice) ask_strip(r, token, j, 0);
             widen_strip(r, token, j, at, u[at], xhat[at]);
             float m[8];
-            if constexpr (kLean) load_weight(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m, turn);
+            if constexpr (kLean) load_weight<kWay>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m, turn);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 dw[j][k] = fmaf(u[at][k], xhat[at][k], dw[j][k]);
@@ -422,18 +416,18 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
                     ask_strip(r, token, j, 0);
                     widen_strip(r, token, j, 0, u[0], xhat[0]);
                     float m[8];
-                    load_weight(weight + base, lane, left, a.weight_quads, m, turn);
+                    load_weight<kWay>(weight + base, lane, left, a.weight_quads, m, turn);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) u[0][k] *= m[k];
                 }
                 float dh[8] = {};
                 if (a.dtotal.p != nullptr) {
                     if constexpr (kLean) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, token < length ? left : 0);
-                    r.dtotal[kLean ? 0 : j].get(dh, lane, turn);
+                    r.dtotal[kLean ? 0 : j].get(dh);
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) dh[k] = fmaf(r.rstd, u[at][k] - xhat[at][k] * along, dh[k]);
-                store_strip<kVec>(a.dx.row(worker, token) + base, lane, left, dh, turn);
+                store_strip<kWay>(a.dx.row(worker, token) + base, lane, left, dh);
             }
         }
     }
@@ -457,7 +451,7 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     float* out = a.partial + (static_cast<int64_t>(worker) * gridDim.x + blockIdx.x) * a.pitch;
 #pragma unroll
     for (int j = 0; j < kStrips; ++j)
-        if (base_of(j) + 8 * lane < a.pitch) store_strip<true>(out + base_of(j), lane, kStrip, dw[j], turn);
+        store_strip<kWay == kDirect ? kDirect : kVector>(out + base_of(j), lane, a.pitch - base_of(j), dw[j]);
 }
 
 // dweight[i][k] = sum_p partial[i][p][k]: a CTA sums 32 columns, 8 rows at a time.
@@ -481,8 +475,8 @@ relay_norm_join_kernel(const float* partial, int parts, int d, int pitch, float*
 
 // The runs of an activation (with its checkpoint's padding), and the CTAs that take
 // them: 0 where there is no device.
-Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint, bool vec, int* ctas) {
-    const int64_t run = kStrip * (vec ? kRun<true> : kRun<false>);
+Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint, int* ctas) {
+    constexpr int64_t run = kStrip * kRun;
     const int64_t pitch = pitch_of(d), runs = ((checkpoint ? pitch : d) + run - 1) / run, rows = n * tokens;
     const int64_t want = (rows * runs + kWarps - 1) / kWarps, most = int64_t(32) * sm_count();
     *ctas = static_cast<int>(want < most ? want : most);
@@ -534,11 +528,11 @@ int relay_checkpoint_pack(int32_t type, int32_t n, int64_t tokens, int64_t d, co
     if (tokens == 0) return RELAY_OK;
     const bool vec = d % 8 == 0 && vectors(x, type, n, tokens);
     int ctas;
-    const Grid g = make_grid(n, tokens, d, true, vec, &ctas);
+    const Grid g = make_grid(n, tokens, d, true, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        (vec ? relay_checkpoint_pack_kernel<T, true> : relay_checkpoint_pack_kernel<T, false>)
+        (vec ? relay_checkpoint_pack_kernel<T, kVector> : relay_checkpoint_pack_kernel<T, kDirect>)
             <<<ctas, 32 * kWarps, 0, stream>>>(g, view<const T>(x, n, tokens), codes, scales);
         return status_of_launch();
     });
@@ -551,11 +545,11 @@ int relay_checkpoint_unpack(int32_t type, int32_t n, int64_t tokens, int64_t d, 
     if (tokens == 0) return RELAY_OK;
     const bool vec = d % 8 == 0 && vectors(out, type, n, tokens);
     int ctas;
-    const Grid g = make_grid(n, tokens, d, false, vec, &ctas);
+    const Grid g = make_grid(n, tokens, d, false, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        (vec ? relay_checkpoint_unpack_kernel<T, true> : relay_checkpoint_unpack_kernel<T, false>)
+        (vec ? relay_checkpoint_unpack_kernel<T, kVector> : relay_checkpoint_unpack_kernel<T, kDirect>)
             <<<ctas, 32 * kWarps, 0, stream>>>(g, codes, scales, view<T>(out, n, tokens));
         return status_of_launch();
     });
@@ -590,7 +584,7 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
         return by_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr int kRows = kNormWarps<kParts> / kParts;
-            (vec ? relay_rms_norm_kernel<T, true, kParts, kStrips> : relay_rms_norm_kernel<T, false, kParts, kStrips>)
+            (vec ? relay_rms_norm_kernel<T, kVector, kParts, kStrips> : relay_rms_norm_kernel<T, kDirect, kParts, kStrips>)
                 <<<(a.rows - 1) / kRows + 1, 32 * kNormWarps<kParts>, 0, stream>>>(a);
             return status_of_launch();
         });
@@ -640,10 +634,10 @@ int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, 
         return by_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr size_t kSmem = (kNormWarps<kParts> / kParts - 1) * kStrips * kParts * kStrip * sizeof(float);
-            (vec ? (eight ? relay_rms_norm_backward_kernel<T, true, kParts, kStrips, true>
-                          : relay_rms_norm_backward_kernel<T, true, kParts, kStrips, false>)
-                 : (eight ? relay_rms_norm_backward_kernel<T, false, kParts, kStrips, true>
-                          : relay_rms_norm_backward_kernel<T, false, kParts, kStrips, false>))
+            (vec ? (eight ? relay_rms_norm_backward_kernel<T, kVector, kParts, kStrips, true>
+                          : relay_rms_norm_backward_kernel<T, kVector, kParts, kStrips, false>)
+                 : (eight ? relay_rms_norm_backward_kernel<T, kDirect, kParts, kStrips, true>
+                          : relay_rms_norm_backward_kernel<T, kDirect, kParts, kStrips, false>))
                 <<<dim3(parts, n), 32 * kNormWarps<kParts>, kSmem, stream>>>(a);
             return status_of_launch();
         });
@@ -672,11 +666,11 @@ int relay_gated(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_
     const bool vec = d % 8 == 0 && vectors(gate, type, n, tokens) && vectors(up, type, n, tokens) &&
                      vectors(out, type, n, tokens);
     int ctas;
-    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr, vec, &ctas);
+    const Grid g = make_grid(n, tokens, d, gate_codes != nullptr || up_codes != nullptr, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        (vec ? relay_gated_kernel<T, true> : relay_gated_kernel<T, false>)<<<ctas, 32 * kWarps, 0, stream>>>(
+        (vec ? relay_gated_kernel<T, kVector> : relay_gated_kernel<T, kDirect>)<<<ctas, 32 * kWarps, 0, stream>>>(
             g, view<const T>(gate, n, tokens), view<const T>(up, n, tokens), view<T>(out, n, tokens), gate_codes,
             gate_scales, up_codes, up_scales);
         return status_of_launch();
@@ -709,13 +703,13 @@ int relay_gated_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, con
                      vectors(dup, type, n, tokens) && vectors(eight ? nullptr : gate, type, n, tokens) &&
                      vectors(eight ? nullptr : up, type, n, tokens);
     int ctas;
-    const Grid g = make_grid(n, tokens, d, out_codes != nullptr, vec, &ctas);
+    const Grid g = make_grid(n, tokens, d, out_codes != nullptr, &ctas);
     if (ctas == 0) return RELAY_ECUDA;
     const GatedSource from{gate_codes, up_codes, gate_scales, up_scales};
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        (vec ? (eight ? relay_gated_backward_kernel<T, true, true> : relay_gated_backward_kernel<T, true, false>)
-             : (eight ? relay_gated_backward_kernel<T, false, true> : relay_gated_backward_kernel<T, false, false>))
+        (vec ? (eight ? relay_gated_backward_kernel<T, kVector, true> : relay_gated_backward_kernel<T, kVector, false>)
+             : (eight ? relay_gated_backward_kernel<T, kDirect, true> : relay_gated_backward_kernel<T, kDirect, false>))
             <<<ctas, 32 * kWarps, 0, stream>>>(g, view<const T>(dout, n, tokens),
                                                view<const T>(eight ? nullptr : gate, n, tokens),
                                                view<const T>(eight ? nullptr : up, n, tokens), from,

@@ -44,13 +44,38 @@ struct View {
 
 // ------------------------------------------------------- a strip of 256 features
 //
-// Lane l has features 8l .. 8l + 7 of the strip.  With kVec they are moved in 16-byte
-// pieces (rows on 16-byte boundaries, d a multiple of 8).  Other rows are moved
-// element by element, each of the warp's accesses one contiguous piece, and change
-// places in `turn`, 256 elements of shared memory of the warp's own: that measured
-// half the time of a warp whose lanes hold every 32nd feature, because codes, scales
-// and block maxima stay those of the other case.  `left`: features of the row from
-// the strip's first on.  All lanes of the warp call these together.
+// Two ways to hold a strip of a row (`left`: the row's features from the strip's first on):
+//   kVector  lane l has features 8l .. 8l + 7, moved in 16-byte pieces: rows on 16-byte
+//            boundaries, d a multiple of 8;
+//   kDirect  lane l has features l, 32 + l, ..., 224 + l, moved element by element, each of
+//            the warp's accesses one contiguous piece: any row.
+// The 8-bit format is kept in octets whichever way the row goes: with kDirect its values
+// change places in `turn`, 256 floats of shared memory of the warp's own.  (At
+// [4][8380][1001] in bf16, the gated step with its checkpoints: 292 us with codes, scales
+// and block maxima element by element, a third of that this way.)  All lanes of the warp
+// call these together.
+enum Way { kDirect, kVector };
+
+template <Way kWay>
+__device__ __forceinline__ int feature(int lane, int k) { return kWay == kDirect ? 32 * k + lane : 8 * lane + k; }
+
+__device__ __forceinline__ void to_octets(float (&v)[8], int lane, float* turn) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) turn[32 * k + lane] = v[k];
+    __syncwarp();
+    const float4 a = reinterpret_cast<const float4*>(turn + 8 * lane)[0], b = reinterpret_cast<const float4*>(turn + 8 * lane)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    __syncwarp();
+}
+
+__device__ __forceinline__ void from_octets(float (&v)[8], int lane, float* turn) {
+    reinterpret_cast<float4*>(turn + 8 * lane)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(turn + 8 * lane)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = turn[32 * k + lane];
+    __syncwarp();
+}
 
 template <typename T>
 __device__ __forceinline__ void widen_octet(const T* e, float (&v)[8]) {
@@ -58,80 +83,73 @@ __device__ __forceinline__ void widen_octet(const T* e, float (&v)[8]) {
     for (int k = 0; k < 8; ++k) v[k] = widen(e[k]);
 }
 
-// A lane's 8 features of 16 bits, or 4 of the 32-bit ones, per piece.
-template <typename T>
-constexpr int kPieces = sizeof(T) * 8 / 16;
-
-// A lane's features as they came from memory, so that they can be asked for long
-// before they are used.
-template <typename T, bool kVec>
+// A lane's 8 features as they lie in memory, so that they can be asked for long before
+// they are used.
+template <typename T, Way kWay>
 struct Piece {
-    T e[8];  // 32 k + lane
+    T e[8];
     __device__ __forceinline__ void load(const T* p, int lane, int left) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) e[k] = 32 * k + lane < left ? p[32 * k + lane] : T(0.0f);
     }
-    __device__ __forceinline__ void get(float (&v)[8], int lane, float* turn) const {
-        T* t = reinterpret_cast<T*>(turn);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[32 * k + lane] = e[k];
-        __syncwarp();
-        uint4 w[kPieces<T>];
-#pragma unroll
-        for (int h = 0; h < kPieces<T>; ++h) w[h] = reinterpret_cast<const uint4*>(t + 8 * lane)[h];
-        widen_octet(reinterpret_cast<const T*>(w), v);
-        __syncwarp();
-    }
+    __device__ __forceinline__ void get(float (&v)[8]) const { widen_octet(e, v); }
 };
 template <typename T>
-struct Piece<T, true> {
-    uint4 w[kPieces<T>];
+struct Piece<T, kVector> {
+    static constexpr int kWords = sizeof(T) / 2;
+    uint4 w[kWords];
     __device__ __forceinline__ void load(const T* p, int lane, int left) {
 #pragma unroll
-        for (int h = 0; h < kPieces<T>; ++h)
+        for (int h = 0; h < kWords; ++h)
             w[h] = 8 * lane < left ? reinterpret_cast<const uint4*>(p + 8 * lane)[h]
                                    : make_uint4(0, 0, 0, 0);  // +0 in every type
     }
-    __device__ __forceinline__ void get(float (&v)[8], int, float*) const {
-        widen_octet(reinterpret_cast<const T*>(w), v);
-    }
+    __device__ __forceinline__ void get(float (&v)[8]) const { widen_octet(reinterpret_cast<const T*>(w), v); }
 };
 
-template <bool kVec, typename T>
-__device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8], float* turn) {
-    Piece<T, kVec> piece;
+template <Way kWay, typename T>
+__device__ __forceinline__ void load_strip(const T* p, int lane, int left, float (&v)[8]) {
+    Piece<T, kWay> piece;
     piece.load(p, lane, left);
-    piece.get(v, lane, turn);
+    piece.get(v);
 }
 
-template <bool kVec, typename T>
-__device__ __forceinline__ void store_strip(T* p, int lane, int left, const float (&v)[8], float* turn) {
-    uint4 w[kPieces<T>];
-    T* e = reinterpret_cast<T*>(w);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) e[k] = narrow<T>(v[k]);
-    if constexpr (kVec) {
-        if (8 * lane >= left) return;
-#pragma unroll
-        for (int h = 0; h < kPieces<T>; ++h) reinterpret_cast<uint4*>(p + 8 * lane)[h] = w[h];
-    } else {
-        T* t = reinterpret_cast<T*>(turn);
-#pragma unroll
-        for (int h = 0; h < kPieces<T>; ++h) reinterpret_cast<uint4*>(t + 8 * lane)[h] = w[h];
-        __syncwarp();
+template <Way kWay, typename T>
+__device__ __forceinline__ void store_strip(T* p, int lane, int left, const float (&v)[8]) {
+    if constexpr (kWay == kDirect) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (32 * k + lane < left) p[32 * k + lane] = t[32 * k + lane];
-        __syncwarp();
+            if (32 * k + lane < left) p[32 * k + lane] = narrow<T>(v[k]);
+    } else {
+        constexpr int kWords = sizeof(T) / 2;
+        if (8 * lane >= left) return;
+        uint4 w[kWords];
+        T* e = reinterpret_cast<T*>(w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = narrow<T>(v[k]);
+#pragma unroll
+        for (int h = 0; h < kWords; ++h) reinterpret_cast<uint4*>(p + 8 * lane)[h] = w[h];
     }
 }
 
 // fp32 weights of the strip; `quads`: on 16-byte boundaries, with whole octets.
+template <Way kWay>
 __device__ __forceinline__ void load_weight(const float* p, int lane, int left, bool quads, float (&v)[8], float* turn) {
-    if (quads)
-        load_strip<true>(p, lane, left, v, turn);
-    else
-        load_strip<false>(p, lane, left, v, turn);
+    if (kWay == kVector && quads) {
+        load_strip<kVector>(p, lane, left, v);
+        return;
+    }
+    load_strip<kDirect>(p, lane, left, v);
+    if (kWay == kVector) to_octets(v, lane, turn);
+}
+
+// v is 0 past the row's end, also where its block reads as NaN.
+template <Way kWay>
+__device__ __forceinline__ void clear_past(float (&v)[8], int lane, int left) {
+    if (left >= kStrip) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (feature<kWay>(lane, k) >= left) v[k] = 0.0f;
 }
 
 // ------------------------------------------------------------- the 8-bit format
@@ -175,7 +193,7 @@ __device__ __forceinline__ uint32_t largest(const float (&v)[8]) {
 // The same from 16-bit features as they lie in memory, two at a time: their bits
 // without the sign order as their magnitudes do, NaN last.
 template <typename T>
-__device__ __forceinline__ uint32_t largest(const Piece<T, true>& p) {
+__device__ __forceinline__ uint32_t largest(const Piece<T, kVector>& p) {
     const uint4 w = p.w[0];
     const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu),
                                 __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
@@ -183,20 +201,29 @@ __device__ __forceinline__ uint32_t largest(const Piece<T, true>& p) {
     return magnitude(widen(*reinterpret_cast<const T*>(&most)));
 }
 
-// The same, by what is at hand.
-template <typename T, bool kVec>
-__device__ __forceinline__ uint32_t largest(const Piece<T, kVec>& p, const float (&v)[8]) {
-    if constexpr (kVec && sizeof(T) == 2)
+// The same, by what is at hand (0 for kDirect, where put_strip finds it).
+template <typename T, Way kWay>
+__device__ __forceinline__ uint32_t largest(const Piece<T, kWay>& p, const float (&v)[8]) {
+    if constexpr (kWay == kDirect)
+        return 0u;
+    else if constexpr (sizeof(T) == 2)
         return largest(p);
     else
         return largest(v);
 }
 
 // Puts the strip that starts at feature `base` of a row away; `codes` and `scales`
-// are the row's.  v is 0 past d; most: the lane's largest().  All lanes of the warp
-// take part.
+// are the row's.  v is 0 past d; most: the lane's largest() (found here for kDirect).
+template <Way kWay>
 __device__ __forceinline__ void put_strip(int8_t* codes, uint8_t* scales, int base, int lane, int pitch,
-                                          const float (&v)[8], uint32_t most) {
+                                          const float (&values)[8], uint32_t most, float* turn) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = values[k];
+    if (kWay == kDirect) {
+        to_octets(v, lane, turn);
+        most = largest(v);
+    }
     most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
     most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
     const uint32_t c = scale_byte(most);
@@ -224,20 +251,14 @@ struct CodePiece {
             c = scales[base / kBlock + lane / 4];
         }
     }
-    __device__ __forceinline__ void get(float (&v)[8]) const {
+    template <Way kWay>
+    __device__ __forceinline__ void get(float (&v)[8], int lane, float* turn) const {
         const float unit = scale_unit(c);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = code_value(k < 4 ? q.x : q.y, k % 4) * unit;
+        if (kWay == kDirect) from_octets(v, lane, turn);
     }
 };
-
-// v is 0 past the row's end, also where its block reads as NaN.
-__device__ __forceinline__ void clear_past(float (&v)[8], int lane, int left) {
-    if (left >= kStrip) return;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (8 * lane + k >= left) v[k] = 0.0f;
-}
 
 // ----------------------------------------------------------- argument checks
 

@@ -200,12 +200,10 @@ struct Recall {
 // dy as bf16 terms [n][kTerms][tokens][width], width = outputs rounded up to a multiple
 // of 8: each term is what is left with all but 8 bits cut off, so that the terms add up
 // exactly.  Rows that do not count are 0.
-template <typename T, int kTerms, bool kVec>
+template <typename T, int kTerms, Way kWay>
 __global__ void __launch_bounds__(256)
 relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bfloat16* to, int n, int tokens,
                                int outputs, int width) {
-    __shared__ __align__(16) float turns[kVec ? 1 : 8][kVec ? 1 : kStrip];
-    float* turn = turns[kVec ? 0 : threadIdx.x / 32];
     const int lane = threadIdx.x % 32, strips = (outputs + kStrip - 1) / kStrip;
     const int64_t all = static_cast<int64_t>(n) * tokens * strips;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
@@ -213,8 +211,8 @@ relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bf
         const int base = static_cast<int>(i - row * strips) * kStrip, worker = static_cast<int>(row / tokens);
         const int token = static_cast<int>(row - static_cast<int64_t>(worker) * tokens);
         float v[8];
-        load_strip<kVec>(dy.row(worker, token) + base, lane,
-                         lengths == nullptr || token < lengths[worker] ? outputs - base : 0, v, turn);
+        load_strip<kWay>(dy.row(worker, token) + base, lane,
+                         lengths == nullptr || token < lengths[worker] ? outputs - base : 0, v);
 #pragma unroll
         for (int term = 0; term < kTerms; ++term) {
             float high[8];
@@ -228,9 +226,8 @@ relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bf
                     v[k] -= high[k];
                 }
             }
-            // the terms' rows are aligned whatever dy's are
-            store_strip<true>(to + ((static_cast<int64_t>(worker) * kTerms + term) * tokens + token) * width + base, lane,
-                              width - base, high, turn);
+            store_strip<kWay>(to + ((static_cast<int64_t>(worker) * kTerms + term) * tokens + token) * width + base, lane,
+                              width - base, high);
         }
     }
 }
@@ -653,7 +650,7 @@ int write_terms(const relay_rows* dy, int32_t type, const int32_t* lengths, void
     const int64_t warps = n * tokens * ((outputs + kStrip - 1) / kStrip), most = 16 * kSms;
     const int ctas = static_cast<int>((warps + 7) / 8 < most ? (warps + 7) / 8 : most);
     const bool vec = outputs % 8 == 0 && vectors(dy, type, n, tokens);
-    (vec ? relay_weight_grad_terms_kernel<T, kTerms, true> : relay_weight_grad_terms_kernel<T, kTerms, false>)
+    (vec ? relay_weight_grad_terms_kernel<T, kTerms, kVector> : relay_weight_grad_terms_kernel<T, kTerms, kDirect>)
         <<<ctas, 256, 0, stream>>>(view<const T>(dy, n, tokens), lengths, static_cast<__nv_bfloat16*>(to), n,
                                    static_cast<int>(tokens), static_cast<int>(outputs),
                                    static_cast<int>(width_of(outputs)));
