@@ -18,7 +18,7 @@
 //
 // The tensor cores cut off what an addition shifts out, so that a long sum in
 // their accumulator drifts towards zero: 6.3e-6 of the result after 384 additions.
-// So they sum 32 to 48 additions at a time, in one of two accumulators, and the
+// So they sum 32 or 36 additions at a time, in one of two accumulators, and the
 // warps that write the stages add the other one to registers, rounded to the
 // nearest.
 #include "blackwell.cuh"
@@ -40,7 +40,7 @@ constexpr int kSms = 152;
 
 // Stages that the tensor cores sum before the sums are added up in registers.
 template <int kTerms>
-constexpr int kGroup = kTerms == 1 ? 8 : 4;
+constexpr int kGroup = kTerms == 1 ? 8 : kTerms == 2 ? 4 : 3;
 
 // An adder's 32 rows x 16 columns on their way to memory, rows 80 bytes apart.
 constexpr int kTurnRow = 20, kTurn = 32 * kTurnRow * 4;
