@@ -314,15 +314,19 @@ struct NormBackwardArgs {
 };
 
 // CTA (p, i) takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i and
-// leaves their sum of dy xhat in its row of `partial`.  The next row is asked for
-// before this one's sum over the CTA, and the weight stays in registers; rows of more
-// than 8192 features, and unaligned ones, leave no room for that (kLean), and the
-// widest are read twice (kTwice), the second time from the caches.
+// leaves their sum of dy xhat in its row of `partial`.  Aligned rows of up to 8192
+// features keep the weight in registers (kHold); they, and others that leave room, ask
+// for the next row before this one's sum over the CTA (kAhead).  16-bit rows stay as they came from memory and are widened
+// again after that sum; others, and those in 8 bits, whose recall costs more than the
+// registers, are kept as fp32 (kKeep).  The widest rows are read twice (kTwice), the
+// second time from the caches.
 template <typename T, Way kWay, int kParts, int kStrips, bool kEight>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>, kNormWarps<kParts> > 8 ? 1 : 2)
 relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
-    constexpr bool kLean = kStrips > 2 || kWay != kVector, kTwice = kParts > 16;
+    constexpr bool kTwice = kParts > 16, kHold = kWay == kVector && kStrips <= 2,
+                   kKeep = !kTwice && (kEight || kWay == kDirect || sizeof(T) == 4),
+                   kAhead = kHold || (kWay == kVector && !kTwice && !kKeep);
     __shared__ float shared[kNormWarps<kParts>];
     WARP_TURN(kNormWarps<kParts>, true);  // kVector: for unaligned weights
     extern __shared__ float sums[];  // kRows > 1: [kRows - 1][kStrips][kParts][256]
@@ -333,7 +337,7 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
     const auto base_of = [&](int j) { return (part + kParts * j) * kStrip; };
 
     struct Row {  // what a lane needs of a row, as it lies in memory
-        Piece<T, kWay> dy[kStrips], total[kEight ? 1 : kStrips], dtotal[kLean ? 1 : kStrips];
+        Piece<T, kWay> dy[kStrips], total[kEight ? 1 : kStrips], dtotal[kHold ? kStrips : 1];
         CodePiece codes[kEight ? kStrips : 1];
         float rstd;
     };
@@ -352,7 +356,7 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
             ask_strip(r, token, j, j);
-            if constexpr (!kLean)
+            if constexpr (kHold)
                 if (a.dtotal.p != nullptr)
                     r.dtotal[j].load(a.dtotal.row(worker, token) + base_of(j), lane, token < length ? a.d - base_of(j) : 0);
         }
@@ -370,63 +374,71 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
         }
     };
 
-    float w[kLean ? 1 : kStrips][8];
-    if constexpr (!kLean) {
+    float w[kHold ? kStrips : 1][8];
+    if constexpr (kHold) {
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) load_weight<kWay>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[j], turn);
     }
+    // u = dy w and xhat of strip j; `before` gets each k's dy and xhat
+    const auto weigh = [&](const Row& r, int token, int j, float (&u)[8], float (&xhat)[8], auto before) {
+        widen_strip(r, token, j, kTwice ? 0 : j, u, xhat);
+        float m[8];
+        if constexpr (!kHold) load_weight<kWay>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m, turn);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            before(k, u[k], xhat[k]);
+            u[k] *= kHold ? w[kHold ? j : 0][k] : m[k];
+        }
+    };
     float dw[kStrips][8] = {};
     const int step = static_cast<int>(gridDim.x) * kRows;
     Row next;
     int first = static_cast<int>(blockIdx.x) * kRows;
-    if (!kTwice && !kLean) ask(next, first + slot);
+    if (kAhead) ask(next, first + slot);
     for (; first < a.tokens; first += step) {
         const int token = first + slot;
         Row r;
         if (kTwice)
             r.rstd = token < length ? a.rstd[static_cast<int64_t>(worker) * a.tokens + token] : 0.0f;
-        else if (kLean)
-            ask(r, token);
-        else
+        else if (kAhead)
             r = next;
-        float u[kTwice ? 1 : kStrips][8], xhat[kTwice ? 1 : kStrips][8];
+        else
+            ask(r, token);
         float along = 0.0f;
+        float us[kKeep ? kStrips : 1][8], xhats[kKeep ? kStrips : 1][8];
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
-            const int at = kTwice ? 0 : j;
             if (kTwice) ask_strip(r, token, j, 0);
-            widen_strip(r, token, j, at, u[at], xhat[at]);
-            float m[8];
-            if constexpr (kLean) load_weight<kWay>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, m, turn);
+            float(&u)[8] = us[kKeep ? j : 0];
+            float(&xhat)[8] = xhats[kKeep ? j : 0];
+            weigh(r, token, j, u, xhat, [&](int k, float dy, float x) { dw[j][k] = fmaf(dy, x, dw[j][k]); });
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                dw[j][k] = fmaf(u[at][k], xhat[at][k], dw[j][k]);
-                u[at][k] *= kLean ? m[k] : w[kLean ? 0 : j][k];
-                along = fmaf(u[at][k], xhat[at][k], along);
-            }
+            for (int k = 0; k < 8; ++k) along = fmaf(u[k], xhat[k], along);
         }
-        if (!kTwice && !kLean && first + step < a.tokens) ask(next, first + step + slot);
+        if (kAhead && first + step < a.tokens) ask(next, first + step + slot);
         along = row_sum<kParts>(along, shared, slot, part) / static_cast<float>(a.d);
         if (token < a.tokens) {
 #pragma unroll
             for (int j = 0; j < kStrips; ++j) {
-                const int base = base_of(j), left = a.d - base, at = kTwice ? 0 : j;
+                const int base = base_of(j), left = a.d - base;
                 if (left <= 0) break;
-                if constexpr (kTwice) {
-                    ask_strip(r, token, j, 0);
-                    widen_strip(r, token, j, 0, u[0], xhat[0]);
-                    float m[8];
-                    load_weight<kWay>(weight + base, lane, left, a.weight_quads, m, turn);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) u[0][k] *= m[k];
-                }
+                if (kTwice) ask_strip(r, token, j, 0);
                 float dh[8] = {};
+                float(&u)[8] = us[kKeep ? j : 0];
+                float(&xhat)[8] = xhats[kKeep ? j : 0];
+                if constexpr (!kKeep) {
+                    if constexpr (!kTwice) {
+                        r.dy[j].forget();
+                        r.total[j].forget();
+                    }
+                    weigh(r, token, j, u, xhat, [](int, float, float) {});
+                }
                 if (a.dtotal.p != nullptr) {
-                    if constexpr (kLean) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, token < length ? left : 0);
-                    r.dtotal[kLean ? 0 : j].get(dh);
+                    if constexpr (!kHold) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, token < length ? left : 0);
+                    r.dtotal[kHold ? j : 0].get(dh);
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) dh[k] = fmaf(r.rstd, u[at][k] - xhat[at][k] * along, dh[k]);
+                for (int k = 0; k < 8; ++k) dh[k] = fmaf(r.rstd, u[k] - xhat[k] * along, dh[k]);
                 store_strip<kWay>(a.dx.row(worker, token) + base, lane, left, dh);
             }
         }

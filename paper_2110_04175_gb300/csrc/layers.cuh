@@ -105,6 +105,11 @@ struct Piece<T, kVector> {
                                    : make_uint4(0, 0, 0, 0);  // +0 in every type
     }
     __device__ __forceinline__ void get(float (&v)[8]) const { widen_octet(reinterpret_cast<const T*>(w), v); }
+    // Lets what was widened from here be widened again rather than kept.
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int h = 0; h < kWords; ++h) asm volatile("" : "+r"(w[h].x), "+r"(w[h].y), "+r"(w[h].z), "+r"(w[h].w));
+    }
 };
 
 template <Way kWay, typename T>
