@@ -520,22 +520,27 @@ struct Cut {
     int wide, splits;
 };
 
-// The cut that should take the least time, by what was measured: a pair takes 0.37 us
-// for a stage of a 256 x 256 tile and 0.26 us for one of 256 x 128 (more where two or
-// three terms keep the tensor cores longer), and 6 us for a tile besides; splits cost
-// the partial sums' way to memory and back and a launch.
+// The cut that should take the least time, by what was measured.  A stage of a 256 x 256
+// tile takes a pair 0.35 us with one term of dy and 0.36 us a term with more, one of
+// 256 x 128 0.215 us and 0.185 us a term; a tile besides 6.7 and 3.5 us (its results' way
+// to memory); splits a launch and the partial sums' way to memory and back.  Of 22 cuts
+// tried by hand the choice was within 6 % of the best but once, 14 % (4 x [2048 tokens, 2048 outputs,
+// 2048 inputs]: bf16 68 us in 256 and 76 us in 128, fp32 164 and 151 us;
+// [8192, 512, 512]: bf16 53 us in one piece and 15 us in splits).
 Cut best_cut(int terms, int64_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
     const int64_t stages = (tokens + kDepth - 1) / kDepth, pairs = kSms / 2;
+    const double results = 4e-6 / 5.0 * static_cast<double>(n * outputs * inputs);  // us at 5 TB/s
     Cut best{256, 1};
     double least = 0.0;
     for (const int wide : {256, 128}) {
         const int64_t tiles = tile_count(n, outputs, inputs, wide);
-        const double stage = wide == 256 ? (terms == 1 ? 0.37 : 0.32 * terms) : (terms == 1 ? 0.26 : 0.2 * terms);
-        for (int64_t splits = 1; splits <= pairs && (splits == 1 || (tiles * (splits - 1) < 2 * pairs && stages >= 4 * splits));
-             ++splits) {
+        const double stage = wide == 256 ? (terms == 1 ? 0.35 : 0.36 * terms) : (terms == 1 ? 0.215 : 0.185 * terms);
+        const double tile = wide == 256 ? 6.7 : 3.5;
+        // no more splits than fill the pairs twice, of at least 4 stages each
+        for (int64_t splits = 1; splits == 1 || (tiles * (splits - 1) < 2 * pairs && stages >= 4 * splits); ++splits) {
             const double rounds = static_cast<double>((tiles * splits + pairs - 1) / pairs);
-            double us = rounds * (6.0 + stage * static_cast<double>((stages + splits - 1) / splits));
-            if (splits > 1) us += 4.0 + 4e-6 * (splits + 1) * static_cast<double>(n * outputs * inputs) / 5.0;
+            double us = rounds * (tile + stage * static_cast<double>((stages + splits - 1) / splits));
+            if (splits > 1) us += 5.0 + results * static_cast<double>(2 * splits + 1);
             if ((wide == 256 && splits == 1) || us < least) least = us, best = Cut{wide, static_cast<int>(splits)};
         }
     }
