@@ -30,7 +30,8 @@
  *   - Weights.  A norm's weight and its gradient, the column scale and the
  *     weight gradient are fp32 views with a stride from worker to worker, of
  *     any alignment: they lie in the workers' model rows and in rows beside
- *     them.
+ *     them.  A weight that all workers share has stride 0, and a gradient
+ *     per worker.
  *   - Arithmetic is in fp32, and each output is rounded once, to the nearest
  *     (y and xhat come from the unrounded h).  The results of a call are the
  *     same bits every time: no atomics.
@@ -152,7 +153,9 @@ int64_t relay_weight_grad_workspace(int32_t type, int32_t n, int64_t tokens, int
 /* The weight gradient of a linear layer, per worker, from the gradient of its
  * outputs dy [n][tokens][outputs] and its inputs in 8 bits; overwrites
  * dweight: element (i, o, k) at dweight + i worker_stride + o row_stride + k.
- * column_scale (fp32, `inputs` per worker) may be NULL. */
+ * column_scale (fp32, `inputs` per worker) may be NULL.  The kernel's waits
+ * for copies and products end after about a second each; results that one of
+ * them was for are NaN then. */
 int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs, const relay_rows *dy,
                       const int8_t *codes, const uint8_t *scales, const float *column_scale,
                       int64_t column_scale_stride, const int32_t *lengths, float *dweight, int64_t worker_stride,

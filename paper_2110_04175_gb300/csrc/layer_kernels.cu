@@ -4,7 +4,12 @@
 //
 // All of them move rows and compute little, so memory bounds them.  A warp
 // works on strips of 256 features (layers.cuh); what a row needs twice stays in
-// registers between its two uses.
+// registers between its two uses.  Measured in bf16, bytes moved against the
+// 6.67 TB/s of a plain copy:
+//   norm, residual, 8-bit output and its recall   [4][4096][4096]  124 us  6.6 TB/s
+//   norm backward from 8 bits                     [4][4096][4096]   85 us  5.6 TB/s
+//   to 8 bits and back                            [4][4096][8192]  128 us  6.4 TB/s
+//   gated forward, backward, recall               [4][4096][8192]  425 us  6.4 TB/s
 #include "layers.cuh"
 
 namespace {
@@ -54,6 +59,8 @@ __device__ __forceinline__ void each_run(const Grid& g, F f) {
     }
 }
 
+// To 8 bits: a block's 32 features are four lanes' octets, its largest magnitude two
+// shuffles.  In 16 bits that is found two features at a time.  Bound by HBM.
 template <typename T, Way kWay>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_checkpoint_pack_kernel(Grid g, View<const T> x, int8_t* codes, uint8_t* scales) {
@@ -124,6 +131,9 @@ struct Sigmoid {
     }
 };
 
+// a = g sigma(g) u, and both inputs to 8 bits from the registers that they came to.  HBM
+// and issue are close: with libm's exponential, divisions and one strip at a time it took
+// 53 us for [1][4096][8192] with both checkpoints where it takes 44 us.
 template <typename T, Way kWay>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_kernel(Grid g, View<const T> gate, View<const T> up, View<T> out, int8_t* gate_codes,
@@ -161,6 +171,8 @@ struct GatedSource {  // one of the two
     const uint8_t *gate_scales, *up_scales;
 };
 
+// du = da g sigma(g) and dg = da u sigma(g) (1 + g (1 - sigma(g))), and a again.  54 us for
+// [1][4096][8192] from 8 bits and back to them (85 us one strip at a time).
 template <typename T, Way kWay, bool kEight>
 __global__ void __launch_bounds__(32 * kWarps)
 relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View<const T> up, GatedSource from,
@@ -249,7 +261,9 @@ __device__ __forceinline__ float row_sum(float v, float* shared, int slot, int p
 template <int kParts>
 constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
 
-// kParts warps share a row, each with kStrips strips of it in registers.
+// kParts warps share a row, each with kStrips strips of it in registers: h is formed once,
+// its squares summed over the CTA, and everything written from the registers, so that a
+// row crosses the chip once.  Sums are fp32, at most 80 additions in a chain.
 template <typename T, Way kWay, int kParts, int kStrips>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel(NormArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;

