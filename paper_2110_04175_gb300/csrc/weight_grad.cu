@@ -48,8 +48,10 @@ constexpr int kSms = 152;
 template <int kTerms>
 constexpr int kGroup = kTerms == 1 ? 8 : kTerms == 2 ? 4 : 3;
 
-// An adder's 32 rows x 16 columns on their way to memory, rows 80 bytes apart.
-constexpr int kTurnRow = 20, kTurn = 32 * kTurnRow * 4;
+// An adder's 32 rows x 32 columns on their way to memory, rows 144 bytes apart: whole
+// lines of 128 bytes a row (16 columns at a time took 268 us for 16 x [3114][4416] results
+// where this takes 213).  After them its columns' scales.
+constexpr int kTurnRow = 36, kTurnTile = 32 * kTurnRow * 4, kTurn = kTurnTile + 128 * 4;
 
 template <int kTerms, int kN>
 struct Stages {  // in a CTA
@@ -58,9 +60,9 @@ struct Stages {  // in a CTA
     static constexpr int kCodes = kN / 2 * kDepth;
     static constexpr int kRoom = 232448 - 1024 - 512 - kAdders * kTurn;  // less alignment, barriers
     static constexpr int kMost = (kRoom - 4 * kCodes) / kBytes, kCount = kMost < 4 ? kMost : 4;
-    static constexpr int kFit = (kRoom - kCount * kBytes) / kCodes, kAhead = kFit < 8 ? 4 : 8;
+    static constexpr int kFit = (kRoom - kCount * kBytes) / kCodes, kAhead = kFit < 8 ? kFit : 8;
     static constexpr int kShared = kCount * kBytes + kAhead * kCodes + kAdders * kTurn + 1024 + 512;
-    static_assert(kFit >= kAhead && kShared <= 232448, "shared memory of a CTA");
+    static_assert(kShared <= 232448, "shared memory of a CTA");
     // Teams at work: no more than stages.  A wait for a phase passes too when the barrier is
     // two phases behind, and a team that goes from stage i to stage i + teams knows only that
     // stage i - kCount was freed, which is the phase before the one it waits for if
@@ -116,6 +118,12 @@ __device__ __forceinline__ uint32_t piece(int j, int t) {
 __device__ __forceinline__ void put_shared(uint32_t at, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                  : "memory");
+}
+
+__device__ __forceinline__ float4 get_shared(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+    return v;
 }
 
 __device__ __forceinline__ uint32_t bits(__nv_bfloat162 v) { return *reinterpret_cast<uint32_t*>(&v); }
@@ -300,6 +308,14 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
         int group = 0;  // of all that the pair has summed
         for (int tile = pair; tile < a.tiles; tile += pairs) {
             const Tile at(a, tile, kN);
+            const int64_t o = at.o0 + kM * rank + row;  // this warp's first output and input
+            const int k0 = at.k0 + column;
+            for (int e = lane; e < kColumns; e += 32) {
+                float m = 1.0f;
+                if (a.column_scale != nullptr && a.splits == 1 && k0 + e < a.inputs)
+                    m = a.column_scale[at.worker * a.column_scale_stride + k0 + e];
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(turn + kTurnTile + 4 * e), "f"(m) : "memory");
+            }
             float sum[kColumns] = {};
             for (int done = 0; done < at.count && ok; done += kGroup<kTerms>, ++group) {
                 const int b = group & 1;
@@ -317,49 +333,43 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                 __syncwarp();
                 if (lane == 0) barrier_arrive(read(b));
             }
-            // through shared memory, so that a warp writes 64 contiguous bytes of each row
-            const int o = at.o0 + kM * rank + row;
+            if (!ok) {
+#pragma unroll
+                for (int e = 0; e < kColumns; ++e) sum[e] = __int_as_float(0x7fffffff);
+            }
+            // through shared memory, so that a warp writes whole lines of each row
             float* out = a.out + at.split * a.split_stride + at.worker * a.worker_stride;
-            const float* scale =
-                a.column_scale == nullptr || a.splits > 1 ? nullptr : a.column_scale + at.worker * a.column_scale_stride;
 #pragma unroll
-            for (int c = 0; c < kColumns; c += 16) {
-                const int k0 = at.k0 + column + c;
-                if (k0 < a.inputs) {
+            for (int c = 0; c < kColumns; c += 32) {
+                if (k0 + c >= a.inputs) break;
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        put_shared(turn + lane * (4 * kTurnRow) + 4 * e,
-                                   make_uint4(__float_as_uint(sum[c + e]), __float_as_uint(sum[c + e + 2]),
-                                              __float_as_uint(sum[c + e + 1]), __float_as_uint(sum[c + e + 3])));
-                    __syncwarp();
-                    if (a.out_quads) {
-                        const int k = k0 + 4 * (lane % 4);
-                        float4 m = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-                        if (scale != nullptr && k < a.inputs) m = make_float4(scale[k], scale[k + 1], scale[k + 2], scale[k + 3]);
-                        if (!ok) m.x = m.y = m.z = m.w = __int_as_float(0x7fffffff);
+                for (int e = 0; e < 32; e += 4)
+                    put_shared(turn + lane * (4 * kTurnRow) + 4 * e,
+                               make_uint4(__float_as_uint(sum[c + e]), __float_as_uint(sum[c + e + 2]),
+                                          __float_as_uint(sum[c + e + 1]), __float_as_uint(sum[c + e + 3])));
+                __syncwarp();
+                if (a.out_quads) {
+                    const int k = k0 + c + 4 * (lane % 8);
+                    const float4 m = get_shared(turn + kTurnTile + 4 * c + 16 * (lane % 8));
+                    float* to = out + (o + lane / 8) * a.row_stride + k;
 #pragma unroll
-                        for (int r = lane / 4; r < 32; r += 8) {
-                            float4 v;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                         : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                                         : "r"(turn + r * (4 * kTurnRow) + 16 * (lane % 4)));
-                            v.x *= m.x, v.y *= m.y, v.z *= m.z, v.w *= m.w;
-                            if (o + r < a.outputs && k < a.inputs)
-                                *reinterpret_cast<float4*>(out + (o + r) * a.row_stride + k) = v;
-                        }
-                    } else {
-                        const int k = k0 + lane % 16;
-                        float m = scale == nullptr || k >= a.inputs ? 1.0f : scale[k];
-                        if (!ok) m = __int_as_float(0x7fffffff);
-#pragma unroll 4
-                        for (int r = lane / 16; r < 32; r += 2) {
-                            float v;
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(turn + r * (4 * kTurnRow) + 4 * (lane % 16)));
-                            if (o + r < a.outputs && k < a.inputs) out[(o + r) * a.row_stride + k] = v * m;
-                        }
+                    for (int r = lane / 8; r < 32; r += 4, to += 4 * a.row_stride) {
+                        float4 v = get_shared(turn + r * (4 * kTurnRow) + 16 * (lane % 8));
+                        v.x *= m.x, v.y *= m.y, v.z *= m.z, v.w *= m.w;
+                        if (o + r < a.outputs && k < a.inputs) *reinterpret_cast<float4*>(to) = v;
                     }
-                    __syncwarp();
+                } else {
+                    const int k = k0 + c + lane;
+                    float m, v;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(m) : "r"(turn + kTurnTile + 4 * (c + lane)));
+                    float* to = out + o * a.row_stride + k;
+#pragma unroll 8
+                    for (int r = 0; r < 32; ++r, to += a.row_stride) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(turn + r * (4 * kTurnRow) + 4 * lane));
+                        if (o + r < a.outputs && k < a.inputs) *to = v * m;
+                    }
                 }
+                __syncwarp();
             }
         }
     } else if (warp < kMaker) {
