@@ -239,7 +239,7 @@ struct NormArgs {
     float* rstd;
     int8_t* codes;
     uint8_t* scales;
-    int32_t rows, tokens, d, pitch;
+    int32_t tokens, d, pitch;
 };
 
 // The sum of v over the kParts warps of a row (each warp's lanes included), the
@@ -261,54 +261,97 @@ __device__ __forceinline__ float row_sum(float v, float* shared, int slot, int p
 template <int kParts>
 constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
 
+// Whether the norm's CTAs stay and take row after row, the next one asked for before this
+// one's sum and the weight in registers: aligned 16-bit rows of up to 8192 features.  Rows
+// of fp32 keep HBM as busy one CTA each (6.6 TB/s with the residual), 16-bit ones do not
+// ([4][4096][4096], no residual: 57 us).
+template <typename T, Way kWay, int kStrips>
+constexpr bool kStays = kWay == kVector && kStrips <= 2 && sizeof(T) == 2;
+
+// CTAs per SM that the norm's registers have to leave room for.
+template <typename T, Way kWay, int kParts, int kStrips>
+constexpr int kNormCtas = kParts > 16    ? 1
+                          : kParts == 16 ? (kStays<T, kWay, kStrips> ? 1 : 2)
+                                         : (kStays<T, kWay, kStrips> ? 3 : 5);
+
 // kParts warps share a row, each with kStrips strips of it in registers: h is formed once,
 // its squares summed over the CTA, and everything written from the registers, so that a
-// row crosses the chip once.  Sums are fp32, at most 80 additions in a chain.
+// row crosses the chip once.  Sums are fp32, at most 80 additions in a chain.  CTA (p, i)
+// takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i.
 template <typename T, Way kWay, int kParts, int kStrips>
-__global__ void __launch_bounds__(32 * kNormWarps<kParts>) relay_rms_norm_kernel(NormArgs<T> a) {
+__global__ void __launch_bounds__(32 * kNormWarps<kParts>, (kNormCtas<T, kWay, kParts, kStrips>))
+relay_rms_norm_kernel(NormArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
+    constexpr bool kAhead = kStays<T, kWay, kStrips>;
     __shared__ float shared[kNormWarps<kParts>];
     WARP_TURN(kNormWarps<kParts>, true);  // kVector: for unaligned weights
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot;
-    const bool on = row < a.rows;
-    const int worker = on ? static_cast<int>(row / a.tokens) : 0;
-    const int token = on ? static_cast<int>(row - static_cast<int64_t>(worker) * a.tokens) : 0;
-    float h[kStrips][8];
-    float squares = 0.0f;
+    const int worker = blockIdx.y, step = static_cast<int>(gridDim.x) * kRows;
+    const float* weight = a.weight + worker * a.weight_stride;
+    const auto base_of = [&](int j) { return (part + kParts * j) * kStrip; };
+
+    Piece<T, kWay> x[kAhead ? kStrips : 1], r[kAhead ? kStrips : 1];
+    const auto ask_strip = [&](int token, int j, int to) {
+        const int left = token < a.tokens ? a.d - base_of(j) : 0;
+        x[to].load(a.x.row(worker, token) + base_of(j), lane, left);
+        if (a.residual.p != nullptr) r[to].load(a.residual.row(worker, token) + base_of(j), lane, left);
+    };
+    const auto ask = [&](int token) {
 #pragma unroll
-    for (int j = 0; j < kStrips; ++j) {
-        const int base = (part + kParts * j) * kStrip, left = on ? a.d - base : 0;
-        load_strip<kWay>(a.x.row(worker, token) + base, lane, left, h[j]);
-        if (a.residual.p != nullptr) {
-            float r[8];
-            load_strip<kWay>(a.residual.row(worker, token) + base, lane, left, r);
+        for (int j = 0; j < kStrips; ++j) ask_strip(token, j, kAhead ? j : 0);
+    };
+    float w[kAhead ? kStrips : 1][8];
+    int first = static_cast<int>(blockIdx.x) * kRows;
+    if (kAhead) {
+        ask(first + slot);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[j][k] += r[k];
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) squares = fmaf(h[j][k], h[j][k], squares);
+        for (int j = 0; j < kStrips; ++j)
+            load_weight<kWay>(weight + base_of(j), lane, a.d - base_of(j), a.weight_quads, w[kAhead ? j : 0], turn);
     }
-    squares = row_sum<kParts>(squares, shared, slot, part);
-    if (!on) return;
-    const float rstd = 1.0f / sqrtf(squares / static_cast<float>(a.d) + a.eps);
-    if (a.rstd != nullptr && part == 0 && lane == 0) a.rstd[row] = rstd;
+    for (; first < a.tokens; first += step) {
+        const int token = first + slot;
+        const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
+        float h[kStrips][8];
+        float squares = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kStrips; ++j) {
-        const int base = (part + kParts * j) * kStrip, left = a.d - base;
-        if (base >= a.pitch) break;
-        if (a.total.p != nullptr) store_strip<kWay>(a.total.row(worker, token) + base, lane, left, h[j]);
+        for (int j = 0; j < kStrips; ++j) {
+            if (!kAhead) ask_strip(token, j, 0);
+            x[kAhead ? j : 0].get(h[j]);
+            if (a.residual.p != nullptr) {
+                float add[8];
+                r[kAhead ? j : 0].get(add);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) h[j][k] *= rstd;
-        clear_past<kWay>(h[j], lane, left);
-        if (a.codes != nullptr)
-            put_strip<kWay>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j],
-                      kWay == kVector ? largest(h[j]) : 0u, turn);
-        float w[8];
-        load_weight<kWay>(a.weight + worker * a.weight_stride + base, lane, left, a.weight_quads, w, turn);
+                for (int k = 0; k < 8; ++k) h[j][k] += add[k];
+            }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) h[j][k] *= w[k];
-        store_strip<kWay>(a.y.row(worker, token) + base, lane, left, h[j]);
+            for (int k = 0; k < 8; ++k) squares = fmaf(h[j][k], h[j][k], squares);
+        }
+        if (kAhead && first + step < a.tokens) ask(first + step + slot);
+        squares = row_sum<kParts>(squares, shared, slot, part);
+        if (token >= a.tokens) {
+            if (!kAhead) break;
+            continue;
+        }
+        const float rstd = 1.0f / sqrtf(squares / static_cast<float>(a.d) + a.eps);
+        if (a.rstd != nullptr && part == 0 && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int j = 0; j < kStrips; ++j) {
+            const int base = base_of(j), left = a.d - base;
+            if (base >= a.pitch) break;
+            if (a.total.p != nullptr) store_strip<kWay>(a.total.row(worker, token) + base, lane, left, h[j]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[j][k] *= rstd;
+            clear_past<kWay>(h[j], lane, left);
+            if (a.codes != nullptr)
+                put_strip<kWay>(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), base, lane, a.pitch, h[j],
+                                kWay == kVector ? largest(h[j]) : 0u, turn);
+            float m[8];
+            if (!kAhead) load_weight<kWay>(weight + base, lane, left, a.weight_quads, m, turn);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[j][k] *= kAhead ? w[kAhead ? j : 0][k] : m[k];
+            store_strip<kWay>(a.y.row(worker, token) + base, lane, left, h[j]);
+        }
+        if (!kAhead) break;  // one row each
     }
 }
 
@@ -605,13 +648,17 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
         const NormArgs<T> a{view<const T>(x, n, tokens), view<const T>(residual, n, tokens),
                             view<T>(total, n, tokens), view<T>(y, n, tokens), weight, n > 1 ? weight_stride : 0,
                             d % 8 == 0 && aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), eps, rstd, codes, scales,
-                            static_cast<int32_t>(n * tokens), static_cast<int32_t>(tokens), static_cast<int32_t>(d),
+                            static_cast<int32_t>(tokens), static_cast<int32_t>(d),
                             static_cast<int32_t>(pitch_of(d))};
         return by_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr int kRows = kNormWarps<kParts> / kParts;
+            // three CTAs per SM where they stay, over all workers, otherwise one for each row (or kRows of them)
+            const int64_t all = (tokens + kRows - 1) / kRows, stay = 3 * 152 / n > 0 ? 3 * 152 / n : 1;
+            const bool stays = vec && kStays<T, kVector, kStrips>;
+            const dim3 grid(static_cast<unsigned>(stays && stay < all ? stay : all), static_cast<unsigned>(n));
             (vec ? relay_rms_norm_kernel<T, kVector, kParts, kStrips> : relay_rms_norm_kernel<T, kDirect, kParts, kStrips>)
-                <<<(a.rows - 1) / kRows + 1, 32 * kNormWarps<kParts>, 0, stream>>>(a);
+                <<<grid, 32 * kNormWarps<kParts>, 0, stream>>>(a);
             return status_of_launch();
         });
     });
