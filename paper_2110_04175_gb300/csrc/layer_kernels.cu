@@ -6,10 +6,11 @@
 // works on strips of 256 features (layers.cuh); what a row needs twice stays in
 // registers between its two uses.  Measured in bf16, bytes moved against the
 // 6.67 TB/s of a plain copy:
-//   norm, residual, 8-bit output and its recall   [4][4096][4096]  124 us  6.6 TB/s
-//   norm backward from 8 bits                     [4][4096][4096]   85 us  5.6 TB/s
-//   to 8 bits and back                            [4][4096][8192]  128 us  6.4 TB/s
-//   gated forward, backward, recall               [4][4096][8192]  425 us  6.4 TB/s
+//   norm, residual, 8-bit output        [4][4096][4096]   92 us  6.6 TB/s
+//   norm backward from 8 bits           [4][4096][4096]   84 us  5.6 TB/s
+//   to 8 bits and back                  [4][4096][8192]  128 us  6.4 TB/s
+//   gated, both inputs put away         [4][4096][8192]  162 us  6.7 TB/s
+//   gated backward from 8 bits          [4][4096][8192]  200 us  6.1 TB/s
 #include "layers.cuh"
 
 namespace {
@@ -261,28 +262,27 @@ __device__ __forceinline__ float row_sum(float v, float* shared, int slot, int p
 template <int kParts>
 constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
 
-// Whether the norm's CTAs stay and take row after row, the next one asked for before this
-// one's sum and the weight in registers: aligned 16-bit rows of up to 8192 features.  Rows
-// of fp32 keep HBM as busy one CTA each (6.6 TB/s with the residual), 16-bit ones do not
-// ([4][4096][4096], no residual: 57 us).
+// Rows of which the norm's CTAs may stay and take one after the other, the next asked for
+// before this one's sum and the weight in registers (kAhead): aligned 16-bit rows of up to
+// 8192 features.  That pays where little moves per row ([4][4096][4096], us, one CTA a row
+// and staying: no residual 57 and 48, with residual 80 and 85, and an 8-bit output 91 and
+// 101) or rows are wide ([4][1024][8192], residual: 52 and 46), so it is done without a
+// residual and past 4096 features.  Rows of fp32 keep HBM as busy one CTA each.
 template <typename T, Way kWay, int kStrips>
-constexpr bool kStays = kWay == kVector && kStrips <= 2 && sizeof(T) == 2;
+constexpr bool kMayStay = kWay == kVector && kStrips <= 2 && sizeof(T) == 2;
 
 // CTAs per SM that the norm's registers have to leave room for.
-template <typename T, Way kWay, int kParts, int kStrips>
-constexpr int kNormCtas = kParts > 16    ? 1
-                          : kParts == 16 ? (kStays<T, kWay, kStrips> ? 1 : 2)
-                                         : (kStays<T, kWay, kStrips> ? 3 : 5);
+template <int kParts, bool kAhead>
+constexpr int kNormCtas = kParts > 16 ? 1 : kParts == 16 ? (kAhead ? 1 : 2) : (kAhead ? 3 : 5);
 
 // kParts warps share a row, each with kStrips strips of it in registers: h is formed once,
 // its squares summed over the CTA, and everything written from the registers, so that a
 // row crosses the chip once.  Sums are fp32, at most 80 additions in a chain.  CTA (p, i)
 // takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i.
-template <typename T, Way kWay, int kParts, int kStrips>
-__global__ void __launch_bounds__(32 * kNormWarps<kParts>, (kNormCtas<T, kWay, kParts, kStrips>))
+template <typename T, Way kWay, int kParts, int kStrips, bool kAhead>
+__global__ void __launch_bounds__(32 * kNormWarps<kParts>, (kNormCtas<kParts, kAhead>))
 relay_rms_norm_kernel(NormArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
-    constexpr bool kAhead = kStays<T, kWay, kStrips>;
     __shared__ float shared[kNormWarps<kParts>];
     WARP_TURN(kNormWarps<kParts>, true);  // kVector: for unaligned weights
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
@@ -656,9 +656,12 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
             constexpr int kRows = kNormWarps<kParts> / kParts;
             // three CTAs per SM where they stay, over all workers, otherwise one for each row (or kRows of them)
             const int64_t all = (tokens + kRows - 1) / kRows, stay = 3 * 152 / n > 0 ? 3 * 152 / n : 1;
-            const bool stays = vec && kStays<T, kVector, kStrips>;
+            constexpr bool kMay = kMayStay<T, kVector, kStrips>;
+            const bool stays = kMay && vec && (residual == nullptr || a.pitch > 4096);
             const dim3 grid(static_cast<unsigned>(stays && stay < all ? stay : all), static_cast<unsigned>(n));
-            (vec ? relay_rms_norm_kernel<T, kVector, kParts, kStrips> : relay_rms_norm_kernel<T, kDirect, kParts, kStrips>)
+            (stays ? relay_rms_norm_kernel<T, kVector, kParts, kStrips, kMay>
+             : vec ? relay_rms_norm_kernel<T, kVector, kParts, kStrips, false>
+                   : relay_rms_norm_kernel<T, kDirect, kParts, kStrips, false>)
                 <<<grid, 32 * kNormWarps<kParts>, 0, stream>>>(a);
             return status_of_launch();
         });
