@@ -71,14 +71,26 @@ __device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity) {
     return done != 0;
 }
 
+constexpr long long kPatience = 2000000000ll;  // cycles, about a second
+
 // Waits for the phase of `parity` to end; false after about a second, when the
-// caller gives up, so that no wait can hold the GPU.
+// caller gives up, so that no wait can hold the GPU.  One thread.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
     if (barrier_passed(bar, parity)) return true;
     const long long start = clock64();
     do {
         if (barrier_passed(bar, parity)) return true;
-    } while (clock64() - start < 2000000000ll);
+    } while (clock64() - start < kPatience);
+    return false;
+}
+
+// The same for all lanes of a warp, which go on or give up together.
+__device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity) {
+    if (__all_sync(0xffffffffu, barrier_passed(bar, parity))) return true;
+    const long long start = clock64();
+    do {
+        if (__all_sync(0xffffffffu, barrier_passed(bar, parity))) return true;
+    } while (__all_sync(0xffffffffu, clock64() - start < kPatience));
     return false;
 }
 

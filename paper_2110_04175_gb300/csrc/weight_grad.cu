@@ -320,7 +320,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
             float sum[kColumns] = {};
             for (int done = 0; done < at.count && ok; done += kGroup<kTerms>, ++group) {
                 const int b = group & 1;
-                if (!(ok = barrier_wait(summed(b), group >> 1 & 1))) break;
+                if (!(ok = barrier_wait_warp(summed(b), group >> 1 & 1))) break;
                 tensor_fence_after();
                 const uint32_t from = tensor + (static_cast<uint32_t>(row) << 16) + b * kN + column;
 #pragma unroll
@@ -383,8 +383,8 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                 for (int n = 0; n < at.count; ++n, ++i) {
                     const int s = i % kCount, place = n % kGroup<kTerms>, b = group & 1;
                     const uint32_t left = stages + s * S::kBytes;
-                    if (place == 0 && group > 1 && !(ok = barrier_wait(read(b), (group >> 1 & 1) ^ 1))) break;
-                    if (!(ok = barrier_wait(full(s), i / kCount & 1))) break;
+                    if (place == 0 && group > 1 && !(ok = barrier_wait_warp(read(b), (group >> 1 & 1) ^ 1))) break;
+                    if (!(ok = barrier_wait_warp(full(s), i / kCount & 1))) break;
                     const int from = at.length - (at.first + n) * kDepth;
                     if (kTerms == 1 && from < kDepth) {  // the copy brought the rows past the length too, whatever they hold
                         for (int e = from * 8 + lane; e < kDepth * 8; e += 32)
@@ -489,8 +489,8 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                     now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
                     next = load_next();
                 }
-                if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-                if (!(ok = barrier_wait(fetched(f), i / S::kAhead & 1))) break;
+                if (!(ok = barrier_wait_warp(freed(s), (i / kCount & 1) ^ 1))) break;
+                if (!(ok = barrier_wait_warp(fetched(f), i / S::kAhead & 1))) break;
                 R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
                 fence_async();
                 __syncwarp();
