@@ -22,10 +22,10 @@
 // other warps add the other one to registers, rounded to the nearest: 4e-7 against
 // 64 bits at 8192 tokens.
 //
-// Measured: 2 x [8192 tokens, 8192 outputs, 4096 inputs], 1.1 TFLOP, takes 0.68 ms in bf16
-// (1610 TFLOP/s, 0.83 of what a library product of 8192^3 does in a burst; 0.75 ms back to
-// back, when power holds the clock), 1.27 ms in fp16 and 2.07 ms in fp32.  A stage of 64
-// tokens takes a pair 610 cycles where its products take 512: shared memory carries 80 KB
+// Measured: 2 x [8192 tokens, 8192 outputs, 4096 inputs], 1.1 TFLOP, takes 0.70 ms in bf16
+// (1570 TFLOP/s, 0.81 of what a library product of 8192^3 does in a burst; 0.77 ms back to
+// back, when power holds the clock), 1.27 ms in fp16 and 2.08 ms in fp32.  A stage of 64
+// tokens takes a pair 620 cycles where its products take 512: shared memory carries 80 KB
 // per SM and stage.  Where tokens are few, the results' way to memory bounds it
 // (16 x [2 tokens, 3114, 4416]: 3.9 TB/s).
 #include "blackwell.cuh"
