@@ -110,20 +110,24 @@ relay_checkpoint_unpack_kernel(Grid g, const int8_t* codes, const uint8_t* scale
     });
 }
 
-// sigma(g) and 1 - sigma(g) without cancellation.  Rows of 16 bits take the hardware's
-// exponential and reciprocal: with e = exp(-g) they are 1 / (1 + e) and e / (1 + e),
-// off by less than (3 + 2 |g|) 2^-23 relative, far below the rows' rounding; e is held
-// at 2^126, where sigma(g) is 2^-126, so that neither turns into 0 times infinity.  fp32
-// rows take the exact ones, of exp(-|g|), in the order that the sign of g gives.
+// sigma(g) and 1 - sigma(g).  Rows of 16 bits take the hardware's exponential and reciprocal:
+// with e = exp(-g), sigma(g) = 1 / (1 + e) is off by less than (3 + 2 |g|) 2^-23 relative, far
+// below the rows' rounding.  It is made from e / 4: the reciprocal, 4 sigma(g), is then a normal
+// number down to sigma(g) = 2^-128 (g = -88.7), about where exp(-g) ends in fp32; below, sigma(g)
+// is 0.  (Holding e at 2^126 instead left g sigma(g) growing with |g|: -4 at bf16's lowest value.)
+// The difference from 1 is off by 2^-23 and exactly 0 where sigma(g) is 1 (g > 17: the reciprocal
+// of a power of two is exact), so g times it is off by 2e-6 at most.  fp32 rows take the exact
+// ones, of exp(-|g|), in the order that the sign of g gives, both without cancellation.
 template <typename T>
 struct Sigmoid {
     float at, rest;
     __device__ __forceinline__ explicit Sigmoid(float g) {
         if constexpr (sizeof(T) == 2) {
-            float e;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(g * -1.44269504f, 126.0f)));
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(at) : "f"(1.0f + e));
-            rest = e * at;
+            float e, r;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(g, -1.44269504f, -2.0f)));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(0.25f + e));
+            at = 0.25f * r;
+            rest = 1.0f - at;
         } else {
             const float e = expf(-fabsf(g)), r = 1.0f / (1.0f + e);
             at = g < 0.0f ? e * r : r;
@@ -172,10 +176,15 @@ struct GatedSource {  // one of the two
     const uint8_t *gate_scales, *up_scales;
 };
 
-// du = da g sigma(g) and dg = da u sigma(g) (1 + g (1 - sigma(g))), and a again.  54 us for
-// [1][4096][8192] from 8 bits and back to them (85 us one strip at a time).
+// du = da g sigma(g) and dg = da u (sigma(g) + g sigma(g) (1 - sigma(g))), and a again.  54 us for
+// [1][4096][8192] from 8 bits and back to them (85 us one strip at a time).  Aligned 16-bit
+// rows from 8 bits keep within the 64 registers that leave room for four CTAs per SM (with
+// three, [4][4096][8192] takes 227 us, with four 190); the others get what they take anyway.
 template <typename T, Way kWay, bool kEight>
-__global__ void __launch_bounds__(32 * kWarps)
+constexpr int kGatedBackwardCtas = kWay == kVector && sizeof(T) == 2 ? (kEight ? 4 : 3) : sizeof(T) == 4 && kEight ? 3 : 2;
+
+template <typename T, Way kWay, bool kEight>
+__global__ void __launch_bounds__(32 * kWarps, (kGatedBackwardCtas<T, kWay, kEight>))
 relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View<const T> up, GatedSource from,
                             View<T> dgate, View<T> dup, int8_t* out_codes, uint8_t* out_scales) {
     WARP_TURN(kWarps, kWay == kDirect);
@@ -212,9 +221,9 @@ relay_gated_backward_kernel(Grid g, View<const T> dout, View<const T> gate, View
             for (int k = 0; k < 8; ++k) {
                 const Sigmoid<T> s(a[k]);
                 const float silu = a[k] * s.at;
-                dg[k] = da[k] * b[k] * s.at * fmaf(a[k], s.rest, 1.0f);
-                da[k] *= silu;
                 a[k] = silu * b[k];
+                dg[k] = fmaf(silu, s.rest, s.at) * b[k] * da[k];
+                da[k] *= silu;
             }
             store_strip<kWay>(dgate.row(worker, token) + first, lane, left, dg);
             store_strip<kWay>(dup.row(worker, token) + first, lane, left, da);
