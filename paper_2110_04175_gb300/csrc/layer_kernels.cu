@@ -488,23 +488,28 @@ relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {
             for (int j = 0; j < kStrips; ++j) {
                 const int base = base_of(j), left = a.d - base;
                 if (left <= 0) break;
-                if (kTwice) ask_strip(r, token, j, 0);
                 float dh[8] = {};
-                float(&u)[8] = us[kKeep ? j : 0];
-                float(&xhat)[8] = xhats[kKeep ? j : 0];
-                if constexpr (!kKeep) {
-                    if constexpr (!kTwice) {
-                        r.dy[j].forget();
-                        r.total[j].forget();
+                // padding is 0 also where 0 times the weight is not: by a branch, or element by element
+                // where that goes faster ([2][2048][16384] from 8 bits: 102 us and 97 us)
+                const bool counts = token < length;
+                if (!kHold || counts) {
+                    if (kTwice) ask_strip(r, token, j, 0);
+                    float(&u)[8] = us[kKeep ? j : 0];
+                    float(&xhat)[8] = xhats[kKeep ? j : 0];
+                    if constexpr (!kKeep) {
+                        if constexpr (!kTwice) {
+                            r.dy[j].forget();
+                            r.total[j].forget();
+                        }
+                        weigh(r, token, j, u, xhat, [](int, float, float) {});
                     }
-                    weigh(r, token, j, u, xhat, [](int, float, float) {});
-                }
-                if (a.dtotal.p != nullptr) {
-                    if constexpr (!kHold) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, token < length ? left : 0);
-                    r.dtotal[kHold ? j : 0].get(dh);
-                }
+                    if (a.dtotal.p != nullptr) {
+                        if constexpr (!kHold) r.dtotal[0].load(a.dtotal.row(worker, token) + base, lane, counts ? left : 0);
+                        r.dtotal[kHold ? j : 0].get(dh);
+                    }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) dh[k] = fmaf(r.rstd, u[k] - xhat[k] * along, dh[k]);
+                    for (int k = 0; k < 8; ++k) dh[k] = kHold || counts ? fmaf(r.rstd, u[k] - xhat[k] * along, dh[k]) : 0.0f;
+                }
                 store_strip<kWay>(a.dx.row(worker, token) + base, lane, left, dh);
             }
         }

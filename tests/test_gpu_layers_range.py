@@ -1,4 +1,5 @@
-"""The layer operators at the ends of their range: gates down to the type's lowest value."""
+"""The layer operators at the ends of their range: gates down to the type's lowest value, weights
+that are not finite beside padding."""
 import numpy as np
 import pytest
 import torch
@@ -10,6 +11,7 @@ from . import layers_util as lu
 from .layers_util import LEAST, ROUND, TYPES, U, np64, within
 
 pytestmark = pytest.mark.gpu
+EPS = 1e-5
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -97,3 +99,38 @@ def test_gates_of_any_size(dtype, layout):
         rs.relay_gated_backward(dv, ov, pv, gate_checkpoint=kg, up_checkpoint=ku)
         _same(pv, du, _rounded(du, dtype, _sigma_error(g, dtype) * np.abs(du)))
         _same(ov, dg, _rounded(dg, dtype, dg_bound))
+
+
+# ------------------------------------------------------------------ padding
+
+
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
+@pytest.mark.parametrize("layout", ["dense", "odd"])
+@pytest.mark.parametrize("source", ["checkpoint", "total"])
+@pytest.mark.parametrize("d", [64, 500, 1000, 2048, 4096, 8192, 16384, 20000])
+def test_padding_is_zero_whatever_the_weight(dtype, layout, source, d):
+    """dx past the lengths is 0 also where a worker's weight holds an infinity or a NaN, which
+    reaches that worker's other rows only."""
+    n, T, lengths = 3, 4, [2, 0, 3]
+    g = np.random.default_rng(0)
+    h, dy, dh = (_held_by(g.standard_normal((n, T, d)), dtype) for _ in range(3))
+    rstd = torch.from_numpy(1 / np.sqrt((h * h).mean(-1) + EPS)).float().cuda()
+    kw = {"lengths": torch.tensor(lengths, dtype=torch.int32, device="cuda"), "dtotal": lu.rows(dh, dtype, layout)[0]}
+    if source == "checkpoint":
+        kw["checkpoint"] = rs.ActivationCheckpoint(n, T, d).pack(lu.rows(h, dtype, "dense")[0])
+    else:
+        kw["total"] = lu.rows(h, dtype, layout)[0]
+    good = torch.ones(n, d, device="cuda")
+    bad = good.clone()
+    bad[0, d // 2], bad[1, 0], bad[1, d - 1] = float("inf"), float("nan"), float("-inf")
+    work = torch.empty(rs.relay_rms_norm_backward_workspace(n, T, d), dtype=torch.uint8, device="cuda")
+    results = []
+    for w in (good, bad):
+        dx, dw = lu.empty_rows(n, T, d, dtype, layout)[0], torch.empty(n, d, device="cuda")
+        rs.relay_rms_norm_backward(lu.rows(dy, dtype, layout)[0], w, rstd, dx, dw, work, **kw)
+        for i, m in enumerate(lengths):
+            assert not dx[i, m:].any()  # (NaN is true)
+        results.append((dx, dw))
+    (dx, dw), (dx_bad, dw_bad) = results
+    assert torch.equal(dw, dw_bad) and torch.equal(dx[2], dx_bad[2])
+    assert dx_bad[0, :2, d // 2].isnan().all()
