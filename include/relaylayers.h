@@ -143,10 +143,13 @@ int relay_gated_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, con
                          relay_stream_t stream);
 
 /* Bytes of workspace for relay_weight_grad (may be 0), or a negative status.
- * dy: the rows that it will get, or NULL for any strides and alignment.  fp16
- * and fp32 rows, and bf16 rows that are not 16-byte aligned or that repeat,
- * are copied into it (2, 3 or 1 times 2 bytes an element).  The size for
- * RELAY_FP32 and NULL is enough for every call of the other sizes. */
+ * dy: the rows that it will get, for which this is the exact size, or NULL for
+ * any strides and alignment.  fp16 and fp32 rows, and bf16 rows that are not
+ * 16-byte aligned or that repeat, are copied into it (2, 3 or 1 times 2 bytes
+ * an element); the rest are the sums of splits of the tokens.  The size for
+ * NULL is enough for every call of the type with the same n, outputs and
+ * inputs and as many tokens or fewer, that for RELAY_FP32 and NULL for every
+ * type. */
 int64_t relay_weight_grad_workspace(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs,
                                     const relay_rows *dy);
 

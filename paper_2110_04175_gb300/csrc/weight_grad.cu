@@ -537,6 +537,13 @@ struct Cut {
     int wide, splits;
 };
 
+// No more splits than fill the pairs twice, of at least 4 stages each.
+int64_t most_splits(int64_t tiles, int64_t stages) {
+    const int64_t fill = (kSms + tiles - 1) / tiles, deep = stages / 4;
+    const int64_t most = fill < deep ? fill : deep;
+    return most > 1 ? most : 1;
+}
+
 // The cut that should take the least time, by what was measured.  A stage of a 256 x 256
 // tile takes a pair 0.35 us with one term of dy and 0.36 us a term with more, one of
 // 256 x 128 0.215 us and 0.185 us a term; a tile besides 6.7 and 3.5 us (its results' way
@@ -553,8 +560,7 @@ Cut best_cut(int terms, int64_t n, int64_t tokens, int64_t outputs, int64_t inpu
         const int64_t tiles = tile_count(n, outputs, inputs, wide);
         const double stage = wide == 256 ? (terms == 1 ? 0.35 : 0.36 * terms) : (terms == 1 ? 0.215 : 0.185 * terms);
         const double tile = wide == 256 ? 6.7 : 3.5;
-        // no more splits than fill the pairs twice, of at least 4 stages each
-        for (int64_t splits = 1; splits == 1 || (tiles * (splits - 1) < 2 * pairs && stages >= 4 * splits); ++splits) {
+        for (int64_t splits = 1; splits <= most_splits(tiles, stages); ++splits) {
             const double rounds = static_cast<double>((tiles * splits + pairs - 1) / pairs);
             double us = rounds * (tile + stage * static_cast<double>((stages + splits - 1) / splits));
             if (splits > 1) us += 5.0 + results * static_cast<double>(2 * splits + 1);
@@ -613,8 +619,7 @@ int64_t terms_bytes(int32_t type, const relay_rows* dy, int32_t n, int64_t token
     if (direct(type, dy, n, tokens, outputs)) return 0;
     return 2 * terms_of(type) * n * tokens * width_of(outputs);
 }
-int64_t partial_bytes(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs) {
-    const int splits = best_cut(terms_of(type), n, tokens, outputs, inputs).splits;
+int64_t partial_bytes(int64_t splits, int32_t n, int64_t outputs, int64_t inputs) {
     return splits > 1 ? 4 * splits * n * outputs * inputs : 0;
 }
 
@@ -688,7 +693,11 @@ int64_t relay_weight_grad_workspace(int32_t type, int32_t n, int64_t tokens, int
     if (const int rc = check_shape(type, n, tokens, inputs)) return rc;
     if (const int rc = check_shape(type, n, tokens, outputs)) return rc;
     if (inputs > RELAY_WEIGHT_GRAD_MAX_INPUTS) return RELAY_EUNSUPPORTED;
-    return terms_bytes(type, dy, n, tokens, outputs) + partial_bytes(type, n, tokens, outputs, inputs);
+    // without dy, the most splits that any type and any smaller number of tokens may take
+    const int64_t splits = dy == nullptr
+                               ? most_splits(tile_count(n, outputs, inputs, 256), (tokens + kDepth - 1) / kDepth)
+                               : best_cut(terms_of(type), n, tokens, outputs, inputs).splits;
+    return terms_bytes(type, dy, n, tokens, outputs) + partial_bytes(splits, n, outputs, inputs);
 }
 
 int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, int64_t inputs, const relay_rows* dy,

@@ -263,12 +263,13 @@ def relay_gated_backward(dout, dgate, dup, gate=None, up=None, gate_checkpoint=N
 
 def relay_weight_grad_workspace(n: int, tokens: int, outputs: int, inputs: int, dy=None) -> int:
     """Bytes of workspace for relay_weight_grad: for the tensor dy, or without one enough
-    for any type and strides.  Rows that are not bf16 on 16-byte boundaries are copied
-    into it as bf16 terms; for those that are it is 0, or the split sums of few outputs."""
+    for any type and strides and for fewer tokens too.  Rows that are not bf16 on 16-byte
+    boundaries are copied into it as bf16 terms; for those that are it is 0, or the split
+    sums of few outputs."""
     lib = _library()
     if dy is None:
-        return _bytes(max(lib.relay_weight_grad_workspace(t, n, tokens, outputs, inputs, None)
-                          for t in (RELAY_BF16, RELAY_FP16, RELAY_FP32)), "relay_weight_grad_workspace")
+        return _bytes(lib.relay_weight_grad_workspace(RELAY_FP32, n, tokens, outputs, inputs, None),
+                      "relay_weight_grad_workspace")
     type_, *_ = _shape_of("dy", dy)
     return _bytes(lib.relay_weight_grad_workspace(type_, n, tokens, outputs, inputs,
                                                   _rows("dy", dy, dy.dtype, (n, tokens, outputs))),
