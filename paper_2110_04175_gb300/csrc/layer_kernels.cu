@@ -592,12 +592,17 @@ int by_width(int64_t pitch, F f) {
     return f(Hold<32, 4>());
 }
 
-// Rows of partial sums per worker in the norm's backward pass: about two CTAs per
-// SM over all workers, no more than there are tokens.
-int64_t norm_partials(int32_t n, int64_t tokens) {
-    const int64_t want = 304 / n > 0 ? 304 / n : 1;
+// Rows of partial sums per worker in the norm's backward pass, one per CTA: about two
+// CTAs per SM over all workers and no more than there are tokens; whole multiples of
+// that where a thread would otherwise add up more than 256 rows in one chain, which
+// for products of random signs is off by 4e-7 ([160][4096][2304] in one chain per
+// worker was off by 6.1e-7).
+int64_t norm_partials(int32_t n, int64_t tokens, int64_t d) {
+    const int64_t pitch = pitch_of(d), side = pitch <= 512 ? 8 : pitch <= 1024 ? 4 : pitch <= 2048 ? 2 : 1;  // kRows
+    const int64_t fill = 304 / n, chain = fill * side * 256, want = tokens > chain ? fill * ((tokens + chain - 1) / chain) : fill;
     return tokens < want ? (tokens > 0 ? tokens : 1) : want;
 }
+static_assert(RELAY_MAX_N <= 304, "a CTA per worker");
 
 }  // namespace
 
@@ -685,7 +690,7 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
 int64_t relay_rms_norm_backward_workspace(int32_t n, int64_t tokens, int64_t d) {
     if (const int rc = check_shape(RELAY_FP32, n, tokens, d)) return rc;
     if (d > RELAY_NORM_MAX_D) return RELAY_EUNSUPPORTED;
-    return 4 * n * norm_partials(n, tokens) * pitch_of(d);
+    return 4 * n * norm_partials(n, tokens, d) * pitch_of(d);
 }
 
 int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* dy,
@@ -713,7 +718,7 @@ int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, 
         return RELAY_EINVAL;
     const bool vec = d % 8 == 0 && vectors(dy, type, n, tokens) && vectors(dtotal, type, n, tokens) &&
                      vectors(eight ? nullptr : total, type, n, tokens) && vectors(dx, type, n, tokens);
-    const int parts = static_cast<int>(norm_partials(n, tokens));
+    const int parts = static_cast<int>(norm_partials(n, tokens, d));
     const int rc = by_type(type, [&](auto t) {
         using T = decltype(t);
         const NormBackwardArgs<T> a{view<const T>(dy, n, tokens), view<const T>(dtotal, n, tokens),

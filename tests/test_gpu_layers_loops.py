@@ -1,5 +1,6 @@
 """The norm where a CTA takes several groups of rows one after the other, forward (rows asked for
-ahead) and backward, at every width's instance, against 64 bits.  References in float64 on the GPU."""
+ahead) and backward, at every width's instance, against 64 bits; and how far the weight's gradient
+is off where one worker has very many rows.  References in float64 on the GPU."""
 import pytest
 import torch
 
@@ -105,3 +106,19 @@ def test_norm_backward_of_many_rows(dtype, source, d, T):
     _within(dx, want, _rounded(want, dtype, 2 * bound))  # xhat from the total is one more rounding
     _within(dw, (g * xhat).sum(1), (T + 64) * U * (g * xhat).abs().sum(1))
     assert not torch.where(used, 0, dx).any()
+
+
+# the sum of N products of random sign in a chain of fp32 additions is off by U sqrt(N / 6) of itself
+# (each addition rounds by U / sqrt(3) of a partial sum, which grows like a random walk); chains of 256,
+# and their join in 8 shorter ones: 3.9e-7 and less than 2e-7
+@pytest.mark.parametrize("n,T,d", [(160, 4096, 2304), (256, 2051, 4096), (16, 16384, 4096), (1, 30000, 8200)])
+def test_norm_weight_gradient_of_many_rows(n, T, d):
+    dtype = torch.bfloat16
+    h, dy = _random(1, n, T, d, dtype=dtype), _random(2, n, T, d, dtype=dtype)
+    s = torch.ones(n, T, device="cuda")
+    dx, dw = torch.empty_like(dy), torch.empty(n, d, device="cuda")
+    work = torch.empty(rs.relay_rms_norm_backward_workspace(n, T, d), dtype=torch.uint8, device="cuda")
+    rs.relay_rms_norm_backward(dy, torch.ones(n, d, device="cuda"), s, dx, dw, work, total=h)
+    for i in sorted({0, n // 2, n - 1}):
+        want = (dy[i].double() * h[i].double()).sum(0)
+        assert float((dw[i].double() - want).norm() / want.norm()) < 5e-7
