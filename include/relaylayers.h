@@ -43,7 +43,8 @@
  *     checked before anything is enqueued.  The sizes that the library cannot
  *     see (of the buffers) are the caller's to get right.  An output may not
  *     be another argument's buffer, with one exception: `total` of
- *     relay_rms_norm may be the view of x or of the residual.
+ *     relay_rms_norm may be the view of x or of the residual (the same rows
+ *     at the same strides).
  *     RELAY_EINVAL: NULL for something needed, a size or stride out of range
  *     (n < 1, tokens < 0, d < 1, overlapping output rows), an address that
  *     is not a multiple of its element's size, checkpoint or workspace

@@ -661,6 +661,7 @@ int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const rel
     if (y->data == x->data || (residual != nullptr && y->data == residual->data) ||
         (total != nullptr && y->data == total->data))
         return RELAY_EINVAL;
+    if (crossed(total, x, n, tokens) || crossed(total, residual, n, tokens)) return RELAY_EINVAL;
     const bool vec = d % 8 == 0 && vectors(x, type, n, tokens) && vectors(residual, type, n, tokens) &&
                      vectors(total, type, n, tokens) && vectors(y, type, n, tokens);
     return by_type(type, [&](auto t) {

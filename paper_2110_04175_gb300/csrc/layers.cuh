@@ -301,6 +301,12 @@ View<T> view(const relay_rows* r, int32_t n, int64_t tokens) {
     return View<T>{static_cast<T*>(r->data), n > 1 ? r->worker_stride : 0, tokens > 1 ? r->token_stride : 0};
 }
 
+// Whether two views start at the same place without being the same rows.
+inline bool crossed(const relay_rows* a, const relay_rows* b, int32_t n, int64_t tokens) {
+    return a != nullptr && b != nullptr && a->data == b->data &&
+           ((n > 1 && a->worker_stride != b->worker_stride) || (tokens > 1 && a->token_stride != b->token_stride));
+}
+
 // Whether the rows can be moved 16 bytes at a time (true for NULL).
 inline bool vectors(const relay_rows* r, int32_t type, int32_t n, int64_t tokens) {
     if (r == nullptr) return true;

@@ -38,3 +38,17 @@ def test_workspace_without_rows_is_enough_for_every_call(lib):
                     rows = layers._pack_rows(address, tokens * wide, wide)
                     assert 0 <= size(type_, n, t, outputs, inputs, rows) <= bound, (type_, n, tokens, t, outputs, inputs)
                 assert size(type_, n, t, outputs, inputs, None) <= bound
+
+
+def test_total_on_other_rows_of_an_inputs_buffer_is_refused(lib):
+    """total may be the view of x or of the residual; one that starts where they do with other strides
+    would overwrite rows that are still to be read (x repeated for all workers, its first row as total's)."""
+    x, r, other = layers._pack_rows(A, 0, 64), layers._pack_rows(2 * A, 640, 64), layers._pack_rows(3 * A, 640, 64)
+
+    def call(x, residual, total, n=2, tokens=10):
+        return lib.relay_rms_norm(0, n, tokens, 64, x, residual, 4 * A, 64, 1e-5, total, other, None, None, None, None)
+
+    repeated, crosswise = layers._pack_rows(A, 640, 64), layers._pack_rows(2 * A, 64, 128)
+    assert call(x, r, repeated) == -1  # RELAY_EINVAL
+    assert call(repeated, r, crosswise) == -1
+    assert call(r, None, crosswise) == -1
