@@ -109,7 +109,9 @@ int relay_checkpoint_unpack(int32_t type, int32_t n, int64_t tokens, int64_t d, 
 
 /* The sum, its root-mean-square norm and, where codes and scales are given,
  * xhat in 8 bits.  residual, total (h in the rows' type), rstd (s, fp32
- * [n][tokens]) and codes with scales may each be NULL.  eps > 0. */
+ * [n][tokens]) and codes with scales may each be NULL.  eps > 0.  The squares
+ * are summed in fp32: a row of which they pass 3.4e38 (values of 1e17 to 1e19
+ * and more) has s = 0 and y = 0. */
 int relay_rms_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *x,
                    const relay_rows *residual, const float *weight, int64_t weight_stride, float eps,
                    const relay_rows *total, const relay_rows *y, float *rstd, int8_t *codes, uint8_t *scales,
