@@ -94,6 +94,22 @@ __device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity)
     return false;
 }
 
+// A count in shared memory that one thread raises, and another's wait until it is `least` or
+// more (false after about a second): what the one has seen before, the other sees after.
+__device__ __forceinline__ void count_store(uint32_t at, int count) {
+    asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(at), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ bool count_wait(uint32_t at, int least) {
+    const long long start = clock64();
+    do {
+        int count;
+        asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(count) : "r"(at) : "memory");
+        if (count >= least) return true;
+    } while (clock64() - start < kPatience);
+    return false;
+}
+
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

@@ -65,12 +65,18 @@ struct Stages {  // in a CTA
     static constexpr int kShared = kCount * kBytes + kAhead * kCodes + kAdders * kTurn + 1024 + 512;
     static_assert(kShared <= 232448, "shared memory of a CTA");
     // Teams at work: no more than stages.  A wait for a phase passes too when the barrier is
-    // two phases behind, and a team that goes from stage i to stage i + teams knows only that
-    // stage i - kCount was freed, which is the phase before the one it waits for if
-    // i + teams - 2 kCount is that stage or an earlier one.  The same for stages of codes, of
-    // which there are as many or more.
+    // two phases behind, so a team that meets stage i has to know that stage i - 2 kCount was
+    // freed.  With as many stages as teams it has met the same barrier before.  With more
+    // (kAsk) it has met that of stage i - kTeamsIn, whose freeing says nothing of another's
+    // arrival: the codes of stage i are copied only when the role that copies dy, which waits
+    // for every stage, has found stage i - kCount free, and a team waits for its codes first.
+    // A wait for codes is safe where the team knows that stage i - kAhead got its own: that
+    // stage was the team's, or is not after stage i - kTeamsIn - kCount, which the team has
+    // seen freed (without kAsk: not after stage i - kCount).
     static constexpr int kTeamsIn = kCount < kTeams ? kCount : kTeams;
+    static constexpr bool kAsk = kTeamsIn < kCount;
     static_assert(kCount >= 2 && kTeamsIn <= kCount && kAhead >= kCount, "phases of the barriers");
+    static_assert(!kAsk || kAhead % kTeamsIn == 0 || kAhead >= kTeamsIn + kCount, "phases of the codes' barriers");
 };
 
 struct WeightGradArgs {
@@ -272,6 +278,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
     const auto fetched = [&](int s) { return bars + 8 * (2 * kCount + 4 + s); };
     const auto used = [&](int s) { return bars + 8 * (2 * kCount + 4 + S::kAhead + s); };
     const uint32_t tensor_at = bars + 8 * (2 * kCount + 4 + 2 * S::kAhead);
+    const uint32_t passed = tensor_at + 4;  // how many stages the copies of dy have found free
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x / 32), 0), lane = threadIdx.x % 32;
     const int rank = static_cast<int>(cluster_rank());
@@ -290,6 +297,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
             barrier_init(fetched(s), 1);
             barrier_init(used(s), kTeam);
         }
+        count_store(passed, 0);
         barriers_ready();
     }
     if (warp == kIssuer) tensor_alloc<2 * kN>(tensor_at);
@@ -422,6 +430,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                 for (int n = 0; n < at.count; ++n, ++i) {
                     const int s = i % kCount;
                     if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
+                    if (S::kAsk) count_store(passed, i + 1);
                     barrier_expect(full(s), S::kLeft);
                     for (int p = 0; p < S::kLeft / kPanel; ++p)
                         copy_box(stages + s * S::kBytes + p * kPanel, &dy_map, at.o0 + kM * rank + 64 * (p % (kM / 64)),
@@ -439,6 +448,7 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                 for (int n = 0; n < at.count; ++n, ++i) {
                     const int f = i % S::kAhead;
                     if (!(ok = barrier_wait(used(f), (i / S::kAhead & 1) ^ 1))) break;
+                    if (S::kAsk && !(ok = count_wait(passed, i - kCount + 1))) break;
                     barrier_expect(fetched(f), S::kCodes);
                     copy_box(codes + f * S::kCodes, &codes_map, half, row0 + n * kDepth, fetched(f));
                 }
@@ -489,8 +499,9 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                     now = __vmaxu4(next, 0x07070707u) - 0x06060606u;
                     next = load_next();
                 }
+                if (S::kAsk && !(ok = barrier_wait_warp(fetched(f), i / S::kAhead & 1))) break;
                 if (!(ok = barrier_wait_warp(freed(s), (i / kCount & 1) ^ 1))) break;
-                if (!(ok = barrier_wait_warp(fetched(f), i / S::kAhead & 1))) break;
+                if (!S::kAsk && !(ok = barrier_wait_warp(fetched(f), i / S::kAhead & 1))) break;
                 R::make(codes + f * S::kCodes, stages + s * S::kBytes + S::kLeft, now, odd, turn, left, member, lane);
                 fence_async();
                 __syncwarp();
