@@ -437,8 +437,11 @@ relay_weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_
                                  (at.first + n) * kDepth, at.worker * kTerms + p / (kM / 64), full(s));
                 }
             }
-            for (int j = max(0, i - kCount); j < i; ++j)  // nothing is left in flight
-                if (!barrier_wait(full(j % kCount), j / kCount & 1)) break;
+            // nothing is left in flight: no copy, and no arrival that the last stages' products
+            // still send to this CTA
+            for (int j = max(0, i - kCount); j < i; ++j)
+                if (!barrier_wait(full(j % kCount), j / kCount & 1) || !barrier_wait(freed(j % kCount), j / kCount & 1))
+                    break;
         } else if (warp == kIssuer + 2 && elected()) {
             int i = 0;
             bool ok = true;
