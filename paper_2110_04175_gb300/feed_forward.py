@@ -99,7 +99,7 @@ def train(n: int = 8, tokens: int = 256, d: int = 256, f: int = 512, steps: int 
     x = torch.randn(n, tokens, d, device="cuda", generator=make)
     x = (x + torch.randn(n, 1, d, device="cuda", generator=make)).bfloat16()  # heterogeneous workers
     target = layer.forward(teacher, x)[0].clone()
-    grads = torch.empty(n, run.ld, device="cuda")
+    grads = torch.zeros(n, run.ld, device="cuda")  # the views leave gaps
     losses = []
     for _ in range(steps):
         out, _ = layer.forward(run.x, x)
