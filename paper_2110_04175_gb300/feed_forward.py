@@ -8,7 +8,7 @@ what the backward pass needs of the activations is held in 8 bits:
 
 ``python -m paper_2110_04175_gb300.feed_forward`` trains it: every worker has
 data of its own, the workers sit on a binary tree, and each step's gradients go
-through ``RelayRun.step`` (RelaySGD's relay, Algorithm 1).
+through ``GradientRun`` (Adam, then RelaySGD's relay, Algorithm 1).
 """
 from __future__ import annotations
 
@@ -79,19 +79,50 @@ class FeedForward:
         return self.dx
 
 
+class GradientRun:
+    """RelaySGD (Algorithm 1 with Adam) on gradients that the caller has computed.
+
+    The step's own objective is a quadratic with the gradient x - mu, and a gradient handed
+    over as mu = x - g would be rounded to the spacing of x.  So Adam runs on its own, as
+    one worker's step from zero with the centre -g, where the gradient 0 - (-g) is g itself;
+    its step goes into the relay as the centre x + step at lr = 1, rounded as any addition
+    to x.  ``x`` (fp32 [n][>= d]): the models.  ``descent`` (like x, zero where nothing is
+    written): the caller puts -g there, then calls ``step``."""
+
+    def __init__(self, n: int, d: int, edges, beta1: float = 0.9, beta2: float = 0.99, eps: float = 1e-8):
+        import numpy as np
+
+        from . import RelayRun
+        self.n, self.relay = n, RelayRun(n, d, edges)
+        self.x = self.relay.x
+        self.adam = RelayRun(1, self.x.numel(), np.zeros((0, 2), np.int32), optimizer=("adam", beta1, beta2, eps))
+        self.descent = self.adam.mu.view_as(self.x)
+
+    def init(self, x0_std: float, seed: int):
+        """The same models everywhere, x0_std times normal values; no gradients yet."""
+        import numpy as np
+        self.relay.init(x0_std, seed, np.ones((self.n, 1)), 0.0, seed, 0.0)
+        self.adam.init(0.0, seed, np.ones((1, 1)), 0.0, seed, 0.0)
+
+    def step(self, lr: float, seed: int = 0):
+        """One step of every worker with the gradients that `descent` holds, and its relay."""
+        import torch
+        self.adam.x.zero_()
+        self.adam.step(lr, seed)
+        torch.add(self.x, self.adam.x.view_as(self.x), out=self.relay.mu)
+        self.relay.step(1.0, seed)
+
+
 def train(n: int = 8, tokens: int = 256, d: int = 256, f: int = 512, steps: int = 100, lr: float = 0.02, seed: int = 0):
     """Trains one layer on n workers, each with inputs of its own mean, towards a common
-    teacher's outputs; returns the mean loss per step.  The gradient enters the relay as the
-    centre of RelayRun's local objective, mu = x - g, with no noise: the gradient that its
-    optimiser (Adam) sees is x - mu = g."""
+    teacher's outputs; returns the mean loss per step."""
     import torch
 
-    from . import RelayRun
     from . import workloads as wl
 
     layer = FeedForward(n, tokens, d, f)
-    run = RelayRun(n, layer.size, wl.binary_tree(n), optimizer=("adam", 0.9, 0.99, 1e-8))
-    run.init(0.04, seed, wl.identity_mix(n), 1.0, seed, 0.0)  # the same models everywhere
+    run = GradientRun(n, layer.size, wl.binary_tree(n))
+    run.init(0.04, seed)  # the same models everywhere
     layer.weights(run.x)[0].fill_(1.0)
     make = torch.Generator(device="cuda").manual_seed(seed)
     teacher = torch.randn(1, layer.size, device="cuda", generator=make).mul_(0.08).expand(n, -1).contiguous()
@@ -99,14 +130,12 @@ def train(n: int = 8, tokens: int = 256, d: int = 256, f: int = 512, steps: int 
     x = torch.randn(n, tokens, d, device="cuda", generator=make)
     x = (x + torch.randn(n, 1, d, device="cuda", generator=make)).bfloat16()  # heterogeneous workers
     target = layer.forward(teacher, x)[0].clone()
-    grads = torch.zeros(n, run.ld, device="cuda")  # the views leave gaps
     losses = []
     for _ in range(steps):
         out, _ = layer.forward(run.x, x)
         off = out.float() - target.float()
         losses.append(off.square().mean())
-        layer.backward(run.x, grads, (off * (1.0 / tokens)).bfloat16())
-        torch.sub(run.x[:, :layer.size], grads[:, :layer.size], out=run.mu[:, :layer.size])
+        layer.backward(run.x, run.descent, (off * (-1.0 / tokens)).bfloat16())  # -g
         run.step(lr, seed)
     return torch.stack(losses).tolist()
 
