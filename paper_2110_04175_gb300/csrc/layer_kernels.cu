@@ -728,9 +728,13 @@ int relay_rms_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, 
                                     d % 8 == 0 && aligned(weight, 16) && (n == 1 || weight_stride % 4 == 0), rstd, codes, scales,
                                     lengths, static_cast<float*>(workspace), static_cast<int32_t>(tokens),
                                     static_cast<int32_t>(d), static_cast<int32_t>(pitch_of(d))};
-        // unaligned narrow rows from 8 bits go faster with the wider instance's two strips at once
-        // (width 94: 249 against 294 us for [4][89240]), aligned ones with one (width 96: 122 and 159)
-        return by_width(eight && !vec && a.pitch <= 256 ? 512 : a.pitch, [&](auto hold) {
+        // Unaligned 16-bit rows of up to 256 features from 8 bits go faster with the wider instance's two
+        // strips where they come from HBM ([16][16384][201]: 153 against 162 us, [4][89240][94] with
+        // dtotal 251 and 267), and slower where L2 holds them ([4][16384][201]: 38 against 29 us,
+        // [4][2048][94] 9.2 and 7.8); fp32 rows and aligned ones always do better with one.
+        const int64_t row_bytes = element_size(type) * d * (dtotal != nullptr ? 3 : 2) + pitch_of(d) * 33 / 32;
+        const bool two = eight && !vec && type != RELAY_FP32 && n * tokens * row_bytes > 120000000;
+        return by_width(two && a.pitch <= 256 ? 512 : a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr size_t kSmem = (kNormWarps<kParts> / kParts - 1) * kStrips * kParts * kStrip * sizeof(float);
             (vec ? (eight ? relay_rms_norm_backward_kernel<T, kVector, kParts, kStrips, true>

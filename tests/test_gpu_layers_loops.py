@@ -77,7 +77,7 @@ def test_norm_of_many_rows(dtype, n, T, d, residual):
 @pytest.mark.parametrize("source", ["checkpoint", "total"])
 @pytest.mark.parametrize("d,T", [(200, 315), (94, 315), (512, 315), (500, 315), (1000, 157), (1001, 157), (2048, 79),
                                  (1999, 79), (4096, 41), (4001, 41), (8192, 41), (8001, 41), (16384, 41), (12001, 41),
-                                 (32768, 41), (20001, 41)])
+                                 (32768, 41), (20001, 41), (201, 16387)])
 def test_norm_backward_of_many_rows(dtype, source, d, T):
     n = 16
     h, dy = _random(1, n, T, d, dtype=dtype), _random(2, n, T, d, dtype=dtype, size=0.01)
