@@ -6,11 +6,11 @@
 // works on strips of 256 features (layers.cuh); what a row needs twice stays in
 // registers between its two uses.  Measured in bf16, bytes moved against the
 // 6.67 TB/s of a plain copy:
-//   norm, residual, 8-bit output        [4][4096][4096]   92 us  6.6 TB/s
+//   norm, residual, 8-bit output        [4][4096][4096]   93 us  6.5 TB/s
 //   norm backward from 8 bits           [4][4096][4096]   84 us  5.6 TB/s
-//   to 8 bits and back                  [4][4096][8192]  128 us  6.4 TB/s
-//   gated, both inputs put away         [4][4096][8192]  162 us  6.7 TB/s
-//   gated backward from 8 bits          [4][4096][8192]  200 us  6.1 TB/s
+//   to 8 bits and back                  [4][4096][8192]  127 us  6.4 TB/s
+//   gated, both inputs put away         [4][4096][8192]  163 us  6.6 TB/s
+//   gated backward from 8 bits          [4][4096][8192]  190 us  6.4 TB/s
 #include "layers.cuh"
 
 namespace {
@@ -273,10 +273,16 @@ constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
 
 // Rows of which the norm's CTAs may stay and take one after the other, the next asked for
 // before this one's sum and the weight in registers (kAhead): aligned 16-bit rows of up to
-// 8192 features.  That pays where little moves per row ([4][4096][4096], us, one CTA a row
-// and staying: no residual 57 and 48, with residual 80 and 85, and an 8-bit output 91 and
-// 101) or rows are wide ([4][1024][8192], residual: 52 and 46), so it is done without a
-// residual and past 4096 features.  Rows of fp32 keep HBM as busy one CTA each.
+// 8192 features.  That pays where little moves per row or rows are wide, so it is done
+// without a residual and past 4096 features.  Measured in us, one CTA a row and staying:
+//   n T d = 2^26   [4][16384][1024]   [4][8192][2048]   [4][4096][4096]   [4][2048][8192]
+//     y alone             63   50           64   50           61   49           74   59
+//     and 8 bits          75   67           75   67           73   60           87   69
+//     residual            84   86           84   85           83   87           97   89
+//     and 8 bits          94   97           94   99           93  101          108   99
+// At 2^23 features the two are within 12 % either way (with 8 bits staying is the slower one,
+// without them the faster), at 2^20 staying is 4 to 13 % faster, but 15 to 20 % slower for rows of
+// 256 features (2.7 and 2.3 us).  Rows of fp32 keep HBM as busy one CTA each.
 template <typename T, Way kWay, int kStrips>
 constexpr bool kMayStay = kWay == kVector && kStrips <= 2 && sizeof(T) == 2;
 
@@ -382,10 +388,12 @@ struct NormBackwardArgs {
 // CTA (p, i) takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i and
 // leaves their sum of dy xhat in its row of `partial`.  Aligned rows of up to 8192
 // features keep the weight in registers (kHold); they, and others that leave room, ask
-// for the next row before this one's sum over the CTA (kAhead).  16-bit rows stay as they came from memory and are widened
-// again after that sum; others, and those in 8 bits, whose recall costs more than the
-// registers, are kept as fp32 (kKeep).  The widest rows are read twice (kTwice), the
-// second time from the caches.
+// for the next row before this one's sum over the CTA (kAhead).  16-bit rows stay as they
+// came from memory and are widened again after that sum; others, and those in 8 bits, whose
+// recall costs more than the registers, are kept as fp32 (kKeep).  The widest rows are read
+// twice (kTwice), the second time from the caches.  The two CTAs' 128 registers are not
+// quite enough for fp32 rows from the sum (72 to 80 bytes a thread go to local memory,
+// [4][4096][4096] 156 us, 0.77 of the copy rate), nor the 64 of the widest rows (130 to 350).
 template <typename T, Way kWay, int kParts, int kStrips, bool kEight>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>, kNormWarps<kParts> > 8 ? 1 : 2)
 relay_rms_norm_backward_kernel(NormBackwardArgs<T> a) {

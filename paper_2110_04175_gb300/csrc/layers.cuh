@@ -52,8 +52,8 @@ struct View {
 // The 8-bit format is kept in octets whichever way the row goes: with kDirect its values
 // change places in `turn`, 256 floats of shared memory of the warp's own.  (At
 // [4][8380][1001] in bf16, the gated step with its checkpoints: 292 us with codes, scales
-// and block maxima element by element, a third of that this way.)  All lanes of the warp
-// call these together.
+// and block maxima element by element, 179 us this way.)  All lanes of the warp call these
+// together.
 enum Way { kDirect, kVector };
 
 template <Way kWay>

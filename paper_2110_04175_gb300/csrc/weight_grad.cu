@@ -11,7 +11,8 @@
 //     bits and its scale a power of two, so the bf16 values are exact;
 //   - dy comes by TMA, as bf16.  fp16 and fp32 rows (and bf16 rows that TMA cannot
 //     take) are written to the workspace first as bf16 terms that add up to them
-//     exactly, 8 bits each: 2 for fp16, 3 for fp32, one product each.
+//     exactly, 8 bits each: 2 for fp16, 3 for fp32, one product each.  (bf16 ends at
+//     2^-133, so what fp32 numbers below 2^-110 have below that is left out.)
 //
 // A pair of CTAs makes a tile of 256 outputs x kN inputs (cta_group::2): each
 // brings half of both operands, so that a code is recalled once for 256 outputs.
@@ -22,12 +23,12 @@
 // other warps add the other one to registers, rounded to the nearest: 4e-7 against
 // 64 bits at 8192 tokens.
 //
-// Measured: 2 x [8192 tokens, 8192 outputs, 4096 inputs], 1.1 TFLOP, takes 0.70 ms in bf16
-// (1570 TFLOP/s, 0.81 of what a library product of 8192^3 does in a burst; 0.77 ms back to
-// back, when power holds the clock), 1.27 ms in fp16 and 2.08 ms in fp32.  A stage of 64
-// tokens takes a pair 620 cycles where its products take 512: shared memory carries 80 KB
-// per SM and stage.  Where tokens are few, the results' way to memory bounds it
-// (16 x [2 tokens, 3114, 4416]: 3.9 TB/s).
+// Measured: 2 x [8192 tokens, 8192 outputs, 4096 inputs], 1.1 TFLOP, takes 0.70 ms in bf16 on
+// its own (1570 TFLOP/s, 0.81 of what a library product of 8192^3 does in a burst), 1.44 ms in
+// fp16 and 2.07 ms in fp32; back to back, when power holds the clock, 0.77, 1.56 and 2.24 ms.
+// A stage of 64 tokens takes a pair 620 cycles where its products take 512: shared memory
+// carries 80 KB per SM and stage.  Where tokens are few, the results' way to memory bounds it
+// (16 x [2 tokens, 3114, 4416]: 218 us, 4.0 TB/s).
 #include "blackwell.cuh"
 #include "layers.cuh"
 
@@ -41,6 +42,7 @@ constexpr int kDepth = 64;     // tokens of a stage
 constexpr int kAdders = 8, kIssuer = 8, kMaker = 12, kTeam = 4, kTeams = 3;
 constexpr int kThreads = 32 * (kMaker + kTeam * kTeams);
 // 6 warpgroups are launched with 80 registers a thread: 2 x 144 + 48 + 3 x 48 = 6 x 80
+// (in tiles of 256 inputs, whose adders hold 128 sums, 118 bytes a thread go to local memory)
 constexpr int kAdderRegisters = 144, kIssuerRegisters = 48, kMakerRegisters = 48;
 constexpr int kPanel = kDepth * 128;  // bytes of 64 outputs or inputs x kDepth tokens
 constexpr int kSms = 152;
@@ -220,7 +222,7 @@ struct Recall {
 
 // dy as bf16 terms [n][kTerms][tokens][width], width = outputs rounded up to a multiple
 // of 8: each term is what is left with all but 8 bits cut off, so that the terms add up
-// exactly.  Rows that do not count are 0.
+// exactly (down to bf16's 2^-133).  Rows that do not count are 0.
 template <typename T, int kTerms, Way kWay>
 __global__ void __launch_bounds__(256)
 relay_weight_grad_terms_kernel(View<const T> dy, const int32_t* lengths, __nv_bfloat16* to, int n, int tokens,

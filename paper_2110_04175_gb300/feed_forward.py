@@ -27,7 +27,7 @@ class FeedForward:
         import torch
         self.n, self.tokens, self.d, self.f, self.eps = n, tokens, d, f, eps
         self.dtype = dtype or torch.bfloat16
-        self.at = [0, -(-d // 4) * 4]  # views start on 16-byte boundaries of the rows
+        self.at = [0, -(-d // 4) * 4]  # gate and up start on a 16-byte boundary of the rows
         self.at.append(self.at[1] + 2 * f * d)
         self.size = self.at[2] + d * f
 
