@@ -11,6 +11,8 @@
  *   relay_gated               a = g sigma(g) u,  sigma(g) = 1 / (1 + exp(-g))
  *   relay_gated_backward      du = da g sigma(g);  dg = da u sigma(g) (1 + g (1 - sigma(g)));  a again
  *   relay_weight_grad         dW[o][i] = scale[i] sum_t dy[t][o] xhat[t][i]
+ *   relay_recurrence          h_t = f_t h_{t-1} + (1 - f_t) v_t,  f = sigma(gate)
+ *   relay_recurrence_backward l_t = dh_t + f_{t+1} l_{t+1};  dv = l (1 - f);  dgate = l (h_{t-1} - v) f (1 - f)
  *   relay_checkpoint_pack     any activation to 8 bits, and
  *   relay_checkpoint_unpack   back
  *
@@ -49,8 +51,9 @@
  *     (n < 1, tokens < 0, d < 1, overlapping output rows), an address that
  *     is not a multiple of its element's size, checkpoint or workspace
  *     addresses that are not multiples of 16, a workspace too small.
- *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N, n tokens >= 2^30, d > 2^24, in
- *     the norm d > RELAY_NORM_MAX_D, in the weight gradient inputs >
+ *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N (in the recurrence
+ *     RELAY_RECURRENCE_MAX_N), n tokens >= 2^30, d > 2^24, in the norm d >
+ *     RELAY_NORM_MAX_D, in the weight gradient inputs >
  *     RELAY_WEIGHT_GRAD_MAX_INPUTS.
  *
  * The 8-bit format.  A row of d features is blocks of 32 with one scale byte
@@ -85,6 +88,7 @@ extern "C" {
 
 #define RELAY_NORM_MAX_D 32768
 #define RELAY_WEIGHT_GRAD_MAX_INPUTS (1 << 22)
+#define RELAY_RECURRENCE_MAX_N (1 << 20)
 
 /* A view [n][tokens][d] of device memory: element (i, t, k) is at
  * data + i worker_stride + t token_stride + k, strides in elements, >= 0. */
@@ -166,6 +170,38 @@ int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, 
                       const int8_t *codes, const uint8_t *scales, const float *column_scale,
                       int64_t column_scale_stride, const int32_t *lengths, float *dweight, int64_t worker_stride,
                       int64_t row_stride, void *workspace, int64_t workspace_bytes, relay_stream_t stream);
+
+/* Bytes of workspace for relay_recurrence and relay_recurrence_backward (may
+ * be 0), or a negative status. */
+int64_t relay_recurrence_workspace(int32_t n, int64_t tokens, int64_t d);
+
+/* The gated linear recurrence along the tokens of each of n workers (or of n
+ * sequences, up to RELAY_RECURRENCE_MAX_N), every feature on its own:
+ * h_t = f_t h_{t-1} + (1 - f_t) v_t with f = sigma(gate).  The state is fp32,
+ * the rows `out` are h rounded.  initial (fp32 [n][d], stride from worker to
+ * worker): the state before the first token, NULL for 0.  last (the same
+ * shape, or NULL): the state behind the last token, for the call that goes on;
+ * it may be `initial`, at the same stride.  begins (uint8 [n][tokens], or
+ * NULL): not 0 at a token that begins a sequence, where h_{t-1} counts as 0
+ * whatever it holds.  lengths: tokens past them are not read, leave the state
+ * as it is, and get rows of 0.  Behind an input that is not finite the states
+ * are not finite up to the next beginning (an infinity may become NaN). */
+int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *gate,
+                     const relay_rows *value, const float *initial, int64_t initial_stride, const uint8_t *begins,
+                     const int32_t *lengths, const relay_rows *out, float *last, int64_t last_stride, void *workspace,
+                     int64_t workspace_bytes, relay_stream_t stream);
+
+/* Its gradients, from the rows of the forward pass: gate, value and out (whose
+ * rounded values are taken as h).  dlast: the gradient of the last state, or
+ * NULL; dinitial: that of the first one, or NULL (it may be dlast, at the same
+ * stride).  begins, lengths and initial as in the forward pass; rows past the
+ * lengths get gradients of 0. */
+int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *dout,
+                              const relay_rows *gate, const relay_rows *value, const relay_rows *out,
+                              const float *initial, int64_t initial_stride, const float *dlast, int64_t dlast_stride,
+                              const uint8_t *begins, const int32_t *lengths, const relay_rows *dgate,
+                              const relay_rows *dvalue, float *dinitial, int64_t dinitial_stride, void *workspace,
+                              int64_t workspace_bytes, relay_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -38,7 +38,8 @@ from ._native import (RELAY_EINVAL, RELAY_ECUDA, RELAY_ENOMEM, RELAY_ENOTTREE, R
 from .layers import (RELAY_BF16, RELAY_FP16, RELAY_FP32, RELAY_NORM_MAX_D, ActivationCheckpoint,  # noqa: E402
                      relay_checkpoint_pack, relay_checkpoint_pitch, relay_checkpoint_unpack,
                      relay_gated, relay_gated_backward, relay_rms_norm, relay_rms_norm_backward,
-                     relay_rms_norm_backward_workspace, relay_weight_grad, relay_weight_grad_workspace)
+                     relay_rms_norm_backward_workspace, relay_weight_grad, relay_weight_grad_workspace,
+                     relay_recurrence, relay_recurrence_backward, relay_recurrence_workspace)
 from .lr_correction import lr_correction  # noqa: E402
 
 __all__ = [
@@ -60,5 +61,6 @@ __all__ = [
     "RELAY_BF16", "RELAY_FP16", "RELAY_FP32", "RELAY_NORM_MAX_D", "ActivationCheckpoint",
     "relay_checkpoint_pack", "relay_checkpoint_pitch", "relay_checkpoint_unpack", "relay_gated",
     "relay_gated_backward", "relay_rms_norm", "relay_rms_norm_backward", "relay_rms_norm_backward_workspace",
-    "relay_weight_grad", "relay_weight_grad_workspace",
+    "relay_weight_grad", "relay_weight_grad_workspace", "relay_recurrence", "relay_recurrence_backward",
+    "relay_recurrence_workspace",
 ]

@@ -15,16 +15,6 @@
 
 namespace {
 
-template <typename F>
-int by_type(int32_t type, F f) {
-    return type == RELAY_BF16 ? f(__nv_bfloat16()) : type == RELAY_FP16 ? f(__half()) : f(float());
-}
-
-// The warp's `turn` (layers.cuh) in a kernel of `warps` warps, if it is `used`.
-#define WARP_TURN(warps, used)                                                  \
-    __shared__ __align__(16) float turns[(used) ? (warps) : 1][(used) ? kStrip : 1]; \
-    float* turn = turns[(used) ? threadIdx.x / 32 : 0]
-
 // ------------------------------------------------------- element-wise kernels
 
 constexpr int kWarps = 8;  // of an element-wise CTA
@@ -251,25 +241,6 @@ struct NormArgs {
     uint8_t* scales;
     int32_t tokens, d, pitch;
 };
-
-// The sum of v over the kParts warps of a row (each warp's lanes included), the
-// same on all of them.  `slot`: the row's place in the CTA.  Called by all threads.
-template <int kParts>
-__device__ __forceinline__ float row_sum(float v, float* shared, int slot, int part) {
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-    if (kParts == 1) return v;
-    __syncthreads();  // the last sum's readers are done
-    if (threadIdx.x % 32 == 0) shared[slot * kParts + part] = v;
-    __syncthreads();
-    float s = 0.0f;
-#pragma unroll
-    for (int p = 0; p < kParts; ++p) s += shared[slot * kParts + p];
-    return s;
-}
-
-template <int kParts>
-constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
 
 // Rows of which the norm's CTAs may stay and take one after the other, the next asked for
 // before this one's sum and the weight in registers (kAhead): aligned 16-bit rows of up to
@@ -581,36 +552,6 @@ Grid make_grid(int32_t n, int64_t tokens, int64_t d, bool checkpoint, int* ctas)
                 static_cast<int32_t>(step_rows % tokens),
                 static_cast<int32_t>(step % runs)};
 }
-
-// Calls f(kParts, kStrips) as constants for the smallest instance that holds a row.
-template <int kParts_, int kStrips_>
-struct Hold {
-    static constexpr int kParts = kParts_, kStrips = kStrips_;
-};
-
-template <typename F>
-int by_width(int64_t pitch, F f) {
-    if (pitch <= 256) return f(Hold<1, 1>());
-    if (pitch <= 512) return f(Hold<1, 2>());
-    if (pitch <= 1024) return f(Hold<2, 2>());
-    if (pitch <= 2048) return f(Hold<4, 2>());
-    if (pitch <= 4096) return f(Hold<8, 2>());
-    if (pitch <= 8192) return f(Hold<16, 2>());
-    if (pitch <= 16384) return f(Hold<16, 4>());
-    return f(Hold<32, 4>());
-}
-
-// Rows of partial sums per worker in the norm's backward pass, one per CTA: about two
-// CTAs per SM over all workers and no more than there are tokens; whole multiples of
-// that where a thread would otherwise add up more than 256 rows in one chain, which
-// for products of random signs is off by 4e-7 ([160][4096][2304] in one chain per
-// worker was off by 6.1e-7).
-int64_t norm_partials(int32_t n, int64_t tokens, int64_t d) {
-    const int64_t pitch = pitch_of(d), side = pitch <= 512 ? 8 : pitch <= 1024 ? 4 : pitch <= 2048 ? 2 : 1;  // kRows
-    const int64_t fill = 304 / n, chain = fill * side * 256, want = tokens > chain ? fill * ((tokens + chain - 1) / chain) : fill;
-    return tokens < want ? (tokens > 0 ? tokens : 1) : want;
-}
-static_assert(RELAY_MAX_N <= 304, "a CTA per worker");
 
 }  // namespace
 

@@ -1,5 +1,5 @@
-// layers.cuh -- what the layer kernels (layer_kernels.cu, weight_grad.cu)
-// share: the activation types, a warp's strip of 256 features, the 8-bit
+// layers.cuh -- what the layer kernels (layer_kernels.cu, weight_grad.cu,
+// recurrence.cu, block_norm.cu) share: the activation types, a warp's strip of 256 features, the 8-bit
 // format of relaylayers.h, and the argument checks.
 #pragma once
 
@@ -18,6 +18,8 @@ constexpr int kStrip = 256;     // features that a warp handles together: 8 per 
 constexpr int kBlock = 32;      // features that share a scale
 constexpr int kPitch = 128;     // checkpoint rows are whole multiples of this
 constexpr int64_t kMaxD = int64_t(1) << 24, kMaxRows = int64_t(1) << 30;
+
+inline int64_t pitch_of(int64_t d) { return (d + kPitch - 1) / kPitch * kPitch; }
 
 // -------------------------------------------------------------------- types
 
@@ -157,6 +159,11 @@ __device__ __forceinline__ void clear_past(float (&v)[8], int lane, int left) {
         if (feature<kWay>(lane, k) >= left) v[k] = 0.0f;
 }
 
+// The warp's `turn` in a kernel of `warps` warps, if it is `used`.
+#define WARP_TURN(warps, used)                                                  \
+    __shared__ __align__(16) float turns[(used) ? (warps) : 1][(used) ? kStrip : 1]; \
+    float* turn = turns[(used) ? threadIdx.x / 32 : 0]
+
 // ------------------------------------------------------------- the 8-bit format
 
 // The scale byte of a block whose largest magnitude has the bits `most` (sign
@@ -265,6 +272,87 @@ struct CodePiece {
     }
 };
 
+// -------------------------------------------------------------------- a gate
+
+// sigma(g) and 1 - sigma(g), both to their own size and from the same exp(-|g|) <= 1, so
+// that they add up to 1 within a rounding.  The gates of 16-bit rows take the hardware's
+// exponential and reciprocal: off by less than (3 + |g|) 2^-23 relative, as if the gate
+// were (3 + |g|) 2^-23 further; below |g| = 87.3 the smaller one is 0.
+template <typename T>
+struct Gate {
+    float at, rest;
+    __device__ __forceinline__ explicit Gate(float g) {
+        float e, r;
+        if constexpr (sizeof(T) == 2) {
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(g) * -1.44269504f));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+        } else {
+            e = expf(-fabsf(g));
+            r = 1.0f / (1.0f + e);
+        }
+        const float s = e * r;
+        at = g < 0.0f ? s : r;
+        rest = g < 0.0f ? r : s;
+    }
+};
+
+// --------------------------------------------------------------- rows of a norm
+
+// The sum of v over the kParts warps of a row (each warp's lanes included), the
+// same on all of them.  `slot`: the row's place in the CTA.  Called by all threads.
+template <int kParts>
+__device__ __forceinline__ float row_sum(float v, float* shared, int slot, int part) {
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    if (kParts == 1) return v;
+    __syncthreads();  // the last sum's readers are done
+    if (threadIdx.x % 32 == 0) shared[slot * kParts + part] = v;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) s += shared[slot * kParts + p];
+    return s;
+}
+
+template <int kParts>
+constexpr int kNormWarps = kParts > 8 ? kParts : 8;  // of a CTA
+
+// Calls f(kParts, kStrips) as constants for the smallest instance that holds a row.
+template <int kParts_, int kStrips_>
+struct Hold {
+    static constexpr int kParts = kParts_, kStrips = kStrips_;
+};
+
+template <typename F>
+int by_width(int64_t pitch, F f) {
+    if (pitch <= 256) return f(Hold<1, 1>());
+    if (pitch <= 512) return f(Hold<1, 2>());
+    if (pitch <= 1024) return f(Hold<2, 2>());
+    if (pitch <= 2048) return f(Hold<4, 2>());
+    if (pitch <= 4096) return f(Hold<8, 2>());
+    if (pitch <= 8192) return f(Hold<16, 2>());
+    if (pitch <= 16384) return f(Hold<16, 4>());
+    return f(Hold<32, 4>());
+}
+
+// Rows of partial sums per worker in a norm's backward pass, one per CTA: about two
+// CTAs per SM over all workers and no more than there are tokens; whole multiples of
+// that where a thread would otherwise add up more than 256 rows in one chain, which
+// for products of random signs is off by 4e-7 ([160][4096][2304] in one chain per
+// worker was off by 6.1e-7).
+inline int64_t norm_partials(int32_t n, int64_t tokens, int64_t d) {
+    const int64_t pitch = pitch_of(d), side = pitch <= 512 ? 8 : pitch <= 1024 ? 4 : pitch <= 2048 ? 2 : 1;  // kRows
+    const int64_t fill = 304 / n, chain = fill * side * 256, want = tokens > chain ? fill * ((tokens + chain - 1) / chain) : fill;
+    return tokens < want ? (tokens > 0 ? tokens : 1) : want;
+}
+static_assert(RELAY_MAX_N <= 304, "a CTA per worker");
+
+// f with a value of the type.
+template <typename F>
+int by_type(int32_t type, F f) {
+    return type == RELAY_BF16 ? f(__nv_bfloat16()) : type == RELAY_FP16 ? f(__half()) : f(float());
+}
+
 // ----------------------------------------------------------- argument checks
 
 inline int64_t element_size(int32_t type) { return type == RELAY_FP32 ? 4 : 2; }
@@ -314,8 +402,6 @@ inline bool vectors(const relay_rows* r, int32_t type, int32_t n, int64_t tokens
     return aligned(r->data, 16) && (n == 1 || r->worker_stride * e % 16 == 0) &&
            (tokens == 1 || r->token_stride * e % 16 == 0);
 }
-
-inline int64_t pitch_of(int64_t d) { return (d + kPitch - 1) / kPitch * kPitch; }
 
 inline int status_of_launch() { return cudaGetLastError() == cudaSuccess ? RELAY_OK : RELAY_ECUDA; }
 

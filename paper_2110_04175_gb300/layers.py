@@ -42,6 +42,11 @@ _SIGNATURES = {
     "relay_weight_grad_workspace": (_i64, [_i32, _i32, _i64, _i64, _i64, _rows_p]),
     "relay_weight_grad": (ctypes.c_int, [_i32, _i32, _i64, _i64, _i64, _rows_p, _vp, _vp, _vp, _i64, _vp, _vp, _i64,
                                          _i64, _vp, _i64, _vp]),
+    "relay_recurrence_workspace": (_i64, [_i32, _i64, _i64]),
+    "relay_recurrence": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _vp, _i64, _vp, _vp, _rows_p, _vp, _i64, _vp, _i64,
+                                                 _vp]),
+    "relay_recurrence_backward": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _rows_p, _rows_p, _vp, _i64, _vp, _i64, _vp,
+                                                          _vp, _rows_p, _rows_p, _vp, _i64, _vp, _i64, _vp]),
 }
 
 _lib = None
@@ -108,6 +113,11 @@ def _weights(name, t, n, d):
     if one != 1 and d > 1:
         _refuse(name, t, f"values next to one another are needed (strides {t.stride()})")
     return t.data_ptr(), worker
+
+
+def _state(name, t, n, d):
+    """The same of a state that may be left out."""
+    return (None, 0) if t is None else _weights(name, t, n, d)
 
 
 def _plain(name, t, dtype, shape):
@@ -293,3 +303,41 @@ def relay_weight_grad(dy, checkpoint, dweight, workspace, column_scale=None, len
         *_held("checkpoint", checkpoint, n, tokens, inputs), scale, scale_stride,
         _plain("lengths", lengths, torch.int32, (n,)), dweight.data_ptr(), worker_stride, row_stride,
         *_workspace("workspace", workspace), _stream(stream)), "relay_weight_grad")
+
+
+def relay_recurrence_workspace(n: int, tokens: int, d: int) -> int:
+    """Bytes of workspace for relay_recurrence and relay_recurrence_backward (0 for most shapes)."""
+    return _bytes(_library().relay_recurrence_workspace(n, tokens, d), "relay_recurrence_workspace")
+
+
+def relay_recurrence(gate, value, out, workspace, initial=None, last=None, begins=None, lengths=None, stream=None):
+    """out_t = f_t out_{t-1} + (1 - f_t) value_t along the tokens, f = sigma(gate).
+
+    initial, last: the states (fp32 [n][d]) before the first and behind the last token; the same
+    tensor may be both.  begins (uint8 [n][tokens]): not 0 where a sequence begins, which takes
+    nothing from before it.  lengths (int32 [n]): the rows of each worker that count; the others
+    get 0 and leave the state as it is."""
+    lib = _library()
+    shape = type_, n, tokens, d = _shape_of("gate", gate)
+    dt, sh = gate.dtype, gate.shape
+    _check(lib.relay_recurrence(
+        *shape, _rows("gate", gate, dt, sh), _rows("value", value, dt, sh), *_state("initial", initial, n, d),
+        _plain("begins", begins, torch.uint8, (n, tokens)), _plain("lengths", lengths, torch.int32, (n,)),
+        _rows("out", out, dt, sh), *_state("last", last, n, d), *_workspace("workspace", workspace), _stream(stream)),
+        "relay_recurrence")
+
+
+def relay_recurrence_backward(dout, gate, value, out, dgate, dvalue, workspace, initial=None, dlast=None, dinitial=None,
+                              begins=None, lengths=None, stream=None):
+    """The gradients of gate and value from the rows of the forward pass, and, where dinitial
+    (fp32 [n][d]) is given, of the state before the first token.  dlast: the gradient that
+    reaches the last state."""
+    lib = _library()
+    shape = type_, n, tokens, d = _shape_of("dout", dout)
+    dt, sh = dout.dtype, dout.shape
+    _check(lib.relay_recurrence_backward(
+        *shape, _rows("dout", dout, dt, sh), _rows("gate", gate, dt, sh), _rows("value", value, dt, sh),
+        _rows("out", out, dt, sh), *_state("initial", initial, n, d), *_state("dlast", dlast, n, d),
+        _plain("begins", begins, torch.uint8, (n, tokens)), _plain("lengths", lengths, torch.int32, (n,)),
+        _rows("dgate", dgate, dt, sh), _rows("dvalue", dvalue, dt, sh), *_state("dinitial", dinitial, n, d),
+        *_workspace("workspace", workspace), _stream(stream)), "relay_recurrence_backward")
