@@ -11,6 +11,8 @@
  *   relay_gated               a = g sigma(g) u,  sigma(g) = 1 / (1 + exp(-g))
  *   relay_gated_backward      du = da g sigma(g);  dg = da u sigma(g) (1 + g (1 - sigma(g)));  a again
  *   relay_weight_grad         dW[o][i] = scale[i] sum_t dy[t][o] xhat[t][i]
+ *   relay_block_norm          h = rho r + sigma(z) (x s_x) w_post;  y = h s_h w_pre,  s the norms' reciprocal roots
+ *   relay_block_norm_backward its gradients
  *   relay_recurrence          h_t = f_t h_{t-1} + (1 - f_t) v_t,  f = sigma(gate)
  *   relay_recurrence_backward l_t = dh_t + f_{t+1} l_{t+1};  dv = l (1 - f);  dgate = l (h_{t-1} - v) f (1 - f)
  *   relay_checkpoint_pack     any activation to 8 bits, and
@@ -44,9 +46,10 @@
  *     device buffers, nothing allocated, nothing synchronised, every argument
  *     checked before anything is enqueued.  The sizes that the library cannot
  *     see (of the buffers) are the caller's to get right.  An output may not
- *     be another argument's buffer, with one exception: `total` of
- *     relay_rms_norm may be the view of x or of the residual (the same rows
- *     at the same strides).
+ *     be another argument's buffer, with the exceptions that a call names:
+ *     `total` of relay_rms_norm and relay_block_norm may be the view of x or
+ *     of the residual (the same rows at the same strides), the recurrence's
+ *     outgoing state its incoming one.
  *     RELAY_EINVAL: NULL for something needed, a size or stride out of range
  *     (n < 1, tokens < 0, d < 1, overlapping output rows), an address that
  *     is not a multiple of its element's size, checkpoint or workspace
@@ -170,6 +173,36 @@ int relay_weight_grad(int32_t type, int32_t n, int64_t tokens, int64_t outputs, 
                       const int8_t *codes, const uint8_t *scales, const float *column_scale,
                       int64_t column_scale_stride, const int32_t *lengths, float *dweight, int64_t worker_stride,
                       int64_t row_stride, void *workspace, int64_t workspace_bytes, relay_stream_t stream);
+
+/* From one block to the next: the norm of the block's output x, its gate, its
+ * addition to the residual r, and the norm of the sum for the next block:
+ *   m = x s_x post;  h = scale r + sigma(gate) m;  y = h s_h pre
+ * with s_x = 1 / sqrt(mean(x^2) + eps) and s_h likewise of the unrounded h.
+ * gate (rows) and scale (fp32, per feature) may be NULL: 1.  total (h in the
+ * rows' type), rstd (fp32 [2][n][tokens]: s_x, s_h) and codes with scales
+ * (h s_h in 8 bits) may each be NULL.  total may be the view of x or of the
+ * residual.  The squares are summed in fp32, as in relay_rms_norm. */
+int relay_block_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *x, const relay_rows *gate,
+                     const relay_rows *residual, const float *post, int64_t post_stride, const float *pre,
+                     int64_t pre_stride, const float *scale, int64_t scale_stride, float eps, const relay_rows *total,
+                     const relay_rows *y, float *rstd, int8_t *codes, uint8_t *scales, relay_stream_t stream);
+
+/* Bytes of workspace for relay_block_norm_backward, or a negative status. */
+int64_t relay_block_norm_backward_workspace(int32_t n, int64_t tokens, int64_t d);
+
+/* Its gradients, from the rows of the forward pass and rstd (h is formed
+ * again): of x, of the gate (given and asked for together), of the residual,
+ * and per worker, overwritten, of post, pre and scale (dscale may be NULL).
+ * dtotal: the gradient that reaches h past the second norm, or NULL.  Rows
+ * past the lengths count nowhere and get gradients of 0. */
+int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *dy,
+                              const relay_rows *dtotal, const relay_rows *x, const relay_rows *gate,
+                              const relay_rows *residual, const float *post, int64_t post_stride, const float *pre,
+                              int64_t pre_stride, const float *scale, int64_t scale_stride, const float *rstd,
+                              const int32_t *lengths, const relay_rows *dx, const relay_rows *dgate,
+                              const relay_rows *dresidual, float *dpost, int64_t dpost_stride, float *dpre,
+                              int64_t dpre_stride, float *dscale, int64_t dscale_stride, void *workspace,
+                              int64_t workspace_bytes, relay_stream_t stream);
 
 /* Bytes of workspace for relay_recurrence and relay_recurrence_backward (may
  * be 0), or a negative status. */

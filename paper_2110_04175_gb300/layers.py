@@ -42,6 +42,11 @@ _SIGNATURES = {
     "relay_weight_grad_workspace": (_i64, [_i32, _i32, _i64, _i64, _i64, _rows_p]),
     "relay_weight_grad": (ctypes.c_int, [_i32, _i32, _i64, _i64, _i64, _rows_p, _vp, _vp, _vp, _i64, _vp, _vp, _i64,
                                          _i64, _vp, _i64, _vp]),
+    "relay_block_norm": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _rows_p, _vp, _i64, _vp, _i64, _vp, _i64, _f32, _rows_p,
+                                                 _rows_p, _vp, _vp, _vp, _vp]),
+    "relay_block_norm_backward_workspace": (_i64, [_i32, _i64, _i64]),
+    "relay_block_norm_backward": (ctypes.c_int, _SHAPE + [_rows_p] * 5 + [_vp, _i64] * 3 + [_vp, _vp] + [_rows_p] * 3 +
+                                  [_vp, _i64] * 3 + [_vp, _i64, _vp]),
     "relay_recurrence_workspace": (_i64, [_i32, _i64, _i64]),
     "relay_recurrence": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _vp, _i64, _vp, _vp, _rows_p, _vp, _i64, _vp, _i64,
                                                  _vp]),
@@ -303,6 +308,46 @@ def relay_weight_grad(dy, checkpoint, dweight, workspace, column_scale=None, len
         *_held("checkpoint", checkpoint, n, tokens, inputs), scale, scale_stride,
         _plain("lengths", lengths, torch.int32, (n,)), dweight.data_ptr(), worker_stride, row_stride,
         *_workspace("workspace", workspace), _stream(stream)), "relay_weight_grad")
+
+
+def relay_block_norm(x, residual, post, pre, total, y, eps: float, gate=None, scale=None, rstd=None, checkpoint=None,
+                     stream=None):
+    """From one block to the next: total = scale residual + sigma(gate) norm(x) post; y = norm(total) pre.
+
+    post, pre, scale: fp32 [n][d]; without gate or scale they are 1.  total (the sum, which may be
+    x or residual itself, or None), rstd (fp32 [2][n][tokens]: the two norms' factors, what
+    relay_block_norm_backward reads) and checkpoint (norm(total) in 8 bits: with pre as
+    column_scale what relay_weight_grad reads) are written where given."""
+    lib = _library()
+    shape = type_, n, tokens, d = _shape_of("x", x)
+    dt, sh = x.dtype, x.shape
+    _check(lib.relay_block_norm(
+        *shape, _rows("x", x, dt, sh), _rows("gate", gate, dt, sh), _rows("residual", residual, dt, sh),
+        *_weights("post", post, n, d), *_weights("pre", pre, n, d), *_state("scale", scale, n, d), eps,
+        _rows("total", total, dt, sh), _rows("y", y, dt, sh), _plain("rstd", rstd, torch.float32, (2, n, tokens)),
+        *_held("checkpoint", checkpoint, n, tokens, d), _stream(stream)), "relay_block_norm")
+
+
+def relay_block_norm_backward_workspace(n: int, tokens: int, d: int) -> int:
+    """Bytes of workspace for relay_block_norm_backward."""
+    return _bytes(_library().relay_block_norm_backward_workspace(n, tokens, d), "relay_block_norm_backward_workspace")
+
+
+def relay_block_norm_backward(dy, x, residual, post, pre, rstd, dx, dresidual, dpost, dpre, workspace, gate=None, scale=None,
+                              dtotal=None, dgate=None, dscale=None, lengths=None, stream=None):
+    """The gradients of relay_block_norm: dx, dresidual and (with a gate) dgate, and dpost, dpre
+    and, where given, dscale (fp32 [n][d], overwritten).  dtotal: the gradient that reaches the
+    sum past the second norm.  lengths (int32 [n]): the rows of each worker that count."""
+    lib = _library()
+    shape = type_, n, tokens, d = _shape_of("dy", dy)
+    dt, sh = dy.dtype, dy.shape
+    _check(lib.relay_block_norm_backward(
+        *shape, _rows("dy", dy, dt, sh), _rows("dtotal", dtotal, dt, sh), _rows("x", x, dt, sh), _rows("gate", gate, dt, sh),
+        _rows("residual", residual, dt, sh), *_weights("post", post, n, d), *_weights("pre", pre, n, d),
+        *_state("scale", scale, n, d), _plain("rstd", rstd, torch.float32, (2, n, tokens)),
+        _plain("lengths", lengths, torch.int32, (n,)), _rows("dx", dx, dt, sh), _rows("dgate", dgate, dt, sh),
+        _rows("dresidual", dresidual, dt, sh), *_weights("dpost", dpost, n, d), *_weights("dpre", dpre, n, d),
+        *_state("dscale", dscale, n, d), *_workspace("workspace", workspace), _stream(stream)), "relay_block_norm_backward")
 
 
 def relay_recurrence_workspace(n: int, tokens: int, d: int) -> int:
