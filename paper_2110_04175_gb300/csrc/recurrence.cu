@@ -27,22 +27,35 @@ constexpr int kWide = 64;  // channels of a warp
 template <Way kWay>
 __device__ __forceinline__ int channel(int lane, int k) { return kWay == kVector ? 2 * lane + k : 32 * k + lane; }
 
+// Two channels as they lie in memory; 16-bit ones share a register.
 template <typename T>
-struct alignas(2 * sizeof(T)) Two {
-    T e[2];
-    __device__ __forceinline__ float get(int k) const { return widen(e[k]); }
+struct Two {
+    uint32_t w;
+    __device__ __forceinline__ float get(int k) const { return widen(reinterpret_cast<const T*>(&w)[k]); }
+    __device__ __forceinline__ void set(T a, T b) {
+        reinterpret_cast<T*>(&w)[0] = a;
+        reinterpret_cast<T*>(&w)[1] = b;
+    }
+};
+template <>
+__device__ __forceinline__ float Two<__nv_bfloat16>::get(int k) const {
+    return __uint_as_float(k == 0 ? w << 16 : w & 0xffff0000u);
+}
+template <>
+struct alignas(8) Two<float> {
+    float v[2];
+    __device__ __forceinline__ float get(int k) const { return v[k]; }
+    __device__ __forceinline__ void set(float a, float b) { v[0] = a, v[1] = b; }
 };
 
 template <Way kWay, typename T>
-__device__ __forceinline__ Two<T> load_two(const T* p, int lane, int left, bool on) {
+__device__ __forceinline__ Two<T> load_two(const T* p, int lane, int left) {
     Two<T> v;
-    v.e[0] = v.e[1] = T(0.0f);
     if constexpr (kWay == kVector) {
-        if (on && 2 * lane < left) v = *reinterpret_cast<const Two<T>*>(p + 2 * lane);
+        v.set(T(0.0f), T(0.0f));
+        if (2 * lane < left) v = *reinterpret_cast<const Two<T>*>(p + 2 * lane);
     } else {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (on && 32 * k + lane < left) v.e[k] = p[32 * k + lane];
+        v.set(lane < left ? p[lane] : T(0.0f), 32 + lane < left ? p[32 + lane] : T(0.0f));
     }
     return v;
 }
@@ -51,7 +64,7 @@ template <Way kWay, typename T>
 __device__ __forceinline__ void store_two(T* p, int lane, int left, const float (&v)[2]) {
     if constexpr (kWay == kVector) {
         Two<T> w;
-        w.e[0] = narrow<T>(v[0]), w.e[1] = narrow<T>(v[1]);
+        w.set(narrow<T>(v[0]), narrow<T>(v[1]));
         if (2 * lane < left) *reinterpret_cast<Two<T>*>(p + 2 * lane) = w;
     } else {
 #pragma unroll
@@ -78,13 +91,15 @@ __device__ __forceinline__ void store_state(float* p, int lane, int left, const 
 
 __device__ __forceinline__ bool starts(float a) { return __float_as_uint(a) == 0x80000000u; }
 
-// The state behind a token or a stretch (a, b).
-__device__ __forceinline__ float carry(float h, float a, float b) { return starts(a) ? b : fmaf(a, h, b); }
+// The state behind a token or a stretch (a, b).  kBegins: there may be beginnings.
+template <bool kBegins>
+__device__ __forceinline__ float carry(float h, float a, float b) { return kBegins && starts(a) ? b : fmaf(a, h, b); }
 
 // The stretch (a, b) with the one after it.
+template <bool kBegins>
 __device__ __forceinline__ void join(float& a, float& b, float a2, float b2) {
-    b = carry(b, a2, b2);
-    a = starts(a2) ? a2 : a * a2;
+    b = carry<kBegins>(b, a2, b2);
+    a = kBegins && starts(a2) ? a2 : a * a2;
 }
 
 // ------------------------------------------------------------------- the kernels
@@ -122,103 +137,131 @@ struct Place {
     }
 };
 
-// Tokens of a warp's run.
-template <typename T>
-constexpr int kRun = sizeof(T) == 2 ? 8 : 4;
+// Row addresses: aligned rows have strides below 2^30 elements (pairs()), which leaves one
+// instruction an address.
+template <Way kWay, typename T>
+__device__ __forceinline__ T* token_of(T* base, int64_t stride, int r) {
+    if constexpr (kWay == kVector) return base + static_cast<int64_t>(r) * static_cast<int32_t>(stride);
+    return base + r * stride;
+}
 
-// A run's rows as they lie in memory, so that the next ones can be on their way.
-template <typename T, Way kWay>
-struct Run {
-    Two<T> gate[kRun<T>], value[kRun<T>];
-    uint32_t begin;  // lane r: of token r
-    // tokens from `to` on are not asked for
-    __device__ __forceinline__ void ask(const RecurrenceArgs<T>& a, const Place<T>& p, int token, int to, int lane) {
-        const int left = a.d - p.strip;
+// kRun tokens of one activation as they lie in memory; those that do not count (from number
+// `counts` on) are `rest`.
+template <Way kWay, int kRun, typename T>
+__device__ __forceinline__ void load_run(Two<T> (&to)[kRun], const View<const T>& v, int worker, int token, int column,
+                                         int lane, int left, int counts, float rest = 0.0f) {
+    const T* from = v.row(worker, token) + column;
+    if (counts >= kRun) {
 #pragma unroll
-        for (int r = 0; r < kRun<T>; ++r) {
-            const bool on = token + r < to;
-            gate[r] = load_two<kWay>(a.gate.row(p.worker, token + r) + p.strip, lane, left, on);
-            value[r] = load_two<kWay>(a.value.row(p.worker, token + r) + p.strip, lane, left, on);
+        for (int r = 0; r < kRun; ++r) to[r] = load_two<kWay>(token_of<kWay>(from, v.ts, r), lane, left);
+    } else {
+#pragma unroll
+        for (int r = 0; r < kRun; ++r) {
+            to[r].set(narrow<T>(rest), narrow<T>(rest));
+            if (r < counts) to[r] = load_two<kWay>(token_of<kWay>(from, v.ts, r), lane, left);
         }
-        begin = 0;
-        if (a.begins != nullptr && lane < kRun<T> && token + lane < to)
-            begin = a.begins[static_cast<int64_t>(p.worker) * a.tokens + token + lane];
     }
-};
+}
 
-// Factor and addend of the run's tokens, and the run as one stretch; tokens from `to` on
-// change nothing.
-template <typename T, Way kWay>
-__device__ __forceinline__ void stretch(const Run<T, kWay>& run, int token, int to, float (&f)[kRun<T>][2],
-                                        float (&b)[kRun<T>][2], float (&ends)[4]) {
-    const uint32_t begins = __ballot_sync(0xffffffffu, run.begin != 0);
-    ends[0] = ends[1] = 1.0f;
-    ends[2] = ends[3] = 0.0f;
+constexpr float kKeeps = INFINITY;  // a gate that leaves the state as it is
+
+// Lane r: whether token r of the run begins a sequence; 0 where nothing says so.
+template <int kRun, bool kBegins, typename T>
+__device__ __forceinline__ uint32_t load_begins(const RecurrenceArgs<T>& a, int worker, int token, int lane, int counts) {
+    if (kBegins && a.begins != nullptr && lane < kRun && lane < counts) return a.begins[static_cast<int64_t>(worker) * a.tokens + token + lane];
+    return 0;
+}
+
+// Factor and addend of the run's tokens, and the run as one stretch.
+template <bool kBegins, int kRun, typename T>
+__device__ __forceinline__ void stretch(const Two<T> (&gate)[kRun], const Two<T> (&value)[kRun], uint32_t begin,
+                                        float (&f)[kRun][2], float (&b)[kRun][2], float (&ends)[4]) {
+    const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
 #pragma unroll
-    for (int r = 0; r < kRun<T>; ++r)
+    for (int r = 0; r < kRun; ++r)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const Gate<T> g(run.gate[r].get(k));
-            const bool on = token + r < to;
-            f[r][k] = !on ? 1.0f : begins >> r & 1 ? -0.0f : g.at;
-            b[r][k] = on ? g.rest * run.value[r].get(k) : 0.0f;
-            join(ends[k], ends[2 + k], f[r][k], b[r][k]);
+            const Gate<T> g(gate[r].get(k));
+            f[r][k] = kBegins && (begins >> r & 1) ? -0.0f : g.at;
+            b[r][k] = g.rest * value[r].get(k);
+            if (r == 0)
+                ends[k] = f[r][k], ends[2 + k] = b[r][k];
+            else
+                join<kBegins>(ends[k], ends[2 + k], f[r][k], b[r][k]);
         }
 }
 
 // The stretches of the kTime warps that share a tile, in their order: `h` goes from the
 // state before the tile to the one behind it, `mine` gets the one before warp `part`.
-template <int kTime>
+template <int kTime, bool kBegins>
 __device__ __forceinline__ void through(const float4 (*shared)[32], int part, int lane, float (&h)[2], float (&mine)[2]) {
 #pragma unroll
     for (int j = 0; j < kTime; ++j) {
         if (j == part) mine[0] = h[0], mine[1] = h[1];
         const float4 e = shared[j][lane];
-        h[0] = carry(h[0], e.x, e.z);
-        h[1] = carry(h[1], e.y, e.w);
+        h[0] = carry<kBegins>(h[0], e.x, e.z);
+        h[1] = carry<kBegins>(h[1], e.y, e.w);
     }
 }
 
-constexpr int kWarps = 16, kBackWarps = 8;
+constexpr int kWarps = 8;  // of a CTA, all of them a strip's, or kTime of them and the others other strips'
 
-// A segment's tokens tile by tile: kTime warps take a run each, the CTA's other warps
-// other strips.
-template <typename T, Way kWay, int kTime>
+// Tokens of a warp's run: as many as leave the next ones on their way too.
+template <typename T>
+constexpr int kRunOf = sizeof(T) == 2 ? 16 : 8;
+template <typename T>
+constexpr int kBackRunOf = sizeof(T) == 2 ? 8 : 4;
+
+// A segment's tokens tile by tile: kTime warps take a run each.
+template <typename T, Way kWay, int kTime, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(RecurrenceArgs<T> a) {
-    constexpr int kSide = kWarps / kTime, kTile = kTime * kRun<T>;
+    constexpr int kRun = kRunOf<T>, kSide = kWarps / kTime, kTile = kTime * kRun;
     __shared__ float4 shared[2][kSide][kTime][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kTime, part = warp % kTime;
     const Place<T> p(a, static_cast<int64_t>(blockIdx.x) * kSide + slot);
     const int left = p.on ? a.d - p.strip : 0, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
-    const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
+    const int end = p.on ? min(p.first + a.segment, a.tokens) : 0, to = min(end, p.length);
     float h[2];
     if (a.segments == 1)
         load_state<kWay>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, h);
     else
         load_state<kWay>(a.a + p.at, lane, left, h);
-    Run<T, kWay> run;
-    run.ask(a, p, p.first + part * kRun<T>, to, lane);
+    Two<T> gate[kRun], value[kRun];
+    uint32_t begin;
+    const auto ask = [&](int token) {
+        load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, to - token, kKeeps);
+        load_run<kWay>(value, a.value, p.worker, token, p.strip, lane, left, to - token);
+        begin = load_begins<kRun, kBegins>(a, p.worker, token, lane, to - token);
+    };
+    ask(p.first + part * kRun);
     for (int i = 0; i < tiles; ++i) {
-        const int token = p.first + i * kTile + part * kRun<T>;
-        float f[kRun<T>][2], b[kRun<T>][2], ends[4], x[2];
-        stretch(run, token, to, f, b, ends);
-        if (i + 1 < tiles) run.ask(a, p, token + kTile, to, lane);
+        const int token = p.first + i * kTile + part * kRun;
+        float f[kRun][2], b[kRun][2], ends[4], x[2];
+        stretch<kBegins>(gate, value, begin, f, b, ends);
+        if (i + 1 < tiles) ask(token + kTile);
         if constexpr (kTime > 1) {
             shared[i & 1][slot][part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
             __syncthreads();
-            through<kTime>(shared[i & 1][slot], part, lane, h, x);
+            through<kTime, kBegins>(shared[i & 1][slot], part, lane, h, x);
         } else {
             x[0] = h[0], x[1] = h[1];
         }
+        T* out = a.out.row(p.worker, token) + p.strip;
+        if (token + kRun <= to) {
 #pragma unroll
-        for (int r = 0; r < kRun<T>; ++r) {
-            float y[2];
+            for (int r = 0; r < kRun; ++r) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                x[k] = carry(x[k], f[r][k], b[r][k]);
-                y[k] = token + r < p.length ? x[k] : 0.0f;
+                for (int k = 0; k < 2; ++k) x[k] = carry<kBegins>(x[k], f[r][k], b[r][k]);
+                store_two<kWay>(token_of<kWay>(out, a.out.ts, r), lane, left, x);
             }
-            if (token + r < end) store_two<kWay>(a.out.row(p.worker, token + r) + p.strip, lane, left, y);
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRun; ++r) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[k] = carry<kBegins>(x[k], f[r][k], b[r][k]);
+                const float y[2] = {token + r < to ? x[0] : 0.0f, token + r < to ? x[1] : 0.0f};
+                if (token + r < end) store_two<kWay>(token_of<kWay>(out, a.out.ts, r), lane, left, y);
+            }
         }
         if constexpr (kTime == 1) h[0] = x[0], h[1] = x[1];
     }
@@ -227,30 +270,37 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(Recurr
 }
 
 // A segment as one stretch: each of the CTA's warps takes a part of its tokens.
-template <typename T, Way kWay>
+template <typename T, Way kWay, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_ends_kernel(RecurrenceArgs<T> a) {
+    constexpr int kRun = kRunOf<T>;
     __shared__ float4 shared[kWarps][32];
     const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
     const Place<T> p(a, blockIdx.x);
     const int left = a.d - p.strip, each = (a.segment + kWarps - 1) / kWarps;
     const int first = p.first + part * each, to = min(min(first + each, p.first + a.segment), p.length);
     float whole[4] = {1.0f, 1.0f, 0.0f, 0.0f};
-    Run<T, kWay> run;
-    run.ask(a, p, first, to, lane);
-    for (int token = first; token < to; token += kRun<T>) {
-        float f[kRun<T>][2], b[kRun<T>][2], ends[4];
-        stretch(run, token, to, f, b, ends);
-        run.ask(a, p, token + kRun<T>, to, lane);
+    Two<T> gate[kRun], value[kRun];
+    uint32_t begin;
+    const auto ask = [&](int token) {
+        load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, to - token, kKeeps);
+        load_run<kWay>(value, a.value, p.worker, token, p.strip, lane, left, to - token);
+        begin = load_begins<kRun, kBegins>(a, p.worker, token, lane, to - token);
+    };
+    ask(first);
+    for (int token = first; token < to; token += kRun) {
+        float f[kRun][2], b[kRun][2], ends[4];
+        stretch<kBegins>(gate, value, begin, f, b, ends);
+        ask(token + kRun);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) join(whole[k], whole[2 + k], ends[k], ends[2 + k]);
+        for (int k = 0; k < 2; ++k) join<kBegins>(whole[k], whole[2 + k], ends[k], ends[2 + k]);
     }
     shared[part][lane] = make_float4(whole[0], whole[1], whole[2], whole[3]);
     __syncthreads();
     if (part > 0) return;
     for (int j = 1; j < kWarps; ++j) {
         const float4 e = shared[j][lane];
-        join(whole[0], whole[2], e.x, e.z);
-        join(whole[1], whole[3], e.y, e.w);
+        join<kBegins>(whole[0], whole[2], e.x, e.z);
+        join<kBegins>(whole[1], whole[3], e.y, e.w);
     }
     const float one[2] = {whole[0], whole[1]}, two[2] = {whole[2], whole[3]};
     store_state<kWay>(a.a + p.at, lane, left, one);
@@ -281,7 +331,7 @@ relay_recurrence_carry_kernel(float* a, const float* b, int segments, int d, con
             const int s = kBack ? segments - 1 - s0 - j : s0 + j;
             if (s0 + j < segments) {
                 a[base + int64_t(s) * d] = h;
-                h = carry(h, fa[j], fb[j]);
+                h = carry<true>(h, fa[j], fb[j]);
             }
         }
     }
@@ -294,103 +344,107 @@ relay_recurrence_carry_kernel(float* a, const float* b, int segments, int d, con
 //   l_t = dout_t + m_{t+1},  dv_t = l_t (1 - f_t),  dgate_t = l_t (h_{t-1} - v_t) f_t (1 - f_t):
 // from the last token to the first m is the same kind of recurrence, m -> f_t m + f_t dout_t.
 
-template <typename T, Way kWay>
-struct BackRun {
-    Two<T> gate[kRun<T>], dout[kRun<T>];
-    uint32_t begin;
-    __device__ __forceinline__ void ask(const RecurrenceArgs<T>& a, const Place<T>& p, int token, int to, int lane) {
-        const int left = a.d - p.strip;
+// The run as one stretch, from its last token to its first.
+template <bool kBegins, int kRun, typename T>
+__device__ __forceinline__ void back_stretch(const Two<T> (&gate)[kRun], const Two<T> (&dout)[kRun], uint32_t begins,
+                                             float (&ends)[4]) {
+    ends[0] = ends[1] = 1.0f;
+    ends[2] = ends[3] = 0.0f;
 #pragma unroll
-        for (int r = 0; r < kRun<T>; ++r) {
-            const bool on = token + r < to && token + r >= 0;
-            gate[r] = load_two<kWay>(a.gate.row(p.worker, token + r) + p.strip, lane, left, on);
-            dout[r] = load_two<kWay>(a.dout.row(p.worker, token + r) + p.strip, lane, left, on);
+    for (int r = kRun - 1; r >= 0; --r)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Gate<T> g(gate[r].get(k));
+            const bool begin = kBegins && (begins >> r & 1);
+            ends[k] = begin ? -0.0f : ends[k] * g.at;
+            ends[2 + k] = begin ? 0.0f : g.at * (ends[2 + k] + dout[r].get(k));
         }
-        begin = 0;
-        if (a.begins != nullptr && lane < kRun<T> && token + lane < to && token + lane >= 0)
-            begin = a.begins[static_cast<int64_t>(p.worker) * a.tokens + token + lane];
-    }
-    // The run as one stretch, from its last token to its first.
-    __device__ __forceinline__ void stretch(int token, int to, uint32_t begins, float (&ends)[4]) const {
-        ends[0] = ends[1] = 1.0f;
-        ends[2] = ends[3] = 0.0f;
-#pragma unroll
-        for (int r = kRun<T> - 1; r >= 0; --r)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const Gate<T> g(gate[r].get(k));
-                const bool on = token + r < to;
-                const float f = !on ? 1.0f : begins >> r & 1 ? -0.0f : g.at;
-                join(ends[k], ends[2 + k], f, on && !starts(f) ? f * dout[r].get(k) : 0.0f);
-            }
-    }
-};
+}
 
 // The forward kernel's tiles, from the segment's end to its start.  What the second sweep
 // needs of the gate is made again from the row.
-template <typename T, Way kWay, int kTime>
-__global__ void __launch_bounds__(32 * kBackWarps, 2) relay_recurrence_backward_kernel(RecurrenceArgs<T> a) {
-    constexpr int kSide = kBackWarps / kTime, kTile = kTime * kRun<T>;
+template <typename T, Way kWay, int kTime, bool kBegins>
+__global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kernel(RecurrenceArgs<T> a) {
+    constexpr int kRun = kBackRunOf<T>, kSide = kWarps / kTime, kTile = kTime * kRun;
     __shared__ float4 shared[2][kSide][kTime][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kTime, part = warp % kTime;
     const Place<T> p(a, static_cast<int64_t>(blockIdx.x) * kSide + slot);
     const int left = p.on ? a.d - p.strip : 0, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
-    const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
+    const int end = p.on ? min(p.first + a.segment, a.tokens) : 0, to = min(end, p.length);
     float m[2], first[2];
     if (a.segments == 1)
         load_state<kWay>(a.dlast == nullptr ? nullptr : a.dlast + p.worker * a.dlast_stride + p.strip, lane, left, m);
     else
         load_state<kWay>(a.a + p.at, lane, left, m);
     load_state<kWay>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, first);
-    BackRun<T, kWay> run;
-    Two<T> value[kRun<T>], before[kRun<T>];
+    Two<T> gate[kRun], dout[kRun], value[kRun], before[kRun];
+    uint32_t begin;
     const auto ask = [&](int token) {
-        run.ask(a, p, token, to, lane);
+        const int counts = to - token;
+        load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, counts, kKeeps);
+        load_run<kWay>(dout, a.dout, p.worker, token, p.strip, lane, left, counts);
+        load_run<kWay>(value, a.value, p.worker, token, p.strip, lane, left, counts);
+        if (token > 0) {
+            load_run<kWay>(before, a.out_in, p.worker, token - 1, p.strip, lane, left, counts);
+        } else {  // there is no row before the first
+            const T* from = a.out_in.row(p.worker, 0) + p.strip;
 #pragma unroll
-        for (int r = 0; r < kRun<T>; ++r) {
-            const int t = token + r;
-            value[r] = load_two<kWay>(a.value.row(p.worker, t) + p.strip, lane, left, t < to && t >= 0);
-            before[r] = load_two<kWay>(a.out_in.row(p.worker, t - 1) + p.strip, lane, left, t < to && t > 0);
+            for (int r = 0; r < kRun; ++r) {
+                before[r].set(T(0.0f), T(0.0f));
+                if (r > 0 && r < counts) before[r] = load_two<kWay>(token_of<kWay>(from, a.out_in.ts, r - 1), lane, left);
+            }
         }
+        begin = load_begins<kRun, kBegins>(a, p.worker, token, lane, counts);
     };
     // warp 0 of a tile takes its last tokens
-    const auto token_of = [&](int i) { return p.first + (tiles - 1 - i) * kTile + (kTime - 1 - part) * kRun<T>; };
-    ask(token_of(0));
+    const auto token_at = [&](int i) { return p.first + (tiles - 1 - i) * kTile + (kTime - 1 - part) * kRun; };
+    if (tiles > 0) ask(token_at(0));  // (without tokens there is no tile, and nothing to read)
     for (int i = 0; i < tiles; ++i) {
-        const int token = token_of(i);
-        const BackRun<T, kWay> now = run;
-        Two<T> v[kRun<T>], h[kRun<T>];
+        const int token = token_at(i);
+        Two<T> g[kRun], dh[kRun], v[kRun], h[kRun];
 #pragma unroll
-        for (int r = 0; r < kRun<T>; ++r) v[r] = value[r], h[r] = before[r];
-        if (i + 1 < tiles) ask(token_of(i + 1));
-        const uint32_t begins = __ballot_sync(0xffffffffu, now.begin != 0);
+        for (int r = 0; r < kRun; ++r) g[r] = gate[r], dh[r] = dout[r], v[r] = value[r], h[r] = before[r];
+        const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
+        if (i + 1 < tiles) ask(token_at(i + 1));
         float ends[4], x[2];
         if constexpr (kTime > 1) {
-            now.stretch(token, to, begins, ends);
+            back_stretch<kBegins>(g, dh, begins, ends);
             shared[i & 1][slot][part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
             __syncthreads();
-            through<kTime>(shared[i & 1][slot], part, lane, m, x);
+            through<kTime, kBegins>(shared[i & 1][slot], part, lane, m, x);
         } else {
             x[0] = m[0], x[1] = m[1];
         }
+        T *to_gate = a.dgate.row(p.worker, token) + p.strip, *to_value = a.dvalue.row(p.worker, token) + p.strip;
+        const auto step = [&](int r, float (&dg)[2], float (&dv)[2]) {
+            const bool starts = kBegins && (begins >> r & 1);
 #pragma unroll
-        for (int r = kRun<T> - 1; r >= 0; --r) {
-            const bool on = token + r < to, begin = begins >> r & 1;
-            float dg[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-            if (on) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const Gate<T> g(now.gate[r].get(k));
-                    const float l = now.dout[r].get(k) + x[k];
-                    const float h0 = begin ? 0.0f : token + r == 0 ? first[k] : h[r].get(k);
-                    dv[k] = l * g.rest;
-                    dg[k] = dv[k] * g.at * (h0 - v[r].get(k));
-                    x[k] = begin ? 0.0f : g.at * l;
-                }
+            for (int k = 0; k < 2; ++k) {
+                const Gate<T> s(g[r].get(k));
+                const float l = dh[r].get(k) + x[k];
+                const float h0 = starts ? 0.0f : r == 0 && token == 0 ? first[k] : h[r].get(k);
+                dv[k] = l * s.rest;
+                dg[k] = dv[k] * s.at * (h0 - v[r].get(k));
+                x[k] = starts ? 0.0f : s.at * l;
             }
-            if (token + r < end && token + r >= p.first) {
-                store_two<kWay>(a.dgate.row(p.worker, token + r) + p.strip, lane, left, dg);
-                store_two<kWay>(a.dvalue.row(p.worker, token + r) + p.strip, lane, left, dv);
+        };
+        if (token + kRun <= to) {
+#pragma unroll
+            for (int r = kRun - 1; r >= 0; --r) {
+                float dg[2], dv[2];
+                step(r, dg, dv);
+                store_two<kWay>(token_of<kWay>(to_gate, a.dgate.ts, r), lane, left, dg);
+                store_two<kWay>(token_of<kWay>(to_value, a.dvalue.ts, r), lane, left, dv);
+            }
+        } else {
+#pragma unroll
+            for (int r = kRun - 1; r >= 0; --r) {
+                float dg[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
+                if (token + r < to) step(r, dg, dv);
+                if (token + r < end) {
+                    store_two<kWay>(token_of<kWay>(to_gate, a.dgate.ts, r), lane, left, dg);
+                    store_two<kWay>(token_of<kWay>(to_value, a.dvalue.ts, r), lane, left, dv);
+                }
             }
         }
         if constexpr (kTime == 1) m[0] = x[0], m[1] = x[1];
@@ -399,24 +453,34 @@ __global__ void __launch_bounds__(32 * kBackWarps, 2) relay_recurrence_backward_
         store_state<kWay>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
 
-template <typename T, Way kWay>
+template <typename T, Way kWay, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends_kernel(RecurrenceArgs<T> a) {
+    constexpr int kRun = kRunOf<T>;
     __shared__ float4 shared[kWarps][32];
     const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
     const Place<T> p(a, blockIdx.x);
     const int left = a.d - p.strip, each = (a.segment + kWarps - 1) / kWarps;
     const int first = p.first + part * each, to = min(min(first + each, p.first + a.segment), p.length);
     float whole[4] = {1.0f, 1.0f, 0.0f, 0.0f};
-    const int runs = to > first ? (to - first + kRun<T> - 1) / kRun<T> : 0;
-    BackRun<T, kWay> run;
-    if (runs > 0) run.ask(a, p, first + (runs - 1) * kRun<T>, to, lane);
+    const int runs = to > first ? (to - first + kRun - 1) / kRun : 0;
+    Two<T> gate[kRun], dout[kRun];
+    uint32_t begin = 0;
+    const auto ask = [&](int token) {
+        load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, to - token, kKeeps);
+        load_run<kWay>(dout, a.dout, p.worker, token, p.strip, lane, left, to - token);
+        begin = load_begins<kRun, kBegins>(a, p.worker, token, lane, to - token);
+    };
+    if (runs > 0) ask(first + (runs - 1) * kRun);
     for (int i = runs - 1; i >= 0; --i) {
-        const BackRun<T, kWay> now = run;
-        if (i > 0) run.ask(a, p, first + (i - 1) * kRun<T>, to, lane);
-        float ends[4];
-        now.stretch(first + i * kRun<T>, to, __ballot_sync(0xffffffffu, now.begin != 0), ends);
+        Two<T> g[kRun], dh[kRun];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) join(whole[k], whole[2 + k], ends[k], ends[2 + k]);
+        for (int r = 0; r < kRun; ++r) g[r] = gate[r], dh[r] = dout[r];
+        const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
+        if (i > 0) ask(first + (i - 1) * kRun);
+        float ends[4];
+        back_stretch<kBegins>(g, dh, begins, ends);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) join<kBegins>(whole[k], whole[2 + k], ends[k], ends[2 + k]);
     }
     shared[part][lane] = make_float4(whole[0], whole[1], whole[2], whole[3]);
     __syncthreads();
@@ -425,8 +489,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends
     whole[0] = e0.x, whole[1] = e0.y, whole[2] = e0.z, whole[3] = e0.w;
     for (int j = kWarps - 2; j >= 0; --j) {
         const float4 e = shared[j][lane];
-        join(whole[0], whole[2], e.x, e.z);
-        join(whole[1], whole[3], e.y, e.w);
+        join<kBegins>(whole[0], whole[2], e.x, e.z);
+        join<kBegins>(whole[1], whole[3], e.y, e.w);
     }
     const float one[2] = {whole[0], whole[1]}, two[2] = {whole[2], whole[3]};
     store_state<kWay>(a.a + p.at, lane, left, one);
@@ -446,7 +510,7 @@ Cut recurrence_cut(int64_t n, int64_t tokens, int64_t d) {
     const int64_t strips = (d + kWide - 1) / kWide, units = n * strips;
     int64_t segments = 1;
     if (units < 152 && tokens >= 1024) {
-        segments = 608 / units;
+        segments = 304 / units;
         if (segments > tokens / 256) segments = tokens / 256;
         if (segments > 128) segments = 128;
     }
@@ -478,15 +542,14 @@ bool apart(const float* out, int64_t out_stride, const float* in, int64_t in_str
 // Rows whose channels go two at a time.
 bool pairs(const relay_rows* r, int32_t type, int32_t n, int64_t tokens) {
     return aligned(r->data, 2 * element_size(type)) && (n == 1 || r->worker_stride % 2 == 0) &&
-           (tokens <= 1 || r->token_stride % 2 == 0);
+           (tokens <= 1 || (r->token_stride % 2 == 0 && r->token_stride < (int64_t(1) << 30)));
 }
 
 // f(warps that share a strip's tile) as a constant.
-template <int kMost, typename F>
+template <typename F>
 int by_time(int64_t tokens, int run, F f) {
     if (tokens <= run) return f(std::integral_constant<int, 1>());
-    if (tokens <= 4 * run) return f(std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, kMost>());
+    return f(std::integral_constant<int, kWarps>());
 }
 
 }  // namespace
@@ -529,14 +592,16 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
         a.strips = cut.strips, a.segments = cut.segments, a.segment = cut.segment;
         const int64_t units = static_cast<int64_t>(n) * cut.segments * cut.strips;
         if (cut.segments > 1) {
-            (vec ? relay_recurrence_ends_kernel<T, kVector> : relay_recurrence_ends_kernel<T, kDirect>)
+            (vec ? (begins != nullptr ? relay_recurrence_ends_kernel<T, kVector, true> : relay_recurrence_ends_kernel<T, kVector, false>)
+                 : relay_recurrence_ends_kernel<T, kDirect, true>)
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
             relay_recurrence_carry_kernel<false><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
                 a.a, a.b, cut.segments, a.d, initial, a.initial_stride, last, a.last_stride);
         }
-        return by_time<kWarps>(cut.segment, kRun<T>, [&](auto time) {
+        return by_time(cut.segment, kRunOf<T>, [&](auto time) {
             constexpr int kTime = decltype(time)::value, kSide = kWarps / kTime;
-            (vec ? relay_recurrence_kernel<T, kVector, kTime> : relay_recurrence_kernel<T, kDirect, kTime>)
+            (vec ? (begins != nullptr ? relay_recurrence_kernel<T, kVector, kTime, true> : relay_recurrence_kernel<T, kVector, kTime, false>)
+                 : relay_recurrence_kernel<T, kDirect, kTime, true>)
                 <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kWarps, 0, stream>>>(a);
             return status_of_launch();
         });
@@ -585,15 +650,19 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
         a.strips = cut.strips, a.segments = cut.segments, a.segment = cut.segment;
         const int64_t units = static_cast<int64_t>(n) * cut.segments * cut.strips;
         if (cut.segments > 1) {
-            (vec ? relay_recurrence_backward_ends_kernel<T, kVector> : relay_recurrence_backward_ends_kernel<T, kDirect>)
+            (vec ? (begins != nullptr ? relay_recurrence_backward_ends_kernel<T, kVector, true>
+                                      : relay_recurrence_backward_ends_kernel<T, kVector, false>)
+                 : relay_recurrence_backward_ends_kernel<T, kDirect, true>)
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
             relay_recurrence_carry_kernel<true><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
                 a.a, a.b, cut.segments, a.d, dlast, a.dlast_stride, dinitial, a.last_stride);
         }
-        return by_time<kBackWarps>(cut.segment, kRun<T>, [&](auto time) {
-            constexpr int kTime = decltype(time)::value, kSide = kBackWarps / kTime;
-            (vec ? relay_recurrence_backward_kernel<T, kVector, kTime> : relay_recurrence_backward_kernel<T, kDirect, kTime>)
-                <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kBackWarps, 0, stream>>>(a);
+        return by_time(cut.segment, kBackRunOf<T>, [&](auto time) {
+            constexpr int kTime = decltype(time)::value, kSide = kWarps / kTime;
+            (vec ? (begins != nullptr ? relay_recurrence_backward_kernel<T, kVector, kTime, true>
+                                      : relay_recurrence_backward_kernel<T, kVector, kTime, false>)
+                 : relay_recurrence_backward_kernel<T, kDirect, kTime, true>)
+                <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kWarps, 0, stream>>>(a);
             return status_of_launch();
         });
     });
