@@ -1,10 +1,12 @@
-// blackwell.cuh -- the sm_103a instructions that the weight gradient is made of:
+// blackwell.cuh -- the sm_103a instructions that the weight gradient, the orthogonal
+// update and the bulk copies are made of:
 // mbarriers, tensor copies (TMA), tensor memory and tcgen05 products.
 #pragma once
 
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 namespace {
@@ -149,6 +151,13 @@ __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, in
         : "memory");
 }
 
+// `bytes` next to one another, all three a multiple of 16 bytes.
+__device__ __forceinline__ void copy_row(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
 // Orders this thread's writes to shared memory before later reads by copies and
 // tensor cores.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -221,6 +230,43 @@ __device__ __forceinline__ void tensor_load(uint32_t at, float (&v)[16]) {
         : "memory");
 #pragma unroll
     for (int c = 0; c < 16; ++c) v[c] = __uint_as_float(r[c]);
+}
+
+// ------------------------------------------------------------------ on the host
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                            const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                            CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's cuTensorMapEncodeTiled, NULL where it has none.
+inline Encode encoder() {
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) !=
+                cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<Encode>(f);
+    }();
+    return encode;
+}
+
+// Lets Kernel use its shared memory, once per device.
+template <auto Kernel>
+bool allow_shared(int bytes) {
+    static std::atomic<bool> set[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    if (dev < 64 && set[dev].load()) return true;
+    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    if (dev < 64) set[dev].store(true);
+    return true;
 }
 
 }  // namespace

@@ -6,6 +6,9 @@
 //
 // All rows in and all rows out once, two sums over a row between them, so memory bounds it.
 // kParts warps share a row, each with kStrips strips of 256 features (layers.cuh).
+#include <type_traits>
+
+#include "blackwell.cuh"
 #include "layers.cuh"
 
 namespace {
@@ -19,6 +22,17 @@ struct Weight {  // fp32, from worker to worker
         load_weight<kWay>(p + worker * stride + base, lane, left, quads, v, turn);
     }
 };
+
+// The lane's octet of a weight of any alignment.
+__device__ __forceinline__ void load_octet(const Weight& w, int worker, int base, int lane, int left, float (&v)[8]) {
+    const float* p = w.p + worker * w.stride + base;
+    if (w.quads) {
+        load_strip<kVector>(p, lane, left, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = 8 * lane + k < left ? p[8 * lane + k] : 0.0f;
+    }
+}
 
 template <typename T>
 struct BlockArgs {
@@ -118,7 +132,12 @@ relay_block_norm_kernel(BlockArgs<T> a) {
 //   p = sigma(z);  dz = dh m p (1 - p);  v = dh p w_post;  dx = s_x (v - xhat mean(v xhat))
 //   dw_post = sum_t dh p xhat;  dw_pre = sum_t dy hhat
 //
-// with xhat = x s_x and hhat = h s_h made again from the rows.
+// with xhat = x s_x and hhat = h s_h made again from the rows.  With a = p xhat w_post (h is
+// rho r + a) the second mean is known with the first,
+//
+//   mean(v xhat) = mean(a (s_h u + dtotal)) - s_h mean(u hhat) mean(a hhat),
+//
+// so that a row waits for one sum over its warps, of three values.
 
 template <typename T>
 struct BlockBackwardArgs {
@@ -131,11 +150,61 @@ struct BlockBackwardArgs {
     int32_t tokens, d, pitch;
 };
 
+// What a lane makes again of 8 features of a row: `x`, `z`, `r` come as x, gate and residual
+// and leave as xhat, p and r; `w` and `rho` are w_post and rho (1 without).
+template <typename T>
+struct Octet {
+    float xhat[8], p[8], q[8], m[8], r[8], hhat[8];
+    __device__ __forceinline__ void make(const float (&w)[8], const float (&rho)[8], bool gated, float sx, float sh) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            xhat[k] *= sx;
+            m[k] = xhat[k] * w[k];
+            if (gated) {
+                const Gate<T> g(p[k]);
+                p[k] = g.at, q[k] = g.rest;
+            } else {
+                p[k] = 1.0f, q[k] = 0.0f;
+            }
+            hhat[k] = fmaf(rho[k], r[k], p[k] * m[k]) * sh;
+        }
+    }
+    // Adds to the three sums and to dw_pre.
+    __device__ __forceinline__ void add(const float (&dy)[8], const float (&pre)[8], const float (&over)[8], float sh,
+                                        float (&sums)[3], float (&dpre)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float u = dy[k] * pre[k], a = p[k] * m[k];
+            dpre[k] = fmaf(dy[k], hhat[k], dpre[k]);
+            sums[0] = fmaf(u, hhat[k], sums[0]);
+            sums[1] = fmaf(a, fmaf(sh, u, over[k]), sums[1]);
+            sums[2] = fmaf(a, hhat[k], sums[2]);
+        }
+    }
+    // The three gradients of the rows (dy becomes dx), and what w_post and rho get of them.
+    __device__ __forceinline__ void leave(float (&dy)[8], const float (&pre)[8], const float (&over)[8], const float (&w)[8],
+                                          const float (&rho)[8], float sx, float sh, float along, float along_x, float (&dz)[8],
+                                          float (&dr)[8], float (&dpost)[8], float (&dscale)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float d = fmaf(sh, fmaf(dy[k], pre[k], -hhat[k] * along), over[k]), dp = d * p[k];
+            dr[k] = rho[k] * d;
+            dz[k] = dp * m[k] * q[k];
+            dscale[k] = fmaf(d, r[k], dscale[k]);
+            dpost[k] = fmaf(dp, xhat[k], dpost[k]);
+            dy[k] = sx * fmaf(dp, w[k], -xhat[k] * along_x);
+        }
+    }
+};
+
+// Any rows: kParts warps share one, kStrips strips each, with what they need of it in
+// registers.  CTA (p, i) takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i and
+// leaves their sums in its rows of `partial`.
 template <typename T, Way kWay, int kParts, int kStrips>
 __global__ void __launch_bounds__(32 * kNormWarps<kParts>, kNormWarps<kParts> > 8 ? 1 : 2)
 relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
     constexpr int kRows = kNormWarps<kParts> / kParts;
-    __shared__ float shared[kNormWarps<kParts>];
+    __shared__ float shared[3][kNormWarps<kParts>];
     WARP_TURN(kNormWarps<kParts>, true);
     extern __shared__ float sums[];  // kRows > 1: [kRows - 1][kStrips][kParts][256]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kParts, part = warp % kParts;
@@ -150,7 +219,7 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
         const bool counts = token < length;
         const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
         const float sx = counts ? a.rstd[row] : 0.0f, sh = counts ? a.rstd[static_cast<int64_t>(n) * a.tokens + row] : 0.0f;
-        Piece<T, kWay> x[kStrips], z[kStrips], r[kStrips], dy[kStrips];
+        Piece<T, kWay> x[kStrips], z[kStrips], r[kStrips], dy[kStrips], dtotal[kStrips];
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
             const int base = base_of(j), left = counts ? a.d - base : 0;
@@ -158,79 +227,53 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
             if (a.gate.p != nullptr) z[j].load(a.gate.row(worker, token) + base, lane, left);
             r[j].load(a.residual.row(worker, token) + base, lane, left);
             dy[j].load(a.dy.row(worker, token) + base, lane, left);
+            dtotal[j].load(a.dtotal.row(worker, token) + base, lane, a.dtotal.p != nullptr ? left : 0);
         }
-        // strip j's xhat, sigma(z) and the rest to 1, m, r, and hhat
-        const auto remake = [&](int j, float (&xhat)[8], float (&p)[8], float (&q)[8], float (&m)[8], float (&res)[8],
-                                float (&hhat)[8], float (&w)[8], float (&rho)[8]) {
+        const auto remake = [&](int j, Octet<T>& o, float (&w)[8], float (&rho)[8], float (&pre)[8], float (&u)[8], float (&over)[8]) {
             const int base = base_of(j), left = counts ? a.d - base : 0;
-            x[j].get(xhat);
-            a.post.template load<kWay>(worker, base, lane, left, w, turn);
-            r[j].get(res);
-            if (a.scale.p != nullptr) a.scale.template load<kWay>(worker, base, lane, left, rho, turn);
-            if (a.gate.p != nullptr) z[j].get(p);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (a.scale.p == nullptr) rho[k] = 1.0f;
-                xhat[k] *= sx;
-                m[k] = xhat[k] * w[k];
-                if (a.gate.p != nullptr) {
-                    const Gate<T> g(p[k]);
-                    p[k] = g.at, q[k] = g.rest;
-                } else {
-                    p[k] = 1.0f, q[k] = 0.0f;
-                }
-                hhat[k] = fmaf(rho[k], res[k], p[k] * m[k]) * sh;
-            }
-        };
-        float along = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kStrips; ++j) {
-            const int base = base_of(j), left = counts ? a.d - base : 0;
-            float xhat[8], p[8], q[8], m[8], res[8], hhat[8], w[8], rho[8], u[8], pre[8];
-            remake(j, xhat, p, q, m, res, hhat, w, rho);
+            x[j].get(o.xhat);
+            r[j].get(o.r);
             dy[j].get(u);
+            dtotal[j].get(over);
+            if (a.gate.p != nullptr) z[j].get(o.p);
+            a.post.template load<kWay>(worker, base, lane, left, w, turn);
             a.pre.template load<kWay>(worker, base, lane, left, pre, turn);
+            if (a.scale.p != nullptr) {
+                a.scale.template load<kWay>(worker, base, lane, left, rho, turn);
+            } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                dpre[j][k] = fmaf(u[k], hhat[k], dpre[j][k]);
-                along = fmaf(u[k] * pre[k], hhat[k], along);
+                for (int k = 0; k < 8; ++k) rho[k] = 1.0f;
             }
-        }
-        along = row_sum<kParts>(along, shared, slot, part) / static_cast<float>(a.d);
-        float along_x = 0.0f, dh[kStrips][8];
+            o.make(w, rho, a.gate.p != nullptr, sx, sh);
+        };
+        float three[3] = {};
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
-            const int base = base_of(j), left = counts ? a.d - base : 0;
-            float xhat[8], p[8], q[8], m[8], res[8], hhat[8], w[8], rho[8], pre[8], over[8] = {}, dg[8], dr[8];
-            remake(j, xhat, p, q, m, res, hhat, w, rho);
-            dy[j].get(dh[j]);
-            a.pre.template load<kWay>(worker, base, lane, left, pre, turn);
-            if (a.dtotal.p != nullptr) load_strip<kWay>(a.dtotal.row(worker, token) + base, lane, left, over);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float d = fmaf(sh, dh[j][k] * pre[k] - hhat[k] * along, over[k]);
-                dr[k] = counts ? rho[k] * d : 0.0f;
-                dg[k] = counts ? d * m[k] * p[k] * q[k] : 0.0f;
-                dscale[j][k] = fmaf(d, res[k], dscale[j][k]);
-                dpost[j][k] = fmaf(d * p[k], xhat[k], dpost[j][k]);
-                dh[j][k] = d * p[k] * w[k];
-                along_x = fmaf(dh[j][k], xhat[k], along_x);
-            }
-            if (token < a.tokens) {
-                store_strip<kWay>(a.dresidual.row(worker, token) + base, lane, a.d - base, dr);
-                if (a.dgate.p != nullptr) store_strip<kWay>(a.dgate.row(worker, token) + base, lane, a.d - base, dg);
-            }
+            Octet<T> o;
+            float w[8], rho[8], pre[8], u[8], over[8];
+            remake(j, o, w, rho, pre, u, over);
+            o.add(u, pre, over, sh, three, dpre[j]);
         }
-        along_x = row_sum<kParts>(along_x, shared, slot, part) / static_cast<float>(a.d);
-        if (token < a.tokens) {
 #pragma unroll
-            for (int j = 0; j < kStrips; ++j) {
-                float xhat[8];
-                x[j].get(xhat);
+        for (int e = 0; e < 3; ++e) three[e] = row_sum<kParts>(three[e], shared[e], slot, part) / static_cast<float>(a.d);
+        if (token >= a.tokens) continue;
+        const float along = three[0], along_x = three[1] - sh * along * three[2];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) dh[j][k] = counts ? sx * (dh[j][k] - xhat[k] * sx * along_x) : 0.0f;
-                store_strip<kWay>(a.dx.row(worker, token) + base_of(j), lane, a.d - base_of(j), dh[j]);
+        for (int j = 0; j < kStrips; ++j) {
+            const int base = base_of(j), left = a.d - base;
+            if (left <= 0) break;
+            Octet<T> o;
+            float w[8], rho[8], pre[8], u[8], over[8], dz[8], dr[8];
+            if (counts) {
+                remake(j, o, w, rho, pre, u, over);
+                o.leave(u, pre, over, w, rho, sx, sh, along, along_x, dz, dr, dpost[j], dscale[j]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) u[k] = dz[k] = dr[k] = 0.0f;
             }
+            store_strip<kWay>(a.dx.row(worker, token) + base, lane, left, u);
+            store_strip<kWay>(a.dresidual.row(worker, token) + base, lane, left, dr);
+            if (a.dgate.p != nullptr) store_strip<kWay>(a.dgate.row(worker, token) + base, lane, left, dz);
         }
     }
     const auto leave = [&](float (&v)[kStrips][8], int which) {
@@ -257,6 +300,180 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
     leave(dpost, 0);
     leave(dpre, 1);
     if (a.scale.p != nullptr) leave(dscale, 2);
+}
+
+// Aligned rows of up to 8192 features in 16 bits and 4096 in 32: rows come by bulk copies to
+// shared memory, two a group of kParts warps, so that the next one is on its way while this
+// one's two sweeps read it there, and registers are left for two strips' sums over the
+// tokens.  The groups of a CTA take rows of their own and wait only for themselves.
+template <typename T, int kParts>
+struct Ring {
+    static constexpr int kWarps = sizeof(T) == 2 ? 16 : 8, kGroups = kWarps / kParts, kStages = 2;
+    static constexpr int kRow = kParts * 2 * kStrip * static_cast<int>(sizeof(T));  // bytes kept free for a row
+    static constexpr int kStage = 5 * kRow;
+    static constexpr bool kWeights = kParts <= 8;  // there is room for the three weights too
+    static constexpr int kWide = kParts * 2 * kStrip;
+    static constexpr int kRows = kGroups * kStages * kStage, kShared = kRows + (kWeights ? 3 * 4 * kWide : 0) + 16;
+    static_assert(kShared <= 232448 - 2048, "shared memory of a CTA");
+};
+
+// A wait that runs out makes a group's results from there on NaN.
+template <typename T, int kParts>
+__global__ void __launch_bounds__(32 * Ring<T, kParts>::kWarps, 1) relay_block_norm_backward_rows_kernel(BlockBackwardArgs<T> a) {
+    using R = Ring<T, kParts>;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[R::kGroups][R::kStages];
+    __shared__ float shared[2][R::kGroups][kParts][3];
+    uint8_t* ring = raw + (16 - shared_address(raw) % 16) % 16;
+    float* weights = reinterpret_cast<float*>(ring + R::kRows);  // post, pre, rho
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, group = warp / kParts, part = warp % kParts;
+    const int worker = blockIdx.y, n = gridDim.y;
+    const int length = a.lengths == nullptr ? a.tokens : min(max(a.lengths[worker], 0), a.tokens);
+    const bool gated = a.gate.p != nullptr, over_too = a.dtotal.p != nullptr, scaled = a.scale.p != nullptr;
+    if (threadIdx.x < R::kGroups * R::kStages) barrier_init(shared_address(&bars[0][0] + threadIdx.x), 1);
+    barriers_ready();
+    if (R::kWeights) {
+        const Weight* from[3] = {&a.post, &a.pre, &a.scale};
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            for (int k = threadIdx.x; k < R::kWide; k += 32 * R::kWarps)
+                weights[e * R::kWide + k] = k >= a.d ? 0.0f : from[e]->p == nullptr ? 1.0f : from[e]->p[worker * from[e]->stride + k];
+    }
+    __syncthreads();
+
+    const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
+    const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
+    const bool brings = part == 0 && elected();
+    uint8_t* mine = ring + group * (R::kStages * R::kStage);
+    const auto bring = [&](int token, int s) {  // one thread of the group
+        const uint32_t bar = shared_address(&bars[group][s]), to = shared_address(mine + s * R::kStage);
+        barrier_expect(bar, bytes * (3 + gated + over_too));
+        copy_row(to, a.x.row(worker, token), bytes, bar);
+        copy_row(to + R::kRow, a.residual.row(worker, token), bytes, bar);
+        copy_row(to + 2 * R::kRow, a.dy.row(worker, token), bytes, bar);
+        if (gated) copy_row(to + 3 * R::kRow, a.gate.row(worker, token), bytes, bar);
+        if (over_too) copy_row(to + 4 * R::kRow, a.dtotal.row(worker, token), bytes, bar);
+    };
+    if (brings) {
+        if (begin < length) bring(begin, 0);
+        if (begin + step < length) bring(begin + step, 1);
+    }
+    float dpost[2][8] = {}, dpre[2][8] = {}, dscale[2][8] = {};
+    bool ok = true;
+    int i = 0;
+    for (int token = begin; token < length; token += step, ++i) {
+        const int s = i % 2;
+        const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
+        float sx = a.rstd[row];
+        const float sh = a.rstd[static_cast<int64_t>(n) * a.tokens + row];
+        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / 2 & 1);
+        if (!ok) sx = __int_as_float(0x7fffffff);
+        const auto remake = [&](int j, Octet<T>& o, float (&w)[8], float (&rho)[8], float (&pre)[8], float (&u)[8], float (&over)[8]) {
+            const int at = (part + kParts * j) * kStrip, left = a.d - at;
+            const T* from = reinterpret_cast<const T*>(mine + s * R::kStage) + at;
+            constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
+            load_strip<kVector>(from, lane, left, o.xhat);
+            load_strip<kVector>(from + kNext, lane, left, o.r);
+            load_strip<kVector>(from + 2 * kNext, lane, left, u);
+            if (gated) load_strip<kVector>(from + 3 * kNext, lane, left, o.p);
+            load_strip<kVector>(from + 4 * kNext, lane, over_too ? left : 0, over);
+            if constexpr (R::kWeights) {
+                load_strip<kVector>(weights + at, lane, left, w);
+                load_strip<kVector>(weights + R::kWide + at, lane, left, pre);
+                load_strip<kVector>(weights + 2 * R::kWide + at, lane, left, rho);
+            } else {
+                load_octet(a.post, worker, at, lane, left, w);
+                load_octet(a.pre, worker, at, lane, left, pre);
+                if (scaled) load_octet(a.scale, worker, at, lane, left, rho);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (!scaled) rho[k] = 1.0f;
+            }
+            o.make(w, rho, gated, sx, sh);
+        };
+        float three[3] = {};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            Octet<T> o;
+            float w[8], rho[8], pre[8], u[8], over[8];
+            remake(j, o, w, rho, pre, u, over);
+            o.add(u, pre, over, sh, three, dpre[j]);
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+#pragma unroll
+            for (int m = 16; m > 0; m >>= 1) three[e] += __shfl_xor_sync(0xffffffffu, three[e], m);
+        if constexpr (kParts > 1) {
+            float(&sums)[kParts][3] = shared[i & 1][group];
+            if (lane < 3) sums[part][lane] = lane == 0 ? three[0] : lane == 1 ? three[1] : three[2];
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kParts) : "memory");
+#pragma unroll
+            for (int e = 0; e < 3; ++e) {
+                three[e] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kParts; ++w) three[e] += sums[w][e];
+            }
+        } else {
+            __syncwarp();
+        }
+        // here every warp of the group is done with the row before this one
+        if (brings && i > 0 && token + step < length) bring(token + step, s ^ 1);
+        const float over_d = 1.0f / static_cast<float>(a.d), along = three[0] * over_d;
+        const float along_x = three[1] * over_d - sh * along * (three[2] * over_d);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = (part + kParts * j) * kStrip, left = a.d - at;
+            Octet<T> o;
+            float w[8], rho[8], pre[8], u[8], over[8], dz[8], dr[8];
+            remake(j, o, w, rho, pre, u, over);
+            o.leave(u, pre, over, w, rho, sx, sh, along, along_x, dz, dr, dpost[j], dscale[j]);
+            store_strip<kVector>(a.dx.row(worker, token) + at, lane, left, u);
+            store_strip<kVector>(a.dresidual.row(worker, token) + at, lane, left, dr);
+            if (gated) store_strip<kVector>(a.dgate.row(worker, token) + at, lane, left, dz);
+        }
+    }
+    // padding
+    for (int token = begin + i * step; token < a.tokens; token += step) {
+        const float none[8] = {};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = (part + kParts * j) * kStrip, left = a.d - at;
+            store_strip<kVector>(a.dx.row(worker, token) + at, lane, left, none);
+            store_strip<kVector>(a.dresidual.row(worker, token) + at, lane, left, none);
+            if (gated) store_strip<kVector>(a.dgate.row(worker, token) + at, lane, left, none);
+        }
+    }
+    // the groups' sums in their order, through the ring's memory: [kGroups - 1][kWide]
+    float* others = reinterpret_cast<float*>(ring);
+    const auto leave = [&](float (&v)[2][8], int which) {
+        if (R::kGroups > 1) {
+            __syncthreads();
+            if (group > 0) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    store_strip<kVector>(others + (group - 1) * R::kWide + (part + kParts * j) * kStrip, lane, kStrip, v[j]);
+            }
+            __syncthreads();
+            if (group > 0) return;
+            for (int g = 0; g < R::kGroups - 1; ++g)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float add[8];
+                    load_strip<kVector>(others + g * R::kWide + (part + kParts * j) * kStrip, lane, kStrip, add);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[j][k] += add[k];
+                }
+        }
+        float* out = a.partial + ((static_cast<int64_t>(which) * n + worker) * gridDim.x + blockIdx.x) * a.pitch;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = (part + kParts * j) * kStrip;
+            store_strip<kVector>(out + at, lane, a.pitch - at, v[j]);
+        }
+    };
+    leave(dpost, 0);
+    leave(dpre, 1);
+    if (scaled) leave(dscale, 2);
 }
 
 struct Sums {  // where the three sums go
@@ -298,13 +515,41 @@ int by_back_width(int64_t pitch, F f) {
 }
 
 // Rows of partial sums per worker, one per CTA: as many CTAs as are resident over all
-// workers, no more than there are tokens to take; multiples where a thread would add up
-// more than 256 rows in one chain.
+// workers (two per SM where they have 8 warps), no more than take a token each; multiples
+// where a thread would add up more than 256 rows in one chain.  The kernel of the aligned
+// rows takes at least as many side by side.
 int64_t block_partials(int32_t n, int64_t tokens, int64_t d) {
     const int64_t pitch = pitch_of(d), side = pitch <= 256 ? 8 : pitch <= 512 ? 4 : pitch <= 1024 ? 2 : 1;  // kRows
     const int64_t slots = pitch <= 2048 ? 304 : 152, fill = slots > n ? slots / n : 1, chain = fill * side * 256;
     const int64_t want = tokens > chain ? fill * ((tokens + chain - 1) / chain) : fill, most = (tokens + side - 1) / side;
     return most < want ? (most > 0 ? most : 1) : want;
+}
+
+// The same for the kernel of the aligned rows, one CTA per SM; never more than the above.
+template <typename T, int kParts>
+int64_t ring_partials(int32_t n, int64_t tokens, int64_t d) {
+    const int64_t side = Ring<T, kParts>::kGroups, fill = 152 > n ? 152 / n : 1, chain = fill * side * 256;
+    const int64_t want = tokens > chain ? fill * ((tokens + chain - 1) / chain) : fill, most = (tokens + side - 1) / side;
+    const int64_t parts = most < want ? (most > 0 ? most : 1) : want, room = block_partials(n, tokens, d);
+    return parts < room ? parts : room;
+}
+
+template <typename T, int kParts>
+int launch_rows(const BlockBackwardArgs<T>& a, int64_t parts, int32_t n, cudaStream_t stream) {
+    constexpr auto kernel = relay_block_norm_backward_rows_kernel<T, kParts>;
+    if (!allow_shared<kernel>(Ring<T, kParts>::kShared)) return RELAY_ECUDA;
+    kernel<<<dim3(static_cast<unsigned>(parts), n), 32 * Ring<T, kParts>::kWarps, Ring<T, kParts>::kShared, stream>>>(a);
+    return status_of_launch();
+}
+
+// f(kParts) for the least that holds a row in two strips a warp.
+template <typename F>
+int by_ring(int64_t pitch, F f) {
+    if (pitch <= 512) return f(std::integral_constant<int, 1>());
+    if (pitch <= 1024) return f(std::integral_constant<int, 2>());
+    if (pitch <= 2048) return f(std::integral_constant<int, 4>());
+    if (pitch <= 4096) return f(std::integral_constant<int, 8>());
+    return f(std::integral_constant<int, 16>());
 }
 
 bool weight_fits(const float* p, int64_t stride) { return p != nullptr && aligned(p, 4) && stride >= 0; }
@@ -404,7 +649,8 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     }
     bool vec = d % 8 == 0;
     for (const relay_rows* r : {dy, dtotal, x, gate, residual, dx, dgate, dresidual}) vec = vec && vectors(r, type, n, tokens);
-    const int parts = static_cast<int>(block_partials(n, tokens, d));
+    int parts = static_cast<int>(block_partials(n, tokens, d));
+    const bool ring = vec && tokens > 0 && d <= (type == RELAY_FP32 ? 4096 : 8192);
     const int rc = by_type(type, [&](auto t) {
         using T = decltype(t);
         const BlockBackwardArgs<T> a{
@@ -414,6 +660,15 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
             weight_of(pre, pre_stride, n, d), weight_of(scale, scale_stride, n, d), rstd, lengths,
             static_cast<float*>(workspace), static_cast<int32_t>(tokens), static_cast<int32_t>(d),
             static_cast<int32_t>(pitch_of(d))};
+        if (ring)
+            return by_ring(a.pitch, [&](auto with) {
+                constexpr int kParts = decltype(with)::value;
+                if constexpr (kParts <= Ring<T, 1>::kWarps) {
+                    parts = static_cast<int>(ring_partials<T, kParts>(n, tokens, d));
+                    return launch_rows<T, kParts>(a, parts, n, stream);
+                }
+                return RELAY_EUNSUPPORTED;  // (not reached: `ring`)
+            });
         return by_back_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr size_t kSmem = (kNormWarps<kParts> / kParts - 1) * kStrips * kParts * kStrip * sizeof(float);

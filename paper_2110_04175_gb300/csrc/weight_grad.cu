@@ -586,26 +586,6 @@ Cut best_cut(int terms, int64_t n, int64_t tokens, int64_t outputs, int64_t inpu
     return best;
 }
 
-using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                            const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                            CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's cuTensorMapEncodeTiled, NULL where it has none.
-Encode encoder() {
-    static const Encode encode = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) !=
-                cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<Encode>(f);
-    }();
-    return encode;
-}
-
 // The map of bf16 rows [planes][tokens][outputs] for boxes of 64 x 64.
 bool map_rows(CUtensorMap* map, const void* rows, int64_t planes, int64_t tokens, int64_t outputs,
               int64_t plane_bytes, int64_t row_bytes) {
@@ -648,21 +628,6 @@ bool map_codes(CUtensorMap* map, const int8_t* codes, int64_t rows, int64_t pitc
     return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(codes), dims, strides, box, steps,
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Lets Kernel use its shared memory, once per device.
-template <auto Kernel>
-bool allow_shared(int bytes) {
-    static std::atomic<bool> set[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    if (dev < 64 && set[dev].load()) return true;
-    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
-    if (dev < 64) set[dev].store(true);
-    return true;
 }
 
 template <int kTerms, int kN>

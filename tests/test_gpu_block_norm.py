@@ -95,7 +95,13 @@ def _backward(dy, over, x, z, r, post, pre, rho, sx, sh, used):
     v = dh * p * post
     ev = np.abs(p * post) * (edh + (off * q + 4 * U) * np.abs(dh))
     along_x = (v * xhat).sum(-1, keepdims=True) / d
-    spread_x = ((ev + (CHAIN + 4) * U * np.abs(v)) * np.abs(xhat)).sum(-1, keepdims=True) / d
+    # The kernels sum a (s_h u + dtotal), a hhat and u hhat, a = p xhat w_post, in one pass: their difference is
+    # the mean of v xhat, and its terms are as large as a Dh, however small v is (one feature: v is nearly 0).  Each
+    # sum is off by CHAIN U of its terms' magnitudes, products and the difference by a few U, and hhat and `along`
+    # by what edh has of them.
+    a = np.abs(p * m)
+    spread_x = (ev * np.abs(xhat) + a * ((CHAIN + 10) * U * Dh + off * q * Dh) + sh * a * (np.abs(hhat) * spread + eH * np.abs(along))
+                ).sum(-1, keepdims=True) / d
     dx = sx * (v - xhat * along_x)
     edx = sx * (ev + 4 * U * (np.abs(v) + np.abs(xhat * along_x)) + np.abs(xhat) * spread_x)
     dz = dh * m * p * q
