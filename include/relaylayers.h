@@ -15,6 +15,7 @@
  *   relay_block_norm_backward its gradients
  *   relay_recurrence          h_t = f_t h_{t-1} + (1 - f_t) v_t,  f = sigma(gate)
  *   relay_recurrence_backward l_t = dh_t + f_{t+1} l_{t+1};  dv = l (1 - f);  dgate = l (h_{t-1} - v) f (1 - f)
+ *   relay_orthogonalise       x = u / |u|, then x <- a x + (b g + c g g) x with g = x x^T, step by step
  *   relay_checkpoint_pack     any activation to 8 bits, and
  *   relay_checkpoint_unpack   back
  *
@@ -49,7 +50,7 @@
  *     be another argument's buffer, with the exceptions that a call names:
  *     `total` of relay_rms_norm and relay_block_norm may be the view of x or
  *     of the residual (the same rows at the same strides), the recurrence's
- *     outgoing state its incoming one.
+ *     outgoing state its incoming one, relay_orthogonalise's out its update.
  *     RELAY_EINVAL: NULL for something needed, a size or stride out of range
  *     (n < 1, tokens < 0, d < 1, overlapping output rows), an address that
  *     is not a multiple of its element's size, checkpoint or workspace
@@ -92,6 +93,8 @@ extern "C" {
 #define RELAY_NORM_MAX_D 32768
 #define RELAY_WEIGHT_GRAD_MAX_INPUTS (1 << 22)
 #define RELAY_RECURRENCE_MAX_N (1 << 20)
+#define RELAY_ORTHOGONALISE_MAX 65536
+#define RELAY_ORTHOGONALISE_MAX_STEPS 100
 
 /* A view [n][tokens][d] of device memory: element (i, t, k) is at
  * data + i worker_stride + t token_stride + k, strides in elements, >= 0. */
@@ -235,6 +238,27 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
                               const uint8_t *begins, const int32_t *lengths, const relay_rows *dgate,
                               const relay_rows *dvalue, float *dinitial, int64_t dinitial_stride, void *workspace,
                               int64_t workspace_bytes, relay_stream_t stream);
+
+/* Bytes of workspace for relay_orthogonalise, or a negative status. */
+int64_t relay_orthogonalise_workspace(int32_t n, int64_t rows, int64_t columns);
+
+/* Makes n fp32 matrices [rows][columns] nearly orthogonal, each by itself, as
+ * the update of a weight matrix: x = update / (|update| + eps) with the root of
+ * the sum of squares |.|, then `steps` times
+ *   g = x x^T;  x <- a x + (b g + c g g) x,  a = 3.4445, b = -4.7750, c = 2.0315,
+ * or the same from the other side where rows outnumber columns; out = scale x.
+ * Five steps bring singular values from 0.002 of |update| up to between 0.68
+ * and 1.21.  Element (i, r, c) is at update + i worker_stride + r row_stride +
+ * c; out likewise, and may be the view of update.  Operands are held in 22 to
+ * 23 bits and summed in fp32.  A matrix of zeros stays zero; one that holds a
+ * value that is not finite becomes NaN, all of it.  rows, columns <=
+ * RELAY_ORTHOGONALISE_MAX, steps in 1 .. RELAY_ORTHOGONALISE_MAX_STEPS, eps >=
+ * 0.  The kernel's waits end after about a second each; results that one of
+ * them was for are NaN then. */
+int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float *update, int64_t worker_stride,
+                        int64_t row_stride, int32_t steps, float eps, float scale, float *out,
+                        int64_t out_worker_stride, int64_t out_row_stride, void *workspace, int64_t workspace_bytes,
+                        relay_stream_t stream);
 
 #ifdef __cplusplus
 }

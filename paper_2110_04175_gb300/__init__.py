@@ -39,6 +39,7 @@ from .layers import (RELAY_BF16, RELAY_FP16, RELAY_FP32, RELAY_NORM_MAX_D, Activ
                      relay_checkpoint_pack, relay_checkpoint_pitch, relay_checkpoint_unpack,
                      relay_gated, relay_gated_backward, relay_rms_norm, relay_rms_norm_backward,
                      relay_rms_norm_backward_workspace, relay_weight_grad, relay_weight_grad_workspace,
+                     relay_orthogonalise, relay_orthogonalise_workspace,
                      relay_block_norm, relay_block_norm_backward, relay_block_norm_backward_workspace,
                      relay_recurrence, relay_recurrence_backward, relay_recurrence_workspace)
 from .lr_correction import lr_correction  # noqa: E402
@@ -64,5 +65,5 @@ __all__ = [
     "relay_gated_backward", "relay_rms_norm", "relay_rms_norm_backward", "relay_rms_norm_backward_workspace",
     "relay_weight_grad", "relay_weight_grad_workspace", "relay_recurrence", "relay_recurrence_backward",
     "relay_recurrence_workspace", "relay_block_norm", "relay_block_norm_backward",
-    "relay_block_norm_backward_workspace",
+    "relay_block_norm_backward_workspace", "relay_orthogonalise", "relay_orthogonalise_workspace",
 ]

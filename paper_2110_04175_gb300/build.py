@@ -24,7 +24,7 @@ LIB = os.path.join(BUILD, "librelaysum.so")
 SOURCES = [("step_kernels.cu", ["-DRELAY_CAP=256", "-DRELAY_SPACE=large"]),
            ("step_kernels.cu", ["-DRELAY_CAP=64", "-DRELAY_SPACE=small"]),
            ("relaysum.cu", []), ("layer_kernels.cu", []), ("weight_grad.cu", []), ("recurrence.cu", []), ("block_norm.cu", []),
-           ("program.cpp", []),
+           ("orthogonalise.cu", []), ("program.cpp", []),
            ("host_step.cpp", [])]
 HEADERS = [os.path.join(CSRC, h) for h in ("program.h", "handle.h", "device.cuh", "step_launch.h", "layers.cuh",
                                               "blackwell.cuh")] + [

@@ -1,0 +1,523 @@
+// orthogonalise.cu -- an update made orthogonal by Newton-Schulz steps (relay_orthogonalise
+// of relaylayers.h) on GB300 (sm_103a):
+//
+//   x = u / (|u| + eps);  a step: g = x x^T,  x <- a x + (b g + c g g) x
+//
+// with x as wide as it is high or wider (u or its transpose).  Three products a step, on the
+// tensor cores, bound by them.
+//
+// A step multiplies small singular values by 3.4, five of them by 480, and what an operand
+// is rounded by with them: bf16 operands would leave 1 % of noise.  So every operand is
+// held as two fp16 terms, hi + lo, 22 to 23 bits, and a product is three of theirs (lo lo is
+// below what an fp32 sum keeps).  Singular values stay within 1.21, b g + c g g within 2.9,
+// and operands are held times 2^12: the terms of an element of 2^-10 still have all their
+// bits, and nothing reaches fp16's 65504.
+//
+// A pair of CTAs makes a tile of 256 x kN (cta_group::2), each brings half of both operands
+// by TMA.  x x^T and g g are symmetric: tiles above the diagonal are copies.  The tensor
+// cores cut off what an addition shifts out, so sums leave them every kGroup stages for
+// registers of other warps, as in the weight gradient.
+#include <cuda_fp16.h>
+
+#include "blackwell.cuh"
+#include "layers.cuh"
+
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kHeld = 4096.0f;  // operands are held times this
+
+constexpr int kM = 128, kDepth = 64;  // rows of a CTA, and what a stage goes along the summed axis
+constexpr int kAdders = 8, kIssuer = 8, kLoader = 9, kThreads = 32 * 12;
+constexpr int kGroup = 3;  // stages that the tensor cores sum: 36 additions
+constexpr int kSms = 152;
+
+template <int kN>
+struct Stages {
+    static constexpr int kLeftTerm = kM * 128, kRightTerm = kN / 2 * 128;  // bytes of a term in a CTA
+    static constexpr int kBytes = 2 * (kLeftTerm + kRightTerm);
+    static constexpr int kCount = kN == 256 ? 3 : 4;
+    static constexpr int kShared = kCount * kBytes + 1024 + 256;
+    static_assert(kShared <= 232448, "shared memory of a CTA");
+};
+
+struct ProductArgs {
+    const __half* c;  // what is added, times beta: [n][2][rows][pitch]
+    __half* out;      // the same shape, or NULL, and
+    float* final;     // fp32: element (i, j) at i row_stride + j column_stride
+    int64_t worker_stride, row_stride, column_stride;
+    float alpha, beta;
+    int32_t n, rows, columns, depth, pitch;
+    int32_t tiles_m, tiles_n, tiles;
+};
+
+// The tile's place; kFlip: all tiles, otherwise those on and below the diagonal.
+template <int kN, bool kFlip>
+struct Tile {
+    int worker, row, column;
+    bool mirror;
+    __device__ __forceinline__ Tile(const ProductArgs& a, int tile) {
+        const int plane = a.tiles / a.n;
+        worker = tile / plane;
+        int at = tile - worker * plane, i, j;
+        if (kFlip) {  // bands of 4 rows, so that those in work at a time share operands
+            const int band = at / (4 * a.tiles_n), in = at - band * 4 * a.tiles_n, high = min(4, a.tiles_m - 4 * band);
+            i = 4 * band + in % high;
+            j = in / high;
+            mirror = false;
+        } else {
+            constexpr int kWide = 256 / kN;  // tiles across a diagonal block
+            for (i = 0;; ++i) {
+                const int across = min(kWide * (i + 1), a.tiles_n);
+                if (at < across) break;
+                at -= across;
+            }
+            j = at;
+            mirror = j < kWide * i;
+        }
+        row = i * 2 * kM;
+        column = j * kN;
+    }
+};
+
+// Operand in shared memory whose fastest axis is K, 64 of it in rows of 128 bytes, in the
+// 128-byte swizzle: groups of 8 rows are 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand_k(uint32_t at) {
+    return static_cast<uint64_t>((at & 0x3FFFFu) >> 4) | uint64_t(1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 |
+           uint64_t(2) << 61;
+}
+
+// fp16 x fp16 to fp32 for a pair of CTAs; kFlip: the right operand has N fastest.
+template <int kN, bool kFlip>
+constexpr uint32_t kKind = 1u << 4 | uint32_t(kFlip) << 16 | uint32_t(kN / 8) << 17 | uint32_t(2 * kM / 16) << 24;
+
+__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
+    hi = __float2half_rn(v);
+    lo = __float2half_rn(v - __half2float(hi));
+}
+
+// out = alpha left right + beta c.  left [n][2][rows][depth]; right [n][2][columns][depth], or with kFlip
+// [n][2][depth][columns].  A wait that runs out ends a pair's work, and its results from there on are NaN.
+template <int kN, bool kFlip>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap left_map,
+                           const __grid_constant__ CUtensorMap right_map) {
+    using S = Stages<kN>;
+    constexpr int kCount = S::kCount;
+    extern __shared__ uint8_t raw[];
+    const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t bars = stages + kCount * S::kBytes;
+    // per stage: full (on CTA 0 of the other CTA's half too) and free again; per accumulator:
+    // summed by the tensor cores, and read
+    const auto full = [&](int s) { return bars + 8 * s; };
+    const auto freed = [&](int s) { return bars + 8 * (kCount + s); };
+    const auto summed = [&](int b) { return bars + 8 * (2 * kCount + b); };
+    const auto read = [&](int b) { return bars + 8 * (2 * kCount + 2 + b); };
+    const uint32_t tensor_at = bars + 8 * (2 * kCount + 4);
+
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x / 32), 0), lane = threadIdx.x % 32;
+    const int rank = static_cast<int>(cluster_rank());
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int count = (a.depth + kDepth - 1) / kDepth;  // stages of a tile
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kCount; ++s) {
+            barrier_init(full(s), 1 + (rank == 0 ? 1 : 0));
+            barrier_init(freed(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            barrier_init(summed(b), 1);
+            barrier_init(read(b), kAdders);
+        }
+        barriers_ready();
+    }
+    if (warp == kIssuer) tensor_alloc<2 * kN>(tensor_at);
+    tensor_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tensor_fence_after();
+    uint32_t tensor;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
+
+    if (warp < kAdders) {
+        constexpr int kColumns = kN / 2;
+        const int row = 32 * (warp % 4), column = kColumns * (warp / 4);  // of the CTA's 128 x kN
+        bool ok = true;
+        int group = 0;  // of all that the pair has summed
+        for (int tile = pair; tile < a.tiles; tile += pairs) {
+            const Tile<kN, kFlip> at(a, tile);
+            float sum[kColumns] = {};
+            for (int done = 0; done < count && ok; done += kGroup, ++group) {
+                const int b = group & 1;
+                if (!(ok = barrier_wait_warp(summed(b), group >> 1 & 1))) break;
+                tensor_fence_after();
+                const uint32_t from = tensor + (static_cast<uint32_t>(row) << 16) + b * kN + column;
+#pragma unroll
+                for (int c = 0; c < kColumns; c += 16) {
+                    float v[16];
+                    tensor_load(from + c, v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[c + e] += v[e];
+                }
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(read(b));
+            }
+            const int i = at.row + kM * rank + row + lane;
+            const int64_t plane = static_cast<int64_t>(a.rows) * a.pitch;
+            const int64_t base = static_cast<int64_t>(at.worker) * 2 * plane;
+#pragma unroll
+            for (int c = 0; c < kColumns; c += 16) {
+                const int j = at.column + column + c;
+                if (j >= a.columns || i >= a.rows) break;
+                float v[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = ok ? a.alpha * sum[c + e] : __int_as_float(0x7fffffff);
+                if (a.c != nullptr) {
+                    const uint4* from = reinterpret_cast<const uint4*>(a.c + base + static_cast<int64_t>(i) * a.pitch + j);
+                    const uint4* from_lo = reinterpret_cast<const uint4*>(a.c + base + plane + static_cast<int64_t>(i) * a.pitch + j);
+                    uint4 hi[2] = {from[0], from[1]}, lo[2] = {from_lo[0], from_lo[1]};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        v[e] = fmaf(a.beta, __half2float(reinterpret_cast<const __half*>(hi)[e]) +
+                                                __half2float(reinterpret_cast<const __half*>(lo)[e]),
+                                    v[e]);
+                }
+                if (a.out != nullptr) {
+                    uint4 hi[2], lo[2];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) split(v[e], reinterpret_cast<__half*>(hi)[e], reinterpret_cast<__half*>(lo)[e]);
+                    __half* to = a.out + base + static_cast<int64_t>(i) * a.pitch + j;
+                    reinterpret_cast<uint4*>(to)[0] = hi[0], reinterpret_cast<uint4*>(to)[1] = hi[1];
+                    reinterpret_cast<uint4*>(to + plane)[0] = lo[0], reinterpret_cast<uint4*>(to + plane)[1] = lo[1];
+                    if (!kFlip && at.mirror) {  // its place above the diagonal
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (j + e >= a.columns) break;
+                            __half* over = a.out + base + static_cast<int64_t>(j + e) * a.pitch + i;
+                            over[0] = reinterpret_cast<const __half*>(hi)[e];
+                            over[plane] = reinterpret_cast<const __half*>(lo)[e];
+                        }
+                    }
+                } else {
+                    float* to = a.final + at.worker * a.worker_stride + i * a.row_stride + j * a.column_stride;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (j + e < a.columns) to[e * a.column_stride] = v[e];
+                }
+            }
+        }
+    } else if (warp == kIssuer) {
+        int i = 0, group = 0;  // of all that the pair has summed
+        bool ok = true;
+        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+            for (int n = 0; n < count; ++n, ++i) {
+                const int s = i % kCount, place = n % kGroup, b = group & 1;
+                if (place == 0 && group > 1 && !(ok = barrier_wait_warp(read(b), (group >> 1 & 1) ^ 1))) break;
+                if (!(ok = barrier_wait_warp(full(s), i / kCount & 1))) break;
+                const bool last = place == kGroup - 1 || n == count - 1;
+                if (rank != 0) {
+                    if (elected()) barrier_arrive_there(in_cta(full(s), 0));
+                } else {
+                    tensor_fence_after();
+                    if (elected()) {
+                        const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
+                        constexpr uint32_t kNext = kFlip ? 16 * 128 / 16 : 2;  // 16 of K, in 16 bytes
+#pragma unroll
+                        for (int k = 0; k < kDepth / 16; ++k)
+#pragma unroll
+                            for (int t = 0; t < 3; ++t) {  // lo hi, hi lo, hi hi
+                                const uint32_t at_r = r + (t == 1 ? S::kRightTerm : 0);
+                                const uint64_t x = operand_k(l + (t == 0 ? S::kLeftTerm : 0)) + 2 * k;
+                                const uint64_t y = (kFlip ? operand(at_r, kDepth * 128, 1024) : operand_k(at_r)) + kNext * k;
+                                product(tensor + b * kN, x, y, kKind<kN, kFlip>, place + k + t > 0);
+                            }
+                        products_arrive(freed(s));
+                        if (last) products_arrive(summed(b));
+                    }
+                    __syncwarp();
+                }
+                if (last) ++group;
+            }
+        }
+    } else if (warp == kLoader && elected()) {
+        int i = 0;
+        bool ok = true;
+        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+            const Tile<kN, kFlip> at(a, tile);
+            for (int n = 0; n < count; ++n, ++i) {
+                const int s = i % kCount, k = n * kDepth;
+                if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
+                barrier_expect(full(s), S::kBytes);
+                const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, 2 * at.worker + t, full(s));
+                    const int column = at.column + kN / 2 * rank;
+                    if (!kFlip)
+                        copy_box(r + t * S::kRightTerm, &right_map, k, column, 2 * at.worker + t, full(s));
+                    else
+#pragma unroll
+                        for (int p = 0; p < kN / 2 / 64; ++p)
+                            copy_box(r + t * S::kRightTerm + p * kDepth * 128, &right_map, column + 64 * p, k, 2 * at.worker + t,
+                                     full(s));
+                }
+            }
+        }
+        // nothing is left in flight: no copy, and no arrival that the last stages' products still send to this CTA
+        for (int j = max(0, i - kCount); j < i; ++j)
+            if (!barrier_wait(full(j % kCount), j / kCount & 1) || !barrier_wait(freed(j % kCount), j / kCount & 1)) break;
+    }
+    __syncwarp();
+    __syncthreads();
+    cluster_sync();  // the other CTA is done with this one's memory too
+    if (warp == kIssuer) tensor_free<2 * kN>(tensor);
+}
+
+// ------------------------------------------------------------------- the start
+
+constexpr int kParts = 128;  // CTAs that sum a matrix's squares, at most
+
+struct Update {
+    const float* p;
+    int64_t worker_stride, row_stride;
+    int32_t rows, columns;
+};
+
+// sums[worker][part][3]: of the squares of values of middling size, of those above 2^40 times
+// 2^-80 and of those below 2^-40 times 2^80, so that no sum leaves fp32.  (Values of one
+// matrix rarely are of more than one kind.)
+__global__ void __launch_bounds__(256) relay_orthogonalise_norm_kernel(Update u, float* sums) {
+    __shared__ float shared[8][3];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, strips = (u.columns + kStrip - 1) / kStrip;
+    const float* from = u.p + blockIdx.y * u.worker_stride;
+    float s[3] = {};
+    const int64_t all = static_cast<int64_t>(u.rows) * strips;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + warp; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
+        const int64_t row = i / strips;
+        const int base = static_cast<int>(i - row * strips) * kStrip;
+        float v[8], near = 0.0f;
+        load_strip<kDirect>(from + row * u.row_stride + base, lane, u.columns - base, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float m = fabsf(v[k]);
+            if (m > 0x1p40f)
+                s[1] = fmaf(v[k] * 0x1p-80f, v[k] * 0x1p-80f, s[1]);
+            else if (m < 0x1p-40f)
+                s[2] = fmaf(v[k] * 0x1p80f, v[k] * 0x1p80f, s[2]);
+            else
+                near = fmaf(v[k], v[k], near);  // NaN too
+        }
+        s[0] += near;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) s[e] += __shfl_xor_sync(0xffffffffu, s[e], m);
+        if (lane == 0) shared[warp][e] = s[e];
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        float t = 0.0f;
+        for (int w = 0; w < 8; ++w) t += shared[w][threadIdx.x];
+        sums[(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 3 + threadIdx.x] = t;
+    }
+}
+
+// kHeld / (|u| + eps), by all threads of a CTA; NaN where |u| is no number.
+__device__ double start_factor(const float* sums, int parts, float eps, double* shared) {
+    if (threadIdx.x == 0) {
+        double s[3] = {};
+        for (int p = 0; p < parts; ++p)
+            for (int e = 0; e < 3; ++e) s[e] += sums[(static_cast<int64_t>(blockIdx.y) * parts + p) * 3 + e];
+        const double length = sqrt(s[0] + s[1] * 0x1p160 + s[2] * 0x1p-160), over = length + eps;
+        *shared = !(length < 1e300) ? __longlong_as_double(0x7fffffffffffffffll) : over > 0.0 ? kHeld / over : 0.0;
+    }
+    __syncthreads();
+    return *shared;
+}
+
+// v f, also where f itself is past fp32 (lengths below 2^-115).
+__device__ __forceinline__ float times(float v, double f) {
+    return f < 1e38 ? v * static_cast<float>(f) : static_cast<float>(v * f);
+}
+
+// x = u f as two terms, [n][2][rows][pitch]: a warp takes strips of 256 columns.
+__global__ void __launch_bounds__(256)
+relay_orthogonalise_start_kernel(Update u, const float* sums, int parts, float eps, __half* x, int pitch) {
+    __shared__ double shared;
+    __shared__ __align__(16) float turns[8][kStrip];
+    const double f = start_factor(sums, parts, eps, &shared);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, strips = (u.columns + kStrip - 1) / kStrip;
+    const float* from = u.p + blockIdx.y * u.worker_stride;
+    const int64_t plane = static_cast<int64_t>(u.rows) * pitch, all = static_cast<int64_t>(u.rows) * strips;
+    __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + warp; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
+        const int64_t row = i / strips;
+        const int base = static_cast<int>(i - row * strips) * kStrip;
+        float v[8], lo[8];
+        load_strip<kDirect>(from + row * u.row_stride + base, lane, u.columns - base, v);
+        to_octets(v, lane, turns[warp]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            v[k] = times(v[k], f);
+            lo[k] = v[k] - __half2float(__float2half_rn(v[k]));
+        }
+        store_strip<kVector>(to + row * pitch + base, lane, pitch - base, v);
+        store_strip<kVector>(to + plane + row * pitch + base, lane, pitch - base, lo);
+    }
+}
+
+// The same of the transpose, x [n][2][columns][pitch]: a CTA takes squares of 64 x 64.
+__global__ void __launch_bounds__(256)
+relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float eps, __half* x, int pitch) {
+    __shared__ double shared;
+    __shared__ float square[64][65];
+    const double f = start_factor(sums, parts, eps, &shared);
+    const float* from = u.p + blockIdx.y * u.worker_stride;
+    const int64_t plane = static_cast<int64_t>(u.columns) * pitch;
+    __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
+    const int across = (u.columns + 63) / 64, all = (u.rows + 63) / 64 * across, lead = threadIdx.x / 64, at = threadIdx.x % 64;
+    for (int i = blockIdx.x; i < all; i += gridDim.x) {
+        const int row = i / across * 64, column = i % across * 64;
+        __syncthreads();
+#pragma unroll 4
+        for (int r = lead; r < 64; r += 4)
+            square[r][at] = row + r < u.rows && column + at < u.columns ? from[(row + r) * u.row_stride + column + at] : 0.0f;
+        __syncthreads();
+#pragma unroll 4
+        for (int c = lead; c < 64; c += 4) {
+            if (column + c >= u.columns || row + at >= u.rows) continue;
+            __half hi, lo;
+            split(times(square[at][c], f), hi, lo);
+            to[static_cast<int64_t>(column + c) * pitch + row + at] = hi;
+            to[plane + static_cast<int64_t>(column + c) * pitch + row + at] = lo;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- launching
+
+int pitch_to(int64_t columns) { return static_cast<int>((columns + 15) / 16 * 16); }  // 32 bytes
+
+// Two terms of n matrices for boxes of 64 columns x `high` rows.
+bool map_terms(CUtensorMap* map, const __half* p, int64_t n, int64_t rows, int64_t columns, int high) {
+    const cuuint64_t pitch = static_cast<cuuint64_t>(pitch_to(columns)) * 2;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(columns), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(2 * n)};
+    const cuuint64_t strides[2] = {pitch, pitch * static_cast<cuuint64_t>(rows)};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(high), 1}, steps[3] = {1, 1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(p), dims, strides, box, steps,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int kN, bool kFlip>
+int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t stream) {
+    constexpr auto kernel = relay_orthogonalise_kernel<kN, kFlip>;
+    constexpr int kShared = Stages<kN>::kShared;
+    if (!allow_shared<kernel>(kShared)) return RELAY_ECUDA;
+    CUtensorMap left_map, right_map;
+    if (!map_terms(&left_map, left, a.n, a.rows, a.depth, kM) ||
+        !(kFlip ? map_terms(&right_map, right, a.n, a.depth, a.columns, kDepth)
+                : map_terms(&right_map, right, a.n, a.columns, a.depth, kN / 2)))
+        return RELAY_ECUDA;
+    a.tiles_m = (a.rows + 2 * kM - 1) / (2 * kM);
+    a.tiles_n = (a.columns + kN - 1) / kN;
+    int64_t tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
+    if (!kFlip) {
+        tiles = 0;
+        for (int i = 0; i < a.tiles_m; ++i) tiles += 256 / kN * (i + 1) < a.tiles_n ? 256 / kN * (i + 1) : a.tiles_n;
+    }
+    tiles *= a.n;
+    if (tiles > INT32_MAX - kSms) return RELAY_EUNSUPPORTED;
+    a.tiles = static_cast<int32_t>(tiles);
+    const int pairs = tiles < kSms / 2 ? static_cast<int>(tiles) : kSms / 2;
+    kernel<<<2 * pairs, kThreads, kShared, stream>>>(a, left_map, right_map);
+    return status_of_launch();
+}
+
+// Where the workspace's parts begin, in bytes.
+struct Parts {
+    int64_t x, g, p, sums, size;
+    Parts(int64_t n, int64_t m, int64_t k) {
+        const int64_t wide = 4 * n * m * pitch_to(k), square = 4 * n * m * pitch_to(m);
+        x = 0, g = 2 * wide, p = g + square, sums = p + square, size = sums + 12 * n * kParts;
+    }
+};
+
+int check_matrices(int32_t n, int64_t rows, int64_t columns) {
+    if (n < 1 || rows < 1 || columns < 1) return RELAY_EINVAL;
+    if (n > RELAY_MAX_N || rows > RELAY_ORTHOGONALISE_MAX || columns > RELAY_ORTHOGONALISE_MAX) return RELAY_EUNSUPPORTED;
+    return RELAY_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t relay_orthogonalise_workspace(int32_t n, int64_t rows, int64_t columns) {
+    if (const int rc = check_matrices(n, rows, columns)) return rc;
+    return rows <= columns ? Parts(n, rows, columns).size : Parts(n, columns, rows).size;
+}
+
+int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* update, int64_t worker_stride,
+                        int64_t row_stride, int32_t steps, float eps, float scale, float* out, int64_t out_worker_stride,
+                        int64_t out_row_stride, void* workspace, int64_t workspace_bytes, relay_stream_t stream) {
+    if (const int rc = check_matrices(n, rows, columns)) return rc;
+    const relay_rows in{const_cast<float*>(update), worker_stride, row_stride}, to{out, out_worker_stride, out_row_stride};
+    if (!rows_fit(&in, RELAY_FP32, n, rows, columns, false) || !rows_fit(&to, RELAY_FP32, n, rows, columns, true) ||
+        crossed(&in, &to, n, rows))
+        return RELAY_EINVAL;
+    if (steps < 1 || steps > RELAY_ORTHOGONALISE_MAX_STEPS || !(eps >= 0.0f) || !(eps < 1e30f) || !(scale > -1e30f) ||
+        !(scale < 1e30f))
+        return RELAY_EINVAL;
+    if (workspace == nullptr || !aligned(workspace, 16) || workspace_bytes < relay_orthogonalise_workspace(n, rows, columns))
+        return RELAY_EINVAL;
+    if (encoder() == nullptr) return RELAY_ECUDA;
+
+    const bool tall = rows > columns;
+    const int64_t m = tall ? columns : rows, k = tall ? rows : columns;
+    const Parts parts(n, m, k);
+    char* base = static_cast<char*>(workspace);
+    __half* x[2] = {reinterpret_cast<__half*>(base), reinterpret_cast<__half*>(base + parts.g / 2)};
+    __half *g = reinterpret_cast<__half*>(base + parts.g), *p = reinterpret_cast<__half*>(base + parts.p);
+    float* sums = reinterpret_cast<float*>(base + parts.sums);
+    const Update u{update, n > 1 ? worker_stride : 0, rows > 1 ? row_stride : 0, static_cast<int32_t>(rows),
+                   static_cast<int32_t>(columns)};
+    const int64_t warps = rows * ((columns + kStrip - 1) / kStrip), want = (warps + 31) / 32;
+    const int cut = static_cast<int>(want < kParts ? want : kParts);
+    relay_orthogonalise_norm_kernel<<<dim3(cut, n), 256, 0, stream>>>(u, sums);
+    if (tall) {
+        const int64_t squares = (rows + 63) / 64 * ((columns + 63) / 64);
+        relay_orthogonalise_turn_kernel<<<dim3(static_cast<unsigned>(squares < 1024 ? squares : 1024), n), 256, 0, stream>>>(
+            u, sums, cut, eps, x[0], pitch_to(k));
+    } else {
+        const int64_t ctas = (warps + 7) / 8;
+        relay_orthogonalise_start_kernel<<<dim3(static_cast<unsigned>(ctas < 1024 ? ctas : 1024), n), 256, 0, stream>>>(
+            u, sums, cut, eps, x[0], pitch_to(k));
+    }
+    if (const int rc = status_of_launch()) return rc;
+
+    for (int step = 0; step < steps; ++step) {
+        const __half* now = x[step & 1];
+        ProductArgs a{};
+        a.n = n, a.rows = static_cast<int32_t>(m);
+        a.columns = static_cast<int32_t>(m), a.depth = static_cast<int32_t>(k), a.pitch = pitch_to(m);
+        a.alpha = 1.0f / kHeld, a.out = g;
+        if (const int rc = launch<256, false>(a, now, now, stream)) return rc;
+        a.depth = static_cast<int32_t>(m);
+        a.alpha = kC / kHeld, a.beta = kB, a.c = g, a.out = p;
+        if (const int rc = launch<256, false>(a, g, g, stream)) return rc;
+        a.columns = static_cast<int32_t>(k), a.pitch = pitch_to(k);
+        a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1];
+        if (step == steps - 1) {
+            a.alpha *= scale / kHeld, a.beta *= scale / kHeld;
+            a.out = nullptr, a.final = out, a.worker_stride = n > 1 ? out_worker_stride : 0;
+            a.row_stride = tall ? 1 : out_row_stride, a.column_stride = tall ? out_row_stride : 1;
+        }
+        if (const int rc = launch<256, true>(a, p, now, stream)) return rc;
+    }
+    return RELAY_OK;
+}
+
+}  // extern "C"

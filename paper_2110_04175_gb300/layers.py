@@ -47,6 +47,9 @@ _SIGNATURES = {
     "relay_block_norm_backward_workspace": (_i64, [_i32, _i64, _i64]),
     "relay_block_norm_backward": (ctypes.c_int, _SHAPE + [_rows_p] * 5 + [_vp, _i64] * 3 + [_vp, _vp] + [_rows_p] * 3 +
                                   [_vp, _i64] * 3 + [_vp, _i64, _vp]),
+    "relay_orthogonalise_workspace": (_i64, [_i32, _i64, _i64]),
+    "relay_orthogonalise": (ctypes.c_int, [_i32, _i64, _i64, _vp, _i64, _i64, _i32, _f32, _f32, _vp, _i64, _i64, _vp, _i64,
+                                           _vp]),
     "relay_recurrence_workspace": (_i64, [_i32, _i64, _i64]),
     "relay_recurrence": (ctypes.c_int, _SHAPE + [_rows_p, _rows_p, _vp, _i64, _vp, _vp, _rows_p, _vp, _i64, _vp, _i64,
                                                  _vp]),
@@ -386,3 +389,23 @@ def relay_recurrence_backward(dout, gate, value, out, dgate, dvalue, workspace, 
         _plain("begins", begins, torch.uint8, (n, tokens)), _plain("lengths", lengths, torch.int32, (n,)),
         _rows("dgate", dgate, dt, sh), _rows("dvalue", dvalue, dt, sh), *_state("dinitial", dinitial, n, d),
         *_workspace("workspace", workspace), _stream(stream)), "relay_recurrence_backward")
+
+
+def relay_orthogonalise_workspace(n: int, rows: int, columns: int) -> int:
+    """Bytes of workspace for relay_orthogonalise."""
+    return _bytes(_library().relay_orthogonalise_workspace(n, rows, columns), "relay_orthogonalise_workspace")
+
+
+def relay_orthogonalise(update, out, workspace, steps: int = 5, eps: float = 1e-7, scale: float = 1.0, stream=None):
+    """out = scale times `update` (fp32 [n][rows][columns], views of any strides with the columns next
+    to one another) made nearly orthogonal, each matrix by itself, by Newton-Schulz steps from
+    update / (|update| + eps).  out may be update itself."""
+    lib = _library()
+    if not isinstance(update, torch.Tensor) or update.dim() != 3:
+        _refuse("update", update, "an fp32 tensor [n][rows][columns] is needed")
+    n, rows, columns = update.shape
+    _rows("update", update, torch.float32, update.shape)
+    _rows("out", out, torch.float32, update.shape)
+    _check(lib.relay_orthogonalise(n, rows, columns, update.data_ptr(), *update.stride()[:2], steps, eps, scale, out.data_ptr(),
+                                   *out.stride()[:2], *_workspace("workspace", workspace), _stream(stream)),
+           "relay_orthogonalise")
