@@ -87,9 +87,15 @@ class GradientRun:
     one worker's step from zero with the centre -g, where the gradient 0 - (-g) is g itself;
     its step goes into the relay as the centre x + step at lr = 1, rounded as any addition
     to x.  ``x`` (fp32 [n][>= d]): the models.  ``descent`` (like x, zero where nothing is
-    written): the caller puts -g there, then calls ``step``."""
+    written): the caller puts -g there, then calls ``step``.
 
-    def __init__(self, n: int, d: int, edges, beta1: float = 0.9, beta2: float = 0.99, eps: float = 1e-8):
+    matrices: a function that gives the views [n][rows][columns] of rows like x which are
+    weight matrices.  Their step is not Adam's but orthogonal: m <- momentum m - g, and the
+    step lr sqrt(max(1, rows / columns)) times what relay_orthogonalise makes of
+    momentum m - g."""
+
+    def __init__(self, n: int, d: int, edges, beta1: float = 0.9, beta2: float = 0.99, eps: float = 1e-8, matrices=None,
+                 momentum: float = 0.95):
         import numpy as np
 
         from . import RelayRun
@@ -97,20 +103,40 @@ class GradientRun:
         self.x = self.relay.x
         self.adam = RelayRun(1, self.x.numel(), np.zeros((0, 2), np.int32), optimizer=("adam", beta1, beta2, eps))
         self.descent = self.adam.mu.view_as(self.x)
+        self.matrices, self.momentum = matrices or (lambda rows: []), momentum
+        views, self.velocity = self.matrices(self.x), None
+        if views:
+            import torch
+            self.velocity = torch.zeros_like(self.x)
+            need = max(rl.relay_orthogonalise_workspace(*m.shape) for m in views)
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.x.device)
 
     def init(self, x0_std: float, seed: int):
         """The same models everywhere, x0_std times normal values; no gradients yet."""
         import numpy as np
         self.relay.init(x0_std, seed, np.ones((self.n, 1)), 0.0, seed, 0.0)
         self.adam.init(0.0, seed, np.ones((1, 1)), 0.0, seed, 0.0)
+        if self.velocity is not None:
+            self.velocity.zero_()
 
     def step(self, lr: float, seed: int = 0):
         """One step of every worker with the gradients that `descent` holds, and its relay."""
         import torch
         self.adam.x.zero_()
         self.adam.step(lr, seed)
+        if self.velocity is not None:
+            self.orthogonal(lr)
         torch.add(self.x, self.adam.x.view_as(self.x), out=self.relay.mu)
         self.relay.step(1.0, seed)
+
+    def orthogonal(self, lr: float):
+        """The matrices' steps, in place of Adam's."""
+        import torch
+        step = self.adam.x.view_as(self.x)
+        for m, down, to in zip(*(self.matrices(rows) for rows in (self.velocity, self.descent, step))):
+            m.mul_(self.momentum).add_(down)
+            torch.add(down, m, alpha=self.momentum, out=to)
+            rl.relay_orthogonalise(to, to, self.workspace, scale=lr * max(1.0, m.shape[1] / m.shape[2]) ** 0.5)
 
 
 def train(n: int = 8, tokens: int = 256, d: int = 256, f: int = 512, steps: int = 100, lr: float = 0.02, seed: int = 0):
