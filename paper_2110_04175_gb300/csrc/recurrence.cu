@@ -49,18 +49,6 @@ struct alignas(8) Two<float> {
 };
 
 template <Way kWay, typename T>
-__device__ __forceinline__ Two<T> load_two(const T* p, int lane, int left) {
-    Two<T> v;
-    if constexpr (kWay == kVector) {
-        v.set(T(0.0f), T(0.0f));
-        if (2 * lane < left) v = *reinterpret_cast<const Two<T>*>(p + 2 * lane);
-    } else {
-        v.set(lane < left ? p[lane] : T(0.0f), 32 + lane < left ? p[32 + lane] : T(0.0f));
-    }
-    return v;
-}
-
-template <Way kWay, typename T>
 __device__ __forceinline__ void store_two(T* p, int lane, int left, const float (&v)[2]) {
     if constexpr (kWay == kVector) {
         Two<T> w;
@@ -145,20 +133,45 @@ __device__ __forceinline__ T* token_of(T* base, int64_t stride, int r) {
     return base + r * stride;
 }
 
+// `bits` or, where `on`, what lies at p.  In one instruction stream whether on or not, so that
+// no move waits for the load before its value is needed: with a branch around the loads of whole
+// runs every run waited for the next one's (310 us for [4][4096][4096] in bf16).
+__device__ __forceinline__ void load_if(uint32_t& v, const uint32_t* p, bool on) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.b32 %0, [%1];\n}" : "+r"(v) : "l"(p), "r"(uint32_t(on)));
+}
+__device__ __forceinline__ void load_if(float (&v)[2], const float* p, bool on) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %3, 0;\n@p ld.global.v2.f32 {%0, %1}, [%2];\n}"
+                 : "+f"(v[0]), "+f"(v[1])
+                 : "l"(p), "r"(uint32_t(on)));
+}
+
 // kRun tokens of one activation as they lie in memory; those that do not count (from number
-// `counts` on) are `rest`.
+// `counts` on, and the first one where `skip` says so, and channels from `left` on) are
+// `rest`.
 template <Way kWay, int kRun, typename T>
 __device__ __forceinline__ void load_run(Two<T> (&to)[kRun], const View<const T>& v, int worker, int token, int column,
-                                         int lane, int left, int counts, float rest = 0.0f) {
-    const T* from = v.row(worker, token) + column;
-    if (counts >= kRun) {
-#pragma unroll
-        for (int r = 0; r < kRun; ++r) to[r] = load_two<kWay>(token_of<kWay>(from, v.ts, r), lane, left);
-    } else {
+                                         int lane, int left, int counts, float rest = 0.0f, bool skip = false) {
+    const T* from = v.row(worker, token) + column + (kWay == kVector ? 2 * lane : lane);
+    if constexpr (kWay == kVector) {
+        if (2 * lane >= left) counts = 0;
 #pragma unroll
         for (int r = 0; r < kRun; ++r) {
             to[r].set(narrow<T>(rest), narrow<T>(rest));
-            if (r < counts) to[r] = load_two<kWay>(token_of<kWay>(from, v.ts, r), lane, left);
+            if constexpr (sizeof(T) == 2)
+                load_if(to[r].w, reinterpret_cast<const uint32_t*>(token_of<kWay>(from, v.ts, r)),
+                        r < counts && (r > 0 || !skip));
+            else
+                load_if(to[r].v, token_of<kWay>(from, v.ts, r), r < counts && (r > 0 || !skip));
+        }
+    } else {
+        const int first = lane < left ? counts : 0, second = 32 + lane < left ? counts : 0;
+#pragma unroll
+        for (int r = 0; r < kRun; ++r) {
+            const T* p = token_of<kWay>(from, v.ts, r);
+            T a = narrow<T>(rest), b = a;
+            if (r < first && (r > 0 || !skip)) a = p[0];
+            if (r < second && (r > 0 || !skip)) b = p[32];
+            to[r].set(a, b);
         }
     }
 }
@@ -384,16 +397,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
         load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, counts, kKeeps);
         load_run<kWay>(dout, a.dout, p.worker, token, p.strip, lane, left, counts);
         load_run<kWay>(value, a.value, p.worker, token, p.strip, lane, left, counts);
-        if (token > 0) {
-            load_run<kWay>(before, a.out_in, p.worker, token - 1, p.strip, lane, left, counts);
-        } else {  // there is no row before the first
-            const T* from = a.out_in.row(p.worker, 0) + p.strip;
-#pragma unroll
-            for (int r = 0; r < kRun; ++r) {
-                before[r].set(T(0.0f), T(0.0f));
-                if (r > 0 && r < counts) before[r] = load_two<kWay>(token_of<kWay>(from, a.out_in.ts, r - 1), lane, left);
-            }
-        }
+        // there is no row before the first
+        load_run<kWay>(before, a.out_in, p.worker, token - 1, p.strip, lane, left, counts, 0.0f, token == 0);
         begin = load_begins<kRun, kBegins>(a, p.worker, token, lane, counts);
     };
     // warp 0 of a tile takes its last tokens
