@@ -14,6 +14,7 @@
 // one has A = -0.
 #include <type_traits>
 
+#include "blackwell.cuh"
 #include "layers.cuh"
 
 namespace {
@@ -282,6 +283,128 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(Recurr
         store_state<kWay>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
 }
 
+// ------------------------------------------------------------- rows by tensor copies
+//
+// Rows that TMA takes (16-byte addresses and strides) come as boxes of 64 channels x a tile's
+// tokens to shared memory, kStages tiles of them, so that neither registers nor addresses are
+// spent on what is on its way.  A box may reach past the segment or the length: what it brings
+// from there is left out.
+
+constexpr int kStages = 3;
+
+template <typename T>
+struct TileMaps {
+    CUtensorMap gate, value, dout, out;
+};
+
+// Stages of kBoxes boxes of kTile tokens: the copies' barriers and the order of their places.
+template <typename T, int kBoxes, int kTile>
+struct Boxes {
+    static constexpr int kBox = kTile * kWide * static_cast<int>(sizeof(T)), kStage = kBoxes * kBox;
+    static constexpr int kShared = kStages * kStage + 128;
+    uint32_t bars, ring;  // in shared memory
+    const uint8_t* at;
+    __device__ __forceinline__ Boxes(uint64_t* barriers, uint8_t* raw) {
+        const uint32_t pad = (128 - shared_address(raw) % 128) % 128;
+        bars = shared_address(barriers), ring = shared_address(raw) + pad, at = raw + pad;
+        if (threadIdx.x < kStages) barrier_init(bars + 8 * threadIdx.x, 1);
+        barriers_ready();
+        __syncthreads();
+    }
+    __device__ __forceinline__ uint32_t expect(int tile) const {  // returns the stage's place
+        const int s = tile % kStages;
+        barrier_expect(bars + 8 * s, kStage);
+        return ring + s * kStage;
+    }
+    __device__ __forceinline__ uint32_t bar(int tile) const { return bars + 8 * (tile % kStages); }
+    // false after about a second; from then on nothing is waited for
+    __device__ __forceinline__ bool wait(int tile) const { return barrier_wait_warp(bar(tile), tile / kStages & 1); }
+    // The lane's two channels of token `token` of box `box`.
+    __device__ __forceinline__ Two<T> get(int tile, int box, int token, int lane) const {
+        return reinterpret_cast<const Two<T>*>(at + tile % kStages * kStage + box * kBox)[token * (kWide / 2) + lane];
+    }
+};
+
+template <typename T, bool kBegins>
+__global__ void __launch_bounds__(32 * kWarps, 2)
+relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const __grid_constant__ TileMaps<T> maps) {
+    constexpr int kRun = kRunOf<T>, kTile = kWarps * kRun;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t barriers[kStages];
+    __shared__ float4 shared[2][kWarps][32];
+    const Boxes<T, 2, kTile> boxes(barriers, raw);
+    const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
+    const Place<T> p(a, blockIdx.x);
+    const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
+    const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
+    const auto bring = [&](int i) {  // one thread
+        const uint32_t at = boxes.expect(i);
+        copy_box(at, &maps.gate, p.strip, p.first + i * kTile, p.worker, boxes.bar(i));
+        copy_box(at + boxes.kBox, &maps.value, p.strip, p.first + i * kTile, p.worker, boxes.bar(i));
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
+    float h[2];
+    if (a.segments == 1)
+        load_state<kVector>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, h);
+    else
+        load_state<kVector>(a.a + p.at, lane, left, h);
+    uint32_t begin = load_begins<kRun, kBegins>(a, p.worker, p.first + part * kRun, lane, to - p.first - part * kRun);
+    bool ok = true;
+    for (int i = 0; i < tiles; ++i) {
+        const int token = p.first + i * kTile + part * kRun, counts = to - token;
+        const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
+        if (kBegins && i + 1 < tiles) begin = load_begins<kRun, kBegins>(a, p.worker, token + kTile, lane, counts - kTile);
+        ok = ok && boxes.wait(i);
+        float f[kRun][2], b[kRun][2], ends[4], x[2];
+#pragma unroll
+        for (int r = 0; r < kRun; ++r) {
+            const Two<T> gate = boxes.get(i, 0, part * kRun + r, lane), value = boxes.get(i, 1, part * kRun + r, lane);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Gate<T> g(gate.get(k));
+                f[r][k] = kBegins && (begins >> r & 1) ? -0.0f : g.at;
+                b[r][k] = g.rest * value.get(k);
+            }
+        }
+        if (counts < kRun) {
+#pragma unroll
+            for (int r = 0; r < kRun; ++r)
+                if (r >= counts) f[r][0] = f[r][1] = 1.0f, b[r][0] = b[r][1] = 0.0f;
+        }
+        if (!ok) b[0][0] = b[0][1] = __int_as_float(0x7fffffff);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            ends[k] = f[0][k], ends[2 + k] = b[0][k];
+#pragma unroll
+            for (int r = 1; r < kRun; ++r) join<kBegins>(ends[k], ends[2 + k], f[r][k], b[r][k]);
+        }
+        shared[i & 1][part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
+        __syncthreads();  // here all warps are done with the tile before this one
+        if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
+        through<kWarps, kBegins>(shared[i & 1], part, lane, h, x);
+        T* out = a.out.row(p.worker, token) + p.strip;
+        if (counts >= kRun) {
+#pragma unroll
+            for (int r = 0; r < kRun; ++r) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[k] = carry<kBegins>(x[k], f[r][k], b[r][k]);
+                store_two<kVector>(token_of<kVector>(out, a.out.ts, r), lane, left, x);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRun; ++r) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[k] = carry<kBegins>(x[k], f[r][k], b[r][k]);
+                const float y[2] = {r < counts ? x[0] : 0.0f, r < counts ? x[1] : 0.0f};
+                if (token + r < end) store_two<kVector>(token_of<kVector>(out, a.out.ts, r), lane, left, y);
+            }
+        }
+    }
+    if (a.segments == 1 && a.last != nullptr && part == 0)
+        store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
+}
+
 // A segment as one stretch: each of the CTA's warps takes a part of its tokens.
 template <typename T, Way kWay, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_ends_kernel(RecurrenceArgs<T> a) {
@@ -458,6 +581,104 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
         store_state<kWay>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
 
+// The same with the rows by tensor copies.  What the first sweep makes of the gates stays for
+// the second one.
+template <typename T, bool kBegins>
+__global__ void __launch_bounds__(32 * kWarps, 2)
+relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const __grid_constant__ TileMaps<T> maps) {
+    constexpr int kRun = kBackRunOf<T>, kTile = kWarps * kRun;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t barriers[kStages];
+    __shared__ float4 shared[2][kWarps][32];
+    const Boxes<T, 4, kTile> boxes(barriers, raw);
+    const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
+    const Place<T> p(a, blockIdx.x);
+    const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
+    const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
+    const auto bring = [&](int i) {  // one thread
+        const uint32_t at = boxes.expect(i), bar = boxes.bar(i);
+        const int token = p.first + (tiles - 1 - i) * kTile;
+        copy_box(at, &maps.gate, p.strip, token, p.worker, bar);
+        copy_box(at + boxes.kBox, &maps.dout, p.strip, token, p.worker, bar);
+        copy_box(at + 2 * boxes.kBox, &maps.value, p.strip, token, p.worker, bar);
+        copy_box(at + 3 * boxes.kBox, &maps.out, p.strip, token - 1, p.worker, bar);  // (row -1 reads as 0)
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
+    float m[2], first[2];
+    if (a.segments == 1)
+        load_state<kVector>(a.dlast == nullptr ? nullptr : a.dlast + p.worker * a.dlast_stride + p.strip, lane, left, m);
+    else
+        load_state<kVector>(a.a + p.at, lane, left, m);
+    load_state<kVector>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, first);
+    // warp 0 of a tile takes its last tokens
+    const int place = (kWarps - 1 - part) * kRun;
+    const auto token_at = [&](int i) { return p.first + (tiles - 1 - i) * kTile + place; };
+    uint32_t begin = tiles > 0 ? load_begins<kRun, kBegins>(a, p.worker, token_at(0), lane, to - token_at(0)) : 0;
+    bool ok = true;
+    for (int i = 0; i < tiles; ++i) {
+        const int token = token_at(i), counts = to - token;
+        const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
+        if (kBegins && i + 1 < tiles) begin = load_begins<kRun, kBegins>(a, p.worker, token - kTile, lane, counts + kTile);
+        ok = ok && boxes.wait(i);
+        float at[kRun][2], rest[kRun][2], ends[4] = {1.0f, 1.0f, 0.0f, 0.0f}, x[2];
+#pragma unroll
+        for (int r = kRun - 1; r >= 0; --r) {
+            const Two<T> gate = boxes.get(i, 0, place + r, lane), dout = boxes.get(i, 1, place + r, lane);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Gate<T> g(gate.get(k));
+                at[r][k] = g.at, rest[r][k] = g.rest;
+                if (r < counts) {
+                    const bool starts = kBegins && (begins >> r & 1);
+                    ends[k] = starts ? -0.0f : ends[k] * g.at;
+                    ends[2 + k] = starts ? 0.0f : g.at * (ends[2 + k] + dout.get(k));
+                }
+            }
+        }
+        if (!ok) ends[2] = ends[3] = m[0] = m[1] = __int_as_float(0x7fffffff);
+        shared[i & 1][part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
+        __syncthreads();  // here all warps are done with the tile before this one
+        if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
+        through<kWarps, kBegins>(shared[i & 1], part, lane, m, x);
+        T *to_gate = a.dgate.row(p.worker, token) + p.strip, *to_value = a.dvalue.row(p.worker, token) + p.strip;
+        const auto step = [&](int r, float (&dg)[2], float (&dv)[2]) {
+            const Two<T> dout = boxes.get(i, 1, place + r, lane), value = boxes.get(i, 2, place + r, lane),
+                         before = boxes.get(i, 3, place + r, lane);
+            const bool starts = kBegins && (begins >> r & 1);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float l = dout.get(k) + x[k];
+                const float h0 = starts ? 0.0f : r == 0 && token == 0 ? first[k] : before.get(k);
+                dv[k] = l * rest[r][k];
+                dg[k] = dv[k] * at[r][k] * (h0 - value.get(k));
+                x[k] = starts ? 0.0f : at[r][k] * l;
+            }
+        };
+        if (counts >= kRun) {
+#pragma unroll
+            for (int r = kRun - 1; r >= 0; --r) {
+                float dg[2], dv[2];
+                step(r, dg, dv);
+                store_two<kVector>(token_of<kVector>(to_gate, a.dgate.ts, r), lane, left, dg);
+                store_two<kVector>(token_of<kVector>(to_value, a.dvalue.ts, r), lane, left, dv);
+            }
+        } else {
+#pragma unroll
+            for (int r = kRun - 1; r >= 0; --r) {
+                float dg[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
+                if (r < counts) step(r, dg, dv);
+                if (token + r < end) {
+                    store_two<kVector>(token_of<kVector>(to_gate, a.dgate.ts, r), lane, left, dg);
+                    store_two<kVector>(token_of<kVector>(to_value, a.dvalue.ts, r), lane, left, dv);
+                }
+            }
+        }
+    }
+    if (a.segments == 1 && a.last != nullptr && part == 0)
+        store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
+}
+
 template <typename T, Way kWay, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends_kernel(RecurrenceArgs<T> a) {
     constexpr int kRun = kRunOf<T>;
@@ -550,6 +771,33 @@ bool pairs(const relay_rows* r, int32_t type, int32_t n, int64_t tokens) {
            (tokens <= 1 || (r->token_stride % 2 == 0 && r->token_stride < (int64_t(1) << 30)));
 }
 
+// Whether TMA takes the rows: 16-byte steps, no row read twice.
+bool boxed(const relay_rows* r, int32_t type, int32_t n, int64_t tokens, int64_t d) {
+    constexpr int64_t kMost = int64_t(1) << 36;  // elements: a map's strides end at 2^40 bytes
+    return vectors(r, type, n, tokens) && r->token_stride >= d && r->token_stride < kMost &&
+           (n == 1 || (r->worker_stride >= d && r->worker_stride < kMost));
+}
+
+// The map of such rows for boxes of 64 channels x `high` tokens.
+bool map_tiles(CUtensorMap* map, const relay_rows* r, int32_t type, int32_t n, int64_t tokens, int64_t d, int high) {
+    const cuuint64_t e = static_cast<cuuint64_t>(element_size(type)), row = static_cast<cuuint64_t>(r->token_stride) * e;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(tokens), static_cast<cuuint64_t>(n)};
+    const cuuint64_t strides[2] = {row, n > 1 ? static_cast<cuuint64_t>(r->worker_stride) * e : row};
+    const cuuint32_t box[3] = {kWide, static_cast<cuuint32_t>(high), 1}, steps[3] = {1, 1, 1};
+    const CUtensorMapDataType as = type == RELAY_BF16   ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                   : type == RELAY_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    return encoder()(map, as, 3, r->data, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <auto Kernel, typename T>
+int launch_tiles(const RecurrenceArgs<T>& a, const TileMaps<T>& maps, int64_t units, int shared, cudaStream_t stream) {
+    if (!allow_shared<Kernel>(shared)) return RELAY_ECUDA;
+    Kernel<<<static_cast<unsigned>(units), 32 * kWarps, static_cast<size_t>(shared), stream>>>(a, maps);
+    return status_of_launch();
+}
+
 // f(warps that share a strip's tile) as a constant.
 template <typename F>
 int by_time(int64_t tokens, int run, F f) {
@@ -602,6 +850,16 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
             relay_recurrence_carry_kernel<false><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
                 a.a, a.b, cut.segments, a.d, initial, a.initial_stride, last, a.last_stride);
+        }
+        if (vec && cut.segment > kRunOf<T> && boxed(gate, type, n, tokens, d) && boxed(value, type, n, tokens, d) &&
+            encoder() != nullptr) {
+            constexpr int kTile = kWarps * kRunOf<T>;
+            TileMaps<T> maps{};
+            if (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile))
+                return RELAY_ECUDA;
+            constexpr int kShared = Boxes<T, 2, kTile>::kShared;
+            return begins != nullptr ? launch_tiles<relay_recurrence_tiles_kernel<T, true>>(a, maps, units, kShared, stream)
+                                     : launch_tiles<relay_recurrence_tiles_kernel<T, false>>(a, maps, units, kShared, stream);
         }
         return by_time(cut.segment, kRunOf<T>, [&](auto time) {
             constexpr int kTime = decltype(time)::value, kSide = kWarps / kTime;
@@ -661,6 +919,19 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
             relay_recurrence_carry_kernel<true><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
                 a.a, a.b, cut.segments, a.d, dlast, a.dlast_stride, dinitial, a.last_stride);
+        }
+        bool boxes = vec && cut.segment > kBackRunOf<T> && encoder() != nullptr;
+        for (const relay_rows* r : {dout, gate, value, out}) boxes = boxes && boxed(r, type, n, tokens, d);
+        if (boxes) {
+            constexpr int kTile = kWarps * kBackRunOf<T>;
+            TileMaps<T> maps{};
+            if (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile) ||
+                !map_tiles(&maps.dout, dout, type, n, tokens, d, kTile) || !map_tiles(&maps.out, out, type, n, tokens, d, kTile))
+                return RELAY_ECUDA;
+            constexpr int kShared = Boxes<T, 4, kTile>::kShared;
+            return begins != nullptr
+                       ? launch_tiles<relay_recurrence_backward_tiles_kernel<T, true>>(a, maps, units, kShared, stream)
+                       : launch_tiles<relay_recurrence_backward_tiles_kernel<T, false>>(a, maps, units, kShared, stream);
         }
         return by_time(cut.segment, kBackRunOf<T>, [&](auto time) {
             constexpr int kTime = decltype(time)::value, kSide = kWarps / kTime;
