@@ -227,9 +227,9 @@ template <typename T>
 constexpr int kBackRunOf = sizeof(T) == 2 ? 8 : 4;
 
 // A segment's tokens tile by tile: kTime warps take a run each.
-template <typename T, Way kWay, int kTime, bool kBegins>
+template <typename T, Way kWay, int kTime, int kRun, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(RecurrenceArgs<T> a) {
-    constexpr int kRun = kRunOf<T>, kSide = kWarps / kTime, kTile = kTime * kRun;
+    constexpr int kSide = kWarps / kTime, kTile = kTime * kRun;
     __shared__ float4 shared[2][kSide][kTime][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kTime, part = warp % kTime;
     const Place<T> p(a, static_cast<int64_t>(blockIdx.x) * kSide + slot);
@@ -499,9 +499,9 @@ __device__ __forceinline__ void back_stretch(const Two<T> (&gate)[kRun], const T
 
 // The forward kernel's tiles, from the segment's end to its start.  What the second sweep
 // needs of the gate is made again from the row.
-template <typename T, Way kWay, int kTime, bool kBegins>
+template <typename T, Way kWay, int kTime, int kRun, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kernel(RecurrenceArgs<T> a) {
-    constexpr int kRun = kBackRunOf<T>, kSide = kWarps / kTime, kTile = kTime * kRun;
+    constexpr int kSide = kWarps / kTime, kTile = kTime * kRun;
     __shared__ float4 shared[2][kSide][kTime][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, slot = warp / kTime, part = warp % kTime;
     const Place<T> p(a, static_cast<int64_t>(blockIdx.x) * kSide + slot);
@@ -735,7 +735,7 @@ struct Cut {
 Cut recurrence_cut(int64_t n, int64_t tokens, int64_t d) {
     const int64_t strips = (d + kWide - 1) / kWide, units = n * strips;
     int64_t segments = 1;
-    if (units < 152 && tokens >= 1024) {
+    if (units < 152 && tokens >= 512) {
         segments = 304 / units;
         if (segments > tokens / 256) segments = tokens / 256;
         if (segments > 128) segments = 128;
@@ -798,11 +798,14 @@ int launch_tiles(const RecurrenceArgs<T>& a, const TileMaps<T>& maps, int64_t un
     return status_of_launch();
 }
 
-// f(warps that share a strip's tile) as a constant.
-template <typename F>
-int by_time(int64_t tokens, int run, F f) {
-    if (tokens <= run) return f(std::integral_constant<int, 1>());
-    return f(std::integral_constant<int, kWarps>());
+// f(warps that share a strip's tile, tokens of a warp's run) as constants: one warp a strip
+// where its run holds all tokens, with a short run for few of them.
+template <int kRun, typename F>
+int by_time(int64_t tokens, F f) {
+    if (tokens <= 1) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    if (tokens <= 4) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+    if (tokens <= kRun) return f(std::integral_constant<int, 1>(), std::integral_constant<int, kRun>());
+    return f(std::integral_constant<int, kWarps>(), std::integral_constant<int, kRun>());
 }
 
 }  // namespace
@@ -861,10 +864,10 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
             return begins != nullptr ? launch_tiles<relay_recurrence_tiles_kernel<T, true>>(a, maps, units, kShared, stream)
                                      : launch_tiles<relay_recurrence_tiles_kernel<T, false>>(a, maps, units, kShared, stream);
         }
-        return by_time(cut.segment, kRunOf<T>, [&](auto time) {
-            constexpr int kTime = decltype(time)::value, kSide = kWarps / kTime;
-            (vec ? (begins != nullptr ? relay_recurrence_kernel<T, kVector, kTime, true> : relay_recurrence_kernel<T, kVector, kTime, false>)
-                 : relay_recurrence_kernel<T, kDirect, kTime, true>)
+        return by_time<kRunOf<T>>(cut.segment, [&](auto time, auto run) {
+            constexpr int kTime = decltype(time)::value, kRun = decltype(run)::value, kSide = kWarps / kTime;
+            (vec ? (begins != nullptr ? relay_recurrence_kernel<T, kVector, kTime, kRun, true> : relay_recurrence_kernel<T, kVector, kTime, kRun, false>)
+                 : relay_recurrence_kernel<T, kDirect, kTime, kRun, true>)
                 <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kWarps, 0, stream>>>(a);
             return status_of_launch();
         });
@@ -933,11 +936,11 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
                        ? launch_tiles<relay_recurrence_backward_tiles_kernel<T, true>>(a, maps, units, kShared, stream)
                        : launch_tiles<relay_recurrence_backward_tiles_kernel<T, false>>(a, maps, units, kShared, stream);
         }
-        return by_time(cut.segment, kBackRunOf<T>, [&](auto time) {
-            constexpr int kTime = decltype(time)::value, kSide = kWarps / kTime;
-            (vec ? (begins != nullptr ? relay_recurrence_backward_kernel<T, kVector, kTime, true>
-                                      : relay_recurrence_backward_kernel<T, kVector, kTime, false>)
-                 : relay_recurrence_backward_kernel<T, kDirect, kTime, true>)
+        return by_time<kBackRunOf<T>>(cut.segment, [&](auto time, auto run) {
+            constexpr int kTime = decltype(time)::value, kRun = decltype(run)::value, kSide = kWarps / kTime;
+            (vec ? (begins != nullptr ? relay_recurrence_backward_kernel<T, kVector, kTime, kRun, true>
+                                      : relay_recurrence_backward_kernel<T, kVector, kTime, kRun, false>)
+                 : relay_recurrence_backward_kernel<T, kDirect, kTime, kRun, true>)
                 <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kWarps, 0, stream>>>(a);
             return status_of_launch();
         });
