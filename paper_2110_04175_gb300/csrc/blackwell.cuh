@@ -166,19 +166,28 @@ __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.
 
 // The products are those of a pair of CTAs (a cluster of two): CTA r brings rows
 // 128 r .. of A and columns kN / 2 r .. of B in its shared memory and gets rows
-// 128 r .. of D in its tensor memory.
+// 128 r .. of D in its tensor memory.  With kCtas = 1 a CTA works alone, on 128 rows.
 
 // One warp of each CTA, all lanes; the address goes to shared memory.
-template <int kColumns>
+template <int kColumns, int kCtas = 2>
 __device__ __forceinline__ void tensor_alloc(uint32_t to) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "n"(kColumns)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    if constexpr (kCtas == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "n"(kColumns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "n"(kColumns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
 }
 
-template <int kColumns>
+template <int kColumns, int kCtas = 2>
 __device__ __forceinline__ void tensor_free(uint32_t at) {
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "n"(kColumns));
+    if constexpr (kCtas == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "n"(kColumns));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "n"(kColumns));
 }
 
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -198,24 +207,47 @@ constexpr uint32_t kProductKind =
     1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | uint32_t(kN / 8) << 17 | uint32_t(kM / 16) << 24;
 
 // D (+)= A B over 16 steps of K; one thread of CTA 0.
+template <int kCtas = 2>
 __device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
-    asm volatile(
-        "{\n"
-        ".reg .pred p;\n"
-        "setp.ne.u32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
-        "}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
-        : "memory");
+    if constexpr (kCtas == 2)
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "setp.ne.u32 p, %4, 0;\n"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+            "}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
+            : "memory");
+    else
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "setp.ne.u32 p, %4, 0;\n"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+            "}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
+            : "memory");
 }
 
-// The thread's products so far arrive at `bar` of both CTAs when they are done.
+// The thread's products so far arrive at `bar` (of both CTAs) when they are done.
+template <int kCtas = 2>
 __device__ __forceinline__ void products_arrive(uint32_t bar) {
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-        "h"(static_cast<uint16_t>(3))
-        : "memory");
+    if constexpr (kCtas == 2)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+            "h"(static_cast<uint16_t>(3))
+            : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+
+// ------------------------------------------------- kernels launched before their time
+
+// A kernel launched as a programmatic dependent starts while the one before it still runs:
+// nothing of that one's may be read or overwritten before this.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// From here on the next one may start.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // 16 columns of the warp's 32 lanes: v[c] is this lane's column c.
 __device__ __forceinline__ void tensor_load(uint32_t at, float (&v)[16]) {

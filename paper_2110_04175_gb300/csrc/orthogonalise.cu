@@ -29,30 +29,47 @@ constexpr float kHeld = 4096.0f;  // operands are held times this
 
 constexpr int kM = 128, kDepth = 64;  // rows of a CTA, and what a stage goes along the summed axis
 constexpr int kAdders = 8, kIssuer = 8, kLoader = 9, kThreads = 32 * 12;
-constexpr int kGroup = 3;  // stages that the tensor cores sum: 36 additions
 constexpr int kSms = 152;
 
-template <int kN>
-struct Stages {
-    static constexpr int kLeftTerm = kM * 128, kRightTerm = kN / 2 * 128;  // bytes of a term in a CTA
-    static constexpr int kBytes = 2 * (kLeftTerm + kRightTerm);
-    static constexpr int kCount = kN == 256 ? 3 : 4;
+// A kernel's shape: tiles of 128 kCtas x kN, operands of kTerms terms.
+template <int kCtas_, int kN_, int kTerms_>
+struct Shape {
+    static constexpr int kCtas = kCtas_, kN = kN_, kTerms = kTerms_, kHigh = kM * kCtas;
+    static constexpr int kRight = kN / kCtas;  // columns that a CTA brings
+    static constexpr int kLeftTerm = kM * 128, kRightTerm = kRight * 128;  // bytes of a term of a stage
+    static constexpr int kBytes = kTerms * (kLeftTerm + kRightTerm);
+    static constexpr int kFit = (232448 - 1024 - 256) / kBytes, kCount = kFit < 4 ? kFit : 4;  // stages
     static constexpr int kShared = kCount * kBytes + 1024 + 256;
-    static_assert(kShared <= 232448, "shared memory of a CTA");
+    static constexpr int kProducts = kTerms == 2 ? 3 : 6;
+    // stages that the tensor cores sum: 36 additions, or 24
+    static constexpr int kGroup = kTerms == 2 ? 3 : 1;
+    static_assert(kCount >= 2 && kShared <= 232448 && kHigh % kN == 0, "shape of the tiles");
 };
 
+// The terms whose products are summed, from the least to the greatest: left, right.
+template <int kTerms>
+__device__ __forceinline__ constexpr int left_term(int t) {
+    constexpr int two[3] = {1, 0, 0}, three[6] = {2, 1, 0, 1, 0, 0};
+    return kTerms == 2 ? two[t % 3] : three[t];
+}
+template <int kTerms>
+__device__ __forceinline__ constexpr int right_term(int t) {
+    constexpr int two[3] = {0, 1, 0}, three[6] = {0, 1, 2, 0, 1, 0};
+    return kTerms == 2 ? two[t % 3] : three[t];
+}
+
 struct ProductArgs {
-    const __half* c;  // what is added, times beta: [n][2][rows][pitch]
+    const __half* c;  // what is added, times beta: [n][kTerms][rows][pitch], or NULL
     __half* out;      // the same shape, or NULL, and
     float* final;     // fp32: element (i, j) at i row_stride + j column_stride
     int64_t worker_stride, row_stride, column_stride;
-    float alpha, beta;
+    float alpha, beta, scale;  // scale: of `final`
     int32_t n, rows, columns, depth, pitch;
     int32_t tiles_m, tiles_n, tiles;
 };
 
 // The tile's place; kFlip: all tiles, otherwise those on and below the diagonal.
-template <int kN, bool kFlip>
+template <typename S, bool kFlip>
 struct Tile {
     int worker, row, column;
     bool mirror;
@@ -66,7 +83,7 @@ struct Tile {
             j = in / high;
             mirror = false;
         } else {
-            constexpr int kWide = 256 / kN;  // tiles across a diagonal block
+            constexpr int kWide = S::kHigh / S::kN;  // tiles across a diagonal block
             for (i = 0;; ++i) {
                 const int across = min(kWide * (i + 1), a.tiles_n);
                 if (at < across) break;
@@ -75,8 +92,8 @@ struct Tile {
             j = at;
             mirror = j < kWide * i;
         }
-        row = i * 2 * kM;
-        column = j * kN;
+        row = i * S::kHigh;
+        column = j * S::kN;
     }
 };
 
@@ -87,23 +104,28 @@ __device__ __forceinline__ uint64_t operand_k(uint32_t at) {
            uint64_t(2) << 61;
 }
 
-// fp16 x fp16 to fp32 for a pair of CTAs; kFlip: the right operand has N fastest.
-template <int kN, bool kFlip>
-constexpr uint32_t kKind = 1u << 4 | uint32_t(kFlip) << 16 | uint32_t(kN / 8) << 17 | uint32_t(2 * kM / 16) << 24;
+// fp16 x fp16 to fp32; kFlip: the right operand has N fastest.
+template <typename S, bool kFlip>
+constexpr uint32_t kKind = 1u << 4 | uint32_t(kFlip) << 16 | uint32_t(S::kN / 8) << 17 | uint32_t(S::kHigh / 16) << 24;
 
-__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
-    hi = __float2half_rn(v);
-    lo = __float2half_rn(v - __half2float(hi));
+// v as terms: each the rest of those before it, rounded to fp16.
+template <int kTerms>
+__device__ __forceinline__ void split(float v, __half (&term)[kTerms]) {
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) {
+        term[t] = __float2half_rn(v);
+        v -= __half2float(term[t]);
+    }
 }
 
-// out = alpha left right + beta c.  left [n][2][rows][depth]; right [n][2][columns][depth], or with kFlip
-// [n][2][depth][columns].  A wait that runs out ends a pair's work, and its results from there on are NaN.
-template <int kN, bool kFlip>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+// out = alpha (left right) + beta c.  left [n][kTerms][rows][depth]; right [n][kTerms][columns][depth], or with
+// kFlip [n][kTerms][depth][columns].  A wait that runs out ends a pair's work, and its results from there on are
+// NaN.
+template <typename S, bool kFlip>
+__global__ void __launch_bounds__(kThreads, 1)
 relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap left_map,
                            const __grid_constant__ CUtensorMap right_map) {
-    using S = Stages<kN>;
-    constexpr int kCount = S::kCount;
+    constexpr int kCtas = S::kCtas, kN = S::kN, kTerms = S::kTerms, kCount = S::kCount;
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t bars = stages + kCount * S::kBytes;
@@ -116,13 +138,13 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
     const uint32_t tensor_at = bars + 8 * (2 * kCount + 4);
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x / 32), 0), lane = threadIdx.x % 32;
-    const int rank = static_cast<int>(cluster_rank());
-    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int rank = kCtas == 2 ? static_cast<int>(cluster_rank()) : 0;
+    const int pair = blockIdx.x / kCtas, pairs = gridDim.x / kCtas;
     const int count = (a.depth + kDepth - 1) / kDepth;  // stages of a tile
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kCount; ++s) {
-            barrier_init(full(s), 1 + (rank == 0 ? 1 : 0));
+            barrier_init(full(s), kCtas == 2 && rank == 0 ? 2 : 1);
             barrier_init(freed(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -131,23 +153,45 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
         }
         barriers_ready();
     }
-    if (warp == kIssuer) tensor_alloc<2 * kN>(tensor_at);
+    if (warp == kIssuer) tensor_alloc<2 * kN, kCtas>(tensor_at);
     tensor_fence_before();
     __syncthreads();
-    cluster_sync();
+    if (kCtas == 2) cluster_sync();
     tensor_fence_after();
     uint32_t tensor;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
+    let_next_start();
+    wait_for_previous();
 
     if (warp < kAdders) {
         constexpr int kColumns = kN / 2;
         const int row = 32 * (warp % 4), column = kColumns * (warp / 4);  // of the CTA's 128 x kN
+        const int64_t plane = static_cast<int64_t>(a.rows) * a.pitch;
         bool ok = true;
         int group = 0;  // of all that the pair has summed
         for (int tile = pair; tile < a.tiles; tile += pairs) {
-            const Tile<kN, kFlip> at(a, tile);
-            float sum[kColumns] = {};
-            for (int done = 0; done < count && ok; done += kGroup, ++group) {
+            const Tile<S, kFlip> at(a, tile);
+            const int i = at.row + kM * rank + row + lane, j0 = at.column + column;
+            const int64_t base = static_cast<int64_t>(at.worker) * kTerms * plane + static_cast<int64_t>(i) * a.pitch + j0;
+            // beta c is where the sum starts, so that it comes while the tensor cores are at work
+            float sum[kColumns];
+            const float start = a.beta / a.alpha;
+#pragma unroll
+            for (int c = 0; c < kColumns; c += 8) {
+                uint4 part[kTerms];
+                const bool there = a.c != nullptr && i < a.rows && j0 + c < a.columns;
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t)
+                    part[t] = there ? *reinterpret_cast<const uint4*>(a.c + base + t * plane + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float v = 0.0f;
+#pragma unroll
+                    for (int t = kTerms - 1; t >= 0; --t) v += __half2float(reinterpret_cast<const __half*>(&part[t])[e]);
+                    sum[c + e] = start * v;
+                }
+            }
+            for (int done = 0; done < count && ok; done += S::kGroup, ++group) {
                 const int b = group & 1;
                 if (!(ok = barrier_wait_warp(summed(b), group >> 1 & 1))) break;
                 tensor_fence_after();
@@ -163,47 +207,36 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
                 __syncwarp();
                 if (lane == 0) barrier_arrive(read(b));
             }
-            const int i = at.row + kM * rank + row + lane;
-            const int64_t plane = static_cast<int64_t>(a.rows) * a.pitch;
-            const int64_t base = static_cast<int64_t>(at.worker) * 2 * plane;
 #pragma unroll
-            for (int c = 0; c < kColumns; c += 16) {
-                const int j = at.column + column + c;
+            for (int c = 0; c < kColumns; c += 8) {
+                const int j = j0 + c;
                 if (j >= a.columns || i >= a.rows) break;
-                float v[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = ok ? a.alpha * sum[c + e] : __int_as_float(0x7fffffff);
-                if (a.c != nullptr) {
-                    const uint4* from = reinterpret_cast<const uint4*>(a.c + base + static_cast<int64_t>(i) * a.pitch + j);
-                    const uint4* from_lo = reinterpret_cast<const uint4*>(a.c + base + plane + static_cast<int64_t>(i) * a.pitch + j);
-                    uint4 hi[2] = {from[0], from[1]}, lo[2] = {from_lo[0], from_lo[1]};
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        v[e] = fmaf(a.beta, __half2float(reinterpret_cast<const __half*>(hi)[e]) +
-                                                __half2float(reinterpret_cast<const __half*>(lo)[e]),
-                                    v[e]);
-                }
                 if (a.out != nullptr) {
-                    uint4 hi[2], lo[2];
+                    uint4 part[kTerms];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) split(v[e], reinterpret_cast<__half*>(hi)[e], reinterpret_cast<__half*>(lo)[e]);
-                    __half* to = a.out + base + static_cast<int64_t>(i) * a.pitch + j;
-                    reinterpret_cast<uint4*>(to)[0] = hi[0], reinterpret_cast<uint4*>(to)[1] = hi[1];
-                    reinterpret_cast<uint4*>(to + plane)[0] = lo[0], reinterpret_cast<uint4*>(to + plane)[1] = lo[1];
+                    for (int e = 0; e < 8; ++e) {
+                        __half term[kTerms];
+                        split(ok ? a.alpha * sum[c + e] : __int_as_float(0x7fffffff), term);
+#pragma unroll
+                        for (int t = 0; t < kTerms; ++t) reinterpret_cast<__half*>(&part[t])[e] = term[t];
+                    }
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(a.out + base + t * plane + c) = part[t];
                     if (!kFlip && at.mirror) {  // its place above the diagonal
+                        __half* over = a.out + static_cast<int64_t>(at.worker) * kTerms * plane + static_cast<int64_t>(j) * a.pitch + i;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
+                        for (int e = 0; e < 8; ++e) {
                             if (j + e >= a.columns) break;
-                            __half* over = a.out + base + static_cast<int64_t>(j + e) * a.pitch + i;
-                            over[0] = reinterpret_cast<const __half*>(hi)[e];
-                            over[plane] = reinterpret_cast<const __half*>(lo)[e];
+#pragma unroll
+                            for (int t = 0; t < kTerms; ++t)
+                                over[e * a.pitch + t * plane] = reinterpret_cast<const __half*>(&part[t])[e];
                         }
                     }
                 } else {
                     float* to = a.final + at.worker * a.worker_stride + i * a.row_stride + j * a.column_stride;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (j + e < a.columns) to[e * a.column_stride] = v[e];
+                    for (int e = 0; e < 8; ++e)
+                        if (j + e < a.columns) to[e * a.column_stride] = ok ? a.scale * sum[c + e] : __int_as_float(0x7fffffff);
                 }
             }
         }
@@ -212,28 +245,28 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
         bool ok = true;
         for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
             for (int n = 0; n < count; ++n, ++i) {
-                const int s = i % kCount, place = n % kGroup, b = group & 1;
+                const int s = i % kCount, place = n % S::kGroup, b = group & 1;
                 if (place == 0 && group > 1 && !(ok = barrier_wait_warp(read(b), (group >> 1 & 1) ^ 1))) break;
                 if (!(ok = barrier_wait_warp(full(s), i / kCount & 1))) break;
-                const bool last = place == kGroup - 1 || n == count - 1;
+                const bool last = place == S::kGroup - 1 || n == count - 1;
                 if (rank != 0) {
                     if (elected()) barrier_arrive_there(in_cta(full(s), 0));
                 } else {
                     tensor_fence_after();
                     if (elected()) {
-                        const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
+                        const uint32_t l = stages + s * S::kBytes, r = l + kTerms * S::kLeftTerm;
                         constexpr uint32_t kNext = kFlip ? 16 * 128 / 16 : 2;  // 16 of K, in 16 bytes
 #pragma unroll
                         for (int k = 0; k < kDepth / 16; ++k)
 #pragma unroll
-                            for (int t = 0; t < 3; ++t) {  // lo hi, hi lo, hi hi
-                                const uint32_t at_r = r + (t == 1 ? S::kRightTerm : 0);
-                                const uint64_t x = operand_k(l + (t == 0 ? S::kLeftTerm : 0)) + 2 * k;
+                            for (int t = 0; t < S::kProducts; ++t) {
+                                const uint32_t at_r = r + right_term<kTerms>(t) * S::kRightTerm;
+                                const uint64_t x = operand_k(l + left_term<kTerms>(t) * S::kLeftTerm) + 2 * k;
                                 const uint64_t y = (kFlip ? operand(at_r, kDepth * 128, 1024) : operand_k(at_r)) + kNext * k;
-                                product(tensor + b * kN, x, y, kKind<kN, kFlip>, place + k + t > 0);
+                                product<kCtas>(tensor + b * kN, x, y, kKind<S, kFlip>, place + k + t > 0);
                             }
-                        products_arrive(freed(s));
-                        if (last) products_arrive(summed(b));
+                        products_arrive<kCtas>(freed(s));
+                        if (last) products_arrive<kCtas>(summed(b));
                     }
                     __syncwarp();
                 }
@@ -244,23 +277,23 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
         int i = 0;
         bool ok = true;
         for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
-            const Tile<kN, kFlip> at(a, tile);
+            const Tile<S, kFlip> at(a, tile);
             for (int n = 0; n < count; ++n, ++i) {
                 const int s = i % kCount, k = n * kDepth;
                 if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
                 barrier_expect(full(s), S::kBytes);
-                const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
+                const uint32_t l = stages + s * S::kBytes, r = l + kTerms * S::kLeftTerm;
+                const int column = at.column + S::kRight * rank;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, 2 * at.worker + t, full(s));
-                    const int column = at.column + kN / 2 * rank;
+                for (int t = 0; t < kTerms; ++t) {
+                    copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, kTerms * at.worker + t, full(s));
                     if (!kFlip)
-                        copy_box(r + t * S::kRightTerm, &right_map, k, column, 2 * at.worker + t, full(s));
+                        copy_box(r + t * S::kRightTerm, &right_map, k, column, kTerms * at.worker + t, full(s));
                     else
 #pragma unroll
-                        for (int p = 0; p < kN / 2 / 64; ++p)
-                            copy_box(r + t * S::kRightTerm + p * kDepth * 128, &right_map, column + 64 * p, k, 2 * at.worker + t,
-                                     full(s));
+                        for (int p = 0; p < S::kRight / 64; ++p)
+                            copy_box(r + t * S::kRightTerm + p * kDepth * 128, &right_map, column + 64 * p, k,
+                                     kTerms * at.worker + t, full(s));
                 }
             }
         }
@@ -270,8 +303,8 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
     }
     __syncwarp();
     __syncthreads();
-    cluster_sync();  // the other CTA is done with this one's memory too
-    if (warp == kIssuer) tensor_free<2 * kN>(tensor);
+    if (kCtas == 2) cluster_sync();  // the other CTA is done with this one's memory too
+    if (warp == kIssuer) tensor_free<2 * kN, kCtas>(tensor);
 }
 
 // ------------------------------------------------------------------- the start
@@ -342,41 +375,48 @@ __device__ __forceinline__ float times(float v, double f) {
     return f < 1e38 ? v * static_cast<float>(f) : static_cast<float>(v * f);
 }
 
-// x = u f as two terms, [n][2][rows][pitch]: a warp takes strips of 256 columns.
+// x = u f as terms, [n][kTerms][rows][pitch]: a warp takes strips of 256 columns.
+template <int kTerms>
 __global__ void __launch_bounds__(256)
 relay_orthogonalise_start_kernel(Update u, const float* sums, int parts, float eps, __half* x, int pitch) {
     __shared__ double shared;
     __shared__ __align__(16) float turns[8][kStrip];
+    let_next_start();
+    wait_for_previous();
     const double f = start_factor(sums, parts, eps, &shared);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, strips = (u.columns + kStrip - 1) / kStrip;
     const float* from = u.p + blockIdx.y * u.worker_stride;
     const int64_t plane = static_cast<int64_t>(u.rows) * pitch, all = static_cast<int64_t>(u.rows) * strips;
-    __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
+    __half* to = x + static_cast<int64_t>(blockIdx.y) * kTerms * plane;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + warp; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
         const int64_t row = i / strips;
         const int base = static_cast<int>(i - row * strips) * kStrip;
-        float v[8], lo[8];
+        float v[8];
         load_strip<kDirect>(from + row * u.row_stride + base, lane, u.columns - base, v);
         to_octets(v, lane, turns[warp]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            v[k] = times(v[k], f);
-            lo[k] = v[k] - __half2float(__float2half_rn(v[k]));
+        for (int k = 0; k < 8; ++k) v[k] = times(v[k], f);
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) {
+            store_strip<kVector>(to + t * plane + row * pitch + base, lane, pitch - base, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
         }
-        store_strip<kVector>(to + row * pitch + base, lane, pitch - base, v);
-        store_strip<kVector>(to + plane + row * pitch + base, lane, pitch - base, lo);
     }
 }
 
-// The same of the transpose, x [n][2][columns][pitch]: a CTA takes squares of 64 x 64.
+// The same of the transpose, x [n][kTerms][columns][pitch]: a CTA takes squares of 64 x 64.
+template <int kTerms>
 __global__ void __launch_bounds__(256)
 relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float eps, __half* x, int pitch) {
     __shared__ double shared;
     __shared__ float square[64][65];
+    let_next_start();
+    wait_for_previous();
     const double f = start_factor(sums, parts, eps, &shared);
     const float* from = u.p + blockIdx.y * u.worker_stride;
     const int64_t plane = static_cast<int64_t>(u.columns) * pitch;
-    __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
+    __half* to = x + static_cast<int64_t>(blockIdx.y) * kTerms * plane;
     const int across = (u.columns + 63) / 64, all = (u.rows + 63) / 64 * across, lead = threadIdx.x / 64, at = threadIdx.x % 64;
     for (int i = blockIdx.x; i < all; i += gridDim.x) {
         const int row = i / across * 64, column = i % across * 64;
@@ -388,10 +428,10 @@ relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float ep
 #pragma unroll 4
         for (int c = lead; c < 64; c += 4) {
             if (column + c >= u.columns || row + at >= u.rows) continue;
-            __half hi, lo;
-            split(times(square[at][c], f), hi, lo);
-            to[static_cast<int64_t>(column + c) * pitch + row + at] = hi;
-            to[plane + static_cast<int64_t>(column + c) * pitch + row + at] = lo;
+            __half term[kTerms];
+            split(times(square[at][c], f), term);
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t) to[t * plane + static_cast<int64_t>(column + c) * pitch + row + at] = term[t];
         }
     }
 }
@@ -400,10 +440,10 @@ relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float ep
 
 int pitch_to(int64_t columns) { return static_cast<int>((columns + 15) / 16 * 16); }  // 32 bytes
 
-// Two terms of n matrices for boxes of 64 columns x `high` rows.
-bool map_terms(CUtensorMap* map, const __half* p, int64_t n, int64_t rows, int64_t columns, int high) {
+// `terms` terms of n matrices for boxes of 64 columns x `high` rows.
+bool map_terms(CUtensorMap* map, const __half* p, int64_t n, int terms, int64_t rows, int64_t columns, int high) {
     const cuuint64_t pitch = static_cast<cuuint64_t>(pitch_to(columns)) * 2;
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(columns), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(2 * n)};
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(columns), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(terms * n)};
     const cuuint64_t strides[2] = {pitch, pitch * static_cast<cuuint64_t>(rows)};
     const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(high), 1}, steps[3] = {1, 1, 1};
     return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(p), dims, strides, box, steps,
@@ -411,36 +451,71 @@ bool map_terms(CUtensorMap* map, const __half* p, int64_t n, int64_t rows, int64
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kN, bool kFlip>
+// Launches a kernel that starts before the one in front of it ends (wait_for_previous).
+template <typename... Args, typename... Given>
+int launch_early(void (*kernel)(Args...), dim3 grid, int threads, int shared, int cluster, cudaStream_t stream, Given... given) {
+    cudaLaunchAttribute with[2] = {};
+    with[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    with[0].val.programmaticStreamSerializationAllowed = 1;
+    with[1].id = cudaLaunchAttributeClusterDimension;
+    with[1].val.clusterDim.x = static_cast<unsigned>(cluster), with[1].val.clusterDim.y = 1, with[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t how = {};
+    how.gridDim = grid, how.blockDim = dim3(static_cast<unsigned>(threads)), how.dynamicSmemBytes = static_cast<size_t>(shared);
+    how.stream = stream, how.attrs = with, how.numAttrs = cluster > 1 ? 2 : 1;
+    if (cudaLaunchKernelEx(&how, kernel, Args(given)...) == cudaSuccess) return RELAY_OK;
+    (void)cudaGetLastError();
+    return RELAY_ECUDA;
+}
+
+// Tiles of all matrices; kFlip: the whole, otherwise on and below the diagonal.
+int64_t tile_count(int64_t n, int64_t rows, int64_t columns, int high, int wide, bool flip) {
+    const int64_t down = (rows + high - 1) / high, across = (columns + wide - 1) / wide;
+    if (flip) return n * down * across;
+    int64_t tiles = 0;
+    for (int64_t i = 0; i < down; ++i) tiles += high / wide * (i + 1) < across ? high / wide * (i + 1) : across;
+    return n * tiles;
+}
+
+template <typename S, bool kFlip>
 int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t stream) {
-    constexpr auto kernel = relay_orthogonalise_kernel<kN, kFlip>;
-    constexpr int kShared = Stages<kN>::kShared;
-    if (!allow_shared<kernel>(kShared)) return RELAY_ECUDA;
+    constexpr auto kernel = relay_orthogonalise_kernel<S, kFlip>;
+    if (!allow_shared<kernel>(S::kShared)) return RELAY_ECUDA;
     CUtensorMap left_map, right_map;
-    if (!map_terms(&left_map, left, a.n, a.rows, a.depth, kM) ||
-        !(kFlip ? map_terms(&right_map, right, a.n, a.depth, a.columns, kDepth)
-                : map_terms(&right_map, right, a.n, a.columns, a.depth, kN / 2)))
+    if (!map_terms(&left_map, left, a.n, S::kTerms, a.rows, a.depth, kM) ||
+        !(kFlip ? map_terms(&right_map, right, a.n, S::kTerms, a.depth, a.columns, kDepth)
+                : map_terms(&right_map, right, a.n, S::kTerms, a.columns, a.depth, S::kRight)))
         return RELAY_ECUDA;
-    a.tiles_m = (a.rows + 2 * kM - 1) / (2 * kM);
-    a.tiles_n = (a.columns + kN - 1) / kN;
-    int64_t tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
-    if (!kFlip) {
-        tiles = 0;
-        for (int i = 0; i < a.tiles_m; ++i) tiles += 256 / kN * (i + 1) < a.tiles_n ? 256 / kN * (i + 1) : a.tiles_n;
-    }
-    tiles *= a.n;
+    a.tiles_m = (a.rows + S::kHigh - 1) / S::kHigh;
+    a.tiles_n = (a.columns + S::kN - 1) / S::kN;
+    const int64_t tiles = tile_count(a.n, a.rows, a.columns, S::kHigh, S::kN, kFlip);
     if (tiles > INT32_MAX - kSms) return RELAY_EUNSUPPORTED;
     a.tiles = static_cast<int32_t>(tiles);
-    const int pairs = tiles < kSms / 2 ? static_cast<int>(tiles) : kSms / 2;
-    kernel<<<2 * pairs, kThreads, kShared, stream>>>(a, left_map, right_map);
-    return status_of_launch();
+    const int64_t most = kSms / S::kCtas, pairs = tiles < most ? tiles : most;
+    return launch_early(kernel, dim3(static_cast<unsigned>(S::kCtas * pairs)), kThreads, S::kShared, S::kCtas, stream, a, left_map,
+                        right_map);
+}
+
+// Three terms for small matrices: their sums are short, so that what two terms leave out is
+// what limits them, and the products are not what they wait for.
+int terms_of(int64_t m) { return m <= 512 ? 3 : 2; }
+
+// The shape that should take the least time.
+template <bool kFlip>
+int launch(int terms, const ProductArgs& a, const __half* left, const __half* right, cudaStream_t stream) {
+    if (terms == 3) return launch<Shape<1, 64, 3>, kFlip>(a, left, right, stream);
+    const int64_t stages = (a.depth + kDepth - 1) / kDepth, pairs = kSms / 2;
+    const int64_t wide = (tile_count(a.n, a.rows, a.columns, 256, 256, kFlip) + pairs - 1) / pairs;
+    const int64_t narrow = (tile_count(a.n, a.rows, a.columns, 256, 128, kFlip) + pairs - 1) / pairs;
+    if (wide * (0.85 * stages + 4.0) <= narrow * (0.5 * stages + 3.0))
+        return launch<Shape<2, 256, 2>, kFlip>(a, left, right, stream);
+    return launch<Shape<2, 128, 2>, kFlip>(a, left, right, stream);
 }
 
 // Where the workspace's parts begin, in bytes.
 struct Parts {
     int64_t x, g, p, sums, size;
     Parts(int64_t n, int64_t m, int64_t k) {
-        const int64_t wide = 4 * n * m * pitch_to(k), square = 4 * n * m * pitch_to(m);
+        const int64_t terms = terms_of(m), wide = 2 * terms * n * m * pitch_to(k), square = 2 * terms * n * m * pitch_to(m);
         x = 0, g = 2 * wide, p = g + square, sums = p + square, size = sums + 12 * n * kParts;
     }
 };
@@ -449,6 +524,16 @@ int check_matrices(int32_t n, int64_t rows, int64_t columns) {
     if (n < 1 || rows < 1 || columns < 1) return RELAY_EINVAL;
     if (n > RELAY_MAX_N || rows > RELAY_ORTHOGONALISE_MAX || columns > RELAY_ORTHOGONALISE_MAX) return RELAY_EUNSUPPORTED;
     return RELAY_OK;
+}
+
+template <int kTerms>
+int launch_start(const Update& u, bool tall, const float* sums, int parts, float eps, __half* x, int pitch, int32_t n,
+                 cudaStream_t stream) {
+    const int64_t ctas = tall ? ((u.rows + 63) / 64) * static_cast<int64_t>((u.columns + 63) / 64)
+                              : (u.rows * static_cast<int64_t>((u.columns + kStrip - 1) / kStrip) + 7) / 8;
+    const dim3 grid(static_cast<unsigned>(ctas < 1024 ? ctas : 1024), static_cast<unsigned>(n));
+    return launch_early(tall ? relay_orthogonalise_turn_kernel<kTerms> : relay_orthogonalise_start_kernel<kTerms>, grid, 256, 0, 1,
+                        stream, u, sums, parts, eps, x, pitch);
 }
 
 }  // namespace
@@ -477,6 +562,7 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
 
     const bool tall = rows > columns;
     const int64_t m = tall ? columns : rows, k = tall ? rows : columns;
+    const int terms = terms_of(m);
     const Parts parts(n, m, k);
     char* base = static_cast<char*>(workspace);
     __half* x[2] = {reinterpret_cast<__half*>(base), reinterpret_cast<__half*>(base + parts.g / 2)};
@@ -486,17 +572,11 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
                    static_cast<int32_t>(columns)};
     const int64_t warps = rows * ((columns + kStrip - 1) / kStrip), want = (warps + 31) / 32;
     const int cut = static_cast<int>(want < kParts ? want : kParts);
-    relay_orthogonalise_norm_kernel<<<dim3(cut, n), 256, 0, stream>>>(u, sums);
-    if (tall) {
-        const int64_t squares = (rows + 63) / 64 * ((columns + 63) / 64);
-        relay_orthogonalise_turn_kernel<<<dim3(static_cast<unsigned>(squares < 1024 ? squares : 1024), n), 256, 0, stream>>>(
-            u, sums, cut, eps, x[0], pitch_to(k));
-    } else {
-        const int64_t ctas = (warps + 7) / 8;
-        relay_orthogonalise_start_kernel<<<dim3(static_cast<unsigned>(ctas < 1024 ? ctas : 1024), n), 256, 0, stream>>>(
-            u, sums, cut, eps, x[0], pitch_to(k));
-    }
+    relay_orthogonalise_norm_kernel<<<dim3(static_cast<unsigned>(cut), static_cast<unsigned>(n)), 256, 0, stream>>>(u, sums);
     if (const int rc = status_of_launch()) return rc;
+    if (const int rc = terms == 3 ? launch_start<3>(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream)
+                                  : launch_start<2>(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream))
+        return rc;
 
     for (int step = 0; step < steps; ++step) {
         const __half* now = x[step & 1];
@@ -504,18 +584,18 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
         a.n = n, a.rows = static_cast<int32_t>(m);
         a.columns = static_cast<int32_t>(m), a.depth = static_cast<int32_t>(k), a.pitch = pitch_to(m);
         a.alpha = 1.0f / kHeld, a.out = g;
-        if (const int rc = launch<256, false>(a, now, now, stream)) return rc;
+        if (const int rc = launch<false>(terms, a, now, now, stream)) return rc;
         a.depth = static_cast<int32_t>(m);
         a.alpha = kC / kHeld, a.beta = kB, a.c = g, a.out = p;
-        if (const int rc = launch<256, false>(a, g, g, stream)) return rc;
+        if (const int rc = launch<false>(terms, a, g, g, stream)) return rc;
         a.columns = static_cast<int32_t>(k), a.pitch = pitch_to(k);
         a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1];
         if (step == steps - 1) {
-            a.alpha *= scale / kHeld, a.beta *= scale / kHeld;
+            a.scale = a.alpha * (scale / kHeld);
             a.out = nullptr, a.final = out, a.worker_stride = n > 1 ? out_worker_stride : 0;
             a.row_stride = tall ? 1 : out_row_stride, a.column_stride = tall ? out_row_stride : 1;
         }
-        if (const int rc = launch<256, true>(a, p, now, stream)) return rc;
+        if (const int rc = launch<true>(terms, a, p, now, stream)) return rc;
     }
     return RELAY_OK;
 }

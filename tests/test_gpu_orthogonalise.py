@@ -74,7 +74,7 @@ def _check(u, out=None, steps=5, scale=1.0):
     return out
 
 
-SHAPES = [(1, 1), (1, 9), (9, 1), (2, 3), (16, 16), (15, 64), (64, 65), (65, 64), (128, 128), (127, 300), (300, 129), (256, 256),
+SHAPES = [(512, 530), (513, 530), (1, 1), (1, 9), (9, 1), (2, 3), (16, 16), (15, 64), (64, 65), (65, 64), (128, 128), (127, 300), (300, 129), (256, 256),
           (257, 256), (256, 513), (511, 257), (640, 640), (200, 4001), (4001, 100), (1000, 777), (1025, 1300)]
 
 
@@ -100,6 +100,7 @@ def test_singular_values_come_near_one():
 def test_steps_and_scale(steps):
     _check(_matrices(steps, 2, 90, 140), steps=steps, scale=-0.25)
     _check(_matrices(steps, 2, 140, 90), steps=steps, scale=3.0)
+    _check(_matrices(steps, 2, 90, 90), steps=steps, scale=0.0)
 
 
 @pytest.mark.parametrize("rows,columns", [(70, 130), (130, 70), (33, 64), (257, 100)])
