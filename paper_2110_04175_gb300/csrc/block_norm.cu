@@ -23,14 +23,16 @@ struct Weight {  // fp32, from worker to worker
     }
 };
 
-// The lane's octet of a weight of any alignment.
-__device__ __forceinline__ void load_octet(const Weight& w, int worker, int base, int lane, int left, float (&v)[8]) {
-    const float* p = w.p + worker * w.stride + base;
+constexpr int kQuads = 128;  // features that a warp takes four a lane
+
+// Four features of a weight of any alignment, from feature `at` on.
+__device__ __forceinline__ void load_quad_of(const Weight& w, int worker, int at, bool on, Pair (&v)[2]) {
+    const float* p = w.p + worker * w.stride + at;
     if (w.quads) {
-        load_strip<kVector>(p, lane, left, v);
+        load_quad(p, on, v);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = 8 * lane + k < left ? p[8 * lane + k] : 0.0f;
+        for (int k = 0; k < 2; ++k) v[k] = on ? Pair(p[2 * k], p[2 * k + 1]) : Pair(0.0f);
     }
 }
 
@@ -126,6 +128,174 @@ relay_block_norm_kernel(BlockArgs<T> a) {
     }
 }
 
+// The 8-bit format of four features a lane, a block on eight lanes: layers.cuh's put_strip.
+__device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at, int lane, bool on, const Pair (&v)[2]) {
+    const float e[4] = {v[0].v.x, v[0].v.y, v[1].v.x, v[1].v.y};
+    uint32_t most = max(max(magnitude(e[0]), magnitude(e[1])), max(magnitude(e[2]), magnitude(e[3])));
+#pragma unroll
+    for (int m = 1; m < 8; m *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, m));
+    const uint32_t c = scale_byte(most);
+    if (!on) return;
+    const uint32_t ab = __byte_perm(code_bits(e[0], c), code_bits(e[1], c), 0x0040);
+    const uint32_t cd = __byte_perm(code_bits(e[2], c), code_bits(e[3], c), 0x0040);
+    *reinterpret_cast<uint32_t*>(codes + at) = c == 255u ? 0u : __byte_perm(ab, cd, 0x5410);
+    if (lane % 8 == 0) scales[at / kBlock] = static_cast<uint8_t>(c);
+}
+
+// Aligned rows of up to 8192 features in 16 bits and 4096 in 32, where there are some for
+// every group of kParts warps: they come by bulk copies to shared memory, two a group, the
+// next one on its way while this one's two sums are waited for; h stays in registers.
+template <typename T, int kParts, int kInputs>
+struct Ring {
+    static constexpr int kWarps = sizeof(T) == 2 ? 16 : 8, kGroups = kWarps / kParts, kStages = 2;
+    static constexpr int kWide = kParts * 4 * kQuads;  // features of a row at most
+    static constexpr int kRow = kWide * static_cast<int>(sizeof(T)), kStage = kInputs * kRow;  // bytes
+    static constexpr bool kWeights = kParts <= 8;  // there is room for the three weights too
+    static constexpr int kRows = kGroups * kStages * kStage, kShared = kRows + (kWeights ? 3 * 4 * kWide : 0) + 16;
+    static_assert(kShared <= 232448 - 2048, "shared memory of a CTA");
+};
+
+// The three weights, next to one another in shared memory: 0 past d, 1 where there are none.
+template <typename R>
+__device__ __forceinline__ void bring_weights(float* to, const Weight& post, const Weight& pre, const Weight& scale, int worker, int d) {
+    const Weight* from[3] = {&post, &pre, &scale};
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        for (int k = threadIdx.x; k < R::kWide; k += 32 * R::kWarps)
+            to[e * R::kWide + k] = k >= d ? 0.0f : from[e]->p == nullptr ? 1.0f : from[e]->p[worker * from[e]->stride + k];
+}
+
+// Weight number e at feature `at`, from there or, in the widest rows, from memory.
+template <typename R>
+__device__ __forceinline__ void weight_at(const float* weights, int e, const Weight& w, int worker, int at, bool on, Pair (&v)[2]) {
+    if constexpr (R::kWeights) {
+        load_quad(weights + e * R::kWide + at, true, v);
+    } else if (w.p != nullptr) {
+        load_quad_of(w, worker, at, on, v);
+    } else {
+        v[0] = v[1] = Pair(1.0f);
+    }
+}
+
+// Sums of kCount values over a group's warps, their lanes included.
+template <int kParts, int kCount>
+__device__ __forceinline__ void group_sum(float (&v)[kCount], float (&shared)[kParts][kCount], int group, int part, int lane) {
+#pragma unroll
+    for (int e = 0; e < kCount; ++e)
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) v[e] += __shfl_xor_sync(0xffffffffu, v[e], m);
+    if constexpr (kParts > 1) {
+#pragma unroll
+        for (int e = 0; e < kCount; ++e)
+            if (lane == e) shared[part][e] = v[e];
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kParts) : "memory");
+#pragma unroll
+        for (int e = 0; e < kCount; ++e) {
+            v[e] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kParts; ++w) v[e] += shared[w][e];
+        }
+    } else {
+        __syncwarp();
+    }
+}
+
+// A wait that runs out makes a group's results from there on NaN.
+template <typename T, int kParts>
+__global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_block_norm_rows_kernel(BlockArgs<T> a) {
+    using R = Ring<T, kParts, 3>;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[R::kGroups][R::kStages];
+    __shared__ float shared[2][R::kGroups][kParts][1];
+    uint8_t* ring = raw + (16 - shared_address(raw) % 16) % 16;
+    float* weights = reinterpret_cast<float*>(ring + R::kRows);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, group = warp / kParts, part = warp % kParts;
+    const int worker = blockIdx.y;
+    const bool gated = a.gate.p != nullptr;
+    if (threadIdx.x < R::kGroups * R::kStages) barrier_init(shared_address(&bars[0][0] + threadIdx.x), 1);
+    barriers_ready();
+    if (R::kWeights) bring_weights<R>(weights, a.post, a.pre, a.scale, worker, a.d);
+    __syncthreads();
+
+    const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
+    const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
+    const bool brings = part == 0 && elected();
+    uint8_t* mine = ring + group * (R::kStages * R::kStage);
+    const auto bring = [&](int token, int s) {  // one thread of the group
+        const uint32_t bar = shared_address(&bars[group][s]), to = shared_address(mine + s * R::kStage);
+        barrier_expect(bar, bytes * (2 + gated));
+        copy_row(to, a.x.row(worker, token), bytes, bar);
+        copy_row(to + R::kRow, a.residual.row(worker, token), bytes, bar);
+        if (gated) copy_row(to + 2 * R::kRow, a.gate.row(worker, token), bytes, bar);
+    };
+    if (brings) {
+        if (begin < a.tokens) bring(begin, 0);
+        if (begin + step < a.tokens) bring(begin + step, 1);
+    }
+    const float over_d = 1.0f / static_cast<float>(a.d);
+    bool ok = true;
+    int i = 0;
+    for (int token = begin; token < a.tokens; token += step, ++i) {
+        const int s = i % 2;
+        const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
+        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / 2 & 1);
+        const T* from = reinterpret_cast<const T*>(mine + s * R::kStage);
+        constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
+        Pair h[4][2], squares(0.0f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            load_quad(from + at, at < a.d, h[j]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) squares = fma(h[j][k], h[j][k], squares);
+        }
+        float sum[1] = {ok ? squares.sum() : __int_as_float(0x7fffffff)};
+        group_sum(sum, shared[0][group], group, part, lane);
+        const float sx = 1.0f / sqrtf(sum[0] * over_d + a.eps);
+        squares = Pair(0.0f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const bool on = at < a.d;
+            Pair w[2], rho[2], z[2], r[2];
+            load_quad(from + kNext + at, on, r);
+            if (gated) load_quad(from + 2 * kNext + at, on, z);
+            weight_at<R>(weights, 0, a.post, worker, at, on, w);
+            weight_at<R>(weights, 2, a.scale, worker, at, on, rho);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                h[j][k] = h[j][k] * Pair(sx) * w[k];
+                if (gated) h[j][k] = h[j][k] * Pair(Gate<T>(z[k].v.x).at, Gate<T>(z[k].v.y).at);
+                h[j][k] = fma(rho[k], r[k], h[j][k]);
+                squares = fma(h[j][k], h[j][k], squares);
+            }
+        }
+        sum[0] = squares.sum();
+        group_sum(sum, shared[1][group], group, part, lane);
+        // here every warp of the group is done with the row in shared memory
+        if (brings && token + 2 * step < a.tokens) bring(token + 2 * step, s);
+        const float sh = 1.0f / sqrtf(sum[0] * over_d + a.eps);
+        if (a.rstd != nullptr && part == 0 && lane == 0) {
+            a.rstd[row] = sx;
+            a.rstd[static_cast<int64_t>(gridDim.y) * a.tokens + row] = sh;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const bool on = at < a.d;
+            Pair w[2];
+            if (a.total.p != nullptr) store_quad(a.total.row(worker, token) + at, on, h[j]);
+            weight_at<R>(weights, 1, a.pre, worker, at, on, w);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) h[j][k] = h[j][k] * Pair(sh);
+            if (a.codes != nullptr) put_quad(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), at, lane, at < a.pitch, h[j]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) h[j][k] = h[j][k] * w[k];
+            store_quad(a.y.row(worker, token) + at, on, h[j]);
+        }
+    }
+}
+
 // ------------------------------------------------------------------ the backward pass
 //
 //   u = dy w_pre;  dh = s_h (u - hhat mean(u hhat)) + dtotal;  dr = rho dh;  drho = sum_t dh r
@@ -150,52 +320,61 @@ struct BlockBackwardArgs {
     int32_t tokens, d, pitch;
 };
 
-// What a lane makes again of 8 features of a row: `x`, `z`, `r` come as x, gate and residual
-// and leave as xhat, p and r; `w` and `rho` are w_post and rho (1 without).
-template <typename T>
-struct Octet {
-    float xhat[8], p[8], q[8], m[8], r[8], hhat[8];
-    __device__ __forceinline__ void make(const float (&w)[8], const float (&rho)[8], bool gated, float sx, float sh) {
+// What a lane makes again of 2 kPairs features of a row, two at a time: `xhat`, `p`, `r` come as x,
+// gate and residual; w and rho are w_post and rho (1 without).
+template <typename T, int kPairs>
+struct Features {
+    Pair xhat[kPairs], p[kPairs], q[kPairs], m[kPairs], r[kPairs], hhat[kPairs];
+    __device__ __forceinline__ void make(const Pair (&w)[kPairs], const Pair (&rho)[kPairs], bool gated, float sx, float sh) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            xhat[k] *= sx;
+        for (int k = 0; k < kPairs; ++k) {
+            xhat[k] = xhat[k] * Pair(sx);
             m[k] = xhat[k] * w[k];
             if (gated) {
-                const Gate<T> g(p[k]);
-                p[k] = g.at, q[k] = g.rest;
+                const Gate<T> a(p[k].v.x), b(p[k].v.y);
+                p[k] = Pair(a.at, b.at), q[k] = Pair(a.rest, b.rest);
             } else {
-                p[k] = 1.0f, q[k] = 0.0f;
+                p[k] = Pair(1.0f), q[k] = Pair(0.0f);
             }
-            hhat[k] = fmaf(rho[k], r[k], p[k] * m[k]) * sh;
+            hhat[k] = fma(rho[k], r[k], p[k] * m[k]) * Pair(sh);
         }
     }
     // Adds to the three sums and to dw_pre.
-    __device__ __forceinline__ void add(const float (&dy)[8], const float (&pre)[8], const float (&over)[8], float sh,
-                                        float (&sums)[3], float (&dpre)[8]) const {
+    __device__ __forceinline__ void add(const Pair (&dy)[kPairs], const Pair (&pre)[kPairs], const Pair (&over)[kPairs], float sh,
+                                        Pair (&sums)[3], Pair (&dpre)[kPairs]) const {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float u = dy[k] * pre[k], a = p[k] * m[k];
-            dpre[k] = fmaf(dy[k], hhat[k], dpre[k]);
-            sums[0] = fmaf(u, hhat[k], sums[0]);
-            sums[1] = fmaf(a, fmaf(sh, u, over[k]), sums[1]);
-            sums[2] = fmaf(a, hhat[k], sums[2]);
+        for (int k = 0; k < kPairs; ++k) {
+            const Pair u = dy[k] * pre[k], a = p[k] * m[k];
+            dpre[k] = fma(dy[k], hhat[k], dpre[k]);
+            sums[0] = fma(u, hhat[k], sums[0]);
+            sums[1] = fma(a, fma(Pair(sh), u, over[k]), sums[1]);
+            sums[2] = fma(a, hhat[k], sums[2]);
         }
     }
     // The three gradients of the rows (dy becomes dx), and what w_post and rho get of them.
-    __device__ __forceinline__ void leave(float (&dy)[8], const float (&pre)[8], const float (&over)[8], const float (&w)[8],
-                                          const float (&rho)[8], float sx, float sh, float along, float along_x, float (&dz)[8],
-                                          float (&dr)[8], float (&dpost)[8], float (&dscale)[8]) const {
+    __device__ __forceinline__ void leave(Pair (&dy)[kPairs], const Pair (&pre)[kPairs], const Pair (&over)[kPairs], const Pair (&w)[kPairs],
+                                          const Pair (&rho)[kPairs], float sx, float sh, float along, float along_x, Pair (&dz)[kPairs],
+                                          Pair (&dr)[kPairs], Pair (&dpost)[kPairs], Pair (&dscale)[kPairs]) const {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float d = fmaf(sh, fmaf(dy[k], pre[k], -hhat[k] * along), over[k]), dp = d * p[k];
+        for (int k = 0; k < kPairs; ++k) {
+            const Pair d = fma(Pair(sh), fma(hhat[k], Pair(-along), dy[k] * pre[k]), over[k]), dp = d * p[k];
             dr[k] = rho[k] * d;
             dz[k] = dp * m[k] * q[k];
-            dscale[k] = fmaf(d, r[k], dscale[k]);
-            dpost[k] = fmaf(dp, xhat[k], dpost[k]);
-            dy[k] = sx * fmaf(dp, w[k], -xhat[k] * along_x);
+            dscale[k] = fma(d, r[k], dscale[k]);
+            dpost[k] = fma(dp, xhat[k], dpost[k]);
+            dy[k] = Pair(sx) * fma(dp, w[k], xhat[k] * Pair(-along_x));
         }
     }
 };
+
+__device__ __forceinline__ void to_pairs(const float (&v)[8], Pair (&to)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[k] = Pair(v[2 * k], v[2 * k + 1]);
+}
+__device__ __forceinline__ void from_pairs(const Pair (&v)[4], float (&to)[8]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[2 * k] = v[k].v.x, to[2 * k + 1] = v[k].v.y;
+}
 
 // Any rows: kParts warps share one, kStrips strips each, with what they need of it in
 // registers.  CTA (p, i) takes tokens p, p + gridDim.x, ... (kRows at a time) of worker i and
@@ -212,7 +391,11 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
     const int length = a.lengths == nullptr ? a.tokens : min(max(a.lengths[worker], 0), a.tokens);
     const auto base_of = [&](int j) { return (part + kParts * j) * kStrip; };
 
-    float dpost[kStrips][8] = {}, dpre[kStrips][8] = {}, dscale[kStrips][8] = {};
+    Pair dpost[kStrips][4], dpre[kStrips][4], dscale[kStrips][4];
+#pragma unroll
+    for (int j = 0; j < kStrips; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) dpost[j][k] = dpre[j][k] = dscale[j][k] = Pair(0.0f);
     const int step = static_cast<int>(gridDim.x) * kRows;
     for (int first = static_cast<int>(blockIdx.x) * kRows; first < a.tokens; first += step) {
         const int token = first + slot;
@@ -229,54 +412,60 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
             dy[j].load(a.dy.row(worker, token) + base, lane, left);
             dtotal[j].load(a.dtotal.row(worker, token) + base, lane, a.dtotal.p != nullptr ? left : 0);
         }
-        const auto remake = [&](int j, Octet<T>& o, float (&w)[8], float (&rho)[8], float (&pre)[8], float (&u)[8], float (&over)[8]) {
+        const auto remake = [&](int j, Features<T, 4>& o, Pair (&w)[4], Pair (&rho)[4], Pair (&pre)[4], Pair (&u)[4], Pair (&over)[4]) {
             const int base = base_of(j), left = counts ? a.d - base : 0;
-            x[j].get(o.xhat);
-            r[j].get(o.r);
-            dy[j].get(u);
-            dtotal[j].get(over);
-            if (a.gate.p != nullptr) z[j].get(o.p);
-            a.post.template load<kWay>(worker, base, lane, left, w, turn);
-            a.pre.template load<kWay>(worker, base, lane, left, pre, turn);
+            float v[8];
+            x[j].get(v), to_pairs(v, o.xhat);
+            r[j].get(v), to_pairs(v, o.r);
+            dy[j].get(v), to_pairs(v, u);
+            dtotal[j].get(v), to_pairs(v, over);
+            if (a.gate.p != nullptr) z[j].get(v), to_pairs(v, o.p);
+            a.post.template load<kWay>(worker, base, lane, left, v, turn), to_pairs(v, w);
+            a.pre.template load<kWay>(worker, base, lane, left, v, turn), to_pairs(v, pre);
             if (a.scale.p != nullptr) {
-                a.scale.template load<kWay>(worker, base, lane, left, rho, turn);
+                a.scale.template load<kWay>(worker, base, lane, left, v, turn), to_pairs(v, rho);
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) rho[k] = 1.0f;
+                for (int k = 0; k < 4; ++k) rho[k] = Pair(1.0f);
             }
             o.make(w, rho, a.gate.p != nullptr, sx, sh);
         };
-        float three[3] = {};
+        Pair parts[3] = {Pair(0.0f), Pair(0.0f), Pair(0.0f)};
+        float three[3];
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
-            Octet<T> o;
-            float w[8], rho[8], pre[8], u[8], over[8];
+            Features<T, 4> o;
+            Pair w[4], rho[4], pre[4], u[4], over[4];
             remake(j, o, w, rho, pre, u, over);
-            o.add(u, pre, over, sh, three, dpre[j]);
+            o.add(u, pre, over, sh, parts, dpre[j]);
         }
 #pragma unroll
-        for (int e = 0; e < 3; ++e) three[e] = row_sum<kParts>(three[e], shared[e], slot, part) / static_cast<float>(a.d);
+        for (int e = 0; e < 3; ++e) three[e] = row_sum<kParts>(parts[e].sum(), shared[e], slot, part) / static_cast<float>(a.d);
         if (token >= a.tokens) continue;
         const float along = three[0], along_x = three[1] - sh * along * three[2];
 #pragma unroll
         for (int j = 0; j < kStrips; ++j) {
             const int base = base_of(j), left = a.d - base;
             if (left <= 0) break;
-            Octet<T> o;
-            float w[8], rho[8], pre[8], u[8], over[8], dz[8], dr[8];
+            Features<T, 4> o;
+            Pair w[4], rho[4], pre[4], u[4], over[4], dz[4], dr[4];
             if (counts) {
                 remake(j, o, w, rho, pre, u, over);
                 o.leave(u, pre, over, w, rho, sx, sh, along, along_x, dz, dr, dpost[j], dscale[j]);
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) u[k] = dz[k] = dr[k] = 0.0f;
+                for (int k = 0; k < 4; ++k) u[k] = dz[k] = dr[k] = Pair(0.0f);
             }
-            store_strip<kWay>(a.dx.row(worker, token) + base, lane, left, u);
-            store_strip<kWay>(a.dresidual.row(worker, token) + base, lane, left, dr);
-            if (a.dgate.p != nullptr) store_strip<kWay>(a.dgate.row(worker, token) + base, lane, left, dz);
+            float v[8];
+            from_pairs(u, v), store_strip<kWay>(a.dx.row(worker, token) + base, lane, left, v);
+            from_pairs(dr, v), store_strip<kWay>(a.dresidual.row(worker, token) + base, lane, left, v);
+            if (a.dgate.p != nullptr) from_pairs(dz, v), store_strip<kWay>(a.dgate.row(worker, token) + base, lane, left, v);
         }
     }
-    const auto leave = [&](float (&v)[kStrips][8], int which) {
+    const auto leave = [&](Pair (&pairs)[kStrips][4], int which) {
+        float v[kStrips][8];
+#pragma unroll
+        for (int j = 0; j < kStrips; ++j) from_pairs(pairs[j], v[j]);
         if (kRows > 1) {  // the rows that went side by side, in their order
             __syncthreads();
             if (slot > 0) {
@@ -302,25 +491,12 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
     if (a.scale.p != nullptr) leave(dscale, 2);
 }
 
-// Aligned rows of up to 8192 features in 16 bits and 4096 in 32: rows come by bulk copies to
-// shared memory, two a group of kParts warps, so that the next one is on its way while this
-// one's two sweeps read it there, and registers are left for two strips' sums over the
-// tokens.  The groups of a CTA take rows of their own and wait only for themselves.
-template <typename T, int kParts>
-struct Ring {
-    static constexpr int kWarps = sizeof(T) == 2 ? 16 : 8, kGroups = kWarps / kParts, kStages = 2;
-    static constexpr int kRow = kParts * 2 * kStrip * static_cast<int>(sizeof(T));  // bytes kept free for a row
-    static constexpr int kStage = 5 * kRow;
-    static constexpr bool kWeights = kParts <= 8;  // there is room for the three weights too
-    static constexpr int kWide = kParts * 2 * kStrip;
-    static constexpr int kRows = kGroups * kStages * kStage, kShared = kRows + (kWeights ? 3 * 4 * kWide : 0) + 16;
-    static_assert(kShared <= 232448 - 2048, "shared memory of a CTA");
-};
-
+// The rows that the forward pass's kernel of bulk copies takes, here with two sweeps over a
+// row in shared memory, so that registers are left for the sums over the tokens.  The groups of a CTA take rows of their own and wait only for themselves.
 // A wait that runs out makes a group's results from there on NaN.
 template <typename T, int kParts>
-__global__ void __launch_bounds__(32 * Ring<T, kParts>::kWarps, 1) relay_block_norm_backward_rows_kernel(BlockBackwardArgs<T> a) {
-    using R = Ring<T, kParts>;
+__global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_block_norm_backward_rows_kernel(BlockBackwardArgs<T> a) {
+    using R = Ring<T, kParts, 5>;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[R::kGroups][R::kStages];
     __shared__ float shared[2][R::kGroups][kParts][3];
@@ -332,13 +508,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts>::kWarps, 1) relay_block_n
     const bool gated = a.gate.p != nullptr, over_too = a.dtotal.p != nullptr, scaled = a.scale.p != nullptr;
     if (threadIdx.x < R::kGroups * R::kStages) barrier_init(shared_address(&bars[0][0] + threadIdx.x), 1);
     barriers_ready();
-    if (R::kWeights) {
-        const Weight* from[3] = {&a.post, &a.pre, &a.scale};
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            for (int k = threadIdx.x; k < R::kWide; k += 32 * R::kWarps)
-                weights[e * R::kWide + k] = k >= a.d ? 0.0f : from[e]->p == nullptr ? 1.0f : from[e]->p[worker * from[e]->stride + k];
-    }
+    if (R::kWeights) bring_weights<R>(weights, a.post, a.pre, a.scale, worker, a.d);
     __syncthreads();
 
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
@@ -358,117 +528,103 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts>::kWarps, 1) relay_block_n
         if (begin < length) bring(begin, 0);
         if (begin + step < length) bring(begin + step, 1);
     }
-    float dpost[2][8] = {}, dpre[2][8] = {}, dscale[2][8] = {};
+    Pair dpost[4][2], dpre[4][2], dscale[4][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) dpost[j][k] = dpre[j][k] = dscale[j][k] = Pair(0.0f);
+    const float* factors = a.rstd + static_cast<int64_t>(worker) * a.tokens;
+    const int64_t second = static_cast<int64_t>(n) * a.tokens;
+    float next_x = begin < length ? factors[begin] : 0.0f, next_h = begin < length ? factors[second + begin] : 0.0f;
+    const float over_d = 1.0f / static_cast<float>(a.d);
     bool ok = true;
     int i = 0;
     for (int token = begin; token < length; token += step, ++i) {
         const int s = i % 2;
-        const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
-        float sx = a.rstd[row];
-        const float sh = a.rstd[static_cast<int64_t>(n) * a.tokens + row];
+        const float sx = next_x, sh = next_h;
+        if (token + step < length) next_x = factors[token + step], next_h = factors[second + token + step];
         ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / 2 & 1);
-        if (!ok) sx = __int_as_float(0x7fffffff);
-        const auto remake = [&](int j, Octet<T>& o, float (&w)[8], float (&rho)[8], float (&pre)[8], float (&u)[8], float (&over)[8]) {
-            const int at = (part + kParts * j) * kStrip, left = a.d - at;
+        const auto remake = [&](int j, Features<T, 2>& o, Pair (&w)[2], Pair (&rho)[2], Pair (&pre)[2], Pair (&u)[2], Pair (&over)[2]) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const bool on = at < a.d;
             const T* from = reinterpret_cast<const T*>(mine + s * R::kStage) + at;
             constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
-            load_strip<kVector>(from, lane, left, o.xhat);
-            load_strip<kVector>(from + kNext, lane, left, o.r);
-            load_strip<kVector>(from + 2 * kNext, lane, left, u);
-            if (gated) load_strip<kVector>(from + 3 * kNext, lane, left, o.p);
-            load_strip<kVector>(from + 4 * kNext, lane, over_too ? left : 0, over);
-            if constexpr (R::kWeights) {
-                load_strip<kVector>(weights + at, lane, left, w);
-                load_strip<kVector>(weights + R::kWide + at, lane, left, pre);
-                load_strip<kVector>(weights + 2 * R::kWide + at, lane, left, rho);
-            } else {
-                load_octet(a.post, worker, at, lane, left, w);
-                load_octet(a.pre, worker, at, lane, left, pre);
-                if (scaled) load_octet(a.scale, worker, at, lane, left, rho);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (!scaled) rho[k] = 1.0f;
-            }
+            load_quad(from, on, o.xhat);
+            load_quad(from + kNext, on, o.r);
+            load_quad(from + 2 * kNext, on, u);
+            if (gated) load_quad(from + 3 * kNext, on, o.p);
+            load_quad(from + 4 * kNext, on && over_too, over);
+            weight_at<R>(weights, 0, a.post, worker, at, on, w);
+            weight_at<R>(weights, 1, a.pre, worker, at, on, pre);
+            weight_at<R>(weights, 2, a.scale, worker, at, on, rho);
             o.make(w, rho, gated, sx, sh);
         };
-        float three[3] = {};
+        Pair parts[3] = {Pair(0.0f), Pair(0.0f), Pair(0.0f)};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            Octet<T> o;
-            float w[8], rho[8], pre[8], u[8], over[8];
+        for (int j = 0; j < 4; ++j) {
+            Features<T, 2> o;
+            Pair w[2], rho[2], pre[2], u[2], over[2];
             remake(j, o, w, rho, pre, u, over);
-            o.add(u, pre, over, sh, three, dpre[j]);
+            o.add(u, pre, over, sh, parts, dpre[j]);
         }
+        float three[3];
 #pragma unroll
-        for (int e = 0; e < 3; ++e)
-#pragma unroll
-            for (int m = 16; m > 0; m >>= 1) three[e] += __shfl_xor_sync(0xffffffffu, three[e], m);
-        if constexpr (kParts > 1) {
-            float(&sums)[kParts][3] = shared[i & 1][group];
-            if (lane < 3) sums[part][lane] = lane == 0 ? three[0] : lane == 1 ? three[1] : three[2];
-            asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(32 * kParts) : "memory");
-#pragma unroll
-            for (int e = 0; e < 3; ++e) {
-                three[e] = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kParts; ++w) three[e] += sums[w][e];
-            }
-        } else {
-            __syncwarp();
-        }
+        for (int e = 0; e < 3; ++e) three[e] = ok ? parts[e].sum() : __int_as_float(0x7fffffff);
+        group_sum(three, shared[i & 1][group], group, part, lane);
         // here every warp of the group is done with the row before this one
         if (brings && i > 0 && token + step < length) bring(token + step, s ^ 1);
-        const float over_d = 1.0f / static_cast<float>(a.d), along = three[0] * over_d;
-        const float along_x = three[1] * over_d - sh * along * (three[2] * over_d);
+        const float along = three[0] * over_d, along_x = three[1] * over_d - sh * along * (three[2] * over_d);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int at = (part + kParts * j) * kStrip, left = a.d - at;
-            Octet<T> o;
-            float w[8], rho[8], pre[8], u[8], over[8], dz[8], dr[8];
+        for (int j = 0; j < 4; ++j) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const bool on = at < a.d;
+            Features<T, 2> o;
+            Pair w[2], rho[2], pre[2], u[2], over[2], dz[2], dr[2];
             remake(j, o, w, rho, pre, u, over);
             o.leave(u, pre, over, w, rho, sx, sh, along, along_x, dz, dr, dpost[j], dscale[j]);
-            store_strip<kVector>(a.dx.row(worker, token) + at, lane, left, u);
-            store_strip<kVector>(a.dresidual.row(worker, token) + at, lane, left, dr);
-            if (gated) store_strip<kVector>(a.dgate.row(worker, token) + at, lane, left, dz);
+            store_quad(a.dx.row(worker, token) + at, on, u);
+            store_quad(a.dresidual.row(worker, token) + at, on, dr);
+            if (gated) store_quad(a.dgate.row(worker, token) + at, on, dz);
         }
     }
     // padding
     for (int token = begin + i * step; token < a.tokens; token += step) {
-        const float none[8] = {};
+        const Pair none[2] = {Pair(0.0f), Pair(0.0f)};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int at = (part + kParts * j) * kStrip, left = a.d - at;
-            store_strip<kVector>(a.dx.row(worker, token) + at, lane, left, none);
-            store_strip<kVector>(a.dresidual.row(worker, token) + at, lane, left, none);
-            if (gated) store_strip<kVector>(a.dgate.row(worker, token) + at, lane, left, none);
+        for (int j = 0; j < 4; ++j) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const bool on = at < a.d;
+            store_quad(a.dx.row(worker, token) + at, on, none);
+            store_quad(a.dresidual.row(worker, token) + at, on, none);
+            if (gated) store_quad(a.dgate.row(worker, token) + at, on, none);
         }
     }
     // the groups' sums in their order, through the ring's memory: [kGroups - 1][kWide]
     float* others = reinterpret_cast<float*>(ring);
-    const auto leave = [&](float (&v)[2][8], int which) {
+    const auto leave = [&](Pair (&v)[4][2], int which) {
         if (R::kGroups > 1) {
             __syncthreads();
             if (group > 0) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    store_strip<kVector>(others + (group - 1) * R::kWide + (part + kParts * j) * kStrip, lane, kStrip, v[j]);
+                for (int j = 0; j < 4; ++j)
+                    store_quad(others + (group - 1) * R::kWide + (part + kParts * j) * kQuads + 4 * lane, true, v[j]);
             }
             __syncthreads();
             if (group > 0) return;
             for (int g = 0; g < R::kGroups - 1; ++g)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float add[8];
-                    load_strip<kVector>(others + g * R::kWide + (part + kParts * j) * kStrip, lane, kStrip, add);
+                for (int j = 0; j < 4; ++j) {
+                    Pair add[2];
+                    load_quad(others + g * R::kWide + (part + kParts * j) * kQuads + 4 * lane, true, add);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[j][k] += add[k];
+                    for (int k = 0; k < 2; ++k) v[j][k] = fma(add[k], Pair(1.0f), v[j][k]);
                 }
         }
         float* out = a.partial + ((static_cast<int64_t>(which) * n + worker) * gridDim.x + blockIdx.x) * a.pitch;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int at = (part + kParts * j) * kStrip;
-            store_strip<kVector>(out + at, lane, a.pitch - at, v[j]);
+        for (int j = 0; j < 4; ++j) {
+            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            store_quad(out + at, at < a.pitch, v[j]);
         }
     };
     leave(dpost, 0);
@@ -528,7 +684,7 @@ int64_t block_partials(int32_t n, int64_t tokens, int64_t d) {
 // The same for the kernel of the aligned rows, one CTA per SM; never more than the above.
 template <typename T, int kParts>
 int64_t ring_partials(int32_t n, int64_t tokens, int64_t d) {
-    const int64_t side = Ring<T, kParts>::kGroups, fill = 152 > n ? 152 / n : 1, chain = fill * side * 256;
+    const int64_t side = Ring<T, kParts, 5>::kGroups, fill = 152 > n ? 152 / n : 1, chain = fill * side * 256;
     const int64_t want = tokens > chain ? fill * ((tokens + chain - 1) / chain) : fill, most = (tokens + side - 1) / side;
     const int64_t parts = most < want ? (most > 0 ? most : 1) : want, room = block_partials(n, tokens, d);
     return parts < room ? parts : room;
@@ -537,12 +693,20 @@ int64_t ring_partials(int32_t n, int64_t tokens, int64_t d) {
 template <typename T, int kParts>
 int launch_rows(const BlockBackwardArgs<T>& a, int64_t parts, int32_t n, cudaStream_t stream) {
     constexpr auto kernel = relay_block_norm_backward_rows_kernel<T, kParts>;
-    if (!allow_shared<kernel>(Ring<T, kParts>::kShared)) return RELAY_ECUDA;
-    kernel<<<dim3(static_cast<unsigned>(parts), n), 32 * Ring<T, kParts>::kWarps, Ring<T, kParts>::kShared, stream>>>(a);
+    if (!allow_shared<kernel>(Ring<T, kParts, 5>::kShared)) return RELAY_ECUDA;
+    kernel<<<dim3(static_cast<unsigned>(parts), n), 32 * Ring<T, kParts, 5>::kWarps, Ring<T, kParts, 5>::kShared, stream>>>(a);
     return status_of_launch();
 }
 
-// f(kParts) for the least that holds a row in two strips a warp.
+// Whether rows go through shared memory: as wide as a CTA's warps hold, and at least four of
+// them for each group of warps, whose start costs as much as two (the weights, the barriers).
+bool takes_ring(int32_t type, int32_t n, int64_t tokens, int64_t d) {
+    const int64_t pitch = pitch_of(d), warps = type == RELAY_FP32 ? 8 : 16;
+    const int64_t side = pitch <= 512 ? warps : pitch <= 1024 ? warps / 2 : pitch <= 2048 ? warps / 4 : pitch <= 4096 ? warps / 8 : 1;
+    return d <= 512 * warps && tokens >= 4 * side * (152 > n ? 152 / n : 1);
+}
+
+// f(kParts) for the least that holds a row in four quads a lane.
 template <typename F>
 int by_ring(int64_t pitch, F f) {
     if (pitch <= 512) return f(std::integral_constant<int, 1>());
@@ -589,12 +753,26 @@ int relay_block_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
         return RELAY_EINVAL;
     const bool vec = d % 8 == 0 && vectors(x, type, n, tokens) && vectors(gate, type, n, tokens) &&
                      vectors(residual, type, n, tokens) && vectors(total, type, n, tokens) && vectors(y, type, n, tokens);
+    const bool ring = vec && takes_ring(type, n, tokens, d);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         const BlockArgs<T> a{view<const T>(x, n, tokens), view<const T>(gate, n, tokens), view<const T>(residual, n, tokens),
                              view<T>(total, n, tokens), view<T>(y, n, tokens), weight_of(post, post_stride, n, d),
                              weight_of(pre, pre_stride, n, d), weight_of(scale, scale_stride, n, d), eps, rstd, codes, scales,
                              static_cast<int32_t>(tokens), static_cast<int32_t>(d), static_cast<int32_t>(pitch_of(d))};
+        if (ring)
+            return by_ring(a.pitch, [&](auto with) {
+                constexpr int kParts = decltype(with)::value;
+                if constexpr (kParts <= Ring<T, 1, 3>::kWarps) {
+                    using R = Ring<T, kParts, 3>;
+                    constexpr auto kernel = relay_block_norm_rows_kernel<T, kParts>;
+                    if (!allow_shared<kernel>(R::kShared)) return RELAY_ECUDA;
+                    kernel<<<dim3(static_cast<unsigned>(152 > n ? 152 / n : 1), static_cast<unsigned>(n)), 32 * R::kWarps, R::kShared,
+                             stream>>>(a);
+                    return status_of_launch();
+                }
+                return RELAY_EUNSUPPORTED;  // (not reached: `ring`)
+            });
         return by_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr int kRows = kNormWarps<kParts> / kParts;
@@ -650,7 +828,7 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     bool vec = d % 8 == 0;
     for (const relay_rows* r : {dy, dtotal, x, gate, residual, dx, dgate, dresidual}) vec = vec && vectors(r, type, n, tokens);
     int parts = static_cast<int>(block_partials(n, tokens, d));
-    const bool ring = vec && tokens > 0 && d <= (type == RELAY_FP32 ? 4096 : 8192);
+    const bool ring = vec && takes_ring(type, n, tokens, d);
     const int rc = by_type(type, [&](auto t) {
         using T = decltype(t);
         const BlockBackwardArgs<T> a{
@@ -663,7 +841,7 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
         if (ring)
             return by_ring(a.pitch, [&](auto with) {
                 constexpr int kParts = decltype(with)::value;
-                if constexpr (kParts <= Ring<T, 1>::kWarps) {
+                if constexpr (kParts <= Ring<T, 1, 5>::kWarps) {
                     parts = static_cast<int>(ring_partials<T, kParts>(n, tokens, d));
                     return launch_rows<T, kParts>(a, parts, n, stream);
                 }

@@ -274,27 +274,91 @@ struct CodePiece {
 
 // -------------------------------------------------------------------- a gate
 
-// sigma(g) and 1 - sigma(g), both to their own size and from the same exp(-|g|) <= 1, so
-// that they add up to 1 within a rounding.  The gates of 16-bit rows take the hardware's
-// exponential and reciprocal: off by less than (3 + |g|) 2^-23 relative, as if the gate
-// were (3 + |g|) 2^-23 further; below |g| = 87.3 the smaller one is 0.
+// sigma(g) and 1 - sigma(g), both to their own size and from the same exponential, so that
+// they add up to 1 within a rounding.  The gates of 16-bit rows take the hardware's
+// exponential and reciprocal, e = exp(-g) held at 2^126 (NaN stays): off by less than
+// (3 + |g|) 2^-23 relative, as if the gate were (3 + |g|) 2^-23 further; below g = -87.3
+// sigma(g) stays at 2^-126, above 87.3 the rest is 0.
 template <typename T>
 struct Gate {
     float at, rest;
     __device__ __forceinline__ explicit Gate(float g) {
-        float e, r;
         if constexpr (sizeof(T) == 2) {
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(g) * -1.44269504f));
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+            float e;
+            asm("min.NaN.f32 %0, %1, 0f42fc0000;" : "=f"(e) : "f"(g * -1.44269504f));  // 126
+            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(at) : "f"(1.0f + e));
+            rest = e * at;
         } else {
-            e = expf(-fabsf(g));
-            r = 1.0f / (1.0f + e);
+            const float e = expf(-fabsf(g)), r = 1.0f / (1.0f + e), s = e * r;
+            at = g < 0.0f ? s : r;
+            rest = g < 0.0f ? r : s;
         }
-        const float s = e * r;
-        at = g < 0.0f ? s : r;
-        rest = g < 0.0f ? r : s;
     }
 };
+
+// ------------------------------------------------------- two fp32 numbers at a time
+
+// What sm_103a adds, multiplies and fuses in one instruction.
+struct Pair {
+    float2 v;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float a, float b) : v(make_float2(a, b)) {}
+    __device__ __forceinline__ explicit Pair(float both) : v(make_float2(both, both)) {}
+    __device__ __forceinline__ unsigned long long bits() const {
+        unsigned long long w;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(v.x), "f"(v.y));
+        return w;
+    }
+    __device__ __forceinline__ static Pair of(unsigned long long w) {
+        Pair p;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(p.v.x), "=f"(p.v.y) : "l"(w));
+        return p;
+    }
+    __device__ __forceinline__ float sum() const { return v.x + v.y; }
+};
+
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a.bits()), "l"(b.bits()));
+    return Pair::of(d);
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a.bits()), "l"(b.bits()), "l"(c.bits()));
+    return Pair::of(d);
+}
+
+// A lane's 4 features as pairs, from and to memory aligned to them (`on`: there are any).
+template <typename T>
+__device__ __forceinline__ void load_quad(const T* p, bool on, Pair (&v)[2]) {
+    if constexpr (sizeof(T) == 4) {
+        const float4 w = on ? *reinterpret_cast<const float4*>(p) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        v[0] = Pair(w.x, w.y), v[1] = Pair(w.z, w.w);
+    } else {
+        const uint2 w = on ? *reinterpret_cast<const uint2*>(p) : make_uint2(0, 0);
+        const T* e = reinterpret_cast<const T*>(&w);
+        v[0] = Pair(widen(e[0]), widen(e[1])), v[1] = Pair(widen(e[2]), widen(e[3]));
+    }
+}
+
+__device__ __forceinline__ uint32_t narrow_two(Pair v, __nv_bfloat16) {
+    const __nv_bfloat162 w = __floats2bfloat162_rn(v.v.x, v.v.y);
+    return *reinterpret_cast<const uint32_t*>(&w);
+}
+__device__ __forceinline__ uint32_t narrow_two(Pair v, __half) {
+    const __half2 w = __floats2half2_rn(v.v.x, v.v.y);
+    return *reinterpret_cast<const uint32_t*>(&w);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_quad(T* p, bool on, const Pair (&v)[2]) {
+    if (!on) return;
+    if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float4*>(p) = make_float4(v[0].v.x, v[0].v.y, v[1].v.x, v[1].v.y);
+    else
+        *reinterpret_cast<uint2*>(p) = make_uint2(narrow_two(v[0], T()), narrow_two(v[1], T()));
+}
 
 // --------------------------------------------------------------- rows of a norm
 

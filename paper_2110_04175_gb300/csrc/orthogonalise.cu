@@ -495,15 +495,23 @@ int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t 
                         right_map);
 }
 
-// Three terms for small matrices: their sums are short, so that what two terms leave out is
-// what limits them, and the products are not what they wait for.
-int terms_of(int64_t m) { return m <= 512 ? 3 : 2; }
+// Three terms where m is small: sums are short there, so that what two terms leave out is what
+// limits them.  Errors against 64 bits, with two terms, three and in plain fp32, in 1e-6:
+// [128][256] 3.4, 1.8, 1.6; [300][2000] 4.9, 1.9, 2.4; [360][5000] 4.8, -, 2.6; [512][4096]
+// 1.7, 0.9, 2.7; [1001][1537] 2.1, -, 3.2.
+int terms_of(int64_t m) { return m <= 448 ? 3 : 2; }
 
 // The shape that should take the least time.
 template <bool kFlip>
 int launch(int terms, const ProductArgs& a, const __half* left, const __half* right, cudaStream_t stream) {
-    if (terms == 3) return launch<Shape<1, 64, 3>, kFlip>(a, left, right, stream);
     const int64_t stages = (a.depth + kDepth - 1) / kDepth, pairs = kSms / 2;
+    if (terms == 3) {
+        const int64_t alone = (tile_count(a.n, a.rows, a.columns, 128, 64, kFlip) + kSms - 1) / kSms;
+        const int64_t paired = (tile_count(a.n, a.rows, a.columns, 256, 128, kFlip) + pairs - 1) / pairs;
+        if (alone * (0.6 * stages + 3.0) <= paired * (1.0 * stages + 3.0))
+            return launch<Shape<1, 64, 3>, kFlip>(a, left, right, stream);
+        return launch<Shape<2, 128, 3>, kFlip>(a, left, right, stream);
+    }
     const int64_t wide = (tile_count(a.n, a.rows, a.columns, 256, 256, kFlip) + pairs - 1) / pairs;
     const int64_t narrow = (tile_count(a.n, a.rows, a.columns, 256, 128, kFlip) + pairs - 1) / pairs;
     if (wide * (0.85 * stages + 4.0) <= narrow * (0.5 * stages + 3.0))

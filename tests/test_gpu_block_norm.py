@@ -194,6 +194,31 @@ def test_many_rows(n, T, d):
     _check(n, T, d, torch.bfloat16, seed=T)
 
 
+# rows by bulk copies: four and more for every group of warps, 152 / n CTAs of 16 warps (8 in fp32), one to 16 a row
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
+@pytest.mark.parametrize("n,T,d", [(150, 67, 200), (77, 131, 512), (151, 35, 520), (151, 35, 1024), (152, 18, 1032), (120, 17, 2048),
+                                   (152, 9, 2056), (140, 11, 4096), (100, 7, 4104), (90, 5, 8192), (3, 1100, 4096), (256, 66, 64)])
+def test_rows_through_shared_memory(dtype, n, T, d):
+    if n * T * d > 4e6 and dtype is torch.float16:
+        pytest.skip("as bf16")
+    lengths = np.random.default_rng(d).integers(0, T + 1, n)
+    lengths[0], lengths[-1] = T, 0
+    _check(n, T, d, dtype, lengths=list(lengths), first=d % 3, seed=d)
+
+
+@pytest.mark.parametrize("gate,scale,over", [(False, False, False), (True, False, True), (False, True, False)])
+def test_options_of_rows_through_shared_memory(gate, scale, over):
+    for dtype in (torch.bfloat16, torch.float32):
+        _check(151, 35, 1000, dtype, gate=gate, scale=scale, over=over, ckpt=over, seed=3)
+    n, T, d = 151, 40, 1024
+    x, r, y = (torch.randn(n, T, d, device="cuda").bfloat16() for _ in range(3))
+    w = _weight(0, n, d)
+    want = torch.empty_like(x)
+    rs.relay_block_norm(x, r, w, w, want, y, EPS)
+    rs.relay_block_norm(x, r, w, w, r, y, EPS)  # the sum in the residual's own rows
+    assert torch.equal(r, want)
+
+
 def test_no_tokens():
     n, d = 2, 40
     x = torch.empty(n, 0, d, device="cuda")
@@ -223,12 +248,12 @@ def test_total_in_place_shared_weights_and_repeated_rows():
     assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3])
 
 
-def test_padding_may_hold_anything():
-    n, T, d = 2, 12, 264
+@pytest.mark.parametrize("n,T,d", [(2, 12, 264), (152, 70, 264)])
+def test_padding_may_hold_anything(n, T, d):
     for dtype in (torch.bfloat16, torch.float32):
         args = [torch.randn(n, T, d, device="cuda").to(dtype) for _ in range(5)]  # dy, dtotal, x, gate, residual
         w, rstd = torch.ones(n, d, device="cuda"), torch.rand(2, n, T, device="cuda")
-        lengths = torch.tensor([7, 0], dtype=torch.int32, device="cuda")
+        lengths = torch.tensor([7, 0] + [T] * (n - 2), dtype=torch.int32, device="cuda")
         work = torch.empty(rs.relay_block_norm_backward_workspace(n, T, d), dtype=torch.uint8, device="cuda")
 
         def run():
