@@ -6,8 +6,6 @@
 //
 // All rows in and all rows out once, two sums over a row between them, so memory bounds it.
 // kParts warps share a row, each with kStrips strips of 256 features (layers.cuh).
-#include <type_traits>
-
 #include "blackwell.cuh"
 #include "layers.cuh"
 
@@ -143,14 +141,20 @@ __device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at,
 }
 
 // Aligned rows of up to 8192 features in 16 bits and 4096 in 32, where there are some for
-// every group of kParts warps: they come by bulk copies to shared memory, two a group, the
-// next one on its way while this one's two sums are waited for; h stays in registers.
-template <typename T, int kParts, int kInputs>
+// every group of kParts warps: they come by bulk copies to shared memory and h stays in
+// registers.  The groups wait only for themselves; while one waits for its row or for one
+// of the two sums, others are at work.
+template <typename T, int kParts_, int kInputs>
 struct Ring {
-    static constexpr int kWarps = sizeof(T) == 2 ? 16 : 8, kGroups = kWarps / kParts, kStages = 2;
-    static constexpr int kWide = kParts * 4 * kQuads;  // features of a row at most
+    static constexpr int kParts = kParts_;
+    // the forward pass: 24 warps (12 in fp32) of 8 quads a lane, a row of each group at a time;
+    // the backward pass: 16 (8) of 4 quads, two rows of each group
+    static constexpr bool kBack = kInputs == 5;
+    static constexpr int kWarps = (kBack ? 16 : 24) / (sizeof(T) == 2 ? 1 : 2), kGroups = kWarps / kParts;
+    static constexpr int kHold = kBack ? 4 : 8, kStages = kBack ? 2 : 1;
+    static constexpr int kWide = kParts * kHold * kQuads;  // features of a row at most
     static constexpr int kRow = kWide * static_cast<int>(sizeof(T)), kStage = kInputs * kRow;  // bytes
-    static constexpr bool kWeights = kParts <= 8;  // there is room for the three weights too
+    static constexpr bool kWeights = kWide <= 4096;  // there is room for the three weights too
     static constexpr int kRows = kGroups * kStages * kStage, kShared = kRows + (kWeights ? 3 * 4 * kWide : 0) + 16;
     static_assert(kShared <= 232448 - 2048, "shared memory of a CTA");
 };
@@ -200,6 +204,13 @@ __device__ __forceinline__ void group_sum(float (&v)[kCount], float (&shared)[kP
     }
 }
 
+// Before a group's end: waits (about a second at most) for the copies of its last rows.
+// They have been waited for before, unless a wait ran out.
+__device__ __forceinline__ void none_in_flight(const uint64_t* bars, int stages, int rows) {
+    for (int i = max(0, rows - stages); i < rows; ++i)
+        if (!barrier_wait(shared_address(bars + i % stages), i / stages & 1)) break;
+}
+
 // A wait that runs out makes a group's results from there on NaN.
 template <typename T, int kParts>
 __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_block_norm_rows_kernel(BlockArgs<T> a) {
@@ -228,22 +239,21 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         copy_row(to + R::kRow, a.residual.row(worker, token), bytes, bar);
         if (gated) copy_row(to + 2 * R::kRow, a.gate.row(worker, token), bytes, bar);
     };
-    if (brings) {
-        if (begin < a.tokens) bring(begin, 0);
-        if (begin + step < a.tokens) bring(begin + step, 1);
-    }
+    if (brings)
+        for (int s = 0; s < R::kStages; ++s)
+            if (begin + s * step < a.tokens) bring(begin + s * step, s);
     const float over_d = 1.0f / static_cast<float>(a.d);
     bool ok = true;
     int i = 0;
     for (int token = begin; token < a.tokens; token += step, ++i) {
-        const int s = i % 2;
+        const int s = i % R::kStages;
         const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
-        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / 2 & 1);
+        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / R::kStages & 1);
         const T* from = reinterpret_cast<const T*>(mine + s * R::kStage);
         constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
-        Pair h[4][2], squares(0.0f);
+        Pair h[R::kHold][2], squares(0.0f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < R::kHold; ++j) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             load_quad(from + at, at < a.d, h[j]);
 #pragma unroll
@@ -254,7 +264,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         const float sx = 1.0f / sqrtf(sum[0] * over_d + a.eps);
         squares = Pair(0.0f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < R::kHold; ++j) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             const bool on = at < a.d;
             Pair w[2], rho[2], z[2], r[2];
@@ -273,14 +283,14 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         sum[0] = squares.sum();
         group_sum(sum, shared[1][group], group, part, lane);
         // here every warp of the group is done with the row in shared memory
-        if (brings && token + 2 * step < a.tokens) bring(token + 2 * step, s);
+        if (brings && token + R::kStages * step < a.tokens) bring(token + R::kStages * step, s);
         const float sh = 1.0f / sqrtf(sum[0] * over_d + a.eps);
         if (a.rstd != nullptr && part == 0 && lane == 0) {
             a.rstd[row] = sx;
             a.rstd[static_cast<int64_t>(gridDim.y) * a.tokens + row] = sh;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < R::kHold; ++j) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             const bool on = at < a.d;
             Pair w[2];
@@ -294,6 +304,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
             store_quad(a.y.row(worker, token) + at, on, h[j]);
         }
     }
+    if (brings) none_in_flight(&bars[group][0], R::kStages, i);
 }
 
 // ------------------------------------------------------------------ the backward pass
@@ -543,7 +554,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
         const int s = i % 2;
         const float sx = next_x, sh = next_h;
         if (token + step < length) next_x = factors[token + step], next_h = factors[second + token + step];
-        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / 2 & 1);
+        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / R::kStages & 1);
         const auto remake = [&](int j, Features<T, 2>& o, Pair (&w)[2], Pair (&rho)[2], Pair (&pre)[2], Pair (&u)[2], Pair (&over)[2]) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             const bool on = at < a.d;
@@ -587,6 +598,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
             if (gated) store_quad(a.dgate.row(worker, token) + at, on, dz);
         }
     }
+    if (brings) none_in_flight(&bars[group][0], R::kStages, i);
     // padding
     for (int token = begin + i * step; token < a.tokens; token += step) {
         const Pair none[2] = {Pair(0.0f), Pair(0.0f)};
@@ -637,21 +649,24 @@ struct Sums {  // where the three sums go
     int64_t stride[3];
 };
 
-// out[i][k] = sum_p partial[i][p][k]: a CTA sums 32 columns, 8 rows at a time.
-__global__ void __launch_bounds__(256) relay_block_norm_join_kernel(const float* partial, int parts, int d, int pitch, Sums to) {
-    __shared__ float shared[8][32];
-    const int column = blockIdx.x * 32 + threadIdx.x % 32, lead = threadIdx.x / 32, which = blockIdx.z;
+// out[i][k] = sum_p partial[i][p][k]: a CTA sums 32 columns, 32 rows at a time.
+__global__ void __launch_bounds__(1024) relay_block_norm_join_kernel(const float* partial, int parts, int d, int pitch, Sums to) {
+    __shared__ float shared[32][33];
+    const int lane = threadIdx.x % 32, column = blockIdx.x * 32 + lane, lead = threadIdx.x / 32, which = blockIdx.z;
     if (to.p[which] == nullptr) return;
     const float* p = partial + (static_cast<int64_t>(which) * gridDim.y + blockIdx.y) * parts * pitch;
     float s = 0.0f;
-    if (column < d)
-        for (int r = lead; r < parts; r += 8) s += p[static_cast<int64_t>(r) * pitch + column];
-    shared[lead][threadIdx.x % 32] = s;
+    if (column < d) {
+#pragma unroll 4
+        for (int r = lead; r < parts; r += 32) s += p[static_cast<int64_t>(r) * pitch + column];
+    }
+    shared[lead][lane] = s;
     __syncthreads();
-    if (lead > 0 || column >= d) return;
+    s = shared[lane][lead];  // lane r: the sum of rows r, 32 + r, ... of column `lead`
 #pragma unroll
-    for (int r = 1; r < 8; ++r) s += shared[r][threadIdx.x];
-    to.p[which][blockIdx.y * to.stride[which] + column] = s;
+    for (int m = 16; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+    const int mine = blockIdx.x * 32 + lead;
+    if (lane == 0 && mine < d) to.p[which][blockIdx.y * to.stride[which] + mine] = s;
 }
 
 // ---------------------------------------------------------------- launching
@@ -698,22 +713,28 @@ int launch_rows(const BlockBackwardArgs<T>& a, int64_t parts, int32_t n, cudaStr
     return status_of_launch();
 }
 
-// Whether rows go through shared memory: as wide as a CTA's warps hold, and at least four of
-// them for each group of warps, whose start costs as much as two (the weights, the barriers).
-bool takes_ring(int32_t type, int32_t n, int64_t tokens, int64_t d) {
-    const int64_t pitch = pitch_of(d), warps = type == RELAY_FP32 ? 8 : 16;
-    const int64_t side = pitch <= 512 ? warps : pitch <= 1024 ? warps / 2 : pitch <= 2048 ? warps / 4 : pitch <= 4096 ? warps / 8 : 1;
-    return d <= 512 * warps && tokens >= 4 * side * (152 > n ? 152 / n : 1);
+// f(R) for the Ring with the fewest warps a row that holds one; none (false) where the CTA's
+// warps do not.
+template <typename T, int kInputs, int kParts = 1, typename F>
+bool by_ring(int64_t d, F f) {
+    using R = Ring<T, kParts, kInputs>;
+    if (d <= R::kWide) {
+        f(R());
+        return true;
+    }
+    if constexpr (R::kWarps % (2 * kParts) == 0 && R::kWarps >= 2 * kParts) return by_ring<T, kInputs, 2 * kParts>(d, f);
+    return false;
 }
 
-// f(kParts) for the least that holds a row in four quads a lane.
-template <typename F>
-int by_ring(int64_t pitch, F f) {
-    if (pitch <= 512) return f(std::integral_constant<int, 1>());
-    if (pitch <= 1024) return f(std::integral_constant<int, 2>());
-    if (pitch <= 2048) return f(std::integral_constant<int, 4>());
-    if (pitch <= 4096) return f(std::integral_constant<int, 8>());
-    return f(std::integral_constant<int, 16>());
+// CTAs of a worker, and whether there are at least four rows for each group of them: their
+// start costs as much as two (the weights, the barriers).
+int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }
+
+template <typename T, int kInputs>
+bool takes_ring(int32_t n, int64_t tokens, int64_t d) {
+    bool takes = false;
+    by_ring<T, kInputs>(d, [&](auto r) { takes = tokens >= 4 * decltype(r)::kGroups * ring_ctas(n); });
+    return takes;
 }
 
 bool weight_fits(const float* p, int64_t stride) { return p != nullptr && aligned(p, 4) && stride >= 0; }
@@ -753,26 +774,24 @@ int relay_block_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
         return RELAY_EINVAL;
     const bool vec = d % 8 == 0 && vectors(x, type, n, tokens) && vectors(gate, type, n, tokens) &&
                      vectors(residual, type, n, tokens) && vectors(total, type, n, tokens) && vectors(y, type, n, tokens);
-    const bool ring = vec && takes_ring(type, n, tokens, d);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         const BlockArgs<T> a{view<const T>(x, n, tokens), view<const T>(gate, n, tokens), view<const T>(residual, n, tokens),
                              view<T>(total, n, tokens), view<T>(y, n, tokens), weight_of(post, post_stride, n, d),
                              weight_of(pre, pre_stride, n, d), weight_of(scale, scale_stride, n, d), eps, rstd, codes, scales,
                              static_cast<int32_t>(tokens), static_cast<int32_t>(d), static_cast<int32_t>(pitch_of(d))};
-        if (ring)
-            return by_ring(a.pitch, [&](auto with) {
-                constexpr int kParts = decltype(with)::value;
-                if constexpr (kParts <= Ring<T, 1, 3>::kWarps) {
-                    using R = Ring<T, kParts, 3>;
-                    constexpr auto kernel = relay_block_norm_rows_kernel<T, kParts>;
-                    if (!allow_shared<kernel>(R::kShared)) return RELAY_ECUDA;
-                    kernel<<<dim3(static_cast<unsigned>(152 > n ? 152 / n : 1), static_cast<unsigned>(n)), 32 * R::kWarps, R::kShared,
-                             stream>>>(a);
-                    return status_of_launch();
-                }
-                return RELAY_EUNSUPPORTED;  // (not reached: `ring`)
+        if (vec && takes_ring<T, 3>(n, tokens, d)) {
+            int rc = RELAY_OK;
+            by_ring<T, 3>(d, [&](auto r) {
+                using R = decltype(r);
+                constexpr auto kernel = relay_block_norm_rows_kernel<T, R::kParts>;
+                rc = allow_shared<kernel>(R::kShared) ? RELAY_OK : RELAY_ECUDA;
+                if (rc != RELAY_OK) return;
+                kernel<<<dim3(static_cast<unsigned>(ring_ctas(n)), static_cast<unsigned>(n)), 32 * R::kWarps, R::kShared, stream>>>(a);
+                rc = status_of_launch();
             });
+            return rc;
+        }
         return by_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr int kRows = kNormWarps<kParts> / kParts;
@@ -828,7 +847,6 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     bool vec = d % 8 == 0;
     for (const relay_rows* r : {dy, dtotal, x, gate, residual, dx, dgate, dresidual}) vec = vec && vectors(r, type, n, tokens);
     int parts = static_cast<int>(block_partials(n, tokens, d));
-    const bool ring = vec && takes_ring(type, n, tokens, d);
     const int rc = by_type(type, [&](auto t) {
         using T = decltype(t);
         const BlockBackwardArgs<T> a{
@@ -838,15 +856,15 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
             weight_of(pre, pre_stride, n, d), weight_of(scale, scale_stride, n, d), rstd, lengths,
             static_cast<float*>(workspace), static_cast<int32_t>(tokens), static_cast<int32_t>(d),
             static_cast<int32_t>(pitch_of(d))};
-        if (ring)
-            return by_ring(a.pitch, [&](auto with) {
-                constexpr int kParts = decltype(with)::value;
-                if constexpr (kParts <= Ring<T, 1, 5>::kWarps) {
-                    parts = static_cast<int>(ring_partials<T, kParts>(n, tokens, d));
-                    return launch_rows<T, kParts>(a, parts, n, stream);
-                }
-                return RELAY_EUNSUPPORTED;  // (not reached: `ring`)
+        if (vec && takes_ring<T, 5>(n, tokens, d)) {
+            int rc = RELAY_OK;
+            by_ring<T, 5>(d, [&](auto r) {
+                constexpr int kParts = decltype(r)::kParts;
+                parts = static_cast<int>(ring_partials<T, kParts>(n, tokens, d));
+                rc = launch_rows<T, kParts>(a, parts, n, stream);
             });
+            return rc;
+        }
         return by_back_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
             constexpr size_t kSmem = (kNormWarps<kParts> / kParts - 1) * kStrips * kParts * kStrip * sizeof(float);
@@ -858,7 +876,7 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     });
     if (rc != RELAY_OK) return rc;
     const Sums to{{dpost, dpre, dscale}, {dpost_stride, dpre_stride, dscale_stride}};
-    relay_block_norm_join_kernel<<<dim3(static_cast<unsigned>((d + 31) / 32), n, dscale == nullptr ? 2 : 3), 256, 0, stream>>>(
+    relay_block_norm_join_kernel<<<dim3(static_cast<unsigned>((d + 31) / 32), n, dscale == nullptr ? 2 : 3), 1024, 0, stream>>>(
         static_cast<const float*>(workspace), parts, static_cast<int>(d), static_cast<int>(pitch_of(d)), to);
     return status_of_launch();
 }

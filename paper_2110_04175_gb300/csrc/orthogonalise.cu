@@ -31,36 +31,23 @@ constexpr int kM = 128, kDepth = 64;  // rows of a CTA, and what a stage goes al
 constexpr int kAdders = 8, kIssuer = 8, kLoader = 9, kThreads = 32 * 12;
 constexpr int kSms = 152;
 
-// A kernel's shape: tiles of 128 kCtas x kN, operands of kTerms terms.
-template <int kCtas_, int kN_, int kTerms_>
+// A kernel's shape: tiles of 128 kCtas x kN.
+template <int kCtas_, int kN_>
 struct Shape {
-    static constexpr int kCtas = kCtas_, kN = kN_, kTerms = kTerms_, kHigh = kM * kCtas;
+    static constexpr int kCtas = kCtas_, kN = kN_, kHigh = kM * kCtas;
     static constexpr int kRight = kN / kCtas;  // columns that a CTA brings
     static constexpr int kLeftTerm = kM * 128, kRightTerm = kRight * 128;  // bytes of a term of a stage
-    static constexpr int kBytes = kTerms * (kLeftTerm + kRightTerm);
+    static constexpr int kBytes = 2 * (kLeftTerm + kRightTerm);
     static constexpr int kFit = (232448 - 1024 - 256) / kBytes, kCount = kFit < 4 ? kFit : 4;  // stages
     static constexpr int kShared = kCount * kBytes + 1024 + 256;
-    static constexpr int kProducts = kTerms == 2 ? 3 : 6;
-    // stages that the tensor cores sum: 36 additions, or 24
-    static constexpr int kGroup = kTerms == 2 ? 3 : 1;
+    static constexpr int kGroup = 3;  // stages that the tensor cores sum: 36 additions
     static_assert(kCount >= 2 && kShared <= 232448 && kHigh % kN == 0, "shape of the tiles");
 };
-
-// The terms whose products are summed, from the least to the greatest: left, right.
-template <int kTerms>
-__device__ __forceinline__ constexpr int left_term(int t) {
-    constexpr int two[3] = {1, 0, 0}, three[6] = {2, 1, 0, 1, 0, 0};
-    return kTerms == 2 ? two[t % 3] : three[t];
-}
-template <int kTerms>
-__device__ __forceinline__ constexpr int right_term(int t) {
-    constexpr int two[3] = {0, 1, 0}, three[6] = {0, 1, 2, 0, 1, 0};
-    return kTerms == 2 ? two[t % 3] : three[t];
-}
 
 struct ProductArgs {
     const __half* c;  // what is added, times beta: [n][kTerms][rows][pitch], or NULL
     __half* out;      // the same shape, or NULL, and
+    int32_t left_terms, right_terms;  // terms that the operands are held in: the first two count
     float* final;     // fp32: element (i, j) at i row_stride + j column_stride
     int64_t worker_stride, row_stride, column_stride;
     float alpha, beta, scale;  // scale: of `final`
@@ -118,14 +105,14 @@ __device__ __forceinline__ void split(float v, __half (&term)[kTerms]) {
     }
 }
 
-// out = alpha (left right) + beta c.  left [n][kTerms][rows][depth]; right [n][kTerms][columns][depth], or with
-// kFlip [n][kTerms][depth][columns].  A wait that runs out ends a pair's work, and its results from there on are
+// out = alpha (left right) + beta c.  left [n][left_terms][rows][depth]; right [n][right_terms][columns][depth],
+// or with kFlip [n][right_terms][depth][columns].  c and out are held in kTerms terms.  A wait that runs out ends a pair's work, and its results from there on are
 // NaN.
-template <typename S, bool kFlip>
+template <typename S, bool kFlip, int kTerms>
 __global__ void __launch_bounds__(kThreads, 1)
 relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap left_map,
                            const __grid_constant__ CUtensorMap right_map) {
-    constexpr int kCtas = S::kCtas, kN = S::kN, kTerms = S::kTerms, kCount = S::kCount;
+    constexpr int kCtas = S::kCtas, kN = S::kN, kCount = S::kCount;
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
     const uint32_t bars = stages + kCount * S::kBytes;
@@ -254,14 +241,14 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
                 } else {
                     tensor_fence_after();
                     if (elected()) {
-                        const uint32_t l = stages + s * S::kBytes, r = l + kTerms * S::kLeftTerm;
+                        const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
                         constexpr uint32_t kNext = kFlip ? 16 * 128 / 16 : 2;  // 16 of K, in 16 bytes
 #pragma unroll
                         for (int k = 0; k < kDepth / 16; ++k)
 #pragma unroll
-                            for (int t = 0; t < S::kProducts; ++t) {
-                                const uint32_t at_r = r + right_term<kTerms>(t) * S::kRightTerm;
-                                const uint64_t x = operand_k(l + left_term<kTerms>(t) * S::kLeftTerm) + 2 * k;
+                            for (int t = 0; t < 3; ++t) {  // lo hi, hi lo, hi hi
+                                const uint32_t at_r = r + (t == 1 ? S::kRightTerm : 0);
+                                const uint64_t x = operand_k(l + (t == 0 ? S::kLeftTerm : 0)) + 2 * k;
                                 const uint64_t y = (kFlip ? operand(at_r, kDepth * 128, 1024) : operand_k(at_r)) + kNext * k;
                                 product<kCtas>(tensor + b * kN, x, y, kKind<S, kFlip>, place + k + t > 0);
                             }
@@ -282,18 +269,18 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
                 const int s = i % kCount, k = n * kDepth;
                 if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
                 barrier_expect(full(s), S::kBytes);
-                const uint32_t l = stages + s * S::kBytes, r = l + kTerms * S::kLeftTerm;
+                const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
                 const int column = at.column + S::kRight * rank;
 #pragma unroll
-                for (int t = 0; t < kTerms; ++t) {
-                    copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, kTerms * at.worker + t, full(s));
+                for (int t = 0; t < 2; ++t) {
+                    copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, a.left_terms * at.worker + t, full(s));
                     if (!kFlip)
-                        copy_box(r + t * S::kRightTerm, &right_map, k, column, kTerms * at.worker + t, full(s));
+                        copy_box(r + t * S::kRightTerm, &right_map, k, column, a.right_terms * at.worker + t, full(s));
                     else
 #pragma unroll
                         for (int p = 0; p < S::kRight / 64; ++p)
                             copy_box(r + t * S::kRightTerm + p * kDepth * 128, &right_map, column + 64 * p, k,
-                                     kTerms * at.worker + t, full(s));
+                                     a.right_terms * at.worker + t, full(s));
                 }
             }
         }
@@ -476,14 +463,14 @@ int64_t tile_count(int64_t n, int64_t rows, int64_t columns, int high, int wide,
     return n * tiles;
 }
 
-template <typename S, bool kFlip>
+template <typename S, bool kFlip, int kTerms>
 int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t stream) {
-    constexpr auto kernel = relay_orthogonalise_kernel<S, kFlip>;
+    constexpr auto kernel = relay_orthogonalise_kernel<S, kFlip, kTerms>;
     if (!allow_shared<kernel>(S::kShared)) return RELAY_ECUDA;
     CUtensorMap left_map, right_map;
-    if (!map_terms(&left_map, left, a.n, S::kTerms, a.rows, a.depth, kM) ||
-        !(kFlip ? map_terms(&right_map, right, a.n, S::kTerms, a.depth, a.columns, kDepth)
-                : map_terms(&right_map, right, a.n, S::kTerms, a.columns, a.depth, S::kRight)))
+    if (!map_terms(&left_map, left, a.n, a.left_terms, a.rows, a.depth, kM) ||
+        !(kFlip ? map_terms(&right_map, right, a.n, a.right_terms, a.depth, a.columns, kDepth)
+                : map_terms(&right_map, right, a.n, a.right_terms, a.columns, a.depth, S::kRight)))
         return RELAY_ECUDA;
     a.tiles_m = (a.rows + S::kHigh - 1) / S::kHigh;
     a.tiles_n = (a.columns + S::kN - 1) / S::kN;
@@ -495,35 +482,30 @@ int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t 
                         right_map);
 }
 
-// Three terms where m is small: sums are short there, so that what two terms leave out is what
-// limits them.  Errors against 64 bits, with two terms, three and in plain fp32, in 1e-6:
-// [128][256] 3.4, 1.8, 1.6; [300][2000] 4.9, 1.9, 2.4; [360][5000] 4.8, -, 2.6; [512][4096]
-// 1.7, 0.9, 2.7; [1001][1537] 2.1, -, 3.2.
-int terms_of(int64_t m) { return m <= 448 ? 3 : 2; }
-
-// The shape that should take the least time.
-template <bool kFlip>
-int launch(int terms, const ProductArgs& a, const __half* left, const __half* right, cudaStream_t stream) {
-    const int64_t stages = (a.depth + kDepth - 1) / kDepth, pairs = kSms / 2;
-    if (terms == 3) {
-        const int64_t alone = (tile_count(a.n, a.rows, a.columns, 128, 64, kFlip) + kSms - 1) / kSms;
-        const int64_t paired = (tile_count(a.n, a.rows, a.columns, 256, 128, kFlip) + pairs - 1) / pairs;
-        if (alone * (0.6 * stages + 3.0) <= paired * (1.0 * stages + 3.0))
-            return launch<Shape<1, 64, 3>, kFlip>(a, left, right, stream);
-        return launch<Shape<2, 128, 3>, kFlip>(a, left, right, stream);
-    }
-    const int64_t wide = (tile_count(a.n, a.rows, a.columns, 256, 256, kFlip) + pairs - 1) / pairs;
-    const int64_t narrow = (tile_count(a.n, a.rows, a.columns, 256, 128, kFlip) + pairs - 1) / pairs;
-    if (wide * (0.85 * stages + 4.0) <= narrow * (0.5 * stages + 3.0))
-        return launch<Shape<2, 256, 2>, kFlip>(a, left, right, stream);
-    return launch<Shape<2, 128, 2>, kFlip>(a, left, right, stream);
+// The shape that should take the least time: rounds of tiles, a stage's time and a tile's.
+template <bool kFlip, int kTerms>
+int launch(const ProductArgs& a, const __half* left, const __half* right, cudaStream_t stream) {
+    const double stages = static_cast<double>((a.depth + kDepth - 1) / kDepth);
+    const auto us = [&](int ctas, int wide, double stage, double tile) {
+        const int64_t most = kSms / ctas;
+        return static_cast<double>((tile_count(a.n, a.rows, a.columns, kM * ctas, wide, kFlip) + most - 1) / most) * (stage * stages + tile);
+    };
+    const double big = us(2, 256, 0.85, 4.0), middle = us(2, 128, 0.5, 3.0), small = us(1, 64, 0.35, 2.0);
+    if (small <= middle && small <= big) return launch<Shape<1, 64>, kFlip, kTerms>(a, left, right, stream);
+    if (middle <= big) return launch<Shape<2, 128>, kFlip, kTerms>(a, left, right, stream);
+    return launch<Shape<2, 256>, kFlip, kTerms>(a, left, right, stream);
 }
+
+// What x is rounded by goes on with a x, and is multiplied by a in every step along small
+// singular values, where the products have little part.  So x is held in a third term, which
+// only that addition reads, where sums are too short to be off by more.
+int terms_of(int64_t m) { return m <= 448 ? 3 : 2; }
 
 // Where the workspace's parts begin, in bytes.
 struct Parts {
     int64_t x, g, p, sums, size;
     Parts(int64_t n, int64_t m, int64_t k) {
-        const int64_t terms = terms_of(m), wide = 2 * terms * n * m * pitch_to(k), square = 2 * terms * n * m * pitch_to(m);
+        const int64_t wide = 2 * terms_of(m) * n * m * pitch_to(k), square = 4 * n * m * pitch_to(m);
         x = 0, g = 2 * wide, p = g + square, sums = p + square, size = sums + 12 * n * kParts;
     }
 };
@@ -591,19 +573,19 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
         ProductArgs a{};
         a.n = n, a.rows = static_cast<int32_t>(m);
         a.columns = static_cast<int32_t>(m), a.depth = static_cast<int32_t>(k), a.pitch = pitch_to(m);
-        a.alpha = 1.0f / kHeld, a.out = g;
-        if (const int rc = launch<false>(terms, a, now, now, stream)) return rc;
+        a.alpha = 1.0f / kHeld, a.out = g, a.left_terms = a.right_terms = terms;
+        if (const int rc = launch<false, 2>(a, now, now, stream)) return rc;
         a.depth = static_cast<int32_t>(m);
-        a.alpha = kC / kHeld, a.beta = kB, a.c = g, a.out = p;
-        if (const int rc = launch<false>(terms, a, g, g, stream)) return rc;
+        a.alpha = kC / kHeld, a.beta = kB, a.c = g, a.out = p, a.left_terms = a.right_terms = 2;
+        if (const int rc = launch<false, 2>(a, g, g, stream)) return rc;
         a.columns = static_cast<int32_t>(k), a.pitch = pitch_to(k);
-        a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1];
+        a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1], a.right_terms = terms;
         if (step == steps - 1) {
             a.scale = a.alpha * (scale / kHeld);
             a.out = nullptr, a.final = out, a.worker_stride = n > 1 ? out_worker_stride : 0;
             a.row_stride = tall ? 1 : out_row_stride, a.column_stride = tall ? out_row_stride : 1;
         }
-        if (const int rc = launch<true>(terms, a, p, now, stream)) return rc;
+        if (const int rc = terms == 3 ? launch<true, 3>(a, p, now, stream) : launch<true, 2>(a, p, now, stream)) return rc;
     }
     return RELAY_OK;
 }

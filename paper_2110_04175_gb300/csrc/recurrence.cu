@@ -319,6 +319,12 @@ struct Boxes {
     __device__ __forceinline__ uint32_t bar(int tile) const { return bars + 8 * (tile % kStages); }
     // false after about a second; from then on nothing is waited for
     __device__ __forceinline__ bool wait(int tile) const { return barrier_wait_warp(bar(tile), tile / kStages & 1); }
+    // Before the end: waits (about a second at most) for the last tiles' copies, which have been
+    // waited for before unless a wait ran out.  One thread.
+    __device__ __forceinline__ void none_in_flight(int tiles) const {
+        for (int i = max(0, tiles - kStages); i < tiles; ++i)
+            if (!barrier_wait(bar(i), i / kStages & 1)) break;
+    }
     // The lane's two channels of token `token` of box `box`.
     __device__ __forceinline__ Two<T> get(int tile, int box, int token, int lane) const {
         return reinterpret_cast<const Two<T>*>(at + tile % kStages * kStage + box * kBox)[token * (kWide / 2) + lane];
@@ -401,6 +407,7 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
             }
         }
     }
+    if (threadIdx.x == 0) boxes.none_in_flight(tiles);
     if (a.segments == 1 && a.last != nullptr && part == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
 }
@@ -675,6 +682,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
             }
         }
     }
+    if (threadIdx.x == 0) boxes.none_in_flight(tiles);
     if (a.segments == 1 && a.last != nullptr && part == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
