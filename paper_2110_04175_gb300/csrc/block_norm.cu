@@ -649,24 +649,25 @@ struct Sums {  // where the three sums go
     int64_t stride[3];
 };
 
-// out[i][k] = sum_p partial[i][p][k]: a CTA sums 32 columns, 32 rows at a time.
-__global__ void __launch_bounds__(1024) relay_block_norm_join_kernel(const float* partial, int parts, int d, int pitch, Sums to) {
-    __shared__ float shared[32][33];
-    const int lane = threadIdx.x % 32, column = blockIdx.x * 32 + lane, lead = threadIdx.x / 32, which = blockIdx.z;
+// out[i][k] = sum_p partial[i][p][k]: a CTA sums 128 columns, 8 rows at a time.
+__global__ void __launch_bounds__(256) relay_block_norm_join_kernel(const float* partial, int parts, int d, int pitch, Sums to) {
+    __shared__ float4 shared[8][32];
+    const int lane = threadIdx.x % 32, column = blockIdx.x * 128 + 4 * lane, lead = threadIdx.x / 32, which = blockIdx.z;
     if (to.p[which] == nullptr) return;
     const float* p = partial + (static_cast<int64_t>(which) * gridDim.y + blockIdx.y) * parts * pitch;
-    float s = 0.0f;
-    if (column < d) {
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const auto add = [&](float4 v) { s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w; };
 #pragma unroll 4
-        for (int r = lead; r < parts; r += 32) s += p[static_cast<int64_t>(r) * pitch + column];
-    }
+    for (int r = lead; r < parts; r += 8) add(*reinterpret_cast<const float4*>(p + static_cast<int64_t>(r) * pitch + column));
     shared[lead][lane] = s;
     __syncthreads();
-    s = shared[lane][lead];  // lane r: the sum of rows r, 32 + r, ... of column `lead`
+    if (lead > 0) return;
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
-    const int mine = blockIdx.x * 32 + lead;
-    if (lane == 0 && mine < d) to.p[which][blockIdx.y * to.stride[which] + mine] = s;
+    for (int r = 1; r < 8; ++r) add(shared[r][lane]);
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (column + k < d) to.p[which][blockIdx.y * to.stride[which] + column + k] = v[k];
 }
 
 // ---------------------------------------------------------------- launching
@@ -876,7 +877,7 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     });
     if (rc != RELAY_OK) return rc;
     const Sums to{{dpost, dpre, dscale}, {dpost_stride, dpre_stride, dscale_stride}};
-    relay_block_norm_join_kernel<<<dim3(static_cast<unsigned>((d + 31) / 32), n, dscale == nullptr ? 2 : 3), 1024, 0, stream>>>(
+    relay_block_norm_join_kernel<<<dim3(static_cast<unsigned>((d + 127) / 128), n, dscale == nullptr ? 2 : 3), 256, 0, stream>>>(
         static_cast<const float*>(workspace), parts, static_cast<int>(d), static_cast<int>(pitch_of(d)), to);
     return status_of_launch();
 }

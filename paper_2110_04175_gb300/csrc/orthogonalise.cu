@@ -29,6 +29,9 @@ constexpr float kHeld = 4096.0f;  // operands are held times this
 
 constexpr int kM = 128, kDepth = 64;  // rows of a CTA, and what a stage goes along the summed axis
 constexpr int kAdders = 8, kIssuer = 8, kLoader = 9, kThreads = 32 * 12;
+constexpr int kTurn = 32 * 128;  // bytes of an adder's 32 rows on their way from or to memory
+// tiles of 256 columns: 3 warpgroups are launched with 168 registers a thread, 2 x 224 + 56 = 3 x 168
+constexpr int kAdderRegisters = 224, kOtherRegisters = 56;
 constexpr int kSms = 152;
 
 // A kernel's shape: tiles of 128 kCtas x kN.
@@ -38,21 +41,20 @@ struct Shape {
     static constexpr int kRight = kN / kCtas;  // columns that a CTA brings
     static constexpr int kLeftTerm = kM * 128, kRightTerm = kRight * 128;  // bytes of a term of a stage
     static constexpr int kBytes = 2 * (kLeftTerm + kRightTerm);
-    static constexpr int kFit = (232448 - 1024 - 256) / kBytes, kCount = kFit < 4 ? kFit : 4;  // stages
-    static constexpr int kShared = kCount * kBytes + 1024 + 256;
-    static constexpr int kGroup = 3;  // stages that the tensor cores sum: 36 additions
+    static constexpr int kFit = (232448 - 1024 - 256 - kAdders * kTurn) / kBytes, kCount = kFit < 4 ? kFit : 4;  // stages
+    static constexpr int kShared = kCount * kBytes + kAdders * kTurn + 1024 + 256;
     static_assert(kCount >= 2 && kShared <= 232448 && kHigh % kN == 0, "shape of the tiles");
 };
 
 struct ProductArgs {
-    const __half* c;  // what is added, times beta: [n][kTerms][rows][pitch], or NULL
+    const __half* c;  // what is added, times beta: [n][2][rows][pitch], or NULL
     __half* out;      // the same shape, or NULL, and
-    int32_t left_terms, right_terms;  // terms that the operands are held in: the first two count
     float* final;     // fp32: element (i, j) at i row_stride + j column_stride
     int64_t worker_stride, row_stride, column_stride;
     float alpha, beta, scale;  // scale: of `final`
     int32_t n, rows, columns, depth, pitch;
     int32_t tiles_m, tiles_n, tiles;
+    int32_t group;  // stages that the tensor cores sum
 };
 
 // The tile's place; kFlip: all tiles, otherwise those on and below the diagonal.
@@ -95,27 +97,44 @@ __device__ __forceinline__ uint64_t operand_k(uint32_t at) {
 template <typename S, bool kFlip>
 constexpr uint32_t kKind = 1u << 4 | uint32_t(kFlip) << 16 | uint32_t(S::kN / 8) << 17 | uint32_t(S::kHigh / 16) << 24;
 
-// v as terms: each the rest of those before it, rounded to fp16.
-template <int kTerms>
-__device__ __forceinline__ void split(float v, __half (&term)[kTerms]) {
-#pragma unroll
-    for (int t = 0; t < kTerms; ++t) {
-        term[t] = __float2half_rn(v);
-        v -= __half2float(term[t]);
-    }
+// v as two terms, each rounded to fp16.
+__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
+    hi = __float2half_rn(v);
+    lo = __float2half_rn(v - __half2float(hi));
 }
 
-// out = alpha (left right) + beta c.  left [n][left_terms][rows][depth]; right [n][right_terms][columns][depth],
-// or with kFlip [n][right_terms][depth][columns].  c and out are held in kTerms terms.  A wait that runs out ends a pair's work, and its results from there on are
+// An adder's 32 rows of 128 bytes in shared memory, 16-byte pieces swizzled by the row: a lane has
+// a row, memory is read and written row by row.  (With every lane at a row of its own in memory
+// an access was 32 lines: 10 to 15 us a tile.)
+struct Turn {
+    uint32_t at;
+    __device__ __forceinline__ uint32_t piece(int row, int q) const { return at + row * 128 + ((q ^ (row & 7)) << 4); }
+    __device__ __forceinline__ void put(int row, int q, uint4 v) const {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece(row, q)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+    __device__ __forceinline__ uint4 get(int row, int q) const {
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(piece(row, q)) : "memory");
+        return v;
+    }
+    __device__ __forceinline__ float number(int row, int k) const {  // fp32 number k of the row
+        float v;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(piece(row, k / 4) + k % 4 * 4) : "memory");
+        return v;
+    }
+};
+
+// out = alpha (left right) + beta c.  left [n][2][rows][depth]; right [n][2][columns][depth], or with kFlip
+// [n][2][depth][columns].  A wait that runs out ends a pair's work, and its results from there on are
 // NaN.
-template <typename S, bool kFlip, int kTerms>
+template <typename S, bool kFlip>
 __global__ void __launch_bounds__(kThreads, 1)
 relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap left_map,
                            const __grid_constant__ CUtensorMap right_map) {
     constexpr int kCtas = S::kCtas, kN = S::kN, kCount = S::kCount;
     extern __shared__ uint8_t raw[];
     const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u;
-    const uint32_t bars = stages + kCount * S::kBytes;
+    const uint32_t turns = stages + kCount * S::kBytes, bars = turns + kAdders * kTurn;
     // per stage: full (on CTA 0 of the other CTA's half too) and free again; per accumulator:
     // summed by the tensor cores, and read
     const auto full = [&](int s) { return bars + 8 * s; };
@@ -151,34 +170,58 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
     wait_for_previous();
 
     if (warp < kAdders) {
-        constexpr int kColumns = kN / 2;
+        if constexpr (kN == 256) more_registers<kAdderRegisters>();
+        constexpr int kColumns = kN / 2, kChunk = kColumns < 64 ? kColumns : 64, kPieces = kChunk / 8;
         const int row = 32 * (warp % 4), column = kColumns * (warp / 4);  // of the CTA's 128 x kN
         const int64_t plane = static_cast<int64_t>(a.rows) * a.pitch;
+        const Turn turn{turns + static_cast<uint32_t>(warp) * kTurn};
         bool ok = true;
         int group = 0;  // of all that the pair has summed
         for (int tile = pair; tile < a.tiles; tile += pairs) {
             const Tile<S, kFlip> at(a, tile);
-            const int i = at.row + kM * rank + row + lane, j0 = at.column + column;
-            const int64_t base = static_cast<int64_t>(at.worker) * kTerms * plane + static_cast<int64_t>(i) * a.pitch + j0;
+            const int i0 = at.row + kM * rank + row, j0 = at.column + column;
+            const int64_t base = static_cast<int64_t>(at.worker) * 2 * plane + static_cast<int64_t>(i0) * a.pitch + j0;
+            // piece p of a lane as memory is read and written: kPieces lanes a row
+            const auto place = [&](int c, int p, int& r, int& q) {
+                r = (p * 32 + lane) / kPieces, q = (p * 32 + lane) % kPieces;
+                return i0 + r < a.rows && j0 + c + 8 * q < a.columns;
+            };
             // beta c is where the sum starts, so that it comes while the tensor cores are at work
-            float sum[kColumns];
-            const float start = a.beta / a.alpha;
+            float sum[kColumns] = {};
+            if (a.c != nullptr) {
+                const float start = a.beta / a.alpha;
 #pragma unroll
-            for (int c = 0; c < kColumns; c += 8) {
-                uint4 part[kTerms];
-                const bool there = a.c != nullptr && i < a.rows && j0 + c < a.columns;
+                for (int c = 0; c < kColumns; c += kChunk) {
+                    uint4 part[2][kPieces];
 #pragma unroll
-                for (int t = 0; t < kTerms; ++t)
-                    part[t] = there ? *reinterpret_cast<const uint4*>(a.c + base + t * plane + c) : make_uint4(0, 0, 0, 0);
+                    for (int p = 0; p < kPieces; ++p) {
+                        int r, q;
+                        const bool there = place(c, p, r, q);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float v = 0.0f;
+                        for (int t = 0; t < 2; ++t)
+                            part[t][p] = there ? *reinterpret_cast<const uint4*>(a.c + base + t * plane + static_cast<int64_t>(r) * a.pitch + c + 8 * q)
+                                               : make_uint4(0, 0, 0, 0);
+                    }
 #pragma unroll
-                    for (int t = kTerms - 1; t >= 0; --t) v += __half2float(reinterpret_cast<const __half*>(&part[t])[e]);
-                    sum[c + e] = start * v;
+                    for (int t = 0; t < 2; ++t) {
+                        __syncwarp();
+#pragma unroll
+                        for (int p = 0; p < kPieces; ++p) turn.put((p * 32 + lane) / kPieces, (p * 32 + lane) % kPieces, part[t][p]);
+                        __syncwarp();
+#pragma unroll
+                        for (int q = 0; q < kPieces; ++q) {
+                            const uint4 v = turn.get(lane, q);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                float& to = sum[c + 8 * q + e];
+                                const float part_of = __half2float(reinterpret_cast<const __half*>(&v)[e]);
+                                to = t == 0 ? part_of : start * (to + part_of);
+                            }
+                        }
+                    }
                 }
             }
-            for (int done = 0; done < count && ok; done += S::kGroup, ++group) {
+            for (int done = 0; done < count && ok; done += a.group, ++group) {
                 const int b = group & 1;
                 if (!(ok = barrier_wait_warp(summed(b), group >> 1 & 1))) break;
                 tensor_fence_after();
@@ -194,99 +237,129 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
                 __syncwarp();
                 if (lane == 0) barrier_arrive(read(b));
             }
+            const float factor = !ok ? __int_as_float(0x7fffffff) : a.out != nullptr ? a.alpha : a.scale;
 #pragma unroll
-            for (int c = 0; c < kColumns; c += 8) {
-                const int j = j0 + c;
-                if (j >= a.columns || i >= a.rows) break;
-                if (a.out != nullptr) {
-                    uint4 part[kTerms];
+            for (int e = 0; e < kColumns; ++e) sum[e] *= factor;
+            if (a.out != nullptr) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        __half term[kTerms];
-                        split(ok ? a.alpha * sum[c + e] : __int_as_float(0x7fffffff), term);
+                for (int c = 0; c < kColumns; c += kChunk) {
+                    if (j0 + c >= a.columns) break;
 #pragma unroll
-                        for (int t = 0; t < kTerms; ++t) reinterpret_cast<__half*>(&part[t])[e] = term[t];
-                    }
+                    for (int t = 0; t < 2; ++t) {
+                        __syncwarp();
 #pragma unroll
-                    for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(a.out + base + t * plane + c) = part[t];
-                    if (!kFlip && at.mirror) {  // its place above the diagonal
-                        __half* over = a.out + static_cast<int64_t>(at.worker) * kTerms * plane + static_cast<int64_t>(j) * a.pitch + i;
+                        for (int q = 0; q < kPieces; ++q) {
+                            uint4 v;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            if (j + e >= a.columns) break;
+                            for (int e = 0; e < 8; ++e) {
+                                __half hi, lo;
+                                split(sum[c + 8 * q + e], hi, lo);
+                                reinterpret_cast<__half*>(&v)[e] = t == 0 ? hi : lo;
+                            }
+                            turn.put(lane, q, v);
+                            if (!kFlip && at.mirror && i0 + lane < a.rows) {  // its place above the diagonal
+                                const int j = j0 + c + 8 * q;
+                                __half* over = a.out + (static_cast<int64_t>(at.worker) * 2 + t) * plane + static_cast<int64_t>(j) * a.pitch + i0 + lane;
 #pragma unroll
-                            for (int t = 0; t < kTerms; ++t)
-                                over[e * a.pitch + t * plane] = reinterpret_cast<const __half*>(&part[t])[e];
+                                for (int e = 0; e < 8; ++e)
+                                    if (j + e < a.columns) over[e * a.pitch] = reinterpret_cast<const __half*>(&v)[e];
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int p = 0; p < kPieces; ++p) {
+                            int r, q;
+                            if (place(c, p, r, q))
+                                *reinterpret_cast<uint4*>(a.out + base + t * plane + static_cast<int64_t>(r) * a.pitch + c + 8 * q) = turn.get(r, q);
                         }
                     }
-                } else {
-                    float* to = a.final + at.worker * a.worker_stride + i * a.row_stride + j * a.column_stride;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (j + e < a.columns) to[e * a.column_stride] = ok ? a.scale * sum[c + e] : __int_as_float(0x7fffffff);
                 }
-            }
-        }
-    } else if (warp == kIssuer) {
-        int i = 0, group = 0;  // of all that the pair has summed
-        bool ok = true;
-        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
-            for (int n = 0; n < count; ++n, ++i) {
-                const int s = i % kCount, place = n % S::kGroup, b = group & 1;
-                if (place == 0 && group > 1 && !(ok = barrier_wait_warp(read(b), (group >> 1 & 1) ^ 1))) break;
-                if (!(ok = barrier_wait_warp(full(s), i / kCount & 1))) break;
-                const bool last = place == S::kGroup - 1 || n == count - 1;
-                if (rank != 0) {
-                    if (elected()) barrier_arrive_there(in_cta(full(s), 0));
-                } else {
-                    tensor_fence_after();
-                    if (elected()) {
-                        const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
-                        constexpr uint32_t kNext = kFlip ? 16 * 128 / 16 : 2;  // 16 of K, in 16 bytes
+            } else if (a.column_stride == 1) {
 #pragma unroll
-                        for (int k = 0; k < kDepth / 16; ++k)
-#pragma unroll
-                            for (int t = 0; t < 3; ++t) {  // lo hi, hi lo, hi hi
-                                const uint32_t at_r = r + (t == 1 ? S::kRightTerm : 0);
-                                const uint64_t x = operand_k(l + (t == 0 ? S::kLeftTerm : 0)) + 2 * k;
-                                const uint64_t y = (kFlip ? operand(at_r, kDepth * 128, 1024) : operand_k(at_r)) + kNext * k;
-                                product<kCtas>(tensor + b * kN, x, y, kKind<S, kFlip>, place + k + t > 0);
-                            }
-                        products_arrive<kCtas>(freed(s));
-                        if (last) products_arrive<kCtas>(summed(b));
-                    }
+                for (int c = 0; c < kColumns; c += 32) {
+                    if (j0 + c >= a.columns) break;
                     __syncwarp();
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        turn.put(lane, q, make_uint4(__float_as_uint(sum[c + 4 * q]), __float_as_uint(sum[c + 4 * q + 1]),
+                                                     __float_as_uint(sum[c + 4 * q + 2]), __float_as_uint(sum[c + 4 * q + 3])));
+                    __syncwarp();
+                    float* to = a.final + at.worker * a.worker_stride + i0 * a.row_stride + j0 + c + lane;
+                    const int rows = min(32, a.rows - i0);
+                    if (j0 + c + lane < a.columns)
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r) to[r * a.row_stride] = turn.number(r, lane);
                 }
-                if (last) ++group;
+            } else if (i0 + lane < a.rows) {
+                float* to = a.final + at.worker * a.worker_stride + (i0 + lane) * a.row_stride + j0 * a.column_stride;
+#pragma unroll
+                for (int e = 0; e < kColumns; ++e)
+                    if (j0 + e < a.columns) to[e * a.column_stride] = sum[e];
             }
         }
-    } else if (warp == kLoader && elected()) {
-        int i = 0;
-        bool ok = true;
-        for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
-            const Tile<S, kFlip> at(a, tile);
-            for (int n = 0; n < count; ++n, ++i) {
-                const int s = i % kCount, k = n * kDepth;
-                if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
-                barrier_expect(full(s), S::kBytes);
-                const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
-                const int column = at.column + S::kRight * rank;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, a.left_terms * at.worker + t, full(s));
-                    if (!kFlip)
-                        copy_box(r + t * S::kRightTerm, &right_map, k, column, a.right_terms * at.worker + t, full(s));
-                    else
-#pragma unroll
-                        for (int p = 0; p < S::kRight / 64; ++p)
-                            copy_box(r + t * S::kRightTerm + p * kDepth * 128, &right_map, column + 64 * p, k,
-                                     a.right_terms * at.worker + t, full(s));
+    } else {
+        if constexpr (kN == 256) fewer_registers<kOtherRegisters>();
+        if (warp == kIssuer) {
+            int i = 0, group = 0;  // of all that the pair has summed
+            bool ok = true;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                for (int n = 0; n < count; ++n, ++i) {
+                    const int s = i % kCount, place = n % a.group, b = group & 1;
+                    if (place == 0 && group > 1 && !(ok = barrier_wait_warp(read(b), (group >> 1 & 1) ^ 1))) break;
+                    if (!(ok = barrier_wait_warp(full(s), i / kCount & 1))) break;
+                    const bool last = place == a.group - 1 || n == count - 1;
+                    if (rank != 0) {
+                        if (elected()) barrier_arrive_there(in_cta(full(s), 0));
+                    } else {
+                        tensor_fence_after();
+                        if (elected()) {
+                            const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
+                            constexpr uint32_t kNext = kFlip ? 16 * 128 / 16 : 2;  // 16 of K, in 16 bytes
+    #pragma unroll
+                            for (int t = 0; t < 3; ++t)  // lo hi, hi lo, hi hi: the small ones first
+    #pragma unroll
+                                for (int k = 0; k < kDepth / 16; ++k) {
+                                    const uint32_t at_r = r + (t == 1 ? S::kRightTerm : 0);
+                                    const uint64_t x = operand_k(l + (t == 0 ? S::kLeftTerm : 0)) + 2 * k;
+                                    const uint64_t y = (kFlip ? operand(at_r, kDepth * 128, 1024) : operand_k(at_r)) + kNext * k;
+                                    product<kCtas>(tensor + b * kN, x, y, kKind<S, kFlip>, place + k + t > 0);
+                                }
+                            products_arrive<kCtas>(freed(s));
+                            if (last) products_arrive<kCtas>(summed(b));
+                        }
+                        __syncwarp();
+                    }
+                    if (last) ++group;
                 }
             }
+        } else if (warp == kLoader && elected()) {
+            int i = 0;
+            bool ok = true;
+            for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+                const Tile<S, kFlip> at(a, tile);
+                for (int n = 0; n < count; ++n, ++i) {
+                    const int s = i % kCount, k = n * kDepth;
+                    if (!(ok = barrier_wait(freed(s), (i / kCount & 1) ^ 1))) break;
+                    barrier_expect(full(s), S::kBytes);
+                    const uint32_t l = stages + s * S::kBytes, r = l + 2 * S::kLeftTerm;
+                    const int column = at.column + S::kRight * rank;
+    #pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        copy_box(l + t * S::kLeftTerm, &left_map, k, at.row + kM * rank, 2 * at.worker + t, full(s));
+                        if (!kFlip)
+                            copy_box(r + t * S::kRightTerm, &right_map, k, column, 2 * at.worker + t, full(s));
+                        else
+    #pragma unroll
+                            for (int p = 0; p < S::kRight / 64; ++p)
+                                copy_box(r + t * S::kRightTerm + p * kDepth * 128, &right_map, column + 64 * p, k,
+                                         2 * at.worker + t, full(s));
+                    }
+                }
+            }
+            // nothing is left in flight: no copy, and no arrival that the last stages' products still send to this CTA
+            for (int j = max(0, i - kCount); j < i; ++j)
+                if (!barrier_wait(full(j % kCount), j / kCount & 1) || !barrier_wait(freed(j % kCount), j / kCount & 1)) break;
         }
-        // nothing is left in flight: no copy, and no arrival that the last stages' products still send to this CTA
-        for (int j = max(0, i - kCount); j < i; ++j)
-            if (!barrier_wait(full(j % kCount), j / kCount & 1) || !barrier_wait(freed(j % kCount), j / kCount & 1)) break;
     }
     __syncwarp();
     __syncthreads();
@@ -344,37 +417,42 @@ __global__ void __launch_bounds__(256) relay_orthogonalise_norm_kernel(Update u,
     }
 }
 
-// kHeld / (|u| + eps), by all threads of a CTA; NaN where |u| is no number.
-__device__ double start_factor(const float* sums, int parts, float eps, double* shared) {
-    if (threadIdx.x == 0) {
-        double s[3] = {};
-        for (int p = 0; p < parts; ++p)
-            for (int e = 0; e < 3; ++e) s[e] += sums[(static_cast<int64_t>(blockIdx.y) * parts + p) * 3 + e];
-        const double length = sqrt(s[0] + s[1] * 0x1p160 + s[2] * 0x1p-160), over = length + eps;
-        *shared = !(length < 1e300) ? __longlong_as_double(0x7fffffffffffffffll) : over > 0.0 ? kHeld / over : 0.0;
+// kHeld / (|u| + eps), by all threads of a CTA of 256; NaN where |u| is no number.
+__device__ double start_factor(const float* sums, int parts, float eps) {
+    __shared__ double shared[8];
+    double v = 0.0;  // a thread adds a part at most
+    if (static_cast<int>(threadIdx.x) < parts) {
+        const float* s = sums + (static_cast<int64_t>(blockIdx.y) * parts + threadIdx.x) * 3;
+        v = s[0] + s[1] * 0x1p160 + s[2] * 0x1p-160;
     }
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
     __syncthreads();
-    return *shared;
+    v = 0.0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += shared[w];
+    const double length = sqrt(v), over = length + eps;
+    return !(length < 1e300) ? __longlong_as_double(0x7fffffffffffffffll) : over > 0.0 ? kHeld / over : 0.0;
 }
+static_assert(kParts <= 256, "a thread a part");
 
 // v f, also where f itself is past fp32 (lengths below 2^-115).
 __device__ __forceinline__ float times(float v, double f) {
     return f < 1e38 ? v * static_cast<float>(f) : static_cast<float>(v * f);
 }
 
-// x = u f as terms, [n][kTerms][rows][pitch]: a warp takes strips of 256 columns.
-template <int kTerms>
+// x = u f as two terms, [n][2][rows][pitch]: a warp takes strips of 256 columns.
 __global__ void __launch_bounds__(256)
 relay_orthogonalise_start_kernel(Update u, const float* sums, int parts, float eps, __half* x, int pitch) {
-    __shared__ double shared;
     __shared__ __align__(16) float turns[8][kStrip];
     let_next_start();
     wait_for_previous();
-    const double f = start_factor(sums, parts, eps, &shared);
+    const double f = start_factor(sums, parts, eps);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, strips = (u.columns + kStrip - 1) / kStrip;
     const float* from = u.p + blockIdx.y * u.worker_stride;
     const int64_t plane = static_cast<int64_t>(u.rows) * pitch, all = static_cast<int64_t>(u.rows) * strips;
-    __half* to = x + static_cast<int64_t>(blockIdx.y) * kTerms * plane;
+    __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + warp; i < all; i += static_cast<int64_t>(gridDim.x) * 8) {
         const int64_t row = i / strips;
         const int base = static_cast<int>(i - row * strips) * kStrip;
@@ -383,27 +461,23 @@ relay_orthogonalise_start_kernel(Update u, const float* sums, int parts, float e
         to_octets(v, lane, turns[warp]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = times(v[k], f);
+        store_strip<kVector>(to + row * pitch + base, lane, pitch - base, v);
 #pragma unroll
-        for (int t = 0; t < kTerms; ++t) {
-            store_strip<kVector>(to + t * plane + row * pitch + base, lane, pitch - base, v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
-        }
+        for (int k = 0; k < 8; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
+        store_strip<kVector>(to + plane + row * pitch + base, lane, pitch - base, v);
     }
 }
 
-// The same of the transpose, x [n][kTerms][columns][pitch]: a CTA takes squares of 64 x 64.
-template <int kTerms>
+// The same of the transpose, x [n][2][columns][pitch]: a CTA takes squares of 64 x 64.
 __global__ void __launch_bounds__(256)
 relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float eps, __half* x, int pitch) {
-    __shared__ double shared;
     __shared__ float square[64][65];
     let_next_start();
     wait_for_previous();
-    const double f = start_factor(sums, parts, eps, &shared);
+    const double f = start_factor(sums, parts, eps);
     const float* from = u.p + blockIdx.y * u.worker_stride;
     const int64_t plane = static_cast<int64_t>(u.columns) * pitch;
-    __half* to = x + static_cast<int64_t>(blockIdx.y) * kTerms * plane;
+    __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
     const int across = (u.columns + 63) / 64, all = (u.rows + 63) / 64 * across, lead = threadIdx.x / 64, at = threadIdx.x % 64;
     for (int i = blockIdx.x; i < all; i += gridDim.x) {
         const int row = i / across * 64, column = i % across * 64;
@@ -415,10 +489,10 @@ relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float ep
 #pragma unroll 4
         for (int c = lead; c < 64; c += 4) {
             if (column + c >= u.columns || row + at >= u.rows) continue;
-            __half term[kTerms];
-            split(times(square[at][c], f), term);
-#pragma unroll
-            for (int t = 0; t < kTerms; ++t) to[t * plane + static_cast<int64_t>(column + c) * pitch + row + at] = term[t];
+            __half hi, lo;
+            split(times(square[at][c], f), hi, lo);
+            __half* out = to + static_cast<int64_t>(column + c) * pitch + row + at;
+            out[0] = hi, out[plane] = lo;
         }
     }
 }
@@ -427,10 +501,10 @@ relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float ep
 
 int pitch_to(int64_t columns) { return static_cast<int>((columns + 15) / 16 * 16); }  // 32 bytes
 
-// `terms` terms of n matrices for boxes of 64 columns x `high` rows.
-bool map_terms(CUtensorMap* map, const __half* p, int64_t n, int terms, int64_t rows, int64_t columns, int high) {
+// Two terms of n matrices for boxes of 64 columns x `high` rows.
+bool map_terms(CUtensorMap* map, const __half* p, int64_t n, int64_t rows, int64_t columns, int high) {
     const cuuint64_t pitch = static_cast<cuuint64_t>(pitch_to(columns)) * 2;
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(columns), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(terms * n)};
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(columns), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(2 * n)};
     const cuuint64_t strides[2] = {pitch, pitch * static_cast<cuuint64_t>(rows)};
     const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(high), 1}, steps[3] = {1, 1, 1};
     return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(p), dims, strides, box, steps,
@@ -463,14 +537,14 @@ int64_t tile_count(int64_t n, int64_t rows, int64_t columns, int high, int wide,
     return n * tiles;
 }
 
-template <typename S, bool kFlip, int kTerms>
+template <typename S, bool kFlip>
 int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t stream) {
-    constexpr auto kernel = relay_orthogonalise_kernel<S, kFlip, kTerms>;
+    constexpr auto kernel = relay_orthogonalise_kernel<S, kFlip>;
     if (!allow_shared<kernel>(S::kShared)) return RELAY_ECUDA;
     CUtensorMap left_map, right_map;
-    if (!map_terms(&left_map, left, a.n, a.left_terms, a.rows, a.depth, kM) ||
-        !(kFlip ? map_terms(&right_map, right, a.n, a.right_terms, a.depth, a.columns, kDepth)
-                : map_terms(&right_map, right, a.n, a.right_terms, a.columns, a.depth, S::kRight)))
+    if (!map_terms(&left_map, left, a.n, a.rows, a.depth, kM) ||
+        !(kFlip ? map_terms(&right_map, right, a.n, a.depth, a.columns, kDepth)
+                : map_terms(&right_map, right, a.n, a.columns, a.depth, S::kRight)))
         return RELAY_ECUDA;
     a.tiles_m = (a.rows + S::kHigh - 1) / S::kHigh;
     a.tiles_n = (a.columns + S::kN - 1) / S::kN;
@@ -483,7 +557,7 @@ int launch(ProductArgs a, const __half* left, const __half* right, cudaStream_t 
 }
 
 // The shape that should take the least time: rounds of tiles, a stage's time and a tile's.
-template <bool kFlip, int kTerms>
+template <bool kFlip>
 int launch(const ProductArgs& a, const __half* left, const __half* right, cudaStream_t stream) {
     const double stages = static_cast<double>((a.depth + kDepth - 1) / kDepth);
     const auto us = [&](int ctas, int wide, double stage, double tile) {
@@ -491,21 +565,21 @@ int launch(const ProductArgs& a, const __half* left, const __half* right, cudaSt
         return static_cast<double>((tile_count(a.n, a.rows, a.columns, kM * ctas, wide, kFlip) + most - 1) / most) * (stage * stages + tile);
     };
     const double big = us(2, 256, 0.85, 4.0), middle = us(2, 128, 0.5, 3.0), small = us(1, 64, 0.35, 2.0);
-    if (small <= middle && small <= big) return launch<Shape<1, 64>, kFlip, kTerms>(a, left, right, stream);
-    if (middle <= big) return launch<Shape<2, 128>, kFlip, kTerms>(a, left, right, stream);
-    return launch<Shape<2, 256>, kFlip, kTerms>(a, left, right, stream);
+    if (small <= middle && small <= big) return launch<Shape<1, 64>, kFlip>(a, left, right, stream);
+    if (middle <= big) return launch<Shape<2, 128>, kFlip>(a, left, right, stream);
+    return launch<Shape<2, 256>, kFlip>(a, left, right, stream);
 }
 
-// What x is rounded by goes on with a x, and is multiplied by a in every step along small
-// singular values, where the products have little part.  So x is held in a third term, which
-// only that addition reads, where sums are too short to be off by more.
-int terms_of(int64_t m) { return m <= 448 ? 3 : 2; }
+// Stages that the tensor cores sum before the sums are added up in registers: 36 additions, or
+// with one stage (its small products first) 4 of the large ones, where m is small: the
+// cut is to one side and shows where sums are short otherwise.
+int group_of(int64_t m) { return m <= 448 ? 1 : 3; }
 
 // Where the workspace's parts begin, in bytes.
 struct Parts {
     int64_t x, g, p, sums, size;
     Parts(int64_t n, int64_t m, int64_t k) {
-        const int64_t wide = 2 * terms_of(m) * n * m * pitch_to(k), square = 4 * n * m * pitch_to(m);
+        const int64_t wide = 4 * n * m * pitch_to(k), square = 4 * n * m * pitch_to(m);
         x = 0, g = 2 * wide, p = g + square, sums = p + square, size = sums + 12 * n * kParts;
     }
 };
@@ -516,13 +590,12 @@ int check_matrices(int32_t n, int64_t rows, int64_t columns) {
     return RELAY_OK;
 }
 
-template <int kTerms>
 int launch_start(const Update& u, bool tall, const float* sums, int parts, float eps, __half* x, int pitch, int32_t n,
                  cudaStream_t stream) {
     const int64_t ctas = tall ? ((u.rows + 63) / 64) * static_cast<int64_t>((u.columns + 63) / 64)
                               : (u.rows * static_cast<int64_t>((u.columns + kStrip - 1) / kStrip) + 7) / 8;
     const dim3 grid(static_cast<unsigned>(ctas < 1024 ? ctas : 1024), static_cast<unsigned>(n));
-    return launch_early(tall ? relay_orthogonalise_turn_kernel<kTerms> : relay_orthogonalise_start_kernel<kTerms>, grid, 256, 0, 1,
+    return launch_early(tall ? relay_orthogonalise_turn_kernel : relay_orthogonalise_start_kernel, grid, 256, 0, 1,
                         stream, u, sums, parts, eps, x, pitch);
 }
 
@@ -552,7 +625,6 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
 
     const bool tall = rows > columns;
     const int64_t m = tall ? columns : rows, k = tall ? rows : columns;
-    const int terms = terms_of(m);
     const Parts parts(n, m, k);
     char* base = static_cast<char*>(workspace);
     __half* x[2] = {reinterpret_cast<__half*>(base), reinterpret_cast<__half*>(base + parts.g / 2)};
@@ -564,28 +636,26 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
     const int cut = static_cast<int>(want < kParts ? want : kParts);
     relay_orthogonalise_norm_kernel<<<dim3(static_cast<unsigned>(cut), static_cast<unsigned>(n)), 256, 0, stream>>>(u, sums);
     if (const int rc = status_of_launch()) return rc;
-    if (const int rc = terms == 3 ? launch_start<3>(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream)
-                                  : launch_start<2>(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream))
-        return rc;
+    if (const int rc = launch_start(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream)) return rc;
 
     for (int step = 0; step < steps; ++step) {
         const __half* now = x[step & 1];
         ProductArgs a{};
         a.n = n, a.rows = static_cast<int32_t>(m);
         a.columns = static_cast<int32_t>(m), a.depth = static_cast<int32_t>(k), a.pitch = pitch_to(m);
-        a.alpha = 1.0f / kHeld, a.out = g, a.left_terms = a.right_terms = terms;
-        if (const int rc = launch<false, 2>(a, now, now, stream)) return rc;
+        a.alpha = 1.0f / kHeld, a.out = g, a.group = group_of(m);
+        if (const int rc = launch<false>(a, now, now, stream)) return rc;
         a.depth = static_cast<int32_t>(m);
-        a.alpha = kC / kHeld, a.beta = kB, a.c = g, a.out = p, a.left_terms = a.right_terms = 2;
-        if (const int rc = launch<false, 2>(a, g, g, stream)) return rc;
+        a.alpha = kC / kHeld, a.beta = kB, a.c = g, a.out = p;
+        if (const int rc = launch<false>(a, g, g, stream)) return rc;
         a.columns = static_cast<int32_t>(k), a.pitch = pitch_to(k);
-        a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1], a.right_terms = terms;
+        a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1];
         if (step == steps - 1) {
             a.scale = a.alpha * (scale / kHeld);
             a.out = nullptr, a.final = out, a.worker_stride = n > 1 ? out_worker_stride : 0;
             a.row_stride = tall ? 1 : out_row_stride, a.column_stride = tall ? out_row_stride : 1;
         }
-        if (const int rc = terms == 3 ? launch<true, 3>(a, p, now, stream) : launch<true, 2>(a, p, now, stream)) return rc;
+        if (const int rc = launch<true>(a, p, now, stream)) return rc;
     }
     return RELAY_OK;
 }
