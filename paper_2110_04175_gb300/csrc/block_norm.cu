@@ -169,6 +169,18 @@ __device__ __forceinline__ void bring_weights(float* to, const Weight& post, con
             to[e * R::kWide + k] = k >= d ? 0.0f : from[e]->p == nullptr ? 1.0f : from[e]->p[worker * from[e]->stride + k];
 }
 
+// What the copies of a row leave out of its place in shared memory, 0 from the start, so that
+// rows are read without asking whether there is any: features past d, and inputs that are
+// not there (bit e of `absent`).
+template <typename R>
+__device__ __forceinline__ void clear_rest(uint8_t* ring, int bytes, uint32_t absent, int inputs) {
+    for (int slot = 0; slot < R::kRows / R::kRow; ++slot) {
+        const int first = absent >> slot % inputs & 1 ? 0 : bytes;
+        for (int at = first + 4 * static_cast<int>(threadIdx.x); at < R::kRow; at += 128 * R::kWarps)
+            *reinterpret_cast<uint32_t*>(ring + slot * R::kRow + at) = 0;
+    }
+}
+
 // Weight number e at feature `at`, from there or, in the widest rows, from memory.
 template <typename R>
 __device__ __forceinline__ void weight_at(const float* weights, int e, const Weight& w, int worker, int at, bool on, Pair (&v)[2]) {
@@ -226,10 +238,11 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
     if (threadIdx.x < R::kGroups * R::kStages) barrier_init(shared_address(&bars[0][0] + threadIdx.x), 1);
     barriers_ready();
     if (R::kWeights) bring_weights<R>(weights, a.post, a.pre, a.scale, worker, a.d);
+    const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
+    clear_rest<R>(ring, static_cast<int>(bytes), gated ? 0u : 1u << 2, 3);
     __syncthreads();
 
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
-    const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
     const bool brings = part == 0 && elected();
     uint8_t* mine = ring + group * (R::kStages * R::kStage);
     const auto bring = [&](int token, int s) {  // one thread of the group
@@ -255,7 +268,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
 #pragma unroll
         for (int j = 0; j < R::kHold; ++j) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
-            load_quad(from + at, at < a.d, h[j]);
+            load_quad(from + at, true, h[j]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) squares = fma(h[j][k], h[j][k], squares);
         }
@@ -268,8 +281,8 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             const bool on = at < a.d;
             Pair w[2], rho[2], z[2], r[2];
-            load_quad(from + kNext + at, on, r);
-            if (gated) load_quad(from + 2 * kNext + at, on, z);
+            load_quad(from + kNext + at, true, r);
+            if (gated) load_quad(from + 2 * kNext + at, true, z);
             weight_at<R>(weights, 0, a.post, worker, at, on, w);
             weight_at<R>(weights, 2, a.scale, worker, at, on, rho);
 #pragma unroll
@@ -520,10 +533,11 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
     if (threadIdx.x < R::kGroups * R::kStages) barrier_init(shared_address(&bars[0][0] + threadIdx.x), 1);
     barriers_ready();
     if (R::kWeights) bring_weights<R>(weights, a.post, a.pre, a.scale, worker, a.d);
+    const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
+    clear_rest<R>(ring, static_cast<int>(bytes), (gated ? 0u : 1u << 3) | (over_too ? 0u : 1u << 4), 5);
     __syncthreads();
 
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
-    const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
     const bool brings = part == 0 && elected();
     uint8_t* mine = ring + group * (R::kStages * R::kStage);
     const auto bring = [&](int token, int s) {  // one thread of the group
@@ -560,11 +574,11 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
             const bool on = at < a.d;
             const T* from = reinterpret_cast<const T*>(mine + s * R::kStage) + at;
             constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
-            load_quad(from, on, o.xhat);
-            load_quad(from + kNext, on, o.r);
-            load_quad(from + 2 * kNext, on, u);
-            if (gated) load_quad(from + 3 * kNext, on, o.p);
-            load_quad(from + 4 * kNext, on && over_too, over);
+            load_quad(from, true, o.xhat);
+            load_quad(from + kNext, true, o.r);
+            load_quad(from + 2 * kNext, true, u);
+            if (gated) load_quad(from + 3 * kNext, true, o.p);
+            load_quad(from + 4 * kNext, true, over);
             weight_at<R>(weights, 0, a.post, worker, at, on, w);
             weight_at<R>(weights, 1, a.pre, worker, at, on, pre);
             weight_at<R>(weights, 2, a.scale, worker, at, on, rho);

@@ -369,7 +369,7 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
 
 // ------------------------------------------------------------------- the start
 
-constexpr int kParts = 128;  // CTAs that sum a matrix's squares, at most
+constexpr int kParts = 512;  // CTAs that sum a matrix's squares, at most
 
 struct Update {
     const float* p;
@@ -417,29 +417,32 @@ __global__ void __launch_bounds__(256) relay_orthogonalise_norm_kernel(Update u,
     }
 }
 
-// kHeld / (|u| + eps), by all threads of a CTA of 256; NaN where |u| is no number.
-__device__ double start_factor(const float* sums, int parts, float eps) {
-    __shared__ double shared[8];
-    double v = 0.0;  // a thread adds a part at most
-    if (static_cast<int>(threadIdx.x) < parts) {
-        const float* s = sums + (static_cast<int64_t>(blockIdx.y) * parts + threadIdx.x) * 3;
-        v = s[0] + s[1] * 0x1p160 + s[2] * 0x1p-160;
-    }
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = 0.0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) v += shared[w];
-    const double length = sqrt(v), over = length + eps;
-    return !(length < 1e300) ? __longlong_as_double(0x7fffffffffffffffll) : over > 0.0 ? kHeld / over : 0.0;
-}
-static_assert(kParts <= 256, "a thread a part");
+// kHeld / (|u| + eps), called by all threads of a CTA; NaN where |u| is no number.  One warp adds
+// the parts and one thread takes the root: 64-bit arithmetic is slow here (with every thread at
+// it this took 180 us of a 268 MB start).
+struct Factor {
+    float lift, near;  // a power of two, 1 but where fp32 does not hold the factor (lengths below 2^-115)
+    __device__ __forceinline__ float times(float v) const { return v * lift * near; }
+};
 
-// v f, also where f itself is past fp32 (lengths below 2^-115).
-__device__ __forceinline__ float times(float v, double f) {
-    return f < 1e38 ? v * static_cast<float>(f) : static_cast<float>(v * f);
+__device__ Factor start_factor(const float* sums, int parts, float eps) {
+    __shared__ Factor shared;
+    if (threadIdx.x < 32) {
+        double v = 0.0;
+        for (int p = threadIdx.x; p < parts; p += 32) {
+            const float* s = sums + (static_cast<int64_t>(blockIdx.y) * parts + p) * 3;
+            v += s[0] + s[1] * 0x1p160 + s[2] * 0x1p-160;
+        }
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+        if (threadIdx.x == 0) {
+            const double length = sqrt(v), over = length + eps, f = over > 0.0 ? kHeld / over : 0.0;
+            const double lift = f < 1e38 ? 1.0 : 0x1p64;
+            shared = Factor{static_cast<float>(lift), length < 1e300 ? static_cast<float>(f / lift) : __int_as_float(0x7fffffff)};
+        }
+    }
+    __syncthreads();
+    return shared;
 }
 
 // x = u f as two terms, [n][2][rows][pitch]: a warp takes strips of 256 columns.
@@ -448,7 +451,7 @@ relay_orthogonalise_start_kernel(Update u, const float* sums, int parts, float e
     __shared__ __align__(16) float turns[8][kStrip];
     let_next_start();
     wait_for_previous();
-    const double f = start_factor(sums, parts, eps);
+    const Factor f = start_factor(sums, parts, eps);
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, strips = (u.columns + kStrip - 1) / kStrip;
     const float* from = u.p + blockIdx.y * u.worker_stride;
     const int64_t plane = static_cast<int64_t>(u.rows) * pitch, all = static_cast<int64_t>(u.rows) * strips;
@@ -460,7 +463,7 @@ relay_orthogonalise_start_kernel(Update u, const float* sums, int parts, float e
         load_strip<kDirect>(from + row * u.row_stride + base, lane, u.columns - base, v);
         to_octets(v, lane, turns[warp]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = times(v[k], f);
+        for (int k = 0; k < 8; ++k) v[k] = f.times(v[k]);
         store_strip<kVector>(to + row * pitch + base, lane, pitch - base, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
@@ -474,7 +477,7 @@ relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float ep
     __shared__ float square[64][65];
     let_next_start();
     wait_for_previous();
-    const double f = start_factor(sums, parts, eps);
+    const Factor f = start_factor(sums, parts, eps);
     const float* from = u.p + blockIdx.y * u.worker_stride;
     const int64_t plane = static_cast<int64_t>(u.columns) * pitch;
     __half* to = x + static_cast<int64_t>(blockIdx.y) * 2 * plane;
@@ -490,7 +493,7 @@ relay_orthogonalise_turn_kernel(Update u, const float* sums, int parts, float ep
         for (int c = lead; c < 64; c += 4) {
             if (column + c >= u.columns || row + at >= u.rows) continue;
             __half hi, lo;
-            split(times(square[at][c], f), hi, lo);
+            split(f.times(square[at][c]), hi, lo);
             __half* out = to + static_cast<int64_t>(column + c) * pitch + row + at;
             out[0] = hi, out[plane] = lo;
         }
@@ -594,7 +597,8 @@ int launch_start(const Update& u, bool tall, const float* sums, int parts, float
                  cudaStream_t stream) {
     const int64_t ctas = tall ? ((u.rows + 63) / 64) * static_cast<int64_t>((u.columns + 63) / 64)
                               : (u.rows * static_cast<int64_t>((u.columns + kStrip - 1) / kStrip) + 7) / 8;
-    const dim3 grid(static_cast<unsigned>(ctas < 1024 ? ctas : 1024), static_cast<unsigned>(n));
+    const int64_t most = 8 * kSms > n ? 8 * kSms / n : 1;
+    const dim3 grid(static_cast<unsigned>(ctas < most ? ctas : most), static_cast<unsigned>(n));
     return launch_early(tall ? relay_orthogonalise_turn_kernel : relay_orthogonalise_start_kernel, grid, 256, 0, 1,
                         stream, u, sums, parts, eps, x, pitch);
 }
@@ -632,8 +636,10 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
     float* sums = reinterpret_cast<float*>(base + parts.sums);
     const Update u{update, n > 1 ? worker_stride : 0, rows > 1 ? row_stride : 0, static_cast<int32_t>(rows),
                    static_cast<int32_t>(columns)};
-    const int64_t warps = rows * ((columns + kStrip - 1) / kStrip), want = (warps + 31) / 32;
-    const int cut = static_cast<int>(want < kParts ? want : kParts);
+    // two strips a warp at least, eight CTAs per SM at most
+    const int64_t warps = rows * ((columns + kStrip - 1) / kStrip), want = (warps + 15) / 16;
+    const int64_t fit = 8 * kSms / n < 1 ? 1 : 8 * kSms / n < kParts ? 8 * kSms / n : kParts;
+    const int cut = static_cast<int>(want < fit ? want : fit);
     relay_orthogonalise_norm_kernel<<<dim3(static_cast<unsigned>(cut), static_cast<unsigned>(n)), 256, 0, stream>>>(u, sums);
     if (const int rc = status_of_launch()) return rc;
     if (const int rc = launch_start(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream)) return rc;
