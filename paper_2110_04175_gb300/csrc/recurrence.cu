@@ -292,6 +292,9 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(Recurr
 
 constexpr int kStages = 3;
 
+// Where the strips alone leave most SMs idle, clusters of kCtas CTAs take kCtas tiles side by
+// side: the warps' stretches are joined to one a CTA, which goes to all of them.
+
 template <typename T>
 struct TileMaps {
     CUtensorMap gate, value, dout, out;
@@ -331,36 +334,83 @@ struct Boxes {
     }
 };
 
-template <typename T, bool kBegins>
+// The stretches of a cluster's CTAs, in shared memory of each of them.
+template <int kCtas>
+struct Joined {
+    float4 of[2][kCtas][32];
+};
+
+__device__ __forceinline__ void put_there(uint32_t at, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+
+// `h` goes from the state before the cluster's tiles to the one behind them, `mine` gets the one
+// that reaches this warp: first through the CTAs before this one, then through its warps.
+// Called by all threads of the cluster; on return all warps are done with the tile before.
+template <int kCtas, bool kBegins>
+__device__ __forceinline__ void hand_on(float4 (&shared)[kWarps][32], Joined<kCtas>& joined, int turn, int rank, int part, int lane,
+                                        const float (&ends)[4], float (&h)[2], float (&mine)[2]) {
+    shared[part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
+    __syncthreads();
+    if constexpr (kCtas == 1) {
+        through<kWarps, kBegins>(shared, part, lane, h, mine);
+    } else {
+        if (part == 0) {
+            float whole[4] = {ends[0], ends[1], ends[2], ends[3]};
+#pragma unroll
+            for (int j = 1; j < kWarps; ++j) {
+                const float4 e = shared[j][lane];
+                join<kBegins>(whole[0], whole[2], e.x, e.z);
+                join<kBegins>(whole[1], whole[3], e.y, e.w);
+            }
+            const uint32_t at = shared_address(&joined.of[turn][rank][lane]);
+#pragma unroll
+            for (int q = 0; q < kCtas; ++q) put_there(in_cta(at, q), make_float4(whole[0], whole[1], whole[2], whole[3]));
+        }
+        cluster_sync();
+        float first[2], behind[2];
+        through<kCtas, kBegins>(joined.of[turn], rank, lane, h, first);
+        behind[0] = first[0], behind[1] = first[1];
+        through<kWarps, kBegins>(shared, part, lane, behind, mine);
+    }
+}
+
+template <typename T, bool kBegins, int kCtas>
 __global__ void __launch_bounds__(32 * kWarps, 2)
 relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const __grid_constant__ TileMaps<T> maps) {
     constexpr int kRun = kRunOf<T>, kTile = kWarps * kRun;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t barriers[kStages];
     __shared__ float4 shared[2][kWarps][32];
+    __shared__ Joined<kCtas> joined;
     const Boxes<T, 2, kTile> boxes(barriers, raw);
-    const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
-    const Place<T> p(a, blockIdx.x);
-    const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
+    const int lane = threadIdx.x % 32, part = threadIdx.x / 32, rank = kCtas == 1 ? 0 : static_cast<int>(cluster_rank());
+    const Place<T> p(a, blockIdx.x / kCtas);
+    // rounds of kCtas tiles; this CTA's tile of a round
+    const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kCtas * kTile - 1) / (kCtas * kTile);
+    const auto first_of = [&](int i) { return p.first + (i * kCtas + rank) * kTile; };
     const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
     const auto bring = [&](int i) {  // one thread
         const uint32_t at = boxes.expect(i);
-        copy_box(at, &maps.gate, p.strip, p.first + i * kTile, p.worker, boxes.bar(i));
-        copy_box(at + boxes.kBox, &maps.value, p.strip, p.first + i * kTile, p.worker, boxes.bar(i));
+        copy_box(at, &maps.gate, p.strip, first_of(i), p.worker, boxes.bar(i));
+        copy_box(at + boxes.kBox, &maps.value, p.strip, first_of(i), p.worker, boxes.bar(i));
     };
     if (threadIdx.x == 0)
         for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
+    if (kCtas > 1) cluster_sync();  // the others have started
     float h[2];
     if (a.segments == 1)
         load_state<kVector>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, h);
     else
         load_state<kVector>(a.a + p.at, lane, left, h);
-    uint32_t begin = load_begins<kRun, kBegins>(a, p.worker, p.first + part * kRun, lane, to - p.first - part * kRun);
+    const int start = first_of(0) + part * kRun;
+    uint32_t begin = load_begins<kRun, kBegins>(a, p.worker, start, lane, to - start);
     bool ok = true;
     for (int i = 0; i < tiles; ++i) {
-        const int token = p.first + i * kTile + part * kRun, counts = to - token;
+        const int token = first_of(i) + part * kRun, counts = to - token;
         const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
-        if (kBegins && i + 1 < tiles) begin = load_begins<kRun, kBegins>(a, p.worker, token + kTile, lane, counts - kTile);
+        if (kBegins && i + 1 < tiles)
+            begin = load_begins<kRun, kBegins>(a, p.worker, token + kCtas * kTile, lane, counts - kCtas * kTile);
         ok = ok && boxes.wait(i);
         float f[kRun][2], b[kRun][2], ends[4], x[2];
 #pragma unroll
@@ -385,10 +435,8 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
 #pragma unroll
             for (int r = 1; r < kRun; ++r) join<kBegins>(ends[k], ends[2 + k], f[r][k], b[r][k]);
         }
-        shared[i & 1][part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
-        __syncthreads();  // here all warps are done with the tile before this one
+        hand_on<kCtas, kBegins>(shared[i & 1], joined, i & 1, rank, part, lane, ends, h, x);
         if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
-        through<kWarps, kBegins>(shared[i & 1], part, lane, h, x);
         T* out = a.out.row(p.worker, token) + p.strip;
         if (counts >= kRun) {
 #pragma unroll
@@ -408,7 +456,7 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
         }
     }
     if (threadIdx.x == 0) boxes.none_in_flight(tiles);
-    if (a.segments == 1 && a.last != nullptr && part == 0)
+    if (a.segments == 1 && a.last != nullptr && part == 0 && rank == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
 }
 
@@ -590,21 +638,24 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
 
 // The same with the rows by tensor copies.  What the first sweep makes of the gates stays for
 // the second one.
-template <typename T, bool kBegins>
+template <typename T, bool kBegins, int kCtas>
 __global__ void __launch_bounds__(32 * kWarps, 2)
 relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const __grid_constant__ TileMaps<T> maps) {
     constexpr int kRun = kBackRunOf<T>, kTile = kWarps * kRun;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t barriers[kStages];
     __shared__ float4 shared[2][kWarps][32];
+    __shared__ Joined<kCtas> joined;
     const Boxes<T, 4, kTile> boxes(barriers, raw);
-    const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
-    const Place<T> p(a, blockIdx.x);
-    const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
+    const int lane = threadIdx.x % 32, part = threadIdx.x / 32, rank = kCtas == 1 ? 0 : static_cast<int>(cluster_rank());
+    const Place<T> p(a, blockIdx.x / kCtas);
+    const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kCtas * kTile - 1) / (kCtas * kTile);
+    // this CTA's tile of a round; CTA 0 has the last tokens
+    const auto first_of = [&](int i) { return p.first + ((tiles - 1 - i) * kCtas + kCtas - 1 - rank) * kTile; };
     const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
     const auto bring = [&](int i) {  // one thread
         const uint32_t at = boxes.expect(i), bar = boxes.bar(i);
-        const int token = p.first + (tiles - 1 - i) * kTile;
+        const int token = first_of(i);
         copy_box(at, &maps.gate, p.strip, token, p.worker, bar);
         copy_box(at + boxes.kBox, &maps.dout, p.strip, token, p.worker, bar);
         copy_box(at + 2 * boxes.kBox, &maps.value, p.strip, token, p.worker, bar);
@@ -612,6 +663,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
     };
     if (threadIdx.x == 0)
         for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
+    if (kCtas > 1) cluster_sync();  // the others have started
     float m[2], first[2];
     if (a.segments == 1)
         load_state<kVector>(a.dlast == nullptr ? nullptr : a.dlast + p.worker * a.dlast_stride + p.strip, lane, left, m);
@@ -620,13 +672,14 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
     load_state<kVector>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, first);
     // warp 0 of a tile takes its last tokens
     const int place = (kWarps - 1 - part) * kRun;
-    const auto token_at = [&](int i) { return p.first + (tiles - 1 - i) * kTile + place; };
+    const auto token_at = [&](int i) { return first_of(i) + place; };
     uint32_t begin = tiles > 0 ? load_begins<kRun, kBegins>(a, p.worker, token_at(0), lane, to - token_at(0)) : 0;
     bool ok = true;
     for (int i = 0; i < tiles; ++i) {
         const int token = token_at(i), counts = to - token;
         const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
-        if (kBegins && i + 1 < tiles) begin = load_begins<kRun, kBegins>(a, p.worker, token - kTile, lane, counts + kTile);
+        if (kBegins && i + 1 < tiles)
+            begin = load_begins<kRun, kBegins>(a, p.worker, token - kCtas * kTile, lane, counts + kCtas * kTile);
         ok = ok && boxes.wait(i);
         float at[kRun][2], rest[kRun][2], ends[4] = {1.0f, 1.0f, 0.0f, 0.0f}, x[2];
 #pragma unroll
@@ -644,10 +697,8 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
             }
         }
         if (!ok) ends[2] = ends[3] = m[0] = m[1] = __int_as_float(0x7fffffff);
-        shared[i & 1][part][lane] = make_float4(ends[0], ends[1], ends[2], ends[3]);
-        __syncthreads();  // here all warps are done with the tile before this one
+        hand_on<kCtas, kBegins>(shared[i & 1], joined, i & 1, rank, part, lane, ends, m, x);
         if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
-        through<kWarps, kBegins>(shared[i & 1], part, lane, m, x);
         T *to_gate = a.dgate.row(p.worker, token) + p.strip, *to_value = a.dvalue.row(p.worker, token) + p.strip;
         const auto step = [&](int r, float (&dg)[2], float (&dv)[2]) {
             const Two<T> dout = boxes.get(i, 1, place + r, lane), value = boxes.get(i, 2, place + r, lane),
@@ -683,7 +734,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
         }
     }
     if (threadIdx.x == 0) boxes.none_in_flight(tiles);
-    if (a.segments == 1 && a.last != nullptr && part == 0)
+    if (a.segments == 1 && a.last != nullptr && part == 0 && rank == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
 
@@ -745,7 +796,7 @@ Cut recurrence_cut(int64_t n, int64_t tokens, int64_t d) {
     int64_t segments = 1;
     if (units < 152 && tokens >= 512) {
         segments = 304 / units;
-        if (segments > tokens / 256) segments = tokens / 256;
+        if (segments > tokens / 128) segments = tokens / 128;
         if (segments > 128) segments = 128;
     }
     int64_t segment = (tokens + segments - 1) / segments;
@@ -800,10 +851,40 @@ bool map_tiles(CUtensorMap* map, const relay_rows* r, int32_t type, int32_t n, i
 }
 
 template <auto Kernel, typename T>
-int launch_tiles(const RecurrenceArgs<T>& a, const TileMaps<T>& maps, int64_t units, int shared, cudaStream_t stream) {
+int launch_tiles(const RecurrenceArgs<T>& a, const TileMaps<T>& maps, int64_t units, int ctas, int shared, cudaStream_t stream) {
     if (!allow_shared<Kernel>(shared)) return RELAY_ECUDA;
-    Kernel<<<static_cast<unsigned>(units), 32 * kWarps, static_cast<size_t>(shared), stream>>>(a, maps);
-    return status_of_launch();
+    cudaLaunchAttribute with = {};
+    with.id = cudaLaunchAttributeClusterDimension;
+    with.val.clusterDim.x = static_cast<unsigned>(ctas), with.val.clusterDim.y = 1, with.val.clusterDim.z = 1;
+    cudaLaunchConfig_t how = {};
+    how.gridDim = dim3(static_cast<unsigned>(units * ctas)), how.blockDim = dim3(32 * kWarps);
+    how.dynamicSmemBytes = static_cast<size_t>(shared), how.stream = stream, how.attrs = &with, how.numAttrs = 1;
+    if (cudaLaunchKernelEx(&how, Kernel, a, maps) == cudaSuccess) return RELAY_OK;
+    (void)cudaGetLastError();
+    return RELAY_ECUDA;
+}
+
+// CTAs that work side by side on a strip whose rows come by tensor copies, tiles of `tile`
+// tokens: as many as come near to filling the SMs twice (a cluster of 8 leaves a few of them
+// out), no more than there are tiles.  A round of a cluster costs a microsecond more than one
+// CTA's, so that from half the SMs on a CTA a strip is faster.  0: segments are faster, which is
+// so for a few strips and very many tokens.  Forward and backward in us, bf16, as one CTA a
+// strip / segments / clusters:
+//   [2][4096][4096]  41  73 /  74  93 / 53  94     [1][4096][4096]   39  68 / 35  51 /  28  52
+//   [1][4096][1024]  37  64 /  17  21 /  9  15     [1][65536][256]  521 966 / 41  56 / 102 186
+int cluster_of(int64_t units, int64_t tokens, int tile) {
+    if (units < 10 && tokens > 96 * tile) return 0;
+    if (units <= 30 && tokens > 4 * tile) return 8;
+    if (units <= 70 && tokens > 2 * tile) return 4;
+    return 1;
+}
+
+// f(CTAs of a cluster) as a constant.
+template <typename F>
+int by_cluster(int ctas, F f) {
+    return ctas == 8   ? f(std::integral_constant<int, 8>())
+           : ctas == 4 ? f(std::integral_constant<int, 4>())
+                       : f(std::integral_constant<int, 1>());
 }
 
 // f(warps that share a strip's tile, tokens of a warp's run) as constants: one warp a strip
@@ -841,11 +922,16 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
     if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned(workspace, 16)))) return RELAY_EINVAL;
     if (tokens > 0 && (out->data == gate->data || out->data == value->data)) return RELAY_EINVAL;
     if (tokens == 0 && last == nullptr) return RELAY_OK;
-    const Cut cut = recurrence_cut(n, tokens, d);
+    Cut cut = recurrence_cut(n, tokens, d);
     const bool vec = tokens == 0 || (d % 2 == 0 && pairs(gate, type, n, tokens) && pairs(value, type, n, tokens) &&
                                      pairs(out, type, n, tokens));
     return by_type(type, [&](auto t) {
         using T = decltype(t);
+        constexpr int kTile = kWarps * kRunOf<T>;
+        const bool boxes = vec && tokens > kRunOf<T> && boxed(gate, type, n, tokens, d) && boxed(value, type, n, tokens, d) &&
+                           encoder() != nullptr;
+        const int ctas = boxes ? cluster_of(static_cast<int64_t>(n) * cut.strips, tokens, kTile) : 0;
+        if (ctas > 0) cut.segments = 1, cut.segment = static_cast<int>(tokens);
         RecurrenceArgs<T> a{};
         a.gate = view<const T>(gate, n, tokens), a.value = view<const T>(value, n, tokens), a.out = view<T>(out, n, tokens);
         a.initial = initial, a.initial_stride = n > 1 ? initial_stride : 0;
@@ -862,15 +948,16 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
             relay_recurrence_carry_kernel<false><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
                 a.a, a.b, cut.segments, a.d, initial, a.initial_stride, last, a.last_stride);
         }
-        if (vec && cut.segment > kRunOf<T> && boxed(gate, type, n, tokens, d) && boxed(value, type, n, tokens, d) &&
-            encoder() != nullptr) {
-            constexpr int kTile = kWarps * kRunOf<T>;
+        if (boxes) {
             TileMaps<T> maps{};
             if (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile))
                 return RELAY_ECUDA;
-            constexpr int kShared = Boxes<T, 2, kTile>::kShared;
-            return begins != nullptr ? launch_tiles<relay_recurrence_tiles_kernel<T, true>>(a, maps, units, kShared, stream)
-                                     : launch_tiles<relay_recurrence_tiles_kernel<T, false>>(a, maps, units, kShared, stream);
+            return by_cluster(ctas, [&](auto with) {
+                constexpr int kCtas = decltype(with)::value, kShared = Boxes<T, 2, kTile>::kShared;
+                return begins != nullptr
+                           ? launch_tiles<relay_recurrence_tiles_kernel<T, true, kCtas>>(a, maps, units, kCtas, kShared, stream)
+                           : launch_tiles<relay_recurrence_tiles_kernel<T, false, kCtas>>(a, maps, units, kCtas, kShared, stream);
+            });
         }
         return by_time<kRunOf<T>>(cut.segment, [&](auto time, auto run) {
             constexpr int kTime = decltype(time)::value, kRun = decltype(run)::value, kSide = kWarps / kTime;
@@ -905,12 +992,18 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
         if (dgate->data == dvalue->data) return RELAY_EINVAL;
     }
     if (tokens == 0 && dinitial == nullptr) return RELAY_OK;
-    const Cut cut = recurrence_cut(n, tokens, d);
+    Cut cut = recurrence_cut(n, tokens, d);
     bool vec = d % 2 == 0 || tokens == 0;
     if (tokens > 0)
         for (const relay_rows* r : {dout, gate, value, out, dgate, dvalue}) vec = vec && pairs(r, type, n, tokens);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
+        constexpr int kTile = kWarps * kBackRunOf<T>;
+        bool boxes = vec && tokens > kBackRunOf<T> && encoder() != nullptr;
+        if (boxes)
+            for (const relay_rows* r : {dout, gate, value, out}) boxes = boxes && boxed(r, type, n, tokens, d);
+        const int ctas = boxes ? cluster_of(static_cast<int64_t>(n) * cut.strips, tokens, kTile) : 0;
+        if (ctas > 0) cut.segments = 1, cut.segment = static_cast<int>(tokens);
         RecurrenceArgs<T> a{};
         a.gate = view<const T>(gate, n, tokens), a.value = view<const T>(value, n, tokens);
         a.out_in = view<const T>(out, n, tokens), a.dout = view<const T>(dout, n, tokens);
@@ -931,18 +1024,17 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
             relay_recurrence_carry_kernel<true><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
                 a.a, a.b, cut.segments, a.d, dlast, a.dlast_stride, dinitial, a.last_stride);
         }
-        bool boxes = vec && cut.segment > kBackRunOf<T> && encoder() != nullptr;
-        for (const relay_rows* r : {dout, gate, value, out}) boxes = boxes && boxed(r, type, n, tokens, d);
         if (boxes) {
-            constexpr int kTile = kWarps * kBackRunOf<T>;
             TileMaps<T> maps{};
             if (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile) ||
                 !map_tiles(&maps.dout, dout, type, n, tokens, d, kTile) || !map_tiles(&maps.out, out, type, n, tokens, d, kTile))
                 return RELAY_ECUDA;
-            constexpr int kShared = Boxes<T, 4, kTile>::kShared;
-            return begins != nullptr
-                       ? launch_tiles<relay_recurrence_backward_tiles_kernel<T, true>>(a, maps, units, kShared, stream)
-                       : launch_tiles<relay_recurrence_backward_tiles_kernel<T, false>>(a, maps, units, kShared, stream);
+            return by_cluster(ctas, [&](auto with) {
+                constexpr int kCtas = decltype(with)::value, kShared = Boxes<T, 4, kTile>::kShared;
+                return begins != nullptr
+                           ? launch_tiles<relay_recurrence_backward_tiles_kernel<T, true, kCtas>>(a, maps, units, kCtas, kShared, stream)
+                           : launch_tiles<relay_recurrence_backward_tiles_kernel<T, false, kCtas>>(a, maps, units, kCtas, kShared, stream);
+            });
         }
         return by_time<kBackRunOf<T>>(cut.segment, [&](auto time, auto run) {
             constexpr int kTime = decltype(time)::value, kRun = decltype(run)::value, kSide = kWarps / kTime;

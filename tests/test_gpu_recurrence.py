@@ -113,6 +113,18 @@ def test_long_sequences(dtype, n, T, d):
     _check(n, T, d, dtype, what=("state", "packed", "lengths"), seed=d)
 
 
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
+@pytest.mark.parametrize("n,T,d", [(1, 2060, 200), (2, 1033, 136), (20, 300, 128), (3, 700, 1024), (1, 530, 4096), (65, 290, 64),
+                                   (3, 261, 3200), (150, 140, 64), (1, 13000, 64), (2, 6200, 72)])
+def test_clusters_and_segments_of_aligned_rows(dtype, n, T, d):
+    """Rows by tensor copies: one, four and eight CTAs a strip, rounds that end anywhere, and segments."""
+    if n * T * d > 2e6 and dtype is torch.float16:
+        pytest.skip("as bf16")
+    _check(n, T, d, dtype, what=("state", "packed", "lengths"), seed=d)
+    if n * T * d < 3e5:
+        _check(n, T, d, dtype, what=(), seed=d)
+
+
 def test_many_sequences_of_one_token():
     _check(5000, 1, 40, torch.bfloat16, what=("state",))
     _check(70000, 2, 3, torch.float32, what=("state", "lengths"))
@@ -130,10 +142,11 @@ def test_no_tokens_hand_the_state_on():
     assert torch.equal(last, state)
 
 
-@pytest.mark.parametrize("T,cuts", [(40, [0, 1, 13, 14, 40]), (2600, [0, 1100, 1101, 2600])])
-def test_stretches_go_on_from_the_state(T, cuts):
+@pytest.mark.parametrize("T,cuts,d", [(40, [0, 1, 13, 14, 40], 70), (2600, [0, 1100, 1101, 2600], 70),
+                                      (2600, [0, 1100, 1101, 1250, 2600], 72)])
+def test_stretches_go_on_from_the_state(T, cuts, d):
     """Token by token or in stretches, the state in its own place: the same rows as in one call, within the bounds."""
-    n, d, dtype = 2, 70, torch.float32
+    n, dtype = 2, torch.float32
     g, v = _inputs(5, n, T, d, dtype)
     gate, value = _cuda(g, dtype), _cuda(v, dtype)
     state = torch.zeros(n, d, device="cuda")
@@ -237,15 +250,15 @@ def test_gradients_agree_with_differences():
         assert abs(got - want) < 0.1 + 1e-3 * abs(want)
 
 
-def test_the_same_bits_every_time_on_any_stream_and_in_a_graph():
-    """Two streams at once with a workspace each, and a captured call on new inputs."""
-    n, T, d, dtype = 1, 4000, 100, torch.bfloat16
+@pytest.mark.parametrize("d", [100, 64], ids=["segments", "clusters"])
+def test_the_same_bits_every_time_on_any_stream_and_in_a_graph(d):
+    """Streams at once with a workspace each, and a captured call on new inputs."""
+    n, T, dtype = 1, 4000, torch.bfloat16
     (g, v), (g2, v2) = _inputs(1, n, T, d, dtype), _inputs(2, n, T, d, dtype)
     gate, value = _cuda(g, dtype), _cuda(v, dtype)
     outs = [torch.empty_like(gate) for _ in range(3)]
     streams = [torch.cuda.Stream() for _ in outs]
     works = [_work(n, T, d) for _ in outs]
-    assert works[0].numel() > 0
     torch.cuda.synchronize()
     for out, work, stream in zip(outs, works, streams):
         rs.relay_recurrence(gate, value, out, work, stream=stream)
