@@ -124,6 +124,139 @@ struct Turn {
     }
 };
 
+// What an adder's 32 rows x kColumns are, one row a lane, and the way between them and memory.  `rows`
+// and `columns`: how many there are from the first on.
+
+// Memory's order: kPieces lanes a row; whether piece p of a lane is there.
+template <int kPieces>
+__device__ __forceinline__ bool piece_of(int p, int lane, int rows, int columns, int& r, int& q) {
+    r = (p * 32 + lane) / kPieces, q = (p * 32 + lane) % kPieces;
+    return r < rows && 8 * q < columns;
+}
+
+template <int kColumns>
+constexpr int kChunkOf = kColumns < 64 ? kColumns : 64;  // columns that go through `turn` together
+
+// sum = start (hi + lo) of what lies at c and c + plane.
+template <int kColumns>
+__device__ __forceinline__ void bring_added(float (&sum)[kColumns], const Turn& turn, const __half* c, int64_t plane, int pitch,
+                                            int rows, int columns, float start, int lane) {
+    constexpr int kChunk = kChunkOf<kColumns>, kPieces = kChunk / 8;
+#pragma unroll
+    for (int j = 0; j < kColumns; j += kChunk) {
+        uint4 part[2][kPieces];
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            int r, q;
+            const bool there = piece_of<kPieces>(p, lane, rows, columns - j, r, q);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                part[t][p] = there ? *reinterpret_cast<const uint4*>(c + t * plane + static_cast<int64_t>(r) * pitch + j + 8 * q)
+                                   : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            __syncwarp();
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) turn.put((p * 32 + lane) / kPieces, (p * 32 + lane) % kPieces, part[t][p]);
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) {
+                const uint4 v = turn.get(lane, q);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float& to = sum[j + 8 * q + e];
+                    const float part_of = __half2float(reinterpret_cast<const __half*>(&v)[e]);
+                    to = t == 0 ? part_of : start * (to + part_of);
+                }
+            }
+        }
+    }
+}
+
+// 8 numbers as the term `t` of two.
+__device__ __forceinline__ uint4 term_of(const float* v, int t) {
+    uint4 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        __half hi, lo;
+        split(v[e], hi, lo);
+        reinterpret_cast<__half*>(&w)[e] = t == 0 ? hi : lo;
+    }
+    return w;
+}
+
+// The terms of `sum` to out and out + plane; `mirror`: their place above the diagonal, at the lane's
+// row, or NULL.
+template <int kColumns>
+__device__ __forceinline__ void put_terms(const float (&sum)[kColumns], const Turn& turn, __half* out, int64_t plane, int pitch,
+                                          int rows, int columns, __half* mirror, int lane) {
+    constexpr int kChunk = kChunkOf<kColumns>, kPieces = kChunk / 8;
+#pragma unroll
+    for (int j = 0; j < kColumns; j += kChunk) {
+        if (j >= columns) break;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) {
+                const uint4 v = term_of(sum + j + 8 * q, t);
+                turn.put(lane, q, v);
+                if (mirror != nullptr && lane < rows) {
+                    __half* over = mirror + t * plane + static_cast<int64_t>(j + 8 * q) * pitch;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (j + 8 * q + e < columns) over[e * pitch] = reinterpret_cast<const __half*>(&v)[e];
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                int r, q;
+                if (piece_of<kPieces>(p, lane, rows, columns - j, r, q))
+                    *reinterpret_cast<uint4*>(out + t * plane + static_cast<int64_t>(r) * pitch + j + 8 * q) = turn.get(r, q);
+            }
+        }
+    }
+}
+
+// `sum` in fp32: element (i, j) at to + i row_stride + j column_stride, one of them 1.
+template <int kColumns>
+__device__ __forceinline__ void put_final(const float (&sum)[kColumns], const Turn& turn, float* to, int64_t row_stride,
+                                          int64_t column_stride, int rows, int columns, int lane) {
+    if (column_stride == 1) {
+#pragma unroll
+        for (int j = 0; j < kColumns; j += 32) {
+            if (j >= columns) break;
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                turn.put(lane, q, make_uint4(__float_as_uint(sum[j + 4 * q]), __float_as_uint(sum[j + 4 * q + 1]),
+                                             __float_as_uint(sum[j + 4 * q + 2]), __float_as_uint(sum[j + 4 * q + 3])));
+            __syncwarp();
+            if (j + lane < columns)
+#pragma unroll 8
+                for (int r = 0; r < min(32, rows); ++r) to[r * row_stride + j + lane] = turn.number(r, lane);
+        }
+    } else if (lane < rows) {
+#pragma unroll
+        for (int j = 0; j < kColumns; ++j)
+            if (j < columns) to[lane * row_stride + j * column_stride] = sum[j];
+    }
+}
+
+// Adds an accumulator's part to the warp's sums.
+template <int kColumns>
+__device__ __forceinline__ void add_accumulator(float (&sum)[kColumns], uint32_t from) {
+#pragma unroll
+    for (int c = 0; c < kColumns; c += 16) {
+        float v[16];
+        tensor_load(from + c, v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[c + e] += v[e];
+    }
+}
+
 // out = alpha (left right) + beta c.  left [n][2][rows][depth]; right [n][2][columns][depth], or with kFlip
 // [n][2][depth][columns].  A wait that runs out ends a pair's work, and its results from there on are
 // NaN.
@@ -171,7 +304,7 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
 
     if (warp < kAdders) {
         if constexpr (kN == 256) more_registers<kAdderRegisters>();
-        constexpr int kColumns = kN / 2, kChunk = kColumns < 64 ? kColumns : 64, kPieces = kChunk / 8;
+        constexpr int kColumns = kN / 2;
         const int row = 32 * (warp % 4), column = kColumns * (warp / 4);  // of the CTA's 128 x kN
         const int64_t plane = static_cast<int64_t>(a.rows) * a.pitch;
         const Turn turn{turns + static_cast<uint32_t>(warp) * kTurn};
@@ -179,60 +312,16 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
         int group = 0;  // of all that the pair has summed
         for (int tile = pair; tile < a.tiles; tile += pairs) {
             const Tile<S, kFlip> at(a, tile);
-            const int i0 = at.row + kM * rank + row, j0 = at.column + column;
-            const int64_t base = static_cast<int64_t>(at.worker) * 2 * plane + static_cast<int64_t>(i0) * a.pitch + j0;
-            // piece p of a lane as memory is read and written: kPieces lanes a row
-            const auto place = [&](int c, int p, int& r, int& q) {
-                r = (p * 32 + lane) / kPieces, q = (p * 32 + lane) % kPieces;
-                return i0 + r < a.rows && j0 + c + 8 * q < a.columns;
-            };
+            const int i0 = at.row + kM * rank + row, j0 = at.column + column, rows = a.rows - i0, columns = a.columns - j0;
+            const int64_t first = static_cast<int64_t>(at.worker) * 2 * plane, base = first + static_cast<int64_t>(i0) * a.pitch + j0;
             // beta c is where the sum starts, so that it comes while the tensor cores are at work
             float sum[kColumns] = {};
-            if (a.c != nullptr) {
-                const float start = a.beta / a.alpha;
-#pragma unroll
-                for (int c = 0; c < kColumns; c += kChunk) {
-                    uint4 part[2][kPieces];
-#pragma unroll
-                    for (int p = 0; p < kPieces; ++p) {
-                        int r, q;
-                        const bool there = place(c, p, r, q);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            part[t][p] = there ? *reinterpret_cast<const uint4*>(a.c + base + t * plane + static_cast<int64_t>(r) * a.pitch + c + 8 * q)
-                                               : make_uint4(0, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        __syncwarp();
-#pragma unroll
-                        for (int p = 0; p < kPieces; ++p) turn.put((p * 32 + lane) / kPieces, (p * 32 + lane) % kPieces, part[t][p]);
-                        __syncwarp();
-#pragma unroll
-                        for (int q = 0; q < kPieces; ++q) {
-                            const uint4 v = turn.get(lane, q);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                float& to = sum[c + 8 * q + e];
-                                const float part_of = __half2float(reinterpret_cast<const __half*>(&v)[e]);
-                                to = t == 0 ? part_of : start * (to + part_of);
-                            }
-                        }
-                    }
-                }
-            }
+            if (a.c != nullptr) bring_added(sum, turn, a.c + base, plane, a.pitch, rows, columns, a.beta / a.alpha, lane);
             for (int done = 0; done < count && ok; done += a.group, ++group) {
                 const int b = group & 1;
                 if (!(ok = barrier_wait_warp(summed(b), group >> 1 & 1))) break;
                 tensor_fence_after();
-                const uint32_t from = tensor + (static_cast<uint32_t>(row) << 16) + b * kN + column;
-#pragma unroll
-                for (int c = 0; c < kColumns; c += 16) {
-                    float v[16];
-                    tensor_load(from + c, v);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sum[c + e] += v[e];
-                }
+                add_accumulator(sum, tensor + (static_cast<uint32_t>(row) << 16) + b * kN + column);
                 tensor_fence_before();
                 __syncwarp();
                 if (lane == 0) barrier_arrive(read(b));
@@ -240,62 +329,12 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
             const float factor = !ok ? __int_as_float(0x7fffffff) : a.out != nullptr ? a.alpha : a.scale;
 #pragma unroll
             for (int e = 0; e < kColumns; ++e) sum[e] *= factor;
-            if (a.out != nullptr) {
-#pragma unroll
-                for (int c = 0; c < kColumns; c += kChunk) {
-                    if (j0 + c >= a.columns) break;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        __syncwarp();
-#pragma unroll
-                        for (int q = 0; q < kPieces; ++q) {
-                            uint4 v;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                __half hi, lo;
-                                split(sum[c + 8 * q + e], hi, lo);
-                                reinterpret_cast<__half*>(&v)[e] = t == 0 ? hi : lo;
-                            }
-                            turn.put(lane, q, v);
-                            if (!kFlip && at.mirror && i0 + lane < a.rows) {  // its place above the diagonal
-                                const int j = j0 + c + 8 * q;
-                                __half* over = a.out + (static_cast<int64_t>(at.worker) * 2 + t) * plane + static_cast<int64_t>(j) * a.pitch + i0 + lane;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (j + e < a.columns) over[e * a.pitch] = reinterpret_cast<const __half*>(&v)[e];
-                            }
-                        }
-                        __syncwarp();
-#pragma unroll
-                        for (int p = 0; p < kPieces; ++p) {
-                            int r, q;
-                            if (place(c, p, r, q))
-                                *reinterpret_cast<uint4*>(a.out + base + t * plane + static_cast<int64_t>(r) * a.pitch + c + 8 * q) = turn.get(r, q);
-                        }
-                    }
-                }
-            } else if (a.column_stride == 1) {
-#pragma unroll
-                for (int c = 0; c < kColumns; c += 32) {
-                    if (j0 + c >= a.columns) break;
-                    __syncwarp();
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        turn.put(lane, q, make_uint4(__float_as_uint(sum[c + 4 * q]), __float_as_uint(sum[c + 4 * q + 1]),
-                                                     __float_as_uint(sum[c + 4 * q + 2]), __float_as_uint(sum[c + 4 * q + 3])));
-                    __syncwarp();
-                    float* to = a.final + at.worker * a.worker_stride + i0 * a.row_stride + j0 + c + lane;
-                    const int rows = min(32, a.rows - i0);
-                    if (j0 + c + lane < a.columns)
-#pragma unroll 8
-                        for (int r = 0; r < rows; ++r) to[r * a.row_stride] = turn.number(r, lane);
-                }
-            } else if (i0 + lane < a.rows) {
-                float* to = a.final + at.worker * a.worker_stride + (i0 + lane) * a.row_stride + j0 * a.column_stride;
-#pragma unroll
-                for (int e = 0; e < kColumns; ++e)
-                    if (j0 + e < a.columns) to[e * a.column_stride] = sum[e];
-            }
+            if (a.out != nullptr)
+                put_terms(sum, turn, a.out + base, plane, a.pitch, rows, columns,
+                          !kFlip && at.mirror ? a.out + first + static_cast<int64_t>(j0) * a.pitch + i0 + lane : nullptr, lane);
+            else
+                put_final(sum, turn, a.final + at.worker * a.worker_stride + i0 * a.row_stride + j0 * a.column_stride, a.row_stride,
+                          a.column_stride, rows, columns, lane);
         }
     } else {
         if constexpr (kN == 256) fewer_registers<kOtherRegisters>();
@@ -365,6 +404,189 @@ relay_orthogonalise_kernel(const __grid_constant__ ProductArgs a, const __grid_c
     __syncthreads();
     if (kCtas == 2) cluster_sync();  // the other CTA is done with this one's memory too
     if (warp == kIssuer) tensor_free<2 * kN, kCtas>(tensor);
+}
+
+// ------------------------------------------------------------------ a whole step
+//
+// Matrices of up to 128 rows: g is one tile, so each CTA makes it for itself, and b g + c g g from
+// it without leaving the SM (the adders write both as operands to shared memory), and then its
+// columns of x.  One launch a step instead of three, while the CTAs of all matrices run at once.
+
+template <int kN>
+struct Whole {
+    static constexpr int kTerm = kM * 128, kStage = 2 * kTerm, kSlice = 2 * kN * 128;  // bytes: of 64 along the summed axis
+    static constexpr int kCount = 4, kOperand = 4 * kTerm;  // stages; b g + c g g: two terms of two panels of 64 columns
+    static constexpr int kShared = kCount * kStage + kOperand + kAdders * kTurn + 1024 + 256;
+    static_assert(kSlice <= kStage && kShared <= 232448, "shared memory of a CTA");
+};
+
+struct StepArgs {
+    const __half* x;  // [n][2][rows][pitch]
+    __half* out;      // the same shape, or NULL, and
+    float* final;     // as in ProductArgs
+    int64_t worker_stride, row_stride, column_stride;
+    float scale;
+    int32_t rows, columns, pitch, slices;
+};
+
+template <int kN>
+__global__ void __launch_bounds__(kThreads, 1)
+relay_orthogonalise_step_kernel(const __grid_constant__ StepArgs a, const __grid_constant__ CUtensorMap rows_map,
+                                const __grid_constant__ CUtensorMap slice_map) {
+    using W = Whole<kN>;
+    constexpr int kCount = W::kCount;
+    constexpr uint32_t kSquare = 1u << 4 | uint32_t(128 / 8) << 17 | uint32_t(kM / 16) << 24;
+    constexpr uint32_t kLast = 1u << 4 | 1u << 16 | uint32_t(kN / 8) << 17 | uint32_t(kM / 16) << 24;
+    extern __shared__ uint8_t raw[];
+    const uint32_t stages = (shared_address(raw) + 1023u) & ~1023u, operand_at = stages + kCount * W::kStage;
+    const uint32_t turns = operand_at + W::kOperand, bars = turns + kAdders * kTurn;
+    const auto full = [&](int s) { return bars + 8 * s; };
+    const auto freed = [&](int s) { return bars + 8 * (kCount + s); };
+    const auto summed = [&](int b) { return bars + 8 * (2 * kCount + b); };
+    const auto read = [&](int b) { return bars + 8 * (2 * kCount + 2 + b); };
+    const uint32_t ready = bars + 8 * (2 * kCount + 4), tensor_at = ready + 8;
+
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x / 32), 0), lane = threadIdx.x % 32;
+    const int worker = blockIdx.x / a.slices, slice = (blockIdx.x % a.slices) * kN;
+    const int count = (a.columns + kDepth - 1) / kDepth, panels = (a.rows + kDepth - 1) / kDepth;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kCount; ++s) {
+            barrier_init(full(s), 1);
+            barrier_init(freed(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            barrier_init(summed(b), 1);
+            barrier_init(read(b), kAdders);
+        }
+        barrier_init(ready, kAdders);
+        barriers_ready();
+    }
+    if (warp == kIssuer) tensor_alloc<256, 1>(tensor_at);
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    uint32_t tensor;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
+    let_next_start();
+    wait_for_previous();
+
+    if (warp < kAdders) {
+        const int row = 32 * (warp % 4), half = warp / 4;
+        const int64_t plane = static_cast<int64_t>(a.rows) * a.pitch;
+        const Turn turn{turns + static_cast<uint32_t>(warp) * kTurn};
+        bool ok = true;
+        int group = 0;
+        const auto sums = [&](auto& sum, int groups, int column) {
+            for (int n = 0; n < groups && ok; ++n, ++group) {
+                const int b = group & 1;
+                if (!(ok = barrier_wait_warp(summed(b), group >> 1 & 1))) break;
+                tensor_fence_after();
+                add_accumulator(sum, tensor + (static_cast<uint32_t>(row) << 16) + b * 128 + column);
+                tensor_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(read(b));
+            }
+        };
+        // 64 columns of the lane's row as a panel of the operand
+        const auto to_operand = [&](const float (&v)[64]) {
+            const Turn panel{operand_at + half * W::kTerm};
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                panel.put(row + lane, q, term_of(v + 8 * q, 0));
+                Turn{panel.at + 2 * W::kTerm}.put(row + lane, q, term_of(v + 8 * q, 1));
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(ready);
+        };
+        float g[64] = {};
+        sums(g, count, 64 * half);
+#pragma unroll
+        for (int e = 0; e < 64; ++e) g[e] *= 1.0f / kHeld;
+        to_operand(g);
+#pragma unroll
+        for (int e = 0; e < 64; ++e) g[e] *= kB * kHeld / kC;  // where the sum starts
+        sums(g, panels, 64 * half);
+#pragma unroll
+        for (int e = 0; e < 64; ++e) g[e] *= kC / kHeld;
+        to_operand(g);
+        constexpr int kColumns = kN / 2;
+        const int j0 = slice + kColumns * half, rows = a.rows - row, columns = a.columns - j0;
+        const int64_t base = static_cast<int64_t>(worker) * 2 * plane + static_cast<int64_t>(row) * a.pitch + j0;
+        float sum[kColumns];
+        bring_added(sum, turn, a.x + base, plane, a.pitch, rows, columns, kA * kHeld, lane);
+        sums(sum, panels, kColumns * half);
+        const float factor = !ok ? __int_as_float(0x7fffffff) : a.out != nullptr ? 1.0f / kHeld : a.scale;
+#pragma unroll
+        for (int e = 0; e < kColumns; ++e) sum[e] *= factor;
+        if (a.out != nullptr)
+            put_terms(sum, turn, a.out + base, plane, a.pitch, rows, columns, static_cast<__half*>(nullptr), lane);
+        else
+            put_final(sum, turn, a.final + worker * a.worker_stride + row * a.row_stride + j0 * a.column_stride, a.row_stride,
+                      a.column_stride, rows, columns, lane);
+    } else if (warp == kIssuer) {
+        int group = 0;
+        bool ok = true;
+        // one group: 64 along the summed axis, terms at `l` and l + lo_l, `r` and r + lo_r
+        const auto multiply = [&](uint32_t l, uint32_t lo_l, uint32_t r, uint32_t lo_r, bool flip, int stage) {
+            tensor_fence_after();
+            if (elected()) {
+#pragma unroll
+                for (int t = 0; t < 3; ++t)  // lo hi, hi lo, hi hi: the small ones first
+#pragma unroll
+                    for (int k = 0; k < kDepth / 16; ++k) {
+                        const uint32_t at_r = r + (t == 1 ? lo_r : 0);
+                        const uint64_t x = operand_k(l + (t == 0 ? lo_l : 0)) + 2 * k;
+                        const uint64_t y = flip ? operand(at_r, kDepth * 128, 1024) + 128 * k : operand_k(at_r) + 2 * k;
+                        product<1>(tensor + (group & 1) * 128, x, y, flip ? kLast : kSquare, t + k > 0);
+                    }
+                if (stage >= 0) products_arrive<1>(freed(stage));
+                products_arrive<1>(summed(group & 1));
+            }
+            __syncwarp();
+            ++group;
+        };
+        const auto accumulator = [&] { return group <= 1 || barrier_wait_warp(read(group & 1), (group >> 1 & 1) ^ 1); };
+        for (int i = 0; i < count && ok; ++i) {
+            const uint32_t at = stages + i % kCount * W::kStage;
+            if ((ok = accumulator() && barrier_wait_warp(full(i % kCount), i / kCount & 1))) multiply(at, W::kTerm, at, W::kTerm, false, i % kCount);
+        }
+        ok = ok && barrier_wait_warp(ready, 0);
+        for (int p = 0; p < panels && ok; ++p) {
+            const uint32_t at = operand_at + p * W::kTerm;
+            if ((ok = accumulator())) multiply(at, 2 * W::kTerm, at, 2 * W::kTerm, false, -1);
+        }
+        ok = ok && barrier_wait_warp(ready, 1);
+        for (int p = 0; p < panels && ok; ++p) {
+            const int i = count + p, s = i % kCount;
+            if ((ok = accumulator() && barrier_wait_warp(full(s), i / kCount & 1)))
+                multiply(operand_at + p * W::kTerm, 2 * W::kTerm, stages + s * W::kStage, W::kSlice / 2, true, s);
+        }
+    } else if (warp == kLoader && elected()) {
+        int i = 0;
+        for (; i < count + panels; ++i) {
+            const int s = i % kCount;
+            const uint32_t at = stages + s * W::kStage;
+            if (!barrier_wait(freed(s), (i / kCount & 1) ^ 1)) break;
+            barrier_expect(full(s), i < count ? W::kStage : W::kSlice);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (i < count)
+                    copy_box(at + t * W::kTerm, &rows_map, i * kDepth, 0, 2 * worker + t, full(s));
+                else
+#pragma unroll
+                    for (int p = 0; p < kN / 64; ++p)
+                        copy_box(at + t * (W::kSlice / 2) + p * kDepth * 128, &slice_map, slice + 64 * p, (i - count) * kDepth,
+                                 2 * worker + t, full(s));
+            }
+        }
+        // nothing is left in flight: no copy, and no arrival of the last products
+        for (int j = max(0, i - kCount); j < i; ++j)
+            if (!barrier_wait(full(j % kCount), j / kCount & 1) || !barrier_wait(freed(j % kCount), j / kCount & 1)) break;
+    }
+    __syncwarp();
+    __syncthreads();
+    if (warp == kIssuer) tensor_free<256, 1>(tensor);
 }
 
 // ------------------------------------------------------------------- the start
@@ -575,6 +797,22 @@ int launch(const ProductArgs& a, const __half* left, const __half* right, cudaSt
     return launch<Shape<2, 256>, kFlip>(a, left, right, stream);
 }
 
+template <int kN>
+int launch_step(const StepArgs& a, int32_t n, cudaStream_t stream) {
+    constexpr auto kernel = relay_orthogonalise_step_kernel<kN>;
+    if (!allow_shared<kernel>(Whole<kN>::kShared)) return RELAY_ECUDA;
+    CUtensorMap rows_map, slice_map;
+    if (!map_terms(&rows_map, a.x, n, a.rows, a.columns, kM) || !map_terms(&slice_map, a.x, n, a.rows, a.columns, kDepth))
+        return RELAY_ECUDA;
+    return launch_early(kernel, dim3(static_cast<unsigned>(n * a.slices)), kThreads, Whole<kN>::kShared, 1, stream, a, rows_map, slice_map);
+}
+
+// Columns of a CTA where a step goes in one launch, 0 where it does not.
+int whole_step(int64_t n, int64_t m, int64_t k) {
+    if (m > kM) return 0;
+    return n * ((k + 63) / 64) <= kSms ? 64 : n * ((k + 127) / 128) <= kSms ? 128 : 0;
+}
+
 // Stages that the tensor cores sum before the sums are added up in registers: 36 additions, or
 // with one stage (its small products first) 4 of the large ones, where m is small: the
 // cut is to one side and shows where sums are short otherwise.
@@ -646,8 +884,23 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
     if (const int rc = status_of_launch()) return rc;
     if (const int rc = launch_start(u, tall, sums, cut, eps, x[0], pitch_to(k), n, stream)) return rc;
 
+    const int whole = whole_step(n, m, k);
     for (int step = 0; step < steps; ++step) {
         const __half* now = x[step & 1];
+        const bool last = step == steps - 1;
+        if (whole != 0) {
+            StepArgs a{};
+            a.x = now, a.rows = static_cast<int32_t>(m), a.columns = static_cast<int32_t>(k), a.pitch = pitch_to(k);
+            a.slices = static_cast<int32_t>((k + whole - 1) / whole);
+            if (last) {
+                a.final = out, a.worker_stride = n > 1 ? out_worker_stride : 0, a.scale = scale / (kHeld * kHeld);
+                a.row_stride = tall ? 1 : out_row_stride, a.column_stride = tall ? out_row_stride : 1;
+            } else {
+                a.out = x[(step & 1) ^ 1];
+            }
+            if (const int rc = whole == 64 ? launch_step<64>(a, n, stream) : launch_step<128>(a, n, stream)) return rc;
+            continue;
+        }
         ProductArgs a{};
         a.n = n, a.rows = static_cast<int32_t>(m);
         a.columns = static_cast<int32_t>(m), a.depth = static_cast<int32_t>(k), a.pitch = pitch_to(m);
@@ -658,7 +911,7 @@ int relay_orthogonalise(int32_t n, int64_t rows, int64_t columns, const float* u
         if (const int rc = launch<false>(a, g, g, stream)) return rc;
         a.columns = static_cast<int32_t>(k), a.pitch = pitch_to(k);
         a.alpha = 1.0f / kHeld, a.beta = kA, a.c = now, a.out = x[(step & 1) ^ 1];
-        if (step == steps - 1) {
+        if (last) {
             a.scale = a.alpha * (scale / kHeld);
             a.out = nullptr, a.final = out, a.worker_stride = n > 1 ? out_worker_stride : 0;
             a.row_stride = tall ? 1 : out_row_stride, a.column_stride = tall ? out_row_stride : 1;

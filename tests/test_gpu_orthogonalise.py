@@ -83,6 +83,15 @@ def test_shapes(rows, columns):
     _check(_matrices(rows, 2, rows, columns))
 
 
+@pytest.mark.parametrize("n,rows,columns", [(1, 128, 9728), (1, 128, 9729), (152, 64, 64), (153, 65, 64), (76, 100, 128), (3, 120, 3000),
+                                            (5, 129, 300), (1, 1, 5000), (38, 33, 257)])
+def test_up_to_128_rows(n, rows, columns):
+    """A step in one launch (in slices of 64 or 128 columns), and where that does not fit."""
+    _check(_matrices(n, n, rows, columns))
+    if n * rows * columns < 3e6:
+        _check(_matrices(n, n, columns, rows))
+
+
 @pytest.mark.parametrize("n", [1, 3, 5, 200, 256])
 def test_many_matrices(n):
     u = _matrices(n, n, 40, 72) * torch.exp(torch.arange(n, device="cuda") % 7 - 3.0)[:, None, None]
