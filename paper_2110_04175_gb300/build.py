@@ -20,11 +20,11 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "librelaysum.so")
 
 # (source, its own flags): the step kernels are built for up to 64 workers
-# (relaysum::kSmallN) and for up to 256 (relaysum::kMaxN)
+# (relaysum::kSmallN) and for up to 256 (relaysum::kMaxN), the step between blocks once per pass
 SOURCES = [("step_kernels.cu", ["-DRELAY_CAP=256", "-DRELAY_SPACE=large"]),
            ("step_kernels.cu", ["-DRELAY_CAP=64", "-DRELAY_SPACE=small"]),
-           ("relaysum.cu", []), ("layer_kernels.cu", []), ("weight_grad.cu", []), ("recurrence.cu", []), ("block_norm.cu", []),
-           ("orthogonalise.cu", []), ("program.cpp", []),
+           ("relaysum.cu", []), ("layer_kernels.cu", []), ("weight_grad.cu", []), ("recurrence.cu", []), ("orthogonalise.cu", []),
+           ("block_norm.cu", ["-DRELAY_PASS=1"]), ("block_norm.cu", ["-DRELAY_PASS=2"]), ("program.cpp", []),
            ("host_step.cpp", [])]
 HEADERS = [os.path.join(CSRC, h) for h in ("program.h", "handle.h", "device.cuh", "step_launch.h", "layers.cuh",
                                               "blackwell.cuh")] + [

@@ -6,9 +6,12 @@
 //
 // All rows in and all rows out once, two sums over a row between them, so memory bounds it.
 // kParts warps share a row, each with kStrips strips of 256 features (layers.cuh).
+#include <type_traits>
+
 #include "blackwell.cuh"
 #include "layers.cuh"
 
+// Compiled once per pass (RELAY_PASS: 1 forward, 2 backward), which halves the build's longest unit.
 namespace {
 
 struct Weight {  // fp32, from worker to worker
@@ -127,28 +130,26 @@ relay_block_norm_kernel(BlockArgs<T> a) {
 }
 
 // The 8-bit format of four features a lane, a block on eight lanes: layers.cuh's put_strip.
-__device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at, int lane, bool on, const Pair (&v)[2]) {
+__device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at, int lane, const Pair (&v)[2]) {
     const float e[4] = {v[0].v.x, v[0].v.y, v[1].v.x, v[1].v.y};
     uint32_t most = max(max(magnitude(e[0]), magnitude(e[1])), max(magnitude(e[2]), magnitude(e[3])));
 #pragma unroll
     for (int m = 1; m < 8; m *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, m));
     const uint32_t c = scale_byte(most);
-    if (!on) return;
     const uint32_t ab = __byte_perm(code_bits(e[0], c), code_bits(e[1], c), 0x0040);
     const uint32_t cd = __byte_perm(code_bits(e[2], c), code_bits(e[3], c), 0x0040);
     *reinterpret_cast<uint32_t*>(codes + at) = c == 255u ? 0u : __byte_perm(ab, cd, 0x5410);
     if (lane % 8 == 0) scales[at / kBlock] = static_cast<uint8_t>(c);
 }
 
-// Aligned rows of up to 8192 features in 16 bits and 4096 in 32, where there are some for
-// every group of kParts warps: they come by bulk copies to shared memory and h stays in
+// Many aligned rows of up to 8192 features (4096 in fp32): they come by bulk copies to shared memory and h stays in
 // registers.  The groups wait only for themselves; while one waits for its row or for one
 // of the two sums, others are at work.
 template <typename T, int kParts_, int kInputs>
 struct Ring {
     static constexpr int kParts = kParts_;
-    // the forward pass: 24 warps (12 in fp32) of 8 quads a lane, a row of each group at a time;
-    // the backward pass: 16 (8) of 4 quads, two rows of each group
+    // the forward pass: 24 warps of 8 quads a lane, a row of each group at a time; the backward
+    // pass: 16 (in fp32 8) of 4 quads, two rows of each group
     static constexpr bool kBack = kInputs == 5;
     static constexpr int kWarps = (kBack ? 16 : 24) / (sizeof(T) == 2 ? 1 : 2), kGroups = kWarps / kParts;
     static constexpr int kHold = kBack ? 4 : 8, kStages = kBack ? 2 : 1;
@@ -169,16 +170,13 @@ __device__ __forceinline__ void bring_weights(float* to, const Weight& post, con
             to[e * R::kWide + k] = k >= d ? 0.0f : from[e]->p == nullptr ? 1.0f : from[e]->p[worker * from[e]->stride + k];
 }
 
-// What the copies of a row leave out of its place in shared memory, 0 from the start, so that
-// rows are read without asking whether there is any: features past d, and inputs that are
-// not there (bit e of `absent`).
-template <typename R>
-__device__ __forceinline__ void clear_rest(uint8_t* ring, int bytes, uint32_t absent, int inputs) {
-    for (int slot = 0; slot < R::kRows / R::kRow; ++slot) {
-        const int first = absent >> slot % inputs & 1 ? 0 : bytes;
-        for (int at = first + 4 * static_cast<int>(threadIdx.x); at < R::kRow; at += 128 * R::kWarps)
-            *reinterpret_cast<uint32_t*>(ring + slot * R::kRow + at) = 0;
-    }
+// Features past d up to the next 128, which a row's copies leave out, are 0 from the start, so
+// that a warp reads its 128 without asking which are there.
+template <typename R, typename T>
+__device__ __forceinline__ void clear_rest(uint8_t* ring, int d) {
+    const int rest = (d + kQuads - 1) / kQuads * kQuads - d;
+    for (int at = threadIdx.x; at < R::kRows / R::kRow * rest; at += 32 * R::kWarps)
+        reinterpret_cast<T*>(ring + at / rest * R::kRow)[d + at % rest] = T(0.0f);
 }
 
 // Weight number e at feature `at`, from there or, in the widest rows, from memory.
@@ -223,8 +221,9 @@ __device__ __forceinline__ void none_in_flight(const uint64_t* bars, int stages,
         if (!barrier_wait(shared_address(bars + i % stages), i / stages & 1)) break;
 }
 
-// A wait that runs out makes a group's results from there on NaN.
-template <typename T, int kParts>
+// kWhole: every warp has all its quads.  A wait that runs out makes a group's results from there
+// on NaN.
+template <typename T, int kParts, bool kWhole>
 __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_block_norm_rows_kernel(BlockArgs<T> a) {
     using R = Ring<T, kParts, 3>;
     extern __shared__ uint8_t raw[];
@@ -239,7 +238,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
     barriers_ready();
     if (R::kWeights) bring_weights<R>(weights, a.post, a.pre, a.scale, worker, a.d);
     const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
-    clear_rest<R>(ring, static_cast<int>(bytes), gated ? 0u : 1u << 2, 3);
+    clear_rest<R, T>(ring, a.d);
     __syncthreads();
 
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
@@ -267,7 +266,8 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         Pair h[R::kHold][2], squares(0.0f);
 #pragma unroll
         for (int j = 0; j < R::kHold; ++j) {
-            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const int base = (part + kParts * j) * kQuads, at = base + 4 * lane;
+            if (!kWhole && base >= a.d) break;
             load_quad(from + at, true, h[j]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) squares = fma(h[j][k], h[j][k], squares);
@@ -278,8 +278,9 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         squares = Pair(0.0f);
 #pragma unroll
         for (int j = 0; j < R::kHold; ++j) {
-            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const int base = (part + kParts * j) * kQuads, at = base + 4 * lane;
             const bool on = at < a.d;
+            if (!kWhole && base >= a.d) break;
             Pair w[2], rho[2], z[2], r[2];
             load_quad(from + kNext + at, true, r);
             if (gated) load_quad(from + 2 * kNext + at, true, z);
@@ -304,14 +305,15 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         }
 #pragma unroll
         for (int j = 0; j < R::kHold; ++j) {
-            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const int base = (part + kParts * j) * kQuads, at = base + 4 * lane;
             const bool on = at < a.d;
+            if (!kWhole && base >= a.d) break;  // (the pitch ends with d's last 128)
             Pair w[2];
             if (a.total.p != nullptr) store_quad(a.total.row(worker, token) + at, on, h[j]);
             weight_at<R>(weights, 1, a.pre, worker, at, on, w);
 #pragma unroll
             for (int k = 0; k < 2; ++k) h[j][k] = h[j][k] * Pair(sh);
-            if (a.codes != nullptr) put_quad(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), at, lane, at < a.pitch, h[j]);
+            if (a.codes != nullptr) put_quad(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), at, lane, h[j]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) h[j][k] = h[j][k] * w[k];
             store_quad(a.y.row(worker, token) + at, on, h[j]);
@@ -517,8 +519,9 @@ relay_block_norm_backward_kernel(BlockBackwardArgs<T> a) {
 
 // The rows that the forward pass's kernel of bulk copies takes, here with two sweeps over a
 // row in shared memory, so that registers are left for the sums over the tokens.  The groups of a CTA take rows of their own and wait only for themselves.
-// A wait that runs out makes a group's results from there on NaN.
-template <typename T, int kParts>
+// kWhole: every warp has all its quads.  A wait that runs out makes a group's results from there
+// on NaN.
+template <typename T, int kParts, bool kWhole>
 __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_block_norm_backward_rows_kernel(BlockBackwardArgs<T> a) {
     using R = Ring<T, kParts, 5>;
     extern __shared__ uint8_t raw[];
@@ -534,7 +537,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
     barriers_ready();
     if (R::kWeights) bring_weights<R>(weights, a.post, a.pre, a.scale, worker, a.d);
     const uint32_t bytes = static_cast<uint32_t>(a.d) * sizeof(T);
-    clear_rest<R>(ring, static_cast<int>(bytes), (gated ? 0u : 1u << 3) | (over_too ? 0u : 1u << 4), 5);
+    clear_rest<R, T>(ring, a.d);
     __syncthreads();
 
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
@@ -578,7 +581,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
             load_quad(from + kNext, true, o.r);
             load_quad(from + 2 * kNext, true, u);
             if (gated) load_quad(from + 3 * kNext, true, o.p);
-            load_quad(from + 4 * kNext, true, over);
+            load_quad(from + 4 * kNext, over_too, over);
             weight_at<R>(weights, 0, a.post, worker, at, on, w);
             weight_at<R>(weights, 1, a.pre, worker, at, on, pre);
             weight_at<R>(weights, 2, a.scale, worker, at, on, rho);
@@ -587,6 +590,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
         Pair parts[3] = {Pair(0.0f), Pair(0.0f), Pair(0.0f)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            if (!kWhole && (part + kParts * j) * kQuads >= a.d) break;
             Features<T, 2> o;
             Pair w[2], rho[2], pre[2], u[2], over[2];
             remake(j, o, w, rho, pre, u, over);
@@ -601,8 +605,9 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
         const float along = three[0] * over_d, along_x = three[1] * over_d - sh * along * (three[2] * over_d);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int at = (part + kParts * j) * kQuads + 4 * lane;
+            const int base = (part + kParts * j) * kQuads, at = base + 4 * lane;
             const bool on = at < a.d;
+            if (!kWhole && base >= a.d) break;
             Features<T, 2> o;
             Pair w[2], rho[2], pre[2], u[2], over[2], dz[2], dr[2];
             remake(j, o, w, rho, pre, u, over);
@@ -720,9 +725,9 @@ int64_t ring_partials(int32_t n, int64_t tokens, int64_t d) {
     return parts < room ? parts : room;
 }
 
-template <typename T, int kParts>
+template <typename T, int kParts, bool kWhole>
 int launch_rows(const BlockBackwardArgs<T>& a, int64_t parts, int32_t n, cudaStream_t stream) {
-    constexpr auto kernel = relay_block_norm_backward_rows_kernel<T, kParts>;
+    constexpr auto kernel = relay_block_norm_backward_rows_kernel<T, kParts, kWhole>;
     if (!allow_shared<kernel>(Ring<T, kParts, 5>::kShared)) return RELAY_ECUDA;
     kernel<<<dim3(static_cast<unsigned>(parts), n), 32 * Ring<T, kParts, 5>::kWarps, Ring<T, kParts, 5>::kShared, stream>>>(a);
     return status_of_launch();
@@ -741,15 +746,18 @@ bool by_ring(int64_t d, F f) {
     return false;
 }
 
-// CTAs of a worker, and whether there are at least four rows for each group of them: their
-// start costs as much as two (the weights, the barriers).
-int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }
+int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }  // of a worker
 
+// Whether rows go through shared memory: where that is faster, by what was measured, old way and
+// this one in us, 4 workers:
+//   backward  [512 rows][1000] bf16  10.5 12.6, [1024][1000] 14.7 12.7, [16384][512] 58 37,
+//             [8192][4096] 226 110, [8192][8192] 735 287, fp32 [8192][4096] 324 228
+//   forward   [2048][4096] bf16 18.7 20.7, [4096][4096] 39 37, [8192][2048] 44 35,
+//             [8192][4096] 70 62, fp32 [8192][4096] 114 116
 template <typename T, int kInputs>
 bool takes_ring(int32_t n, int64_t tokens, int64_t d) {
-    bool takes = false;
-    by_ring<T, kInputs>(d, [&](auto r) { takes = tokens >= 4 * decltype(r)::kGroups * ring_ctas(n); });
-    return takes;
+    const bool fits = by_ring<T, kInputs>(d, [](auto) {});
+    return fits && (kInputs == 5 ? n * tokens * d >= 1 << 20 : n * tokens * d >= 1 << 24);
 }
 
 bool weight_fits(const float* p, int64_t stride) { return p != nullptr && aligned(p, 4) && stride >= 0; }
@@ -765,6 +773,8 @@ Weight weight_of(const float* p, int64_t stride, int32_t n, int64_t d) {
 }  // namespace
 
 extern "C" {
+
+#if RELAY_PASS == 1
 
 int relay_block_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* x, const relay_rows* gate,
                      const relay_rows* residual, const float* post, int64_t post_stride, const float* pre, int64_t pre_stride,
@@ -795,17 +805,22 @@ int relay_block_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
                              view<T>(total, n, tokens), view<T>(y, n, tokens), weight_of(post, post_stride, n, d),
                              weight_of(pre, pre_stride, n, d), weight_of(scale, scale_stride, n, d), eps, rstd, codes, scales,
                              static_cast<int32_t>(tokens), static_cast<int32_t>(d), static_cast<int32_t>(pitch_of(d))};
-        if (vec && takes_ring<T, 3>(n, tokens, d)) {
-            int rc = RELAY_OK;
-            by_ring<T, 3>(d, [&](auto r) {
-                using R = decltype(r);
-                constexpr auto kernel = relay_block_norm_rows_kernel<T, R::kParts>;
-                rc = allow_shared<kernel>(R::kShared) ? RELAY_OK : RELAY_ECUDA;
-                if (rc != RELAY_OK) return;
-                kernel<<<dim3(static_cast<unsigned>(ring_ctas(n)), static_cast<unsigned>(n)), 32 * R::kWarps, R::kShared, stream>>>(a);
-                rc = status_of_launch();
-            });
-            return rc;
+        if constexpr (sizeof(T) == 2) {
+            if (vec && takes_ring<T, 3>(n, tokens, d)) {
+                int rc = RELAY_OK;
+                by_ring<T, 3>(d, [&](auto r) {
+                    using R = decltype(r);
+                    const auto go = [&](auto whole) {
+                        constexpr auto kernel = relay_block_norm_rows_kernel<T, R::kParts, decltype(whole)::value>;
+                        if (!allow_shared<kernel>(R::kShared)) return RELAY_ECUDA;
+                        const dim3 grid(static_cast<unsigned>(ring_ctas(n)), static_cast<unsigned>(n));
+                        kernel<<<grid, 32 * R::kWarps, R::kShared, stream>>>(a);
+                        return status_of_launch();
+                    };
+                    rc = d > R::kWide - kQuads ? go(std::true_type()) : go(std::false_type());
+                });
+                return rc;
+            }
         }
         return by_width(a.pitch, [&](auto hold) {
             constexpr int kParts = decltype(hold)::kParts, kStrips = decltype(hold)::kStrips;
@@ -817,6 +832,8 @@ int relay_block_norm(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
         });
     });
 }
+
+#else
 
 int64_t relay_block_norm_backward_workspace(int32_t n, int64_t tokens, int64_t d) {
     if (const int rc = check_shape(RELAY_FP32, n, tokens, d)) return rc;
@@ -876,7 +893,8 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
             by_ring<T, 5>(d, [&](auto r) {
                 constexpr int kParts = decltype(r)::kParts;
                 parts = static_cast<int>(ring_partials<T, kParts>(n, tokens, d));
-                rc = launch_rows<T, kParts>(a, parts, n, stream);
+                rc = d > decltype(r)::kWide - kQuads ? launch_rows<T, kParts, true>(a, parts, n, stream)
+                                                     : launch_rows<T, kParts, false>(a, parts, n, stream);
             });
             return rc;
         }
@@ -895,5 +913,7 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
         static_cast<const float*>(workspace), parts, static_cast<int>(d), static_cast<int>(pitch_of(d)), to);
     return status_of_launch();
 }
+
+#endif
 
 }  // extern "C"

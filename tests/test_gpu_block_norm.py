@@ -194,7 +194,7 @@ def test_many_rows(n, T, d):
     _check(n, T, d, torch.bfloat16, seed=T)
 
 
-# rows by bulk copies: four and more for every group of warps, 152 / n CTAs of 16 warps (8 in fp32), one to 16 a row
+# the backward pass takes rows by bulk copies from 2^20 features on: 152 / n CTAs of 16 warps (8 in fp32), one to 16 a row
 @pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES)
 @pytest.mark.parametrize("n,T,d", [(150, 67, 200), (77, 131, 512), (151, 35, 520), (151, 35, 1024), (152, 18, 1032), (120, 17, 2048),
                                    (152, 9, 2056), (140, 11, 4096), (100, 7, 4104), (90, 5, 8192), (3, 1100, 4096), (256, 66, 64)])
@@ -207,16 +207,57 @@ def test_rows_through_shared_memory(dtype, n, T, d):
 
 
 @pytest.mark.parametrize("gate,scale,over", [(False, False, False), (True, False, True), (False, True, False)])
-def test_options_of_rows_through_shared_memory(gate, scale, over):
+def test_options_of_backward_rows_through_shared_memory(gate, scale, over):
     for dtype in (torch.bfloat16, torch.float32):
         _check(151, 35, 1000, dtype, gate=gate, scale=scale, over=over, ckpt=over, seed=3)
-    n, T, d = 151, 40, 1024
-    x, r, y = (torch.randn(n, T, d, device="cuda").bfloat16() for _ in range(3))
-    w = _weight(0, n, d)
-    want = torch.empty_like(x)
-    rs.relay_block_norm(x, r, w, w, want, y, EPS)
-    rs.relay_block_norm(x, r, w, w, r, y, EPS)  # the sum in the residual's own rows
-    assert torch.equal(r, want)
+
+
+# and the forward pass of 16-bit rows from 2^24 on: 24 warps a CTA, one to 8 a row
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("n,T,d,gate,scale", [(3, 10000, 568, True, True), (150, 112, 1024, True, True), (2, 8200, 1032, False, True),
+                                              (5, 1700, 2000, True, False), (4, 1025, 4096, True, True), (1, 4100, 4104, True, True),
+                                              (256, 9, 8192, False, False)])
+def test_forward_rows_through_shared_memory(dtype, n, T, d, gate, scale):
+    """The definition and _forward's bounds, in 64 bits on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+
+    def values(size):
+        v = torch.randn(n, T, d, generator=g, device="cuda") * torch.where(torch.rand(d, generator=g, device="cuda") < 1 / 16, 20.0, 1.0)
+        return (v * size).to(dtype)
+
+    x, r, z = values(0.7), values(1.0), values(0.5) if gate else None
+    post, pre, rho = (_weight(k, n, d, first=k) for k in range(3))
+    total, y, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(2, n, T, device="cuda")
+    kept = rs.ActivationCheckpoint(n, T, d)
+    rs.relay_block_norm(x, r, post, pre, total, y, EPS, gate=z, scale=rho if scale else None, rstd=rstd, checkpoint=kept)
+    X, R, W, V = x.double(), r.double(), post.double()[:, None], pre.double()[:, None]
+    sx, sx_off = 1 / (X.square().mean(-1, keepdim=True) + EPS).sqrt(), (CHAIN / 2 + 6) * U
+    p = torch.sigmoid(z.double()) if gate else torch.ones_like(X)
+    off = (4 + z.double().abs()) * 2.0 ** -23 * torch.sigmoid(-z.double()) if gate else 0
+    a, b = p * X * sx * W, R * (rho.double()[:, None] if scale else 1)
+    h = a + b
+    eh = a.abs() * (sx_off + 5 * U + off) + 2 * U * (a.abs() + b.abs())
+    sh = 1 / (h.square().mean(-1, keepdim=True) + EPS).sqrt()
+    sh_off = (CHAIN / 2 + 6) * U + (h.abs() * eh).sum(-1, keepdim=True) / d * sh * sh
+    want, ey = h * sh * V, V.abs() * sh * (eh + h.abs() * (sh_off + 4 * U))
+
+    def near(got, want, bound):
+        far = (got.double() - want).abs() - bound
+        assert bool((far <= 0).all()), (int((far > 0).sum()), float(far.max()))
+
+    def rounded(want, bound):
+        return bound + ROUND[dtype] * (want.abs() + bound) + LEAST[dtype]
+
+    near(total, h, rounded(h, eh))
+    near(y, want, rounded(want, ey))
+    near(rstd, torch.stack([sx, sh])[..., 0], torch.stack([sx * sx_off, sh * sh_off])[..., 0])
+    hhat = h * sh
+    wide = torch.nn.functional.pad(hhat, (0, -d % 32)).unflatten(-1, (-1, 32))
+    step = (wide.abs().amax(-1) / 127.5).clamp(min=2.0 ** -127).repeat_interleave(32, -1)[..., :d]
+    near(kept.unpack(torch.float32), hhat, step * (1 + 1e-5) + ey / V.abs() + U * hhat.abs())
+    there = r.clone()
+    rs.relay_block_norm(x, there, post, pre, there, y, EPS, gate=z, scale=rho if scale else None)  # the sum in the residual's rows
+    assert torch.equal(there, total)
 
 
 def test_no_tokens():
