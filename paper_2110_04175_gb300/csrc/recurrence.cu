@@ -103,7 +103,7 @@ struct RecurrenceArgs {
     int64_t initial_stride, last_stride, dlast_stride;
     const uint8_t* begins;
     const int32_t* lengths;
-    float *a, *b;  // [n][segments][d], with several segments: A, then the state that reaches the segment; B
+    float *a, *b, *first;  // with several segments: their A and B, [n][segments][d], and the state before them, [n][d]
     int32_t n, tokens, d, strips, segments, segment;  // segment: tokens
 };
 
@@ -226,6 +226,54 @@ constexpr int kRunOf = sizeof(T) == 2 ? 16 : 8;
 template <typename T>
 constexpr int kBackRunOf = sizeof(T) == 2 ? 8 : 4;
 
+// The state that reaches segment p.segment, from the stretches of those before it (behind it:
+// kBack), which the CTA's warps join side by side.  The first one's holds the incoming state
+// (keep_ends) and lets nothing through.
+template <Way kWay, bool kBack, typename T>
+__device__ __forceinline__ void reach(const RecurrenceArgs<T>& a, const Place<T>& p, int part, int lane, int left,
+                                      float4 (&shared)[kWarps][32], float (&h)[2]) {
+    const int before = kBack ? a.segments - 1 - p.segment : p.segment, each = (before + kWarps - 1) / kWarps;
+    if (before == 0) {
+        load_state<kWay>(a.first + static_cast<int64_t>(p.worker) * a.d + p.strip, lane, left, h);
+        return;
+    }
+    float whole[4] = {1.0f, 1.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int j = part * each; j < min(part * each + each, before); ++j) {
+        const int64_t at = p.at + static_cast<int64_t>(kBack ? a.segments - 1 - j - p.segment : j - p.segment) * a.d;
+        float f[2], b[2];
+        load_state<kWay>(a.a + at, lane, left, f);
+        load_state<kWay>(a.b + at, lane, left, b);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) join<true>(whole[k], whole[2 + k], f[k], b[k]);
+    }
+    shared[part][lane] = make_float4(whole[0], whole[1], whole[2], whole[3]);
+    __syncthreads();
+    h[0] = h[1] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kWarps; ++j) {
+        const float4 e = shared[j][lane];
+        h[0] = carry<true>(h[0], e.x, e.z);
+        h[1] = carry<true>(h[1], e.y, e.w);
+    }
+}
+
+// Puts a segment's stretch away, that of the first segment with the incoming state in it.
+template <Way kWay, typename T>
+__device__ __forceinline__ void keep_ends(const RecurrenceArgs<T>& a, const Place<T>& p, int lane, int left, bool first,
+                                          const float* state, int64_t stride, float (&whole)[4]) {
+    if (first) {
+        float h[2];
+        load_state<kWay>(state == nullptr ? nullptr : state + p.worker * stride + p.strip, lane, left, h);
+        store_state<kWay>(a.first + static_cast<int64_t>(p.worker) * a.d + p.strip, lane, left, h);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) whole[2 + k] = carry<true>(h[k], whole[k], whole[2 + k]), whole[k] = -0.0f;
+    }
+    const float one[2] = {whole[0], whole[1]}, two[2] = {whole[2], whole[3]};
+    store_state<kWay>(a.a + p.at, lane, left, one);
+    store_state<kWay>(a.b + p.at, lane, left, two);
+}
+
 // A segment's tokens tile by tile: kTime warps take a run each.
 template <typename T, Way kWay, int kTime, int kRun, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(RecurrenceArgs<T> a) {
@@ -236,10 +284,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(Recurr
     const int left = p.on ? a.d - p.strip : 0, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
     const int end = p.on ? min(p.first + a.segment, a.tokens) : 0, to = min(end, p.length);
     float h[2];
-    if (a.segments == 1)
+    if (kTime < kWarps || a.segments == 1)
         load_state<kWay>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, h);
-    else
-        load_state<kWay>(a.a + p.at, lane, left, h);
+    else if constexpr (kTime == kWarps)
+        reach<kWay, false>(a, p, part, lane, left, shared[1][0], h);
     Two<T> gate[kRun], value[kRun];
     uint32_t begin;
     const auto ask = [&](int token) {
@@ -279,7 +327,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(Recurr
         }
         if constexpr (kTime == 1) h[0] = x[0], h[1] = x[1];
     }
-    if (a.segments == 1 && a.last != nullptr && part == 0)
+    if (p.segment == a.segments - 1 && a.last != nullptr && part == 0)
         store_state<kWay>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
 }
 
@@ -399,10 +447,10 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
         for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
     if (kCtas > 1) cluster_sync();  // the others have started
     float h[2];
-    if (a.segments == 1)
+    if (kCtas > 1 || a.segments == 1)
         load_state<kVector>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, h);
     else
-        load_state<kVector>(a.a + p.at, lane, left, h);
+        reach<kVector, false>(a, p, part, lane, left, shared[1], h);
     const int start = first_of(0) + part * kRun;
     uint32_t begin = load_begins<kRun, kBegins>(a, p.worker, start, lane, to - start);
     bool ok = true;
@@ -456,7 +504,7 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
         }
     }
     if (threadIdx.x == 0) boxes.none_in_flight(tiles);
-    if (a.segments == 1 && a.last != nullptr && part == 0 && rank == 0)
+    if (p.segment == a.segments - 1 && a.last != nullptr && part == 0 && rank == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
 }
 
@@ -493,40 +541,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_ends_kernel(R
         join<kBegins>(whole[0], whole[2], e.x, e.z);
         join<kBegins>(whole[1], whole[3], e.y, e.w);
     }
-    const float one[2] = {whole[0], whole[1]}, two[2] = {whole[2], whole[3]};
-    store_state<kWay>(a.a + p.at, lane, left, one);
-    store_state<kWay>(a.b + p.at, lane, left, two);
-}
-
-// Through a channel's segments (from the last to the first: kBack): a gets the state that
-// reaches each of them, `last` what leaves the last of them.
-template <bool kBack>
-__global__ void __launch_bounds__(64)
-relay_recurrence_carry_kernel(float* a, const float* b, int segments, int d, const float* initial, int64_t initial_stride,
-                              float* last, int64_t last_stride) {
-    const int c = blockIdx.x * 64 + threadIdx.x, worker = blockIdx.y;
-    if (c >= d) return;
-    constexpr int kAtOnce = 8;
-    const int64_t base = static_cast<int64_t>(worker) * segments * d + c;
-    float h = initial == nullptr ? 0.0f : initial[worker * initial_stride + c];
-    for (int s0 = 0; s0 < segments; s0 += kAtOnce) {
-        float fa[kAtOnce], fb[kAtOnce];
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int s = kBack ? segments - 1 - s0 - j : s0 + j;
-            fa[j] = 0.0f, fb[j] = 0.0f;
-            if (s0 + j < segments) fa[j] = a[base + int64_t(s) * d], fb[j] = b[base + int64_t(s) * d];
-        }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int s = kBack ? segments - 1 - s0 - j : s0 + j;
-            if (s0 + j < segments) {
-                a[base + int64_t(s) * d] = h;
-                h = carry<true>(h, fa[j], fb[j]);
-            }
-        }
-    }
-    if (last != nullptr) last[worker * last_stride + c] = h;
+    keep_ends<kWay>(a, p, lane, left, p.segment == 0, a.initial, a.initial_stride, whole);
 }
 
 // ------------------------------------------------------------------ the backward pass
@@ -563,10 +578,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
     const int left = p.on ? a.d - p.strip : 0, tiles = (min(a.segment, a.tokens) + kTile - 1) / kTile;
     const int end = p.on ? min(p.first + a.segment, a.tokens) : 0, to = min(end, p.length);
     float m[2], first[2];
-    if (a.segments == 1)
+    if (kTime < kWarps || a.segments == 1)
         load_state<kWay>(a.dlast == nullptr ? nullptr : a.dlast + p.worker * a.dlast_stride + p.strip, lane, left, m);
-    else
-        load_state<kWay>(a.a + p.at, lane, left, m);
+    else if constexpr (kTime == kWarps)
+        reach<kWay, true>(a, p, part, lane, left, shared[1][0], m);
     load_state<kWay>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, first);
     Two<T> gate[kRun], dout[kRun], value[kRun], before[kRun];
     uint32_t begin;
@@ -632,7 +647,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
         }
         if constexpr (kTime == 1) m[0] = x[0], m[1] = x[1];
     }
-    if (a.segments == 1 && a.last != nullptr && part == 0)
+    if (p.segment == 0 && a.last != nullptr && part == 0)
         store_state<kWay>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
 
@@ -665,10 +680,10 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
         for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
     if (kCtas > 1) cluster_sync();  // the others have started
     float m[2], first[2];
-    if (a.segments == 1)
+    if (kCtas > 1 || a.segments == 1)
         load_state<kVector>(a.dlast == nullptr ? nullptr : a.dlast + p.worker * a.dlast_stride + p.strip, lane, left, m);
     else
-        load_state<kVector>(a.a + p.at, lane, left, m);
+        reach<kVector, true>(a, p, part, lane, left, shared[1], m);
     load_state<kVector>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, first);
     // warp 0 of a tile takes its last tokens
     const int place = (kWarps - 1 - part) * kRun;
@@ -734,7 +749,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
         }
     }
     if (threadIdx.x == 0) boxes.none_in_flight(tiles);
-    if (a.segments == 1 && a.last != nullptr && part == 0 && rank == 0)
+    if (p.segment == 0 && a.last != nullptr && part == 0 && rank == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
 
@@ -777,9 +792,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends
         join<kBegins>(whole[0], whole[2], e.x, e.z);
         join<kBegins>(whole[1], whole[3], e.y, e.w);
     }
-    const float one[2] = {whole[0], whole[1]}, two[2] = {whole[2], whole[3]};
-    store_state<kWay>(a.a + p.at, lane, left, one);
-    store_state<kWay>(a.b + p.at, lane, left, two);
+    keep_ends<kWay>(a, p, lane, left, p.segment == a.segments - 1, a.dlast, a.dlast_stride, whole);
 }
 
 // ---------------------------------------------------------------- launching
@@ -904,7 +917,7 @@ extern "C" {
 int64_t relay_recurrence_workspace(int32_t n, int64_t tokens, int64_t d) {
     if (const int rc = check_recurrence(RELAY_FP32, n, tokens, d)) return rc;
     const Cut cut = recurrence_cut(n, tokens, d);
-    return cut.segments > 1 ? 8 * static_cast<int64_t>(n) * cut.segments * d : 0;
+    return cut.segments > 1 ? (8 * static_cast<int64_t>(cut.segments) + 4) * n * d : 0;
 }
 
 int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows* gate, const relay_rows* value,
@@ -938,6 +951,7 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
         a.last = last, a.last_stride = n > 1 ? last_stride : 0;
         a.begins = begins, a.lengths = lengths;
         a.a = static_cast<float*>(workspace), a.b = a.a + static_cast<int64_t>(n) * cut.segments * d;
+        a.first = a.b + static_cast<int64_t>(n) * cut.segments * d;
         a.n = n, a.tokens = static_cast<int32_t>(tokens), a.d = static_cast<int32_t>(d);
         a.strips = cut.strips, a.segments = cut.segments, a.segment = cut.segment;
         const int64_t units = static_cast<int64_t>(n) * cut.segments * cut.strips;
@@ -945,8 +959,6 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
             (vec ? (begins != nullptr ? relay_recurrence_ends_kernel<T, kVector, true> : relay_recurrence_ends_kernel<T, kVector, false>)
                  : relay_recurrence_ends_kernel<T, kDirect, true>)
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
-            relay_recurrence_carry_kernel<false><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
-                a.a, a.b, cut.segments, a.d, initial, a.initial_stride, last, a.last_stride);
         }
         if (boxes) {
             TileMaps<T> maps{};
@@ -1013,6 +1025,7 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
         a.last = dinitial, a.last_stride = n > 1 ? dinitial_stride : 0;
         a.begins = begins, a.lengths = lengths;
         a.a = static_cast<float*>(workspace), a.b = a.a + static_cast<int64_t>(n) * cut.segments * d;
+        a.first = a.b + static_cast<int64_t>(n) * cut.segments * d;
         a.n = n, a.tokens = static_cast<int32_t>(tokens), a.d = static_cast<int32_t>(d);
         a.strips = cut.strips, a.segments = cut.segments, a.segment = cut.segment;
         const int64_t units = static_cast<int64_t>(n) * cut.segments * cut.strips;
@@ -1021,8 +1034,6 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
                                       : relay_recurrence_backward_ends_kernel<T, kVector, false>)
                  : relay_recurrence_backward_ends_kernel<T, kDirect, true>)
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
-            relay_recurrence_carry_kernel<true><<<dim3(static_cast<unsigned>((d + 63) / 64), n), 64, 0, stream>>>(
-                a.a, a.b, cut.segments, a.d, dlast, a.dlast_stride, dinitial, a.last_stride);
         }
         if (boxes) {
             TileMaps<T> maps{};
