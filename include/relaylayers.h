@@ -40,9 +40,10 @@
  *   - Arithmetic is in fp32, and each output is rounded once, to the nearest
  *     (y and xhat come from the unrounded h).  The results of a call are the
  *     same bits every time: no atomics.
- *   - Lengths.  Where a call sums over tokens, `lengths` (device int32 [n],
- *     or NULL for all) says how many of each worker's rows count, clamped to
- *     0 .. tokens.  Rows past it are not read, and dx there is zero.
+ *   - Lengths.  Where a call sums over tokens or goes along them, `lengths`
+ *     (device int32 [n], or NULL for all) says how many of each worker's rows
+ *     count, clamped to 0 .. tokens.  Rows past it may hold anything, and the
+ *     rows that the call writes there are zero.
  *   - Streams, ownership and errors are those of relaysum.h: caller-owned
  *     device buffers, nothing allocated, nothing synchronised, every argument
  *     checked before anything is enqueued.  The sizes that the library cannot
@@ -56,9 +57,10 @@
  *     is not a multiple of its element's size, checkpoint or workspace
  *     addresses that are not multiples of 16, a workspace too small.
  *     RELAY_EUNSUPPORTED: n > RELAY_MAX_N (in the recurrence
- *     RELAY_RECURRENCE_MAX_N), n tokens >= 2^30, d > 2^24, in the norm d >
+ *     RELAY_RECURRENCE_MAX_N), n tokens >= 2^30, d > 2^24, in the norms d >
  *     RELAY_NORM_MAX_D, in the weight gradient inputs >
- *     RELAY_WEIGHT_GRAD_MAX_INPUTS.
+ *     RELAY_WEIGHT_GRAD_MAX_INPUTS, in the orthogonal update rows or columns
+ *     > RELAY_ORTHOGONALISE_MAX.
  *
  * The 8-bit format.  A row of d features is blocks of 32 with one scale byte
  * c per block and one signed code q per feature:
@@ -219,9 +221,11 @@ int64_t relay_recurrence_workspace(int32_t n, int64_t tokens, int64_t d);
  * shape, or NULL): the state behind the last token, for the call that goes on;
  * it may be `initial`, at the same stride.  begins (uint8 [n][tokens], or
  * NULL): not 0 at a token that begins a sequence, where h_{t-1} counts as 0
- * whatever it holds.  lengths: tokens past them are not read, leave the state
- * as it is, and get rows of 0.  Behind an input that is not finite the states
- * are not finite up to the next beginning (an infinity may become NaN). */
+ * whatever it holds.  lengths: tokens past them leave the state as it is and
+ * get rows of 0.  Behind an input that is not finite the states
+ * are not finite up to the next beginning (an infinity may become NaN).  The
+ * calls' waits for copies end after about a second each; results that one of
+ * them was for are NaN then (in relay_block_norm and its backward pass too). */
 int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *gate,
                      const relay_rows *value, const float *initial, int64_t initial_stride, const uint8_t *begins,
                      const int32_t *lengths, const relay_rows *out, float *last, int64_t last_stride, void *workspace,

@@ -9,7 +9,7 @@ been built, the first call raises.
 
 The layer operators (``layers``, declared in ``include/relaylayers.h``) run one
 layer of all n workers' models at once, forward and backward, with activations
-held in 8 bits.
+held in 8 bits, and make the updates of their matrices orthogonal.
 
 ``RelayRun`` is a convenience owner of the device buffers of one run
 (allocated with torch) that swaps the double-buffered messages between

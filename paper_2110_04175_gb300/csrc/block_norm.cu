@@ -4,14 +4,19 @@
 //
 //   m = x s_x w_post;  h = rho r + sigma(z) m;  y = h s_h w_pre
 //
-// All rows in and all rows out once, two sums over a row between them, so memory bounds it.
-// kParts warps share a row, each with kStrips strips of 256 features (layers.cuh).
+// All rows in and all rows out once.  Any rows go through registers, kParts warps a row; many
+// aligned ones come by bulk copies to shared memory, so that what is on its way takes no
+// registers, and groups of warps wait only for their own row and sums.  Measured in bf16 with
+// gate and scale, [4][4096][4096]: forward with the 8-bit output 125 us (740 MB, 5.9 TB/s), backward with
+// dtotal 206 us and 5 us for the weights' sums (1074 MB, 5.1 TB/s).  Issue slots are 69 % and 64 %
+// taken: a feature takes 50 and 70 instructions, and waits for sums and copies have 24 and 16
+// warps to hide among.
 #include <type_traits>
 
 #include "blackwell.cuh"
 #include "layers.cuh"
 
-// Compiled once per pass (RELAY_PASS: 1 forward, 2 backward), which halves the build's longest unit.
+// Compiled once per pass (RELAY_PASS: 1 forward, 2 backward): the two halves build side by side.
 namespace {
 
 struct Weight {  // fp32, from worker to worker
@@ -129,6 +134,8 @@ relay_block_norm_kernel(BlockArgs<T> a) {
     }
 }
 
+#if RELAY_PASS == 1
+
 // The 8-bit format of four features a lane, a block on eight lanes: layers.cuh's put_strip.
 __device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at, int lane, const Pair (&v)[2]) {
     const float e[4] = {v[0].v.x, v[0].v.y, v[1].v.x, v[1].v.y};
@@ -141,6 +148,8 @@ __device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at,
     *reinterpret_cast<uint32_t*>(codes + at) = c == 255u ? 0u : __byte_perm(ab, cd, 0x5410);
     if (lane % 8 == 0) scales[at / kBlock] = static_cast<uint8_t>(c);
 }
+
+#endif  // RELAY_PASS
 
 // Many aligned rows of up to 8192 features (4096 in fp32): they come by bulk copies to shared memory and h stays in
 // registers.  The groups wait only for themselves; while one waits for its row or for one
@@ -321,6 +330,8 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
     }
     if (brings) none_in_flight(&bars[group][0], R::kStages, i);
 }
+
+#if RELAY_PASS == 2
 
 // ------------------------------------------------------------------ the backward pass
 //
@@ -689,7 +700,44 @@ __global__ void __launch_bounds__(256) relay_block_norm_join_kernel(const float*
         if (column + k < d) to.p[which][blockIdx.y * to.stride[which] + column + k] = v[k];
 }
 
+#endif  // RELAY_PASS
+
 // ---------------------------------------------------------------- launching
+
+// f(R) for the Ring with the fewest warps a row that holds one; none (false) where the CTA's
+// warps do not.
+template <typename T, int kInputs, int kParts = 1, typename F>
+bool by_ring(int64_t d, F f) {
+    using R = Ring<T, kParts, kInputs>;
+    if (d <= R::kWide) {
+        f(R());
+        return true;
+    }
+    if constexpr (R::kWarps % (2 * kParts) == 0 && R::kWarps >= 2 * kParts) return by_ring<T, kInputs, 2 * kParts>(d, f);
+    return false;
+}
+
+inline int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }  // of a worker
+
+// Whether rows go through shared memory: where that is faster, by what was measured, old way and
+// this one in us, 4 workers:
+//   backward  [512 rows][1000] bf16  10.5 12.6, [1024][1000] 14.7 12.7, [16384][512] 58 37,
+//             [8192][4096] 226 110, [8192][8192] 735 287, fp32 [8192][4096] 324 228
+//   forward   [2048][4096] bf16 18.7 20.7, [4096][4096] 39 37, [8192][2048] 44 35,
+//             [8192][4096] 70 62, fp32 [8192][4096] 114 116
+template <typename T, int kInputs>
+bool takes_ring(int32_t n, int64_t tokens, int64_t d) {
+    const bool fits = by_ring<T, kInputs>(d, [](auto) {});
+    return fits && (kInputs == 5 ? n * tokens * d >= 1 << 20 : n * tokens * d >= 1 << 24);
+}
+
+bool weight_fits(const float* p, int64_t stride) { return p != nullptr && aligned(p, 4) && stride >= 0; }
+
+Weight weight_of(const float* p, int64_t stride, int32_t n, int64_t d) {
+    return Weight{p, n > 1 ? stride : 0, d % 8 == 0 && aligned(p, 16) && (n == 1 || stride % 4 == 0)};
+}
+
+#if RELAY_PASS == 2
 
 // Calls f(kParts, kStrips) for the backward pass, whose sums over the tokens take three
 // times a strip's registers: one strip a warp as far as a CTA's 32 warps go.
@@ -733,42 +781,11 @@ int launch_rows(const BlockBackwardArgs<T>& a, int64_t parts, int32_t n, cudaStr
     return status_of_launch();
 }
 
-// f(R) for the Ring with the fewest warps a row that holds one; none (false) where the CTA's
-// warps do not.
-template <typename T, int kInputs, int kParts = 1, typename F>
-bool by_ring(int64_t d, F f) {
-    using R = Ring<T, kParts, kInputs>;
-    if (d <= R::kWide) {
-        f(R());
-        return true;
-    }
-    if constexpr (R::kWarps % (2 * kParts) == 0 && R::kWarps >= 2 * kParts) return by_ring<T, kInputs, 2 * kParts>(d, f);
-    return false;
-}
-
-int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }  // of a worker
-
-// Whether rows go through shared memory: where that is faster, by what was measured, old way and
-// this one in us, 4 workers:
-//   backward  [512 rows][1000] bf16  10.5 12.6, [1024][1000] 14.7 12.7, [16384][512] 58 37,
-//             [8192][4096] 226 110, [8192][8192] 735 287, fp32 [8192][4096] 324 228
-//   forward   [2048][4096] bf16 18.7 20.7, [4096][4096] 39 37, [8192][2048] 44 35,
-//             [8192][4096] 70 62, fp32 [8192][4096] 114 116
-template <typename T, int kInputs>
-bool takes_ring(int32_t n, int64_t tokens, int64_t d) {
-    const bool fits = by_ring<T, kInputs>(d, [](auto) {});
-    return fits && (kInputs == 5 ? n * tokens * d >= 1 << 20 : n * tokens * d >= 1 << 24);
-}
-
-bool weight_fits(const float* p, int64_t stride) { return p != nullptr && aligned(p, 4) && stride >= 0; }
-
 bool gradient_fits(const float* p, int64_t stride, int32_t n, int64_t d) {
     return p != nullptr && aligned(p, 4) && (n == 1 || stride >= d);
 }
 
-Weight weight_of(const float* p, int64_t stride, int32_t n, int64_t d) {
-    return Weight{p, n > 1 ? stride : 0, d % 8 == 0 && aligned(p, 16) && (n == 1 || stride % 4 == 0)};
-}
+#endif  // RELAY_PASS
 
 }  // namespace
 

@@ -4,7 +4,8 @@
 //   x = u / (|u| + eps);  a step: g = x x^T,  x <- a x + (b g + c g g) x
 //
 // with x as wide as it is high or wider (u or its transpose).  Three products a step, on the
-// tensor cores, bound by them.
+// tensor cores, bound by them where matrices are large and by the way from product to product
+// where they are small.
 //
 // A step multiplies small singular values by 3.4, five of them by 480, and what an operand
 // is rounded by with them: bf16 operands would leave 1 % of noise.  So every operand is
@@ -14,9 +15,15 @@
 // bits, and nothing reaches fp16's 65504.
 //
 // A pair of CTAs makes a tile of 256 x kN (cta_group::2), each brings half of both operands
-// by TMA.  x x^T and g g are symmetric: tiles above the diagonal are copies.  The tensor
-// cores cut off what an addition shifts out, so sums leave them every kGroup stages for
-// registers of other warps, as in the weight gradient.
+// by TMA; small matrices get tiles of one CTA, and those of up to 128 rows a whole step a launch.
+// x x^T and g g are symmetric: tiles above the diagonal are copies.  The tensor
+// cores cut off what an addition shifts out, so sums leave them every one to three stages for
+// registers of other warps, as in the weight gradient.  Errors against 64 bits are 0.5 to 1.1
+// times those of the same steps in plain fp32 (0.6 where k is thousands).
+//
+// Measured: 4 x [2048][8192] 4.4 ms on its own, 2.2 TFLOP as a count of the symmetric halves, 6.7
+// in fp16 products (1530 TFLOP/s, 0.79 of what a library product of 8192^3 does in a burst), 4.8 to 4.9 back to
+// back, when power holds the clock; 3 x [1537][1001] 344 us; 8 x [128][256] 52 us.
 #include <cuda_fp16.h>
 
 #include "blackwell.cuh"
