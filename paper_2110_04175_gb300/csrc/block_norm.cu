@@ -9,7 +9,7 @@
 // registers, and groups of warps wait only for their own row and sums.  Measured in bf16 with
 // gate and scale, [4][4096][4096]: forward with the 8-bit output 125 us (740 MB, 5.9 TB/s), backward with
 // dtotal 206 us and 5 us for the weights' sums (1074 MB, 5.1 TB/s).  Issue slots are 69 % and 64 %
-// taken: a feature takes 50 and 70 instructions, and waits for sums and copies have 24 and 16
+// taken: a feature takes 52 and 78 instructions, and waits for sums and copies have 24 and 16
 // warps to hide among.
 #include <type_traits>
 

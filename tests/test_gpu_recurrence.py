@@ -158,6 +158,21 @@ def test_stretches_go_on_from_the_state(T, cuts, d):
     within(state, end, end_bound)
 
 
+@pytest.mark.parametrize("T,d", [(1, 40), (9, 33), (300, 64), (1100, 33), (13000, 64)])
+def test_the_states_gradient_in_its_own_place(T, d):
+    """dinitial over dlast: one warp, a CTA, a cluster, segments."""
+    n, dtype = 2, torch.bfloat16
+    g, v = _inputs(9, n, T, d, dtype)
+    gate, value = _cuda(g, dtype), _cuda(v, dtype)
+    dout, dlast = torch.randn_like(gate), torch.randn(n, d, device="cuda")
+    out, dg, dv = (torch.empty_like(gate) for _ in range(3))
+    rs.relay_recurrence(gate, value, out, _work(n, T, d))
+    want = torch.empty_like(dlast)
+    rs.relay_recurrence_backward(dout, gate, value, out, dg, dv, _work(n, T, d), dlast=dlast, dinitial=want)
+    rs.relay_recurrence_backward(dout, gate, value, out, dg, dv, _work(n, T, d), dlast=dlast, dinitial=dlast)
+    assert torch.equal(dlast, want)
+
+
 @pytest.mark.parametrize("T", [20, 1100])
 def test_nothing_passes_a_beginning(T):
     """Infinities and NaN before a beginning, in the padding and in a state that is not taken leave no trace."""
