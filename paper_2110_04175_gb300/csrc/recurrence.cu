@@ -36,26 +36,40 @@ constexpr int kWide = 64;  // channels of a warp
 template <Way kWay>
 __device__ __forceinline__ int channel(int lane, int k) { return kWay == kVector ? 2 * lane + k : 32 * k + lane; }
 
-// Two channels as they lie in memory; 16-bit ones share a register.
-template <typename T>
+// Two channels as they lie in memory: 16-bit ones that come together share a register, and ones
+// that come apart have one each, since putting them together would wait for them.
+template <typename T, Way kWay = kVector>
 struct Two {
     uint32_t w;
-    __device__ __forceinline__ float get(int k) const { return widen(reinterpret_cast<const T*>(&w)[k]); }
+    __device__ __forceinline__ float get(int k) const {
+        if constexpr (std::is_same_v<T, __nv_bfloat16>) return __uint_as_float(k == 0 ? w << 16 : w & 0xffff0000u);
+        return widen(reinterpret_cast<const T*>(&w)[k]);
+    }
     __device__ __forceinline__ void set(T a, T b) {
         reinterpret_cast<T*>(&w)[0] = a;
         reinterpret_cast<T*>(&w)[1] = b;
     }
 };
-template <>
-__device__ __forceinline__ float Two<__nv_bfloat16>::get(int k) const {
-    return __uint_as_float(k == 0 ? w << 16 : w & 0xffff0000u);
-}
+template <typename T>
+struct Two<T, kDirect> {
+    uint32_t e[2];
+    __device__ __forceinline__ float get(int k) const {
+        if constexpr (std::is_same_v<T, __nv_bfloat16>) return __uint_as_float(e[k] << 16);
+        return widen(*reinterpret_cast<const T*>(&e[k]));
+    }
+    __device__ __forceinline__ void set(T a, T b) {
+        e[0] = *reinterpret_cast<const uint16_t*>(&a);
+        e[1] = *reinterpret_cast<const uint16_t*>(&b);
+    }
+};
 template <>
 struct alignas(8) Two<float> {
     float v[2];
     __device__ __forceinline__ float get(int k) const { return v[k]; }
     __device__ __forceinline__ void set(float a, float b) { v[0] = a, v[1] = b; }
 };
+template <>
+struct Two<float, kDirect> : Two<float> {};
 
 template <Way kWay, typename T>
 __device__ __forceinline__ void store_two(T* p, int lane, int left, const float (&v)[2]) {
@@ -153,12 +167,18 @@ __device__ __forceinline__ void load_if(float (&v)[2], const float* p, bool on) 
                  : "+f"(v[0]), "+f"(v[1])
                  : "l"(p), "r"(uint32_t(on)));
 }
+__device__ __forceinline__ void load_if(float& v, const float* p, bool on) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.f32 %0, [%1];\n}" : "+f"(v) : "l"(p), "r"(uint32_t(on)));
+}
+__device__ __forceinline__ void load_if(uint32_t& v, const uint16_t* p, bool on) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.u16 %0, [%1];\n}" : "+r"(v) : "l"(p), "r"(uint32_t(on)));
+}
 
 // kRun tokens of one activation as they lie in memory; those that do not count (from number
 // `counts` on, and the first one where `skip` says so, and channels from `left` on) are
 // `rest`.
 template <Way kWay, int kRun, typename T>
-__device__ __forceinline__ void load_run(Two<T> (&to)[kRun], const View<const T>& v, int worker, int token, int column,
+__device__ __forceinline__ void load_run(Two<T, kWay> (&to)[kRun], const View<const T>& v, int worker, int token, int column,
                                          int lane, int left, int counts, float rest = 0.0f, bool skip = false) {
     const T* from = v.row(worker, token) + column + (kWay == kVector ? 2 * lane : lane);
     if constexpr (kWay == kVector) {
@@ -177,10 +197,15 @@ __device__ __forceinline__ void load_run(Two<T> (&to)[kRun], const View<const T>
 #pragma unroll
         for (int r = 0; r < kRun; ++r) {
             const T* p = token_of<kWay>(from, v.ts, r);
-            T a = narrow<T>(rest), b = a;
-            if (r < first && (r > 0 || !skip)) a = p[0];
-            if (r < second && (r > 0 || !skip)) b = p[32];
-            to[r].set(a, b);
+            const bool on = r > 0 || !skip;
+            to[r].set(narrow<T>(rest), narrow<T>(rest));
+            if constexpr (sizeof(T) == 2) {
+                load_if(to[r].e[0], reinterpret_cast<const uint16_t*>(p), on && r < first);
+                load_if(to[r].e[1], reinterpret_cast<const uint16_t*>(p + 32), on && r < second);
+            } else {
+                load_if(to[r].v[0], p, on && r < first);
+                load_if(to[r].v[1], p + 32, on && r < second);
+            }
         }
     }
 }
@@ -195,8 +220,8 @@ __device__ __forceinline__ uint32_t load_begins(const RecurrenceArgs<T>& a, int 
 }
 
 // Factor and addend of the run's tokens, and the run as one stretch.
-template <bool kBegins, int kRun, typename T>
-__device__ __forceinline__ void stretch(const Two<T> (&gate)[kRun], const Two<T> (&value)[kRun], uint32_t begin,
+template <bool kBegins, int kRun, typename T, Way kWay>
+__device__ __forceinline__ void stretch(const Two<T, kWay> (&gate)[kRun], const Two<T, kWay> (&value)[kRun], uint32_t begin,
                                         float (&f)[kRun][2], float (&b)[kRun][2], float (&ends)[4]) {
     const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
 #pragma unroll
@@ -229,10 +254,10 @@ __device__ __forceinline__ void through(const float4 (*shared)[32], int part, in
 constexpr int kWarps = 8;  // of a CTA, all of them a strip's, or kTime of them and the others other strips'
 
 // Tokens of a warp's run: as many as leave the next ones on their way too.
-template <typename T>
-constexpr int kRunOf = sizeof(T) == 2 ? 16 : 8;
-template <typename T>
-constexpr int kBackRunOf = sizeof(T) == 2 ? 8 : 4;
+template <typename T, Way kWay = kVector>
+constexpr int kRunOf = sizeof(T) == 2 && kWay == kVector ? 16 : 8;
+template <typename T, Way kWay = kVector>
+constexpr int kBackRunOf = kRunOf<T, kWay> / 2;
 
 // The state that reaches segment p.segment, from the stretches of those before it (behind it:
 // kBack), which the CTA's warps join side by side.  The first one's holds the incoming state
@@ -296,7 +321,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_kernel(Recurr
         load_state<kWay>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, h);
     else if constexpr (kTime == kWarps)
         reach<kWay, false>(a, p, part, lane, left, shared[1][0], h);
-    Two<T> gate[kRun], value[kRun];
+    Two<T, kWay> gate[kRun], value[kRun];
     uint32_t begin;
     const auto ask = [&](int token) {
         load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, to - token, kKeeps);
@@ -519,14 +544,14 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
 // A segment as one stretch: each of the CTA's warps takes a part of its tokens.
 template <typename T, Way kWay, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_ends_kernel(RecurrenceArgs<T> a) {
-    constexpr int kRun = kRunOf<T>;
+    constexpr int kRun = kRunOf<T, kWay>;
     __shared__ float4 shared[kWarps][32];
     const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
     const Place<T> p(a, blockIdx.x);
     const int left = a.d - p.strip, each = (a.segment + kWarps - 1) / kWarps;
     const int first = p.first + part * each, to = min(min(first + each, p.first + a.segment), p.length);
     float whole[4] = {1.0f, 1.0f, 0.0f, 0.0f};
-    Two<T> gate[kRun], value[kRun];
+    Two<T, kWay> gate[kRun], value[kRun];
     uint32_t begin;
     const auto ask = [&](int token) {
         load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, to - token, kKeeps);
@@ -559,8 +584,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_ends_kernel(R
 // from the last token to the first m is the same kind of recurrence, m -> f_t m + f_t dout_t.
 
 // The run as one stretch, from its last token to its first.
-template <bool kBegins, int kRun, typename T>
-__device__ __forceinline__ void back_stretch(const Two<T> (&gate)[kRun], const Two<T> (&dout)[kRun], uint32_t begins,
+template <bool kBegins, int kRun, typename T, Way kWay>
+__device__ __forceinline__ void back_stretch(const Two<T, kWay> (&gate)[kRun], const Two<T, kWay> (&dout)[kRun], uint32_t begins,
                                              float (&ends)[4]) {
     ends[0] = ends[1] = 1.0f;
     ends[2] = ends[3] = 0.0f;
@@ -591,7 +616,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
     else if constexpr (kTime == kWarps)
         reach<kWay, true>(a, p, part, lane, left, shared[1][0], m);
     load_state<kWay>(a.initial == nullptr ? nullptr : a.initial + p.worker * a.initial_stride + p.strip, lane, left, first);
-    Two<T> gate[kRun], dout[kRun], value[kRun], before[kRun];
+    Two<T, kWay> gate[kRun], dout[kRun], value[kRun], before[kRun];
     uint32_t begin;
     const auto ask = [&](int token) {
         const int counts = to - token;
@@ -607,7 +632,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
     if (tiles > 0) ask(token_at(0));  // (without tokens there is no tile, and nothing to read)
     for (int i = 0; i < tiles; ++i) {
         const int token = token_at(i);
-        Two<T> g[kRun], dh[kRun], v[kRun], h[kRun];
+        Two<T, kWay> g[kRun], dh[kRun], v[kRun], h[kRun];
 #pragma unroll
         for (int r = 0; r < kRun; ++r) g[r] = gate[r], dh[r] = dout[r], v[r] = value[r], h[r] = before[r];
         const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
@@ -763,7 +788,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
 
 template <typename T, Way kWay, bool kBegins>
 __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends_kernel(RecurrenceArgs<T> a) {
-    constexpr int kRun = kRunOf<T>;
+    constexpr int kRun = kRunOf<T, kWay>;
     __shared__ float4 shared[kWarps][32];
     const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
     const Place<T> p(a, blockIdx.x);
@@ -771,7 +796,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends
     const int first = p.first + part * each, to = min(min(first + each, p.first + a.segment), p.length);
     float whole[4] = {1.0f, 1.0f, 0.0f, 0.0f};
     const int runs = to > first ? (to - first + kRun - 1) / kRun : 0;
-    Two<T> gate[kRun], dout[kRun];
+    Two<T, kWay> gate[kRun], dout[kRun];
     uint32_t begin = 0;
     const auto ask = [&](int token) {
         load_run<kWay>(gate, a.gate, p.worker, token, p.strip, lane, left, to - token, kKeeps);
@@ -780,7 +805,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_ends
     };
     if (runs > 0) ask(first + (runs - 1) * kRun);
     for (int i = runs - 1; i >= 0; --i) {
-        Two<T> g[kRun], dh[kRun];
+        Two<T, kWay> g[kRun], dh[kRun];
 #pragma unroll
         for (int r = 0; r < kRun; ++r) g[r] = gate[r], dh[r] = dout[r];
         const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
@@ -908,14 +933,14 @@ int by_cluster(int ctas, F f) {
                        : f(std::integral_constant<int, 1>());
 }
 
-// f(warps that share a strip's tile, tokens of a warp's run) as constants: one warp a strip
+// f(way, warps that share a strip's tile, tokens of a warp's run) as constants: one warp a strip
 // where its run holds all tokens, with a short run for few of them.
-template <int kRun, typename F>
-int by_time(int64_t tokens, F f) {
-    if (tokens <= 1) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-    if (tokens <= 4) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-    if (tokens <= kRun) return f(std::integral_constant<int, 1>(), std::integral_constant<int, kRun>());
-    return f(std::integral_constant<int, kWarps>(), std::integral_constant<int, kRun>());
+template <int kRun, typename W, typename F>
+int by_time(W way, int64_t tokens, F f) {
+    if (tokens <= 1) return f(way, std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    if (tokens <= 4) return f(way, std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+    if (tokens <= kRun) return f(way, std::integral_constant<int, 1>(), std::integral_constant<int, kRun>());
+    return f(way, std::integral_constant<int, kWarps>(), std::integral_constant<int, kRun>());
 }
 
 }  // namespace
@@ -979,13 +1004,16 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
                            : launch_tiles<relay_recurrence_tiles_kernel<T, false, kCtas>>(a, maps, units, kCtas, kShared, stream);
             });
         }
-        return by_time<kRunOf<T>>(cut.segment, [&](auto time, auto run) {
+        const auto go = [&](auto way, auto time, auto run) {
+            constexpr Way kWay = decltype(way)::value;
             constexpr int kTime = decltype(time)::value, kRun = decltype(run)::value, kSide = kWarps / kTime;
-            (vec ? (begins != nullptr ? relay_recurrence_kernel<T, kVector, kTime, kRun, true> : relay_recurrence_kernel<T, kVector, kTime, kRun, false>)
-                 : relay_recurrence_kernel<T, kDirect, kTime, kRun, true>)
+            (kWay == kVector && begins == nullptr ? relay_recurrence_kernel<T, kWay, kTime, kRun, kWay == kDirect>
+                                                  : relay_recurrence_kernel<T, kWay, kTime, kRun, true>)
                 <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kWarps, 0, stream>>>(a);
             return status_of_launch();
-        });
+        };
+        return vec ? by_time<kRunOf<T, kVector>>(std::integral_constant<Way, kVector>(), cut.segment, go)
+                   : by_time<kRunOf<T, kDirect>>(std::integral_constant<Way, kDirect>(), cut.segment, go);
     });
 }
 
@@ -1055,14 +1083,16 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
                            : launch_tiles<relay_recurrence_backward_tiles_kernel<T, false, kCtas>>(a, maps, units, kCtas, kShared, stream);
             });
         }
-        return by_time<kBackRunOf<T>>(cut.segment, [&](auto time, auto run) {
+        const auto go = [&](auto way, auto time, auto run) {
+            constexpr Way kWay = decltype(way)::value;
             constexpr int kTime = decltype(time)::value, kRun = decltype(run)::value, kSide = kWarps / kTime;
-            (vec ? (begins != nullptr ? relay_recurrence_backward_kernel<T, kVector, kTime, kRun, true>
-                                      : relay_recurrence_backward_kernel<T, kVector, kTime, kRun, false>)
-                 : relay_recurrence_backward_kernel<T, kDirect, kTime, kRun, true>)
+            (kWay == kVector && begins == nullptr ? relay_recurrence_backward_kernel<T, kWay, kTime, kRun, kWay == kDirect>
+                                                  : relay_recurrence_backward_kernel<T, kWay, kTime, kRun, true>)
                 <<<static_cast<unsigned>((units + kSide - 1) / kSide), 32 * kWarps, 0, stream>>>(a);
             return status_of_launch();
-        });
+        };
+        return vec ? by_time<kBackRunOf<T, kVector>>(std::integral_constant<Way, kVector>(), cut.segment, go)
+                   : by_time<kBackRunOf<T, kDirect>>(std::integral_constant<Way, kDirect>(), cut.segment, go);
     });
 }
 
