@@ -934,12 +934,13 @@ int by_cluster(int ctas, F f) {
 }
 
 // f(way, warps that share a strip's tile, tokens of a warp's run) as constants: one warp a strip
-// where its run holds all tokens, with a short run for few of them.
+// where its run holds all tokens, with a short run for few of them, and two where two runs do.
 template <int kRun, typename W, typename F>
 int by_time(W way, int64_t tokens, F f) {
     if (tokens <= 1) return f(way, std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
     if (tokens <= 4) return f(way, std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
     if (tokens <= kRun) return f(way, std::integral_constant<int, 1>(), std::integral_constant<int, kRun>());
+    if (tokens <= 2 * kRun) return f(way, std::integral_constant<int, 2>(), std::integral_constant<int, kRun>());
     return f(way, std::integral_constant<int, kWarps>(), std::integral_constant<int, kRun>());
 }
 
@@ -974,7 +975,7 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int kTile = kWarps * kRunOf<T>;
-        const bool boxes = vec && tokens > kRunOf<T> && boxed(gate, type, n, tokens, d) && boxed(value, type, n, tokens, d) &&
+        const bool boxes = vec && tokens > 2 * kRunOf<T> && boxed(gate, type, n, tokens, d) && boxed(value, type, n, tokens, d) &&
                            encoder() != nullptr;
         const int ctas = boxes ? cluster_of(static_cast<int64_t>(n) * cut.strips, tokens, kTile) : 0;
         if (ctas > 0) cut.segments = 1, cut.segment = static_cast<int>(tokens);
@@ -1047,7 +1048,7 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int kTile = kWarps * kBackRunOf<T>;
-        bool boxes = vec && tokens > kBackRunOf<T> && encoder() != nullptr;
+        bool boxes = vec && tokens > 2 * kBackRunOf<T> && encoder() != nullptr;
         if (boxes)
             for (const relay_rows* r : {dout, gate, value, out}) boxes = boxes && boxed(r, type, n, tokens, d);
         const int ctas = boxes ? cluster_of(static_cast<int64_t>(n) * cut.strips, tokens, kTile) : 0;

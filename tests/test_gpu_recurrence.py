@@ -102,7 +102,7 @@ def test_types_and_layouts(dtype, layout):
 @pytest.mark.parametrize("what", [(), ("state",), ("packed",), ("lengths",), ("state", "packed"), ("packed", "lengths")],
                          ids=lambda w: "+".join(w) or "plain")
 def test_options(what):
-    for T in (4, 8, 31, 32, 127, 128, 129, 257):
+    for T in (4, 8, 9, 16, 17, 31, 32, 33, 127, 128, 129, 257):
         _check(3, T, 72, torch.bfloat16, what=what, seed=T)
 
 
