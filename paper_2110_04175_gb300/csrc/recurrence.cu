@@ -17,9 +17,9 @@
 // one has A = -0.
 //
 // Memory bounds it where strips are many: [4][4096][4096] in bf16 takes 66 us forward (403 MB,
-// 6.1 TB/s) and 134 to 138 us backward (805 MB, 5.9 TB/s); issue slots are 61 % taken.  With few strips the
+// 6.1 TB/s) and 127 to 138 us backward (805 MB, 5.9 to 6.3 TB/s); issue slots are 61 % taken.  With few strips the
 // chain of joins bounds it: [1][4096][1024] 9 us; [1][50021][257] in fp32, whose rows TMA does
-// not take and whose segments read two rows in three twice, 83 us (154 MB, 1.9 TB/s).
+// not take and whose segments read two rows in three twice, 84 us (154 MB, 1.8 TB/s).
 #include <type_traits>
 
 #include "blackwell.cuh"
