@@ -876,8 +876,9 @@ int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
     for (const relay_rows* in : {dtotal, gate})
         if (in != nullptr && !rows_fit(in, type, n, tokens, d, false)) return RELAY_EINVAL;
     if ((gate == nullptr) != (dgate == nullptr) || (scale == nullptr && dscale != nullptr)) return RELAY_EINVAL;
-    for (const relay_rows* out : {dx, dresidual, dgate})
-        if ((out != nullptr || gate != nullptr || out != dgate) && !rows_fit(out, type, n, tokens, d, true)) return RELAY_EINVAL;
+    if (!rows_fit(dx, type, n, tokens, d, true) || !rows_fit(dresidual, type, n, tokens, d, true) ||
+        (dgate != nullptr && !rows_fit(dgate, type, n, tokens, d, true)))
+        return RELAY_EINVAL;
     if (tokens > 0 && (rstd == nullptr || !aligned(rstd, 4))) return RELAY_EINVAL;
     if (!aligned(lengths, 4)) return RELAY_EINVAL;
     if (!gradient_fits(dpost, dpost_stride, n, d) || !gradient_fits(dpre, dpre_stride, n, d) ||
