@@ -113,6 +113,22 @@ __device__ __forceinline__ void join(float& a, float& b, float a2, float b2) {
     a = kBegins && starts(a2) ? a2 : a * a2;
 }
 
+// A wait for rows that ran out: whatever reaches the run and whatever begins in it, its states and
+// the stretch that it leaves are NaN, up to the next beginning in rows that did come.
+template <int kRun>
+__device__ __forceinline__ void lose(float (&b)[kRun][2]) {
+#pragma unroll
+    for (int r = 0; r < kRun; ++r) b[r][0] = b[r][1] = NAN;
+}
+
+// The same on the way back, where a run's gradients are made of f and 1 - f.
+template <int kRun>
+__device__ __forceinline__ void lose(float (&at)[kRun][2], float (&rest)[kRun][2], float (&ends)[4]) {
+#pragma unroll
+    for (int r = 0; r < kRun; ++r) at[r][0] = at[r][1] = rest[r][0] = rest[r][1] = NAN;
+    ends[2] = ends[3] = NAN;
+}
+
 // ------------------------------------------------------------------- the kernels
 
 template <typename T>
@@ -504,12 +520,12 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
                 b[r][k] = g.rest * value.get(k);
             }
         }
+        if (!ok) lose(b);
         if (counts < kRun) {
 #pragma unroll
             for (int r = 0; r < kRun; ++r)
                 if (r >= counts) f[r][0] = f[r][1] = 1.0f, b[r][0] = b[r][1] = 0.0f;
         }
-        if (!ok) b[0][0] = b[0][1] = __int_as_float(0x7fffffff);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             ends[k] = f[0][k], ends[2 + k] = b[0][k];
@@ -583,6 +599,21 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_ends_kernel(R
 //   l_t = dout_t + m_{t+1},  dv_t = l_t (1 - f_t),  dgate_t = l_t (h_{t-1} - v_t) f_t (1 - f_t):
 // from the last token to the first m is the same kind of recurrence, m -> f_t m + f_t dout_t.
 
+// One token on the way back: `m` comes from behind it and goes on before it.
+__device__ __forceinline__ void back_step(bool starts, float at, float rest, float dout, float before, float value, float& m,
+                                          float& dg, float& dv) {
+    const float l = dout + m;
+    dv = l * rest;
+    dg = dv * at * (before - value);
+    m = starts ? 0.0f : at * l;
+}
+
+// The stretch (a, b) with the token before it.
+__device__ __forceinline__ void back_join(bool starts, float at, float dout, float& a, float& b) {
+    a = starts ? -0.0f : a * at;
+    b = starts ? 0.0f : at * (b + dout);
+}
+
 // The run as one stretch, from its last token to its first.
 template <bool kBegins, int kRun, typename T, Way kWay>
 __device__ __forceinline__ void back_stretch(const Two<T, kWay> (&gate)[kRun], const Two<T, kWay> (&dout)[kRun], uint32_t begins,
@@ -594,9 +625,7 @@ __device__ __forceinline__ void back_stretch(const Two<T, kWay> (&gate)[kRun], c
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const Gate<T> g(gate[r].get(k));
-            const bool begin = kBegins && (begins >> r & 1);
-            ends[k] = begin ? -0.0f : ends[k] * g.at;
-            ends[2 + k] = begin ? 0.0f : g.at * (ends[2 + k] + dout[r].get(k));
+            back_join(kBegins && (begins >> r & 1), g.at, dout[r].get(k), ends[k], ends[2 + k]);
         }
 }
 
@@ -652,11 +681,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) relay_recurrence_backward_kern
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const Gate<T> s(g[r].get(k));
-                const float l = dh[r].get(k) + x[k];
                 const float h0 = starts ? 0.0f : r == 0 && token == 0 ? first[k] : h[r].get(k);
-                dv[k] = l * s.rest;
-                dg[k] = dv[k] * s.at * (h0 - v[r].get(k));
-                x[k] = starts ? 0.0f : s.at * l;
+                back_step(starts, s.at, s.rest, dh[r].get(k), h0, v[r].get(k), x[k], dg[k], dv[k]);
             }
         };
         if (token + kRun <= to) {
@@ -737,14 +763,10 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
             for (int k = 0; k < 2; ++k) {
                 const Gate<T> g(gate.get(k));
                 at[r][k] = g.at, rest[r][k] = g.rest;
-                if (r < counts) {
-                    const bool starts = kBegins && (begins >> r & 1);
-                    ends[k] = starts ? -0.0f : ends[k] * g.at;
-                    ends[2 + k] = starts ? 0.0f : g.at * (ends[2 + k] + dout.get(k));
-                }
+                if (r < counts) back_join(kBegins && (begins >> r & 1), g.at, dout.get(k), ends[k], ends[2 + k]);
             }
         }
-        if (!ok) ends[2] = ends[3] = m[0] = m[1] = __int_as_float(0x7fffffff);
+        if (!ok && counts > 0) lose(at, rest, ends);
         hand_on<kCtas, kBegins>(shared[i & 1], joined, i & 1, rank, part, lane, ends, m, x);
         if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
         T *to_gate = a.dgate.row(p.worker, token) + p.strip, *to_value = a.dvalue.row(p.worker, token) + p.strip;
@@ -754,11 +776,8 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
             const bool starts = kBegins && (begins >> r & 1);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float l = dout.get(k) + x[k];
                 const float h0 = starts ? 0.0f : r == 0 && token == 0 ? first[k] : before.get(k);
-                dv[k] = l * rest[r][k];
-                dg[k] = dv[k] * at[r][k] * (h0 - value.get(k));
-                x[k] = starts ? 0.0f : at[r][k] * l;
+                back_step(starts, at[r][k], rest[r][k], dout.get(k), h0, value.get(k), x[k], dg[k], dv[k]);
             }
         };
         if (counts >= kRun) {
