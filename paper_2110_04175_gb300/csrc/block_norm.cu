@@ -357,6 +357,10 @@ struct BlockBackwardArgs {
     int32_t tokens, d, pitch;
 };
 
+// The factor of a row's norm where the row has come; NaN where the wait for it ran out, which
+// makes everything NaN that Features make of the row.
+__device__ __forceinline__ float factor_of(bool came, float s) { return came ? s : NAN; }
+
 // What a lane makes again of 2 kPairs features of a row, two at a time: `xhat`, `p`, `r` come as x,
 // gate and residual; w and rho are w_post and rho (1 without).
 template <typename T, int kPairs>
@@ -580,9 +584,10 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
     int i = 0;
     for (int token = begin; token < length; token += step, ++i) {
         const int s = i % 2;
-        const float sx = next_x, sh = next_h;
+        const float row_x = next_x, row_h = next_h;
         if (token + step < length) next_x = factors[token + step], next_h = factors[second + token + step];
         ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / R::kStages & 1);
+        const float sx = factor_of(ok, row_x), sh = factor_of(ok, row_h);
         const auto remake = [&](int j, Features<T, 2>& o, Pair (&w)[2], Pair (&rho)[2], Pair (&pre)[2], Pair (&u)[2], Pair (&over)[2]) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             const bool on = at < a.d;
@@ -609,7 +614,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
         }
         float three[3];
 #pragma unroll
-        for (int e = 0; e < 3; ++e) three[e] = ok ? parts[e].sum() : __int_as_float(0x7fffffff);
+        for (int e = 0; e < 3; ++e) three[e] = parts[e].sum();
         group_sum(three, shared[i & 1][group], group, part, lane);
         // here every warp of the group is done with the row before this one
         if (brings && i > 0 && token + step < length) bring(token + step, s ^ 1);
