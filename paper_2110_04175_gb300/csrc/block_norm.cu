@@ -136,8 +136,9 @@ relay_block_norm_kernel(BlockArgs<T> a) {
 
 #if RELAY_PASS == 1
 
-// The 8-bit format of four features a lane, a block on eight lanes: layers.cuh's put_strip.
-__device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at, int lane, const Pair (&v)[2]) {
+// The 8-bit format of four features a lane, a block on eight lanes: layers.cuh's put_strip.  `on`:
+// there are any; past d v is 0, or NaN in a row whose factors are, and such a block's scale stays 7.
+__device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at, int lane, bool on, const Pair (&v)[2]) {
     const float e[4] = {v[0].v.x, v[0].v.y, v[1].v.x, v[1].v.y};
     uint32_t most = max(max(magnitude(e[0]), magnitude(e[1])), max(magnitude(e[2]), magnitude(e[3])));
 #pragma unroll
@@ -146,7 +147,7 @@ __device__ __forceinline__ void put_quad(int8_t* codes, uint8_t* scales, int at,
     const uint32_t ab = __byte_perm(code_bits(e[0], c), code_bits(e[1], c), 0x0040);
     const uint32_t cd = __byte_perm(code_bits(e[2], c), code_bits(e[3], c), 0x0040);
     *reinterpret_cast<uint32_t*>(codes + at) = c == 255u ? 0u : __byte_perm(ab, cd, 0x5410);
-    if (lane % 8 == 0) scales[at / kBlock] = static_cast<uint8_t>(c);
+    if (lane % 8 == 0) scales[at / kBlock] = static_cast<uint8_t>(on ? c : 7u);
 }
 
 #endif  // RELAY_PASS
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
             weight_at<R>(weights, 1, a.pre, worker, at, on, w);
 #pragma unroll
             for (int k = 0; k < 2; ++k) h[j][k] = h[j][k] * Pair(sh);
-            if (a.codes != nullptr) put_quad(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), at, lane, h[j]);
+            if (a.codes != nullptr) put_quad(a.codes + row * a.pitch, a.scales + row * (a.pitch / kBlock), at, lane, on, h[j]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) h[j][k] = h[j][k] * w[k];
             store_quad(a.y.row(worker, token) + at, on, h[j]);
