@@ -1008,15 +1008,16 @@ int relay_recurrence(int32_t type, int32_t n, int64_t tokens, int64_t d, const r
         a.n = n, a.tokens = static_cast<int32_t>(tokens), a.d = static_cast<int32_t>(d);
         a.strips = cut.strips, a.segments = cut.segments, a.segment = cut.segment;
         const int64_t units = static_cast<int64_t>(n) * cut.segments * cut.strips;
+        TileMaps<T> maps{};  // before anything is enqueued
+        if (boxes && (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile)))
+            return RELAY_ECUDA;
         if (cut.segments > 1) {
             (vec ? (begins != nullptr ? relay_recurrence_ends_kernel<T, kVector, true> : relay_recurrence_ends_kernel<T, kVector, false>)
                  : relay_recurrence_ends_kernel<T, kDirect, true>)
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
+            if (const int rc = status_of_launch()) return rc;
         }
         if (boxes) {
-            TileMaps<T> maps{};
-            if (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile))
-                return RELAY_ECUDA;
             return by_cluster(ctas, [&](auto with) {
                 constexpr int kCtas = decltype(with)::value, kShared = Boxes<T, 2, kTile>::kShared;
                 return begins != nullptr
@@ -1085,17 +1086,18 @@ int relay_recurrence_backward(int32_t type, int32_t n, int64_t tokens, int64_t d
         a.n = n, a.tokens = static_cast<int32_t>(tokens), a.d = static_cast<int32_t>(d);
         a.strips = cut.strips, a.segments = cut.segments, a.segment = cut.segment;
         const int64_t units = static_cast<int64_t>(n) * cut.segments * cut.strips;
+        TileMaps<T> maps{};  // before anything is enqueued
+        if (boxes && (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile) ||
+                      !map_tiles(&maps.dout, dout, type, n, tokens, d, kTile) || !map_tiles(&maps.out, out, type, n, tokens, d, kTile)))
+            return RELAY_ECUDA;
         if (cut.segments > 1) {
             (vec ? (begins != nullptr ? relay_recurrence_backward_ends_kernel<T, kVector, true>
                                       : relay_recurrence_backward_ends_kernel<T, kVector, false>)
                  : relay_recurrence_backward_ends_kernel<T, kDirect, true>)
                 <<<static_cast<unsigned>(units), 32 * kWarps, 0, stream>>>(a);
+            if (const int rc = status_of_launch()) return rc;
         }
         if (boxes) {
-            TileMaps<T> maps{};
-            if (!map_tiles(&maps.gate, gate, type, n, tokens, d, kTile) || !map_tiles(&maps.value, value, type, n, tokens, d, kTile) ||
-                !map_tiles(&maps.dout, dout, type, n, tokens, d, kTile) || !map_tiles(&maps.out, out, type, n, tokens, d, kTile))
-                return RELAY_ECUDA;
             return by_cluster(ctas, [&](auto with) {
                 constexpr int kCtas = decltype(with)::value, kShared = Boxes<T, 4, kTile>::kShared;
                 return begins != nullptr
