@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <climits>
 #include <cstdint>
 
 namespace {
@@ -95,6 +96,36 @@ __device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity)
     } while (__all_sync(0xffffffffu, clock64() - start < kPatience));
     return false;
 }
+
+// What goes through kStages places of shared memory by copies, number after number from 0 on: a
+// barrier a place (one arrival, that of the thread that asks), and the phase in which a number lands.
+// In number i's turn the readers of number i - kBehind are done with its place, and one thread asks
+// for what comes there next.
+template <int kStages, int kBehind>
+struct Numbers {
+    uint32_t bars;
+    int lost = INT_MAX;  // the first number that was waited for in vain
+    __device__ __forceinline__ static int place(int i) { return i % kStages; }
+    __device__ __forceinline__ uint32_t bar(int i) const { return bars + 8 * place(i); }
+    __device__ __forceinline__ static uint32_t parity(int i) { return i / kStages & 1; }
+    // Number i is there; false from the first wait on that ran out, after about a second.  All lanes
+    // of a warp.
+    __device__ __forceinline__ bool wait(int i) {
+        if (lost == INT_MAX && !barrier_wait_warp(bar(i), parity(i))) lost = i;
+        return lost == INT_MAX;
+    }
+    // The number to ask for in number i's turn, if there are as many, and whether it may be (the first
+    // kStages are asked for before).  Not once a wait has run out: its phase has not ended, and
+    // takes no second arrival.
+    __device__ __forceinline__ static int next(int i) { return i - kBehind + kStages; }
+    __device__ __forceinline__ bool asks(int i) const { return i >= kBehind && lost == INT_MAX; }
+    // Before the end: none of the copies is in flight (about a second each at most).  They have been
+    // waited for before, unless a wait ran out.  The thread that asks.
+    __device__ __forceinline__ void drain(int count) const {
+        const int asked = lost == INT_MAX ? count : min(count, max(lost - kBehind, 0) + kStages);
+        for (int i = max(0, asked - kStages); i < asked; ++i) barrier_wait(bar(i), parity(i));
+    }
+};
 
 // A count in shared memory that one thread raises, and another's wait until it is `least` or
 // more (false after about a second): what the one has seen before, the other sees after.

@@ -224,13 +224,6 @@ __device__ __forceinline__ void group_sum(float (&v)[kCount], float (&shared)[kP
     }
 }
 
-// Before a group's end: waits (about a second at most) for the copies of its last rows.
-// They have been waited for before, unless a wait ran out.
-__device__ __forceinline__ void none_in_flight(const uint64_t* bars, int stages, int rows) {
-    for (int i = max(0, rows - stages); i < rows; ++i)
-        if (!barrier_wait(shared_address(bars + i % stages), i / stages & 1)) break;
-}
-
 // kWhole: every warp has all its quads.  A wait that runs out makes a group's results from there
 // on NaN.
 template <typename T, int kParts, bool kWhole>
@@ -254,24 +247,23 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
     const bool brings = part == 0 && elected();
     uint8_t* mine = ring + group * (R::kStages * R::kStage);
-    const auto bring = [&](int token, int s) {  // one thread of the group
-        const uint32_t bar = shared_address(&bars[group][s]), to = shared_address(mine + s * R::kStage);
+    Numbers<R::kStages, 0> numbers{shared_address(&bars[group][0])};
+    const auto bring = [&](int token, int i) {  // one thread of the group: its row number i
+        const uint32_t bar = numbers.bar(i), to = shared_address(mine + numbers.place(i) * R::kStage);
         barrier_expect(bar, bytes * (2 + gated));
         copy_row(to, a.x.row(worker, token), bytes, bar);
         copy_row(to + R::kRow, a.residual.row(worker, token), bytes, bar);
         if (gated) copy_row(to + 2 * R::kRow, a.gate.row(worker, token), bytes, bar);
     };
     if (brings)
-        for (int s = 0; s < R::kStages; ++s)
-            if (begin + s * step < a.tokens) bring(begin + s * step, s);
+        for (int i = 0; i < R::kStages; ++i)
+            if (begin + i * step < a.tokens) bring(begin + i * step, i);
     const float over_d = 1.0f / static_cast<float>(a.d);
-    bool ok = true;
     int i = 0;
     for (int token = begin; token < a.tokens; token += step, ++i) {
-        const int s = i % R::kStages;
         const int64_t row = static_cast<int64_t>(worker) * a.tokens + token;
-        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / R::kStages & 1);
-        const T* from = reinterpret_cast<const T*>(mine + s * R::kStage);
+        const bool ok = numbers.wait(i);
+        const T* from = reinterpret_cast<const T*>(mine + numbers.place(i) * R::kStage);
         constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
         Pair h[R::kHold][2], squares(0.0f);
 #pragma unroll
@@ -307,7 +299,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
         sum[0] = squares.sum();
         group_sum(sum, shared[1][group], group, part, lane);
         // here every warp of the group is done with the row in shared memory
-        if (brings && token + R::kStages * step < a.tokens) bring(token + R::kStages * step, s);
+        if (brings && numbers.asks(i) && token + R::kStages * step < a.tokens) bring(token + R::kStages * step, numbers.next(i));
         const float sh = 1.0f / sqrtf(sum[0] * over_d + a.eps);
         if (a.rstd != nullptr && part == 0 && lane == 0) {
             a.rstd[row] = sx;
@@ -329,7 +321,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 3>::kWarps, 1) relay_bloc
             store_quad(a.y.row(worker, token) + at, on, h[j]);
         }
     }
-    if (brings) none_in_flight(&bars[group][0], R::kStages, i);
+    if (brings) numbers.drain(i);
 }
 
 #if RELAY_PASS == 2
@@ -559,8 +551,9 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
     const int step = static_cast<int>(gridDim.x) * R::kGroups, begin = static_cast<int>(blockIdx.x) * R::kGroups + group;
     const bool brings = part == 0 && elected();
     uint8_t* mine = ring + group * (R::kStages * R::kStage);
-    const auto bring = [&](int token, int s) {  // one thread of the group
-        const uint32_t bar = shared_address(&bars[group][s]), to = shared_address(mine + s * R::kStage);
+    Numbers<R::kStages, 1> numbers{shared_address(&bars[group][0])};
+    const auto bring = [&](int token, int i) {  // one thread of the group: its row number i
+        const uint32_t bar = numbers.bar(i), to = shared_address(mine + numbers.place(i) * R::kStage);
         barrier_expect(bar, bytes * (3 + gated + over_too));
         copy_row(to, a.x.row(worker, token), bytes, bar);
         copy_row(to + R::kRow, a.residual.row(worker, token), bytes, bar);
@@ -568,10 +561,9 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
         if (gated) copy_row(to + 3 * R::kRow, a.gate.row(worker, token), bytes, bar);
         if (over_too) copy_row(to + 4 * R::kRow, a.dtotal.row(worker, token), bytes, bar);
     };
-    if (brings) {
-        if (begin < length) bring(begin, 0);
-        if (begin + step < length) bring(begin + step, 1);
-    }
+    if (brings)
+        for (int i = 0; i < R::kStages; ++i)
+            if (begin + i * step < length) bring(begin + i * step, i);
     Pair dpost[4][2], dpre[4][2], dscale[4][2];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -581,18 +573,16 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
     const int64_t second = static_cast<int64_t>(n) * a.tokens;
     float next_x = begin < length ? factors[begin] : 0.0f, next_h = begin < length ? factors[second + begin] : 0.0f;
     const float over_d = 1.0f / static_cast<float>(a.d);
-    bool ok = true;
     int i = 0;
     for (int token = begin; token < length; token += step, ++i) {
-        const int s = i % 2;
         const float row_x = next_x, row_h = next_h;
         if (token + step < length) next_x = factors[token + step], next_h = factors[second + token + step];
-        ok = ok && barrier_wait_warp(shared_address(&bars[group][s]), i / R::kStages & 1);
+        const bool ok = numbers.wait(i);
         const float sx = factor_of(ok, row_x), sh = factor_of(ok, row_h);
         const auto remake = [&](int j, Features<T, 2>& o, Pair (&w)[2], Pair (&rho)[2], Pair (&pre)[2], Pair (&u)[2], Pair (&over)[2]) {
             const int at = (part + kParts * j) * kQuads + 4 * lane;
             const bool on = at < a.d;
-            const T* from = reinterpret_cast<const T*>(mine + s * R::kStage) + at;
+            const T* from = reinterpret_cast<const T*>(mine + numbers.place(i) * R::kStage) + at;
             constexpr int kNext = R::kRow / static_cast<int>(sizeof(T));
             load_quad(from, true, o.xhat);
             load_quad(from + kNext, true, o.r);
@@ -618,7 +608,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
         for (int e = 0; e < 3; ++e) three[e] = parts[e].sum();
         group_sum(three, shared[i & 1][group], group, part, lane);
         // here every warp of the group is done with the row before this one
-        if (brings && i > 0 && token + step < length) bring(token + step, s ^ 1);
+        if (brings && numbers.asks(i) && token + step < length) bring(token + step, numbers.next(i));
         const float along = three[0] * over_d, along_x = three[1] * over_d - sh * along * (three[2] * over_d);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -634,7 +624,7 @@ __global__ void __launch_bounds__(32 * Ring<T, kParts, 5>::kWarps, 1) relay_bloc
             if (gated) store_quad(a.dgate.row(worker, token) + at, on, dz);
         }
     }
-    if (brings) none_in_flight(&bars[group][0], R::kStages, i);
+    if (brings) numbers.drain(i);
     // padding
     for (int token = begin + i * step; token < a.tokens; token += step) {
         const Pair none[2] = {Pair(0.0f), Pair(0.0f)};

@@ -402,32 +402,23 @@ template <typename T, int kBoxes, int kTile>
 struct Boxes {
     static constexpr int kBox = kTile * kWide * static_cast<int>(sizeof(T)), kStage = kBoxes * kBox;
     static constexpr int kShared = kStages * kStage + 128;
-    uint32_t bars, ring;  // in shared memory
+    Numbers<kStages, 1> tiles;
+    uint32_t ring;  // in shared memory
     const uint8_t* at;
     __device__ __forceinline__ Boxes(uint64_t* barriers, uint8_t* raw) {
         const uint32_t pad = (128 - shared_address(raw) % 128) % 128;
-        bars = shared_address(barriers), ring = shared_address(raw) + pad, at = raw + pad;
-        if (threadIdx.x < kStages) barrier_init(bars + 8 * threadIdx.x, 1);
+        tiles.bars = shared_address(barriers), ring = shared_address(raw) + pad, at = raw + pad;
+        if (threadIdx.x < kStages) barrier_init(tiles.bar(threadIdx.x), 1);
         barriers_ready();
         __syncthreads();
     }
     __device__ __forceinline__ uint32_t expect(int tile) const {  // returns the stage's place
-        const int s = tile % kStages;
-        barrier_expect(bars + 8 * s, kStage);
-        return ring + s * kStage;
-    }
-    __device__ __forceinline__ uint32_t bar(int tile) const { return bars + 8 * (tile % kStages); }
-    // false after about a second; from then on nothing is waited for
-    __device__ __forceinline__ bool wait(int tile) const { return barrier_wait_warp(bar(tile), tile / kStages & 1); }
-    // Before the end: waits (about a second at most) for the last tiles' copies, which have been
-    // waited for before unless a wait ran out.  One thread.
-    __device__ __forceinline__ void none_in_flight(int tiles) const {
-        for (int i = max(0, tiles - kStages); i < tiles; ++i)
-            if (!barrier_wait(bar(i), i / kStages & 1)) break;
+        barrier_expect(tiles.bar(tile), kStage);
+        return ring + tiles.place(tile) * kStage;
     }
     // The lane's two channels of token `token` of box `box`.
     __device__ __forceinline__ Two<T> get(int tile, int box, int token, int lane) const {
-        return reinterpret_cast<const Two<T>*>(at + tile % kStages * kStage + box * kBox)[token * (kWide / 2) + lane];
+        return reinterpret_cast<const Two<T>*>(at + tiles.place(tile) * kStage + box * kBox)[token * (kWide / 2) + lane];
     }
 };
 
@@ -480,7 +471,7 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
     __shared__ __align__(8) uint64_t barriers[kStages];
     __shared__ float4 shared[2][kWarps][32];
     __shared__ Joined<kCtas> joined;
-    const Boxes<T, 2, kTile> boxes(barriers, raw);
+    Boxes<T, 2, kTile> boxes(barriers, raw);
     const int lane = threadIdx.x % 32, part = threadIdx.x / 32, rank = kCtas == 1 ? 0 : static_cast<int>(cluster_rank());
     const Place<T> p(a, blockIdx.x / kCtas);
     // rounds of kCtas tiles; this CTA's tile of a round
@@ -489,8 +480,8 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
     const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
     const auto bring = [&](int i) {  // one thread
         const uint32_t at = boxes.expect(i);
-        copy_box(at, &maps.gate, p.strip, first_of(i), p.worker, boxes.bar(i));
-        copy_box(at + boxes.kBox, &maps.value, p.strip, first_of(i), p.worker, boxes.bar(i));
+        copy_box(at, &maps.gate, p.strip, first_of(i), p.worker, boxes.tiles.bar(i));
+        copy_box(at + boxes.kBox, &maps.value, p.strip, first_of(i), p.worker, boxes.tiles.bar(i));
     };
     if (threadIdx.x == 0)
         for (int i = 0; i < min(kStages, tiles); ++i) bring(i);
@@ -502,13 +493,12 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
         reach<kVector, false>(a, p, part, lane, left, shared[1], h);
     const int start = first_of(0) + part * kRun;
     uint32_t begin = load_begins<kRun, kBegins>(a, p.worker, start, lane, to - start);
-    bool ok = true;
     for (int i = 0; i < tiles; ++i) {
         const int token = first_of(i) + part * kRun, counts = to - token;
         const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
         if (kBegins && i + 1 < tiles)
             begin = load_begins<kRun, kBegins>(a, p.worker, token + kCtas * kTile, lane, counts - kCtas * kTile);
-        ok = ok && boxes.wait(i);
+        const bool ok = boxes.tiles.wait(i);
         float f[kRun][2], b[kRun][2], ends[4], x[2];
 #pragma unroll
         for (int r = 0; r < kRun; ++r) {
@@ -533,7 +523,8 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
             for (int r = 1; r < kRun; ++r) join<kBegins>(ends[k], ends[2 + k], f[r][k], b[r][k]);
         }
         hand_on<kCtas, kBegins>(shared[i & 1], joined, i & 1, rank, part, lane, ends, h, x);
-        if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
+        const int next = boxes.tiles.asks(i) && boxes.tiles.next(i) < tiles ? boxes.tiles.next(i) : -1;
+        if (threadIdx.x == 0 && next >= 0) bring(next);
         T* out = a.out.row(p.worker, token) + p.strip;
         if (counts >= kRun) {
 #pragma unroll
@@ -552,7 +543,7 @@ relay_recurrence_tiles_kernel(const __grid_constant__ RecurrenceArgs<T> a, const
             }
         }
     }
-    if (threadIdx.x == 0) boxes.none_in_flight(tiles);
+    if (threadIdx.x == 0) boxes.tiles.drain(tiles);
     if (p.segment == a.segments - 1 && a.last != nullptr && part == 0 && rank == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, h);
 }
@@ -720,7 +711,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
     __shared__ __align__(8) uint64_t barriers[kStages];
     __shared__ float4 shared[2][kWarps][32];
     __shared__ Joined<kCtas> joined;
-    const Boxes<T, 4, kTile> boxes(barriers, raw);
+    Boxes<T, 4, kTile> boxes(barriers, raw);
     const int lane = threadIdx.x % 32, part = threadIdx.x / 32, rank = kCtas == 1 ? 0 : static_cast<int>(cluster_rank());
     const Place<T> p(a, blockIdx.x / kCtas);
     const int left = a.d - p.strip, tiles = (min(a.segment, a.tokens) + kCtas * kTile - 1) / (kCtas * kTile);
@@ -728,7 +719,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
     const auto first_of = [&](int i) { return p.first + ((tiles - 1 - i) * kCtas + kCtas - 1 - rank) * kTile; };
     const int end = min(p.first + a.segment, a.tokens), to = min(end, p.length);
     const auto bring = [&](int i) {  // one thread
-        const uint32_t at = boxes.expect(i), bar = boxes.bar(i);
+        const uint32_t at = boxes.expect(i), bar = boxes.tiles.bar(i);
         const int token = first_of(i);
         copy_box(at, &maps.gate, p.strip, token, p.worker, bar);
         copy_box(at + boxes.kBox, &maps.dout, p.strip, token, p.worker, bar);
@@ -748,13 +739,12 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
     const int place = (kWarps - 1 - part) * kRun;
     const auto token_at = [&](int i) { return first_of(i) + place; };
     uint32_t begin = tiles > 0 ? load_begins<kRun, kBegins>(a, p.worker, token_at(0), lane, to - token_at(0)) : 0;
-    bool ok = true;
     for (int i = 0; i < tiles; ++i) {
         const int token = token_at(i), counts = to - token;
         const uint32_t begins = kBegins ? __ballot_sync(0xffffffffu, begin != 0) : 0u;
         if (kBegins && i + 1 < tiles)
             begin = load_begins<kRun, kBegins>(a, p.worker, token - kCtas * kTile, lane, counts + kCtas * kTile);
-        ok = ok && boxes.wait(i);
+        const bool ok = boxes.tiles.wait(i);
         float at[kRun][2], rest[kRun][2], ends[4] = {1.0f, 1.0f, 0.0f, 0.0f}, x[2];
 #pragma unroll
         for (int r = kRun - 1; r >= 0; --r) {
@@ -768,7 +758,8 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
         }
         if (!ok && counts > 0) lose(at, rest, ends);
         hand_on<kCtas, kBegins>(shared[i & 1], joined, i & 1, rank, part, lane, ends, m, x);
-        if (threadIdx.x == 0 && i > 0 && i - 1 + kStages < tiles) bring(i - 1 + kStages);
+        const int next = boxes.tiles.asks(i) && boxes.tiles.next(i) < tiles ? boxes.tiles.next(i) : -1;
+        if (threadIdx.x == 0 && next >= 0) bring(next);
         T *to_gate = a.dgate.row(p.worker, token) + p.strip, *to_value = a.dvalue.row(p.worker, token) + p.strip;
         const auto step = [&](int r, float (&dg)[2], float (&dv)[2]) {
             const Two<T> dout = boxes.get(i, 1, place + r, lane), value = boxes.get(i, 2, place + r, lane),
@@ -800,7 +791,7 @@ relay_recurrence_backward_tiles_kernel(const __grid_constant__ RecurrenceArgs<T>
             }
         }
     }
-    if (threadIdx.x == 0) boxes.none_in_flight(tiles);
+    if (threadIdx.x == 0) boxes.tiles.drain(tiles);
     if (p.segment == 0 && a.last != nullptr && part == 0 && rank == 0)
         store_state<kVector>(a.last + p.worker * a.last_stride + p.strip, lane, left, m);
 }
