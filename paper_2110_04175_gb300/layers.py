@@ -401,8 +401,9 @@ def relay_orthogonalise(update, out, workspace, steps: int = 5, eps: float = 1e-
     to one another) made nearly orthogonal, each matrix by itself, by Newton-Schulz steps from
     update / (|update| + eps).  out may be update itself."""
     lib = _library()
-    if not isinstance(update, torch.Tensor) or update.dim() != 3:
-        _refuse("update", update, "an fp32 tensor [n][rows][columns] is needed")
+    for name, t in (("update", update), ("out", out)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            _refuse(name, t, "an fp32 tensor [n][rows][columns] is needed")
     n, rows, columns = update.shape
     _rows("update", update, torch.float32, update.shape)
     _rows("out", out, torch.float32, update.shape)
