@@ -38,7 +38,9 @@
  *     them.  A weight that all workers share has stride 0, and a gradient
  *     per worker.
  *   - Arithmetic is in fp32, and each output is rounded once, to the nearest
- *     (y and xhat come from the unrounded h).  The results of a call are the
+ *     (y and xhat come from the unrounded h).  sigma of 16-bit gates is off by
+ *     less than (3 + |g|) 2^-23 relative, by which an 8-bit code behind it can
+ *     land beside the nearest one.  The results of a call are the
  *     same bits every time: no atomics.
  *   - Lengths.  Where a call sums over tokens or goes along them, `lengths`
  *     (device int32 [n], or NULL for all) says how many of each worker's rows
@@ -199,7 +201,10 @@ int64_t relay_block_norm_backward_workspace(int32_t n, int64_t tokens, int64_t d
  * again): of x, of the gate (given and asked for together), of the residual,
  * and per worker, overwritten, of post, pre and scale (dscale may be NULL).
  * dtotal: the gradient that reaches h past the second norm, or NULL.  Rows
- * past the lengths count nowhere and get gradients of 0. */
+ * past the lengths count nowhere and get gradients of 0.  The mean that dx
+ * takes off is a difference of sums over the row, whose terms are those of
+ * sigma(gate) x s_x post times h's gradient: off by what fp32 leaves of them,
+ * also where dx itself is small. */
 int relay_block_norm_backward(int32_t type, int32_t n, int64_t tokens, int64_t d, const relay_rows *dy,
                               const relay_rows *dtotal, const relay_rows *x, const relay_rows *gate,
                               const relay_rows *residual, const float *post, int64_t post_stride, const float *pre,
@@ -253,8 +258,9 @@ int64_t relay_orthogonalise_workspace(int32_t n, int64_t rows, int64_t columns);
  * or the same from the other side where rows outnumber columns; out = scale x.
  * Five steps bring singular values from 0.002 of |update| up to between 0.68
  * and 1.21.  Element (i, r, c) is at update + i worker_stride + r row_stride +
- * c; out likewise, and may be the view of update.  Operands are held in 22 to
- * 23 bits and summed in fp32.  A matrix of zeros stays zero; one that holds a
+ * c; out likewise, and may be the view of update.  The coefficients are those
+ * of the Muon optimiser (K. Jordan and others, 2024).  Operands are held in 22
+ * to 23 bits and summed in fp32.  A matrix of zeros stays zero; one that holds a
  * value that is not finite becomes NaN, all of it.  rows, columns <=
  * RELAY_ORTHOGONALISE_MAX, steps in 1 .. RELAY_ORTHOGONALISE_MAX_STEPS, eps >=
  * 0.  The kernel's waits end after about a second each; results that one of

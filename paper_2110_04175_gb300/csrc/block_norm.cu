@@ -713,8 +713,6 @@ bool by_ring(int64_t d, F f) {
     return false;
 }
 
-inline int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }  // of a worker
-
 // Whether rows go through shared memory: where that is faster, by what was measured, old way and
 // this one in us, 4 workers:
 //   backward  [512 rows][1000] bf16  10.5 12.6, [1024][1000] 14.7 12.7, [16384][512] 58 37,
@@ -733,7 +731,11 @@ Weight weight_of(const float* p, int64_t stride, int32_t n, int64_t d) {
     return Weight{p, n > 1 ? stride : 0, d % 8 == 0 && aligned(p, 16) && (n == 1 || stride % 4 == 0)};
 }
 
-#if RELAY_PASS == 2
+#if RELAY_PASS == 1
+
+int64_t ring_ctas(int32_t n) { return 152 > n ? 152 / n : 1; }  // of a worker
+
+#else
 
 // Calls f(kParts, kStrips) for the backward pass, whose sums over the tokens take three
 // times a strip's registers: one strip a warp as far as a CTA's 32 warps go.

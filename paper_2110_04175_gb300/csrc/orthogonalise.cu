@@ -3,7 +3,8 @@
 //
 //   x = u / (|u| + eps);  a step: g = x x^T,  x <- a x + (b g + c g g) x
 //
-// with x as wide as it is high or wider (u or its transpose).  Three products a step, on the
+// with the coefficients of the Muon optimiser (K. Jordan and others, 2024) and x as wide as it is
+// high or wider (u or its transpose).  Three products a step, on the
 // tensor cores, bound by them where matrices are large and by the way from product to product
 // where they are small.
 //

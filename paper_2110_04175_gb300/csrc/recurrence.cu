@@ -18,7 +18,7 @@
 //
 // Memory bounds it where strips are many: [4][4096][4096] in bf16 takes 66 us forward (403 MB,
 // 6.1 TB/s) and 127 to 138 us backward (805 MB, 5.9 to 6.3 TB/s); issue slots are 61 % taken.  With few strips the
-// chain of joins bounds it: [1][4096][1024] 9 us; [1][50021][257] in fp32, whose rows TMA does
+// chain of joins bounds it: [1][4096][1024] 13 us; [1][50021][257] in fp32, whose rows TMA does
 // not take and whose segments read two rows in three twice, 84 us (154 MB, 1.8 TB/s).
 #include <type_traits>
 
@@ -924,10 +924,13 @@ int launch_tiles(const RecurrenceArgs<T>& a, const TileMaps<T>& maps, int64_t un
 // tokens: as many as come near to filling the SMs twice (a cluster of 8 leaves a few of them
 // out), no more than there are tiles.  A round of a cluster costs a microsecond more than one
 // CTA's, so that from half the SMs on a CTA a strip is faster.  0: segments are faster, which is
-// so for a few strips and very many tokens.  Forward and backward in us, bf16, as one CTA a
-// strip / segments / clusters:
-//   [2][4096][4096]  41  73 /  74  93 / 53  94     [1][4096][4096]   39  68 / 35  51 /  28  52
-//   [1][4096][1024]  37  64 /  17  21 /  9  15     [1][65536][256]  521 966 / 41  56 / 102 186
+// so for a few strips and very many tokens.  Forward and backward in us, bf16, four calls one
+// behind the other, as one CTA a strip / segments / clusters (of 4 from 64 strips on, else of 8):
+//   [2][4096][4096]  43  75 / 63  90 /  57  99     [1][4096][4096]  38  67 / 32  47 /  26  50
+//   [1][65536][256] 545 963 / 32  46 / 127 234     [1][4096][1024]  37  63 / 12  15 /  14  23
+//   [1][2048][1024]           9  10 /   9  13
+// The rule is from before segments found their states without a launch of their own; since then
+// they are ahead of clusters at 16 strips of 4096 tokens, which it does not know.
 int cluster_of(int64_t units, int64_t tokens, int tile) {
     if (units < 10 && tokens > 96 * tile) return 0;
     if (units <= 30 && tokens > 4 * tile) return 8;

@@ -92,7 +92,8 @@ class GradientRun:
     matrices: a function that gives the views [n][rows][columns] of rows like x which are
     weight matrices.  Their step is not Adam's but orthogonal: m <- momentum m - g, and the
     step lr sqrt(max(1, rows / columns)) times what relay_orthogonalise makes of
-    momentum m - g."""
+    momentum m - g, as in the Muon optimiser (K. Jordan and others, 2024), whose momentum
+    is the default."""
 
     def __init__(self, n: int, d: int, edges, beta1: float = 0.9, beta2: float = 0.99, eps: float = 1e-8, matrices=None,
                  momentum: float = 0.95):
